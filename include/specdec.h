@@ -49,6 +49,7 @@ extern "C" {
 
 #define SPECDEC_DTYPE_F32   0
 #define SPECDEC_DTYPE_BF16  1
+#define SPECDEC_DTYPE_F16   2      /* operators on the caller's tensors only: handles take the first two */
 
 #define SPECDEC_ACT_RELU    0
 #define SPECDEC_ACT_GELU    1
@@ -183,6 +184,111 @@ int specdec_accept_scan(const float* d_logits, const int32_t* d_draft, int B, in
  * different streams or host threads do not disturb one another. */
 int specdec_accept_scan_static(const float* d_logits, const int32_t* d_draft, int B, int k, int V,
                                int beta, float tau, int32_t* d_accepted, int32_t* d_bif, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Tree speculation on the caller's tensors.  A chain of drafts is verified by a handle, greedily, over the handle's
+ * cache.  These operators serve a program that drafts several continuations of every sequence (a tree), samples
+ * instead of taking the top token, and keeps the paged K/V cache in its own memory.  One decoding step is
+ *     cache_reserve, (cache_append, tree_attention) in every layer, sample, tree_accept, cache_compact;
+ * cache_fork and cache_release begin and end branches.  No handle; nothing is allocated; failures are reported as by
+ * every other call (message: specdec_last_error(NULL)).  Operators on one cache are ordered by the caller (one stream,
+ * or events).
+ *
+ * A tree is its nodes' parents: node 0 is the root (the last committed token), node i > 0 hangs off parents[i] in
+ * [0, i).  Any other value is no parent: the node begins a tree of its own, which a walk from node 0 never reaches.
+ *
+ * The cache: page p holds page_tokens token slots of every layer; a slot's row of n_heads x head_dim elements is found
+ * by the strides (elements; head_dim is contiguous; stride_side leads from a layer's keys to its values), so pages of
+ * [token, head] and of [head, token] order both do.  d_kv and all strides are multiples of 16 bytes.  Slot t of
+ * sequence s is slot t % page_tokens of page d_table[s * max_pages + t / page_tokens].  d_length[s] tokens are
+ * committed, d_held[s] pages are in the sequence's table (entries behind them are -1), d_refs[p] sequences hold page p
+ * (0: free).  Pages are given out lowest number first, so what a call does depends on its arguments alone.  A new cache has
+ * d_table = -1 and everything else 0.  d_status[0] gathers SPECDEC_CACHE_* bits until the caller clears it; d_scratch holds
+ * specdec_cache_scratch() int32 values, zero at first, and belongs to the calls in between.  Tokens are only ever
+ * written to pages that one sequence holds: branches share full pages and copy the last, partly filled one. */
+#define SPECDEC_CACHE_NO_PAGES    1   /* not enough free pages: the call changed nothing                              */
+#define SPECDEC_CACHE_ROW_FULL    2   /* a sequence would hold more than max_pages: the call changed nothing           */
+#define SPECDEC_CACHE_BAD_INDEX   4   /* a sequence number or a path out of range: that entry was skipped              */
+#define SPECDEC_CACHE_UNRESERVED  8   /* a token's slot is in no page of the sequence's own: the token (compact: the
+                                         sequence) was skipped                                                         */
+typedef struct {
+    void*     d_kv;
+    int       dtype;                       /* SPECDEC_DTYPE_*                                                          */
+    int       n_layers, n_heads, head_dim; /* K/V heads                                                                */
+    int       n_pages, page_tokens;        /* page_tokens: a power of two                                              */
+    int       n_seqs, max_pages;
+    long long stride_layer, stride_side, stride_page, stride_token, stride_head;
+    int32_t  *d_table, *d_length, *d_held, *d_refs, *d_status, *d_scratch;
+} specdec_cache;
+
+/* int32 values of d_scratch; negative on a bad argument. */
+long long specdec_cache_scratch(int n_seqs, int max_pages, int n_pages);
+
+/* The calls below take n sequence numbers d_seqs [n], all different.
+ * reserve: pages for n_tokens slots behind the committed ones (those already held count).
+ * append: writes rows t < (d_count ? d_count[i] : T) of d_k, d_v [n_layers, n, T, n_heads, head_dim] (head_dim contiguous, strides and
+ *   addresses multiples of 16 bytes) of layers layer .. layer + n_layers - 1 into slots d_length + t.  Lengths stay.
+ * compact: slots d_length + d_path[i, 0 .. d_n_path[i]) move to d_length, d_length + 1, ... in every layer; the length grows by d_n_path[i], and
+ *   pages behind it are given back.  A path rises strictly (as the paths of specdec_tree_accept do); a sequence
+ *   whose path does not is skipped (BAD_INDEX).
+ * release: gives a sequence's pages back; its length is 0.
+ * fork: sequence d_dst[i] becomes a copy of d_src[i] as that was before the call (so a permutation reorders beams), its old pages are
+ *   given back.  Full pages are shared, the last, partly filled one is copied.  d_dst all different; a pair of equal numbers does nothing. */
+int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream);
+int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int T,
+                         long long stride_layer, long long stride_seq, long long stride_token, long long stride_head,
+                         const int32_t* d_count, void* stream);
+int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride,
+                          const int32_t* d_n_path, void* stream);
+int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, void* stream);
+int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream);
+
+/* Trees of up to 1024 nodes.  d_n_nodes [B] (or NULL: T each) cuts a tree short.
+ * ancestors: bit j of d_mask [B, T, ceil(T / 32)] row i is set iff node j is node i or one of its ancestors; d_depth [B, T] is the
+ *   number of ancestors (-1 behind the last node, whose mask is 0).  Either output may be NULL.
+ * accept: the walk from the root along the sampled tokens: from node i on to its first child whose token is d_sampled[i].  d_path [B, T]
+ *   receives the nodes passed (the root first; -1 behind), d_n_path [B] their number, d_emitted [B, T] the sampled token of each (-1
+ *   behind): the accepted drafts and, last, the token that no child had.  With tokens sampled from the verifier this emits what sampling
+ *   token by token would.  A tree of no nodes has no path. */
+int specdec_tree_ancestors(const int32_t* d_parents, const int32_t* d_n_nodes, int B, int T, uint32_t* d_mask, int32_t* d_depth, void* stream);
+int specdec_tree_accept(const int32_t* d_parents, const int32_t* d_tokens, const int32_t* d_sampled, const int32_t* d_n_nodes, int B, int T,
+                        int32_t* d_path, int32_t* d_n_path, int32_t* d_emitted, void* stream);
+
+/* Attention of tree nodes over the cache: query t of batch row b sees the d_length committed tokens of sequence s = d_seqs[b] and the nodes
+ * j < n_nodes (their keys and values are in slots d_length + j) whose bit is set in d_mask[b, t]:
+ *     out[b, t, h] = sum_j p_j v_j,   p = softmax(scale q . k_j) over what it sees,   K/V head h / (n_q_heads / n_heads).
+ * A query that sees nothing, and every query t >= n_nodes, gives zeros.  What is in slots that no query of the row may see (behind the
+ * nodes, or masked for all) never matters.  T = 1 with a mask of 1 is the decoding of single tokens; nodes may attend to later ones. */
+typedef struct {
+    const void *d_q;                       /* [B, T, n_q_heads, head_dim] of the cache's type, head_dim contiguous       */
+    void       *d_out;                     /* the same shape                                                             */
+    long long   q_stride_b, q_stride_t, q_stride_h, out_stride_b, out_stride_t, out_stride_h;     /* elements            */
+    int         B, T, n_q_heads, layer;
+    const int32_t  *d_seqs;                /* [B]                                                                        */
+    const uint32_t *d_mask; long long mask_stride_b;      /* [B, T, ceil(T / 32)]; stride 0: one tree for all            */
+    const int32_t  *d_n_nodes;             /* [B] or NULL: T                                                             */
+    int         max_length;                /* no d_length of the batch is larger (0: unknown, max_pages * page_tokens)  */
+    float       scale;
+    void       *d_workspace; long long workspace_bytes;   /* see below                                                   */
+} specdec_tree_attention_args;
+/* Bytes of workspace (0: none) that spread a call of these sizes over the GPU; 16-byte aligned, no state between calls.  With less, a call
+ * returns SPECDEC_ERR_CAPACITY.  head_dim: multiples of 8 up to 128. */
+long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int max_length);
+int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* a, void* stream);
+
+/* One token per row of d_logits [rows, V] (row r at r * stride; V contiguous) from a given uniform random number in [0, 1).
+ * With l = fp32 logits (NaN: never taken) and m their maximum, w_i = floor(2^40 exp((l_i - m) / T)) 2^-40: weights are whole numbers of
+ * units, so that their sums are exact, and a token is the same however the work is split.
+ *   top_k  > 0: the k largest (ties: lower index first) stay;
+ *   top_p  < 1: of those, in that order, entry i stays if the weight ahead of it is below top_p times their total;
+ *   min_p  > 0: entries with exp((l_i - m) / T) >= min_p stay;     the largest always stays.
+ *   token = the first index at which the running sum of the kept weights exceeds floor(uniform * total).
+ * temperature <= 0 (or NaN) takes the largest entry (lowest index).  d_logprob (or NULL) = log of the token's share of the kept weights.  A row
+ * of only -inf and NaN gives token -1, log probability -inf.
+ * d_temperature, d_top_k, d_top_p, d_min_p (each or NULL: 1, 0, 1, 0) hold one entry for each rows_per_param rows. */
+int specdec_sample(const void* d_logits, int dtype, long long stride, int rows, int V, const float* d_uniform,
+                   const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, int rows_per_param,
+                   int32_t* d_token, float* d_logprob, void* stream);
 
 /* Debug / parity helpers (not on the hot path).
  * specdec_debug_logits: re-runs the vocabulary projection of the last verify

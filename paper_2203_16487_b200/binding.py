@@ -26,6 +26,9 @@ EXPORTS = [
     "specdec_launch_count", "specdec_last_error", "specdec_set_draft_script", "specdec_profile_read",
     "specdec_accept_scan_static", "specdec_debug_trace", "specdec_debug_link_cost", "specdec_debug_mma_rate", "specdec_debug_cluster_round",
     "specdec_debug_integrity", "specdec_debug_mma_rate_bg",
+    "specdec_cache_scratch", "specdec_cache_reserve", "specdec_cache_append", "specdec_cache_compact", "specdec_cache_release",
+    "specdec_cache_fork", "specdec_tree_ancestors", "specdec_tree_accept", "specdec_tree_attention_workspace",
+    "specdec_tree_attention", "specdec_sample",
 ]
 
 
@@ -48,6 +51,21 @@ class Integrity(C.Structure):
 class Tensor(C.Structure):
     _fields_ = [("name", C.c_char_p), ("d_ptr", C.c_void_p), ("dtype", C.c_int), ("ndim", C.c_int),
                 ("shape", C.c_longlong * 4)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("d_kv", C.c_void_p)] + [(n, C.c_int) for n in (
+        "dtype", "n_layers", "n_heads", "head_dim", "n_pages", "page_tokens", "n_seqs", "max_pages")] + [
+        (n, C.c_longlong) for n in ("stride_layer", "stride_side", "stride_page", "stride_token", "stride_head")] + [
+        (n, C.c_void_p) for n in ("d_table", "d_length", "d_held", "d_refs", "d_status", "d_scratch")]
+
+
+class TreeAttentionArgs(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("d_out", C.c_void_p)] + [(n, C.c_longlong) for n in (
+        "q_stride_b", "q_stride_t", "q_stride_h", "out_stride_b", "out_stride_t", "out_stride_h")] + [
+        (n, C.c_int) for n in ("B", "T", "n_q_heads", "layer")] + [
+        ("d_seqs", C.c_void_p), ("d_mask", C.c_void_p), ("mask_stride_b", C.c_longlong), ("d_n_nodes", C.c_void_p),
+        ("max_length", C.c_int), ("scale", C.c_float), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_longlong)]
 
 
 class Stats(C.Structure):
@@ -95,9 +113,22 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.specdec_launch_count.restype = C.c_longlong
     lib.specdec_last_error.argtypes = [vp]
     lib.specdec_last_error.restype = C.c_char_p
+    L, cp = C.c_longlong, C.POINTER(Cache)
+    lib.specdec_cache_scratch.argtypes = [i, i, i]
+    lib.specdec_cache_reserve.argtypes = [cp, ip, i, i, vp]
+    lib.specdec_cache_append.argtypes = [cp, ip, i, i, i, vp, vp, i, L, L, L, L, ip, vp]
+    lib.specdec_cache_compact.argtypes = [cp, ip, i, ip, i, ip, vp]
+    lib.specdec_cache_release.argtypes = [cp, ip, i, vp]
+    lib.specdec_cache_fork.argtypes = [cp, ip, ip, i, vp]
+    lib.specdec_tree_ancestors.argtypes = [ip, ip, i, i, vp, ip, vp]
+    lib.specdec_tree_accept.argtypes = [ip, ip, ip, ip, i, i, ip, ip, ip, vp]
+    lib.specdec_tree_attention_workspace.argtypes = [i, i, i, i, i, i, i]
+    lib.specdec_tree_attention.argtypes = [cp, C.POINTER(TreeAttentionArgs), vp]
+    lib.specdec_sample.argtypes = [vp, i, L, i, i, vp, vp, ip, vp, vp, i, ip, vp, vp]
     for name in EXPORTS:
         if name not in ("specdec_launch_count", "specdec_last_error"):
             getattr(lib, name).restype = i
+    lib.specdec_cache_scratch.restype = lib.specdec_tree_attention_workspace.restype = L
     return lib
 
 

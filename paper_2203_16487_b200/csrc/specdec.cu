@@ -25,6 +25,7 @@
 #include "gemm_tc_splitk.cuh"
 #include "kernels.cuh"
 #include "mma_rate.cuh"
+#include "op_error.cuh"
 #include "rows_f32.cuh"
 #include "rows_gemm.cuh"
 #include "vocab_rows.cuh"
@@ -1487,6 +1488,11 @@ int post_check(specdec_handle* h, int rc, void* stream) {
         return fail(h, SPECDEC_ERR_CORRUPT, "integrity: " + std::to_string(rep.nonfinite) + " non-finite value(s), first in " +
                                                 h->scan_names[rep.first_nonfinite_buffer]);
     return SPECDEC_OK;
+}
+
+int sd::op_fail(int code, const char* who, const char* why) noexcept {
+    try { g_create_error = std::string(who) + ": " + why; } catch (...) { g_create_error.clear(); }
+    return code;
 }
 
 extern "C" {
