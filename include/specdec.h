@@ -211,6 +211,7 @@ int specdec_accept_scan_static(const float* d_logits, const int32_t* d_draft, in
 #define SPECDEC_CACHE_BAD_INDEX   4   /* a sequence number or a path out of range: that entry was skipped              */
 #define SPECDEC_CACHE_UNRESERVED  8   /* a token's slot is in no page of the sequence's own: the token (compact: the
                                          sequence) was skipped                                                         */
+#define SPECDEC_CACHE_TIMEOUT    16   /* tree_attention: a bounded wait inside a kernel gave up; its output is not valid */
 typedef struct {
     void*     d_kv;
     int       dtype;                       /* SPECDEC_DTYPE_*                                                          */
@@ -273,7 +274,7 @@ typedef struct {
 } specdec_tree_attention_args;
 /* Bytes of workspace (0: none) that spread a call of these sizes over the GPU; 16-byte aligned, no state between calls.  With less, a call
  * returns SPECDEC_ERR_CAPACITY.  head_dim: multiples of 8 up to 128. */
-long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int max_length);
+long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length);
 int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* a, void* stream);
 
 /* One token per row of d_logits [rows, V] (row r at r * stride; V contiguous) from a given uniform random number in [0, 1).

@@ -3,127 +3,67 @@
 // out = sum_j p_j v_j over the keys a query sees, p = softmax(scale q . k).  One pass over the keys with the running maximum m and sum l of
 // 2^(s - m): s in units of log2, sums and outputs in fp32, rescaled where m grows.  All query heads of a K/V head share its keys, so a row tile
 // mixes nodes and heads; few rows: the keys of a sequence are split over CTAs, whose partial outputs k_ta_merge joins.
-#include "barriers.cuh"
 #include "tree_attention.cuh"
 
 namespace sd {
 namespace {
 
-__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t* r) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-template <typename T> struct Half;
-template <> struct Half<__nv_bfloat16> {
-    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-};
-template <> struct Half<__half> {
-    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-};
-
-// The mask rows of a tile's queries (cut at n_nodes), and any[w]: the nodes that one of them sees.  rows: query rows r0 ..; `words` a row.
-__device__ void load_masks(const TreeAttn& a, int b, int r0, int rows, int nodes, uint32_t* mask, uint32_t* any) {
-    for (int w = threadIdx.x; w < a.words; w += blockDim.x) any[w] = 0;
-    __syncthreads();
-    const int t0 = r0 / a.group, t1 = min((r0 + rows - 1) / a.group, a.T - 1);
-    for (int i = threadIdx.x; i < (t1 - t0 + 1) * a.words; i += blockDim.x) {
-        const int t = t0 + i / a.words, w = i % a.words;
-        uint32_t m = t < nodes ? a.mask[b * a.mask_sb + (long long)t * a.words + w] : 0u;
-        const int left = nodes - w * 32;
-        if (left < 32) m &= left <= 0 ? 0u : (1u << left) - 1u;
-        mask[i] = m;
-        if (m) atomicOr(any + w, m);
-    }
-    __syncthreads();
-}
-
-// ------------------------------------------------------------------ 16-bit types: mma.sync
-// CTA = (split, row tile, K/V head, sequence); WM x WK warps: 16 rows each, the WK key groups take every WK-th block of keys and merge at the end.  Each group
-// walks its blocks through a ring of NS cp.async stages of its own.  Rows of DP elements, 16-byte pieces XORed with the row's low three bits.
-template <typename T, int DP, int WM, int WK, int KT, int NS>
-__global__ void __launch_bounds__(32 * WM * WK) k_ta_mma(TreeAttn a) {
-    constexpr int ROWS = 16 * WM, PITCH = DP * 2, PIECES = DP / 8, GT = 32 * WM, STAGE = 2 * KT * PITCH;
-    constexpr int NK = KT / 8, ND = DP / 8;
+// ------------------------------------------------------------------ 16-bit types, pages of fewer than TA_MIN_PAGE tokens
+// Such pages are no TMA boxes: every thread fetches 16-byte pieces (cp.async).  One item a CTA: 4 warps of 16 rows, a ring of NS blocks of 64 keys, rows of
+// DP elements whose 16-byte pieces are XORed with the row's low three bits.
+template <typename T, int DP, int NS>
+__global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
+    constexpr int ROWS = 64, KT = TA_BLOCK, PITCH = DP * 2, PIECES = DP / 8, STAGE = 2 * KT * PITCH;
     extern __shared__ __align__(128) char sm[];
-    char* ring = sm;                                      // [WK][NS][K, V][KT][PITCH]; at first the queries, at last the groups' partial outputs
-    uint32_t* any = (uint32_t*)(sm + WK * NS * STAGE);
+    char* ring = sm;                                      // [NS][K, V][KT][PITCH]; at first the queries
+    uint32_t* any = (uint32_t*)(sm + NS * STAGE);
     uint32_t* mask = any + a.words;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM, gt = tid % GT;
-    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, h = blockIdx.y, b = blockIdx.z;
-    const int r0 = tile * ROWS, all_rows = a.T * a.group;
-    const SeqKeys s = ta_keys(a, b);
-    int per;
-    const int used = ta_used(a, s.keys, per);
-    if (split >= max(used, 1)) return;
-    const int t0 = r0 / a.group;
-    load_masks(a, b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
-
-    // queries: rows through shared memory into fragments
-    {
-        for (int i = tid; i < ROWS * PIECES; i += 32 * WM * WK) {
-            const int r = i / PIECES, c = i % PIECES, gr = r0 + r;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (gr < all_rows && c * 8 < a.dim) {
-                const char* p = a.q + b * a.q_sb + (gr / a.group) * a.q_st + (h * a.group + gr % a.group) * a.q_sh + c * 16;
-                if (a.q_vec) x = *reinterpret_cast<const uint4*>(p);
-                else {
-                    const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
-                    x = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-                }
+    const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
+    const Item it = ta_item(a, (int*)ring);
+    if (it.b < 0) return;
+    const int h = it.h, r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
+    const SeqKeys s = ta_keys(a, it.b);
+    ta_load_masks(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
+    for (int i = tid; i < ROWS * PIECES; i += 128) {      // queries: rows through shared memory into fragments
+        const int r = i / PIECES, c = i % PIECES, gr = r0 + r;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (gr < all_rows && c * 8 < a.dim) {
+            const char* p = a.q + it.b * a.q_sb + (gr / a.group) * a.q_st + (h * a.group + gr % a.group) * a.q_sh + c * 16;
+            if (a.q_vec) x = *reinterpret_cast<const uint4*>(p);
+            else {
+                const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
+                x = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
             }
-            *reinterpret_cast<uint4*>(ring + r * PITCH + ((c ^ (r & 7)) << 4)) = x;
         }
+        *reinterpret_cast<uint4*>(ring + r * PITCH + ((c ^ (r & 7)) << 4)) = x;
     }
     __syncthreads();
     uint32_t qf[DP / 16][4];
 #pragma unroll
     for (int kk = 0; kk < DP / 16; ++kk) {
         const int r = wm * 16 + (lane & 15), c = kk * 2 + (lane >> 4);
-        ldsm4(smem_u32(ring + r * PITCH + ((c ^ (r & 7)) << 4)), qf[kk]);
+        ta_ldsm4(smem_u32(ring + r * PITCH + ((c ^ (r & 7)) << 4)), qf[kk]);
     }
     __syncthreads();
 
     const char* kbase = a.k + h * a.s_head;
     const char* vbase = a.v + h * a.s_head;
-    char* my_ring = ring + wk * NS * STAGE;
-    if (a.dim < DP) {                                     // pieces beyond the head: zero once, never written again
-        for (int i = gt; i < NS * 2 * KT * PIECES; i += GT) {
+    if (a.dim < DP)                                       // pieces beyond the head: zero once, never written again
+        for (int i = tid; i < NS * 2 * KT * PIECES; i += 128) {
             const int r = (i / PIECES) % KT, c = i % PIECES;
-            if (c * 8 >= a.dim) *reinterpret_cast<uint4*>(my_ring + (i / PIECES) * PITCH + ((c ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+            if (c * 8 >= a.dim) *reinterpret_cast<uint4*>(ring + (i / PIECES) * PITCH + ((c ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
         }
-    }
-    const int k_begin = split * per * TA_BLOCK, k_end = min(s.keys, (split + 1) * per * TA_BLOCK);
-    const int blocks = (max(k_end - k_begin, 0) + KT - 1) / KT, mine = (blocks - wk + WK - 1) / WK;
-    const int real_pieces = a.dim / 8;
-    auto load = [&](int j) {                              // the group's j-th block
-        if (j < mine) {
-            const int k0 = k_begin + (j * WK + wk) * KT;
-            char* st = my_ring + (j % NS) * STAGE;
-            for (int i = gt; i < KT * PIECES; i += GT) {
-                const int r = i / PIECES, c = i % PIECES, key = k0 + r;
+    const int k_begin = it.split * it.per * KT, k_end = min(s.keys, (int)min((long long)(it.split + 1) * it.per * KT, (long long)s.keys));
+    const int blocks = max(0, (k_end - k_begin + KT - 1) / KT), real_pieces = a.dim / 8;
+    auto load = [&](int j) {
+        if (j < blocks) {
+            char* st = ring + (j % NS) * STAGE;
+            for (int i = tid; i < KT * PIECES; i += 128) {
+                const int r = i / PIECES, c = i % PIECES, key = k_begin + j * KT + r, pi = key >> a.page_shift;
                 if (c >= real_pieces) continue;
-                bool real = key < k_end;
-                if (real && key >= s.len) real = any[(key - s.len) >> 5] >> ((key - s.len) & 31) & 1;
-                const int pi = key >> a.page_shift;
                 int page = -1;
-                if (real && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
-                real = real && (unsigned)page < (unsigned)a.n_pages;
+                if (key < k_end && ta_seen(any, s, key) && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
+                const bool real = (unsigned)page < (unsigned)a.n_pages;
                 const long long off = real ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + c * 16 : 0;
                 const uint32_t d = smem_u32(st + r * PITCH + ((c ^ (r & 7)) << 4));
                 ta_copy16(d, kbase + off, real);
@@ -132,168 +72,26 @@ __global__ void __launch_bounds__(32 * WM * WK) k_ta_mma(TreeAttn a) {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto group_sync = [&]() {
-        if constexpr (WM == 1) __syncwarp();
-        else if constexpr (WK == 1) __syncthreads();
-        else asm volatile("bar.sync %0, %1;" ::"r"(1 + wk), "n"(GT) : "memory");
-    };
     const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
     const int ta = (r0 + ra) / a.group, tb = (r0 + rb) / a.group;
     const bool live_a = r0 + ra < all_rows && ta < s.nodes, live_b = r0 + rb < all_rows && tb < s.nodes;
     const uint32_t* mask_a = mask + (live_a ? ta - t0 : 0) * a.words;
     const uint32_t* mask_b = mask + (live_b ? tb - t0 : 0) * a.words;
-    float o[ND][4];
-#pragma unroll
-    for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float ma = -INFINITY, mb = -INFINITY, la = 0.f, lb = 0.f;
-    group_sync();
+    TaRows<T, DP> rows;
+    rows.clear();
+    __syncthreads();
     for (int j = 0; j < NS - 1; ++j) load(j);
-    for (int j = 0; j < mine; ++j) {
+    for (int j = 0; j < blocks; ++j) {
         asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
-        group_sync();
+        __syncthreads();
         load(j + NS - 1);
-        const uint32_t ks = smem_u32(my_ring + (j % NS) * STAGE), vs = ks + KT * PITCH;
-        const int k0 = k_begin + (j * WK + wk) * KT;
-        float sc[NK][4];
-#pragma unroll
-        for (int i = 0; i < NK; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < DP / 16; ++kk)
-#pragma unroll
-            for (int n = 0; n < KT / 16; ++n) {
-                const int r = n * 16 + (lane & 7) + ((lane >> 4) << 3), c = kk * 2 + ((lane >> 3) & 1);
-                uint32_t kf[4];
-                ldsm4(ks + r * PITCH + ((c ^ (r & 7)) << 4), kf);
-                Half<T>::mma(sc[2 * n], qf[kk], kf[0], kf[1]);
-                Half<T>::mma(sc[2 * n + 1], qf[kk], kf[2], kf[3]);
-            }
-        if (k0 + KT > s.len) {                            // a block with nodes, or behind the last key
-#pragma unroll
-            for (int n = 0; n < KT / 32; ++n) {
-                const int base = k0 + n * 32 - s.len;
-                uint32_t wa = live_a ? ta_window(mask_a, a.words, base) : 0u, wb = live_b ? ta_window(mask_b, a.words, base) : 0u;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int bit = i * 8 + (lane & 3) * 2;
-                    float* c = sc[n * 4 + i];
-                    if (!(wa >> bit & 1)) c[0] = -INFINITY;
-                    if (!(wa >> bit & 2)) c[1] = -INFINITY;
-                    if (!(wb >> bit & 1)) c[2] = -INFINITY;
-                    if (!(wb >> bit & 2)) c[3] = -INFINITY;
-                }
-            }
-        }
-        float na = ma, nb = mb;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) { na = fmaxf(na, fmaxf(sc[i][0], sc[i][1]) * a.scale); nb = fmaxf(nb, fmaxf(sc[i][2], sc[i][3]) * a.scale); }
-        na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 1)); na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 2));
-        nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
-        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
-        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
-        ma = na; mb = nb;
-        la *= fa; lb *= fb;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
-#pragma unroll
-        for (int n = 0; n < KT / 16; ++n) {
-            uint32_t pf[4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float* c = sc[2 * n + e];
-                c[0] = ta_exp2(fmaf(c[0], a.scale, -za)); c[1] = ta_exp2(fmaf(c[1], a.scale, -za));
-                c[2] = ta_exp2(fmaf(c[2], a.scale, -zb)); c[3] = ta_exp2(fmaf(c[3], a.scale, -zb));
-                la += c[0] + c[1]; lb += c[2] + c[3];
-                pf[2 * e] = Half<T>::pack(c[0], c[1]);
-                pf[2 * e + 1] = Half<T>::pack(c[2], c[3]);
-            }
-#pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-                const int r = n * 16 + (lane & 15), c = d * 2 + (lane >> 4);
-                uint32_t vf[4];
-                ldsm4_t(vs + r * PITCH + ((c ^ (r & 7)) << 4), vf);
-                Half<T>::mma(o[2 * d], pf, vf[0], vf[1]);
-                Half<T>::mma(o[2 * d + 1], pf, vf[2], vf[3]);
-            }
-        }
+        const uint32_t ks = smem_u32(ring + (j % NS) * STAGE), vs = ks + KT * PITCH;
+        rows.block(qf, k_begin + j * KT, s.len, a.scale, a.words, live_a ? mask_a : nullptr, live_b ? mask_b : nullptr,
+                   [&](int r, int c) { return ks + r * PITCH + ((c ^ (r & 7)) << 4); }, [&](int r, int c) { return vs + r * PITCH + ((c ^ (r & 7)) << 4); });
     }
-    la += __shfl_xor_sync(0xffffffffu, la, 1); la += __shfl_xor_sync(0xffffffffu, la, 2);
-    lb += __shfl_xor_sync(0xffffffffu, lb, 1); lb += __shfl_xor_sync(0xffffffffu, lb, 2);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    // a query behind the nodes has taken the committed keys of blocks without a mask; one that sees nothing has multiplied values by 0
-    if (!live_a) la = 0.f;
-    if (!live_b) lb = 0.f;
-    if (la == 0.f) { ma = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = 0.f;
-    }
-    if (lb == 0.f) { mb = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) o[i][2] = o[i][3] = 0.f;
-    }
-    if constexpr (WK > 1) {                               // the groups' partial outputs meet in the first group
-        constexpr int RP = DP + 8;
-        float* red = reinterpret_cast<float*>(ring);      // [WK - 1][ROWS][RP], then [WK - 1][ROWS] (maximum, sum)
-        float2* red_ml = reinterpret_cast<float2*>(red + (WK - 1) * ROWS * RP);
-        static_assert((WK - 1) * ROWS * (RP * 4 + 8) <= WK * NS * STAGE, "partial outputs fit the ring");
-        __syncthreads();
-        if (wk > 0) {
-            float* pa = red + ((wk - 1) * ROWS + ra) * RP + (lane & 3) * 2;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                *reinterpret_cast<float2*>(pa + i * 8) = make_float2(o[i][0], o[i][1]);
-                *reinterpret_cast<float2*>(pa + 8 * RP + i * 8) = make_float2(o[i][2], o[i][3]);
-            }
-            if ((lane & 3) == 0) { red_ml[(wk - 1) * ROWS + ra] = make_float2(ma, la); red_ml[(wk - 1) * ROWS + rb] = make_float2(mb, lb); }
-        }
-        __syncthreads();
-        if (wk > 0) return;
-#pragma unroll
-        for (int g = 0; g < WK - 1; ++g) {
-            const float2 xa = red_ml[g * ROWS + ra], xb = red_ml[g * ROWS + rb];
-            const float na = fmaxf(ma, xa.x), nb = fmaxf(mb, xb.x);
-            const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
-            const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb), ga = ta_exp2(xa.x - za), gb = ta_exp2(xb.x - zb);
-            ma = na; mb = nb;
-            la = la * fa + xa.y * ga; lb = lb * fb + xb.y * gb;
-            const float* pa = red + (g * ROWS + ra) * RP + (lane & 3) * 2;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                const float2 u = *reinterpret_cast<const float2*>(pa + i * 8), w = *reinterpret_cast<const float2*>(pa + 8 * RP + i * 8);
-                o[i][0] = o[i][0] * fa + u.x * ga; o[i][1] = o[i][1] * fa + u.y * ga;
-                o[i][2] = o[i][2] * fb + w.x * gb; o[i][3] = o[i][3] * fb + w.y * gb;
-            }
-        }
-    }
-    if (used <= 1) {
-        const float ia = la > 0.f || la != la ? 1.f / la : 0.f, ib = lb > 0.f || lb != lb ? 1.f / lb : 0.f;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int gr = r0 + (e ? rb : ra);
-            if (gr >= all_rows) continue;
-            char* p = a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh + (lane & 3) * 4;
-            const float inv = e ? ib : ia;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                if (i * 8 >= a.dim) break;
-                const uint32_t x = Half<T>::pack(o[i][2 * e] * inv, o[i][2 * e + 1] * inv);
-                if (a.out_vec) *reinterpret_cast<uint32_t*>(p + i * 16) = x;
-                else { reinterpret_cast<unsigned short*>(p + i * 16)[0] = (unsigned short)x; reinterpret_cast<unsigned short*>(p + i * 16)[1] = (unsigned short)(x >> 16); }
-            }
-        }
-    } else {
-        const long long slot = ((((long long)b * a.kv_heads + h) * a.tiles + tile) * a.splits + split) * ROWS;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = e ? rb : ra;
-            float* p = a.part + (slot + r) * a.dim + (lane & 3) * 2;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                if (i * 8 >= a.dim) break;
-                *reinterpret_cast<float2*>(p + i * 8) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
-            }
-            if ((lane & 3) == 0) a.part_ml[slot + r] = make_float2(e ? mb : ma, e ? lb : la);
-        }
-    }
+    rows.finish(live_a, live_b);
+    rows.store(a, it, r0, ra, ROWS);
 }
 
 // ------------------------------------------------------------------ fp32: FFMA
@@ -311,13 +109,11 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
     uint32_t* any = reinterpret_cast<uint32_t*>(row_f + 48);
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, h = blockIdx.y, b = blockIdx.z;
-    const int r0 = tile * TF_ROWS, all_rows = a.T * a.group;
+    const Item it = ta_item(a, reinterpret_cast<int*>(sm));
+    if (it.b < 0) return;
+    const int b = it.b, h = it.h, r0 = it.tile * TF_ROWS, all_rows = a.T * a.group;
     const SeqKeys s = ta_keys(a, b);
-    int per;
-    const int used = ta_used(a, s.keys, per);
-    if (split >= max(used, 1)) return;
-    load_masks(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
+    ta_load_masks(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
     for (int i = tid; i < TF_ROWS * DP; i += 128) {
         const int r = i / DP, d = i % DP, gr = r0 + r;
         float x = 0.f;
@@ -326,7 +122,7 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
     }
     if (tid < 16) { row_f[16 + tid] = -INFINITY; row_f[32 + tid] = 0.f; }
     const int t0 = r0 / a.group;
-    const int k_begin = split * per * TA_BLOCK, k_end = min(s.keys, (split + 1) * per * TA_BLOCK);
+    const int k_begin = it.split * it.per * TA_BLOCK, k_end = min(s.keys, (int)min((long long)(it.split + 1) * it.per * TA_BLOCK, (long long)s.keys));
     constexpr int DC = DP / 4, RG = 128 / DC, RR = TF_ROWS / RG;           // output: DC column groups of 4, RG row groups of RR rows
     const int oc = tid % DC, og = tid / DC;
     float4 o[RR];
@@ -336,8 +132,7 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
         __syncthreads();
         for (int i = tid; i < TF_KT * (DP / 4); i += 128) {
             const int r = i / (DP / 4), c = i % (DP / 4), key = k0 + r;
-            bool real = key < k_end && c * 4 < a.dim;
-            if (real && key >= s.len) real = any[(key - s.len) >> 5] >> ((key - s.len) & 31) & 1;
+            bool real = key < k_end && c * 4 < a.dim && ta_seen(any, s, key);
             const int pi = key >> a.page_shift;
             int page = -1;
             if (real && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
@@ -399,14 +194,14 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
         }
     }
     __syncthreads();
-    const long long slot = ((((long long)b * a.kv_heads + h) * a.tiles + tile) * a.splits + split) * TF_ROWS;
+    const long long slot = (long long)blockIdx.x * TF_ROWS;
 #pragma unroll
     for (int i = 0; i < RR; ++i) {
         const int r = og * RR + i, gr = r0 + r;
         if (gr >= all_rows || oc * 4 >= a.dim) continue;
         const float l = row_f[32 + r];
         if (l == 0.f) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);               // sees nothing: values times 0
-        if (used <= 1) {
+        if (it.splits == 1) {
             const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
             float* p = reinterpret_cast<float*>(a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh) + oc * 4;
             if (a.out_vec) *reinterpret_cast<float4*>(p) = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
@@ -426,78 +221,102 @@ template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *rei
 
 // One warp a query row: the splits' outputs, each rescaled to the largest maximum.
 template <typename T>
-__global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows_per_tile) {
+__global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
     const int gr = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z;
+    cudaGridDependencySynchronize();
     if (gr >= a.T * a.group) return;
-    int per;
-    const int used = ta_used(a, ta_keys(a, b).keys, per);
-    if (used <= 1) return;
-    const int tile = gr / rows_per_tile, r = gr % rows_per_tile;
-    const long long slot0 = (((long long)b * a.kv_heads + h) * a.tiles + tile) * a.splits * rows_per_tile + r;
+    const int tile = gr / rows, r = gr % rows, ht = a.kv_heads * a.tiles;
+    const int2 at = a.where[(b * a.kv_heads + h) * a.tiles + tile];       // first item, splits
+    if (at.y <= 1) return;
+    const long long slot0 = (long long)at.x * rows + r, step = (long long)ht * rows;
     float m = -INFINITY;
-    for (int s = lane; s < used; s += 32) m = fmaxf(m, a.part_ml[slot0 + (long long)s * rows_per_tile].x);
+    for (int s = lane; s < at.y; s += 32) m = fmaxf(m, a.part_ml[slot0 + s * step].x);
 #pragma unroll
     for (int of = 16; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
     const float z = m == -INFINITY ? 0.f : m;
-    float o[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-    for (int s = 0; s < used; ++s) {
-        const long long slot = slot0 + (long long)s * rows_per_tile;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);           // lane: four columns
+    float l = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < at.y; ++s) {
+        const long long slot = slot0 + s * step;
         const float2 ml = a.part_ml[slot];
         const float f = exp2f(ml.x - z);
         l += ml.y * f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (lane + 32 * i < a.dim) o[i] = fmaf(a.part[slot * a.dim + lane + 32 * i], f, o[i]);
+        if (lane * 4 < a.dim) {
+            const float4 x = *reinterpret_cast<const float4*>(a.part + slot * a.dim + lane * 4);
+            o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+        }
     }
+    if (lane * 4 >= a.dim) return;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    char* p = a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) if (lane + 32 * i < a.dim) put<T>(p + (lane + 32 * i) * sizeof(T), o[i] * inv);
+    char* p = a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh + lane * 4 * sizeof(T);
+    put<T>(p, o.x * inv); put<T>(p + sizeof(T), o.y * inv); put<T>(p + 2 * sizeof(T), o.z * inv); put<T>(p + 3 * sizeof(T), o.w * inv);
 }
 
 // ------------------------------------------------------------------ host
-struct Plan { int rows, tiles, splits, min_blocks; };     // rows of a tile; see TreeAttn
-Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, long long max_keys) {
+constexpr int TA_SMS = 148;
+struct Plan { int rows, tiles, direct, slots, min_blocks; long long grid; };
+// Rows of a tile: 16, 32 or 64 by the rows there are (64 share a block's keys among four warps; fewer rows give the warps keys of their own instead).
+Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, int page_tokens, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
-    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : all <= 16 ? 16 : all <= 32 ? 32 : 64;
+    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : 64;
     p.tiles = (all + p.rows - 1) / p.rows;
-    const long long ctas = (long long)B * n_kv_heads * p.tiles, blocks = (max_keys + TA_BLOCK - 1) / TA_BLOCK;
-    long long s = (4 * 148 + ctas - 1) / ctas;            // about four CTAs an SM
-    p.min_blocks = 2;
-    s = s < blocks / p.min_blocks ? s : blocks / p.min_blocks;
-    p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    p.slots = TA_SMS * (head_dim > 64 ? 2 : 3);           // CTAs that an SM holds at least
+    p.min_blocks = 4;
+    const long long whole = (long long)B * n_kv_heads * p.tiles, blocks = (max_keys + TA_BLOCK - 1) / TA_BLOCK;
+    p.direct = blocks <= p.min_blocks || B > TA_MAX_B || whole >= 4LL * p.slots;
+    p.grid = p.direct ? whole : whole >= p.slots ? whole + 2LL * p.slots : p.slots;
+    if (!p.direct && p.grid > whole * ((blocks + p.min_blocks - 1) / p.min_blocks)) p.grid = whole * ((blocks + p.min_blocks - 1) / p.min_blocks);
     return p;
 }
-long long part_bytes(const Plan& p, int B, int n_kv_heads, int head_dim) {
-    return p.splits <= 1 ? 0 : (long long)B * n_kv_heads * p.tiles * p.splits * p.rows * (head_dim * 4 + 8);
+// Bytes: partial outputs, then (maximum, sum), then where a tile's items are.
+long long part_floats(const Plan& p, int head_dim) { return p.direct ? 0 : p.grid * p.rows * head_dim; }
+long long workspace(const Plan& p, int B, int n_kv_heads, int head_dim) {
+    return p.direct ? 0 : part_floats(p, head_dim) * 4 + p.grid * p.rows * 8 + (long long)B * n_kv_heads * p.tiles * 8;
 }
 
-template <typename T, int DP, int WM, int WK, int KT, int NS>
-cudaError_t run_mma(const TreeAttn& a, cudaStream_t st) {
-    const size_t smem = (size_t)WK * NS * 2 * KT * DP * 2 + (size_t)(16 * WM + 1) * a.words * 4;
-    const cudaError_t e = cudaFuncSetAttribute(k_ta_mma<T, DP, WM, WK, KT, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
-    if (e != cudaSuccess) return e;
-    k_ta_mma<T, DP, WM, WK, KT, NS><<<dim3(a.tiles * a.splits, a.kv_heads, a.B), 32 * WM * WK, smem, st>>>(a);
-    return cudaGetLastError();
-}
 template <typename T, int DP>
-cudaError_t run_half(const TreeAttn& a, int rows, cudaStream_t st) {
-    if (rows == 16) return run_mma<T, DP, 1, 4, 32, 3>(a, st);
-    if (rows == 32) return run_mma<T, DP, 2, 2, 32, 3>(a, st);
-    return run_mma<T, DP, 4, 1, 64, 3>(a, st);
+cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
+    constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4);
+    if (attr != cudaSuccess) return attr;
+    k_ta_small_pages<T, DP, NS><<<grid, 128, RING + 65 * a.words * 4, st>>>(a);
+    return cudaGetLastError();
 }
 template <int DP>
-cudaError_t run_f32(const TreeAttn& a, cudaStream_t st) {
-    const size_t smem = ((size_t)(TF_ROWS + 2 * TF_KT) * (DP + 4) + TF_ROWS * (TF_KT + 4) + 48) * 4 + (size_t)(TF_ROWS + 1) * a.words * 4;
-    const cudaError_t e = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
-    if (e != cudaSuccess) return e;
-    k_ta_f32<DP><<<dim3(a.tiles * a.splits, a.kv_heads, a.B), 128, smem, st>>>(a);
+cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
+    constexpr size_t FLOATS = (TF_ROWS + 2 * TF_KT) * (DP + 4) + TF_ROWS * (TF_KT + 4) + 48;
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4 + (TF_ROWS + 1) * 32 * 4);
+    if (attr != cudaSuccess) return attr;
+    k_ta_f32<DP><<<grid, 128, FLOATS * 4 + (TF_ROWS + 1) * a.words * 4, st>>>(a);
     return cudaGetLastError();
 }
+// The merge is launched while the items run, and waits for them.
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
-    k_ta_merge<T><<<dim3((a.T * a.group + 3) / 4, a.kv_heads, a.B), 128, 0, st>>>(a, rows);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((a.T * a.group + 3) / 4, a.kv_heads, a.B); cfg.blockDim = dim3(128); cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization; at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_ta_merge<T>, a, rows);
+}
+PFN_encodeTiled encoder() {
+    static const PFN_encodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess ? (PFN_encodeTiled)p : nullptr;
+    }();
+    return fn;
+}
+bool tensor_map(CUtensorMap& tm, const specdec_cache* c, const void* keys) {
+    const cuuint64_t e = 2;
+    cuuint64_t dims[5] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->n_heads, (cuuint64_t)c->page_tokens, (cuuint64_t)c->n_pages, 2};
+    cuuint64_t strides[4] = {c->stride_head * e, c->stride_token * e, c->stride_page * e, c->stride_side * e};
+    cuuint32_t box[5] = {64, 1, (cuuint32_t)(c->page_tokens < TA_BLOCK ? c->page_tokens : TA_BLOCK), 1, 1}, one[5] = {1, 1, 1, 1, 1};
+    return encoder() && encoder()(&tm, c->dtype == SPECDEC_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void*>(keys), dims, strides,
+                                  box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -507,17 +326,17 @@ using namespace sd;
 
 extern "C" {
 
-long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int max_length) {
+long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length) {
     if (B < 0 || T < 1 || T > 1024 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads || head_dim < 8 || head_dim > 128 || head_dim % 8 ||
-        !op_elem_bytes(dtype) || max_length < 0)
+        !op_elem_bytes(dtype) || page_tokens < 1 || max_length < 0)
         return op_bad("tree_attention_workspace", "sizes that tree_attention does not take");
     if (B == 0) return 0;
-    return part_bytes(plan(B, T, n_q_heads, n_kv_heads, dtype, (long long)max_length + T), B, n_kv_heads, head_dim);
+    return workspace(plan(B, T, n_q_heads, n_kv_heads, dtype, head_dim, page_tokens, (long long)max_length + T), B, n_kv_heads, head_dim);
 }
 
 int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* g, void* stream) {
     const char* who = "tree_attention";
-    if (!c || !g || !c->d_kv || !c->d_table || !c->d_length || (g->B && (!g->d_q || !g->d_out || !g->d_seqs || !g->d_mask))) return op_bad(who, "a pointer is NULL");
+    if (!c || !g || !c->d_kv || !c->d_table || !c->d_length || !c->d_status || (g->B && (!g->d_q || !g->d_out || !g->d_seqs || !g->d_mask))) return op_bad(who, "a pointer is NULL");
     const int e = op_elem_bytes(c->dtype);
     if (!e) return op_bad(who, "unknown dtype");
     if (g->B < 0 || g->B > 65535 || g->T < 1 || c->n_layers < 1 || g->layer < 0 || g->layer >= c->n_layers || c->n_heads < 1 || c->n_heads > 65535 ||
@@ -538,7 +357,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     a.q_sb = g->q_stride_b * e; a.q_st = g->q_stride_t * e; a.q_sh = g->q_stride_h * e;
     a.o_sb = g->out_stride_b * e; a.o_st = g->out_stride_t * e; a.o_sh = g->out_stride_h * e;
     a.s_page = c->stride_page * e; a.s_token = c->stride_token * e; a.s_head = c->stride_head * e;
-    a.table = c->d_table; a.length = c->d_length; a.held = c->d_held; a.seqs = g->d_seqs; a.n_nodes = g->d_n_nodes;
+    a.table = c->d_table; a.length = c->d_length; a.status = c->d_status; a.seqs = g->d_seqs; a.n_nodes = g->d_n_nodes;
     a.mask = g->d_mask; a.mask_sb = g->mask_stride_b;
     a.n_pages = c->n_pages; a.n_seqs = c->n_seqs; a.max_pages = c->max_pages; a.page_shift = __builtin_ctz(c->page_tokens);
     const long long cap = (long long)c->max_pages * c->page_tokens;
@@ -548,21 +367,28 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     a.scale = g->scale * 1.4426950408889634f;
     a.q_vec = (((uintptr_t)g->d_q | a.q_sb | a.q_st | a.q_sh) & 15) == 0;
     a.out_vec = (((uintptr_t)g->d_out | a.o_sb | a.o_st | a.o_sh) & 15) == 0;
-    const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, (long long)a.max_length + a.T);
-    a.tiles = p.tiles; a.splits = p.splits; a.min_blocks = p.min_blocks;
-    const long long need = part_bytes(p, a.B, c->n_heads, c->head_dim);
+    const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, a.dim, c->page_tokens, (long long)a.max_length + a.T);
+    if (p.grid > 0x7fffffff) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
+    a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks;
+    const long long need = workspace(p, a.B, c->n_heads, c->head_dim);
     if (need && (!g->d_workspace || (uintptr_t)g->d_workspace % 16 || g->workspace_bytes < need))
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_tree_attention_workspace says, or not 16-byte aligned");
     a.part = (float*)g->d_workspace;
-    a.part_ml = need ? (float2*)(a.part + (long long)a.B * a.kv_heads * a.tiles * a.splits * p.rows * a.dim) : nullptr;
+    a.part_ml = (float2*)(a.part + part_floats(p, a.dim));
+    a.where = (int2*)(a.part_ml + p.grid * p.rows);
     const cudaStream_t s = (cudaStream_t)stream;
-    const bool wide = a.dim > 64;
+    const bool wide = a.dim > 64, bf = c->dtype == SPECDEC_DTYPE_BF16;
     cudaError_t rc;
-    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? run_f32<128>(a, s) : run_f32<64>(a, s);
-    else if (c->dtype == SPECDEC_DTYPE_BF16) rc = wide ? run_half<__nv_bfloat16, 128>(a, p.rows, s) : run_half<__nv_bfloat16, 64>(a, p.rows, s);
-    else rc = wide ? run_half<__half, 128>(a, p.rows, s) : run_half<__half, 64>(a, p.rows, s);
-    if (rc == cudaSuccess && need)
-        rc = c->dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, p.rows, s) : c->dtype == SPECDEC_DTYPE_BF16 ? run_merge<__nv_bfloat16>(a, p.rows, s) : run_merge<__half>(a, p.rows, s);
+    CUtensorMap tm;
+    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? run_f32<128>(a, (int)p.grid, s) : run_f32<64>(a, (int)p.grid, s);
+    else if (c->page_tokens < TA_MIN_PAGE) {
+        if (bf) rc = wide ? run_small_pages<__nv_bfloat16, 128>(a, (int)p.grid, s) : run_small_pages<__nv_bfloat16, 64>(a, (int)p.grid, s);
+        else rc = wide ? run_small_pages<__half, 128>(a, (int)p.grid, s) : run_small_pages<__half, 64>(a, (int)p.grid, s);
+    } else {
+        if (!tensor_map(tm, c, a.k)) return op_fail(SPECDEC_ERR_CUDA, who, "the driver makes no tensor map of this cache");
+        rc = ta_tma_mma(tm, a, c->dtype, p.rows, (int)p.grid, s);
+    }
+    if (rc == cudaSuccess && need) rc = c->dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, p.rows, s) : bf ? run_merge<__nv_bfloat16>(a, p.rows, s) : run_merge<__half>(a, p.rows, s);
     return rc == cudaSuccess ? SPECDEC_OK : op_fail(SPECDEC_ERR_CUDA, who, cudaGetErrorString(rc));
 }
 

@@ -5,23 +5,30 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "barriers.cuh"
 #include "op_error.cuh"
+#include "tensor_core.cuh"
 
 namespace sd {
 
-// Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's ROWS; the keys of a sequence are its
-// length committed tokens and n nodes behind them, cut into `splits` runs of blocks of TA_BLOCK keys.
-constexpr int TA_BLOCK = 64;
+// Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's rows.  The keys of a sequence are its
+// length committed tokens and n nodes behind them, in blocks of TA_BLOCK.
+//
+// Work: an item is (sequence, split, K/V head, row tile).  direct: a sequence is never split, CTA i is item i.  Otherwise every sequence's blocks are cut into
+// splits of `per` blocks, the same for all, which every CTA works out from the lengths (ta_item); items that share a sequence's keys follow one another.  An item of a
+// sequence with one split writes the output, others write partial results that k_ta_merge joins.
+constexpr int TA_BLOCK = 64, TA_MAX_B = 2048;             // sequences at most where they are split
 struct TreeAttn {
     const char* q; char* out; const char* k; const char* v;
     long long q_sb, q_st, q_sh, o_sb, o_st, o_sh, s_page, s_token, s_head;             // bytes
-    const int* table; const int* length; const int* held; const int* seqs; const int* n_nodes;
+    const int* table; const int* length; const int* seqs; const int* n_nodes; int* status;
     const uint32_t* mask; long long mask_sb;                                           // words
     int n_pages, n_seqs, max_pages, page_shift, max_length;
     int T, words, group, kv_heads, dim, B;
-    int tiles, splits, min_blocks;                                                     // row tiles; splits at most, and blocks a split takes at least
+    int tiles, direct, slots, min_blocks;                                              // row tiles; CTAs that run at once; blocks a split takes at least
     float scale;                                                                       // times log2(e)
-    float* part; float2* part_ml;                                                      // [b, kv head, tile, split, row]: output [dim] and (maximum, sum)
+    float* part; float2* part_ml;                                                      // [item, row of the tile]: output [dim] and (maximum, sum)
+    int2* where;                                                                       // [b, kv head, tile]: first item, splits
     int q_vec, out_vec;                                                                // whether q / out allow 16-byte accesses
 };
 
@@ -35,22 +42,89 @@ __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
     s.keys = s.nodes ? s.len + s.nodes : 0;
     return s;
 }
-// Blocks per split and splits in use for a sequence.
-__device__ __forceinline__ int ta_per_split(const TreeAttn& a, int blocks) { return max((blocks + a.splits - 1) / a.splits, a.min_blocks); }
-__device__ __forceinline__ int ta_used(const TreeAttn& a, int keys, int& per) {
-    const int blocks = (keys + TA_BLOCK - 1) / TA_BLOCK;
-    per = ta_per_split(a, blocks);
-    return (blocks + per - 1) / per;
+
+struct Item { int b, h, tile, split, splits, per; };      // b < 0: none
+// Item number blockIdx.x, for the whole CTA.  scratch: B ints of shared memory, free again behind it.
+__device__ __forceinline__ Item ta_item(const TreeAttn& a, int* scratch) {
+    const int ht = a.kv_heads * a.tiles, unit = blockIdx.x / ht, rest = blockIdx.x - unit * ht;
+    Item it;
+    it.h = rest / a.tiles; it.tile = rest - it.h * a.tiles;
+    if (a.direct) { it.b = unit; it.split = 0; it.splits = 1; it.per = 1 << 24; return it; }
+    __shared__ int found[4];
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) scratch[b] = (ta_keys(a, b).keys + TA_BLOCK - 1) / TA_BLOCK;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        long long total = 0;
+        int most = 1;
+        for (int b = lane; b < a.B; b += 32) { total += scratch[b]; most = max(most, scratch[b]); }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) { total += __shfl_xor_sync(0xffffffffu, total, o); most = max(most, __shfl_xor_sync(0xffffffffu, most, o)); }
+        int per;
+        if (a.B * ht >= a.slots) {                        // more items than fit at once anyway: long sequences are cut so that none runs on alone
+            per = (int)max((total * ht + 2 * a.slots - 1) / (2 * a.slots), (long long)a.min_blocks * 2);
+        } else {                                          // the shortest splits whose items all run at once: 32 candidates at a time
+            int lo = (int)max((total * ht + a.slots - 1) / a.slots, (long long)a.min_blocks), hi = max(most, lo);
+            while (lo < hi) {
+                const int c = lo + (int)((long long)(hi - lo) * lane / 31);
+                int n = 0;
+                for (int b = 0; b < a.B; ++b) n += max(1, (scratch[b] + c - 1) / c);
+                const unsigned fits = __ballot_sync(0xffffffffu, lane == 31 || n * ht <= a.slots);
+                const int f = __ffs(fits) - 1;
+                const int below = __shfl_sync(0xffffffffu, c, max(f - 1, 0));
+                hi = __shfl_sync(0xffffffffu, c, f);
+                lo = f ? min(below + 1, hi) : hi;
+            }
+            per = hi;
+        }
+        int b = -1, split = 0, splits = 1, run = 0;       // the sequence in which unit falls
+        for (int b0 = 0; b0 < a.B && b < 0; b0 += 32) {
+            const int n = b0 + lane < a.B ? max(1, (scratch[b0 + lane] + per - 1) / per) : 0;
+            int upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+            const unsigned m = __ballot_sync(0xffffffffu, run + upto > unit);
+            if (m) {
+                const int f = __ffs(m) - 1;
+                b = b0 + f; splits = __shfl_sync(0xffffffffu, n, f);
+                split = unit - (run + __shfl_sync(0xffffffffu, upto, f) - splits);
+            }
+            run += __shfl_sync(0xffffffffu, upto, 31);
+        }
+        if (lane == 0) { found[0] = b; found[1] = split; found[2] = splits; found[3] = per; }
+    }
+    __syncthreads();
+    it.b = found[0]; it.split = found[1]; it.splits = found[2]; it.per = found[3];
+    if (it.b >= 0 && it.split == 0 && threadIdx.x == 0) a.where[(it.b * a.kv_heads + it.h) * a.tiles + it.tile] = make_int2(blockIdx.x, it.splits);
+    return it;
 }
 
-// What the queries of a row tile see of the nodes: their mask rows, cut at n, in shared memory; and the nodes that any of them sees.
-// 32 keys from key k0 on as bits: committed ones all, nodes by the row's words.
-__device__ __forceinline__ uint32_t ta_window(const uint32_t* row, int words, int base) {      // base = k0 - length
+// What a query sees of 32 keys from key k0 on, as bits: committed ones all, nodes by its row of words; base = k0 - length.
+__device__ __forceinline__ uint32_t ta_window(const uint32_t* row, int words, int base) {
     if (base <= -32) return 0xffffffffu;
     if (base < 0) return ((1u << -base) - 1u) | (words ? row[0] << -base : 0u);
     const int w = base >> 5, s = base & 31;
     const uint32_t a = w < words ? row[w] : 0u, b = w + 1 < words ? row[w + 1] : 0u;
     return __funnelshift_r(a, b, s);
+}
+// The mask rows of a tile's queries (cut at the nodes), and any[w]: the nodes that one of them sees.  Query rows r0 .. r0 + rows - 1.
+__device__ __forceinline__ void ta_load_masks(const TreeAttn& a, int b, int r0, int rows, int nodes, uint32_t* mask, uint32_t* any) {
+    for (int w = threadIdx.x; w < a.words; w += blockDim.x) any[w] = 0;
+    __syncthreads();
+    const int t0 = r0 / a.group, t1 = min((r0 + rows - 1) / a.group, a.T - 1);
+    for (int i = threadIdx.x; i < (t1 - t0 + 1) * a.words; i += blockDim.x) {
+        const int t = t0 + i / a.words, w = i % a.words;
+        uint32_t m = t < nodes ? a.mask[b * a.mask_sb + (long long)t * a.words + w] : 0u;
+        const int left = nodes - w * 32;
+        if (left < 32) m &= left <= 0 ? 0u : (1u << left) - 1u;
+        mask[i] = m;
+        if (m) atomicOr(any + w, m);
+    }
+    __syncthreads();
+}
+// Whether one of the tile's queries may see key `key` < keys.
+__device__ __forceinline__ bool ta_seen(const uint32_t* any, const SeqKeys& s, int key) {
+    return key < s.len || (key < s.keys && (any[(key - s.len) >> 5] >> ((key - s.len) & 31) & 1));
 }
 
 // 16-byte pieces of shared memory from global memory, or zeros.
@@ -62,5 +136,192 @@ __device__ __forceinline__ float ta_exp2(float x) {       // results below 2^-12
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ void ta_ldsm4(uint32_t addr, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ta_ldsm4_t(uint32_t addr, uint32_t* r) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+template <typename T> struct Half;
+template <> struct Half<__nv_bfloat16> {
+    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+template <> struct Half<__half> {
+    static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+};
+
+
+// Sixteen query rows of a warp over blocks of 64 keys: lane l holds rows l / 4 and l / 4 + 8.  Running maximum m and sum l of 2^(s - m), output o; scores
+// in units of log2.  kf(row, piece) / vf(row, piece): shared-memory address of 16-byte piece `piece` of a key's row.
+template <typename T, int DP>
+struct TaRows {
+    static constexpr int NK = TA_BLOCK / 8, ND = DP / 8;
+    float o[ND][4], ma, mb, la, lb;
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        ma = mb = -INFINITY; la = lb = 0.f;
+    }
+    // mask_a, mask_b: the rows' words (null: a row that sees nothing), looked at where the block holds nodes or ends behind the last key
+    template <typename KF, typename VF>
+    __device__ __forceinline__ void block(const uint32_t (*qf)[4], int k0, int len, float scale, int words, const uint32_t* mask_a, const uint32_t* mask_b, KF kf, VF vf) {
+        const int lane = threadIdx.x & 31;
+        float sc[NK][4];
+#pragma unroll
+        for (int i = 0; i < NK; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < DP / 16; ++kk)
+#pragma unroll
+            for (int n = 0; n < TA_BLOCK / 16; ++n) {
+                uint32_t x[4];
+                ta_ldsm4(kf(n * 16 + (lane & 7) + ((lane >> 4) << 3), kk * 2 + ((lane >> 3) & 1)), x);
+                Half<T>::mma(sc[2 * n], qf[kk], x[0], x[1]);
+                Half<T>::mma(sc[2 * n + 1], qf[kk], x[2], x[3]);
+            }
+        if (k0 + TA_BLOCK > len) {
+#pragma unroll
+            for (int n = 0; n < TA_BLOCK / 32; ++n) {
+                const int base = k0 + n * 32 - len;
+                const uint32_t wa = mask_a ? ta_window(mask_a, words, base) : 0u, wb = mask_b ? ta_window(mask_b, words, base) : 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int bit = i * 8 + (lane & 3) * 2;
+                    float* c = sc[n * 4 + i];
+                    if (!(wa >> bit & 1)) c[0] = -INFINITY;
+                    if (!(wa >> bit & 2)) c[1] = -INFINITY;
+                    if (!(wb >> bit & 1)) c[2] = -INFINITY;
+                    if (!(wb >> bit & 2)) c[3] = -INFINITY;
+                }
+            }
+        }
+        float na = -INFINITY, nb = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) { na = fmaxf(na, fmaxf(sc[i][0], sc[i][1])); nb = fmaxf(nb, fmaxf(sc[i][2], sc[i][3])); }
+        na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 1)); na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 2));
+        nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
+        na = fmaxf(ma, na * scale); nb = fmaxf(mb, nb * scale);
+        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
+        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
+        ma = na; mb = nb;
+        la *= fa; lb *= fb;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
+#pragma unroll
+        for (int n = 0; n < TA_BLOCK / 16; ++n) {
+            uint32_t pf[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float* c = sc[2 * n + e];
+                c[0] = ta_exp2(fmaf(c[0], scale, -za)); c[1] = ta_exp2(fmaf(c[1], scale, -za));
+                c[2] = ta_exp2(fmaf(c[2], scale, -zb)); c[3] = ta_exp2(fmaf(c[3], scale, -zb));
+                la += c[0] + c[1]; lb += c[2] + c[3];
+                pf[2 * e] = Half<T>::pack(c[0], c[1]);
+                pf[2 * e + 1] = Half<T>::pack(c[2], c[3]);
+            }
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                uint32_t x[4];
+                ta_ldsm4_t(vf(n * 16 + (lane & 15), d * 2 + (lane >> 4)), x);
+                Half<T>::mma(o[2 * d], pf, x[0], x[1]);
+                Half<T>::mma(o[2 * d + 1], pf, x[2], x[3]);
+            }
+        }
+    }
+    // The lanes' sums together.  A query behind the nodes has taken the committed keys of blocks without a mask; one that sees nothing has multiplied values by 0.
+    __device__ __forceinline__ void finish(bool live_a, bool live_b) {
+        la += __shfl_xor_sync(0xffffffffu, la, 1); la += __shfl_xor_sync(0xffffffffu, la, 2);
+        lb += __shfl_xor_sync(0xffffffffu, lb, 1); lb += __shfl_xor_sync(0xffffffffu, lb, 2);
+        if (!live_a || la == 0.f) {
+            ma = -INFINITY; la = 0.f;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = 0.f;
+        }
+        if (!live_b || lb == 0.f) {
+            mb = -INFINITY; lb = 0.f;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) o[i][2] = o[i][3] = 0.f;
+        }
+    }
+    // Partial results in shared memory: rows of RP floats, and (maximum, sum) of each.
+    static constexpr int RP = DP + 8;
+    __device__ __forceinline__ void leave(float* red, float2* red_ml, int ra) const {
+        const int lane = threadIdx.x & 31;
+        float* pa = red + ra * RP + (lane & 3) * 2;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            *reinterpret_cast<float2*>(pa + i * 8) = make_float2(o[i][0], o[i][1]);
+            *reinterpret_cast<float2*>(pa + 8 * RP + i * 8) = make_float2(o[i][2], o[i][3]);
+        }
+        if ((lane & 3) == 0) { red_ml[ra] = make_float2(ma, la); red_ml[ra + 8] = make_float2(mb, lb); }
+    }
+    __device__ __forceinline__ void join(const float* red, const float2* red_ml, int ra) {
+        const float2 xa = red_ml[ra], xb = red_ml[ra + 8];
+        const float na = fmaxf(ma, xa.x), nb = fmaxf(mb, xb.x);
+        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
+        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb), ea = ta_exp2(xa.x - za), eb = ta_exp2(xb.x - zb);
+        ma = na; mb = nb;
+        la = la * fa + xa.y * ea; lb = lb * fb + xb.y * eb;
+        const float* pa = red + ra * RP + (threadIdx.x & 3) * 2;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const float2 u = *reinterpret_cast<const float2*>(pa + i * 8), w = *reinterpret_cast<const float2*>(pa + 8 * RP + i * 8);
+            o[i][0] = o[i][0] * fa + u.x * ea; o[i][1] = o[i][1] * fa + u.y * ea;
+            o[i][2] = o[i][2] * fb + w.x * eb; o[i][3] = o[i][3] * fb + w.y * eb;
+        }
+    }
+    // Rows ra and ra + 8 of a tile of `rows` that begins at query row r0: the output, or the item's partial results.
+    __device__ __forceinline__ void store(const TreeAttn& a, const Item& it, int r0, int ra, int rows) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = ra + 8 * e, gr = r0 + r;
+            const float l = e ? lb : la, inv = l > 0.f || l != l ? 1.f / l : 0.f;
+            if (gr >= a.T * a.group) continue;
+            if (it.splits == 1) {
+                char* p = a.out + it.b * a.o_sb + (gr / a.group) * a.o_st + (it.h * a.group + gr % a.group) * a.o_sh + (lane & 3) * 4;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    if (i * 8 >= a.dim) break;
+                    const uint32_t x = Half<T>::pack(o[i][2 * e] * inv, o[i][2 * e + 1] * inv);
+                    if (a.out_vec) *reinterpret_cast<uint32_t*>(p + i * 16) = x;
+                    else { reinterpret_cast<unsigned short*>(p + i * 16)[0] = (unsigned short)x; reinterpret_cast<unsigned short*>(p + i * 16)[1] = (unsigned short)(x >> 16); }
+                }
+            } else {
+                const long long slot = (long long)blockIdx.x * rows + r;
+                float* p = a.part + slot * a.dim + (lane & 3) * 2;
+#pragma unroll
+                for (int i = 0; i < ND; ++i) {
+                    if (i * 8 >= a.dim) break;
+                    *reinterpret_cast<float2*>(p + i * 8) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
+                }
+                if ((lane & 3) == 0) a.part_ml[slot] = make_float2(e ? mb : ma, l);
+            }
+        }
+    }
+};
+
+// A tensor map of one layer's keys and values: {head_dim, heads, tokens of a page, pages, 2 sides}; a box is 64 elements (128 bytes, swizzled) of min(page, TA_BLOCK)
+// tokens of one head.  What lies beyond head_dim or the pages arrives as zeros.
+__device__ __forceinline__ void ta_box(uint32_t dst, const CUtensorMap* tm, int d, int head, int token, int page, int side, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+                 ::"r"(dst), "l"(tm), "r"(bar), "r"(d), "r"(head), "r"(token), "r"(page), "r"(side) : "memory");
+}
+constexpr int TA_MIN_PAGE = 8;                            // tokens: a box fills whole swizzle groups of 8 rows
+
+cudaError_t ta_tma_mma(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);
 
 }  // namespace sd

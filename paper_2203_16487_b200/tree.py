@@ -117,7 +117,7 @@ class PagedCache:
         if s:
             self.status.zero_()
             what = [m for bit, m in ((1, "not enough free pages"), (2, "a sequence has no room for more pages"), (4, "a sequence number or path out of range"),
-                                     (8, "tokens outside the pages reserved")) if s & bit]
+                                     (8, "tokens outside the pages reserved"), (16, "a wait inside a kernel gave up")) if s & bit]
             raise SpecDecError(-3, "cache: " + ", ".join(what))
 
 
@@ -155,7 +155,7 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     if mask.shape[0] != B and mask.shape[0] != 1:
         raise ValueError("mask: one for each row of q, or one for all")
     bound = min(max_length, cache.max_length) if max_length > 0 else cache.max_length
-    n = _check(lib().specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._c.dtype, bound))
+    n = _check(lib().specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._c.dtype, cache._c.page_tokens, bound))
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     sq, so = q.stride(), out.stride()
     a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, B), m,
