@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     if (it.b < 0) return;
     const int h = it.h, r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
     const SeqKeys s = ta_keys(a, it.b);
-    ta_load_masks(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
+    ta_load_masks<128, 0>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
     for (int i = tid; i < ROWS * PIECES; i += 128) {      // queries: rows through shared memory into fragments
         const int r = i / PIECES, c = i % PIECES, gr = r0 + r;
         uint4 x = make_uint4(0, 0, 0, 0);
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
     if (it.b < 0) return;
     const int b = it.b, h = it.h, r0 = it.tile * TF_ROWS, all_rows = a.T * a.group;
     const SeqKeys s = ta_keys(a, b);
-    ta_load_masks(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
+    ta_load_masks<128, 0>(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
     for (int i = tid; i < TF_ROWS * DP; i += 128) {
         const int r = i / DP, d = i % DP, gr = r0 + r;
         float x = 0.f;
@@ -219,38 +219,40 @@ template <> __device__ __forceinline__ void put<float>(char* p, float x) { *rein
 template <> __device__ __forceinline__ void put<__nv_bfloat16>(char* p, float x) { *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *reinterpret_cast<__half*>(p) = __float2half_rn(x); }
 
-// One warp a query row: the splits' outputs, each rescaled to the largest maximum.
+// The splits' outputs, each rescaled to the largest maximum: one warp a query row, CTAs that stay.
 template <typename T>
 __global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
-    const int gr = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31, h = blockIdx.y, b = blockIdx.z;
+    const int lane = threadIdx.x & 31, ht = a.kv_heads * a.tiles, all = a.T * a.group;
     cudaGridDependencySynchronize();
-    if (gr >= a.T * a.group) return;
-    const int tile = gr / rows, r = gr % rows, ht = a.kv_heads * a.tiles;
-    const int2 at = a.where[(b * a.kv_heads + h) * a.tiles + tile];       // first item, splits
-    if (at.y <= 1) return;
-    const long long slot0 = (long long)at.x * rows + r, step = (long long)ht * rows;
-    float m = -INFINITY;
-    for (int s = lane; s < at.y; s += 32) m = fmaxf(m, a.part_ml[slot0 + s * step].x);
+    for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * all; w += gridDim.x * 4) {
+        const int bh = w / all, gr = w - bh * all, b = bh / a.kv_heads, h = bh - b * a.kv_heads, tile = gr / rows, r = gr - tile * rows;
+        const int2 at = a.where[bh * a.tiles + tile];     // first item, splits
+        if (at.y <= 1) continue;
+        const long long slot0 = (long long)at.x * rows + r, step = (long long)ht * rows;
+        float m = -INFINITY;
+        for (int s = lane; s < at.y; s += 32) m = fmaxf(m, a.part_ml[slot0 + s * step].x);
 #pragma unroll
-    for (int of = 16; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
-    const float z = m == -INFINITY ? 0.f : m;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);           // lane: four columns
-    float l = 0.f;
+        for (int of = 16; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
+        const float z = m == -INFINITY ? 0.f : m;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);       // lane: four columns
+        float l = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < at.y; ++s) {
-        const long long slot = slot0 + s * step;
-        const float2 ml = a.part_ml[slot];
-        const float f = exp2f(ml.x - z);
-        l += ml.y * f;
-        if (lane * 4 < a.dim) {
-            const float4 x = *reinterpret_cast<const float4*>(a.part + slot * a.dim + lane * 4);
-            o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+        for (int s = 0; s < at.y; ++s) {
+            const long long slot = slot0 + s * step;
+            const float2 ml = a.part_ml[slot];
+            const float f = exp2f(ml.x - z);
+            l += ml.y * f;
+            if (lane * 4 < a.dim) {
+                const float4 x = *reinterpret_cast<const float4*>(a.part + slot * a.dim + lane * 4);
+                o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+            }
         }
+        if (lane * 4 >= a.dim) continue;
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+        const int t = ta_node(a, gr);
+        char* p = a.out + b * a.o_sb + t * a.o_st + (h * a.group + gr - t * a.group) * a.o_sh + lane * 4 * sizeof(T);
+        put<T>(p, o.x * inv); put<T>(p + sizeof(T), o.y * inv); put<T>(p + 2 * sizeof(T), o.z * inv); put<T>(p + 3 * sizeof(T), o.w * inv);
     }
-    if (lane * 4 >= a.dim) return;
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    char* p = a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh + lane * 4 * sizeof(T);
-    put<T>(p, o.x * inv); put<T>(p + sizeof(T), o.y * inv); put<T>(p + 2 * sizeof(T), o.z * inv); put<T>(p + 3 * sizeof(T), o.w * inv);
 }
 
 // ------------------------------------------------------------------ host
@@ -265,7 +267,9 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     p.slots = TA_SMS * (head_dim > 64 ? 2 : 3);           // CTAs that an SM holds at least
     p.min_blocks = 4;
     const long long whole = (long long)B * n_kv_heads * p.tiles, blocks = (max_keys + TA_BLOCK - 1) / TA_BLOCK;
-    p.direct = blocks <= p.min_blocks || B > TA_MAX_B || whole >= 4LL * p.slots;
+    const int least = whole >= p.slots ? 4 * p.min_blocks : p.min_blocks;              // with an item for every SM, only long sequences are worth a merge
+    p.direct = blocks <= least || B > TA_MAX_B || whole >= 4LL * p.slots;
+    if (whole >= p.slots) p.min_blocks = 2 * p.min_blocks;
     p.grid = p.direct ? whole : whole >= p.slots ? whole + 2LL * p.slots : p.slots;
     if (!p.direct && p.grid > whole * ((blocks + p.min_blocks - 1) / p.min_blocks)) p.grid = whole * ((blocks + p.min_blocks - 1) / p.min_blocks);
     return p;
@@ -296,7 +300,8 @@ cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((a.T * a.group + 3) / 4, a.kv_heads, a.B); cfg.blockDim = dim3(128); cfg.stream = st;
+    const long long ctas = ((long long)a.B * a.kv_heads * a.T * a.group + 3) / 4;
+    cfg.gridDim = dim3((unsigned)(ctas < 8 * TA_SMS ? ctas : 8 * TA_SMS)); cfg.blockDim = dim3(128); cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization; at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at; cfg.numAttrs = 1;
@@ -363,13 +368,14 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     const long long cap = (long long)c->max_pages * c->page_tokens;
     a.max_length = (int)(g->max_length && g->max_length < cap ? g->max_length : cap);
     a.T = g->T; a.words = (g->T + 31) / 32; a.group = g->n_q_heads / c->n_heads; a.kv_heads = c->n_heads; a.dim = c->head_dim; a.B = g->B;
-    if ((long long)a.T * a.group > 1 << 20) return op_fail(SPECDEC_ERR_CAPACITY, who, "nodes times query heads of a K/V head pass 2^20");
+    a.group_mul = a.group > 1 ? (uint32_t)(0x100000000ULL / a.group + 1) : 0;
+    if ((long long)a.T * a.group * a.group > 0x7fffffffLL || a.T * a.group > 1 << 20) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many query heads for each K/V head");
     a.scale = g->scale * 1.4426950408889634f;
     a.q_vec = (((uintptr_t)g->d_q | a.q_sb | a.q_st | a.q_sh) & 15) == 0;
     a.out_vec = (((uintptr_t)g->d_out | a.o_sb | a.o_st | a.o_sh) & 15) == 0;
     const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, a.dim, c->page_tokens, (long long)a.max_length + a.T);
-    if (p.grid > 0x7fffffff) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
-    a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks;
+    if (p.grid > 0x7fffffff || (long long)a.B * a.kv_heads * a.T * a.group > 0x7fffffff - 65536) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
+    a.items = (int)p.grid; a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks;
     const long long need = workspace(p, a.B, c->n_heads, c->head_dim);
     if (need && (!g->d_workspace || (uintptr_t)g->d_workspace % 16 || g->workspace_bytes < need))
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_tree_attention_workspace says, or not 16-byte aligned");

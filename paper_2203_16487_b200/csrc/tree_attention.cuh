@@ -25,12 +25,16 @@ struct TreeAttn {
     const uint32_t* mask; long long mask_sb;                                           // words
     int n_pages, n_seqs, max_pages, page_shift, max_length;
     int T, words, group, kv_heads, dim, B;
-    int tiles, direct, slots, min_blocks;                                              // row tiles; CTAs that run at once; blocks a split takes at least
+    uint32_t group_mul;                                                                // see ta_node
+    int items, tiles, direct, slots, min_blocks;                                       // row tiles; CTAs that run at once; blocks a split takes at least
     float scale;                                                                       // times log2(e)
     float* part; float2* part_ml;                                                      // [item, row of the tile]: output [dim] and (maximum, sum)
     int2* where;                                                                       // [b, kv head, tile]: first item, splits
     int q_vec, out_vec;                                                                // whether q / out allow 16-byte accesses
 };
+
+// Node of query row gr: gr / group as a product (gr < 2^20, group * gr < 2^32), 0 for a group of one.
+__device__ __forceinline__ int ta_node(const TreeAttn& a, int gr) { return a.group_mul ? (int)__umulhi((uint32_t)gr, a.group_mul) : gr; }
 
 struct SeqKeys { int seq, len, nodes, keys; };
 __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
@@ -44,12 +48,17 @@ __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
 }
 
 struct Item { int b, h, tile, split, splits, per; };      // b < 0: none
+// Item number i where no sequence is split.
+__device__ __forceinline__ Item ta_direct(const TreeAttn& a, int i) {
+    const int ht = a.kv_heads * a.tiles, b = i / ht, rest = i - b * ht;
+    return Item{b, rest / a.tiles, rest % a.tiles, 0, 1, 1 << 24};
+}
 // Item number blockIdx.x, for the whole CTA.  scratch: B ints of shared memory, free again behind it.
 __device__ __forceinline__ Item ta_item(const TreeAttn& a, int* scratch) {
+    if (a.direct) return ta_direct(a, blockIdx.x);
     const int ht = a.kv_heads * a.tiles, unit = blockIdx.x / ht, rest = blockIdx.x - unit * ht;
     Item it;
     it.h = rest / a.tiles; it.tile = rest - it.h * a.tiles;
-    if (a.direct) { it.b = unit; it.split = 0; it.splits = 1; it.per = 1 << 24; return it; }
     __shared__ int found[4];
     for (int b = threadIdx.x; b < a.B; b += blockDim.x) scratch[b] = (ta_keys(a, b).keys + TA_BLOCK - 1) / TA_BLOCK;
     __syncthreads();
@@ -108,11 +117,14 @@ __device__ __forceinline__ uint32_t ta_window(const uint32_t* row, int words, in
     return __funnelshift_r(a, b, s);
 }
 // The mask rows of a tile's queries (cut at the nodes), and any[w]: the nodes that one of them sees.  Query rows r0 .. r0 + rows - 1.
+// By the first NT threads of the CTA, which meet at barrier BAR.
+template <int NT, int BAR>
 __device__ __forceinline__ void ta_load_masks(const TreeAttn& a, int b, int r0, int rows, int nodes, uint32_t* mask, uint32_t* any) {
-    for (int w = threadIdx.x; w < a.words; w += blockDim.x) any[w] = 0;
-    __syncthreads();
-    const int t0 = r0 / a.group, t1 = min((r0 + rows - 1) / a.group, a.T - 1);
-    for (int i = threadIdx.x; i < (t1 - t0 + 1) * a.words; i += blockDim.x) {
+    auto sync = [] { asm volatile("bar.sync %0, %1;" ::"n"(BAR), "n"(NT) : "memory"); };
+    for (int w = threadIdx.x; w < a.words; w += NT) any[w] = 0;
+    sync();
+    const int t0 = ta_node(a, r0), t1 = min(ta_node(a, r0 + rows - 1), a.T - 1);
+    for (int i = threadIdx.x; i < (t1 - t0 + 1) * a.words; i += NT) {
         const int t = t0 + i / a.words, w = i % a.words;
         uint32_t m = t < nodes ? a.mask[b * a.mask_sb + (long long)t * a.words + w] : 0u;
         const int left = nodes - w * 32;
@@ -120,11 +132,31 @@ __device__ __forceinline__ void ta_load_masks(const TreeAttn& a, int b, int r0, 
         mask[i] = m;
         if (m) atomicOr(any + w, m);
     }
-    __syncthreads();
+    sync();
 }
 // Whether one of the tile's queries may see key `key` < keys.
 __device__ __forceinline__ bool ta_seen(const uint32_t* any, const SeqKeys& s, int key) {
     return key < s.len || (key < s.keys && (any[(key - s.len) >> 5] >> ((key - s.len) & 31) & 1));
+}
+
+// Zeros for the values, in a block of 64 rows of HALVES x 128 bytes, that none of the tile's queries sees: whatever is in them is multiplied by 0.  Rows
+// [row0, row0 + ROWS) by one warp (32 of them share a word of what is seen).
+template <int ROWS, int HALVES>
+__device__ __forceinline__ void ta_zero_unseen(char* values, int row0, int k0, const SeqKeys& s, const uint32_t* any, int words) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int r0 = 0; r0 < ROWS; r0 += 32) {
+        constexpr int N = ROWS < 32 ? ROWS : 32;
+        const uint32_t seen = ta_window(any, words, k0 + row0 + r0 - s.len);
+#pragma unroll
+        for (int r = 0; r < N; r += 4) {
+            const int mine = r + (lane >> 3);
+            if (!(seen >> mine & 1))
+#pragma unroll
+                for (int hf = 0; hf < HALVES; ++hf)
+                    *reinterpret_cast<uint4*>(values + hf * TA_BLOCK * 128 + (row0 + r0 + mine) * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+        }
+    }
 }
 
 // 16-byte pieces of shared memory from global memory, or zeros.
@@ -292,7 +324,8 @@ struct TaRows {
             const float l = e ? lb : la, inv = l > 0.f || l != l ? 1.f / l : 0.f;
             if (gr >= a.T * a.group) continue;
             if (it.splits == 1) {
-                char* p = a.out + it.b * a.o_sb + (gr / a.group) * a.o_st + (it.h * a.group + gr % a.group) * a.o_sh + (lane & 3) * 4;
+                const int t = ta_node(a, gr);
+                char* p = a.out + it.b * a.o_sb + t * a.o_st + (it.h * a.group + gr - t * a.group) * a.o_sh + (lane & 3) * 4;
 #pragma unroll
                 for (int i = 0; i < ND; ++i) {
                     if (i * 8 >= a.dim) break;

@@ -23,129 +23,155 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     __shared__ int abort_flag;
     char* ring = ta_smem + (1024 - (smem_u32(ta_smem) & 1023)) % 1024;
     uint32_t* any = (uint32_t*)(ring + NS * STAGE);
-    uint32_t* mask = any + a.words;
+    uint32_t* mask = any + (a.words + 1) / 2 * 2;         // (8-byte aligned, as the partial results behind it are)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
-    if (tid == 0) {
+    if (warp == TM_WARPS && lane == 0) {
         for (int i = 0; i < NS; ++i) { mbar_init(full + i * 8, 1); mbar_init(empty + i * 8, WM); }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
-    const Item it = ta_item(a, (int*)ring);
-    if (it.b < 0) return;
+    const Item first = ta_item(a, (int*)ring);
+    if (first.b < 0) return;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ta_item's use of the ring, ahead of the boxes
-    const SeqKeys s = ta_keys(a, it.b);
-    const int r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
-    ta_load_masks(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
-    const int k_begin = it.split * it.per * KT, k_end = min(s.keys, (int)min((long long)(it.split + 1) * it.per * KT, (long long)s.keys));
-    const int blocks = max(0, (k_end - k_begin + KT - 1) / KT);
+    __syncthreads();
+    int done = 0;                                         // blocks of the items before
+    auto range = [&](const Item& it, const SeqKeys& s, int& k_begin, int& k_end) {
+        k_begin = it.split * it.per * KT;
+        k_end = (int)min((long long)(it.split + 1) * it.per * KT, (long long)s.keys);
+        return max(0, (k_end - k_begin + KT - 1) / KT);
+    };
 
-    if (warp == TM_WARPS) {                               // loads
-        const int page = 1 << a.page_shift, rows = min(page, KT), n_pages = KT / rows;
-        const int* table = a.table + (long long)s.seq * a.max_pages;
-        auto page_of = [&](int j) {                       // this lane's page of block j: out of range where there is none
-            const int key = k_begin + j * KT + lane * rows, i = key >> a.page_shift;
-            int p = -1;
-            if (lane < n_pages && key < k_end && i < a.max_pages) p = table[i];
-            return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
-        };
-        int p = blocks ? page_of(0) : 0;
-        for (int j = 0; j < blocks; ++j) {
-            const int st = j % NS, key = k_begin + j * KT + lane * rows;
-            const int cur = p;
-            if (j + 1 < blocks) p = page_of(j + 1);
-            if (j >= NS && !mbar_wait_warp(empty + st * 8, (j / NS - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
-            const bool mine = lane < n_pages && key < k_end;
-            const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
-            if (lane == 0) mbar_expect_tx(full + st * 8, boxes * rows * 128 * HALVES * 2);
-            __syncwarp();
-            if (mine) {
-                const uint32_t d = smem_u32(ring + st * STAGE) + lane * rows * 128;
+    if (warp == TM_WARPS) {                               // loads, running ahead into the next items
+        const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
+        Item it = first;
+        SeqKeys s = ta_keys(a, it.b);
+        for (int item = blockIdx.x; item < a.items; item += gridDim.x) {
+            int k_begin, k_end;
+            const int blocks = range(it, s, k_begin, k_end);
+            const int* table = a.table + (long long)s.seq * a.max_pages;
+            auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
+                const int key = k_begin + j * KT + lane * box, i = key >> a.page_shift;
+                int p = -1;
+                if (lane < n_pages && key < k_end && i < a.max_pages) p = table[i];
+                return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
+            };
+            int p = blocks ? page_of(0) : 0;
+            const int h = it.h;
+            if (item + gridDim.x < a.items) { it = ta_direct(a, item + gridDim.x); s = ta_keys(a, it.b); }
+            for (int j = 0; j < blocks; ++j) {
+                const int n = done + j, st = n % NS, key = k_begin + j * KT + lane * box, cur = p;
+                if (j + 1 < blocks) p = page_of(j + 1);
+                if (n >= NS && !mbar_wait_warp(empty + st * 8, (n / NS - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
+                const bool mine = lane < n_pages && key < k_end;
+                const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                if (lane == 0) mbar_expect_tx(full + st * 8, boxes * box * 128 * HALVES * 2);
+                __syncwarp();
+                if (mine) {
+                    const uint32_t d = smem_u32(ring + st * STAGE) + lane * box * 128;
 #pragma unroll
-                for (int side = 0; side < 2; ++side)
+                    for (int side = 0; side < 2; ++side)
 #pragma unroll
-                    for (int hf = 0; hf < HALVES; ++hf)
-                        ta_box(d + side * SIDE + hf * KT * 128, &tm, hf * 64, it.h, key & (page - 1), cur, side, full + st * 8);
+                        for (int hf = 0; hf < HALVES; ++hf)
+                            ta_box(d + side * SIDE + hf * KT * 128, &tm, hf * 64, h, key & (page - 1), cur, side, full + st * 8);
+                }
             }
+            if (abort_flag) break;
+            done += (blocks + WK - 1) / WK * WK;          // the next item's first block is group 0's again
         }
-        __syncthreads();
-        if constexpr (WK > 1) __syncthreads();
         return;
     }
 
-    const int wm = warp % WM, wk = warp / WM;
-    const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
-    const int ga = r0 + ra, gb = r0 + rb, ta = ga / a.group, tb = gb / a.group;
-    const bool live_a = ga < all_rows && ta < s.nodes, live_b = gb < all_rows && tb < s.nodes;
-    const uint32_t* mask_a = mask + (live_a ? ta - t0 : 0) * a.words;
-    const uint32_t* mask_b = mask + (live_b ? tb - t0 : 0) * a.words;
-    uint32_t qf[DP / 16][4];                              // the rows as fragments, straight from memory
-    {
-        const char* qa = a.q + it.b * a.q_sb + ta * a.q_st + (it.h * a.group + ga % a.group) * a.q_sh + (lane & 3) * 4;
-        const char* qb = a.q + it.b * a.q_sb + tb * a.q_st + (it.h * a.group + gb % a.group) * a.q_sh + (lane & 3) * 4;
-        auto two = [&](const char* p) -> uint32_t {
-            if (a.q_vec) return *reinterpret_cast<const uint32_t*>(p);
-            return reinterpret_cast<const unsigned short*>(p)[0] | (uint32_t)reinterpret_cast<const unsigned short*>(p)[1] << 16;
-        };
+    const int wm = warp % WM, wk = warp / WM, all_rows = a.T * a.group;
+    auto consumers = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * TM_WARPS) : "memory"); };
+    Item next = first;
+    SeqKeys next_s = ta_keys(a, next.b);
+    for (int item = blockIdx.x; item < a.items; item += gridDim.x) {
+        const Item it = next;
+        const SeqKeys s = next_s;
+        if (item + gridDim.x < a.items) { next = ta_direct(a, item + gridDim.x); next_s = ta_keys(a, next.b); }
+        int k_begin, k_end;
+        const int blocks = range(it, s, k_begin, k_end), r0 = it.tile * ROWS, t0 = ta_node(a, r0);
+        const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
+        const int ga = r0 + ra, gb = r0 + rb, ta = ta_node(a, ga), tb = ta_node(a, gb);
+        const bool live_a = ga < all_rows && ta < s.nodes, live_b = gb < all_rows && tb < s.nodes;
+        uint32_t qf[DP / 16][4];                          // the rows as fragments, straight from memory
+        {
+            const char* qa = a.q + it.b * a.q_sb + ta * a.q_st + (it.h * a.group + ga - ta * a.group) * a.q_sh + (lane & 3) * 4;
+            const char* qb = a.q + it.b * a.q_sb + tb * a.q_st + (it.h * a.group + gb - tb * a.group) * a.q_sh + (lane & 3) * 4;
+            auto two = [&](const char* p) -> uint32_t {
+                if (a.q_vec) return *reinterpret_cast<const uint32_t*>(p);
+                return reinterpret_cast<const unsigned short*>(p)[0] | (uint32_t)reinterpret_cast<const unsigned short*>(p)[1] << 16;
+            };
 #pragma unroll
-        for (int kk = 0; kk < DP / 16; ++kk) {
-            const bool lo = kk * 16 < a.dim, hi = kk * 16 + 8 < a.dim;
-            qf[kk][0] = live_a && lo ? two(qa + kk * 32) : 0u;
-            qf[kk][1] = live_b && lo ? two(qb + kk * 32) : 0u;
-            qf[kk][2] = live_a && hi ? two(qa + kk * 32 + 16) : 0u;
-            qf[kk][3] = live_b && hi ? two(qb + kk * 32 + 16) : 0u;
+            for (int kk = 0; kk < DP / 16; ++kk) {
+                const bool lo = kk * 16 < a.dim, hi = kk * 16 + 8 < a.dim;
+                qf[kk][0] = live_a && lo ? two(qa + kk * 32) : 0u;
+                qf[kk][1] = live_b && lo ? two(qb + kk * 32) : 0u;
+                qf[kk][2] = live_a && hi ? two(qa + kk * 32 + 16) : 0u;
+                qf[kk][3] = live_b && hi ? two(qb + kk * 32 + 16) : 0u;
+            }
         }
-    }
-    TaRows<T, DP> rows;
-    rows.clear();
-    for (int j = wk; j < blocks; j += WK) {
-        const int st = j % NS, k0 = k_begin + j * KT;
-        if (!mbar_wait_warp(full + st * 8, (j / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
-        const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
-        const bool tail = k0 + KT > s.len;                // nodes, or what is behind the last key
-        if (tail) {                                       // values that no query sees: whatever is in them is multiplied by 0
-            for (int r = wm * (KT / WM); r < (wm + 1) * (KT / WM); ++r)
-                if (k0 + r >= k_end || !ta_seen(any, s, k0 + r))
-                    if (lane < DP / 8) *reinterpret_cast<uint4*>(ring + st * STAGE + SIDE + (lane >> 3) * KT * 128 + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-            if constexpr (WM == 1) __syncwarp();
-            else asm volatile("bar.sync %0, %1;" ::"r"(1 + wk), "n"(32 * WM) : "memory");
+        ta_load_masks<32 * TM_WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
+        const uint32_t* mask_a = live_a ? mask + (ta - t0) * a.words : nullptr;
+        const uint32_t* mask_b = live_b ? mask + (tb - t0) * a.words : nullptr;
+        TaRows<T, DP> rows;
+        rows.clear();
+        for (int j = wk; j < blocks; j += WK) {
+            const int n = done + j, st = n % NS, k0 = k_begin + j * KT;
+            if (!mbar_wait_warp(full + st * 8, (n / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
+            const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
+            const bool tail = k0 + KT > s.len;            // nodes, or what is behind the last key
+            if (tail) {                                   // values that no query sees: whatever is in them is multiplied by 0
+                ta_zero_unseen<KT / WM, HALVES>(ring + st * STAGE + SIDE, wm * (KT / WM), k0, s, any, a.words);
+                if constexpr (WM == 1) __syncwarp();
+                else asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "n"(32 * WM) : "memory");
+            }
+            rows.block(qf, k0, s.len, a.scale, a.words, mask_a, mask_b,
+                       [&](int r, int c) { return ks + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); },
+                       [&](int r, int c) { return vs + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); });
+            if (tail) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the zeros, ahead of the stage's next boxes
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + st * 8);
         }
-        rows.block(qf, k0, s.len, a.scale, a.words, live_a ? mask_a : nullptr, live_b ? mask_b : nullptr,
-                   [&](int r, int c) { return ks + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); },
-                   [&](int r, int c) { return vs + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); });
-        if (tail) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");         // the zeros, ahead of the stage's next boxes
-        __syncwarp();
-        if (lane == 0) mbar_arrive(empty + st * 8);
-    }
-    rows.finish(live_a, live_b);
-    __syncthreads();                                      // the ring is free
-    if constexpr (WK > 1) {
-        constexpr int RP = TaRows<T, DP>::RP;
-        float* red = reinterpret_cast<float*>(ring);      // [WK - 1][ROWS][RP], then [WK - 1][ROWS] (maximum, sum)
-        float2* red_ml = reinterpret_cast<float2*>(red + (WK - 1) * ROWS * RP);
-        static_assert((WK - 1) * ROWS * (RP * 4 + 8) <= NS * STAGE, "partial outputs fit the ring");
-        if (wk > 0) rows.leave(red + (wk - 1) * ROWS * RP, red_ml + (wk - 1) * ROWS, ra);
-        __syncthreads();
-        if (wk > 0) return;
+        done += (blocks + WK - 1) / WK * WK;
+        rows.finish(live_a, live_b);
+        if constexpr (WK > 1) {                           // the groups' results meet in the first group
+            constexpr int RP = TaRows<T, DP>::RP;
+            float* red = reinterpret_cast<float*>(mask + ROWS * a.words);    // [WK - 1][ROWS][RP], then [WK - 1][ROWS] (maximum, sum)
+            float2* red_ml = reinterpret_cast<float2*>(red + (WK - 1) * ROWS * RP);
+            if (wk > 0) rows.leave(red + (wk - 1) * ROWS * RP, red_ml + (wk - 1) * ROWS, ra);
+            consumers();
+            if (wk == 0) {
 #pragma unroll
-        for (int g = 0; g < WK - 1; ++g) rows.join(red + g * ROWS * RP, red_ml + g * ROWS, ra);
+                for (int g = 0; g < WK - 1; ++g) rows.join(red + g * ROWS * RP, red_ml + g * ROWS, ra);
+            }
+        }
+        if (wk == 0) rows.store(a, it, r0, ra, ROWS);
+        consumers();                                      // masks and partial results may be overwritten
     }
-    rows.store(a, it, r0, ra, ROWS);
 }
 
 template <typename T, int DP, int WM, int WK, int NS>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr int RING = NS * 2 * TA_BLOCK * DP * 2;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tma<T, DP, WM, WK, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 1024 + (16 * WM + 1) * 32 * 4);
+    constexpr int ROWS = 16 * WM, RING = NS * 2 * TA_BLOCK * DP * 2, RED = (WK - 1) * ROWS * ((DP + 8) * 4 + 8);
+    constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4;
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tma<T, DP, WM, WK, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
-    k_ta_tma<T, DP, WM, WK, NS><<<grid, 32 * (WM * WK + 1), RING + 1024 + (16 * WM + 1) * a.words * 4, st>>>(tm, a);
+    static const int per_sm = [] {
+        int n = 1;
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_ta_tma<T, DP, WM, WK, NS>, 32 * (WM * WK + 1), MOST);
+        return n < 1 ? 1 : n;
+    }();
+    const int most = a.direct ? per_sm * 148 : grid;      // whole sequences: CTAs that stay, each with every gridDim.x-th item
+    k_ta_tma<T, DP, WM, WK, NS><<<grid < most ? grid : most, 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4, st>>>(tm, a);
     return cudaGetLastError();
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {
     if (a.dim > 64) return rows == 16 ? run<T, 128, 1, 3, 3>(tm, a, grid, st) : rows == 32 ? run<T, 128, 2, 1, 3>(tm, a, grid, st) : run<T, 128, 4, 1, 3>(tm, a, grid, st);
-    return rows == 16 ? run<T, 64, 1, 4, 4>(tm, a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 4>(tm, a, grid, st) : run<T, 64, 4, 1, 3>(tm, a, grid, st);
+    return rows == 16 ? run<T, 64, 1, 4, 4>(tm, a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 2>(tm, a, grid, st) : run<T, 64, 4, 1, 3>(tm, a, grid, st);
 }
 
 }  // namespace
