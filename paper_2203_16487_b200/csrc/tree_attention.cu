@@ -3,6 +3,7 @@
 // out = sum_j p_j v_j over the keys a query sees, p = softmax(scale q . k).  One pass over the keys with the running maximum m and sum l of
 // 2^(s - m): s in units of log2, sums and outputs in fp32, rescaled where m grows.  All query heads of a K/V head share its keys, so a row tile
 // mixes nodes and heads; few rows: the keys of a sequence are split over CTAs, whose partial outputs k_ta_merge joins.
+#include <cstdlib>
 #include "tree_attention.cuh"
 
 namespace sd {
@@ -262,9 +263,10 @@ struct Plan { int rows, tiles, direct, slots, min_blocks; long long grid; };
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, int page_tokens, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
-    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : 64;
+    static const int thr = getenv("TA_THR") ? atoi(getenv("TA_THR")) : 64;
+    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 && thr >= 16 ? 16 : all <= 32 && thr>=32 ? 32 : all <= thr ? 64 : all <= 128 ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
-    p.slots = TA_SMS * (head_dim > 64 ? 2 : 3);           // CTAs that an SM holds at least
+    p.slots = TA_SMS * (p.rows >= 128 ? 1 : head_dim > 64 ? 2 : 3);        // CTAs that an SM holds at least
     p.min_blocks = 4;
     const long long whole = (long long)B * n_kv_heads * p.tiles, blocks = (max_keys + TA_BLOCK - 1) / TA_BLOCK;
     const int least = whole >= p.slots ? 4 * p.min_blocks : p.min_blocks;              // with an item for every SM, only long sequences are worth a merge
@@ -375,7 +377,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     a.out_vec = (((uintptr_t)g->d_out | a.o_sb | a.o_st | a.o_sh) & 15) == 0;
     const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, a.dim, c->page_tokens, (long long)a.max_length + a.T);
     if (p.grid > 0x7fffffff || (long long)a.B * a.kv_heads * a.T * a.group > 0x7fffffff - 65536) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
-    a.items = (int)p.grid; a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks;
+    a.items = (int)p.grid; a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks; a.even = p.rows >= 128;
     const long long need = workspace(p, a.B, c->n_heads, c->head_dim);
     if (need && (!g->d_workspace || (uintptr_t)g->d_workspace % 16 || g->workspace_bytes < need))
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_tree_attention_workspace says, or not 16-byte aligned");
@@ -392,7 +394,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
         else rc = wide ? run_small_pages<__half, 128>(a, (int)p.grid, s) : run_small_pages<__half, 64>(a, (int)p.grid, s);
     } else {
         if (!tensor_map(tm, c, a.k)) return op_fail(SPECDEC_ERR_CUDA, who, "the driver makes no tensor map of this cache");
-        rc = ta_tma_mma(tm, a, c->dtype, p.rows, (int)p.grid, s);
+        rc = p.rows >= 128 ? ta_tc(tm, a, c->dtype, p.rows, (int)p.grid, s) : ta_tma_mma(tm, a, c->dtype, p.rows, (int)p.grid, s);
     }
     if (rc == cudaSuccess && need) rc = c->dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, p.rows, s) : bf ? run_merge<__nv_bfloat16>(a, p.rows, s) : run_merge<__half>(a, p.rows, s);
     return rc == cudaSuccess ? SPECDEC_OK : op_fail(SPECDEC_ERR_CUDA, who, cudaGetErrorString(rc));

@@ -26,7 +26,7 @@ struct TreeAttn {
     int n_pages, n_seqs, max_pages, page_shift, max_length;
     int T, words, group, kv_heads, dim, B;
     uint32_t group_mul;                                                                // see ta_node
-    int items, tiles, direct, slots, min_blocks;                                       // row tiles; CTAs that run at once; blocks a split takes at least
+    int items, tiles, direct, slots, min_blocks, even;                                      // row tiles; CTAs that run at once; blocks a split takes at least
     float scale;                                                                       // times log2(e)
     float* part; float2* part_ml;                                                      // [item, row of the tile]: output [dim] and (maximum, sum)
     int2* where;                                                                       // [b, kv head, tile]: first item, splits
@@ -86,6 +86,7 @@ __device__ __forceinline__ Item ta_item(const TreeAttn& a, int* scratch) {
             }
             per = hi;
         }
+        per += per & a.even;                              // whole blocks of 128 keys
         int b = -1, split = 0, splits = 1, run = 0;       // the sequence in which unit falls
         for (int b0 = 0; b0 < a.B && b < 0; b0 += 32) {
             const int n = b0 + lane < a.B ? max(1, (scratch[b0 + lane] + per - 1) / per) : 0;
@@ -355,6 +356,7 @@ __device__ __forceinline__ void ta_box(uint32_t dst, const CUtensorMap* tm, int 
 }
 constexpr int TA_MIN_PAGE = 8;                            // tokens: a box fills whole swizzle groups of 8 rows
 
-cudaError_t ta_tma_mma(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);
+cudaError_t ta_tma_mma(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);         // tiles of 16, 32, 64 rows
+cudaError_t ta_tc(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);              // of 128, 256
 
 }  // namespace sd
