@@ -10,20 +10,24 @@ namespace sd {
 namespace {
 
 // ------------------------------------------------------------------ 16-bit types, pages of fewer than TA_MIN_PAGE tokens
-// Such pages are no TMA boxes: every thread fetches 16-byte pieces (cp.async).  One item a CTA: 4 warps of 16 rows, a ring of NS blocks of 64 keys, rows of
+// Such pages are no TMA boxes: every thread fetches 16-byte pieces (cp.async).  4 warps of 16 rows, a ring of NS blocks of 64 keys, rows of
 // DP elements whose 16-byte pieces are XORed with the row's low three bits.
 template <typename T, int DP, int NS>
 __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     constexpr int ROWS = 64, KT = TA_BLOCK, PITCH = DP * 2, PIECES = DP / 8, STAGE = 2 * KT * PITCH;
     extern __shared__ __align__(128) char sm[];
     char* ring = sm;                                      // [NS][K, V][KT][PITCH]; at first the queries
-    uint32_t* any = (uint32_t*)(sm + NS * STAGE);
+    int* units = (int*)(sm + NS * STAGE);
+    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
-    const Item it = ta_item(a, (int*)ring);
-    if (it.b < 0) return;
+    TaWork work;
+    work.begin(a, units);
+    Part it;
+    while (work.next(a, units, it, tid == 0)) {
+    __syncthreads();
     const int h = it.h, r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
-    const SeqKeys s = ta_keys(a, it.b);
+    const SeqKeys& s = it.s;
     ta_load_masks<128, 0>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
     for (int i = tid; i < ROWS * PIECES; i += 128) {      // queries: rows through shared memory into fragments
         const int r = i / PIECES, c = i % PIECES, gr = r0 + r;
@@ -54,8 +58,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
             const int r = (i / PIECES) % KT, c = i % PIECES;
             if (c * 8 >= a.dim) *reinterpret_cast<uint4*>(ring + (i / PIECES) * PITCH + ((c ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
         }
-    const int k_begin = it.split * it.per * KT, k_end = min(s.keys, (int)min((long long)(it.split + 1) * it.per * KT, (long long)s.keys));
-    const int blocks = max(0, (k_end - k_begin + KT - 1) / KT), real_pieces = a.dim / 8;
+    const int k_begin = it.k_begin, k_end = it.k_end, blocks = it.blocks, real_pieces = a.dim / 8;
     auto load = [&](int j) {
         if (j < blocks) {
             char* st = ring + (j % NS) * STAGE;
@@ -93,6 +96,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     rows.finish(live_a, live_b);
     rows.store(a, it, r0, ra, ROWS);
+    }
 }
 
 // ------------------------------------------------------------------ fp32: FFMA
@@ -107,13 +111,17 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
     float* vt = kt + TF_KT * KP;
     float* sc = vt + TF_KT * KP;                          // [16][SP]
     float* row_f = sc + TF_ROWS * SP;                     // [16] rescale, [16] maximum, [16] sum
-    uint32_t* any = reinterpret_cast<uint32_t*>(row_f + 48);
+    int* units = reinterpret_cast<int*>(row_f + 48);
+    uint32_t* any = reinterpret_cast<uint32_t*>(units + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Item it = ta_item(a, reinterpret_cast<int*>(sm));
-    if (it.b < 0) return;
+    TaWork work;
+    work.begin(a, units);
+    Part it;
+    while (work.next(a, units, it, tid == 0)) {
+    __syncthreads();
     const int b = it.b, h = it.h, r0 = it.tile * TF_ROWS, all_rows = a.T * a.group;
-    const SeqKeys s = ta_keys(a, b);
+    const SeqKeys& s = it.s;
     ta_load_masks<128, 0>(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
     for (int i = tid; i < TF_ROWS * DP; i += 128) {
         const int r = i / DP, d = i % DP, gr = r0 + r;
@@ -123,7 +131,7 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
     }
     if (tid < 16) { row_f[16 + tid] = -INFINITY; row_f[32 + tid] = 0.f; }
     const int t0 = r0 / a.group;
-    const int k_begin = it.split * it.per * TA_BLOCK, k_end = min(s.keys, (int)min((long long)(it.split + 1) * it.per * TA_BLOCK, (long long)s.keys));
+    const int k_begin = it.k_begin, k_end = it.k_end;
     constexpr int DC = DP / 4, RG = 128 / DC, RR = TF_ROWS / RG;           // output: DC column groups of 4, RG row groups of RR rows
     const int oc = tid % DC, og = tid / DC;
     float4 o[RR];
@@ -195,14 +203,14 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
         }
     }
     __syncthreads();
-    const long long slot = (long long)blockIdx.x * TF_ROWS;
+    const long long slot = it.slot * TF_ROWS;
 #pragma unroll
     for (int i = 0; i < RR; ++i) {
         const int r = og * RR + i, gr = r0 + r;
         if (gr >= all_rows || oc * 4 >= a.dim) continue;
         const float l = row_f[32 + r];
         if (l == 0.f) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);               // sees nothing: values times 0
-        if (it.splits == 1) {
+        if (it.whole) {
             const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
             float* p = reinterpret_cast<float*>(a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh) + oc * 4;
             if (a.out_vec) *reinterpret_cast<float4*>(p) = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
@@ -212,6 +220,7 @@ __global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
             if (oc == 0) a.part_ml[slot + r] = make_float2(row_f[16 + r], l);
         }
     }
+    }
 }
 
 // ------------------------------------------------------------------ merge
@@ -220,14 +229,14 @@ template <> __device__ __forceinline__ void put<float>(char* p, float x) { *rein
 template <> __device__ __forceinline__ void put<__nv_bfloat16>(char* p, float x) { *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *reinterpret_cast<__half*>(p) = __float2half_rn(x); }
 
-// The splits' outputs, each rescaled to the largest maximum: one warp a query row, CTAs that stay.
+// The parts' outputs, each rescaled to the largest maximum: one warp a query row, CTAs that stay.
 template <typename T>
 __global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
     const int lane = threadIdx.x & 31, ht = a.kv_heads * a.tiles, all = a.T * a.group;
     cudaGridDependencySynchronize();
     for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * all; w += gridDim.x * 4) {
         const int bh = w / all, gr = w - bh * all, b = bh / a.kv_heads, h = bh - b * a.kv_heads, tile = gr / rows, r = gr - tile * rows;
-        const int2 at = a.where[bh * a.tiles + tile];     // first item, splits
+        const int2 at = a.where[bh * a.tiles + tile];     // first slot, parts
         if (at.y <= 1) continue;
         const long long slot0 = (long long)at.x * rows + r, step = (long long)ht * rows;
         float m = -INFINITY;
@@ -257,8 +266,7 @@ __global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
 }
 
 // ------------------------------------------------------------------ host
-constexpr int TA_SMS = 148;
-struct Plan { int rows, tiles, direct, slots, min_blocks; long long grid; };
+struct Plan { int rows, tiles, direct, ctas, unit, min_units; long long grid, slots; };       // see TreeAttn; slots of partial results
 // Rows of a tile: 16, 32 or 64 by the rows there are (64 share a block's keys among four warps; fewer rows give the warps keys of their own instead).
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, int page_tokens, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
@@ -266,36 +274,39 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     static const int thr = getenv("TA_THR") ? atoi(getenv("TA_THR")) : 64;
     p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 && thr >= 16 ? 16 : all <= 32 && thr>=32 ? 32 : all <= thr ? 64 : all <= 128 ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
-    p.slots = TA_SMS * (p.rows >= 128 ? 1 : head_dim > 64 ? 2 : 3);        // CTAs that an SM holds at least
-    p.min_blocks = 4;
-    const long long whole = (long long)B * n_kv_heads * p.tiles, blocks = (max_keys + TA_BLOCK - 1) / TA_BLOCK;
-    const int least = whole >= p.slots ? 4 * p.min_blocks : p.min_blocks;              // with an item for every SM, only long sequences are worth a merge
-    p.direct = blocks <= least || B > TA_MAX_B || whole >= 4LL * p.slots;
-    if (whole >= p.slots) p.min_blocks = 2 * p.min_blocks;
-    p.grid = p.direct ? whole : whole >= p.slots ? whole + 2LL * p.slots : p.slots;
-    if (!p.direct && p.grid > whole * ((blocks + p.min_blocks - 1) / p.min_blocks)) p.grid = whole * ((blocks + p.min_blocks - 1) / p.min_blocks);
+    p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
+    p.min_units = p.rows >= 128 ? 4 : 4;
+    const int at_once = TA_SMS * (p.rows >= 128 ? 1 : head_dim > 64 ? 2 : 3);          // CTAs that an SM holds at least
+    const long long columns = (long long)n_kv_heads * p.tiles, whole = B * columns, units = (max_keys + p.unit - 1) / p.unit;
+    // With work for every CTA twice over, only long sequences are worth cutting, and the merge that follows.
+    p.direct = units <= (whole >= 2 * at_once ? 4 * p.min_units : p.min_units) || B > TA_MAX_B;
+    p.ctas = (int)(at_once / columns < 1 ? 1 : at_once / columns);
+    const long long most = (B * units + p.min_units - 1) / p.min_units;                // stretches at most
+    if (p.ctas > most) p.ctas = (int)most;
+    p.grid = p.direct ? whole : p.ctas * columns;
+    p.slots = p.direct ? 0 : (p.ctas + B) * columns;
     return p;
 }
-// Bytes: partial outputs, then (maximum, sum), then where a tile's items are.
-long long part_floats(const Plan& p, int head_dim) { return p.direct ? 0 : p.grid * p.rows * head_dim; }
+// Bytes: partial outputs, then (maximum, sum), then where a tile's parts are.
+long long part_floats(const Plan& p, int head_dim) { return p.slots * p.rows * head_dim; }
 long long workspace(const Plan& p, int B, int n_kv_heads, int head_dim) {
-    return p.direct ? 0 : part_floats(p, head_dim) * 4 + p.grid * p.rows * 8 + (long long)B * n_kv_heads * p.tiles * 8;
+    return p.direct ? 0 : part_floats(p, head_dim) * 4 + p.slots * p.rows * 8 + (long long)B * n_kv_heads * p.tiles * 8;
 }
 
 template <typename T, int DP>
 cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4);
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 4);
     if (attr != cudaSuccess) return attr;
-    k_ta_small_pages<T, DP, NS><<<grid, 128, RING + 65 * a.words * 4, st>>>(a);
+    k_ta_small_pages<T, DP, NS><<<grid, 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
     return cudaGetLastError();
 }
 template <int DP>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr size_t FLOATS = (TF_ROWS + 2 * TF_KT) * (DP + 4) + TF_ROWS * (TF_KT + 4) + 48;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4 + (TF_ROWS + 1) * 32 * 4);
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4 + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 4);
     if (attr != cudaSuccess) return attr;
-    k_ta_f32<DP><<<grid, 128, FLOATS * 4 + (TF_ROWS + 1) * a.words * 4, st>>>(a);
+    k_ta_f32<DP><<<grid, 128, FLOATS * 4 + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
     return cudaGetLastError();
 }
 // The merge is launched while the items run, and waits for them.
@@ -376,14 +387,14 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     a.q_vec = (((uintptr_t)g->d_q | a.q_sb | a.q_st | a.q_sh) & 15) == 0;
     a.out_vec = (((uintptr_t)g->d_out | a.o_sb | a.o_st | a.o_sh) & 15) == 0;
     const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, a.dim, c->page_tokens, (long long)a.max_length + a.T);
-    if (p.grid > 0x7fffffff || (long long)a.B * a.kv_heads * a.T * a.group > 0x7fffffff - 65536) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
-    a.items = (int)p.grid; a.tiles = p.tiles; a.direct = p.direct; a.slots = p.slots; a.min_blocks = p.min_blocks; a.even = p.rows >= 128;
+    if (p.grid > 0x7fffffff || p.slots > 0x7fffffff || (long long)a.B * a.kv_heads * a.T * a.group > 0x7fffffff - 65536) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
+    a.tiles = p.tiles; a.direct = p.direct; a.ctas = p.ctas; a.unit = p.unit; a.min_units = p.min_units;
     const long long need = workspace(p, a.B, c->n_heads, c->head_dim);
     if (need && (!g->d_workspace || (uintptr_t)g->d_workspace % 16 || g->workspace_bytes < need))
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_tree_attention_workspace says, or not 16-byte aligned");
     a.part = (float*)g->d_workspace;
     a.part_ml = (float2*)(a.part + part_floats(p, a.dim));
-    a.where = (int2*)(a.part_ml + p.grid * p.rows);
+    a.where = (int2*)(a.part_ml + p.slots * p.rows);
     const cudaStream_t s = (cudaStream_t)stream;
     const bool wide = a.dim > 64, bf = c->dtype == SPECDEC_DTYPE_BF16;
     cudaError_t rc;

@@ -11,13 +11,14 @@
 
 namespace sd {
 
-// Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's rows.  The keys of a sequence are its
-// length committed tokens and n nodes behind them, in blocks of TA_BLOCK.
+// Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's rows; (K/V head, tile) is a column of work.  The keys of a
+// sequence are its length committed tokens and n nodes behind them, in blocks of `unit` keys (64 or 128).
 //
-// Work: an item is (sequence, split, K/V head, row tile).  direct: a sequence is never split, CTA i is item i.  Otherwise every sequence's blocks are cut into
-// splits of `per` blocks, the same for all, which every CTA works out from the lengths (ta_item); items that share a sequence's keys follow one another.  An item of a
-// sequence with one split writes the output, others write partial results that k_ta_merge joins.
-constexpr int TA_BLOCK = 64, TA_MAX_B = 2048;             // sequences at most where they are split
+// direct: sequences are never cut; CTAs that stay take every gridDim.x-th (sequence, column).
+// Otherwise a column's blocks of all sequences form one line, of which each of its `ctas` CTAs takes an equal stretch (TaWork), so that all CTAs run equally long
+// whatever the lengths are.  A stretch begins and ends inside sequences: a part that is a whole sequence writes the output, other parts write partial results
+// into slots that k_ta_merge joins.  The part of sequence b in the column's CTA c has slot (c + b) * columns + column: along the line either c or b grows.
+constexpr int TA_SMS = 148, TA_BLOCK = 64, TA_MAX_B = 128;            // sequences at most where they are cut
 struct TreeAttn {
     const char* q; char* out; const char* k; const char* v;
     long long q_sb, q_st, q_sh, o_sb, o_st, o_sh, s_page, s_token, s_head;             // bytes
@@ -26,10 +27,10 @@ struct TreeAttn {
     int n_pages, n_seqs, max_pages, page_shift, max_length;
     int T, words, group, kv_heads, dim, B;
     uint32_t group_mul;                                                                // see ta_node
-    int items, tiles, direct, slots, min_blocks, even;                                      // row tiles; CTAs that run at once; blocks a split takes at least
+    int tiles, direct, ctas, unit, min_units;                                               // row tiles; CTAs of a column; keys of a block; blocks of a stretch at least
     float scale;                                                                       // times log2(e)
-    float* part; float2* part_ml;                                                      // [item, row of the tile]: output [dim] and (maximum, sum)
-    int2* where;                                                                       // [b, kv head, tile]: first item, splits
+    float* part; float2* part_ml;                                                      // [slot, row of the tile]: output [dim] and (maximum, sum)
+    int2* where;                                                                       // [b, column]: first slot, parts
     int q_vec, out_vec;                                                                // whether q / out allow 16-byte accesses
 };
 
@@ -47,67 +48,76 @@ __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
     return s;
 }
 
-struct Item { int b, h, tile, split, splits, per; };      // b < 0: none
-// Item number i where no sequence is split.
-__device__ __forceinline__ Item ta_direct(const TreeAttn& a, int i) {
-    const int ht = a.kv_heads * a.tiles, b = i / ht, rest = i - b * ht;
-    return Item{b, rest / a.tiles, rest % a.tiles, 0, 1, 1 << 24};
-}
-// Item number blockIdx.x, for the whole CTA.  scratch: B ints of shared memory, free again behind it.
-__device__ __forceinline__ Item ta_item(const TreeAttn& a, int* scratch) {
-    if (a.direct) return ta_direct(a, blockIdx.x);
-    const int ht = a.kv_heads * a.tiles, unit = blockIdx.x / ht, rest = blockIdx.x - unit * ht;
-    Item it;
-    it.h = rest / a.tiles; it.tile = rest - it.h * a.tiles;
-    __shared__ int found[4];
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) scratch[b] = (ta_keys(a, b).keys + TA_BLOCK - 1) / TA_BLOCK;
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        const int lane = threadIdx.x;
-        long long total = 0;
-        int most = 1;
-        for (int b = lane; b < a.B; b += 32) { total += scratch[b]; most = max(most, scratch[b]); }
+struct Part { int b, h, tile, k_begin, k_end, blocks, whole; long long slot; SeqKeys s; };     // keys [k_begin, k_end) in `blocks` blocks
+struct TaWork {
+    int column, at, b, skip, left, stretch;               // direct: at = number of the next (sequence, column).  Else: the CTA, and what is next on the line: sequence, blocks of it to skip; blocks left, blocks of a stretch
+    // For the whole CTA; units: B ints of shared memory that stay (not direct).
+    __device__ __forceinline__ void begin(const TreeAttn& a, int* units) {
+        const int columns = a.kv_heads * a.tiles;
+        at = blockIdx.x;
+        if (a.direct) return;
+        __shared__ int found[4];
+        column = blockIdx.x % columns; at = blockIdx.x / columns;
+        for (int i = threadIdx.x; i < a.B; i += blockDim.x) units[i] = max(1, (ta_keys(a, i).keys + a.unit - 1) / a.unit);      // (at least 1: rows that see nothing are written too)
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const int lane = threadIdx.x;
+            long long total = 0;
+            for (int i = lane; i < a.B; i += 32) total += units[i];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) { total += __shfl_xor_sync(0xffffffffu, total, o); most = max(most, __shfl_xor_sync(0xffffffffu, most, o)); }
-        int per;
-        if (a.B * ht >= a.slots) {                        // more items than fit at once anyway: long sequences are cut so that none runs on alone
-            per = (int)max((total * ht + 2 * a.slots - 1) / (2 * a.slots), (long long)a.min_blocks * 2);
-        } else {                                          // the shortest splits whose items all run at once: 32 candidates at a time
-            int lo = (int)max((total * ht + a.slots - 1) / a.slots, (long long)a.min_blocks), hi = max(most, lo);
-            while (lo < hi) {
-                const int c = lo + (int)((long long)(hi - lo) * lane / 31);
-                int n = 0;
-                for (int b = 0; b < a.B; ++b) n += max(1, (scratch[b] + c - 1) / c);
-                const unsigned fits = __ballot_sync(0xffffffffu, lane == 31 || n * ht <= a.slots);
-                const int f = __ffs(fits) - 1;
-                const int below = __shfl_sync(0xffffffffu, c, max(f - 1, 0));
-                hi = __shfl_sync(0xffffffffu, c, f);
-                lo = f ? min(below + 1, hi) : hi;
-            }
-            per = hi;
-        }
-        per += per & a.even;                              // whole blocks of 128 keys
-        int b = -1, split = 0, splits = 1, run = 0;       // the sequence in which unit falls
-        for (int b0 = 0; b0 < a.B && b < 0; b0 += 32) {
-            const int n = b0 + lane < a.B ? max(1, (scratch[b0 + lane] + per - 1) / per) : 0;
-            int upto = n;
+            for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            const long long per = max((total + a.ctas - 1) / a.ctas, (long long)a.min_units), start = at * per;
+            long long run = 0;
+            int fb = 0, fskip = 0;
+            for (int i0 = 0; i0 < a.B; i0 += 32) {        // the sequence in which the stretch begins
+                const int n = i0 + lane < a.B ? units[i0 + lane] : 0;
+                int upto = n;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
-            const unsigned m = __ballot_sync(0xffffffffu, run + upto > unit);
-            if (m) {
-                const int f = __ffs(m) - 1;
-                b = b0 + f; splits = __shfl_sync(0xffffffffu, n, f);
-                split = unit - (run + __shfl_sync(0xffffffffu, upto, f) - splits);
+                for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+                const unsigned m = __ballot_sync(0xffffffffu, run + upto > start);
+                if (m) {
+                    const int f = __ffs(m) - 1;
+                    fb = i0 + f;
+                    fskip = (int)(start - (run + __shfl_sync(0xffffffffu, upto - n, f)));
+                    break;
+                }
+                run += __shfl_sync(0xffffffffu, upto, 31);
             }
-            run += __shfl_sync(0xffffffffu, upto, 31);
+            if (lane == 0) { found[0] = fb; found[1] = fskip; found[2] = (int)max(0ll, min(per, total - start)); found[3] = (int)min(per, 0x3fffffffll); }
         }
-        if (lane == 0) { found[0] = b; found[1] = split; found[2] = splits; found[3] = per; }
+        __syncthreads();
+        b = found[0]; skip = found[1]; left = found[2]; stretch = found[3];
     }
-    __syncthreads();
-    it.b = found[0]; it.split = found[1]; it.splits = found[2]; it.per = found[3];
-    if (it.b >= 0 && it.split == 0 && threadIdx.x == 0) a.where[(it.b * a.kv_heads + it.h) * a.tiles + it.tile] = make_int2(blockIdx.x, it.splits);
-    return it;
-}
+    // The next part.  notes: whether this thread tells the merge where a sequence's parts are.
+    __device__ __forceinline__ bool next(const TreeAttn& a, const int* units, Part& p, bool notes = false) {
+        const int columns = a.kv_heads * a.tiles;
+        if (a.direct) {
+            if (at >= a.B * columns) return false;
+            p.b = at / columns; column = at - p.b * columns;
+            at += gridDim.x;
+            p.s = ta_keys(a, p.b);
+            p.k_begin = 0; p.k_end = p.s.keys; p.whole = 1; p.slot = 0;
+            p.blocks = (p.s.keys + a.unit - 1) / a.unit;
+        } else {
+            if (left <= 0) return false;
+            const int n = units[b], take = min(n - skip, left);
+            p.b = b;
+            p.s = ta_keys(a, b);
+            p.k_begin = skip * a.unit; p.k_end = min(p.s.keys, (skip + take) * a.unit);
+            p.blocks = max(0, (p.k_end - p.k_begin + a.unit - 1) / a.unit);
+            p.whole = take == n;
+            p.slot = (long long)(at + b) * columns + column;
+            if (notes && skip == 0) {                     // the rest, if any, lies in the CTAs that follow
+                const int rest = n - take, parts = 1 + (rest + stretch - 1) / stretch;
+                a.where[b * columns + column] = make_int2((int)p.slot, parts);
+            }
+            left -= take;
+            ++b; skip = 0;
+        }
+        p.h = column / a.tiles; p.tile = column - p.h * a.tiles;
+        return true;
+    }
+};
 
 // What a query sees of 32 keys from key k0 on, as bits: committed ones all, nodes by its row of words; base = k0 - length.
 __device__ __forceinline__ uint32_t ta_window(const uint32_t* row, int words, int base) {
@@ -316,15 +326,15 @@ struct TaRows {
             o[i][2] = o[i][2] * fb + w.x * eb; o[i][3] = o[i][3] * fb + w.y * eb;
         }
     }
-    // Rows ra and ra + 8 of a tile of `rows` that begins at query row r0: the output, or the item's partial results.
-    __device__ __forceinline__ void store(const TreeAttn& a, const Item& it, int r0, int ra, int rows) const {
+    // Rows ra and ra + 8 of a tile of `rows` that begins at query row r0: the output, or the part's partial results.
+    __device__ __forceinline__ void store(const TreeAttn& a, const Part& it, int r0, int ra, int rows) const {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = ra + 8 * e, gr = r0 + r;
             const float l = e ? lb : la, inv = l > 0.f || l != l ? 1.f / l : 0.f;
             if (gr >= a.T * a.group) continue;
-            if (it.splits == 1) {
+            if (it.whole) {
                 const int t = ta_node(a, gr);
                 char* p = a.out + it.b * a.o_sb + t * a.o_st + (it.h * a.group + gr - t * a.group) * a.o_sh + (lane & 3) * 4;
 #pragma unroll
@@ -335,7 +345,7 @@ struct TaRows {
                     else { reinterpret_cast<unsigned short*>(p + i * 16)[0] = (unsigned short)x; reinterpret_cast<unsigned short*>(p + i * 16)[1] = (unsigned short)(x >> 16); }
                 }
             } else {
-                const long long slot = (long long)blockIdx.x * rows + r;
+                const long long slot = it.slot * rows + r;
                 float* p = a.part + slot * a.dim + (lane & 3) * 2;
 #pragma unroll
                 for (int i = 0; i < ND; ++i) {

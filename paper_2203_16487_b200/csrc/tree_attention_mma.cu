@@ -1,6 +1,6 @@
 // Attention of drafted trees over the paged cache for 16-bit types and few query rows: keys by TMA, mma.sync (contract: specdec.h, work: tree_attention.cuh).
 //
-// CTA = one item: WM x WK consumer warps and one that loads.  A block of 64 keys is a stage of a ring: one TMA box a page, keys and values each in column halves of
+// CTA = WM x WK consumer warps and one that loads.  A block of 64 keys is a stage of a ring: one TMA box a page, keys and values each in column halves of
 // 128 swizzled bytes a row.  Warp (wm, wk) takes 16 rows and every WK-th block: scores (m16n8k16, fp32), running maximum and sum in registers, probabilities (rounded
 // to the type; the sum keeps the unrounded ones) straight from the score registers into the second product.  The WK groups' partial outputs
 // meet in shared memory at the end.
@@ -12,17 +12,18 @@
 namespace sd {
 namespace {
 
-// NS is a multiple of WK: a stage always serves the same group, which so sees every one of its phases.
+// Group wk has the stages wk, wk + WK, ... to itself and so waits for every phase of their barriers.
 template <typename T, int DP, int WM, int WK, int NS>
 __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(const __grid_constant__ CUtensorMap tm, TreeAttn a) {
     static_assert(NS % WK == 0, "a stage serves one group");
-    constexpr int TM_WARPS = WM * WK, ROWS = 16 * WM, KT = TA_BLOCK, HALVES = DP / 64;
+    constexpr int TM_WARPS = WM * WK, NG = NS / WK, ROWS = 16 * WM, KT = TA_BLOCK, HALVES = DP / 64;
     constexpr int SIDE = KT * DP * 2, STAGE = 2 * SIDE;
     extern __shared__ __align__(1024) char ta_smem[];
     __shared__ __align__(8) uint64_t bars[2 * NS];
     __shared__ int abort_flag;
     char* ring = ta_smem + (1024 - (smem_u32(ta_smem) & 1023)) % 1024;
-    uint32_t* any = (uint32_t*)(ring + NS * STAGE);
+    int* units = (int*)(ring + NS * STAGE);               // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : (a.B + 1) / 2 * 2));
     uint32_t* mask = any + (a.words + 1) / 2 * 2;         // (8-byte aligned, as the partial results behind it are)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
@@ -32,39 +33,30 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
-    const Item first = ta_item(a, (int*)ring);
-    if (first.b < 0) return;
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ta_item's use of the ring, ahead of the boxes
+    TaWork work;
+    work.begin(a, units);
     __syncthreads();
-    int done = 0;                                         // blocks of the items before
-    auto range = [&](const Item& it, const SeqKeys& s, int& k_begin, int& k_end) {
-        k_begin = it.split * it.per * KT;
-        k_end = (int)min((long long)(it.split + 1) * it.per * KT, (long long)s.keys);
-        return max(0, (k_end - k_begin + KT - 1) / KT);
-    };
 
-    if (warp == TM_WARPS) {                               // loads, running ahead into the next items
+    if (warp == TM_WARPS) {                               // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
-        Item it = first;
-        SeqKeys s = ta_keys(a, it.b);
-        for (int item = blockIdx.x; item < a.items; item += gridDim.x) {
-            int k_begin, k_end;
-            const int blocks = range(it, s, k_begin, k_end);
-            const int* table = a.table + (long long)s.seq * a.max_pages;
+        int count = 0;                                    // lane g: blocks that group g had in the parts before
+        Part it, ahead;
+        for (bool more = work.next(a, units, ahead); more;) {
+            it = ahead;
+            const int* table = a.table + (long long)it.s.seq * a.max_pages;
             auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
-                const int key = k_begin + j * KT + lane * box, i = key >> a.page_shift;
+                const int key = it.k_begin + j * KT + lane * box, i = key >> a.page_shift;
                 int p = -1;
-                if (lane < n_pages && key < k_end && i < a.max_pages) p = table[i];
+                if (lane < n_pages && key < it.k_end && i < a.max_pages) p = table[i];
                 return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
             };
-            int p = blocks ? page_of(0) : 0;
-            const int h = it.h;
-            if (item + gridDim.x < a.items) { it = ta_direct(a, item + gridDim.x); s = ta_keys(a, it.b); }
-            for (int j = 0; j < blocks; ++j) {
-                const int n = done + j, st = n % NS, key = k_begin + j * KT + lane * box, cur = p;
-                if (j + 1 < blocks) p = page_of(j + 1);
-                if (n >= NS && !mbar_wait_warp(empty + st * 8, (n / NS - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
-                const bool mine = lane < n_pages && key < k_end;
+            int p = it.blocks ? page_of(0) : 0;
+            more = work.next(a, units, ahead);
+            for (int j = 0; j < it.blocks; ++j) {
+                const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), key = it.k_begin + j * KT + lane * box, cur = p;
+                if (j + 1 < it.blocks) p = page_of(j + 1);
+                if (n >= NG && !mbar_wait_warp(empty + st * 8, (n / NG - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
+                const bool mine = lane < n_pages && key < it.k_end;
                 const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
                 if (lane == 0) mbar_expect_tx(full + st * 8, boxes * box * 128 * HALVES * 2);
                 __syncwarp();
@@ -74,25 +66,23 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
                     for (int side = 0; side < 2; ++side)
 #pragma unroll
                         for (int hf = 0; hf < HALVES; ++hf)
-                            ta_box(d + side * SIDE + hf * KT * 128, &tm, hf * 64, h, key & (page - 1), cur, side, full + st * 8);
+                            ta_box(d + side * SIDE + hf * KT * 128, &tm, hf * 64, it.h, key & (page - 1), cur, side, full + st * 8);
                 }
             }
-            if (abort_flag) break;
-            done += (blocks + WK - 1) / WK * WK;          // the next item's first block is group 0's again
+            count += (it.blocks - lane + WK - 1) / WK;    // (lanes below WK)
         }
         return;
     }
 
     const int wm = warp % WM, wk = warp / WM, all_rows = a.T * a.group;
     auto consumers = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * TM_WARPS) : "memory"); };
-    Item next = first;
-    SeqKeys next_s = ta_keys(a, next.b);
-    for (int item = blockIdx.x; item < a.items; item += gridDim.x) {
-        const Item it = next;
-        const SeqKeys s = next_s;
-        if (item + gridDim.x < a.items) { next = ta_direct(a, item + gridDim.x); next_s = ta_keys(a, next.b); }
-        int k_begin, k_end;
-        const int blocks = range(it, s, k_begin, k_end), r0 = it.tile * ROWS, t0 = ta_node(a, r0);
+    int count = 0;                                        // this group's blocks so far
+    Part it, ahead;
+    for (bool more = work.next(a, units, ahead, tid == 0); more;) {
+        it = ahead;
+        more = work.next(a, units, ahead, tid == 0);
+        const SeqKeys& s = it.s;
+        const int r0 = it.tile * ROWS, t0 = ta_node(a, r0);
         const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
         const int ga = r0 + ra, gb = r0 + rb, ta = ta_node(a, ga), tb = ta_node(a, gb);
         const bool live_a = ga < all_rows && ta < s.nodes, live_b = gb < all_rows && tb < s.nodes;
@@ -118,9 +108,9 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         const uint32_t* mask_b = live_b ? mask + (tb - t0) * a.words : nullptr;
         TaRows<T, DP> rows;
         rows.clear();
-        for (int j = wk; j < blocks; j += WK) {
-            const int n = done + j, st = n % NS, k0 = k_begin + j * KT;
-            if (!mbar_wait_warp(full + st * 8, (n / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
+        for (int j = wk; j < it.blocks; j += WK, ++count) {
+            const int st = wk + WK * (count % NG), k0 = it.k_begin + j * KT;
+            if (!mbar_wait_warp(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
             const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
             const bool tail = k0 + KT > s.len;            // nodes, or what is behind the last key
             if (tail) {                                   // values that no query sees: whatever is in them is multiplied by 0
@@ -135,7 +125,6 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + st * 8);
         }
-        done += (blocks + WK - 1) / WK * WK;
         rows.finish(live_a, live_b);
         if constexpr (WK > 1) {                           // the groups' results meet in the first group
             constexpr int RP = TaRows<T, DP>::RP;
@@ -156,7 +145,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
 template <typename T, int DP, int WM, int WK, int NS>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int ROWS = 16 * WM, RING = NS * 2 * TA_BLOCK * DP * 2, RED = (WK - 1) * ROWS * ((DP + 8) * 4 + 8);
-    constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4;
+    constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4 + TA_MAX_B * 4;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tma<T, DP, WM, WK, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
     static const int per_sm = [] {
@@ -164,8 +153,8 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_ta_tma<T, DP, WM, WK, NS>, 32 * (WM * WK + 1), MOST);
         return n < 1 ? 1 : n;
     }();
-    const int most = a.direct ? per_sm * 148 : grid;      // whole sequences: CTAs that stay, each with every gridDim.x-th item
-    k_ta_tma<T, DP, WM, WK, NS><<<grid < most ? grid : most, 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4, st>>>(tm, a);
+    const int most = a.direct ? per_sm * TA_SMS : grid;   // whole sequences: as many CTAs as run at once
+    k_ta_tma<T, DP, WM, WK, NS><<<grid < most ? grid : most, 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B + 1) * 4, st>>>(tm, a);
     return cudaGetLastError();
 }
 template <typename T>

@@ -1,6 +1,6 @@
 // Attention of drafted trees over the paged cache for 16-bit types and many query rows: tcgen05 (contract: specdec.h, work: tree_attention.cuh).
 //
-// CTA = one item, one CTA an SM.  A block is 128 keys; the scores of 128 rows against it are one accumulator in tensor memory (a row a lane), from which the
+// One CTA an SM.  A block is 128 keys; the scores of 128 rows against it are one accumulator in tensor memory (a row a lane), from which the
 // row's thread takes maximum and exponentials; the probabilities go back into the same columns as 16-bit pairs and are the second product's A operand, the values
 // its B operand as they lie ([key, column], N-major).  Two groups of four softmax warps keep the tensor pipe busy in turn:
 //   TILES = 2: the groups have 128 rows each and share the blocks of a 256-row tile.
@@ -44,6 +44,22 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
+// Two fp32 at a time.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <int DP, int TILES> struct TcAttn {
@@ -62,10 +78,12 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     __shared__ __align__(8) uint64_t bars[4 * NS + 6];
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_base;
+    __shared__ float2 other[TILES == 1 ? TC_ROWS : 1];    // maximum and sum of the second group's rows
     char* qs = tc_smem + (1024 - (smem_u32(tc_smem) & 1023)) % 1024;
     char* kring = qs + TILES * Cfg::Q;
     char* vring = kring + NS * SIDE;
-    uint32_t* any = (uint32_t*)(vring + NS * SIDE);
+    int* units = (int*)(vring + NS * SIDE);               // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t kfull = smem_u32(bars), kempty = kfull + NS * 8, vfull = kempty + NS * 8, vempty = vfull + NS * 8;
@@ -77,53 +95,102 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
-    const Item it = ta_item(a, (int*)kring);
-    if (it.b < 0) return;
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // ta_item's use of the ring, ahead of the boxes
+    TaWork work;
+    work.begin(a, units);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;                      // columns: scores 0, scores 1 (128 each), outputs 0, 1 (DP each)
-    const SeqKeys s = ta_keys(a, it.b);
-    const int k_begin = it.split * it.per * TA_BLOCK, k_end = (int)min((long long)(it.split + 1) * it.per * TA_BLOCK, (long long)s.keys);
-    const int blocks = max(0, (k_end - k_begin + KT - 1) / KT);
-    auto steps = [&](int g) { return TILES == 2 ? blocks : (blocks + 1 - g) / 2; };    // of group g; its i-th is block_of(g, i)
-    auto block_of = [&](int g, int i) { return TILES == 2 ? i : 2 * i + g; };
+    // steps of group g in a part of `blocks` blocks; its i-th is block_of(g, i)
+    auto steps = [](int blocks, int g) { return TILES == 2 ? blocks : (blocks + 1 - g) / 2; };
+    auto block_of = [](int g, int i) { return TILES == 2 ? i : 2 * i + g; };
+    auto wait = [&](uint32_t bar, int n) { return mbar_wait_warp(bar, n & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT); };     // for its completion number n
+    Part it;
+    int done = 0;                                         // blocks of the parts before: block j is in stage (done + j) % NS
+    bool ok = true;
 
-    if (warp == 0) {                                      // loads
+    if (warp == 0) {                                      // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, TA_BLOCK), n_boxes = KT / box;
-        const int* table = a.table + (long long)s.seq * a.max_pages;
-        auto page_of = [&](int j) {                       // this lane's page of block j: out of range where there is none
-            const int key = k_begin + j * KT + lane * box, i = key >> a.page_shift;
-            int p = -1;
-            if (lane < n_boxes && key < k_end && i < a.max_pages) p = table[i];
-            return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
-        };
-        int p = blocks ? page_of(0) : 0;
-        bool ok = true;
-        for (int j = 0; j < blocks && ok; ++j) {
-            const int st = j % NS, key = k_begin + j * KT + lane * box, cur = p;
-            if (j + 1 < blocks) p = page_of(j + 1);
-            const bool mine = lane < n_boxes && key < k_end;
-            const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
+        for (; ok && work.next(a, units, it); done += it.blocks) {
+            const int* table = a.table + (long long)it.s.seq * a.max_pages;
+            auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
+                const int key = it.k_begin + j * KT + lane * box, i = key >> a.page_shift;
+                int p = -1;
+                if (lane < n_boxes && key < it.k_end && i < a.max_pages) p = table[i];
+                return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
+            };
+            int p = it.blocks ? page_of(0) : 0;
+            for (int j = 0; j < it.blocks && ok; ++j) {
+                const int n = done + j, st = n % NS, key = it.k_begin + j * KT + lane * box, cur = p;
+                if (j + 1 < it.blocks) p = page_of(j + 1);
+                const bool mine = lane < n_boxes && key < it.k_end;
+                const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
 #pragma unroll
-            for (int side = 0; side < 2 && ok; ++side) {
-                const uint32_t full = (side ? vfull : kfull) + st * 8, empty = (side ? vempty : kempty) + st * 8;
-                if (j >= NS) ok = mbar_wait_warp(empty, (j / NS - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
-                if (!ok) break;
-                if (lane == 0) mbar_expect_tx(full, boxes * box * 128 * HALVES);
-                __syncwarp();
-                if (mine) {
-                    const uint32_t d = smem_u32((side ? vring : kring) + st * SIDE) + lane * box * 128;
+                for (int side = 0; side < 2; ++side) {
+                    const uint32_t full = (side ? vfull : kfull) + st * 8, empty = (side ? vempty : kempty) + st * 8;
+                    if (n >= NS) ok = ok && wait(empty, n / NS - 1);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(full, boxes * box * 128 * HALVES);
+                    __syncwarp();
+                    if (mine) {
+                        const uint32_t d = smem_u32((side ? vring : kring) + st * SIDE) + lane * box * 128;
 #pragma unroll
-                    for (int hf = 0; hf < HALVES; ++hf) ta_box(d + hf * KT * 128, &tm, hf * 64, it.h, key & (page - 1), cur, side, full);
+                        for (int hf = 0; hf < HALVES; ++hf) ta_box(d + hf * KT * 128, &tm, hf * 64, it.h, key & (page - 1), cur, side, full);
+                    }
                 }
             }
         }
-    } else if (warp >= 4) {                               // the queries, and what they see
-        const int t = tid - 128, r0 = it.tile * ROWS, all_rows = a.T * a.group;
-        for (int i = t; i < ROWS * (DP / 8); i += 256) {
+    } else if (warp == 1) {                               // products
+        int taken[2] = {0, 0};                            // steps of the groups in the parts before
+        for (; work.next(a, units, it); done += it.blocks, taken[0] += steps(it.blocks, 0), taken[1] += steps(it.blocks, 1)) {
+            asm volatile("bar.sync 2, 288;" ::: "memory");            // the queries are there, the last outputs have been read
+            tc_fence_after();
+            auto second = [&](int g, int i) {             // output += probabilities x values
+                const int n = done + block_of(g, i), st = n % NS;
+                ok = ok && wait(pready + g * 8, taken[g] + i) && wait(vfull + st * 8, n / NS);
+                if (!ok) return;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t v = umma_desc_n_sw128(smem_u32(vring + st * SIDE), KT * 128);
+#pragma unroll
+                    for (int kk = 0; kk < KT / 16; ++kk)  // 16 keys: 2048 bytes of values, 8 columns of probabilities
+                        umma_ts(tmem + 256 + g * DP, tmem + g * 128 + kk * 8, v + kk * 128, IDESC_O, i || kk ? 1u : 0u);
+                    if (TILES == 1 || g == 1) umma_commit(vempty + st * 8);
+                    if (i + 1 == steps(it.blocks, g)) umma_commit(ofin + g * 8);
+                }
+            };
+            const int most = steps(it.blocks, 0);
+            for (int i = 0; i <= most && ok; ++i)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    if (!ok) break;
+                    if (i > 0 && i <= steps(it.blocks, g)) second(g, i - 1);
+                    if (!ok || i >= steps(it.blocks, g)) continue;
+                    const int n = done + block_of(g, i), st = n % NS;
+                    ok = wait(kfull + st * 8, n / NS);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < DP / 16; ++kk) {
+                            const uint64_t q = umma_desc_k_sw128(smem_u32(qs + (TILES == 2 ? g : 0) * Cfg::Q) + (kk / 4) * TC_ROWS * 128) + (kk % 4) * 2;
+                            const uint64_t k = umma_desc_k_sw128(smem_u32(kring + st * SIDE) + (kk / 4) * KT * 128) + (kk % 4) * 2;
+                            umma_bf16(tmem + g * 128, q, k, IDESC_S, kk ? 1u : 0u);
+                        }
+                        umma_commit(sfull + g * 8);
+                        if (TILES == 1 || g == 1) umma_commit(kempty + st * 8);
+                    }
+                }
+        }
+    } else if (warp >= 4) {                               // softmax: one row a thread
+        const int g = (warp - 4) >> 2, t = tid - 128, all_rows = a.T * a.group;
+        int taken = 0, outputs = 0;                       // this group's steps and outputs in the parts before
+        auto softmax_warps = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+        while (work.next(a, units, it, t == 0)) {
+        const SeqKeys& s = it.s;
+        const int r0 = it.tile * ROWS;
+        for (int i = t; i < ROWS * (DP / 8); i += 256) {  // the queries
             const int r = i / (DP / 8), c = i % (DP / 8), gr = r0 + r, node = ta_node(a, gr);
             uint4 x = make_uint4(0, 0, 0, 0);
             if (gr < all_rows && node < s.nodes && c * 8 < a.dim) {
@@ -137,91 +204,53 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
             *reinterpret_cast<uint4*>(qs + (r / TC_ROWS) * Cfg::Q + (c >> 3) * TC_ROWS * 128 + (r % TC_ROWS) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        // (the mask rows: by these 256 threads, which count from 128)
-        auto sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-        for (int w = t; w < a.words; w += 256) any[w] = 0;
-        sync();
-        const int t0 = ta_node(a, r0), t1 = min(ta_node(a, min(r0 + ROWS, all_rows) - 1), a.T - 1);
-        for (int i = t; i < (t1 - t0 + 1) * a.words; i += 256) {
-            const int node = t0 + i / a.words, w = i % a.words, left = s.nodes - w * 32;
+        for (int w = t; w < a.words; w += 256) any[w] = 0;            // what they see (as ta_load_masks, by the threads from 128 on)
+        softmax_warps();
+        const int t0n = ta_node(a, r0), t1n = min(ta_node(a, min(r0 + ROWS, all_rows) - 1), a.T - 1);
+        for (int i = t; i < (t1n - t0n + 1) * a.words; i += 256) {
+            const int node = t0n + i / a.words, w = i % a.words, left = s.nodes - w * 32;
             uint32_t m = node < s.nodes ? a.mask[it.b * a.mask_sb + (long long)node * a.words + w] : 0u;
             if (left < 32) m &= left <= 0 ? 0u : (1u << left) - 1u;
             mask[i] = m;
             if (m) atomicOr(any + w, m);
         }
-    }
-    // the queries are there (the loads run meanwhile)
-    if (warp == 1 || warp >= 4) asm volatile("bar.sync 2, 288;" ::: "memory");
+        tc_fence_before();
+        asm volatile("bar.sync 2, 288;" ::: "memory");
 
-    if (warp == 1) {                                      // products
-        bool ok = true;
-        const int most = max(steps(0), steps(1));
-        auto second = [&](int g, int i) {                 // output += probabilities x values
-            const int j = block_of(g, i), st = j % NS;
-            ok = ok && mbar_wait_warp(pready + g * 8, i & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT) &&
-                 mbar_wait_warp(vfull + st * 8, (j / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
-            if (!ok) return;
-            tc_fence_after();
-            if (elect_one()) {
-                const uint64_t v = umma_desc_n_sw128(smem_u32(vring + st * SIDE), KT * 128);
-#pragma unroll
-                for (int kk = 0; kk < KT / 16; ++kk)      // 16 keys: 2048 bytes of values, 8 columns of probabilities
-                    umma_ts(tmem + 256 + g * DP, tmem + g * 128 + kk * 8, v + kk * 128, IDESC_O, i || kk ? 1u : 0u);
-                if (TILES == 1 || g == 1) umma_commit(vempty + st * 8);
-                if (i + 1 == steps(g)) umma_commit(ofin + g * 8);
-            }
-        };
-        for (int i = 0; i <= most && ok; ++i)
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                if (!ok) break;
-                if (i > 0 && i <= steps(g)) second(g, i - 1);
-                if (!ok || i >= steps(g)) continue;
-                const int j = block_of(g, i), st = j % NS;
-                ok = mbar_wait_warp(kfull + st * 8, (j / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk) {
-                        const uint64_t q = umma_desc_k_sw128(smem_u32(qs + (TILES == 2 ? g : 0) * Cfg::Q) + (kk / 4) * TC_ROWS * 128) + (kk % 4) * 2;
-                        const uint64_t k = umma_desc_k_sw128(smem_u32(kring + st * SIDE) + (kk / 4) * KT * 128) + (kk % 4) * 2;
-                        umma_bf16(tmem + g * 128, q, k, IDESC_S, kk ? 1u : 0u);
-                    }
-                    umma_commit(sfull + g * 8);
-                    if (TILES == 1 || g == 1) umma_commit(kempty + st * 8);
-                }
-            }
-    } else if (warp >= 4) {                               // softmax: one row a thread
-        const int g = (warp - 4) >> 2, r = (TILES == 2 ? g * TC_ROWS : 0) + (warp & 3) * 32 + lane, r0 = it.tile * ROWS, gr = r0 + r;
-        const int node = ta_node(a, gr), n = steps(g);
+        const int r = (TILES == 2 ? g * TC_ROWS : 0) + (warp & 3) * 32 + lane, gr = r0 + r, node = ta_node(a, gr), n = steps(it.blocks, g);
         const bool live = gr < a.T * a.group && node < s.nodes;
-        const uint32_t* row = mask + (live ? (node - ta_node(a, r0)) * a.words : 0);
+        const uint32_t* row = mask + (live ? (node - t0n) * a.words : 0);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;                  // this warp's lanes: 32 (warp % 4) in bits 16..31
         const uint32_t ts = tmem + g * 128 + lanes, to = tmem + 256 + g * DP + lanes;
         float m = -INFINITY, l = 0.f;
-        bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int j = block_of(g, i), k0 = k_begin + j * KT;
-            ok = mbar_wait_warp(sfull + g * 8, i & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
+            const int j = block_of(g, i), k0 = it.k_begin + j * KT;
+            ok = ok && wait(sfull + g * 8, taken + i);
             if (!ok) break;
             tc_fence_after();
             const bool tail = k0 + KT > s.len;
-            float top = -INFINITY;
+            // the row's scores, 32 at a time and twice, for the maximum and for the exponentials; the next 32 are on their way meanwhile
+            uint32_t x[2][32];
+            auto hide = [&](uint32_t* x, int c) {
+                const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = w >> e & 1 ? x[e] : 0xff800000u;
+            };
+            float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+            tmem_ld_issue<32>(ts, x[0]);
 #pragma unroll
             for (int c = 0; c < KT / 32; ++c) {
-                float x[32];
-                tmem_ld32(ts + c * 32, x);
-                if (tail) {
-                    const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
+                tmem_ld_done<32>(x[c & 1]);
+                tmem_ld_issue<32>(ts + (c + 1) % (KT / 32) * 32, x[(c + 1) & 1]);
+                if (tail) hide(x[c & 1], c);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = w >> e & 1 ? x[e] : -INFINITY;
+                for (int e = 0; e < 32; e += 8) {
+                    auto y = [&](int q) { return __uint_as_float(x[c & 1][e + q]); };
+                    t0 = fmaxf(t0, fmaxf(y(0), y(1))); t1 = fmaxf(t1, fmaxf(y(2), y(3)));
+                    t2 = fmaxf(t2, fmaxf(y(4), y(5))); t3 = fmaxf(t3, fmaxf(y(6), y(7)));
                 }
-                float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) { t0 = fmaxf(t0, fmaxf(x[e], x[e + 1])); t1 = fmaxf(t1, fmaxf(x[e + 2], x[e + 3])); }
-                top = fmaxf(top, fmaxf(t0, t1));
             }
+            float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
             top *= a.scale;
             const bool grow = top > (m == -INFINITY ? m : m + 8.f);
             if (__any_sync(0xffffffffu, grow)) {
@@ -231,40 +260,39 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                 if (i > 0) {
 #pragma unroll
                     for (int c = 0; c < DP / 16; ++c) {
-                        float x[16];
                         uint32_t y[16];
-                        tmem_ld<16>(to + c * 16, x);
+                        tmem_ld_issue<16>(to + c * 16, y);
+                        tmem_ld_done<16>(y);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(f == 0.f ? 0.f : x[e] * f);
+                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[e]) * f);
                         tmem_st16(to + c * 16, y);
                     }
                     tmem_st_wait();
                 }
             }
             const float z = m == -INFINITY ? 0.f : m;
-            float l0 = 0.f, l1 = 0.f;
+            uint64_t sum[2] = {0, 0};                     // two pairs of fp32
+            const uint64_t scale2 = pair2(a.scale, a.scale), z2 = pair2(-z, -z);
 #pragma unroll
             for (int c = 0; c < KT / 32; ++c) {
-                float x[32];
                 uint32_t y[16];
-                tmem_ld32(ts + c * 32, x);
-                if (tail) {
-                    const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
+                tmem_ld_done<32>(x[c & 1]);
+                if (c + 1 < KT / 32) tmem_ld_issue<32>(ts + (c + 1) * 32, x[(c + 1) & 1]);
+                if (tail) hide(x[c & 1], c);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = w >> e & 1 ? x[e] : -INFINITY;
+                for (int e = 0; e < 16; ++e) {
+                    const uint64_t d = fma2(pair2(__uint_as_float(x[c & 1][2 * e]), __uint_as_float(x[c & 1][2 * e + 1])), scale2, z2);
+                    const float u = ta_exp2(__uint_as_float((uint32_t)d)), v = ta_exp2(__uint_as_float((uint32_t)(d >> 32)));
+                    sum[e & 1] = add2(sum[e & 1], pair2(u, v));
+                    y[e] = Half<T>::pack(u, v);
                 }
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float u = ta_exp2(fmaf(x[e], a.scale, -z)), v = ta_exp2(fmaf(x[e + 1], a.scale, -z));
-                    l0 += u; l1 += v;
-                    y[e / 2] = Half<T>::pack(u, v);
-                }
-                tmem_st16(ts + c * 16, y);                // over scores that have been read
+                tmem_st16(ts + c * 16, y);                // over scores that have been read: columns 16 c .., the next 32 (c + 1) ..
             }
-            l += l0 + l1;
+            const uint64_t both = add2(sum[0], sum[1]);
+            l += __uint_as_float((uint32_t)both) + __uint_as_float((uint32_t)(both >> 32));
             if (tail && (TILES == 1 || g == 0)) {         // values that no query sees: whatever is in them is multiplied by 0
-                const int st = j % NS;
-                ok = mbar_wait_warp(vfull + st * 8, (j / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
+                const int st = (done + j) % NS;
+                ok = wait(vfull + st * 8, (done + j) / NS);
                 if (!ok) break;
                 // (each of the group's warps a quarter of the rows)
                 const uint32_t seen = ta_window(any, a.words, k0 + (warp & 3) * 32 - s.len);
@@ -279,28 +307,19 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(pready + g * 8);
         }
-        if (ok && n) ok = mbar_wait_warp(ofin + g * 8, 0, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
+        if (ok && n) ok = wait(ofin + g * 8, outputs++);
+        taken += n;
+        done += it.blocks;
         tc_fence_after();
         if (!live) { m = -INFINITY; l = 0.f; }
         if (l == 0.f) m = -INFINITY;
         float f = l == 0.f ? 0.f : 1.f, f1 = 0.f;         // shares of this group's output and, TILES = 1, of the other's
-        const float* red = reinterpret_cast<const float*>(kring) + (warp & 3) * 32 + lane;             // [DP + 2][128]: columns, maximum, sum
-        if constexpr (TILES == 1) {                       // the second group's results through the ring, once the products have read it
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (g == 1) {
-                float* to_red = const_cast<float*>(red);
-#pragma unroll
-                for (int c = 0; c < DP / 32; ++c) {
-                    float x[32];
-                    if (n) tmem_ld32(to + c * 32, x);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) to_red[(c * 32 + e) * 128] = n && l != 0.f ? x[e] : 0.f;
-                }
-                to_red[DP * 128] = m; to_red[(DP + 1) * 128] = l;
-            }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+        const int rr = (warp & 3) * 32 + lane, n1 = steps(it.blocks, 1);
+        if constexpr (TILES == 1) {                       // both outputs are in this lane's tensor memory: the first group adds them up
+            if (g == 1) other[rr] = make_float2(m, l);
+            softmax_warps();
             if (g == 0) {
-                const float m1 = red[DP * 128], l1 = red[(DP + 1) * 128], mm = fmaxf(m, m1), z = mm == -INFINITY ? 0.f : mm;
+                const float m1 = other[rr].x, l1 = other[rr].y, mm = fmaxf(m, m1), z = mm == -INFINITY ? 0.f : mm;
                 f = ta_exp2(m - z); f1 = ta_exp2(m1 - z);
                 l = l * f + l1 * f1;
                 m = mm;
@@ -308,21 +327,25 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         }
         if (TILES == 2 || g == 0) {
             const bool real = gr < a.T * a.group;
-            const float inv = it.splits > 1 ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
+            const float inv = !it.whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
             char* p = a.out + it.b * a.o_sb + node * a.o_st + (it.h * a.group + gr - node * a.group) * a.o_sh;
-            const long long slot = (long long)blockIdx.x * ROWS + r;
+            const long long slot = it.slot * ROWS + r;
 #pragma unroll
             for (int c = 0; c < DP / 32; ++c) {
                 float x[32];
                 if (n) tmem_ld32(to + c * 32, x);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    float y = n && f != 0.f ? x[e] * f : 0.f;
-                    if constexpr (TILES == 1) y = fmaf(red[(c * 32 + e) * 128], f1, y);
-                    x[e] = y * inv;
+                for (int e = 0; e < 32; ++e) x[e] = n && f != 0.f ? x[e] * f : 0.f;
+                if (TILES == 1 && n1) {
+                    float x1[32];
+                    tmem_ld32(to + DP + c * 32, x1);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e] = f1 != 0.f ? fmaf(x1[e], f1, x[e]) : x[e];
                 }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] *= inv;
                 if (!real) continue;
-                if (it.splits == 1) {
+                if (it.whole) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         if (c * 32 + e >= a.dim) break;
@@ -340,7 +363,9 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                         if (c * 32 + e < a.dim) *reinterpret_cast<float4*>(a.part + slot * a.dim + c * 32 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 }
             }
-            if (real && it.splits > 1) a.part_ml[slot] = make_float2(m, l);
+            if (real && !it.whole) a.part_ml[slot] = make_float2(m, l);
+        }
+        softmax_warps();                                  // queries and masks may be overwritten
         }
     }
     tc_fence_before();
@@ -350,11 +375,11 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
 
 template <typename T, int DP, int TILES>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr int BYTES = TcAttn<DP, TILES>::BYTES + 1024, MOST = BYTES + (TILES * TC_ROWS + 1) * 32 * 4;
-    static_assert(MOST <= 232448 - 1024, "shared memory of an SM");
+    constexpr int BYTES = TcAttn<DP, TILES>::BYTES + 1024, MOST = BYTES + (TILES * TC_ROWS + 1) * 32 * 4 + TA_MAX_B * 4;
+    static_assert(MOST <= 232448 - (TILES == 1 ? 1536 : 512), "shared memory of an SM");
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tc<T, DP, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
-    k_ta_tc<T, DP, TILES><<<grid, 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4, st>>>(tm, a);
+    k_ta_tc<T, DP, TILES><<<grid < TA_SMS || !a.direct ? grid : TA_SMS, 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(tm, a);
     return cudaGetLastError();
 }
 template <typename T>

@@ -228,6 +228,28 @@ def test_attention_split_keys(dtype, T, H, Hkv, D, lens):
     check_attention(got, want, mag, dtype, 3100)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("T,H,Hkv,D,n", [(2, 12, 12, 64, 41), (2, 12, 12, 128, 41), (20, 12, 12, 64, 41), (3, 48, 4, 64, 60), (20, 12, 12, 128, 30), (66, 7, 7, 64, 30), (130, 6, 3, 64, 30),
+                                         (66, 7, 7, 128, 30)])
+def test_attention_many_short_sequences(dtype, T, H, Hkv, D, n):
+    """More sequences and heads than CTAs that run at once, of every number of key blocks: CTAs that take several."""
+    if T > 30 and dtype == torch.float32:
+        T = 30
+    lens = [(i * 37) % 331 for i in range(n)]
+    got, want, mag, _ = attention_case(dtype, lens, T, H, Hkv, D, 16, seed=T, one_mask=True)
+    check_attention(got, want, mag, dtype, 500)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,Hkv,D", [(1, 4, 2, 64), (9, 2, 2, 128), (12, 4, 2, 64), (40, 2, 1, 64), (100, 2, 2, 128), (90, 3, 1, 64)])
+def test_attention_uneven_long_sequences(dtype, T, H, Hkv, D):
+    """Sequences of one to thousands of keys: CTAs whose stretch of keys begins and ends inside sequences, or holds several."""
+    if T > 12 and dtype == torch.float32:
+        T = 3
+    got, want, mag, _ = attention_case(dtype, [5000, 0, 3, 1900, 64, 65, 0, 700], T, H, Hkv, D, 16, seed=T, one_mask=True, nodes=[T, T, 1, T, 0, T, 0, T])
+    check_attention(got, want, mag, dtype, 5100)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("kw", [dict(nodes=[9, 0, 3]), dict(one_mask=True), dict(strided=True), dict(heads_first=True), dict(layer=2), dict(nodes=[1, 9, 8], strided=True, heads_first=True)])
 def test_attention_ragged_shared_strided(dtype, kw):

@@ -46,19 +46,14 @@ def accept(parents, tokens, sampled, n):
 def attention(q, k, v, see, scale):
     """q [T, H, D], k, v [S, Hkv, D], see [T, S]: (out, sum of p |v|, in float64)."""
     T, H, D = q.shape
-    g = H // k.shape[1]
-    out, mag = torch.zeros(T, H, D, dtype=torch.float64), torch.zeros(T, H, D, dtype=torch.float64)
-    for t in range(T):
-        on = see[t].nonzero()[:, 0]
-        if not len(on):
-            continue
-        for h in range(H):
-            kk, vv = k[on, h // g].double(), v[on, h // g].double()
-            s = (kk @ q[t, h].double()) * scale
-            p = torch.exp(s - s.max())
-            p /= p.sum()
-            out[t, h], mag[t, h] = p @ vv, p @ vv.abs()
-    return out, mag
+    kk, vv = (x.double().repeat_interleave(H // k.shape[1], 1).transpose(0, 1) for x in (k, v))      # [H, S, D]
+    s = (q.double().transpose(0, 1) @ kk.transpose(1, 2)) * scale
+    s = s.masked_fill(~see, -math.inf)
+    top = s.max(-1, keepdim=True).values if s.shape[2] else s.new_zeros(H, T, 1)
+    p = torch.exp(s - torch.where(top > -math.inf, top, torch.zeros_like(top)))
+    total = p.sum(-1, keepdim=True)
+    p = p / torch.where(total > 0, total, torch.ones_like(total))
+    return (p @ vv).transpose(0, 1), (p @ vv.abs()).transpose(0, 1)
 
 
 def sample_row(logits, u, temperature, top_k, top_p, min_p):
