@@ -3,7 +3,6 @@
 // out = sum_j p_j v_j over the keys a query sees, p = softmax(scale q . k).  One pass over the keys with the running maximum m and sum l of
 // 2^(s - m): s in units of log2, sums and outputs in fp32, rescaled where m grows.  All query heads of a K/V head share its keys, so a row tile
 // mixes nodes and heads; few rows: the keys of a sequence are split over CTAs, whose partial outputs k_ta_merge joins.
-#include <cstdlib>
 #include "tree_attention.cuh"
 
 namespace sd {
@@ -17,14 +16,14 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     constexpr int ROWS = 64, KT = TA_BLOCK, PITCH = DP * 2, PIECES = DP / 8, STAGE = 2 * KT * PITCH;
     extern __shared__ __align__(128) char sm[];
     char* ring = sm;                                      // [NS][K, V][KT][PITCH]; at first the queries
-    int* units = (int*)(sm + NS * STAGE);
-    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : a.B));
+    int* blocks_of = (int*)(sm + NS * STAGE);
+    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
     TaWork work;
-    work.begin(a, units);
+    work.begin(a, blocks_of);
     Part it;
-    while (work.next(a, units, it, tid == 0)) {
+    while (work.next(a, blocks_of, it, tid == 0)) {
     __syncthreads();
     const int h = it.h, r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
     const SeqKeys& s = it.s;
@@ -100,126 +99,187 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
 }
 
 // ------------------------------------------------------------------ fp32: FFMA
-// CTA of 128 threads = 16 rows x a split's blocks of 64 keys; keys and values pass through shared memory, scores between the two products too.
-constexpr int TF_ROWS = 16, TF_KT = 64;
+// CTA = WK warps over the same 16 rows, each with every WK-th block of 32 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
+// another warp until the results meet).  Lane (rg, x): four rows, for the scores the keys x + 8 i, for the output the columns 4 x + 32 c.  The next block's keys are
+// fetched under this block's second product, its values under the next scores.  A call of few rows is bounded by the chain of one warp, one of many
+// by the fused multiply-adds and the shared-memory reads that feed them (8 of 16 bytes for 64).
+constexpr int TF_ROWS = 16, TF_KT = 32;
+template <int DP> struct TfCfg {
+    static constexpr int WK = DP > 64 ? 4 : 8, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
+    static constexpr int WARP = 2 * TF_KT * KP + TF_ROWS * PP;                         // a warp's keys, values and probabilities
+    static constexpr int FLOATS = TF_ROWS * KP + WK * WARP;
+};
 template <int DP>
-__global__ void __launch_bounds__(128) k_ta_f32(TreeAttn a) {
-    constexpr int KP = DP + 4, SP = TF_KT + 4;
+__global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
+    using Cfg = TfCfg<DP>;
+    constexpr int WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32;
     extern __shared__ __align__(128) char sm[];
     float* q = reinterpret_cast<float*>(sm);              // [16][KP]
-    float* kt = q + TF_ROWS * KP;                         // [64][KP]
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rg = lane >> 3, x = lane & 7;
+    float* kt = q + TF_ROWS * KP + warp * Cfg::WARP;      // [32][KP]
     float* vt = kt + TF_KT * KP;
-    float* sc = vt + TF_KT * KP;                          // [16][SP]
-    float* row_f = sc + TF_ROWS * SP;                     // [16] rescale, [16] maximum, [16] sum
-    int* units = reinterpret_cast<int*>(row_f + 48);
-    uint32_t* any = reinterpret_cast<uint32_t*>(units + (a.direct ? 0 : a.B));
+    float* pt = vt + TF_KT * KP;                          // [16][PP]
+    int* blocks_of = reinterpret_cast<int*>(q + Cfg::FLOATS);
+    uint32_t* any = reinterpret_cast<uint32_t*>(blocks_of + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     TaWork work;
-    work.begin(a, units);
+    work.begin(a, blocks_of);
+    const int chunks = a.dim / 4;
     Part it;
-    while (work.next(a, units, it, tid == 0)) {
-    __syncthreads();
-    const int b = it.b, h = it.h, r0 = it.tile * TF_ROWS, all_rows = a.T * a.group;
-    const SeqKeys& s = it.s;
-    ta_load_masks<128, 0>(a, b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
-    for (int i = tid; i < TF_ROWS * DP; i += 128) {
-        const int r = i / DP, d = i % DP, gr = r0 + r;
-        float x = 0.f;
-        if (gr < all_rows && d < a.dim) x = *reinterpret_cast<const float*>(a.q + b * a.q_sb + (gr / a.group) * a.q_st + (h * a.group + gr % a.group) * a.q_sh + d * 4);
-        q[r * KP + d] = x;
-    }
-    if (tid < 16) { row_f[16 + tid] = -INFINITY; row_f[32 + tid] = 0.f; }
-    const int t0 = r0 / a.group;
-    const int k_begin = it.k_begin, k_end = it.k_end;
-    constexpr int DC = DP / 4, RG = 128 / DC, RR = TF_ROWS / RG;           // output: DC column groups of 4, RG row groups of RR rows
-    const int oc = tid % DC, og = tid / DC;
-    float4 o[RR];
-#pragma unroll
-    for (int i = 0; i < RR; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = k_begin; k0 < k_end; k0 += TF_KT) {
+    while (work.next(a, blocks_of, it, tid == 0)) {
         __syncthreads();
-        for (int i = tid; i < TF_KT * (DP / 4); i += 128) {
-            const int r = i / (DP / 4), c = i % (DP / 4), key = k0 + r;
-            bool real = key < k_end && c * 4 < a.dim && ta_seen(any, s, key);
-            const int pi = key >> a.page_shift;
+        const int r0 = it.tile * TF_ROWS, all_rows = a.T * a.group, t0 = ta_node(a, r0);
+        const SeqKeys& s = it.s;
+        for (int i = tid; i < TF_ROWS * DP; i += NT) {
+            const int r = i / DP, d = i % DP, gr = r0 + r, node = ta_node(a, gr);
+            float v = 0.f;
+            if (gr < all_rows && node < s.nodes && d < a.dim) v = *reinterpret_cast<const float*>(a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + d * 4);
+            q[r * KP + d] = v;
+        }
+        if (a.dim < DP)                                   // columns beyond the head
+            for (int i = lane; i < 2 * TF_KT * (DP - a.dim); i += 32) kt[i / (DP - a.dim) * KP + a.dim + i % (DP - a.dim)] = 0.f;
+        ta_load_masks<NT, 0>(a, it.b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
+        const int blocks = (it.k_end - it.k_begin + TF_KT - 1) / TF_KT;
+        auto offset = [&](int j) -> long long {           // of this lane's key in block j; -1: zeros instead
+            const int key = it.k_begin + j * TF_KT + lane, pi = key >> a.page_shift;
             int page = -1;
-            if (real && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
-            real = real && (unsigned)page < (unsigned)a.n_pages;
-            const long long off = real ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + c * 16 + h * a.s_head : 0;
-            ta_copy16(smem_u32(kt + r * KP + c * 4), a.k + off, real);
-            ta_copy16(smem_u32(vt + r * KP + c * 4), a.v + off, real);
+            if (j < blocks && key < it.k_end && ta_seen(any, s, key) && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
+            return (unsigned)page < (unsigned)a.n_pages ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + it.h * a.s_head : -1;
+        };
+        auto fetch = [&](float* to, const char* base, long long off) {
+            for (int i = lane; i < TF_KT * chunks; i += 32) {
+                const int r = i / chunks, c = i - r * chunks;
+                const long long o = __shfl_sync(0xffffffffu, off, r);
+                ta_copy16(smem_u32(to + r * KP + c * 4), base + (o < 0 ? 0 : o + c * 16), o >= 0);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        bool live[4];
+        const uint32_t* row[4];
+        float m[4], l[4];
+        float4 o[4][DC];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int gr = r0 + rg * 4 + i, node = ta_node(a, gr);
+            live[i] = gr < all_rows && node < s.nodes;
+            row[i] = mask + (live[i] ? (node - t0) * a.words : 0);
+            m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < DC; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
-        __syncthreads();
-        {   // scores: key tid % 64, eight rows
-            const int key = tid & 63, rr = (tid >> 6) * 8;
-            float x[8];
+        long long off = offset(warp);
+        fetch(kt, a.k, off);
+        for (int j = warp; j < blocks; j += WK) {
+            fetch(vt, a.v, off);
+            off = offset(j + WK);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+            float sc[4][4];                               // [row][key x + 8 i]
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-            for (int d = 0; d < a.dim; d += 4) {
-                const float4 kv = *reinterpret_cast<const float4*>(kt + key * KP + d);
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 qv = *reinterpret_cast<const float4*>(q + (rr + i) * KP + d);
-                    x[i] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, x[i]))));
+                for (int e = 0; e < 4; ++e) sc[i][e] = 0.f;
+#pragma unroll 4
+            for (int d = 0; d < DP; d += 4) {
+                float4 qv[4], kv[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(q + (rg * 4 + i) * KP + d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kv[e] = *reinterpret_cast<const float4*>(kt + (x + 8 * e) * KP + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sc[i][e] = fmaf(qv[i].x, kv[e].x, fmaf(qv[i].y, kv[e].y, fmaf(qv[i].z, kv[e].z, fmaf(qv[i].w, kv[e].w, sc[i][e]))));
+            }
+            __syncwarp();
+            fetch(kt, a.k, off);
+            const int base = it.k_begin + j * TF_KT - s.len;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = live[i] ? ta_window(row[i], a.words, base) : 0u;
+                float top = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[i][e] = w >> (x + 8 * e) & 1 ? sc[i][e] * a.scale : -INFINITY;
+                    top = fmaxf(top, sc[i][e]);
                 }
-            }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)); top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                top = fmaxf(top, m[i]);
+                const float z = top == -INFINITY ? 0.f : top, f = exp2f(m[i] - z);
+                m[i] = top;
+                l[i] *= f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int gr = r0 + rr + i, t = gr / a.group, base = k0 + (key & 32) - s.len;
-                const bool live = gr < all_rows && t < s.nodes;
-                const uint32_t w = live ? ta_window(mask + (t - t0) * a.words, a.words, base) : 0u;
-                sc[(rr + i) * SP + key] = (w >> (key & 31) & 1) && k0 + key < k_end ? x[i] * a.scale : -INFINITY;
+                for (int e = 0; e < 4; ++e) {
+                    const float p = exp2f(sc[i][e] - z);
+                    l[i] += p;
+                    pt[(rg * 4 + i) * PP + x + 8 * e] = p;
+                }
+#pragma unroll
+                for (int c = 0; c < DC; ++c) { o[i][c].x *= f; o[i][c].y *= f; o[i][c].z *= f; o[i][c].w *= f; }
             }
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+#pragma unroll 2
+            for (int key = 0; key < TF_KT; key += 4) {
+                float4 p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(pt + (rg * 4 + i) * PP + key);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int c = 0; c < DC; ++c) {
+                        const float4 v = *reinterpret_cast<const float4*>(vt + (key + e) * KP + x * 4 + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
+                            o[i][c].x = fmaf(w, v.x, o[i][c].x); o[i][c].y = fmaf(w, v.y, o[i][c].y); o[i][c].z = fmaf(w, v.z, o[i][c].z); o[i][c].w = fmaf(w, v.w, o[i][c].w);
+                        }
+                    }
+            }
+            __syncwarp();
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        // the warps' results meet: output in the keys' place, (maximum, sum) in the probabilities'
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1); l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2); l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
+            const bool none = l[i] == 0.f;                // sees nothing here: values times 0
+#pragma unroll
+            for (int c = 0; c < DC; ++c) *reinterpret_cast<float4*>(kt + (rg * 4 + i) * KP + x * 4 + 32 * c) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : o[i][c];
+            if (x == 0) { pt[rg * 4 + i] = none ? -INFINITY : m[i]; pt[16 + rg * 4 + i] = l[i]; }
         }
         __syncthreads();
+        const float* w0 = q + TF_ROWS * KP;               // warp w's keys: + w * WARP; its probabilities: + 2 * TF_KT * KP
+        for (int i = tid; i < TF_ROWS * (DP / 4); i += NT) {
+            const int r = i / (DP / 4), c = i % (DP / 4), gr = r0 + r;
+            float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                     // running maximum and sum: four rows a warp
-            const int r = warp * 4 + i;
-            const float x = sc[r * SP + lane], y = sc[r * SP + lane + 32], m0 = row_f[16 + r];
-            float m = fmaxf(x, y);
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, w0[w * Cfg::WARP + 2 * TF_KT * KP + r]);
+            const float z = top == -INFINITY ? 0.f : top;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int of = 16; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
-            m = fmaxf(m, m0);
-            const float z = m == -INFINITY ? 0.f : m, p = exp2f(x - z), u = exp2f(y - z);
-            sc[r * SP + lane] = p; sc[r * SP + lane + 32] = u;
-            float l = p + u;
-#pragma unroll
-            for (int of = 16; of; of >>= 1) l += __shfl_xor_sync(0xffffffffu, l, of);
-            if (lane == 0) { const float f = exp2f(m0 - z); row_f[r] = f; row_f[16 + r] = m; row_f[32 + r] = row_f[32 + r] * f + l; }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < RR; ++i) { const float f = row_f[og * RR + i]; o[i].x *= f; o[i].y *= f; o[i].z *= f; o[i].w *= f; }
-        const int kn = min(TF_KT, k_end - k0);
-        for (int key = 0; key < kn; ++key) {
-            const float4 v = *reinterpret_cast<const float4*>(vt + key * KP + oc * 4);
-#pragma unroll
-            for (int i = 0; i < RR; ++i) {
-                const float p = sc[(og * RR + i) * SP + key];
-                o[i].x = fmaf(p, v.x, o[i].x); o[i].y = fmaf(p, v.y, o[i].y); o[i].z = fmaf(p, v.z, o[i].z); o[i].w = fmaf(p, v.w, o[i].w);
+            for (int w = 0; w < WK; ++w) {
+                const float* p = w0 + w * Cfg::WARP;
+                const float f = exp2f(p[2 * TF_KT * KP + r] - z);
+                const float4 v = *reinterpret_cast<const float4*>(p + r * KP + c * 4);
+                sum += p[2 * TF_KT * KP + 16 + r] * f;
+                y.x = fmaf(v.x, f, y.x); y.y = fmaf(v.y, f, y.y); y.z = fmaf(v.z, f, y.z); y.w = fmaf(v.w, f, y.w);
+            }
+            if (gr >= all_rows || c * 4 >= a.dim) continue;
+            if (it.whole) {
+                const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                const int node = ta_node(a, gr);
+                float* p = reinterpret_cast<float*>(a.out + it.b * a.o_sb + node * a.o_st + (it.h * a.group + gr - node * a.group) * a.o_sh) + c * 4;
+                if (a.out_vec) *reinterpret_cast<float4*>(p) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+                else { p[0] = y.x * inv; p[1] = y.y * inv; p[2] = y.z * inv; p[3] = y.w * inv; }
+            } else {
+                const long long slot = it.slot * TF_ROWS + r;
+                *reinterpret_cast<float4*>(a.part + slot * a.dim + c * 4) = y;
+                if (c == 0) a.part_ml[slot] = make_float2(top, sum);
             }
         }
-    }
-    __syncthreads();
-    const long long slot = it.slot * TF_ROWS;
-#pragma unroll
-    for (int i = 0; i < RR; ++i) {
-        const int r = og * RR + i, gr = r0 + r;
-        if (gr >= all_rows || oc * 4 >= a.dim) continue;
-        const float l = row_f[32 + r];
-        if (l == 0.f) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);               // sees nothing: values times 0
-        if (it.whole) {
-            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-            float* p = reinterpret_cast<float*>(a.out + b * a.o_sb + (gr / a.group) * a.o_st + (h * a.group + gr % a.group) * a.o_sh) + oc * 4;
-            if (a.out_vec) *reinterpret_cast<float4*>(p) = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
-            else { p[0] = o[i].x * inv; p[1] = o[i].y * inv; p[2] = o[i].z * inv; p[3] = o[i].w * inv; }
-        } else {
-            *reinterpret_cast<float4*>(a.part + (slot + r) * a.dim + oc * 4) = o[i];
-            if (oc == 0) a.part_ml[slot + r] = make_float2(row_f[16 + r], l);
-        }
-    }
     }
 }
 
@@ -231,7 +291,7 @@ template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *rei
 
 // The parts' outputs, each rescaled to the largest maximum: one warp a query row, CTAs that stay.
 template <typename T>
-__global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
+__global__ void __launch_bounds__(128, 8) k_ta_merge(TreeAttn a, int rows) {
     const int lane = threadIdx.x & 31, ht = a.kv_heads * a.tiles, all = a.T * a.group;
     cudaGridDependencySynchronize();
     for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * all; w += gridDim.x * 4) {
@@ -266,22 +326,25 @@ __global__ void __launch_bounds__(128) k_ta_merge(TreeAttn a, int rows) {
 }
 
 // ------------------------------------------------------------------ host
-struct Plan { int rows, tiles, direct, ctas, unit, min_units; long long grid, slots; };       // see TreeAttn; slots of partial results
-// Rows of a tile: 16, 32 or 64 by the rows there are (64 share a block's keys among four warps; fewer rows give the warps keys of their own instead).
+struct Plan { int rows, tiles, direct, ctas, unit, min_blocks; long long grid, slots; };       // see TreeAttn; slots of partial results
+// Rows of a tile.  16-bit types: 16, 32 or 64 with mma.sync by the rows there are (64 share a block's keys among four warps; fewer rows give the warps keys of their own
+// instead), 128 or 256 with tcgen05 beyond 64 rows, of heads wider than 64 beyond 32.  (64 rows, 2 x 8 heads of 128 over 8000 keys: 31 us with tcgen05, 33 without; over 2000 keys of 64
+// sequences 43 and 48; heads of 64: 24.5 and 23, 32 and 27.  128 rows: 69 and 120, 136 and 243; heads of 64 50 and 67, 93 and 138.)
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, int page_tokens, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
-    static const int thr = getenv("TA_THR") ? atoi(getenv("TA_THR")) : 64;
-    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 && thr >= 16 ? 16 : all <= 32 && thr>=32 ? 32 : all <= thr ? 64 : all <= 128 ? 128 : 256;
+    const int most_mma = head_dim > 64 ? 32 : 64;
+    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma ? 64 : all <= 128 ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
-    p.min_units = p.rows >= 128 ? 4 : 4;
-    const int at_once = TA_SMS * (p.rows >= 128 ? 1 : head_dim > 64 ? 2 : 3);          // CTAs that an SM holds at least
-    const long long columns = (long long)n_kv_heads * p.tiles, whole = B * columns, units = (max_keys + p.unit - 1) / p.unit;
-    // With work for every CTA twice over, only long sequences are worth cutting, and the merge that follows.
-    p.direct = units <= (whole >= 2 * at_once ? 4 * p.min_units : p.min_units) || B > TA_MAX_B;
+    p.min_blocks = 4;
+    const int at_once = TA_SMS * (p.rows >= 128 || dtype == SPECDEC_DTYPE_F32 ? 1 : head_dim > 64 ? 2 : 3);     // CTAs that an SM holds at least
+    const long long columns = (long long)n_kv_heads * p.tiles, whole = B * columns, blocks = (max_keys + p.unit - 1) / p.unit;
+    // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge, which costs about as much as eight
+    // blocks.
+    p.direct = (whole + at_once - 1) / at_once * blocks <= whole * blocks / at_once + 8 || B > TA_MAX_B;
     p.ctas = (int)(at_once / columns < 1 ? 1 : at_once / columns);
-    const long long most = (B * units + p.min_units - 1) / p.min_units;                // stretches at most
+    const long long most = (B * blocks + p.min_blocks - 1) / p.min_blocks;                // stretches at most
     if (p.ctas > most) p.ctas = (int)most;
     p.grid = p.direct ? whole : p.ctas * columns;
     p.slots = p.direct ? 0 : (p.ctas + B) * columns;
@@ -303,10 +366,10 @@ cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
 }
 template <int DP>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr size_t FLOATS = (TF_ROWS + 2 * TF_KT) * (DP + 4) + TF_ROWS * (TF_KT + 4) + 48;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FLOATS * 4 + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 4);
+    constexpr int BYTES = TfCfg<DP>::FLOATS * 4;
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 4);
     if (attr != cudaSuccess) return attr;
-    k_ta_f32<DP><<<grid, 128, FLOATS * 4 + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
+    k_ta_f32<DP><<<!a.direct || grid < TA_SMS ? grid : TA_SMS, 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
     return cudaGetLastError();
 }
 // The merge is launched while the items run, and waits for them.
@@ -388,7 +451,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     a.out_vec = (((uintptr_t)g->d_out | a.o_sb | a.o_st | a.o_sh) & 15) == 0;
     const Plan p = plan(a.B, a.T, g->n_q_heads, c->n_heads, c->dtype, a.dim, c->page_tokens, (long long)a.max_length + a.T);
     if (p.grid > 0x7fffffff || p.slots > 0x7fffffff || (long long)a.B * a.kv_heads * a.T * a.group > 0x7fffffff - 65536) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many sequences, heads and nodes for one launch");
-    a.tiles = p.tiles; a.direct = p.direct; a.ctas = p.ctas; a.unit = p.unit; a.min_units = p.min_units;
+    a.tiles = p.tiles; a.direct = p.direct; a.ctas = p.ctas; a.unit = p.unit; a.min_blocks = p.min_blocks;
     const long long need = workspace(p, a.B, c->n_heads, c->head_dim);
     if (need && (!g->d_workspace || (uintptr_t)g->d_workspace % 16 || g->workspace_bytes < need))
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_tree_attention_workspace says, or not 16-byte aligned");

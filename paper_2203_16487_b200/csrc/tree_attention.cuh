@@ -12,7 +12,7 @@
 namespace sd {
 
 // Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's rows; (K/V head, tile) is a column of work.  The keys of a
-// sequence are its length committed tokens and n nodes behind them, in blocks of `unit` keys (64 or 128).
+// sequence are its length committed tokens and n nodes behind them, in blocks of `unit` keys (64, or 128).
 //
 // direct: sequences are never cut; CTAs that stay take every gridDim.x-th (sequence, column).
 // Otherwise a column's blocks of all sequences form one line, of which each of its `ctas` CTAs takes an equal stretch (TaWork), so that all CTAs run equally long
@@ -27,7 +27,7 @@ struct TreeAttn {
     int n_pages, n_seqs, max_pages, page_shift, max_length;
     int T, words, group, kv_heads, dim, B;
     uint32_t group_mul;                                                                // see ta_node
-    int tiles, direct, ctas, unit, min_units;                                               // row tiles; CTAs of a column; keys of a block; blocks of a stretch at least
+    int tiles, direct, ctas, unit, min_blocks;                                              // row tiles; CTAs of a column; keys of a block; blocks of a stretch at least
     float scale;                                                                       // times log2(e)
     float* part; float2* part_ml;                                                      // [slot, row of the tile]: output [dim] and (maximum, sum)
     int2* where;                                                                       // [b, column]: first slot, parts
@@ -51,26 +51,26 @@ __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
 struct Part { int b, h, tile, k_begin, k_end, blocks, whole; long long slot; SeqKeys s; };     // keys [k_begin, k_end) in `blocks` blocks
 struct TaWork {
     int column, at, b, skip, left, stretch;               // direct: at = number of the next (sequence, column).  Else: the CTA, and what is next on the line: sequence, blocks of it to skip; blocks left, blocks of a stretch
-    // For the whole CTA; units: B ints of shared memory that stay (not direct).
-    __device__ __forceinline__ void begin(const TreeAttn& a, int* units) {
+    // For the whole CTA; blocks_of: B ints of shared memory that stay (not direct).
+    __device__ __forceinline__ void begin(const TreeAttn& a, int* blocks_of) {
         const int columns = a.kv_heads * a.tiles;
         at = blockIdx.x;
         if (a.direct) return;
         __shared__ int found[4];
         column = blockIdx.x % columns; at = blockIdx.x / columns;
-        for (int i = threadIdx.x; i < a.B; i += blockDim.x) units[i] = max(1, (ta_keys(a, i).keys + a.unit - 1) / a.unit);      // (at least 1: rows that see nothing are written too)
+        for (int i = threadIdx.x; i < a.B; i += blockDim.x) blocks_of[i] = max(1, (ta_keys(a, i).keys + a.unit - 1) / a.unit);      // (at least 1: rows that see nothing are written too)
         __syncthreads();
         if (threadIdx.x < 32) {
             const int lane = threadIdx.x;
             long long total = 0;
-            for (int i = lane; i < a.B; i += 32) total += units[i];
+            for (int i = lane; i < a.B; i += 32) total += blocks_of[i];
 #pragma unroll
             for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            const long long per = max((total + a.ctas - 1) / a.ctas, (long long)a.min_units), start = at * per;
+            const long long per = max((total + a.ctas - 1) / a.ctas, (long long)a.min_blocks), start = at * per;
             long long run = 0;
             int fb = 0, fskip = 0;
             for (int i0 = 0; i0 < a.B; i0 += 32) {        // the sequence in which the stretch begins
-                const int n = i0 + lane < a.B ? units[i0 + lane] : 0;
+                const int n = i0 + lane < a.B ? blocks_of[i0 + lane] : 0;
                 int upto = n;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
@@ -89,7 +89,7 @@ struct TaWork {
         b = found[0]; skip = found[1]; left = found[2]; stretch = found[3];
     }
     // The next part.  notes: whether this thread tells the merge where a sequence's parts are.
-    __device__ __forceinline__ bool next(const TreeAttn& a, const int* units, Part& p, bool notes = false) {
+    __device__ __forceinline__ bool next(const TreeAttn& a, const int* blocks_of, Part& p, bool notes = false) {
         const int columns = a.kv_heads * a.tiles;
         if (a.direct) {
             if (at >= a.B * columns) return false;
@@ -100,7 +100,7 @@ struct TaWork {
             p.blocks = (p.s.keys + a.unit - 1) / a.unit;
         } else {
             if (left <= 0) return false;
-            const int n = units[b], take = min(n - skip, left);
+            const int n = blocks_of[b], take = min(n - skip, left);
             p.b = b;
             p.s = ta_keys(a, b);
             p.k_begin = skip * a.unit; p.k_end = min(p.s.keys, (skip + take) * a.unit);

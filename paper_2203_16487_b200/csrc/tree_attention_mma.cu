@@ -22,8 +22,8 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     __shared__ __align__(8) uint64_t bars[2 * NS];
     __shared__ int abort_flag;
     char* ring = ta_smem + (1024 - (smem_u32(ta_smem) & 1023)) % 1024;
-    int* units = (int*)(ring + NS * STAGE);               // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : (a.B + 1) / 2 * 2));
+    int* blocks_of = (int*)(ring + NS * STAGE);               // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : (a.B + 1) / 2 * 2));
     uint32_t* mask = any + (a.words + 1) / 2 * 2;         // (8-byte aligned, as the partial results behind it are)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
@@ -34,14 +34,14 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         tma_prefetch_map(&tm);
     }
     TaWork work;
-    work.begin(a, units);
+    work.begin(a, blocks_of);
     __syncthreads();
 
     if (warp == TM_WARPS) {                               // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
         int count = 0;                                    // lane g: blocks that group g had in the parts before
         Part it, ahead;
-        for (bool more = work.next(a, units, ahead); more;) {
+        for (bool more = work.next(a, blocks_of, ahead); more;) {
             it = ahead;
             const int* table = a.table + (long long)it.s.seq * a.max_pages;
             auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
                 return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
             };
             int p = it.blocks ? page_of(0) : 0;
-            more = work.next(a, units, ahead);
+            more = work.next(a, blocks_of, ahead);
             for (int j = 0; j < it.blocks; ++j) {
                 const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), key = it.k_begin + j * KT + lane * box, cur = p;
                 if (j + 1 < it.blocks) p = page_of(j + 1);
@@ -78,9 +78,9 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     auto consumers = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * TM_WARPS) : "memory"); };
     int count = 0;                                        // this group's blocks so far
     Part it, ahead;
-    for (bool more = work.next(a, units, ahead, tid == 0); more;) {
+    for (bool more = work.next(a, blocks_of, ahead, tid == 0); more;) {
         it = ahead;
-        more = work.next(a, units, ahead, tid == 0);
+        more = work.next(a, blocks_of, ahead, tid == 0);
         const SeqKeys& s = it.s;
         const int r0 = it.tile * ROWS, t0 = ta_node(a, r0);
         const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
@@ -159,7 +159,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {
-    if (a.dim > 64) return rows == 16 ? run<T, 128, 1, 3, 3>(tm, a, grid, st) : rows == 32 ? run<T, 128, 2, 1, 3>(tm, a, grid, st) : run<T, 128, 4, 1, 3>(tm, a, grid, st);
+    if (a.dim > 64) return rows == 16 ? run<T, 128, 1, 3, 3>(tm, a, grid, st) : run<T, 128, 2, 1, 3>(tm, a, grid, st);
     return rows == 16 ? run<T, 64, 1, 4, 4>(tm, a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 2>(tm, a, grid, st) : run<T, 64, 4, 1, 3>(tm, a, grid, st);
 }
 

@@ -1,17 +1,18 @@
 // Attention of drafted trees over the paged cache for 16-bit types and many query rows: tcgen05 (contract: specdec.h, work: tree_attention.cuh).
 //
-// One CTA an SM.  A block is 128 keys; the scores of 128 rows against it are one accumulator in tensor memory (a row a lane), from which the
-// row's thread takes maximum and exponentials; the probabilities go back into the same columns as 16-bit pairs and are the second product's A operand, the values
-// its B operand as they lie ([key, column], N-major).  Two groups of four softmax warps keep the tensor pipe busy in turn:
+// One CTA an SM.  A block is 128 keys; the scores of 128 rows against it are one accumulator in tensor memory (a row a lane), which the row's thread takes into
+// registers for maximum and exponentials; the probabilities go back into the same columns as 16-bit pairs and are the second product's A operand, the
+// values its B operand as they lie ([key, column], N-major).  Two groups of four softmax warps keep the tensor pipe busy in turn:
 //   TILES = 2: the groups have 128 rows each and share the blocks of a 256-row tile.
 //   TILES = 1: the groups have the same 128 rows and take every second block; their results meet at the end.
 // Warps: 0 loads (one TMA box a page), 1 issues the products, 4-7 and 8-11 are the groups.
 //
+// A group's chain is scores (512 clocks at D = 128), maximum, exponentials (1024: 16 a clock and SM), second product (512, its first half under the second half of the
+// exponentials), and its scores' columns are taken by the probabilities until that is done.  Blocks of 64 keys leave room for both, so that
+// the next scores can be under way meanwhile, but each issue of products costs some 200 clocks beside their own: 256 rows took 5760 clocks for 128 keys instead of 3700.
+//
 // The running maximum is only moved (and the output, in tensor memory, rescaled) when it grows by more than 2^8: until then probabilities up to 2^8 are relative to
 // the old one, which changes neither the quotient nor its relative precision.
-//
-// Per block and 128 rows the tensor pipe takes 8 D clocks (D = 128: 1024) and the exponentials 1024 (16 a clock and SM), so neither can hide the other wholly: with two groups
-// the pair takes about the sum of a group's two parts.
 #include <type_traits>
 
 #include "tree_attention.cuh"
@@ -75,34 +76,34 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     constexpr uint32_t IDESC = (1u << 4) | (std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(TC_ROWS >> 4) << 24);
     constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(KT >> 3) << 17), IDESC_O = IDESC | (1u << 16) | ((uint32_t)(DP >> 3) << 17);   // O: B is N-major
     extern __shared__ __align__(1024) char tc_smem[];
-    __shared__ __align__(8) uint64_t bars[4 * NS + 6];
+    __shared__ __align__(8) uint64_t bars[4 * NS + 8];
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_base;
     __shared__ float2 other[TILES == 1 ? TC_ROWS : 1];    // maximum and sum of the second group's rows
     char* qs = tc_smem + (1024 - (smem_u32(tc_smem) & 1023)) % 1024;
     char* kring = qs + TILES * Cfg::Q;
     char* vring = kring + NS * SIDE;
-    int* units = (int*)(vring + NS * SIDE);               // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(units + (a.direct ? 0 : a.B));
+    int* blocks_of = (int*)(vring + NS * SIDE);               // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t kfull = smem_u32(bars), kempty = kfull + NS * 8, vfull = kempty + NS * 8, vempty = vfull + NS * 8;
-    const uint32_t sfull = vempty + NS * 8, pready = sfull + 16, ofin = pready + 16;
+    const uint32_t sfull = vempty + NS * 8, pready = sfull + 16, ofin = pready + 32;            // of group g: + 8 g; pready: of a half, + 16 g + 8 half
     if (tid == 0) {
         for (int i = 0; i < 4 * NS; ++i) mbar_init(kfull + i * 8, 1);
-        for (int g = 0; g < 2; ++g) { mbar_init(sfull + g * 8, 1); mbar_init(pready + g * 8, 4); mbar_init(ofin + g * 8, 1); }
+        for (int g = 0; g < 2; ++g) { mbar_init(sfull + g * 8, 1); mbar_init(pready + g * 16, 4); mbar_init(pready + g * 16 + 8, 4); mbar_init(ofin + g * 8, 1); }
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
     TaWork work;
-    work.begin(a, units);
+    work.begin(a, blocks_of);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base;                      // columns: scores 0, scores 1 (128 each), outputs 0, 1 (DP each)
-    // steps of group g in a part of `blocks` blocks; its i-th is block_of(g, i)
+    const uint32_t tmem = tmem_base;                      // columns: scores of the groups (128 each), outputs from 256 (DP each)
+    // steps of group g in a part of `blocks` blocks of 128 keys; its i-th is block_of(g, i)
     auto steps = [](int blocks, int g) { return TILES == 2 ? blocks : (blocks + 1 - g) / 2; };
     auto block_of = [](int g, int i) { return TILES == 2 ? i : 2 * i + g; };
     auto wait = [&](uint32_t bar, int n) { return mbar_wait_warp(bar, n & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT); };     // for its completion number n
@@ -110,9 +111,12 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     int done = 0;                                         // blocks of the parts before: block j is in stage (done + j) % NS
     bool ok = true;
 
+    // 384 threads have 168 registers each: the first warpgroup passes on what the softmax groups need (128 x 104 + 256 x 200 = 384 x 168)
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0) {                                      // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, TA_BLOCK), n_boxes = KT / box;
-        for (; ok && work.next(a, units, it); done += it.blocks) {
+        for (; ok && work.next(a, blocks_of, it); done += it.blocks) {
             const int* table = a.table + (long long)it.s.seq * a.max_pages;
             auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
                 const int key = it.k_begin + j * KT + lane * box, i = key >> a.page_shift;
@@ -143,65 +147,85 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         }
     } else if (warp == 1) {                               // products
         int taken[2] = {0, 0};                            // steps of the groups in the parts before
-        for (; work.next(a, units, it); done += it.blocks, taken[0] += steps(it.blocks, 0), taken[1] += steps(it.blocks, 1)) {
+        for (; work.next(a, blocks_of, it); done += it.blocks, taken[0] += steps(it.blocks, 0), taken[1] += steps(it.blocks, 1)) {
             asm volatile("bar.sync 2, 288;" ::: "memory");            // the queries are there, the last outputs have been read
             tc_fence_after();
-            auto second = [&](int g, int i) {             // output += probabilities x values
+            const int n0 = steps(it.blocks, 0), n1 = steps(it.blocks, 1);
+            auto first = [&](int g, int i) {              // scores = queries x keys
                 const int n = done + block_of(g, i), st = n % NS;
-                ok = ok && wait(pready + g * 8, taken[g] + i) && wait(vfull + st * 8, n / NS);
+                ok = ok && wait(kfull + st * 8, n / NS);
                 if (!ok) return;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t v = umma_desc_n_sw128(smem_u32(vring + st * SIDE), KT * 128);
 #pragma unroll
-                    for (int kk = 0; kk < KT / 16; ++kk)  // 16 keys: 2048 bytes of values, 8 columns of probabilities
-                        umma_ts(tmem + 256 + g * DP, tmem + g * 128 + kk * 8, v + kk * 128, IDESC_O, i || kk ? 1u : 0u);
-                    if (TILES == 1 || g == 1) umma_commit(vempty + st * 8);
-                    if (i + 1 == steps(it.blocks, g)) umma_commit(ofin + g * 8);
+                    for (int kk = 0; kk < DP / 16; ++kk) {
+                        const uint64_t q = umma_desc_k_sw128(smem_u32(qs + (TILES == 2 ? g : 0) * Cfg::Q) + (kk / 4) * TC_ROWS * 128) + (kk % 4) * 2;
+                        const uint64_t k = umma_desc_k_sw128(smem_u32(kring + st * SIDE) + (kk / 4) * KT * 128) + (kk % 4) * 2;
+                        umma_bf16(tmem + g * KT, q, k, IDESC_S, kk ? 1u : 0u);
+                    }
+                    umma_commit(sfull + g * 8);
+                    if (TILES == 1 || g == 1) umma_commit(kempty + st * 8);
                 }
             };
-            const int most = steps(it.blocks, 0);
-            for (int i = 0; i <= most && ok; ++i)
+            auto second = [&](int g, int i, bool last) {  // output += probabilities x values, 64 keys at a time
+                const int n = done + block_of(g, i), st = n % NS;
+                ok = ok && wait(vfull + st * 8, n / NS);
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    if (!ok) break;
-                    if (i > 0 && i <= steps(it.blocks, g)) second(g, i - 1);
-                    if (!ok || i >= steps(it.blocks, g)) continue;
-                    const int n = done + block_of(g, i), st = n % NS;
-                    ok = wait(kfull + st * 8, n / NS);
-                    if (!ok) break;
+                for (int hf = 0; hf < 2; ++hf) {
+                    ok = ok && wait(pready + g * 16 + hf * 8, taken[g] + i);
+                    if (!ok) return;
                     tc_fence_after();
                     if (elect_one()) {
+                        const uint64_t v = umma_desc_n_sw128(smem_u32(vring + st * SIDE), KT * 128);
 #pragma unroll
-                        for (int kk = 0; kk < DP / 16; ++kk) {
-                            const uint64_t q = umma_desc_k_sw128(smem_u32(qs + (TILES == 2 ? g : 0) * Cfg::Q) + (kk / 4) * TC_ROWS * 128) + (kk % 4) * 2;
-                            const uint64_t k = umma_desc_k_sw128(smem_u32(kring + st * SIDE) + (kk / 4) * KT * 128) + (kk % 4) * 2;
-                            umma_bf16(tmem + g * 128, q, k, IDESC_S, kk ? 1u : 0u);
+                        for (int kk = hf * 4; kk < hf * 4 + 4; ++kk)           // 16 keys: 2048 bytes of values, 8 columns of probabilities
+                            umma_ts(tmem + 256 + g * DP, tmem + g * KT + kk * 8, v + kk * 128, IDESC_O, i || kk ? 1u : 0u);
+                        if (hf == 1) {
+                            if (TILES == 1 || g == 1) umma_commit(vempty + st * 8);
+                            if (last) umma_commit(ofin + g * 8);
                         }
-                        umma_commit(sfull + g * 8);
-                        if (TILES == 1 || g == 1) umma_commit(kempty + st * 8);
                     }
                 }
+            };
+            for (int i = 0; i <= n0 && ok; ++i)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int n = g ? n1 : n0;
+                    if (i > 0 && i <= n) second(g, i - 1, i == n);
+                    if (i < n) first(g, i);               // (behind the second product, which reads the probabilities in its columns)
+                }
         }
-    } else if (warp >= 4) {                               // softmax: one row a thread
+    }
+    } else {                                              // softmax: one row a thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int g = (warp - 4) >> 2, t = tid - 128, all_rows = a.T * a.group;
         int taken = 0, outputs = 0;                       // this group's steps and outputs in the parts before
         auto softmax_warps = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-        while (work.next(a, units, it, t == 0)) {
+        while (work.next(a, blocks_of, it, t == 0)) {
         const SeqKeys& s = it.s;
         const int r0 = it.tile * ROWS;
-        for (int i = t; i < ROWS * (DP / 8); i += 256) {  // the queries
-            const int r = i / (DP / 8), c = i % (DP / 8), gr = r0 + r, node = ta_node(a, gr);
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (gr < all_rows && node < s.nodes && c * 8 < a.dim) {
-                const char* p = a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + c * 16;
-                if (a.q_vec) x = *reinterpret_cast<const uint4*>(p);
-                else {
-                    const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
-                    x = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+#pragma unroll
+        for (int i0 = 0; i0 < ROWS * (DP / 8); i0 += 8 * 256) {       // the queries, eight pieces a thread at a time
+            uint4 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * 256 + t, r = i / (DP / 8), c = i % (DP / 8), gr = r0 + r, node = ta_node(a, gr);
+                x[u] = make_uint4(0, 0, 0, 0);
+                if (i < ROWS * (DP / 8) && gr < all_rows && node < s.nodes && c * 8 < a.dim) {
+                    const char* p = a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + c * 16;
+                    if (a.q_vec) x[u] = *reinterpret_cast<const uint4*>(p);
+                    else {
+                        const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
+                        x[u] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                    }
                 }
             }
-            *reinterpret_cast<uint4*>(qs + (r / TC_ROWS) * Cfg::Q + (c >> 3) * TC_ROWS * 128 + (r % TC_ROWS) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * 256 + t, r = i / (DP / 8), c = i % (DP / 8);
+                if (i < ROWS * (DP / 8))
+                    *reinterpret_cast<uint4*>(qs + (r / TC_ROWS) * Cfg::Q + (c >> 3) * TC_ROWS * 128 + (r % TC_ROWS) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x[u];
+            }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         for (int w = t; w < a.words; w += 256) any[w] = 0;            // what they see (as ta_load_masks, by the threads from 128 on)
@@ -221,44 +245,50 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         const bool live = gr < a.T * a.group && node < s.nodes;
         const uint32_t* row = mask + (live ? (node - t0n) * a.words : 0);
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;                  // this warp's lanes: 32 (warp % 4) in bits 16..31
-        const uint32_t ts = tmem + g * 128 + lanes, to = tmem + 256 + g * DP + lanes;
+        const uint32_t ts = tmem + g * KT + lanes, to = tmem + 256 + g * DP + lanes;
         float m = -INFINITY, l = 0.f;
         for (int i = 0; i < n; ++i) {
             const int j = block_of(g, i), k0 = it.k_begin + j * KT;
-            ok = ok && wait(sfull + g * 8, taken + i);
+            ok = ok && wait(sfull + g * 8, taken + i);    // (and with it the last second product, which was issued before)
             if (!ok) break;
             tc_fence_after();
+            uint32_t x[KT / 32][32];                      // the row's scores
+#pragma unroll
+            for (int c = 0; c < KT / 32; ++c) tmem_ld_issue<32>(ts + c * 32, x[c]);
+#pragma unroll
+            for (int c = 0; c < KT / 32; ++c) tmem_ld_done<32>(x[c]);
             const bool tail = k0 + KT > s.len;
-            // the row's scores, 32 at a time and twice, for the maximum and for the exponentials; the next 32 are on their way meanwhile
-            uint32_t x[2][32];
-            auto hide = [&](uint32_t* x, int c) {
-                const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
+            if (tail) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = w >> e & 1 ? x[e] : 0xff800000u;
-            };
-            float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
-            tmem_ld_issue<32>(ts, x[0]);
+                for (int c = 0; c < KT / 32; ++c) {
+                    const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
 #pragma unroll
-            for (int c = 0; c < KT / 32; ++c) {
-                tmem_ld_done<32>(x[c & 1]);
-                tmem_ld_issue<32>(ts + (c + 1) % (KT / 32) * 32, x[(c + 1) & 1]);
-                if (tail) hide(x[c & 1], c);
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    auto y = [&](int q) { return __uint_as_float(x[c & 1][e + q]); };
-                    t0 = fmaxf(t0, fmaxf(y(0), y(1))); t1 = fmaxf(t1, fmaxf(y(2), y(3)));
-                    t2 = fmaxf(t2, fmaxf(y(4), y(5))); t3 = fmaxf(t3, fmaxf(y(6), y(7)));
+                    for (int e = 0; e < 32; ++e) x[c][e] = w >> e & 1 ? x[c][e] : 0xff800000u;
+                }
+                if (TILES == 1 || g == 0) {               // values that no query sees: whatever is in them is multiplied by 0
+                    const int st = (done + j) % NS;
+                    ok = wait(vfull + st * 8, (done + j) / NS);
+                    if (!ok) break;
+                    const uint32_t seen = ta_window(any, a.words, k0 + (warp & 3) * 32 - s.len);      // each of the group's warps a quarter of the rows
+                    for (int q = lane; q < 32 * 8 * HALVES; q += 32) {
+                        const int rr = q / 8 % 32, hf = q / 256;
+                        if (!(seen >> rr & 1)) *reinterpret_cast<uint4*>(vring + st * SIDE + hf * KT * 128 + ((warp & 3) * 32 + rr) * 128 + (q & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
             }
-            float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
-            top *= a.scale;
+            float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < KT; e += 2)
+                t4[e / 2 % 4] = fmaxf(t4[e / 2 % 4], fmaxf(__uint_as_float(x[e / 32][e % 32]), __uint_as_float(x[e / 32][e % 32 + 1])));
+            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale;
             const bool grow = top > (m == -INFINITY ? m : m + 8.f);
             if (__any_sync(0xffffffffu, grow)) {
                 const float f = grow ? ta_exp2(m - top) : 1.f;              // (m = -inf: 0)
                 if (grow) m = top;
                 l *= f;
                 if (i > 0) {
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < DP / 16; ++c) {
                         uint32_t y[16];
                         tmem_ld_issue<16>(to + c * 16, y);
@@ -267,45 +297,32 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                         for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[e]) * f);
                         tmem_st16(to + c * 16, y);
                     }
-                    tmem_st_wait();
                 }
             }
             const float z = m == -INFINITY ? 0.f : m;
             uint64_t sum[2] = {0, 0};                     // two pairs of fp32
             const uint64_t scale2 = pair2(a.scale, a.scale), z2 = pair2(-z, -z);
 #pragma unroll
-            for (int c = 0; c < KT / 32; ++c) {
-                uint32_t y[16];
-                tmem_ld_done<32>(x[c & 1]);
-                if (c + 1 < KT / 32) tmem_ld_issue<32>(ts + (c + 1) * 32, x[(c + 1) & 1]);
-                if (tail) hide(x[c & 1], c);
+            for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint64_t d = fma2(pair2(__uint_as_float(x[c & 1][2 * e]), __uint_as_float(x[c & 1][2 * e + 1])), scale2, z2);
-                    const float u = ta_exp2(__uint_as_float((uint32_t)d)), v = ta_exp2(__uint_as_float((uint32_t)(d >> 32)));
-                    sum[e & 1] = add2(sum[e & 1], pair2(u, v));
-                    y[e] = Half<T>::pack(u, v);
+                for (int c = hf * 2; c < hf * 2 + 2; ++c) {
+                    uint32_t y[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint64_t d = fma2(pair2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale2, z2);
+                        const float u = ta_exp2(__uint_as_float((uint32_t)d)), v = ta_exp2(__uint_as_float((uint32_t)(d >> 32)));
+                        sum[e & 1] = add2(sum[e & 1], pair2(u, v));
+                        y[e] = Half<T>::pack(u, v);
+                    }
+                    tmem_st16(ts + c * 16, y);
                 }
-                tmem_st16(ts + c * 16, y);                // over scores that have been read: columns 16 c .., the next 32 (c + 1) ..
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pready + g * 16 + hf * 8);
             }
             const uint64_t both = add2(sum[0], sum[1]);
             l += __uint_as_float((uint32_t)both) + __uint_as_float((uint32_t)(both >> 32));
-            if (tail && (TILES == 1 || g == 0)) {         // values that no query sees: whatever is in them is multiplied by 0
-                const int st = (done + j) % NS;
-                ok = wait(vfull + st * 8, (done + j) / NS);
-                if (!ok) break;
-                // (each of the group's warps a quarter of the rows)
-                const uint32_t seen = ta_window(any, a.words, k0 + (warp & 3) * 32 - s.len);
-                for (int q = lane; q < 32 * 8 * HALVES; q += 32) {
-                    const int rr = q / 8 % 32, hf = q / 256;
-                    if (!(seen >> rr & 1)) *reinterpret_cast<uint4*>(vring + st * SIDE + hf * KT * 128 + ((warp & 3) * 32 + rr) * 128 + (q & 7) * 16) = make_uint4(0, 0, 0, 0);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(pready + g * 8);
         }
         if (ok && n) ok = wait(ofin + g * 8, outputs++);
         taken += n;
@@ -326,13 +343,11 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
             }
         }
         if (TILES == 2 || g == 0) {
-            const bool real = gr < a.T * a.group;
+            // through this group's queries' place in shared memory, 128 rows of 128 bytes at a time, so that rows leave in whole lines
             const float inv = !it.whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
-            char* p = a.out + it.b * a.o_sb + node * a.o_st + (it.h * a.group + gr - node * a.group) * a.o_sh;
-            const long long slot = it.slot * ROWS + r;
-#pragma unroll
-            for (int c = 0; c < DP / 32; ++c) {
-                float x[32];
+            char* stage = qs + (TILES == 2 ? g : 0) * Cfg::Q;
+            auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(3 + g) : "memory"); };
+            auto columns = [&](int c, float* x) {         // 32 columns of this thread's row
                 if (n) tmem_ld32(to + c * 32, x);
 #pragma unroll
                 for (int e = 0; e < 32; ++e) x[e] = n && f != 0.f ? x[e] * f : 0.f;
@@ -344,26 +359,48 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                 }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) x[e] *= inv;
-                if (!real) continue;
-                if (it.whole) {
+            };
+            const int per = it.whole ? 64 : 32;           // columns of 128 bytes
+            for (int c0 = 0; c0 < a.dim; c0 += per) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        if (c * 32 + e >= a.dim) break;
-                        uint32_t y[4];
+                for (int hf = 0; hf < 2; ++hf) {
+                    if (hf && !it.whole) break;
+                    float x[32];
+                    columns(c0 / 32 + hf, x);
+                    if (it.whole) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) y[q] = Half<T>::pack(x[e + 2 * q], x[e + 2 * q + 1]);
-                        if (a.out_vec) *reinterpret_cast<uint4*>(p + (c * 32 + e) * 2) = make_uint4(y[0], y[1], y[2], y[3]);
-                        else
+                        for (int q = 0; q < 4; ++q)
+                            *reinterpret_cast<uint4*>(stage + rr * 128 + (((hf * 4 + q) ^ (rr & 7)) << 4)) =
+                                make_uint4(Half<T>::pack(x[8 * q], x[8 * q + 1]), Half<T>::pack(x[8 * q + 2], x[8 * q + 3]), Half<T>::pack(x[8 * q + 4], x[8 * q + 5]),
+                                           Half<T>::pack(x[8 * q + 6], x[8 * q + 7]));
+                    } else {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) reinterpret_cast<unsigned short*>(p + (c * 32 + e) * 2)[q] = (unsigned short)(y[q / 2] >> (q & 1) * 16);
+                        for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(stage + rr * 128 + ((q ^ (rr & 7)) << 4)) = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        if (c * 32 + e < a.dim) *reinterpret_cast<float4*>(a.part + slot * a.dim + c * 32 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                 }
+                group_sync();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {             // a warp: its 32 rows, four at a time
+                    const int row_in = (warp & 3) * 32 + k * 4 + (lane >> 3), piece = lane & 7, r_out = r - rr + row_in, g_out = r0 + r_out;
+                    const int col = c0 + piece * (per / 8);
+                    if (g_out >= all_rows || col >= a.dim) continue;
+                    const uint4 y = *reinterpret_cast<const uint4*>(stage + row_in * 128 + ((piece ^ (row_in & 7)) << 4));
+                    if (it.whole) {
+                        const int nd = ta_node(a, g_out);
+                        char* p = a.out + it.b * a.o_sb + nd * a.o_st + (it.h * a.group + g_out - nd * a.group) * a.o_sh + col * 2;
+                        if (a.out_vec) *reinterpret_cast<uint4*>(p) = y;
+                        else {
+                            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) reinterpret_cast<unsigned short*>(p)[q] = (unsigned short)(w[q / 2] >> (q & 1) * 16);
+                        }
+                    } else {
+                        *reinterpret_cast<uint4*>(a.part + (it.slot * ROWS + r_out) * a.dim + col) = y;
+                    }
+                }
+                group_sync();
             }
-            if (real && !it.whole) a.part_ml[slot] = make_float2(m, l);
+            if (gr < all_rows && !it.whole) a.part_ml[it.slot * ROWS + r] = make_float2(m, l);
         }
         softmax_warps();                                  // queries and masks may be overwritten
         }

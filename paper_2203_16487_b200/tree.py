@@ -21,28 +21,19 @@ import torch
 from .binding import Cache, SpecDecError, TreeAttentionArgs, lib
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_I32 = torch.int32
+_raw_stream = torch._C._cuda_getCurrentRawStream           # torch.cuda.current_stream(i).cuda_stream, 3 us cheaper: small calls are bounded by the host
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _fail(rc):
+    raise SpecDecError(rc, lib().specdec_last_error(None).decode())
 
 
-def _check(rc):
-    if rc < 0:
-        raise SpecDecError(rc, lib().specdec_last_error(None).decode())
-    return rc
-
-
-def _ints(name, t, *shape):
-    """A contiguous int32 device tensor of that shape (None: any extent)."""
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or len(t.shape) != len(shape) or any(
-            n is not None and m != n for m, n in zip(t.shape, shape)):
-        raise ValueError(f"{name}: a contiguous int32 device tensor of shape {shape} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _opt(name, t, *shape):
-    return None if t is None else _ints(name, t, *shape)
+def _ints(name, t, shape):
+    """Address of a contiguous int32 device tensor of that shape."""
+    if t.dtype is _I32 and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: a contiguous int32 device tensor of shape {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class PagedCache:
@@ -68,48 +59,66 @@ class PagedCache:
             raise ValueError("kv: a device tensor [n_layers, 2, n_pages, page_tokens, n_heads, head_dim] with a contiguous last dimension is wanted")
         L, _, P, page, H, D = kv.shape
         n_seqs = length.numel()
-        _ints("table", table, n_seqs, None), _ints("length", length, n_seqs), _ints("held", held, n_seqs), _ints("refs", refs, P)
+        _ints("table", table, (n_seqs, table.shape[1])), _ints("length", length, (n_seqs,)), _ints("held", held, (n_seqs,)), _ints("refs", refs, (P,))
         self.kv, self.table, self.length, self.held, self.refs = kv, table, length, held, refs
         self.status = torch.zeros(1, dtype=torch.int32, device=kv.device)
-        n = _check(lib().specdec_cache_scratch(n_seqs, table.shape[1], P))
+        n = lib().specdec_cache_scratch(n_seqs, table.shape[1], P)
+        if n < 0:
+            _fail(n)
         self._scratch = torch.zeros(n, dtype=torch.int32, device=kv.device)
         s = kv.stride()
         self._c = Cache(kv.data_ptr(), DTYPES[kv.dtype], L, H, D, P, page, n_seqs, table.shape[1], s[0], s[1], s[2], s[3], s[4],
                         table.data_ptr(), length.data_ptr(), held.data_ptr(), refs.data_ptr(), self.status.data_ptr(), self._scratch.data_ptr())
-        self._ref = C.byref(self._c)
+        self._ref, self._lib, self._device = C.byref(self._c), lib(), kv.get_device()
+        self._code, self._page = DTYPES[kv.dtype], page
         self.dtype, self.n_heads, self.head_dim, self.max_length = kv.dtype, H, D, table.shape[1] * page
 
     def reserve(self, seqs, n_tokens: int):
         """Pages for n_tokens tokens behind the committed ones."""
-        _check(lib().specdec_cache_reserve(self._ref, _ints("seqs", seqs, None), seqs.numel(), n_tokens, _stream()))
+        n = seqs.numel()
+        rc = self._lib.specdec_cache_reserve(self._ref, _ints("seqs", seqs, (n,)), n, n_tokens, _raw_stream(self._device))
+        if rc:
+            _fail(rc)
 
     def append(self, seqs, k, v, layer: Optional[int] = None, count=None):
         """Writes k, v [n, T, n_heads, head_dim] (layer=None: [n_layers, n, T, n_heads, head_dim], every layer) behind the committed tokens; of
         sequence i the first count[i] of the T.  Lengths stay: compact moves them."""
-        if layer is not None:
-            k, v = k.unsqueeze(0), v.unsqueeze(0)
-        n = seqs.numel()
-        if k.shape != v.shape or k.stride() != v.stride() or k.dim() != 5 or k.dtype != self.dtype or v.dtype != self.dtype or k.stride(4) != 1 \
-                or not k.is_cuda or not v.is_cuda or k.shape[0] != (1 if layer is not None else self._c.n_layers) or k.shape[1] != n \
-                or k.shape[3] != self.n_heads or k.shape[4] != self.head_dim:
+        n, shape, s = seqs.numel(), k.shape, k.stride()
+        if layer is None:
+            layer, layers = 0, self._c.n_layers
+            good = len(shape) == 5 and shape[0] == layers
+        else:
+            layers, shape, s = 1, (1,) + tuple(shape), (0,) + tuple(s)
+            good = len(shape) == 5
+        if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.is_cuda and v.is_cuda
+                and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
             raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")
-        s = k.stride()
-        _check(lib().specdec_cache_append(self._ref, _ints("seqs", seqs, None), n, layer or 0, k.shape[0], k.data_ptr(), v.data_ptr(), k.shape[2],
-                                          s[0], s[1], s[2], s[3], _opt("count", count, n), _stream()))
+        rc = self._lib.specdec_cache_append(self._ref, _ints("seqs", seqs, (n,)), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2], s[0], s[1], s[2], s[3],
+                                            None if count is None else _ints("count", count, (n,)), _raw_stream(self._device))
+        if rc:
+            _fail(rc)
 
     def compact(self, seqs, path, n_path):
         """Commits the nodes path[i, :n_path[i]] of each sequence's block and gives back the pages behind them."""
-        n = seqs.numel()
-        _check(lib().specdec_cache_compact(self._ref, _ints("seqs", seqs, None), n, _ints("path", path, n, None), path.shape[1],
-                                           _ints("n_path", n_path, n), _stream()))
+        n, T = seqs.numel(), path.shape[-1]
+        rc = self._lib.specdec_cache_compact(self._ref, _ints("seqs", seqs, (n,)), n, _ints("path", path, (n, T)), T, _ints("n_path", n_path, (n,)),
+                                             _raw_stream(self._device))
+        if rc:
+            _fail(rc)
 
     def release(self, seqs):
         """Gives back all pages of the sequences; their lengths are 0."""
-        _check(lib().specdec_cache_release(self._ref, _ints("seqs", seqs, None), seqs.numel(), _stream()))
+        n = seqs.numel()
+        rc = self._lib.specdec_cache_release(self._ref, _ints("seqs", seqs, (n,)), n, _raw_stream(self._device))
+        if rc:
+            _fail(rc)
 
     def fork(self, src, dst):
         """Sequence dst[i] becomes a copy of what src[i] was before the call: full pages shared, the last, partly filled one copied."""
-        _check(lib().specdec_cache_fork(self._ref, _ints("src", src, None), _ints("dst", dst, src.numel()), src.numel(), _stream()))
+        n = src.numel()
+        rc = self._lib.specdec_cache_fork(self._ref, _ints("src", src, (n,)), _ints("dst", dst, (n,)), n, _raw_stream(self._device))
+        if rc:
+            _fail(rc)
 
     def check(self):
         """Raises if a call found too few pages or bad numbers since the last check (waits for the stream)."""
@@ -124,19 +133,25 @@ class PagedCache:
 def ancestors(parents, n_nodes=None):
     """(mask [B, T, ceil(T / 32)] int32 of ancestor bits, depth [B, T] int32) of trees given by their parents [B, T]."""
     B, T = parents.shape
-    mask = torch.empty(B, T, (T + 31) // 32, dtype=torch.int32, device=parents.device)
-    depth = torch.empty(B, T, dtype=torch.int32, device=parents.device)
-    _check(lib().specdec_tree_ancestors(_ints("parents", parents, None, None), _opt("n_nodes", n_nodes, B), B, T, mask.data_ptr(), depth.data_ptr(), _stream()))
+    p = _ints("parents", parents, (B, T))
+    mask, depth = parents.new_empty((B, T, (T + 31) // 32)), torch.empty_like(parents)
+    rc = lib().specdec_tree_ancestors(p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)), B, T, mask.data_ptr(), depth.data_ptr(),
+                                      _raw_stream(parents.get_device()))
+    if rc:
+        _fail(rc)
     return mask, depth
 
 
 def accept(parents, tokens, sampled, n_nodes=None):
     """(path [B, T], n_path [B], emitted [B, T]): the nodes from the root along the sampled tokens, and the sampled token of each (-1 behind)."""
-    B, T = parents.shape
-    path, emitted = torch.empty_like(parents), torch.empty_like(parents)
-    n_path = torch.empty(B, dtype=torch.int32, device=parents.device)
-    _check(lib().specdec_tree_accept(_ints("parents", parents, None, None), _ints("tokens", tokens, B, T), _ints("sampled", sampled, B, T),
-                                     _opt("n_nodes", n_nodes, B), B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _stream()))
+    shape = parents.shape
+    B, T = shape
+    p = _ints("parents", parents, shape)
+    path, emitted, n_path = torch.empty_like(parents), torch.empty_like(parents), parents.new_empty((B,))
+    rc = lib().specdec_tree_accept(p, _ints("tokens", tokens, shape), _ints("sampled", sampled, shape), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)),
+                                   B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _raw_stream(parents.get_device()))
+    if rc:
+        _fail(rc)
     return path, n_path, emitted
 
 
@@ -144,48 +159,58 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     """Attention of tree nodes q [B, T, n_q_heads, head_dim] over the committed tokens of sequences seqs [B] and, by mask [B or 1, T, ceil(T / 32)], over
     the block's nodes (appended before).  max_length: an upper bound of the committed lengths, if known.  scale: 1 / sqrt(head_dim)."""
     B, T, H, D = q.shape
-    if q.dtype != cache.dtype or D != cache.head_dim or q.stride(3) != 1 or not q.is_cuda:
+    sq = q.stride()
+    if q.dtype is not cache.dtype or D != cache.head_dim or sq[3] != 1 or not q.is_cuda:
         raise ValueError(f"q: a device tensor [B, T, heads, {cache.head_dim}] of {cache.dtype} with a contiguous last dimension is wanted")
     if out is None:
-        out = torch.empty((B, T, H, D), dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.stride(3) != 1 or not out.is_cuda:
+        out = q.new_empty((B, T, H, D))
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(3) != 1 or not out.is_cuda:
         raise ValueError("out: of q's shape and type, with a contiguous last dimension")
-    W = (T + 31) // 32
-    m = _ints("mask", mask, None, T, W)
-    if mask.shape[0] != B and mask.shape[0] != 1:
-        raise ValueError("mask: one for each row of q, or one for all")
-    bound = min(max_length, cache.max_length) if max_length > 0 else cache.max_length
-    n = _check(lib().specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._c.dtype, cache._c.page_tokens, bound))
+    W, so = (T + 31) // 32, out.stride()
+    one = mask.shape[0] == 1
+    m = _ints("mask", mask, (1 if one else B, T, W))
+    bound = cache.max_length
+    if 0 < max_length < bound:
+        bound = max_length
+    L = cache._lib
+    n = L.specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._code, cache._page, bound)
+    if n < 0:
+        _fail(n)
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    sq, so = q.stride(), out.stride()
-    a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, B), m,
-                          0 if mask.shape[0] == 1 else T * W, _opt("n_nodes", n_nodes, B), bound, D ** -0.5 if scale is None else scale,
+    a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, (B,)), m,
+                          0 if one else T * W, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)), bound, D ** -0.5 if scale is None else scale,
                           ws.data_ptr() if n else None, n)
-    _check(lib().specdec_tree_attention(cache._ref, C.byref(a), _stream()))
+    rc = L.specdec_tree_attention(cache._ref, C.byref(a), _raw_stream(cache._device))
+    if rc:
+        _fail(rc)
     return out
 
 
 def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None):
     """One token for each row of logits [..., V] (the last dimension contiguous, rows evenly spaced) from uniform [...] fp32 in [0, 1): (token int32 [...], log
     probability fp32 [...]).  The parameters (fp32, top_k int32; None: off) are tensors of one entry for each row, or for each equal run of rows ([n] for logits [n, T, V])."""
-    V = logits.shape[-1]
-    flat = logits.reshape(-1, V) if logits.dim() != 2 else logits
-    rows = flat.shape[0]
-    if logits.dtype not in DTYPES or not logits.is_cuda or flat.stride(1) != 1:
+    shape = logits.shape
+    V, lead = shape[-1], shape[:-1]
+    if logits.dtype not in DTYPES or not logits.is_cuda or logits.stride(-1) != 1:
         raise ValueError("logits: a device tensor of fp32, bf16 or fp16 with a contiguous last dimension is wanted")
-    if uniform.shape != logits.shape[:-1] or uniform.dtype != torch.float32 or not uniform.is_cuda or not uniform.is_contiguous():
+    flat = logits if len(shape) == 2 else logits.reshape(-1, V)
+    rows = flat.shape[0]
+    if uniform.shape != lead or uniform.dtype is not torch.float32 or not uniform.is_cuda or not uniform.is_contiguous():
         raise ValueError("uniform: a contiguous fp32 device tensor, one number a row, is wanted")
-    n, ptrs = None, []
-    for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+    n, ptrs = 0, []
+    for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, _I32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
         if t is None:
             ptrs.append(None)
             continue
-        if t.dtype != dt or not t.is_cuda or not t.is_contiguous() or t.numel() < 1 or rows % t.numel() or n not in (None, t.numel()):
+        m = t.numel()
+        if t.dtype is not dt or not t.is_cuda or not t.is_contiguous() or m < 1 or rows % m or (n and n != m):
             raise ValueError(f"{name}: a contiguous {dt} device tensor is wanted, one entry for each equal run of rows, as many as the other parameters")
-        n = t.numel()
+        n = m
         ptrs.append(t.data_ptr())
-    token = torch.empty(uniform.shape, dtype=torch.int32, device=logits.device)
-    logprob = torch.empty(uniform.shape, dtype=torch.float32, device=logits.device)
-    _check(lib().specdec_sample(flat.data_ptr(), DTYPES[logits.dtype], flat.stride(0) if rows > 1 else V, rows, V, uniform.data_ptr(), *ptrs,
-                                rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _stream()))
+    logprob = torch.empty_like(uniform)
+    token = torch.empty_like(uniform, dtype=_I32)
+    rc = lib().specdec_sample(flat.data_ptr(), DTYPES[logits.dtype], flat.stride(0) if rows > 1 else V, rows, V, uniform.data_ptr(), *ptrs,
+                              rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _raw_stream(logits.get_device()))
+    if rc:
+        _fail(rc)
     return token, logprob
