@@ -130,27 +130,37 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
         __syncthreads();
         const int r0 = it.tile * TF_ROWS, all_rows = a.T * a.group, t0 = ta_node(a, r0);
         const SeqKeys& s = it.s;
-        for (int i = tid; i < TF_ROWS * DP; i += NT) {
-            const int r = i / DP, d = i % DP, gr = r0 + r, node = ta_node(a, gr);
-            float v = 0.f;
-            if (gr < all_rows && node < s.nodes && d < a.dim) v = *reinterpret_cast<const float*>(a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + d * 4);
-            q[r * KP + d] = v;
+        const int blocks = (it.k_end - it.k_begin + TF_KT - 1) / TF_KT;
+        auto page_of = [&](int j) -> int {                // of this lane's key in block j
+            const int key = it.k_begin + j * TF_KT + lane, pi = key >> a.page_shift;
+            return j < blocks && key < it.k_end && pi < a.max_pages ? a.table[(long long)s.seq * a.max_pages + pi] : -1;
+        };
+        auto offset = [&](int j, int page) -> long long { // of the key itself; -1: zeros instead
+            const int key = it.k_begin + j * TF_KT + lane;
+            return (unsigned)page < (unsigned)a.n_pages && ta_seen(any, s, key) ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + it.h * a.s_head : -1;
+        };
+        int page = page_of(warp);
+#pragma unroll
+        for (int i0 = 0; i0 < TF_ROWS * (DP / 4); i0 += NT) {
+            const int i = i0 + tid, r = i / (DP / 4), d = i % (DP / 4) * 4, gr = r0 + r, node = ta_node(a, gr);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (gr < all_rows && node < s.nodes && d < a.dim) {
+                const float* p = reinterpret_cast<const float*>(a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh) + d;
+                v = a.q_vec ? *reinterpret_cast<const float4*>(p) : make_float4(p[0], p[1], p[2], p[3]);
+            }
+            *reinterpret_cast<float4*>(q + r * KP + d) = v;
         }
         if (a.dim < DP)                                   // columns beyond the head
             for (int i = lane; i < 2 * TF_KT * (DP - a.dim); i += 32) kt[i / (DP - a.dim) * KP + a.dim + i % (DP - a.dim)] = 0.f;
         ta_load_masks<NT, 0>(a, it.b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
-        const int blocks = (it.k_end - it.k_begin + TF_KT - 1) / TF_KT;
-        auto offset = [&](int j) -> long long {           // of this lane's key in block j; -1: zeros instead
-            const int key = it.k_begin + j * TF_KT + lane, pi = key >> a.page_shift;
-            int page = -1;
-            if (j < blocks && key < it.k_end && ta_seen(any, s, key) && pi < a.max_pages) page = a.table[(long long)s.seq * a.max_pages + pi];
-            return (unsigned)page < (unsigned)a.n_pages ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + it.h * a.s_head : -1;
-        };
         auto fetch = [&](float* to, const char* base, long long off) {
-            for (int i = lane; i < TF_KT * chunks; i += 32) {
-                const int r = i / chunks, c = i - r * chunks;
+#pragma unroll
+            for (int r0 = 0; r0 < TF_KT; r0 += 4) {       // four keys at a time, eight lanes each
+                const int r = r0 + rg;
                 const long long o = __shfl_sync(0xffffffffu, off, r);
-                ta_copy16(smem_u32(to + r * KP + c * 4), base + (o < 0 ? 0 : o + c * 16), o >= 0);
+#pragma unroll
+                for (int c = x; c < DP / 4; c += 8)
+                    if (c < chunks) ta_copy16(smem_u32(to + r * KP + c * 4), base + (o < 0 ? 0 : o + c * 16), o >= 0);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
@@ -167,11 +177,11 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
 #pragma unroll
             for (int c = 0; c < DC; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        long long off = offset(warp);
+        long long off = offset(warp, page);
         fetch(kt, a.k, off);
         for (int j = warp; j < blocks; j += WK) {
             fetch(vt, a.v, off);
-            off = offset(j + WK);
+            page = page_of(j + WK);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
             float sc[4][4];                               // [row][key x + 8 i]
@@ -193,6 +203,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
                         sc[i][e] = fmaf(qv[i].x, kv[e].x, fmaf(qv[i].y, kv[e].y, fmaf(qv[i].z, kv[e].z, fmaf(qv[i].w, kv[e].w, sc[i][e]))));
             }
             __syncwarp();
+            off = offset(j + WK, page);
             fetch(kt, a.k, off);
             const int base = it.k_begin + j * TF_KT - s.len;
 #pragma unroll
