@@ -99,20 +99,21 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
 }
 
 // ------------------------------------------------------------------ fp32: FFMA
-// CTA = WK warps over the same 16 rows, each with every WK-th block of 32 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
-// another warp until the results meet).  Lane (rg, x): four rows, for the scores the keys x + 8 i, for the output the columns 4 x + 32 c.  The next block's keys are
+// CTA = WK warps over the same 16 rows, each with every WK-th block of 16 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
+// another warp until the results meet).  Lane (rg, x): four rows, for the scores the keys x and x + 8, for the output the columns 4 x + 32 c.  The next block's keys are
 // fetched under this block's second product, its values under the next scores.  A call of few rows is bounded by the chain of one warp, one of many
-// by the fused multiply-adds and the shared-memory reads that feed them (8 of 16 bytes for 64).
-constexpr int TF_ROWS = 16, TF_KT = 32;
+// by the fused multiply-adds and the shared-memory reads that feed them (6 of 16 bytes for 32).  (8 warps with blocks of 32 keys, two to a scheduler:
+// 20.5 us for 8 x 9 queries over 300 to 512 keys.)
+constexpr int TF_ROWS = 16, TF_KT = 16;
 template <int DP> struct TfCfg {
-    static constexpr int WK = DP > 64 ? 4 : 8, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
+    static constexpr int WK = DP > 64 ? 8 : 16, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
     static constexpr int WARP = 2 * TF_KT * KP + TF_ROWS * PP;                         // a warp's keys, values and probabilities
     static constexpr int FLOATS = TF_ROWS * KP + WK * WARP;
 };
 template <int DP>
 __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
     using Cfg = TfCfg<DP>;
-    constexpr int WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32;
+    constexpr int WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32, KE = TF_KT / 8;
     extern __shared__ __align__(128) char sm[];
     float* q = reinterpret_cast<float*>(sm);              // [16][KP]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rg = lane >> 3, x = lane & 7;
@@ -132,11 +133,11 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
         const SeqKeys& s = it.s;
         const int blocks = (it.k_end - it.k_begin + TF_KT - 1) / TF_KT;
         auto page_of = [&](int j) -> int {                // of this lane's key in block j
-            const int key = it.k_begin + j * TF_KT + lane, pi = key >> a.page_shift;
+            const int key = it.k_begin + j * TF_KT + lane % TF_KT, pi = key >> a.page_shift;
             return j < blocks && key < it.k_end && pi < a.max_pages ? a.table[(long long)s.seq * a.max_pages + pi] : -1;
         };
         auto offset = [&](int j, int page) -> long long { // of the key itself; -1: zeros instead
-            const int key = it.k_begin + j * TF_KT + lane;
+            const int key = it.k_begin + j * TF_KT + lane % TF_KT;
             return (unsigned)page < (unsigned)a.n_pages && ta_seen(any, s, key) ? page * a.s_page + (key & ((1 << a.page_shift) - 1)) * a.s_token + it.h * a.s_head : -1;
         };
         int page = page_of(warp);
@@ -184,22 +185,22 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
             page = page_of(j + WK);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
-            float sc[4][4];                               // [row][key x + 8 i]
+            float sc[4][KE];                              // [row][key x + 8 e]
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[i][e] = 0.f;
+                for (int e = 0; e < KE; ++e) sc[i][e] = 0.f;
 #pragma unroll 4
             for (int d = 0; d < DP; d += 4) {
-                float4 qv[4], kv[4];
+                float4 qv[4], kv[KE];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(q + (rg * 4 + i) * KP + d);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) kv[e] = *reinterpret_cast<const float4*>(kt + (x + 8 * e) * KP + d);
+                for (int e = 0; e < KE; ++e) kv[e] = *reinterpret_cast<const float4*>(kt + (x + 8 * e) * KP + d);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < KE; ++e)
                         sc[i][e] = fmaf(qv[i].x, kv[e].x, fmaf(qv[i].y, kv[e].y, fmaf(qv[i].z, kv[e].z, fmaf(qv[i].w, kv[e].w, sc[i][e]))));
             }
             __syncwarp();
@@ -211,18 +212,18 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
                 const uint32_t w = live[i] ? ta_window(row[i], a.words, base) : 0u;
                 float top = -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < KE; ++e) {
                     sc[i][e] = w >> (x + 8 * e) & 1 ? sc[i][e] * a.scale : -INFINITY;
                     top = fmaxf(top, sc[i][e]);
                 }
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)); top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 top = fmaxf(top, m[i]);
-                const float z = top == -INFINITY ? 0.f : top, f = exp2f(m[i] - z);
+                const float z = top == -INFINITY ? 0.f : top, f = ta_exp2(m[i] - z);
                 m[i] = top;
                 l[i] *= f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = exp2f(sc[i][e] - z);
+                for (int e = 0; e < KE; ++e) {
+                    const float p = ta_exp2(sc[i][e] - z);
                     l[i] += p;
                     pt[(rg * 4 + i) * PP + x + 8 * e] = p;
                 }
