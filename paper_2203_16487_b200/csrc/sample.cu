@@ -3,14 +3,17 @@
 // Weights are whole numbers of 2^-40 of the largest, so every sum is exact and neither the order of atomics nor the split of the work can
 // change a token.  With x = (l - max) / T falling along the order of the logits, an entry's weight is 0 beyond x = -27.73.
 //
-// One CTA a row, which it reads from memory once: the row stays in shared memory, rows beyond that are read again (from L2).  What a row goes through depends on
-// its parameters:
+// A row is read from memory once, into the shared memory of one CTA or, where rows are few or long, of a cluster of up to 8, each with an equal stretch.  What a row
+// goes through depends on its parameters:
 //   greedy  the first index of the maximum.
-//   few     top-k of at most SA_FEW.  The k-th largest of the threads' own maxima is a bound below the k-th largest entry, so only the entries above it are
-//           looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No exponential of the others is taken.
-//   order   other cuts: a histogram over 2048 equal steps of x gives the step in which the cut falls; that step's range of logits (as ordered integers) is split
-//           into 2048 again until a bin is one value: entries equal to it have equal weights, so how many of them stay is arithmetic; which, is by index.
-//   then    the kept weights by stretches of the row, one a warp, then of the stretch that holds the goal, then entry by entry.
+//   few     top-k of at most SA_FEW.  The k-th largest of a CTA's threads' own maxima is a bound below the k-th largest entry, so only the entries above the best such
+//           bound are looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No exponential of the others is taken.
+//   order   other cuts: a histogram over 1024 equal steps of x gives the step in which the cut falls, and a list of that step's entries, ranked by counting,
+//           the cut itself.  (More entries in a step than the list holds: that step's range of logits, as ordered integers, is split into 1024 again until a bin is
+//           one value; entries equal to it have equal weights, so how many of them stay is arithmetic; which, is by index.)
+//   then    the kept weights by stretches of the row, one a warp, and the goal's stretch entry by entry.
+//
+// Per entry the exponential and its two whole parts are some 20 instructions; the histogram adds one atomic (shared memory takes about ten lanes a clock).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -23,7 +26,7 @@ namespace sd {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int SA_BINS = 2048, SA_FEW = 128, SA_LIST = 1024;
+constexpr int SA_BINS = 1024, SA_FEW = 128, SA_LIST = 512;
 constexpr float SA_RANGE = 27.75f;                        // e^-27.73 = 2^-40
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -85,59 +88,114 @@ __device__ __forceinline__ u64 warp_scan(u64 v) {
 }
 
 struct Hist {
-    uint32_t cnt[SA_BINS], lo[SA_BINS], hi[SA_BINS];      // entries; weight as two words
+    uint32_t cnt[SA_BINS], lo[SA_BINS + 32], hi[SA_BINS]; // entries; weight as two words (bins beyond the last: a lane each for what weighs nothing)
     template <int NT> __device__ __forceinline__ void clear() { for (int i = threadIdx.x; i < SA_BINS; i += NT) { cnt[i] = 0; lo[i] = 0; hi[i] = 0; } }
-    __device__ __forceinline__ void add(int b, u64 u) {   // (most weights are below 2^32 units: one addition)
-        const uint32_t l = (uint32_t)u, old = atomicAdd(lo + b, l);
-        const uint32_t h = (uint32_t)(u >> 32) + (old + l < old);
+    __device__ __forceinline__ u64 sum(int b) const { return (u64)hi[b] << 32 | lo[b]; }
+    __device__ __forceinline__ void add(int b, u64 u) {
+        const uint32_t l = (uint32_t)u, old = atomicAdd(lo + b, l), h = (uint32_t)(u >> 32) + (old + l < old);
         if (h) atomicAdd(hi + b, h);
     }
-    __device__ __forceinline__ u64 sum(int b) const { return (u64)hi[b] << 32 | lo[b]; }
 };
-struct List {                                             // the entries that may be among the k largest
-    u64 any[SA_LIST], sorted[SA_FEW], units[SA_FEW], part[8][SA_FEW];
+template <int NT> struct Shared {
+    union {
+        Hist h;
+        struct { u64 units[SA_FEW], part[8][SA_FEW]; };   // few, once the histogram of maxima has been searched
+    };
+    u64 any[SA_LIST], sorted[SA_LIST];                    // entries as key << 32 | ~index: the order's composite
     int rank[SA_LIST];
+    u64 w_sum[32];
+    int w_cnt[32];
+    float w_max[32];
+    // what the CTAs of a cluster tell one another (each written once between two barriers)
+    float x_top, x_bound;
+    int x_first, x_bin, x_n;
+    u64 x_cnt, x_sum, x_cnt_before, x_sum_before, x_all, x_total;
+    // answers
+    int bin, n_list, index, winner;
+    u64 cnt_before, sum_before, total, cut, cut_sum;
 };
 
-template <int NT> struct Shared {
-    union { Hist h; List list; };
-    u64 w_sum[NT / 32];
-    int w_cnt[NT / 32];
-    float w_max[NT / 32];
-    // a search's answer
-    int bin; u64 cnt_before, sum_before;
-    int index, n_list, n_kept;
-    u64 total;
+// The CTAs of a row: their barrier, and the shared memory of the others.
+template <int C> struct Group {
+    int rank;
+    __device__ __forceinline__ Group() { if (C > 1) asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank)); else rank = 0; }
+    __device__ __forceinline__ void sync() const { if (C > 1) tc_cluster_sync(); else __syncthreads(); }
+    template <typename S> __device__ __forceinline__ S* of(S* mine, int r) const {
+        if (C == 1) return mine;
+        u64 p;
+        asm("mapa.u64 %0, %1, %2;" : "=l"(p) : "l"((u64)mine), "r"(r));
+        return (S*)p;
+    }
 };
+// Sum over the warps ahead of this one, and over all, of what each warp's lane 0 left in v[].
+template <int NT, typename V> __device__ __forceinline__ V warps_before(const V* v, V& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    V x = lane < NT / 32 ? v[lane] : V(0);
+    const V own = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const V y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+    all = __shfl_sync(0xffffffffu, x, 31);
+    return __shfl_sync(0xffffffffu, x - own, warp);
+}
 
 // First bin, in ascending order, behind which the search ends: by entries (the bin that holds entry number `k` from 1) or by weight (the last bin of any
-// weight with sum_before + weight ahead < thr).  Entries and weight ahead of it in sh.*_before, added to what was given.  sh.bin = -1: none (k beyond all).
-template <int NT>
-__device__ void find_bin(Shared<NT>& sh, bool by_weight, u64 k, double thr, u64 cnt0, u64 sum0) {
-    constexpr int PER = SA_BINS / NT;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    u64 c = 0, s = 0;
+// weight with weight ahead < thr), over the histograms of C CTAs (1: this one's alone).  sh.cnt_before / sum_before: what is ahead of it, added to what was given.  sh.bin = -1: none
+// (k beyond all).  Each CTA searches its share of the bins.
+template <int NT, int C>
+__device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u64 k, double thr, u64 cnt0, u64 sum0) {
+    constexpr int SHARE = SA_BINS / C, PER = SHARE >= NT ? SHARE / NT : 1;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = cta.rank * SHARE + threadIdx.x * PER;
+    const bool mine = threadIdx.x * PER < SHARE;
+    uint32_t n[PER];
+    u64 w[PER], c = 0, s = 0;
+    cta.sync();                                           // the histograms are complete
 #pragma unroll
-    for (int j = 0; j < PER; ++j) { c += sh.h.cnt[threadIdx.x * PER + j]; s += sh.h.sum(threadIdx.x * PER + j); }
-    u64 ic = warp_scan(c), is = warp_scan(s);
+    for (int j = 0; j < PER; ++j) { n[j] = 0; w[j] = 0; }
+    if (mine)
+#pragma unroll
+        for (int r = 0; r < C; ++r) {
+            const Hist* h = cta.of(&sh.h, r);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) { n[j] += h->cnt[b0 + j]; w[j] += h->sum(b0 + j); }
+        }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) { c += n[j]; s += w[j]; }
+    const u64 ic = warp_scan(c), is = warp_scan(s);
     if (lane == 31) { sh.w_cnt[warp] = (int)ic; sh.w_sum[warp] = is; }
     if (threadIdx.x == 0) sh.bin = -1;
     __syncthreads();
-    u64 bc = cnt0 + ic - c, bs = sum0 + is - s;
-    for (int w = 0; w < warp; ++w) { bc += sh.w_cnt[w]; bs += sh.w_sum[w]; }
-    int mine = -1;
+    int cta_c;
+    u64 cta_s;
+    u64 bc = cnt0 + warps_before<NT>(sh.w_cnt, cta_c) + ic - c, bs = sum0 + warps_before<NT>(sh.w_sum, cta_s) + is - s;
+    if (C > 1) {                                          // shares ahead of this CTA's
+        if (threadIdx.x == 0) { sh.x_cnt = cta_c; sh.x_sum = cta_s; }
+        cta.sync();
+        for (int r = 0; r < cta.rank; ++r) { const Shared<NT>* o = cta.of(&sh, r); bc += o->x_cnt; bs += o->x_sum; }
+    }
+    int found = -1;
     u64 mc = 0, ms = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        const int b = threadIdx.x * PER + j;
-        const u64 n = sh.h.cnt[b], w = sh.h.sum(b);
-        if (by_weight ? w && (double)bs < thr : (bc < k && k <= bc + n)) { mine = b; mc = bc; ms = bs; }
-        bc += n; bs += w;
+        if (by_weight ? w[j] && (double)bs < thr : (bc < k && k <= bc + n[j])) { found = b0 + j; mc = bc; ms = bs; }
+        bc += n[j]; bs += w[j];
     }
-    if (mine >= 0) atomicMax(&sh.bin, mine);
+    if (found >= 0) atomicMax(&sh.bin, found);
     __syncthreads();
-    if (mine >= 0 && sh.bin == mine) { sh.cnt_before = mc; sh.sum_before = ms; }
+    if (found >= 0 && sh.bin == found) { sh.cnt_before = mc; sh.sum_before = ms; }
     __syncthreads();
+    if (C > 1) {                                          // of the CTAs' answers the last
+        if (threadIdx.x == 0) { sh.x_bin = sh.bin; sh.x_cnt_before = sh.cnt_before; sh.x_sum_before = sh.sum_before; }
+        cta.sync();
+        if (threadIdx.x == 0) {
+            int best = -1;
+            for (int r = 0; r < C; ++r) {
+                const Shared<NT>* o = cta.of(&sh, r);
+                if (o->x_bin > best) { best = o->x_bin; sh.cnt_before = o->x_cnt_before; sh.sum_before = o->x_sum_before; }
+            }
+            sh.bin = best;
+        }
+        __syncthreads();
+    }
 }
 
 // Keys whose step is b: [lo, hi].  The step falls as the key grows, so both ends are found by a search of 32 probes at a time.
@@ -162,53 +220,68 @@ __device__ void key_range(const Row& row, int b, uint32_t top_key, uint32_t& lo,
     hi = b == 0 ? top_key : first_with(b - 1) - 1;
 }
 
-// A row as 16-byte vectors of N entries, the first of which may begin ahead of the row: in shared memory (what is ahead and behind is -inf) or, if it does not fit,
-// in global memory.  Warp w owns a stretch of vectors; f(value, index) of one warp's share, lane by lane.
+// A CTA's stretch of a row as 16-byte vectors of N entries in shared memory; the row's first vector may begin ahead of the row (what is ahead and behind is -inf).
+// Warp w owns a stretch of vectors; f(value, index) of one warp's share, lane by lane.
 template <typename T> struct RowData {
     static constexpr int N = 16 / sizeof(T);
-    const T* smem;                                        // vector 0, or null
-    const T* global;                                      // entry 0
-    int lead, V, nvec;                                    // entries of vector 0 that lie ahead of the row
-    __device__ __forceinline__ float at(int i) const { return to_f(smem ? smem[lead + i] : global[i]); }
+    const T* smem;                                        // the stretch's vector 0
+    int first;                                            // index in the row of its entry 0 (the row's lead: negative)
+    __device__ __forceinline__ float at(int i) const { return to_f(smem[i - first]); }
+    template <typename F> __device__ __forceinline__ void vec(int v, F f) const {
+        union { int4 raw; T x[N]; } u;
+        u.raw = reinterpret_cast<const int4*>(smem)[v];
+#pragma unroll
+        for (int j = 0; j < N; ++j) f(to_f(u.x[j]), first + v * N + j);
+    }
     template <typename F> __device__ __forceinline__ void each(int v0, int v1, F f) const {       // vectors [v0, v1), by one warp
-        for (int v = v0 + (threadIdx.x & 31); v < v1; v += 32) {
-            const int i0 = v * N - lead;
-            if (smem) {
-                union { int4 raw; T x[N]; } u;
-                u.raw = reinterpret_cast<const int4*>(smem)[v];
-#pragma unroll
-                for (int j = 0; j < N; ++j) f(to_f(u.x[j]), i0 + j);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) if (i0 + j >= 0 && i0 + j < V) f(to_f(global[i0 + j]), i0 + j);
-            }
-        }
+        for (int v = v0 + (threadIdx.x & 31); v < v1; v += 32) vec(v, f);
     }
 };
+__device__ __forceinline__ u64 composite(float l, int i) { return (u64)key_of(l) << 32 | (uint32_t)~i; }
+__device__ __forceinline__ float logit_of(u64 e) { return of_key((uint32_t)(e >> 32)); }
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a, int resident) {
+// sh.any[0 .. n) in falling order into sh.sorted (n at most SA_LIST): every entry counts those ahead of it, several threads an entry.
+template <int NT>
+__device__ void rank_list(Shared<NT>& sh, int n) {
+    const int width = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512, parts = NT / width;
+    for (int i = threadIdx.x; i < n; i += NT) sh.rank[i] = 0;
+    __syncthreads();
+    const int e = threadIdx.x % width;
+    if (e < n) {
+        const u64 x = sh.any[e];
+        int c = 0;
+#pragma unroll 4
+        for (int j = threadIdx.x / width; j < n; j += parts) c += sh.any[j] > x;
+        if (c) atomicAdd(sh.rank + e, c);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) sh.sorted[sh.rank[i]] = sh.any[i];
+    __syncthreads();
+}
+
+template <typename T, int NT, int C>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     constexpr int NW = NT / 32, N = RowData<T>::N;
     extern __shared__ __align__(16) char row_smem[];
     __shared__ Shared<NT> sh;
+    const Group<C> cta;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
-    const int r = blockIdx.x, pr = r / a.per_param;
-    RowData<T> data;
-    data.global = (const T*)a.logits + r * a.stride;
-    data.lead = (int)((uintptr_t)data.global & 15) / (int)sizeof(T);
-    data.V = V; data.nvec = (data.lead + V + N - 1) / N;
-    data.smem = resident ? (const T*)row_smem : nullptr;
-    const int per_warp = (data.nvec + NW - 1) / NW, v0 = min(warp * per_warp, data.nvec), v1 = min(v0 + per_warp, data.nvec);
-    if (resident) {                                       // each thread fetches the vectors that it reads first
-        const int4* from = reinterpret_cast<const int4*>(data.global - data.lead);
+    const int r = blockIdx.x / C, pr = r / a.per_param;
+    const T* global = (const T*)a.logits + r * a.stride;
+    const int lead = (int)((uintptr_t)global & 15) / (int)sizeof(T), nvec = (lead + V + N - 1) / N;
+    const int per_cta = (nvec + C - 1) / C, c0 = min(cta.rank * per_cta, nvec), mine_vec = min(c0 + per_cta, nvec) - c0;
+    const RowData<T> data{(const T*)row_smem, c0 * N - lead};
+    const int per_warp = (per_cta + NW - 1) / NW, v0 = min(warp * per_warp, mine_vec), v1 = min(v0 + per_warp, mine_vec);
+    {                                                     // each thread fetches the vectors that it reads first
+        const int4* from = reinterpret_cast<const int4*>(global - lead) + c0;
         for (int v = v0 + lane; v < v1; v += 32) {
-            const int i0 = v * N - data.lead;
+            const int i0 = data.first + v * N;
             if (i0 >= 0 && i0 + N <= V) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(row_smem + v * 16)), "l"(from + v) : "memory");
             } else {
                 union { int4 raw; T x[N]; } u;
 #pragma unroll
-                for (int j = 0; j < N; ++j) u.x[j] = i0 + j >= 0 && i0 + j < V ? data.global[i0 + j] : lowest<T>();
+                for (int j = 0; j < N; ++j) u.x[j] = i0 + j >= 0 && i0 + j < V ? global[i0 + j] : lowest<T>();
                 reinterpret_cast<int4*>(row_smem)[v] = u.raw;
             }
         }
@@ -216,11 +289,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a, int resi
     const float temperature = a.temperature ? a.temperature[pr] : 1.f;
     const float top_p = a.top_p ? a.top_p[pr] : 1.f, min_p = a.min_p ? a.min_p[pr] : 0.f;
     const int k_in = a.top_k ? a.top_k[pr] : 0;
+    const float u = a.uniform[r];
     const int k = k_in <= 0 || k_in > V ? V : k_in;
     const bool greedy = !(temperature > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f) || k == 1;        // the largest entry alone
-    const bool few = k <= SA_FEW && k < V;
-    sh.h.template clear<NT>();
-    if (tid == 0) { sh.index = V; sh.n_list = 0; }
+    const bool few = k <= SA_FEW && k < V, cuts = k < V || top_p < 1.f;
+    if (cuts) sh.h.template clear<NT>();
+    if (tid == 0) { sh.index = V; sh.n_list = 0; sh.winner = -1; }
     asm volatile("cp.async.wait_all;" ::: "memory");
 
     float mine = -INFINITY;                               // this thread's maximum (NaN does not count)
@@ -230,69 +304,76 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a, int resi
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (lane == 0) sh.w_max[warp] = top;
     __syncthreads();
+    top = lane < NW ? sh.w_max[lane] : -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, sh.w_max[w]);
-    if (top == -INFINITY) {
-        if (tid == 0) { a.token[r] = -1; if (a.logprob) a.logprob[r] = -INFINITY; }
-        return;
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float cta_top = top;
+    if (C > 1) {
+        if (tid == 0) sh.x_top = top;
+        cta.sync();
+        for (int q = 0; q < C; ++q) top = fmaxf(top, cta.of(&sh, q)->x_top);
     }
-    if (greedy) {
-        if (mine == top) {
+    if (top == -INFINITY || greedy) {
+        if (top > -INFINITY && mine == top) {
             int first = V;
             data.each(v0, v1, [&](float l, int i) { if (l == top) first = min(first, i); });
             atomicMin(&sh.index, first);
         }
-        __syncthreads();
-        if (tid == 0) { a.token[r] = sh.index; if (a.logprob) a.logprob[r] = 0.f; }
+        if (C > 1) {                                      // the first CTA that holds the maximum answers
+            __syncthreads();
+            if (tid == 0) {
+                bool ahead = false;
+                for (int q = 0; q < cta.rank; ++q) ahead |= cta.of(&sh, q)->x_top == top;
+                if (!ahead && (cta_top == top)) { a.token[r] = top > -INFINITY ? sh.index : -1; if (a.logprob) a.logprob[r] = top > -INFINITY ? 0.f : -INFINITY; }
+            }
+            cta.sync();                                   // until the others have read x_top
+        } else {
+            __syncthreads();
+            if (tid == 0) { a.token[r] = top > -INFINITY ? sh.index : -1; if (a.logprob) a.logprob[r] = top > -INFINITY ? 0.f : -INFINITY; }
+        }
         return;
     }
     const Row row{top + 0.f, 1.f / temperature};
     const uint32_t top_key = key_of(top);
-    const float u = a.uniform[r];
     auto goal_of = [&](u64 total) -> u64 { return u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0; };
     auto log_of = [](u64 total) { return logf((float)total * 9.094947017729282e-13f); };             // total 2^-40
 
     if (few) {
         const int b = Row::bin_of(row.x_of(mine));
         if (b < SA_BINS) atomicAdd(sh.h.cnt + b, 1u);
-        __syncthreads();
-        find_bin<NT>(sh, false, k, 0., 0, 0);
+        const Group<1> alone;
+        find_bin<NT, 1>(sh, alone, false, k, 0., 0, 0);
         const int bin = sh.bin;
         // entries from here on up: all of steps 0 .. bin (a little more does no harm)
         const float depth = (bin + 1) * (SA_RANGE / SA_BINS) * temperature;
-        const float bound = bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
-        if (bin >= 0 && bound > -INFINITY) {
-            __syncthreads();                              // the list takes the histogram's place
-            if (mine >= bound)
-                data.each(v0, v1, [&](float l, int i) {
-                    if (l >= bound) {
-                        const int at = atomicAdd(&sh.n_list, 1);
-                        if (at < SA_LIST) sh.list.any[at] = (u64)key_of(l) << 32 | (uint32_t)~i;
-                    }
-                });
-            __syncthreads();
+        float bound = bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
+        if (!(bound > -INFINITY)) bound = -INFINITY;      // (NaN: a maximum of +inf)
+        if (C > 1) {
+            if (tid == 0) sh.x_bound = bound;
+            cta.sync();
+            for (int q = 0; q < C; ++q) bound = fmaxf(bound, cta.of(&sh, q)->x_bound);
         }
-        const int n = sh.n_list;
+        Shared<NT>* lead_sh = cta.of(&sh, 0);
+        if (bound > -INFINITY && mine >= bound)
+            data.each(v0, v1, [&](float l, int i) {
+                if (l >= bound) {
+                    const int at = atomicAdd(&lead_sh->n_list, 1);
+                    if (at < SA_LIST) lead_sh->any[at] = composite(l, i);
+                }
+            });
+        cta.sync();
+        const int n = lead_sh->n_list;
+        cta.sync();                                       // all have read it
         if (n >= k && n <= SA_LIST) {
-            const int width = n <= 128 ? 128 : n <= 256 ? 256 : n <= 512 ? 512 : 1024, parts = max(NT / width, 1);   // entry, share of the others
-            for (int i = tid; i < n; i += NT) sh.list.rank[i] = 0;
-            __syncthreads();
-            for (int e = tid % width; e < n; e += NT) {
-                const u64 x = sh.list.any[e];
-                int c = 0;
-                for (int j = tid / width; j < n; j += parts) c += sh.list.any[j] > x;
-                if (c) atomicAdd(sh.list.rank + e, c);
-            }
-            __syncthreads();
-            for (int e = tid; e < n; e += NT) { const int at = sh.list.rank[e]; if (at < k) sh.list.sorted[at] = sh.list.any[e]; }
-            __syncthreads();
+            if (cta.rank) return;
+            rank_list<NT>(sh, n);
             if (warp == 0) {                              // the order's cut, and the smaller entries that min_p drops: at most SA_FEW, four a lane
                 u64 un[SA_FEW / 32], all = 0;
                 float w[SA_FEW / 32];
 #pragma unroll
                 for (int j = 0; j < SA_FEW / 32; ++j) {
                     const int e = lane * (SA_FEW / 32) + j;
-                    w[j] = e < k ? row.w_of(of_key((uint32_t)(sh.list.sorted[e] >> 32))) : 0.f;
+                    w[j] = e < k ? row.w_of(logit_of(sh.sorted[e])) : 0.f;
                     un[j] = Row::units(w[j]);
                     all += un[j];
                 }
@@ -306,80 +387,161 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a, int resi
                     before += un[j];
                     un[j] = keep ? un[j] : 0;
                     kept += un[j];
-                    sh.list.units[lane * (SA_FEW / 32) + j] = un[j];
+                    sh.units[lane * (SA_FEW / 32) + j] = un[j];
                 }
                 kept = warp_sum(kept);
                 if (lane == 0) sh.total = kept;
             }
             __syncthreads();
-            {   // weight of the kept entries with a lower index, eight or four threads an entry
-                constexpr int PARTS = NT / SA_FEW;
-                const int e = tid % SA_FEW, p = tid / SA_FEW;
-                if (e < k) {
-                    const uint32_t me = (uint32_t)sh.list.sorted[e];                   // ~index
-                    u64 s = 0;
-                    for (int j = p; j < k; j += PARTS) if ((uint32_t)sh.list.sorted[j] > me) s += sh.list.units[j];
-                    sh.list.part[p][e] = s;
-                }
-                __syncthreads();
-                if (tid < k) {
-                    u64 before = 0;
+            // weight of the kept entries with a lower index, several threads an entry
+            constexpr int PARTS = NT / SA_FEW;
+            const int e = tid % SA_FEW, p = tid / SA_FEW;
+            if (e < k) {
+                const uint32_t me = (uint32_t)sh.sorted[e];            // ~index
+                u64 s = 0;
+#pragma unroll 4
+                for (int j = p; j < k; j += PARTS) if ((uint32_t)sh.sorted[j] > me) s += sh.units[j];
+                sh.part[p][e] = s;
+            }
+            __syncthreads();
+            if (tid < k) {
+                u64 before = 0;
 #pragma unroll
-                    for (int j = 0; j < PARTS; ++j) before += sh.list.part[j][tid];
-                    const u64 total = sh.total, goal = goal_of(total);
-                    if (before <= goal && goal < before + sh.list.units[tid]) {
-                        const u64 x = sh.list.sorted[tid];
-                        a.token[r] = (int)~(uint32_t)x;
-                        if (a.logprob) a.logprob[r] = row.x_of(of_key((uint32_t)(x >> 32))) - log_of(total);
-                    }
+                for (int j = 0; j < PARTS; ++j) before += sh.part[j][tid];
+                const u64 total = sh.total, goal = goal_of(total);
+                if (before <= goal && goal < before + sh.units[tid]) {
+                    const u64 x = sh.sorted[tid];
+                    a.token[r] = (int)~(uint32_t)x;
+                    if (a.logprob) a.logprob[r] = row.x_of(logit_of(x)) - log_of(total);
                 }
             }
             return;
         }
-        __syncthreads();
         sh.h.template clear<NT>();
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
     }
 
-    // the key and the number of its entries at which the order is cut
-    uint32_t cut_key = KEY_NEG_INF + 1;                   // entries above stay; of those equal to it the first cut_n
-    u64 cut_n = ~0ull;
-    if (k < V || top_p < 1.f) {
-        const bool count = k < V;
+    u64 cut = 0;                                          // entries with a composite from here on stay
+    u64 s = 0;                                            // of this warp's stretch: kept weight
+    if (cuts) {
+        // the histogram over steps
         u64 all = 0;
-        __syncthreads();
-        auto fill = [&](bool count) {
-            data.each(v0, v1, [&](float l, int) {
-                const float x = row.x_of(l);
-                const int b = Row::bin_of(x);
-                if (b < SA_BINS) {
-                    const u64 u = Row::units(expf(x));
-                    sh.h.add(b, u);
-                    if (count) atomicAdd(sh.h.cnt + b, 1u);
-                    all += u;
+        {
+            const bool count = k < V;
+            for (int v = v0 + lane; v < v1; v += 32) {
+                int b[N];
+                uint32_t lo[N], hi[N], old[N];
+                int j = 0;
+                data.vec(v, [&](float l, int) {           // (all atomics of a vector are on their way before the first answer is looked at)
+                    const float x = row.x_of(l);
+                    const bool in = x > -SA_RANGE;
+                    b[j] = in ? min((int)(-x * (SA_BINS / SA_RANGE)), SA_BINS - 1) : SA_BINS + lane;
+                    const u64 w = in ? Row::units(expf(x)) : 0;
+                    all += w;
+                    lo[j] = (uint32_t)w; hi[j] = (uint32_t)(w >> 32);
+                    old[j] = atomicAdd(sh.h.lo + b[j], lo[j]);
+                    if (count && in) atomicAdd(sh.h.cnt + b[j], 1u);
+                    ++j;
+                });
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const uint32_t h = hi[q] + (old[q] + lo[q] < old[q]);
+                    if (h) atomicAdd(sh.h.hi + min(b[q], SA_BINS - 1), h);
                 }
-            });
-            __syncthreads();
-        };
-        fill(count);
+            }
+        }
         all = warp_sum(all);
+        __syncthreads();
         if (lane == 0) sh.w_sum[warp] = all;
         __syncthreads();
-        u64 total = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) total += sh.w_sum[w];
+        u64 total;
+        warps_before<NT>(sh.w_sum, total);
+        if (C > 1) {
+            if (tid == 0) sh.x_all = total;
+            cta.sync();
+            total = 0;
+            for (int q = 0; q < C; ++q) total += cta.of(&sh, q)->x_all;
+        }
         __syncthreads();
-        bool first_level = true;                          // whether sh.h is the histogram of x
-        auto refine = [&](bool by_weight, double thr) {
-            // sh.bin, sh.*_before: the step.  Afterwards cut_key, cut_n, and sh.sum_before = the weight ahead of the key's first entry
-            uint32_t lo, hi;
-            key_range(row, sh.bin, top_key, lo, hi);
-            while (true) {
-                const u64 c0 = sh.cnt_before, s0 = sh.sum_before;
-                const int width = 32 - __clz(hi - lo), shift = max(0, width - 11);
+        // The cut in sh.bin: sh.cut = composite of the last entry that stays, sh.cut_sum = weight of all that stay.  sum: whether to add up the kept weights ahead of the step.
+        bool filled = true;                               // whether sh.h is the histogram over steps
+        auto locate = [&](bool by_weight, double thr, bool sum) {
+            const int bin = sh.bin;
+            const u64 c0 = sh.cnt_before, s0 = sh.sum_before;
+            // logits of step bin, and a little more on either side
+            const float unit = SA_RANGE / SA_BINS * temperature, slack = (fabsf(row.top) + (bin + 1) * unit) * 1e-6f;
+            const float high = row.top - bin * unit + slack, low = row.top - (bin + 1) * unit - slack;
+            const bool usable = low > -INFINITY && high < INFINITY;                     // (not for a maximum of +inf, or a temperature near the type's ends)
+            s = 0;
+            if (usable)
+                data.each(v0, v1, [&](float l, int i) {
+                    if (l >= low) {
+                        if (l <= high) {
+                            const int b = Row::bin_of(row.x_of(l));
+                            if (b == bin) {
+                                const int at = atomicAdd(&sh.n_list, 1);
+                                if (at < SA_LIST) sh.any[at] = composite(l, i);
+                            }
+                            if (b >= bin) return;
+                        }
+                        if (sum) { const float w = row.w_of(l); if (w >= min_p) s += Row::units(w); }
+                    }
+                });
+            __syncthreads();
+            int n = usable ? sh.n_list : SA_LIST + 1;
+            __syncthreads();                              // all have read it
+            if (C > 1) {                                  // every CTA takes all lists
+                if (tid == 0) sh.x_n = n;
+                cta.sync();
+                int at = n;
+                for (int q = 0; q < C; ++q) if (q != cta.rank) {
+                    const Shared<NT>* o = cta.of(&sh, q);
+                    const int m = o->x_n;
+                    if (at + m <= SA_LIST) for (int i = tid; i < m; i += NT) sh.sorted[at + i] = o->any[i];
+                    at += m;
+                }
+                cta.sync();                               // the others have read this CTA's list
+                if (at <= SA_LIST) for (int i = n + tid; i < at; i += NT) sh.any[i] = sh.sorted[i];
+                n = at;
                 __syncthreads();
+            }
+            if (tid == 0) sh.n_list = 0;
+            if (n <= SA_LIST) {
+                rank_list<NT>(sh, n);
+                u64 w = 0;
+                if (tid < n) w = Row::units(row.w_of(logit_of(sh.sorted[tid])));
+                const u64 upto = warp_scan(w);
+                if (lane == 31) sh.w_sum[warp] = upto;
+                __syncthreads();
+                u64 unused;
+                const u64 before = s0 + warps_before<NT>(sh.w_sum, unused) + upto - w;
+                // the last entry that stays: by weight the last whose weight ahead is below thr
+                const bool stays = tid < n && (by_weight ? (double)before < thr : c0 + tid + 1 <= (u64)k);
+                const bool next = tid + 1 < n && (by_weight ? (double)(before + w) < thr : c0 + tid + 2 <= (u64)k);
+                if (stays && !next) { sh.cut = sh.sorted[tid]; sh.cut_sum = before + w; }
+                __syncthreads();
+                if (sum)                                  // the step's own entries, those of this warp's stretch
+                    for (int e = lane; e < n; e += 32) {
+                        const u64 y = sh.sorted[e];
+                        const int i = (int)~(uint32_t)y;
+                        if (y >= sh.cut && i >= data.first + v0 * N && i < data.first + v1 * N) {
+                            const float w2 = row.w_of(logit_of(y));
+                            if (w2 >= min_p) s += Row::units(w2);
+                        }
+                    }
+                return sum;
+            }
+            // more than the list holds
+            filled = false;
+            uint32_t lo, hi;
+            key_range(row, bin, top_key, lo, hi);
+            u64 cb = c0, sb = s0;
+            while (true) {
+                const int width = 32 - __clz(hi - lo), shift = max(0, width - 10);                    // 2^10 bins
+                cta.sync();
                 sh.h.template clear<NT>();
                 __syncthreads();
-                first_level = false;
                 data.each(v0, v1, [&](float l, int) {
                     const uint32_t key = key_of(l);
                     if (key >= lo && key <= hi) {
@@ -388,126 +550,173 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a, int resi
                         atomicAdd(sh.h.cnt + b, 1u);
                     }
                 });
-                __syncthreads();
-                find_bin<NT>(sh, by_weight, k, thr, c0, s0);
+                find_bin<NT, C>(sh, cta, by_weight, k, thr, cb, sb);
                 const uint32_t h2 = hi - ((uint32_t)sh.bin << shift);
                 lo = shift ? max(lo, h2 - ((1u << shift) - 1)) : h2;
                 hi = h2;
+                cb = sh.cnt_before; sb = sh.sum_before;
                 if (shift == 0) break;
             }
-            cut_key = lo;
-            const u64 n = sh.h.cnt[sh.bin], w = sh.h.sum(sh.bin) / n;      // n entries of weight w each
-            if (!by_weight) { cut_n = k - sh.cnt_before; if (cut_n == n && !(top_p < 1.f)) cut_n = ~0ull; return; }
-            u64 m = n;                                    // entries j < n with sum_before + j w < thr
-            if (w) {
-                const double gap = thr - (double)sh.sum_before;
-                m = gap > 0 ? min((u64)(gap / (double)w) + 2, n) : 0;
-                while (m > 0 && !((double)(sh.sum_before + (m - 1) * w) < thr)) --m;
+            // entries equal to one key, of weight w each: how many stay
+            u64 n_eq = 0;
+            for (int q = 0; q < C; ++q) n_eq += cta.of(&sh, q)->h.cnt[sh.bin];
+            const u64 w = Row::units(row.w_of(of_key(lo)));
+            u64 m = n_eq;
+            if (!by_weight) m = k - cb;
+            else if (w) {                                 // entries j with sb + j w < thr
+                const double gap = thr - (double)sb;
+                m = gap > 0 ? min((u64)(gap / (double)w) + 2, n_eq) : 0;
+                while (m > 0 && !((double)(sb + (m - 1) * w) < thr)) --m;
             }
-            cut_n = m == n ? ~0ull : m;
+            // the index of the m-th: counts by CTA, by warp, then 32 entries at a time
+            int ne = 0;
+            data.each(v0, v1, [&](float l, int) { ne += key_of(l) == lo; });
+#pragma unroll
+            for (int o = 16; o; o >>= 1) ne += __shfl_xor_sync(0xffffffffu, ne, o);
+            __syncthreads();
+            if (lane == 0) sh.w_cnt[warp] = ne;
+            __syncthreads();
+            int cta_n;
+            u64 ahead = warps_before<NT>(sh.w_cnt, cta_n);
+            if (C > 1) {
+                if (tid == 0) { sh.x_n = cta_n; sh.winner = -1; }
+                cta.sync();
+                for (int q = 0; q < cta.rank; ++q) ahead += cta.of(&sh, q)->x_n;
+            }
+            if (ahead < m && m <= ahead + ne)
+                for (int v = v0 * N; v < v1 * N; v += 32) {
+                    const int i = data.first + v + lane;
+                    const bool is = v + lane < v1 * N && key_of(data.at(i)) == lo;
+                    const unsigned ms = __ballot_sync(0xffffffffu, is);
+                    if (m <= ahead + __popc(ms)) {
+                        if (is && ahead + __popc(ms & ((2u << lane) - 1)) == m) {
+                            for (int q = 0; q < C; ++q) cta.of(&sh, q)->cut = (u64)lo << 32 | (uint32_t)~i;
+                        }
+                        break;
+                    }
+                    ahead += __popc(ms);
+                }
+            if (tid == 0) sh.cut_sum = sb + m * w;
+            cta.sync();
+            return false;
         };
-        if (count) {
-            find_bin<NT>(sh, false, k, 0., 0, 0);
+        bool summed = false;
+        if (k < V) {
+            find_bin<NT, C>(sh, cta, false, k, 0., 0, 0);
             if (sh.bin >= 0) {
-                refine(false, 0.);
-                const u64 w = sh.h.sum(sh.bin) / sh.h.cnt[sh.bin];
-                total = sh.sum_before + (k - sh.cnt_before) * w;
+                summed = locate(false, 0., !(top_p < 1.f));
+                cut = sh.cut; total = sh.cut_sum;
             }
         }
         if (top_p < 1.f) {
             const double thr = (double)top_p * (double)total;
-            if (!first_level) {                           // the search for the k-th entry took the histogram
-                __syncthreads();
+            if (!filled) {                                // the search for the k-th entry took the histogram
+                cta.sync();
                 sh.h.template clear<NT>();
                 __syncthreads();
-                fill(false);
+                data.each(v0, v1, [&](float l, int) {
+                    const float x = row.x_of(l);
+                    const int b = Row::bin_of(x);
+                    if (b < SA_BINS) sh.h.add(b, Row::units(expf(x)));
+                });
             }
-            find_bin<NT>(sh, true, 0, thr, 0, 0);
-            refine(true, thr);
+            find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0);
+            summed = locate(true, thr, true);
+            cut = sh.cut;
         }
-    }
-    // of the entries equal to cut_key, the index of the last that stays
-    int cut_index = V;
-    if (cut_n != ~0ull) {
-        int n = 0;
-        data.each(v0, v1, [&](float l, int) { n += key_of(l) == cut_key; });
-#pragma unroll
-        for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        __syncthreads();
-        if (lane == 0) sh.w_cnt[warp] = n;
-        __syncthreads();
-        u64 ahead = 0;
-        for (int w = 0; w < warp; ++w) ahead += sh.w_cnt[w];
-        if (ahead < cut_n && cut_n <= ahead + n)
-            for (int i0 = max(v0 * N - data.lead, 0); i0 < V; i0 += 32) {
-                const unsigned m = __ballot_sync(0xffffffffu, i0 + lane < V && key_of(data.at(min(i0 + lane, V - 1))) == cut_key);
-                if (cut_n <= ahead + __popc(m)) {
-                    if ((m >> lane & 1) && ahead + __popc(m & ((2u << lane) - 1)) == cut_n) sh.index = i0 + lane;
-                    break;
-                }
-                ahead += __popc(m);
-            }
-        __syncthreads();
-        cut_index = sh.index;
-    }
-    // the goal's entry
-    auto kept = [&](float l, int i) -> float {            // weight, or 0
-        const uint32_t key = key_of(l);
-        if (key < cut_key || (key == cut_key && i > cut_index)) return 0.f;
-        const float w = row.w_of(l);
-        return w >= min_p ? w : 0.f;
-    };
-    int lo = 0, hi = data.nvec;                           // vectors
-    u64 goal = 0, ahead = 0, total = 0;
-    for (int len = per_warp, first = 1; ; len = (hi - lo + NW - 1) / NW, first = 0) {
-        uint32_t sum_hi = 0, sum_lo = 0, n = 0;           // as split_units gives them: at most 2^18 / NT entries of up to 2^20 each a thread
-        const int a0 = min(lo + warp * len, hi), a1 = min(a0 + len, hi);
-        data.each(a0, a1, [&](float l, int i) {
+        if (!summed) {
+            s = 0;
+            data.each(v0, v1, [&](float l, int i) {
+                if (composite(l, i) >= cut) { const float w = row.w_of(l); if (w >= min_p) s += Row::units(w); }
+            });
+        }
+    } else {                                              // all entries, or all that min_p leaves
+        uint32_t hi = 0, lo = 0, n = 0;                   // as split_units gives them: at most 2^18 / NT entries of up to 2^20 each
+        data.each(v0, v1, [&](float l, int) {
+            const float w = row.w_of(l);
             uint32_t x, y;
-            split_units(kept(l, i), x, y);
-            sum_hi += x; sum_lo += y; ++n;
+            split_units(w >= min_p ? w : 0.f, x, y);
+            hi += x; lo += y; ++n;
         });
-        const u64 s = warp_sum(((u64)(sum_hi - n * MAGIC) << 20) + (sum_lo - n * MAGIC));
-        __syncthreads();
-        if (lane == 0) sh.w_sum[warp] = s;
-        __syncthreads();
-        if (first) {
-#pragma unroll
-            for (int w = 0; w < NW; ++w) total += sh.w_sum[w];
-            goal = goal_of(total);
-        }
-        int w = 0;
-        for (; w < NW - 1 && ahead + sh.w_sum[w] <= goal; ++w) ahead += sh.w_sum[w];
-        lo = min(lo + w * len, hi); hi = min(lo + len, hi);
-        if (len <= 32 / N) break;
+        s = ((u64)(hi - n * MAGIC) << 20) + (lo - n * MAGIC);
     }
-    if (warp == 0) {                                      // at most 32 entries are left
-        const int i = lo * N - data.lead + lane;
-        const bool in = i >= 0 && i < V && i < hi * N - data.lead;
-        const float l = in ? data.at(i) : 0.f;
-        const u64 s = ahead + warp_scan(in ? Row::units(kept(l, i)) : 0);
-        const unsigned m = __ballot_sync(0xffffffffu, s > goal);
-        if (lane == __ffs(m) - 1) {
-            a.token[r] = i;
-            if (a.logprob) a.logprob[r] = row.x_of(l) - log_of(total);
+
+    // the warp whose stretch holds the goal
+    s = warp_sum(s);
+    __syncthreads();
+    if (lane == 0) sh.w_sum[warp] = s;
+    __syncthreads();
+    u64 total;
+    u64 before = warps_before<NT>(sh.w_sum, total);
+    if (C > 1) {
+        if (tid == 0) sh.x_total = total;
+        cta.sync();
+        u64 all = 0;
+        for (int q = 0; q < C; ++q) {
+            const u64 t = cta.of(&sh, q)->x_total;
+            if (q < cta.rank) before += t;
+            all += t;
         }
+        total = all;
+        cta.sync();                                       // the others have read this CTA's total
     }
+    const u64 goal = goal_of(total);
+    if (lane == 0 && before <= goal && goal < before + s) { sh.winner = warp; sh.sum_before = before; }
+    __syncthreads();
+    if (sh.winner < 0) return;                            // in another CTA
+    // its stretch again, consecutive vectors to a thread
+    const int w0 = min(sh.winner * per_warp, mine_vec), w1 = min(w0 + per_warp, mine_vec), each = (w1 - w0 + NT - 1) / NT;
+    const int t0 = min(w0 + tid * each, w1), t1 = min(t0 + each, w1);
+    auto kept = [&](float l, int i) -> u64 {
+        if (composite(l, i) < cut) return 0;
+        const float w = row.w_of(l);
+        return w >= min_p ? Row::units(w) : 0;
+    };
+    u64 t = 0;
+    for (int v = t0; v < t1; ++v) data.vec(v, [&](float l, int i) { t += kept(l, i); });
+    const u64 start = sh.sum_before, upto = warp_scan(t);
+    if (lane == 31) sh.w_sum[warp] = upto;
+    __syncthreads();
+    u64 unused;
+    u64 at = start + warps_before<NT>(sh.w_sum, unused) + upto - t;
+    if (at <= goal && goal < at + t)
+        for (int v = t0; v < t1; ++v)
+            data.vec(v, [&](float l, int i) {
+                const u64 w = kept(l, i);
+                if (at <= goal && goal < at + w) {
+                    a.token[r] = i;
+                    if (a.logprob) a.logprob[r] = row.x_of(l) - log_of(total);
+                }
+                at += w;
+            });
 }
 
-template <typename T, int NT>
-cudaError_t run(const SampleArgs& a, int rows, int resident, size_t smem, cudaStream_t st) {
-    static const cudaError_t attr = cudaFuncSetAttribute(k_sample<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 28 * 1024);
+constexpr size_t SA_STATIC = 25 * 1024, SA_SMEM = 232448; // shared memory beside the row, and of an SM at most
+template <typename T, int NT, int C>
+cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
+    static_assert(sizeof(Shared<NT>) <= SA_STATIC, "what is beside the row");
+    static const cudaError_t attr = cudaFuncSetAttribute(k_sample<T, NT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SA_SMEM - SA_STATIC));
     if (attr != cudaSuccess) return attr;
-    k_sample<T, NT><<<rows, NT, smem, st>>>(a, resident);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(rows * C); cfg.blockDim = dim3(NT); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = C; at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at; cfg.numAttrs = C > 1;
+    return cudaLaunchKernelEx(&cfg, k_sample<T, NT, C>, a);
 }
+// CTAs of a row: as few as hold it, and more while all rows' run at once and have some work each.  Two CTAs of 512 threads share an SM while two stretches fit its
+// shared memory; beyond, one CTA of 1024 has the SM to itself.
 template <typename T>
 cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
-    size_t smem = ((size_t)a.V * sizeof(T) + 47) / 16 * 16;
-    const int resident = smem <= 232448 - 28 * 1024;
-    if (!resident) smem = 0;
-    // two CTAs of 512 threads share an SM while two rows fit its shared memory; beyond, one CTA has the SM to itself
-    return smem <= 84 * 1024 ? run<T, 512>(a, rows, resident, smem, st) : run<T, 1024>(a, rows, resident, smem, st);
+    auto bytes = [&](int c) { return ((size_t)a.V * sizeof(T) / 16 + 2 + c) / c * 16 + 16; };
+    auto two = [&](int c) { return 2 * (bytes(c) + SA_STATIC + 1024) <= SA_SMEM; };
+    int c = 1;
+    while (bytes(c) > SA_SMEM - SA_STATIC) c *= 2;
+    while (c < 8 && (long long)rows * 2 * c <= 148 * (two(2 * c) ? 2 : 1) && a.V >= 2 * c * 4096) c *= 2;
+    const size_t smem = bytes(c);
+    if (two(c)) return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
+    return c == 1 ? run<T, 1024, 1>(a, rows, smem, st) : c == 2 ? run<T, 1024, 2>(a, rows, smem, st) : c == 4 ? run<T, 1024, 4>(a, rows, smem, st) : run<T, 1024, 8>(a, rows, smem, st);
 }
 
 }  // namespace
@@ -523,6 +732,7 @@ extern "C" int specdec_sample(const void* d_logits, int dtype, long long stride,
     if (V > 1 << 18) return op_fail(SPECDEC_ERR_CAPACITY, "sample", "at most 262144 entries a row");       // 2^18 weights of up to 2^40 units stay far below 2^64
     if (rows == 0) return SPECDEC_OK;
     if (!d_logits || !d_uniform || !d_token || (uintptr_t)d_logits % op_elem_bytes(dtype)) return op_bad("sample", "a pointer is NULL, or d_logits not aligned to its type");
+    if (rows > 1 << 27) return op_fail(SPECDEC_ERR_CAPACITY, "sample", "at most 2^27 rows");
     const SampleArgs a{d_logits, stride, V, d_uniform, d_temperature, d_top_k, d_top_p, d_min_p, rows_per_param, d_token, d_logprob};
     const cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = dtype == SPECDEC_DTYPE_F32 ? launch<float>(a, rows, st) : dtype == SPECDEC_DTYPE_BF16 ? launch<__nv_bfloat16>(a, rows, st) : launch<__half>(a, rows, st);
