@@ -38,6 +38,11 @@ template <> __device__ __forceinline__ float lowest<float>() { return -INFINITY;
 template <> __device__ __forceinline__ __nv_bfloat16 lowest<__nv_bfloat16>() { return __float2bfloat16_rn(-INFINITY); }
 template <> __device__ __forceinline__ __half lowest<__half>() { return __float2half_rn(-INFINITY); }
 
+template <typename T> __device__ __forceinline__ T zero();
+template <> __device__ __forceinline__ float zero<float>() { return 0.f; }
+template <> __device__ __forceinline__ __nv_bfloat16 zero<__nv_bfloat16>() { return __float2bfloat16_rn(0.f); }
+template <> __device__ __forceinline__ __half zero<__half>() { return __float2half_rn(0.f); }
+
 // Order-preserving integer of a logit; NaN lowest, the two zeros equal.
 __device__ __forceinline__ uint32_t key_of(float l) {
     const uint32_t u = __float_as_uint(l + 0.f);
@@ -60,19 +65,35 @@ __device__ __forceinline__ void split_units(float w, uint32_t& hi, uint32_t& lo)
     hi = __float_as_uint(t);
     lo = __float_as_uint(__fmaf_rd(rest, 1048576.f, 8388608.f));
 }
-struct Row {                                              // what turns a logit into a weight
+// Two floats at a time (the same results as one at a time).
+__device__ __forceinline__ u64 pair2(float lo, float hi) { u64 d; asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi)); return d; }
+__device__ __forceinline__ float lo2(u64 d) { return __uint_as_float((uint32_t)d); }
+__device__ __forceinline__ float hi2(u64 d) { return __uint_as_float((uint32_t)(d >> 32)); }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) { u64 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ u64 fma2_rd(u64 a, u64 b, u64 c) { u64 d; asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+// split_units of two weights.
+__device__ __forceinline__ void split_units2(u64 w, u64& hi, u64& lo) {
+    const u64 scale = pair2(1048576.f, 1048576.f), magic = pair2(8388608.f, 8388608.f);
+    hi = fma2_rd(w, scale, magic);
+    lo = fma2_rd(fma2(w, scale, fma2(hi, pair2(-1.f, -1.f), magic)), scale, magic);
+}
+
+// What turns a logit into a weight.  (Rows whose maximum is +inf, or whose 1 / T is, have been rewritten to 0 and -inf: nothing here is inf - inf.)
+struct Row {
     float top, inv_t;
-    __device__ __forceinline__ float x_of(float l) const { return l == top ? 0.f : (l - top) * inv_t; }
+    __device__ __forceinline__ float x_of(float l) const { return __fmul_rn(l - top, inv_t); }        // (never one rounding with what follows)
+    __device__ __forceinline__ u64 x_of2(u64 l) const { return mul2(add2(l, pair2(-top, -top)), pair2(inv_t, inv_t)); }
     __device__ __forceinline__ float w_of(float l) const { return fmaxf(expf(x_of(l)), 0.f); }          // NaN: 0
     __device__ __forceinline__ static u64 units(float w) {
         uint32_t hi, lo;
         split_units(w, hi, lo);
         return ((u64)(hi - MAGIC) << 20) + (lo - MAGIC);
     }
-    // step of x: 0 for the largest; SA_BINS: weight 0 (NaN, -inf and all that is too small)
-    __device__ __forceinline__ static int bin_of(float x) {
-        return x > -SA_RANGE ? min((int)(-x * (SA_BINS / SA_RANGE)), SA_BINS - 1) : SA_BINS;
-    }
+    // step of x, to the nearest: 0 for the largest; SA_BINS and more: weight 0 (NaN, -inf and all that is too small)
+    static constexpr float STEPS = SA_BINS / SA_RANGE;
+    __device__ __forceinline__ static uint32_t bin_of(float x) { return __float_as_uint(fmaf(x, -STEPS, 8388608.f)) - MAGIC; }
 };
 
 __device__ __forceinline__ u64 warp_sum(u64 v) {
@@ -199,9 +220,9 @@ __device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u6
 }
 
 // Keys whose step is b: [lo, hi].  The step falls as the key grows, so both ends are found by a search of 32 probes at a time.
-__device__ void key_range(const Row& row, int b, uint32_t top_key, uint32_t& lo, uint32_t& hi) {
+__device__ void key_range(const Row& row, uint32_t b, uint32_t top_key, uint32_t& lo, uint32_t& hi) {
     const int lane = threadIdx.x & 31;
-    auto first_with = [&](int most) {                     // smallest key in (KEY_NEG_INF, top_key] whose step is <= most
+    auto first_with = [&](uint32_t most) {                     // smallest key in (KEY_NEG_INF, top_key] whose step is <= most
         uint32_t a = KEY_NEG_INF + 1, n = top_key - a;    // the answer is in [a, a + n]
         while (n) {
             const uint32_t step = n / 32 + 1;
@@ -232,6 +253,12 @@ template <typename T> struct RowData {
         u.raw = reinterpret_cast<const int4*>(smem)[v];
 #pragma unroll
         for (int j = 0; j < N; ++j) f(to_f(u.x[j]), first + v * N + j);
+    }
+    __device__ __forceinline__ void pairs(int v, u64* l) const {      // a vector's entries, two by two
+        union { int4 raw; T x[N]; } u;
+        u.raw = reinterpret_cast<const int4*>(smem)[v];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) l[j] = pair2(to_f(u.x[2 * j]), to_f(u.x[2 * j + 1]));
     }
     template <typename F> __device__ __forceinline__ void each(int v0, int v1, F f) const {       // vectors [v0, v1), by one warp
         for (int v = v0 + (threadIdx.x & 31); v < v1; v += 32) vec(v, f);
@@ -333,21 +360,33 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         }
         return;
     }
-    const Row row{top + 0.f, 1.f / temperature};
+    float inv_t = 1.f / temperature;
+    if (top == INFINITY || inv_t == INFINITY) {           // only what equals the maximum weighs anything
+        for (int v = v0 + lane; v < v1; v += 32) {
+            union { int4 raw; T x[N]; } y;
+            y.raw = reinterpret_cast<const int4*>(row_smem)[v];
+#pragma unroll
+            for (int j = 0; j < N; ++j) y.x[j] = to_f(y.x[j]) == top ? zero<T>() : lowest<T>();
+            reinterpret_cast<int4*>(row_smem)[v] = y.raw;
+        }
+        mine = mine == top ? 0.f : -INFINITY;
+        top = 0.f; inv_t = 1.f;
+        __syncthreads();
+    }
+    const Row row{top + 0.f, inv_t};
     const uint32_t top_key = key_of(top);
     auto goal_of = [&](u64 total) -> u64 { return u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0; };
     auto log_of = [](u64 total) { return logf((float)total * 9.094947017729282e-13f); };             // total 2^-40
 
     if (few) {
-        const int b = Row::bin_of(row.x_of(mine));
+        const uint32_t b = Row::bin_of(row.x_of(mine));
         if (b < SA_BINS) atomicAdd(sh.h.cnt + b, 1u);
         const Group<1> alone;
         find_bin<NT, 1>(sh, alone, false, k, 0., 0, 0);
         const int bin = sh.bin;
         // entries from here on up: all of steps 0 .. bin (a little more does no harm)
-        const float depth = (bin + 1) * (SA_RANGE / SA_BINS) * temperature;
+        const float depth = (bin + 0.5f) * (SA_RANGE / SA_BINS) / inv_t;
         float bound = bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
-        if (!(bound > -INFINITY)) bound = -INFINITY;      // (NaN: a maximum of +inf)
         if (C > 1) {
             if (tid == 0) sh.x_bound = bound;
             cta.sync();
@@ -427,30 +466,41 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     if (cuts) {
         // the histogram over steps
         u64 all = 0;
-        {
-            const bool count = k < V;
-            for (int v = v0 + lane; v < v1; v += 32) {
-                int b[N];
-                uint32_t lo[N], hi[N], old[N];
-                int j = 0;
-                data.vec(v, [&](float l, int) {           // (all atomics of a vector are on their way before the first answer is looked at)
-                    const float x = row.x_of(l);
-                    const bool in = x > -SA_RANGE;
-                    b[j] = in ? min((int)(-x * (SA_BINS / SA_RANGE)), SA_BINS - 1) : SA_BINS + lane;
-                    const u64 w = in ? Row::units(expf(x)) : 0;
-                    all += w;
-                    lo[j] = (uint32_t)w; hi[j] = (uint32_t)(w >> 32);
-                    old[j] = atomicAdd(sh.h.lo + b[j], lo[j]);
-                    if (count && in) atomicAdd(sh.h.cnt + b[j], 1u);
-                    ++j;
-                });
+        auto fill = [&](bool count) {
+            uint32_t sum_hi = 0, sum_lo = 0, n = 0;
+            for (int v = v0 + lane; v < v1; v += 32, n += N) {
+                u64 l[N / 2];
+                uint32_t b[N], wl[N], wh[N], old[N];
+                data.pairs(v, l);
 #pragma unroll
-                for (int q = 0; q < N; ++q) {
-                    const uint32_t h = hi[q] + (old[q] + lo[q] < old[q]);
-                    if (h) atomicAdd(sh.h.hi + min(b[q], SA_BINS - 1), h);
+                for (int j = 0; j < N / 2; ++j) {
+                    const u64 x = row.x_of2(l[j]), step = fma2(x, pair2(-Row::STEPS, -Row::STEPS), pair2(8388608.f, 8388608.f));
+                    u64 hi, lo;
+                    split_units2(pair2(fmaxf(expf(lo2(x)), 0.f), fmaxf(expf(hi2(x)), 0.f)), hi, lo);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t h = e ? (uint32_t)(hi >> 32) : (uint32_t)hi, w = e ? (uint32_t)(lo >> 32) : (uint32_t)lo;
+                        b[2 * j + e] = min((e ? (uint32_t)(step >> 32) : (uint32_t)step) - MAGIC, (uint32_t)SA_BINS + lane);
+                        sum_hi += h; sum_lo += w;
+                        wl[2 * j + e] = (h << 20) + (w - MAGIC);       // (h's offset is a multiple of 2^12)
+                        wh[2 * j + e] = (h - MAGIC) >> 12;
+                    }
+                }
+                // all atomics of a vector are on their way before the first answer is looked at
+#pragma unroll
+                for (int j = 0; j < N; ++j) old[j] = atomicAdd(sh.h.lo + b[j], wl[j]);
+                if (count)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) if (b[j] < SA_BINS) atomicAdd(sh.h.cnt + b[j], 1u);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const uint32_t h = wh[j] + (old[j] + wl[j] < old[j]);
+                    if (h) atomicAdd(sh.h.hi + min(b[j], SA_BINS - 1u), h);
                 }
             }
-        }
+            all = ((u64)(sum_hi - n * MAGIC) << 20) + (sum_lo - n * MAGIC);
+        };
+        fill(k < V);
         all = warp_sum(all);
         __syncthreads();
         if (lane == 0) sh.w_sum[warp] = all;
@@ -470,24 +520,44 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             const int bin = sh.bin;
             const u64 c0 = sh.cnt_before, s0 = sh.sum_before;
             // logits of step bin, and a little more on either side
-            const float unit = SA_RANGE / SA_BINS * temperature, slack = (fabsf(row.top) + (bin + 1) * unit) * 1e-6f;
-            const float high = row.top - bin * unit + slack, low = row.top - (bin + 1) * unit - slack;
-            const bool usable = low > -INFINITY && high < INFINITY;                     // (not for a maximum of +inf, or a temperature near the type's ends)
-            s = 0;
+            const float unit = SA_RANGE / SA_BINS / row.inv_t, slack = (fabsf(row.top) + (bin + 1) * unit) * 1e-6f;
+            const float high = row.top - (bin - 0.5f) * unit + slack, low = row.top - (bin + 0.5f) * unit - slack;
+            const bool usable = low > -INFINITY && high < INFINITY;                     // (not for a temperature near the type's ends)
+            uint32_t sum_hi = 0, sum_lo = 0, added = 0;
             if (usable)
-                data.each(v0, v1, [&](float l, int i) {
-                    if (l >= low) {
-                        if (l <= high) {
-                            const int b = Row::bin_of(row.x_of(l));
-                            if (b == bin) {
-                                const int at = atomicAdd(&sh.n_list, 1);
-                                if (at < SA_LIST) sh.any[at] = composite(l, i);
+                for (int v = v0 + lane; v < v1; v += 32) {
+                    u64 l[N / 2];
+                    data.pairs(v, l);
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j) most = fmaxf(most, fmaxf(lo2(l[j]), hi2(l[j])));
+                    if (!(most >= low)) continue;
+                    added += N;
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j) {
+                        const u64 x = row.x_of2(l[j]);
+                        float w[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float le = e ? hi2(l[j]) : lo2(l[j]), xe = e ? hi2(x) : lo2(x);
+                            bool ahead = le > high;
+                            if (le >= low && !ahead) {    // in the step, or next to it
+                                const uint32_t b = Row::bin_of(xe);
+                                if (b == (uint32_t)bin) {
+                                    const int at = atomicAdd(&sh.n_list, 1);
+                                    if (at < SA_LIST) sh.any[at] = composite(le, data.first + v * N + 2 * j + e);
+                                }
+                                ahead = b < (uint32_t)bin;
                             }
-                            if (b >= bin) return;
+                            w[e] = sum && ahead ? expf(xe) : 0.f;
+                            w[e] = w[e] >= min_p ? w[e] : 0.f;
                         }
-                        if (sum) { const float w = row.w_of(l); if (w >= min_p) s += Row::units(w); }
+                        u64 hi, lo;
+                        split_units2(pair2(w[0], w[1]), hi, lo);
+                        sum_hi += (uint32_t)hi + (uint32_t)(hi >> 32); sum_lo += (uint32_t)lo + (uint32_t)(lo >> 32);
                     }
-                });
+                }
+            s = ((u64)(sum_hi - added * MAGIC) << 20) + (sum_lo - added * MAGIC);
             __syncthreads();
             int n = usable ? sh.n_list : SA_LIST + 1;
             __syncthreads();                              // all have read it
@@ -614,11 +684,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                 cta.sync();
                 sh.h.template clear<NT>();
                 __syncthreads();
-                data.each(v0, v1, [&](float l, int) {
-                    const float x = row.x_of(l);
-                    const int b = Row::bin_of(x);
-                    if (b < SA_BINS) sh.h.add(b, Row::units(expf(x)));
-                });
+                fill(false);
             }
             find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0);
             summed = locate(true, thr, true);
@@ -631,14 +697,20 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             });
         }
     } else {                                              // all entries, or all that min_p leaves
-        uint32_t hi = 0, lo = 0, n = 0;                   // as split_units gives them: at most 2^18 / NT entries of up to 2^20 each
-        data.each(v0, v1, [&](float l, int) {
-            const float w = row.w_of(l);
-            uint32_t x, y;
-            split_units(w >= min_p ? w : 0.f, x, y);
-            hi += x; lo += y; ++n;
-        });
-        s = ((u64)(hi - n * MAGIC) << 20) + (lo - n * MAGIC);
+        uint32_t sum_hi = 0, sum_lo = 0, n = 0;           // with MAGIC in each: at most 2^18 / NT entries of up to 2^20
+        for (int v = v0 + lane; v < v1; v += 32, n += N) {
+            u64 l[N / 2];
+            data.pairs(v, l);
+#pragma unroll
+            for (int j = 0; j < N / 2; ++j) {
+                const u64 x = row.x_of2(l[j]);
+                const float w0 = expf(lo2(x)), w1 = expf(hi2(x));
+                u64 hi, lo;
+                split_units2(pair2(w0 >= min_p ? w0 : 0.f, w1 >= min_p ? w1 : 0.f), hi, lo);
+                sum_hi += (uint32_t)hi + (uint32_t)(hi >> 32); sum_lo += (uint32_t)lo + (uint32_t)(lo >> 32);
+            }
+        }
+        s = ((u64)(sum_hi - n * MAGIC) << 20) + (sum_lo - n * MAGIC);
     }
 
     // the warp whose stretch holds the goal
