@@ -129,8 +129,8 @@ template <int NT> struct Shared {
     float w_max[32];
     // what the CTAs of a cluster tell one another (each written once between two barriers)
     float x_top, x_bound;
-    int x_first, x_bin, x_n;
-    u64 x_cnt, x_sum, x_cnt_before, x_sum_before, x_all, x_total;
+    int x_bin, x_n;
+    u64 x_cnt, x_sum, x_cnt_before, x_sum_before, x_total;
     // answers
     int bin, n_list, index, winner;
     u64 cnt_before, sum_before, total, cut, cut_sum;
@@ -162,8 +162,9 @@ template <int NT, typename V> __device__ __forceinline__ V warps_before(const V*
 // First bin, in ascending order, behind which the search ends: by entries (the bin that holds entry number `k` from 1) or by weight (the last bin of any
 // weight with weight ahead < thr), over the histograms of C CTAs (1: this one's alone).  sh.cnt_before / sum_before: what is ahead of it, added to what was given.  sh.bin = -1: none
 // (k beyond all).  Each CTA searches its share of the bins.
+// share > 0: thr is that share of all weight, which is left in sh.total.
 template <int NT, int C>
-__device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u64 k, double thr, u64 cnt0, u64 sum0) {
+__device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u64 k, double thr, u64 cnt0, u64 sum0, float share = 0.f) {
     constexpr int SHARE = SA_BINS / C, PER = SHARE >= NT ? SHARE / NT : 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = cta.rank * SHARE + threadIdx.x * PER;
     const bool mine = threadIdx.x * PER < SHARE;
@@ -187,12 +188,19 @@ __device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u6
     __syncthreads();
     int cta_c;
     u64 cta_s;
-    u64 bc = cnt0 + warps_before<NT>(sh.w_cnt, cta_c) + ic - c, bs = sum0 + warps_before<NT>(sh.w_sum, cta_s) + is - s;
+    u64 bc = cnt0 + warps_before<NT>(sh.w_cnt, cta_c) + ic - c, bs = sum0 + warps_before<NT>(sh.w_sum, cta_s) + is - s, all = cta_s;
     if (C > 1) {                                          // shares ahead of this CTA's
         if (threadIdx.x == 0) { sh.x_cnt = cta_c; sh.x_sum = cta_s; }
         cta.sync();
-        for (int r = 0; r < cta.rank; ++r) { const Shared<NT>* o = cta.of(&sh, r); bc += o->x_cnt; bs += o->x_sum; }
+        all = 0;
+        for (int r = 0; r < C; ++r) {
+            const Shared<NT>* o = cta.of(&sh, r);
+            if (r < cta.rank) { bc += o->x_cnt; bs += o->x_sum; }
+            all += o->x_sum;
+        }
     }
+    if (share > 0.f) thr = (double)share * (double)all;
+    if (threadIdx.x == 0) sh.total = all;
     int found = -1;
     u64 mc = 0, ms = 0;
 #pragma unroll
@@ -241,6 +249,20 @@ __device__ void key_range(const Row& row, uint32_t b, uint32_t top_key, uint32_t
     hi = b == 0 ? top_key : first_with(b - 1) - 1;
 }
 
+// Maximum of a vector: packed for the 16-bit types.
+template <typename T> struct TwoOf { typedef float type; };
+template <> struct TwoOf<__nv_bfloat16> { typedef __nv_bfloat162 type; };
+template <> struct TwoOf<__half> { typedef __half2 type; };
+template <typename T> using Two = typename TwoOf<T>::type;
+__device__ __forceinline__ float max4(const float* x) { return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])); }
+__device__ __forceinline__ float max4(const __nv_bfloat162* x) {
+    const __nv_bfloat162 m = __hmax2(__hmax2(x[0], x[1]), __hmax2(x[2], x[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float max4(const __half2* x) {
+    const __half2 m = __hmax2(__hmax2(x[0], x[1]), __hmax2(x[2], x[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
 // A CTA's stretch of a row as 16-byte vectors of N entries in shared memory; the row's first vector may begin ahead of the row (what is ahead and behind is -inf).
 // Warp w owns a stretch of vectors; f(value, index) of one warp's share, lane by lane.
 template <typename T> struct RowData {
@@ -253,6 +275,11 @@ template <typename T> struct RowData {
         u.raw = reinterpret_cast<const int4*>(smem)[v];
 #pragma unroll
         for (int j = 0; j < N; ++j) f(to_f(u.x[j]), first + v * N + j);
+    }
+    __device__ __forceinline__ float most(int v) const {              // a vector's maximum (NaN does not count)
+        union { int4 raw; T x[N]; Two<T> two[4]; } u;
+        u.raw = reinterpret_cast<const int4*>(smem)[v];
+        return max4(u.two);
     }
     __device__ __forceinline__ void pairs(int v, u64* l) const {      // a vector's entries, two by two
         union { int4 raw; T x[N]; } u;
@@ -325,7 +352,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     asm volatile("cp.async.wait_all;" ::: "memory");
 
     float mine = -INFINITY;                               // this thread's maximum (NaN does not count)
-    data.each(v0, v1, [&](float l, int) { mine = fmaxf(mine, l); });
+    for (int v = v0 + lane; v < v1; v += 32) mine = fmaxf(mine, data.most(v));
     float top = mine;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -394,12 +421,14 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         }
         Shared<NT>* lead_sh = cta.of(&sh, 0);
         if (bound > -INFINITY && mine >= bound)
-            data.each(v0, v1, [&](float l, int i) {
-                if (l >= bound) {
-                    const int at = atomicAdd(&lead_sh->n_list, 1);
-                    if (at < SA_LIST) lead_sh->any[at] = composite(l, i);
-                }
-            });
+            for (int v = v0 + lane; v < v1; v += 32)
+                if (data.most(v) >= bound)
+                    data.vec(v, [&](float l, int i) {
+                        if (l >= bound) {
+                            const int at = atomicAdd(&lead_sh->n_list, 1);
+                            if (at < SA_LIST) lead_sh->any[at] = composite(l, i);
+                        }
+                    });
         cta.sync();
         const int n = lead_sh->n_list;
         cta.sync();                                       // all have read it
@@ -465,10 +494,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     u64 s = 0;                                            // of this warp's stretch: kept weight
     if (cuts) {
         // the histogram over steps
-        u64 all = 0;
         auto fill = [&](bool count) {
-            uint32_t sum_hi = 0, sum_lo = 0, n = 0;
-            for (int v = v0 + lane; v < v1; v += 32, n += N) {
+            for (int v = v0 + lane; v < v1; v += 32) {
                 u64 l[N / 2];
                 uint32_t b[N], wl[N], wh[N], old[N];
                 data.pairs(v, l);
@@ -481,7 +508,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t h = e ? (uint32_t)(hi >> 32) : (uint32_t)hi, w = e ? (uint32_t)(lo >> 32) : (uint32_t)lo;
                         b[2 * j + e] = min((e ? (uint32_t)(step >> 32) : (uint32_t)step) - MAGIC, (uint32_t)SA_BINS + lane);
-                        sum_hi += h; sum_lo += w;
                         wl[2 * j + e] = (h << 20) + (w - MAGIC);       // (h's offset is a multiple of 2^12)
                         wh[2 * j + e] = (h - MAGIC) >> 12;
                     }
@@ -498,22 +524,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                     if (h) atomicAdd(sh.h.hi + min(b[j], SA_BINS - 1u), h);
                 }
             }
-            all = ((u64)(sum_hi - n * MAGIC) << 20) + (sum_lo - n * MAGIC);
         };
         fill(k < V);
-        all = warp_sum(all);
-        __syncthreads();
-        if (lane == 0) sh.w_sum[warp] = all;
-        __syncthreads();
-        u64 total;
-        warps_before<NT>(sh.w_sum, total);
-        if (C > 1) {
-            if (tid == 0) sh.x_all = total;
-            cta.sync();
-            total = 0;
-            for (int q = 0; q < C; ++q) total += cta.of(&sh, q)->x_all;
-        }
-        __syncthreads();
+        u64 total = 0;                                    // of the k largest, where k cuts
         // The cut in sh.bin: sh.cut = composite of the last entry that stays, sh.cut_sum = weight of all that stay.  sum: whether to add up the kept weights ahead of the step.
         bool filled = true;                               // whether sh.h is the histogram over steps
         auto locate = [&](bool by_weight, double thr, bool sum) {
@@ -526,12 +539,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             uint32_t sum_hi = 0, sum_lo = 0, added = 0;
             if (usable)
                 for (int v = v0 + lane; v < v1; v += 32) {
+                    if (!(data.most(v) >= low)) continue;
                     u64 l[N / 2];
                     data.pairs(v, l);
-                    float most = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < N / 2; ++j) most = fmaxf(most, fmaxf(lo2(l[j]), hi2(l[j])));
-                    if (!(most >= low)) continue;
                     added += N;
 #pragma unroll
                     for (int j = 0; j < N / 2; ++j) {
@@ -561,18 +571,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             __syncthreads();
             int n = usable ? sh.n_list : SA_LIST + 1;
             __syncthreads();                              // all have read it
-            if (C > 1) {                                  // every CTA takes all lists
+            if (C > 1) {                                  // every CTA takes all lists, behind its own
                 if (tid == 0) sh.x_n = n;
                 cta.sync();
                 int at = n;
                 for (int q = 0; q < C; ++q) if (q != cta.rank) {
                     const Shared<NT>* o = cta.of(&sh, q);
                     const int m = o->x_n;
-                    if (at + m <= SA_LIST) for (int i = tid; i < m; i += NT) sh.sorted[at + i] = o->any[i];
+                    if (at + m <= SA_LIST) for (int i = tid; i < m; i += NT) sh.any[at + i] = o->any[i];
                     at += m;
                 }
-                cta.sync();                               // the others have read this CTA's list
-                if (at <= SA_LIST) for (int i = n + tid; i < at; i += NT) sh.any[i] = sh.sorted[i];
                 n = at;
                 __syncthreads();
             }
@@ -679,14 +687,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             }
         }
         if (top_p < 1.f) {
-            const double thr = (double)top_p * (double)total;
             if (!filled) {                                // the search for the k-th entry took the histogram
                 cta.sync();
                 sh.h.template clear<NT>();
                 __syncthreads();
                 fill(false);
             }
-            find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0);
+            double thr = (double)top_p * (double)total;
+            find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0, total ? 0.f : top_p);
+            if (!total) thr = (double)top_p * (double)sh.total;
             summed = locate(true, thr, true);
             cut = sh.cut;
         }
@@ -730,12 +739,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             all += t;
         }
         total = all;
-        cta.sync();                                       // the others have read this CTA's total
+        cluster_arrive();                                 // (a CTA stays until the others have read its total)
     }
     const u64 goal = goal_of(total);
     if (lane == 0 && before <= goal && goal < before + s) { sh.winner = warp; sh.sum_before = before; }
     __syncthreads();
-    if (sh.winner < 0) return;                            // in another CTA
+    if (sh.winner < 0) {                                  // in another CTA
+        if (C > 1) cluster_wait();
+        return;
+    }
     // its stretch again, consecutive vectors to a thread
     const int w0 = min(sh.winner * per_warp, mine_vec), w1 = min(w0 + per_warp, mine_vec), each = (w1 - w0 + NT - 1) / NT;
     const int t0 = min(w0 + tid * each, w1), t1 = min(t0 + each, w1);
@@ -761,6 +773,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                 }
                 at += w;
             });
+    if (C > 1) { __syncwarp(); cluster_wait(); }
 }
 
 constexpr size_t SA_STATIC = 25 * 1024, SA_SMEM = 232448; // shared memory beside the row, and of an SM at most
@@ -777,7 +790,7 @@ cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
     cfg.attrs = &at; cfg.numAttrs = C > 1;
     return cudaLaunchKernelEx(&cfg, k_sample<T, NT, C>, a);
 }
-// CTAs of a row: as few as hold it, and more while all rows' run at once and have some work each.  Two CTAs of 512 threads share an SM while two stretches fit its
+// CTAs of a row: as few as hold it, and more while all rows' run at once and have 8192 entries each (26 rows of 32768, top-p: 1, 2, 4, 8 CTAs 20.8, 20.4, 18.2, 22.6 us).  Two CTAs of 512 threads share an SM while two stretches fit its
 // shared memory; beyond, one CTA of 1024 has the SM to itself.
 template <typename T>
 cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
@@ -785,7 +798,7 @@ cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
     auto two = [&](int c) { return 2 * (bytes(c) + SA_STATIC + 1024) <= SA_SMEM; };
     int c = 1;
     while (bytes(c) > SA_SMEM - SA_STATIC) c *= 2;
-    while (c < 8 && (long long)rows * 2 * c <= 148 * (two(2 * c) ? 2 : 1) && a.V >= 2 * c * 4096) c *= 2;
+    while (c < 8 && (long long)rows * 2 * c <= 148 * (two(2 * c) ? 2 : 1) && a.V >= 2 * c * 8192) c *= 2;
     const size_t smem = bytes(c);
     if (two(c)) return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
     return c == 1 ? run<T, 1024, 1>(a, rows, smem, st) : c == 2 ? run<T, 1024, 2>(a, rows, smem, st) : c == 4 ? run<T, 1024, 4>(a, rows, smem, st) : run<T, 1024, 8>(a, rows, smem, st);
