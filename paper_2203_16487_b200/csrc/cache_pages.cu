@@ -66,7 +66,7 @@ __device__ bool find_pages(const Cache& c, int want, int* warp_sums) {
     const int lo = min(warp * per, c.n_pages), hi = min(lo + per, c.n_pages);
     int n = 0;
 #pragma unroll 8
-    for (int p = lo + lane; p < hi; p += 32) n += c.refs[p] == 0;
+    for (int p = lo + lane; p < hi; p += 32) n += __ldcg(c.refs + p) == 0;
 #pragma unroll
     for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     int total;
@@ -76,7 +76,7 @@ __device__ bool find_pages(const Cache& c, int want, int* warp_sums) {
     for (int p0 = lo; p0 < hi && first < want; p0 += 128) {
         bool f[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { const int p = p0 + 32 * j + lane; f[j] = p < hi && c.refs[p] == 0; }
+        for (int j = 0; j < 4; ++j) { const int p = p0 + 32 * j + lane; f[j] = p < hi && __ldcg(c.refs + p) == 0; }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const unsigned m = __ballot_sync(0xffffffffu, f[j]);
@@ -89,8 +89,9 @@ __device__ bool find_pages(const Cache& c, int want, int* warp_sums) {
     return true;
 }
 
-__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_cache_reserve(Cache c, const int* __restrict__ seqs, int n, int n_tokens) {
+__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_cache_reserve(Cache c, const int* seqs, int n, int n_tokens) {
     __shared__ int warp_sums[32];
+    op_begin();
     int run = 0;
     bool full = false;
     for (int i0 = 0; i0 < n; i0 += CP_ALLOC_THREADS) {
@@ -127,7 +128,8 @@ __global__ void __launch_bounds__(CP_ALLOC_THREADS) k_cache_reserve(Cache c, con
     }
 }
 
-__global__ void k_cache_release(Cache c, const int* __restrict__ seqs) {
+__global__ void k_cache_release(Cache c, const int* seqs) {
+    op_begin();
     const int s = seqs[blockIdx.x];
     if (!c.seq_ok(s)) { if (threadIdx.x == 0) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX); return; }
     const int held = c.held_of(s);
@@ -158,6 +160,7 @@ struct AppendArgs {
 };
 // One CTA a token and layer; a thread copies one piece of the keys and one of the values at a time.
 __global__ void k_cache_append(Cache c, AppendArgs a) {
+    op_begin();
     const int t = blockIdx.x, i = blockIdx.y, s = a.seqs[i];
     if (a.count && t >= a.count[i]) return;
     const long long slot = c.seq_ok(s) ? own_slot(c, s, c.length[s] + t) : -1;
@@ -178,10 +181,11 @@ __global__ void k_cache_append(Cache c, AppendArgs a) {
 // up to eight at a time, all eight read before the first is written: path[i] >= i, so a write goes to a slot whose own token was read before or is dropped.
 // The CTA that finishes a sequence last moves its length and gives pages back.
 constexpr int CC_PATH = 1024;
-__global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* __restrict__ seqs, const int* __restrict__ path, int path_stride,
-                                                       const int* __restrict__ n_path, int sides) {
+__global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* seqs, const int* path, int path_stride,
+                                                       const int* n_path, int sides) {
     __shared__ long long from[CC_PATH], to[CC_PATH];
     __shared__ int s_last;
+    op_begin();
     const int b = blockIdx.y, s = seqs[b], n = n_path[b];
     const int* pa = path + (long long)b * path_stride;
     if (!c.seq_ok(s)) { if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX); return; }
@@ -226,47 +230,53 @@ __global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* __res
     if (threadIdx.x == 0) { c.length[s] = len + n; c.held[s] = min(held, keep); }
 }
 
-// fork, 1 of 3: one CTA a pair.  The source's table as it is now; references of the pages that will be shared and, until the copy is done, of the page to be copied
-// (so that nobody is given it); the destination's old pages lose theirs.
-__global__ void k_fork_take(Cache c, const int* __restrict__ src, const int* __restrict__ dst) {
-    const int i = blockIdx.x, s = src[i], d = dst[i];
+// fork, 1 of 2: one CTA a pair.  The source's table as it is now; references of the pages that will be shared and, until the copy is done, of the page to be copied
+// (so that nobody is given it); the destination's old pages lose theirs.  The CTA that is through last gives a new page to each pair that copies one.
+__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_fork_take(Cache c, const int* src, const int* dst) {
+    __shared__ int warp_sums[32];
+    __shared__ int s_last;
+    op_begin();
+    const int i = blockIdx.x, n = gridDim.x, s = src[i], d = dst[i];
     int* pair = c.sc_pair() + 2 * i;
     if (!c.seq_ok(s) || !c.seq_ok(d) || s == d) {
         if (threadIdx.x == 0) { pair[0] = -1; if (s != d || !c.seq_ok(s)) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX); }
-        return;
+    } else {
+        const int pt = 1 << c.page_shift, len = min(max(c.length[s], 0), c.held_of(s) << c.page_shift), used = (len + pt - 1) / pt;
+        for (int j = threadIdx.x; j < used; j += blockDim.x) {
+            const int p = c.table[(long long)s * c.max_pages + j];
+            c.sc_rows()[(long long)i * c.max_pages + j] = p;
+            if (c.page_ok(p)) atomicAdd(c.refs + p, 1);
+        }
+        for (int j = threadIdx.x; j < c.held_of(d); j += blockDim.x) {
+            const int p = c.table[(long long)d * c.max_pages + j];
+            if (c.page_ok(p)) atomicAdd(c.refs + p, -1);
+        }
+        if (threadIdx.x == 0) { pair[0] = len; pair[1] = (len & (pt - 1)) != 0; }
     }
-    const int pt = 1 << c.page_shift, len = min(max(c.length[s], 0), c.held_of(s) << c.page_shift), used = (len + pt - 1) / pt;
-    for (int j = threadIdx.x; j < used; j += blockDim.x) {
-        const int p = c.table[(long long)s * c.max_pages + j];
-        c.sc_rows()[(long long)i * c.max_pages + j] = p;
-        if (c.page_ok(p)) atomicAdd(c.refs + p, 1);
-    }
-    for (int j = threadIdx.x; j < c.held_of(d); j += blockDim.x) {
-        const int p = c.table[(long long)d * c.max_pages + j];
-        if (c.page_ok(p)) atomicAdd(c.refs + p, -1);
-    }
-    if (threadIdx.x == 0) { pair[0] = len; pair[1] = (len & (pt - 1)) != 0; }
-}
-// 2 of 3: one CTA gives a new page to each pair that copies one.
-__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_fork_pages(Cache c, int n) {
-    __shared__ int warp_sums[32];
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicInc((unsigned*)c.sc_ticket(), n - 1) == (unsigned)n - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
     int run = 0;
     for (int i0 = 0; i0 < n; i0 += CP_ALLOC_THREADS) {
-        const int i = i0 + threadIdx.x;
+        const int j = i0 + threadIdx.x;
         int total;
-        const int need = i < n && c.sc_pair()[2 * i] >= 0 ? c.sc_pair()[2 * i + 1] : 0;
+        const int need = j < n && __ldcg(c.sc_pair() + 2 * j) >= 0 ? __ldcg(c.sc_pair() + 2 * j + 1) : 0;
         const int upto = cta_scan(need, warp_sums, &total);
-        if (i < n) c.sc_first()[i] = run + upto - need;
+        if (j < n) c.sc_first()[j] = run + upto - need;
         run += total;
     }
     const bool ok = find_pages(c, run, warp_sums);
     if (ok) for (int r = threadIdx.x; r < run; r += CP_ALLOC_THREADS) c.refs[c.sc_pages()[r]] = 1;
     if (threadIdx.x == 0) { *c.sc_ok() = ok; if (!ok) atomicOr(c.status, SPECDEC_CACHE_NO_PAGES); }
 }
-// 3 of 3: CTAs (share of the copy, pair) copy the tokens of the last page; the first of a pair writes its table.  Without pages the first
+// 2 of 2: CTAs (share of the copy, pair) copy the tokens of the last page; the first of a pair writes its table.  Without pages the first
 // part is undone.  CONTIG: a page's tokens are one stretch of memory.
 template <bool CONTIG>
-__global__ void __launch_bounds__(256) k_fork_copy(Cache c, const int* __restrict__ dst, int sides, int splits) {
+__global__ void __launch_bounds__(256) k_fork_copy(Cache c, const int* dst, int sides, int splits) {
+    op_begin();
     const int i = blockIdx.y, d = dst[i], len = c.sc_pair()[2 * i];
     if (len < 0) return;
     const bool ok = *c.sc_ok();
@@ -351,8 +361,7 @@ int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, 
     if (const char* why = view(c, v)) return op_bad("cache_reserve", why);
     if ((n && !d_seqs) || n < 0 || n > c->n_seqs || n_tokens < 0) return op_bad("cache_reserve", "d_seqs is NULL, n not in 0..n_seqs or n_tokens negative");
     if (n == 0) return SPECDEC_OK;
-    k_cache_reserve<<<1, CP_ALLOC_THREADS, 0, (cudaStream_t)stream>>>(v, d_seqs, n, n_tokens);
-    return op_launched("cache_reserve");
+    return op_done("cache_reserve", op_launch(k_cache_reserve, dim3(1), CP_ALLOC_THREADS, 0, (cudaStream_t)stream, 1, v, d_seqs, n, n_tokens));
 }
 
 int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, void* stream) {
@@ -360,8 +369,7 @@ int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, 
     if (const char* why = view(c, v)) return op_bad("cache_release", why);
     if ((n && !d_seqs) || n < 0 || n > c->n_seqs) return op_bad("cache_release", "d_seqs is NULL or n not in 0..n_seqs");
     if (n == 0) return SPECDEC_OK;
-    k_cache_release<<<n, 256, 0, (cudaStream_t)stream>>>(v, d_seqs);
-    return op_launched("cache_release");
+    return op_done("cache_release", op_launch(k_cache_release, dim3(n), 256, 0, (cudaStream_t)stream, 1, v, d_seqs));
 }
 
 int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int T,
@@ -379,8 +387,7 @@ int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, i
     AppendArgs a{(const char*)d_k, (const char*)d_v, st[0] * e, st[1] * e, st[2] * e, st[3] * e, d_seqs, d_count, layer, T, c->n_heads, c->head_dim * e / 16, v.s_head};
     if (v.heads == 1 && (c->n_heads == 1 || a.s_head == a.chunks * 16LL)) { a.chunks *= a.heads; a.heads = 1; }
     const int all = a.heads * a.chunks, threads = all <= 32 ? 32 : all <= 64 ? 64 : all <= 128 ? 128 : 256;
-    k_cache_append<<<dim3(T, n, n_layers), threads, 0, (cudaStream_t)stream>>>(v, a);
-    return op_launched("cache_append");
+    return op_done("cache_append", op_launch(k_cache_append, dim3(T, n, n_layers), threads, 0, (cudaStream_t)stream, 1, v, a));
 }
 
 int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride,
@@ -392,8 +399,7 @@ int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, 
     if (n == 0) return SPECDEC_OK;
     const int sides = 2 * c->n_layers;
     const long long ctas = ((long long)sides * v.heads * v.chunks + 127) / 128;
-    k_cache_compact<<<dim3((unsigned)(ctas < 1024 ? ctas : 1024), n), 128, 0, (cudaStream_t)stream>>>(v, d_seqs, d_path, path_stride, d_n_path, sides);
-    return op_launched("cache_compact");
+    return op_done("cache_compact", op_launch(k_cache_compact, dim3((unsigned)(ctas < 1024 ? ctas : 1024), n), 128, 0, (cudaStream_t)stream, 1, v, d_seqs, d_path, path_stride, d_n_path, sides));
 }
 
 int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream) {
@@ -402,15 +408,13 @@ int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32
     if ((n && (!d_src || !d_dst)) || n < 0 || n > c->n_seqs || n > 65535) return op_bad("cache_fork", "a pointer is NULL or n not in 0..n_seqs");
     if (n == 0) return SPECDEC_OK;
     const cudaStream_t st = (cudaStream_t)stream;
-    k_fork_take<<<n, 256, 0, st>>>(v, d_src, d_dst);
-    k_fork_pages<<<1, CP_ALLOC_THREADS, 0, st>>>(v, n);
+    const cudaError_t e = op_launch(k_fork_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, d_src, d_dst);
+    if (e != cudaSuccess) return op_done("cache_fork", e);
     const int sides = 2 * c->n_layers;
     const long long most = (long long)c->page_tokens * v.heads * v.chunks;             // pieces of a side's page
     const int splits = most <= 4096 ? 1 : most >= 32768 ? 8 : (int)(most / 4096);
     const bool contig = v.heads == 1 && v.s_token == v.chunks * 16LL;
-    if (contig) k_fork_copy<true><<<dim3(sides * splits, n), 256, 0, st>>>(v, d_dst, sides, splits);
-    else k_fork_copy<false><<<dim3(sides * splits, n), 256, 0, st>>>(v, d_dst, sides, splits);
-    return op_launched("cache_fork");
+    return op_done("cache_fork", op_launch(contig ? k_fork_copy<true> : k_fork_copy<false>, dim3(sides * splits, n), 256, 0, st, 1, v, d_dst, sides, splits));
 }
 
 }  // extern "C"

@@ -318,6 +318,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     constexpr int NW = NT / 32, N = RowData<T>::N;
     extern __shared__ __align__(16) char row_smem[];
     __shared__ Shared<NT> sh;
+    op_begin();
     const Group<C> cta;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
     const int r = blockIdx.x / C, pr = r / a.per_param;
@@ -782,13 +783,7 @@ cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
     static_assert(sizeof(Shared<NT>) <= SA_STATIC, "what is beside the row");
     static const cudaError_t attr = cudaFuncSetAttribute(k_sample<T, NT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SA_SMEM - SA_STATIC));
     if (attr != cudaSuccess) return attr;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(rows * C); cfg.blockDim = dim3(NT); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = C; at.val.clusterDim.y = at.val.clusterDim.z = 1;
-    cfg.attrs = &at; cfg.numAttrs = C > 1;
-    return cudaLaunchKernelEx(&cfg, k_sample<T, NT, C>, a);
+    return op_launch(k_sample<T, NT, C>, dim3(rows * C), NT, smem, st, C, a);
 }
 // CTAs of a row: as few as hold it, and more while all rows' run at once and have 8192 entries each (26 rows of 32768, top-p: 1, 2, 4, 8 CTAs 20.8, 20.4, 18.2, 22.6 us).  Two CTAs of 512 threads share an SM while two stretches fit its
 // shared memory; beyond, one CTA of 1024 has the SM to itself.
@@ -821,5 +816,5 @@ extern "C" int specdec_sample(const void* d_logits, int dtype, long long stride,
     const SampleArgs a{d_logits, stride, V, d_uniform, d_temperature, d_top_k, d_top_p, d_min_p, rows_per_param, d_token, d_logprob};
     const cudaStream_t st = (cudaStream_t)stream;
     const cudaError_t e = dtype == SPECDEC_DTYPE_F32 ? launch<float>(a, rows, st) : dtype == SPECDEC_DTYPE_BF16 ? launch<__nv_bfloat16>(a, rows, st) : launch<__half>(a, rows, st);
-    return e == cudaSuccess ? SPECDEC_OK : op_fail(SPECDEC_ERR_CUDA, "sample", cudaGetErrorString(e));
+    return op_done("sample", e);
 }

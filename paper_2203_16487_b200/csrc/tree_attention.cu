@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
+    op_begin();
     TaWork work;
     work.begin(a, blocks_of);
     Part it;
@@ -123,6 +124,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
     int* blocks_of = reinterpret_cast<int*>(q + Cfg::FLOATS);
     uint32_t* any = reinterpret_cast<uint32_t*>(blocks_of + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
+    op_begin();
     TaWork work;
     work.begin(a, blocks_of);
     const int chunks = a.dim / 4;
@@ -305,7 +307,7 @@ template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *rei
 template <typename T>
 __global__ void __launch_bounds__(128, 8) k_ta_merge(TreeAttn a, int rows) {
     const int lane = threadIdx.x & 31, ht = a.kv_heads * a.tiles, all = a.T * a.group;
-    cudaGridDependencySynchronize();
+    op_begin();
     for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * all; w += gridDim.x * 4) {
         const int bh = w / all, gr = w - bh * all, b = bh / a.kv_heads, h = bh - b * a.kv_heads, tile = gr / rows, r = gr - tile * rows;
         const int2 at = a.where[bh * a.tiles + tile];     // first slot, parts
@@ -373,27 +375,19 @@ cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 4);
     if (attr != cudaSuccess) return attr;
-    k_ta_small_pages<T, DP, NS><<<grid, 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
-    return cudaGetLastError();
+    return op_launch(k_ta_small_pages<T, DP, NS>, dim3(grid), 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, a);
 }
 template <int DP>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int BYTES = TfCfg<DP>::FLOATS * 4;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 4);
     if (attr != cudaSuccess) return attr;
-    k_ta_f32<DP><<<!a.direct || grid < TA_SMS ? grid : TA_SMS, 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(a);
-    return cudaGetLastError();
+    return op_launch(k_ta_f32<DP>, dim3(!a.direct || grid < TA_SMS ? grid : TA_SMS), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, a);
 }
-// The merge is launched while the items run, and waits for them.
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
     const long long ctas = ((long long)a.B * a.kv_heads * a.T * a.group + 3) / 4;
-    cfg.gridDim = dim3((unsigned)(ctas < 8 * TA_SMS ? ctas : 8 * TA_SMS)); cfg.blockDim = dim3(128); cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization; at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_ta_merge<T>, a, rows);
+    return op_launch(k_ta_merge<T>, dim3((unsigned)(ctas < 8 * TA_SMS ? ctas : 8 * TA_SMS)), 128, 0, st, 1, a, rows);
 }
 PFN_encodeTiled encoder() {
     static const PFN_encodeTiled fn = [] {
@@ -483,7 +477,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
         rc = p.rows >= 128 ? ta_tc(tm, a, c->dtype, p.rows, (int)p.grid, s) : ta_tma_mma(tm, a, c->dtype, p.rows, (int)p.grid, s);
     }
     if (rc == cudaSuccess && need) rc = c->dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, p.rows, s) : bf ? run_merge<__nv_bfloat16>(a, p.rows, s) : run_merge<__half>(a, p.rows, s);
-    return rc == cudaSuccess ? SPECDEC_OK : op_fail(SPECDEC_ERR_CUDA, who, cudaGetErrorString(rc));
+    return op_done(who, rc);
 }
 
 }  // extern "C"

@@ -33,6 +33,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
+    op_begin();
     TaWork work;
     work.begin(a, blocks_of);
     __syncthreads();
@@ -154,8 +155,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
         return n < 1 ? 1 : n;
     }();
     const int most = a.direct ? per_sm * TA_SMS : grid;   // whole sequences: as many CTAs as run at once
-    k_ta_tma<T, DP, WM, WK, NS><<<grid < most ? grid : most, 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B + 1) * 4, st>>>(tm, a);
-    return cudaGetLastError();
+    return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(grid < most ? grid : most), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B + 1) * 4, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {

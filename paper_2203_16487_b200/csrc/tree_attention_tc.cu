@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_map(&tm);
     }
+    op_begin();
     TaWork work;
     work.begin(a, blocks_of);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 512);
@@ -416,8 +417,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
     static_assert(MOST <= 232448 - (TILES == 1 ? 1536 : 512), "shared memory of an SM");
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tc<T, DP, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
-    k_ta_tc<T, DP, TILES><<<grid < TA_SMS || !a.direct ? grid : TA_SMS, 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st>>>(tm, a);
-    return cudaGetLastError();
+    return op_launch(k_ta_tc<T, DP, TILES>, dim3(grid < TA_SMS || !a.direct ? grid : TA_SMS), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {

@@ -71,6 +71,7 @@ class PagedCache:
                         table.data_ptr(), length.data_ptr(), held.data_ptr(), refs.data_ptr(), self.status.data_ptr(), self._scratch.data_ptr())
         self._ref, self._lib, self._device = C.byref(self._c), lib(), kv.get_device()
         self._code, self._page = DTYPES[kv.dtype], page
+        self._workspaces = {}                              # bytes by sizes of a call
         self.dtype, self.n_heads, self.head_dim, self.max_length = kv.dtype, H, D, table.shape[1] * page
 
     def reserve(self, seqs, n_tokens: int):
@@ -173,9 +174,14 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     if 0 < max_length < bound:
         bound = max_length
     L = cache._lib
-    n = L.specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._code, cache._page, bound)
-    if n < 0:
-        _fail(n)
+    n = cache._workspaces.get((B, T, H, bound))
+    if n is None:
+        n = L.specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._code, cache._page, bound)
+        if n < 0:
+            _fail(n)
+        if len(cache._workspaces) > 4096:
+            cache._workspaces.clear()
+        cache._workspaces[B, T, H, bound] = n
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, (B,)), m,
                           0 if one else T * W, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)), bound, D ** -0.5 if scale is None else scale,
@@ -191,26 +197,28 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     probability fp32 [...]).  The parameters (fp32, top_k int32; None: off) are tensors of one entry for each row, or for each equal run of rows ([n] for logits [n, T, V])."""
     shape = logits.shape
     V, lead = shape[-1], shape[:-1]
-    if logits.dtype not in DTYPES or not logits.is_cuda or logits.stride(-1) != 1:
+    code = DTYPES.get(logits.dtype)
+    if code is None or not logits.is_cuda or logits.stride(-1) != 1:
         raise ValueError("logits: a device tensor of fp32, bf16 or fp16 with a contiguous last dimension is wanted")
-    flat = logits if len(shape) == 2 else logits.reshape(-1, V)
-    rows = flat.shape[0]
     if uniform.shape != lead or uniform.dtype is not torch.float32 or not uniform.is_cuda or not uniform.is_contiguous():
         raise ValueError("uniform: a contiguous fp32 device tensor, one number a row, is wanted")
-    n, ptrs = 0, []
-    for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, _I32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if t is None:
-            ptrs.append(None)
-            continue
-        m = t.numel()
-        if t.dtype is not dt or not t.is_cuda or not t.is_contiguous() or m < 1 or rows % m or (n and n != m):
-            raise ValueError(f"{name}: a contiguous {dt} device tensor is wanted, one entry for each equal run of rows, as many as the other parameters")
-        n = m
-        ptrs.append(t.data_ptr())
+    rows, stride = uniform.numel(), V
+    if not logits.is_contiguous():
+        logits = logits if len(shape) == 2 else logits.reshape(-1, V)
+        stride = logits.stride(0) if rows > 1 else V
+    n, ptrs = 0, [None] * 4
+    for i, t in enumerate((temperature, top_k, top_p, min_p)):
+        if t is not None:
+            m = t.numel()
+            if t.dtype is not (_I32 if i == 1 else torch.float32) or not t.is_cuda or not t.is_contiguous() or m < 1 or rows % m or (n and n != m):
+                raise ValueError(("temperature", "top_k", "top_p", "min_p")[i] + ": a contiguous fp32 (top_k: int32) device tensor is wanted, one entry for each "
+                                 "equal run of rows, as many as the other parameters")
+            n = m
+            ptrs[i] = t.data_ptr()
     logprob = torch.empty_like(uniform)
     token = torch.empty_like(uniform, dtype=_I32)
-    rc = lib().specdec_sample(flat.data_ptr(), DTYPES[logits.dtype], flat.stride(0) if rows > 1 else V, rows, V, uniform.data_ptr(), *ptrs,
-                              rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _raw_stream(logits.get_device()))
+    rc = lib().specdec_sample(logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(),
+                              _raw_stream(logits.get_device()))
     if rc:
         _fail(rc)
     return token, logprob
