@@ -8,7 +8,7 @@ namespace sd {
 int op_fail(int code, const char* who, const char* why) noexcept;      // returns code
 inline int op_bad(const char* who, const char* why) { return op_fail(SPECDEC_ERR_INVALID_ARG, who, why); }
 inline int op_elem_bytes(int dtype) { return dtype == SPECDEC_DTYPE_F32 ? 4 : dtype == SPECDEC_DTYPE_BF16 || dtype == SPECDEC_DTYPE_F16 ? 2 : 0; }
-// Launches behind one another: a kernel that begins with op_begin() may be launched while its predecessor in the stream still runs, and waits for it there.  What such a kernel
+// Launches behind one another: a kernel that begins with op_begin() is set up while its predecessor in the stream still runs, and waits for it there.  What such a kernel
 // reads comes by pointers without __restrict__: the compiler may fetch what those lead to ahead of the wait.
 // (cluster > 1: CTAs of a cluster.)
 template <typename... P, typename... A>
@@ -22,7 +22,7 @@ inline cudaError_t op_launch(void (*kernel)(P...), dim3 grid, int threads, size_
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 #ifdef __CUDACC__
-__device__ __forceinline__ void op_begin() { asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void op_begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 inline int op_done(const char* who, cudaError_t e) {
     if (e == cudaSuccess) return SPECDEC_OK;

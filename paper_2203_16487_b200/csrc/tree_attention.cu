@@ -298,44 +298,76 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
 }
 
 // ------------------------------------------------------------------ merge
-template <typename T> __device__ __forceinline__ void put(char* p, float x);
-template <> __device__ __forceinline__ void put<float>(char* p, float x) { *reinterpret_cast<float*>(p) = x; }
-template <> __device__ __forceinline__ void put<__nv_bfloat16>(char* p, float x) { *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ void put<__half>(char* p, float x) { *reinterpret_cast<__half*>(p) = __float2half_rn(x); }
+// Four columns; `whole`: as one store.
+template <typename T> __device__ __forceinline__ void put4(char* p, float4 x, int whole) {
+    if constexpr (sizeof(T) == 4) {
+        if (whole) { *reinterpret_cast<float4*>(p) = x; return; }
+        float* f = reinterpret_cast<float*>(p);
+        f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+    } else {
+        const uint32_t u = Half<T>::pack(x.x, x.y), v = Half<T>::pack(x.z, x.w);
+        if (whole) { *reinterpret_cast<uint2*>(p) = make_uint2(u, v); return; }
+        unsigned short* f = reinterpret_cast<unsigned short*>(p);
+        f[0] = (unsigned short)u; f[1] = (unsigned short)(u >> 16); f[2] = (unsigned short)v; f[3] = (unsigned short)(v >> 16);
+    }
+}
 
-// The parts' outputs, each rescaled to the largest maximum: one warp a query row, CTAs that stay.
-template <typename T>
+// The parts' outputs, each rescaled to the largest maximum: one warp R query rows of a tile, CTAs that stay.  Three reads that wait for one another: a tile's
+// parts; their maxima and sums (32 / R lanes a row, one a part); their outputs (lane: four columns), U parts on their way at a time.  R = 4 where there are rows enough for
+// all warps of the GPU that way (16384 rows of 2 or 3 parts: 16.5 us with R = 1), else 1.
+template <typename T, int R, int U>
 __global__ void __launch_bounds__(128, 8) k_ta_merge(TreeAttn a, int rows) {
-    const int lane = threadIdx.x & 31, ht = a.kv_heads * a.tiles, all = a.T * a.group;
+    constexpr int L = 32 / R;
+    const int lane = threadIdx.x & 31, columns = a.kv_heads * a.tiles, all = a.T * a.group, sets = (all + R - 1) / R, x = lane / L, e = lane % L;
     op_begin();
-    for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * all; w += gridDim.x * 4) {
-        const int bh = w / all, gr = w - bh * all, b = bh / a.kv_heads, h = bh - b * a.kv_heads, tile = gr / rows, r = gr - tile * rows;
+    for (int w = blockIdx.x * 4 + (threadIdx.x >> 5); w < a.B * a.kv_heads * sets; w += gridDim.x * 4) {
+        const int bh = w / sets, gr0 = (w - bh * sets) * R, b = bh / a.kv_heads, h = bh - b * a.kv_heads, tile = gr0 / rows, r0 = gr0 - tile * rows;
         const int2 at = a.where[bh * a.tiles + tile];     // first slot, parts
         if (at.y <= 1) continue;
-        const long long slot0 = (long long)at.x * rows + r, step = (long long)ht * rows;
-        float m = -INFINITY;
-        for (int s = lane; s < at.y; s += 32) m = fmaxf(m, a.part_ml[slot0 + s * step].x);
+        const long long slot0 = (long long)at.x * rows + r0, step = (long long)columns * rows;
+        float m = -INFINITY;                              // of row x
+        for (int s = e; s < at.y; s += L) m = fmaxf(m, a.part_ml[slot0 + x + s * step].x);
 #pragma unroll
-        for (int of = 16; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
+        for (int of = L / 2; of; of >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, of));
         const float z = m == -INFINITY ? 0.f : m;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);       // lane: four columns
+        float4 o[R];
         float l = 0.f;
-#pragma unroll 4
-        for (int s = 0; s < at.y; ++s) {
-            const long long slot = slot0 + s * step;
-            const float2 ml = a.part_ml[slot];
-            const float f = exp2f(ml.x - z);
-            l += ml.y * f;
-            if (lane * 4 < a.dim) {
-                const float4 x = *reinterpret_cast<const float4*>(a.part + slot * a.dim + lane * 4);
-                o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+#pragma unroll
+        for (int i = 0; i < R; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < at.y; s0 += L) {
+            float f = 0.f;                                // of row x, part s0 + e
+            if (s0 + e < at.y) {
+                const float2 ml = a.part_ml[slot0 + x + (s0 + e) * step];
+                f = exp2f(ml.x - z);
+                l += ml.y * f;
+            }
+            for (int s = s0; s < min(s0 + L, at.y); s += U) {
+                float4 v[U][R];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+                        v[u][i] = lane * 4 < a.dim && s + u < at.y ? *reinterpret_cast<const float4*>(a.part + (slot0 + (s + u) * step + i) * a.dim + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < R; ++i) {
+                        const float g = __shfl_sync(0xffffffffu, f, i * L + (s + u - s0) % L);
+                        o[i].x = fmaf(v[u][i].x, g, o[i].x); o[i].y = fmaf(v[u][i].y, g, o[i].y); o[i].z = fmaf(v[u][i].z, g, o[i].z); o[i].w = fmaf(v[u][i].w, g, o[i].w);
+                    }
             }
         }
-        if (lane * 4 >= a.dim) continue;
-        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-        const int t = ta_node(a, gr);
-        char* p = a.out + b * a.o_sb + t * a.o_st + (h * a.group + gr - t * a.group) * a.o_sh + lane * 4 * sizeof(T);
-        put<T>(p, o.x * inv); put<T>(p + sizeof(T), o.y * inv); put<T>(p + 2 * sizeof(T), o.z * inv); put<T>(p + 3 * sizeof(T), o.w * inv);
+#pragma unroll
+        for (int of = L / 2; of; of >>= 1) l += __shfl_xor_sync(0xffffffffu, l, of);
+        const float inv_x = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float inv = __shfl_sync(0xffffffffu, inv_x, i * L);
+            const int gr = gr0 + i;
+            if (gr >= all || lane * 4 >= a.dim) continue;
+            const int t = ta_node(a, gr);
+            put4<T>(a.out + b * a.o_sb + t * a.o_st + (h * a.group + gr - t * a.group) * a.o_sh + lane * 4 * sizeof(T), make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
+        }
     }
 }
 
@@ -386,8 +418,10 @@ cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
-    const long long ctas = ((long long)a.B * a.kv_heads * a.T * a.group + 3) / 4;
-    return op_launch(k_ta_merge<T>, dim3((unsigned)(ctas < 8 * TA_SMS ? ctas : 8 * TA_SMS)), 128, 0, st, 1, a, rows);
+    const long long every = (long long)a.B * a.kv_heads * a.T * a.group, most = 8 * TA_SMS;
+    const bool four = every >= 4 * most;
+    const long long ctas = (four ? every / 4 : every) / 4 + 1;
+    return op_launch(four ? k_ta_merge<T, 4, 1> : k_ta_merge<T, 1, 8>, dim3((unsigned)(ctas < most ? ctas : most)), 128, 0, st, 1, a, rows);
 }
 PFN_encodeTiled encoder() {
     static const PFN_encodeTiled fn = [] {

@@ -205,30 +205,28 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         while (work.next(a, blocks_of, it, t == 0)) {
         const SeqKeys& s = it.s;
         const int r0 = it.tile * ROWS;
-#pragma unroll
-        for (int i0 = 0; i0 < ROWS * (DP / 8); i0 += 8 * 256) {       // the queries, eight pieces a thread at a time
-            uint4 x[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int i = i0 + u * 256 + t, r = i / (DP / 8), c = i % (DP / 8), gr = r0 + r, node = ta_node(a, gr);
-                x[u] = make_uint4(0, 0, 0, 0);
-                if (i < ROWS * (DP / 8) && gr < all_rows && node < s.nodes && c * 8 < a.dim) {
-                    const char* p = a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + c * 16;
-                    if (a.q_vec) x[u] = *reinterpret_cast<const uint4*>(p);
-                    else {
-                        const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
-                        x[u] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-                    }
+        // the queries: thread t takes piece t % PIECES of every (256 / PIECES)-th row
+        constexpr int PIECES = DP / 8;
+        const int qc = t % PIECES;
+        char* q_to = qs + (qc >> 3) * TC_ROWS * 128;
+        const char* q_from = a.q + it.b * a.q_sb + it.h * a.group * a.q_sh + qc * 16;
+#pragma unroll 4
+        for (int r = t / PIECES; r < ROWS; r += 256 / PIECES) {
+            const int gr = r0 + r, node = ta_node(a, gr);
+            const bool real = gr < all_rows && node < s.nodes && qc * 8 < a.dim;
+            const char* p = q_from + (real ? node * a.q_st + (gr - node * a.group) * a.q_sh : 0);
+            char* to = q_to + (r / TC_ROWS) * Cfg::Q + (r % TC_ROWS) * 128 + (((qc & 7) ^ (r & 7)) << 4);
+            if (a.q_vec) ta_copy16(smem_u32(to), real ? p : a.q, real);
+            else {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (real) {
+                    const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
+                    x = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
                 }
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int i = i0 + u * 256 + t, r = i / (DP / 8), c = i % (DP / 8);
-                if (i < ROWS * (DP / 8))
-                    *reinterpret_cast<uint4*>(qs + (r / TC_ROWS) * Cfg::Q + (c >> 3) * TC_ROWS * 128 + (r % TC_ROWS) * 128 + (((c & 7) ^ (r & 7)) << 4)) = x[u];
+                *reinterpret_cast<uint4*>(to) = x;
             }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
         for (int w = t; w < a.words; w += 256) any[w] = 0;            // what they see (as ta_load_masks, by the threads from 128 on)
         softmax_warps();
         const int t0n = ta_node(a, r0), t1n = min(ta_node(a, min(r0 + ROWS, all_rows) - 1), a.T - 1);
@@ -239,6 +237,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
             mask[i] = m;
             if (m) atomicOr(any + w, m);
         }
+        asm volatile("cp.async.wait_all;\n\tfence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         asm volatile("bar.sync 2, 288;" ::: "memory");
 
@@ -346,6 +345,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         if (TILES == 2 || g == 0) {
             // through this group's queries' place in shared memory, 128 rows of 128 bytes at a time, so that rows leave in whole lines
             const float inv = !it.whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;
+            constexpr int BUFFERS = Cfg::Q / (TC_ROWS * 128);                            // 2 (one is filled while the other leaves), or 1
             char* stage = qs + (TILES == 2 ? g : 0) * Cfg::Q;
             auto group_sync = [&] { asm volatile("bar.sync %0, 128;" ::"r"(3 + g) : "memory"); };
             auto columns = [&](int c, float* x) {         // 32 columns of this thread's row
@@ -363,6 +363,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
             };
             const int per = it.whole ? 64 : 32;           // columns of 128 bytes
             for (int c0 = 0; c0 < a.dim; c0 += per) {
+                if (BUFFERS == 2) stage = qs + (TILES == 2 ? g : 0) * Cfg::Q + (c0 / per & 1) * TC_ROWS * 128;
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf) {
                     if (hf && !it.whole) break;
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                         *reinterpret_cast<uint4*>(a.part + (it.slot * ROWS + r_out) * a.dim + col) = y;
                     }
                 }
-                group_sync();
+                if (BUFFERS == 1) group_sync();
             }
             if (gr < all_rows && !it.whole) a.part_ml[it.slot * ROWS + r] = make_float2(m, l);
         }
