@@ -16,15 +16,15 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     constexpr int ROWS = 64, KT = TA_BLOCK, PITCH = DP * 2, PIECES = DP / 8, STAGE = 2 * KT * PITCH;
     extern __shared__ __align__(128) char sm[];
     char* ring = sm;                                      // [NS][K, V][KT][PITCH]; at first the queries
-    int* blocks_of = (int*)(sm + NS * STAGE);
-    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : a.B));
+    int4* seqs = (int4*)(sm + NS * STAGE);
+    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
     op_begin();
     TaWork work;
-    work.begin(a, blocks_of);
+    work.begin(a, seqs);
     Part it;
-    while (work.next(a, blocks_of, it, tid == 0)) {
+    while (work.next(a, seqs, it, tid == 0)) {
     __syncthreads();
     const int h = it.h, r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = r0 / a.group;
     const SeqKeys& s = it.s;
@@ -121,15 +121,15 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
     float* kt = q + TF_ROWS * KP + warp * Cfg::WARP;      // [32][KP]
     float* vt = kt + TF_KT * KP;
     float* pt = vt + TF_KT * KP;                          // [16][PP]
-    int* blocks_of = reinterpret_cast<int*>(q + Cfg::FLOATS);
-    uint32_t* any = reinterpret_cast<uint32_t*>(blocks_of + (a.direct ? 0 : a.B));
+    int4* seqs = reinterpret_cast<int4*>(q + Cfg::FLOATS);
+    uint32_t* any = reinterpret_cast<uint32_t*>(seqs + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     op_begin();
     TaWork work;
-    work.begin(a, blocks_of);
+    work.begin(a, seqs);
     const int chunks = a.dim / 4;
     Part it;
-    while (work.next(a, blocks_of, it, tid == 0)) {
+    while (work.next(a, seqs, it, tid == 0)) {
         __syncthreads();
         const int r0 = it.tile * TF_ROWS, all_rows = a.T * a.group, t0 = ta_node(a, r0);
         const SeqKeys& s = it.s;
@@ -380,7 +380,7 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
     const int most_mma = head_dim > 64 ? 32 : 64;
-    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma ? 64 : all <= 128 ? 128 : 256;
+    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma ? 64 : all <= 128 || (head_dim > 64 && T > TA_WIDE_T) ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
     p.min_blocks = 4;
@@ -405,16 +405,16 @@ long long workspace(const Plan& p, int B, int n_kv_heads, int head_dim) {
 template <typename T, int DP>
 cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 4);
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_small_pages<T, DP, NS>, dim3(grid), 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, a);
+    return op_launch(k_ta_small_pages<T, DP, NS>, dim3(grid), 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, a);
 }
 template <int DP>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int BYTES = TfCfg<DP>::FLOATS * 4;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 4);
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_f32<DP>, dim3(!a.direct || grid < TA_SMS ? grid : TA_SMS), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, a);
+    return op_launch(k_ta_f32<DP>, dim3(!a.direct || grid < TA_SMS ? grid : TA_SMS), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, a);
 }
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {

@@ -19,6 +19,7 @@ namespace sd {
 // whatever the lengths are.  A stretch begins and ends inside sequences: a part that is a whole sequence writes the output, other parts write partial results
 // into slots that k_ta_merge joins.  The part of sequence b in the column's CTA c has slot (c + b) * columns + column: along the line either c or b grows.
 constexpr int TA_SMS = 148, TA_BLOCK = 64, TA_MAX_B = 128;            // sequences at most where they are cut
+constexpr int TA_WIDE_T = 960;                            // nodes at most whose masks fit beside a 256-row tile of 128-wide heads
 struct TreeAttn {
     const char* q; char* out; const char* k; const char* v;
     long long q_sb, q_st, q_sh, o_sb, o_st, o_sh, s_page, s_token, s_head;             // bytes
@@ -50,30 +51,35 @@ __device__ __forceinline__ SeqKeys ta_keys(const TreeAttn& a, int b) {
 
 struct Part { int b, h, tile, k_begin, k_end, blocks, whole; long long slot; SeqKeys s; };     // keys [k_begin, k_end) in `blocks` blocks
 struct TaWork {
-    int column, at, b, skip, left, stretch;               // direct: at = number of the next (sequence, column).  Else: the CTA, and what is next on the line: sequence, blocks of it to skip; blocks left, blocks of a stretch
-    // For the whole CTA; blocks_of: B ints of shared memory that stay (not direct).
-    __device__ __forceinline__ void begin(const TreeAttn& a, int* blocks_of) {
+    // direct: at = number of the next (sequence, column).  Else: the CTA, and what is next on the line: sequence, blocks of it to skip; blocks left, blocks of a stretch
+    int column, at, b, skip, left, stretch;
+    // For the whole CTA; seqs: B entries (sequence, length, nodes, blocks) of shared memory that stay (not direct).
+    __device__ __forceinline__ void begin(const TreeAttn& a, int4* seqs) {
         const int columns = a.kv_heads * a.tiles;
         at = blockIdx.x;
         if (a.direct) return;
         __shared__ int found[4];
         column = blockIdx.x % columns; at = blockIdx.x / columns;
-        for (int i = threadIdx.x; i < a.B; i += blockDim.x) blocks_of[i] = max(1, (ta_keys(a, i).keys + a.unit - 1) / a.unit);      // (at least 1: rows that see nothing are written too)
+        for (int i = threadIdx.x; i < a.B; i += blockDim.x) {
+            const SeqKeys s = ta_keys(a, i);
+            seqs[i] = make_int4(s.seq, s.len, s.nodes, max(1, (s.keys + a.unit - 1) / a.unit));        // (at least 1: rows that see nothing are written too)
+        }
         __syncthreads();
         if (threadIdx.x < 32) {
             const int lane = threadIdx.x;
-            long long total = 0;
-            for (int i = lane; i < a.B; i += 32) total += blocks_of[i];
+            unsigned long long total = 0;
+            for (int i = lane; i < a.B; i += 32) total += seqs[i].w;
 #pragma unroll
             for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            const long long per = max((total + a.ctas - 1) / a.ctas, (long long)a.min_blocks), start = at * per;
-            long long run = 0;
+            const unsigned long long per = max(total < 0x40000000ull ? ((uint32_t)total + a.ctas - 1) / (uint32_t)a.ctas : (total + a.ctas - 1) / a.ctas, (unsigned long long)a.min_blocks);
+            const unsigned long long start = at * per;
+            unsigned long long run = 0;
             int fb = 0, fskip = 0;
             for (int i0 = 0; i0 < a.B; i0 += 32) {        // the sequence in which the stretch begins
-                const int n = i0 + lane < a.B ? blocks_of[i0 + lane] : 0;
-                int upto = n;
+                const int n = i0 + lane < a.B ? seqs[i0 + lane].w : 0;
+                unsigned long long upto = n;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
+                for (int o = 1; o < 32; o <<= 1) { const unsigned long long x = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += x; }
                 const unsigned m = __ballot_sync(0xffffffffu, run + upto > start);
                 if (m) {
                     const int f = __ffs(m) - 1;
@@ -83,13 +89,17 @@ struct TaWork {
                 }
                 run += __shfl_sync(0xffffffffu, upto, 31);
             }
-            if (lane == 0) { found[0] = fb; found[1] = fskip; found[2] = (int)max(0ll, min(per, total - start)); found[3] = (int)min(per, 0x3fffffffll); }
+            if (lane == 0) {
+                found[0] = fb; found[1] = fskip;
+                found[2] = start < total ? (int)min(per, total - start) : 0;
+                found[3] = (int)min(per, 0x3fffffffull);
+            }
         }
         __syncthreads();
         b = found[0]; skip = found[1]; left = found[2]; stretch = found[3];
     }
     // The next part.  notes: whether this thread tells the merge where a sequence's parts are.
-    __device__ __forceinline__ bool next(const TreeAttn& a, const int* blocks_of, Part& p, bool notes = false) {
+    __device__ __forceinline__ bool next(const TreeAttn& a, const int4* seqs, Part& p, bool notes = false) {
         const int columns = a.kv_heads * a.tiles;
         if (a.direct) {
             if (at >= a.B * columns) return false;
@@ -100,9 +110,10 @@ struct TaWork {
             p.blocks = (p.s.keys + a.unit - 1) / a.unit;
         } else {
             if (left <= 0) return false;
-            const int n = blocks_of[b], take = min(n - skip, left);
+            const int4 q = seqs[b];
+            const int n = q.w, take = min(n - skip, left);
             p.b = b;
-            p.s = ta_keys(a, b);
+            p.s.seq = q.x; p.s.len = q.y; p.s.nodes = q.z; p.s.keys = q.z ? q.y + q.z : 0;
             p.k_begin = skip * a.unit; p.k_end = min(p.s.keys, (skip + take) * a.unit);
             p.blocks = max(0, (p.k_end - p.k_begin + a.unit - 1) / a.unit);
             p.whole = take == n;

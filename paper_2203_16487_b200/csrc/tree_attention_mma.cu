@@ -22,8 +22,8 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     __shared__ __align__(8) uint64_t bars[2 * NS];
     __shared__ int abort_flag;
     char* ring = ta_smem + (1024 - (smem_u32(ta_smem) & 1023)) % 1024;
-    int* blocks_of = (int*)(ring + NS * STAGE);               // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : (a.B + 1) / 2 * 2));
+    int4* seqs = (int4*)(ring + NS * STAGE);              // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
     uint32_t* mask = any + (a.words + 1) / 2 * 2;         // (8-byte aligned, as the partial results behind it are)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
@@ -35,14 +35,14 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     }
     op_begin();
     TaWork work;
-    work.begin(a, blocks_of);
+    work.begin(a, seqs);
     __syncthreads();
 
     if (warp == TM_WARPS) {                               // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
         int count = 0;                                    // lane g: blocks that group g had in the parts before
         Part it, ahead;
-        for (bool more = work.next(a, blocks_of, ahead); more;) {
+        for (bool more = work.next(a, seqs, ahead); more;) {
             it = ahead;
             const int* table = a.table + (long long)it.s.seq * a.max_pages;
             auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
                 return (unsigned)p < (unsigned)a.n_pages ? p : a.n_pages;
             };
             int p = it.blocks ? page_of(0) : 0;
-            more = work.next(a, blocks_of, ahead);
+            more = work.next(a, seqs, ahead);
             for (int j = 0; j < it.blocks; ++j) {
                 const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), key = it.k_begin + j * KT + lane * box, cur = p;
                 if (j + 1 < it.blocks) p = page_of(j + 1);
@@ -79,9 +79,9 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     auto consumers = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * TM_WARPS) : "memory"); };
     int count = 0;                                        // this group's blocks so far
     Part it, ahead;
-    for (bool more = work.next(a, blocks_of, ahead, tid == 0); more;) {
+    for (bool more = work.next(a, seqs, ahead, tid == 0); more;) {
         it = ahead;
-        more = work.next(a, blocks_of, ahead, tid == 0);
+        more = work.next(a, seqs, ahead, tid == 0);
         const SeqKeys& s = it.s;
         const int r0 = it.tile * ROWS, t0 = ta_node(a, r0);
         const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
@@ -129,13 +129,13 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         rows.finish(live_a, live_b);
         if constexpr (WK > 1) {                           // the groups' results meet in the first group
             constexpr int RP = TaRows<T, DP>::RP;
-            float* red = reinterpret_cast<float*>(mask + ROWS * a.words);    // [WK - 1][ROWS][RP], then [WK - 1][ROWS] (maximum, sum)
-            float2* red_ml = reinterpret_cast<float2*>(red + (WK - 1) * ROWS * RP);
-            if (wk > 0) rows.leave(red + (wk - 1) * ROWS * RP, red_ml + (wk - 1) * ROWS, ra);
-            consumers();
-            if (wk == 0) {
-#pragma unroll
-                for (int g = 0; g < WK - 1; ++g) rows.join(red + g * ROWS * RP, red_ml + g * ROWS, ra);
+            float* red = reinterpret_cast<float*>(mask + ROWS * a.words);      // [ROWS][RP], then [ROWS] (maximum, sum): one group's at a time, so that two CTAs fit an SM
+            float2* red_ml = reinterpret_cast<float2*>(red + ROWS * RP);
+            for (int g = 1; g < WK; ++g) {
+                if (wk == g) rows.leave(red, red_ml, ra);
+                consumers();
+                if (wk == 0) rows.join(red, red_ml, ra);
+                if (g + 1 < WK) consumers();
             }
         }
         if (wk == 0) rows.store(a, it, r0, ra, ROWS);
@@ -145,8 +145,8 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
 
 template <typename T, int DP, int WM, int WK, int NS>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr int ROWS = 16 * WM, RING = NS * 2 * TA_BLOCK * DP * 2, RED = (WK - 1) * ROWS * ((DP + 8) * 4 + 8);
-    constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4 + TA_MAX_B * 4;
+    constexpr int ROWS = 16 * WM, RING = NS * 2 * TA_BLOCK * DP * 2, RED = (WK > 1) * ROWS * ((DP + 8) * 4 + 8);
+    constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4 + TA_MAX_B * 16;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tma<T, DP, WM, WK, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
     static const int per_sm = [] {
@@ -155,7 +155,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
         return n < 1 ? 1 : n;
     }();
     const int most = a.direct ? per_sm * TA_SMS : grid;   // whole sequences: as many CTAs as run at once
-    return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(grid < most ? grid : most), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B + 1) * 4, st, 1, tm, a);
+    return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(grid < most ? grid : most), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {

@@ -83,8 +83,8 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     char* qs = tc_smem + (1024 - (smem_u32(tc_smem) & 1023)) % 1024;
     char* kring = qs + TILES * Cfg::Q;
     char* vring = kring + NS * SIDE;
-    int* blocks_of = (int*)(vring + NS * SIDE);               // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(blocks_of + (a.direct ? 0 : a.B));
+    int4* seqs = (int4*)(vring + NS * SIDE);              // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t kfull = smem_u32(bars), kempty = kfull + NS * 8, vfull = kempty + NS * 8, vempty = vfull + NS * 8;
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     }
     op_begin();
     TaWork work;
-    work.begin(a, blocks_of);
+    work.begin(a, seqs);
     if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0) {                                      // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, TA_BLOCK), n_boxes = KT / box;
-        for (; ok && work.next(a, blocks_of, it); done += it.blocks) {
+        for (; ok && work.next(a, seqs, it); done += it.blocks) {
             const int* table = a.table + (long long)it.s.seq * a.max_pages;
             auto page_of = [&](int j) {                   // this lane's page of block j: out of range where there is none
                 const int key = it.k_begin + j * KT + lane * box, i = key >> a.page_shift;
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         }
     } else if (warp == 1) {                               // products
         int taken[2] = {0, 0};                            // steps of the groups in the parts before
-        for (; work.next(a, blocks_of, it); done += it.blocks, taken[0] += steps(it.blocks, 0), taken[1] += steps(it.blocks, 1)) {
+        for (; work.next(a, seqs, it); done += it.blocks, taken[0] += steps(it.blocks, 0), taken[1] += steps(it.blocks, 1)) {
             asm volatile("bar.sync 2, 288;" ::: "memory");            // the queries are there, the last outputs have been read
             tc_fence_after();
             const int n0 = steps(it.blocks, 0), n1 = steps(it.blocks, 1);
@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         const int g = (warp - 4) >> 2, t = tid - 128, all_rows = a.T * a.group;
         int taken = 0, outputs = 0;                       // this group's steps and outputs in the parts before
         auto softmax_warps = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-        while (work.next(a, blocks_of, it, t == 0)) {
+        while (work.next(a, seqs, it, t == 0)) {
         const SeqKeys& s = it.s;
         const int r0 = it.tile * ROWS;
         // the queries: thread t takes piece t % PIECES of every (256 / PIECES)-th row
@@ -414,11 +414,11 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
 
 template <typename T, int DP, int TILES>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr int BYTES = TcAttn<DP, TILES>::BYTES + 1024, MOST = BYTES + (TILES * TC_ROWS + 1) * 32 * 4 + TA_MAX_B * 4;
-    static_assert(MOST <= 232448 - (TILES == 1 ? 1536 : 512), "shared memory of an SM");
+    constexpr int BYTES = TcAttn<DP, TILES>::BYTES + 1024, MOST = BYTES + (TILES * TC_ROWS + 1) * (TILES == 2 && DP > 64 ? TA_WIDE_T / 32 : 32) * 4 + TA_MAX_B * 16;
+    static_assert(MOST <= 232448 - (TILES == 1 ? 2048 : 1024), "shared memory of an SM");
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tc<T, DP, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_tc<T, DP, TILES>, dim3(grid < TA_SMS || !a.direct ? grid : TA_SMS), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 4, st, 1, tm, a);
+    return op_launch(k_ta_tc<T, DP, TILES>, dim3(grid < TA_SMS || !a.direct ? grid : TA_SMS), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {
