@@ -437,3 +437,40 @@ def test_sample_refusals():
             bad()
     with pytest.raises(binding.SpecDecError, match="262144"):
         tree.sample(torch.zeros(1, 262145, device="cuda"), u[:1])
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("batch,prompt,tokens", [(1, 1, 20), (5, 12, 48)])
+def test_tree_decoding_is_sampling_token_by_token(batch, prompt, tokens):
+    """The example: the same text with trees as without, in fewer steps (fp32: a near-tie that rounding decides is rarer than the run is long)."""
+    from paper_2203_16487_b200 import tree_decode
+    steps, fewer, same = tree_decode.main(["--batch", str(batch), "--prompt", str(prompt), "--tokens", str(tokens)])
+    assert same == 1.0 and steps == tokens and fewer < steps
+
+
+def test_branches_of_a_prompt():
+    """Forked sequences continue a shared prompt each its own way, as sequences that hold copies of it would."""
+    from paper_2203_16487_b200 import tree
+    g = torch.Generator(device="cuda").manual_seed(5)
+    H, D, n, ways = 2, 64, 37, 3
+    cache = tree.PagedCache(1, H, D, n_pages=40, n_seqs=2 * ways + 1, max_pages=8, page_tokens=16, dtype=torch.float32)
+    k, v = (torch.randn(1, n, H, D, generator=g, device="cuda") for _ in "kv")
+    chain = torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    copies = ints(list(range(ways + 1, 2 * ways + 1)))
+    for seqs in [ints([0])] + [copies[i:i + 1] for i in range(ways)]:
+        cache.reserve(seqs, n)
+        cache.append(seqs, k, v, layer=0)
+        cache.compact(seqs, chain, ints([n]))
+    branches = ints(list(range(1, ways + 1)))
+    cache.fork(ints([0] * ways), branches)
+    assert cache.refs.max() == ways + 1
+    new = torch.randn(ways, 20, H, D, generator=g, device="cuda")
+    q = torch.randn(ways, 20, 4, D, generator=g, device="cuda")
+    mask, _ = tree.ancestors(torch.arange(-1, 19, dtype=torch.int32, device="cuda").expand(ways, -1).contiguous())
+    outs = []
+    for seqs in (branches, copies):
+        cache.reserve(seqs, 20)
+        cache.append(seqs, new, new, layer=0)
+        outs.append(tree.attention(q, cache, 0, seqs, mask))
+    cache.check()
+    assert torch.equal(outs[0], outs[1])
