@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
         __syncthreads();
         load(j + NS - 1);
         const uint32_t ks = smem_u32(ring + (j % NS) * STAGE), vs = ks + KT * PITCH;
-        rows.block(qf, k_begin + j * KT, s.len, a.scale, a.words, live_a ? mask_a : nullptr, live_b ? mask_b : nullptr,
+        rows.block(qf, k_begin + j * KT, s.len, a.scale, [&](int base) { return live_a ? ta_window(mask_a, a.words, base) : 0u; }, [&](int base) { return live_b ? ta_window(mask_b, a.words, base) : 0u; },
                    [&](int r, int c) { return ks + r * PITCH + ((c ^ (r & 7)) << 4); }, [&](int r, int c) { return vs + r * PITCH + ((c ^ (r & 7)) << 4); });
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");

@@ -138,6 +138,12 @@ __device__ __forceinline__ uint32_t ta_window(const uint32_t* row, int words, in
     const uint32_t a = w < words ? row[w] : 0u, b = w + 1 < words ? row[w + 1] : 0u;
     return __funnelshift_r(a, b, s);
 }
+// The same from one or two words.
+__device__ __forceinline__ uint32_t ta_window2(uint32_t m0, uint32_t m1, int base) {
+    if (base <= -32) return 0xffffffffu;
+    if (base < 0) return ((1u << -base) - 1u) | m0 << -base;
+    return base < 32 ? __funnelshift_r(m0, m1, base) : base < 64 ? m1 >> (base - 32) : 0u;
+}
 // The mask rows of a tile's queries (cut at the nodes), and any[w]: the nodes that one of them sees.  Query rows r0 .. r0 + rows - 1.
 // By the first NT threads of the CTA, which meet at barrier BAR.
 template <int NT, int BAR>
@@ -162,14 +168,14 @@ __device__ __forceinline__ bool ta_seen(const uint32_t* any, const SeqKeys& s, i
 }
 
 // Zeros for the values, in a block of 64 rows of HALVES x 128 bytes, that none of the tile's queries sees: whatever is in them is multiplied by 0.  Rows
-// [row0, row0 + ROWS) by one warp (32 of them share a word of what is seen).
-template <int ROWS, int HALVES>
-__device__ __forceinline__ void ta_zero_unseen(char* values, int row0, int k0, const SeqKeys& s, const uint32_t* any, int words) {
+// [row0, row0 + ROWS) by one warp; seen(row): 32 rows from there on as bits.
+template <int ROWS, int HALVES, typename F>
+__device__ __forceinline__ void ta_zero_unseen(char* values, int row0, F seen_from) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int r0 = 0; r0 < ROWS; r0 += 32) {
         constexpr int N = ROWS < 32 ? ROWS : 32;
-        const uint32_t seen = ta_window(any, words, k0 + row0 + r0 - s.len);
+        const uint32_t seen = seen_from(row0 + r0);
 #pragma unroll
         for (int r = 0; r < N; r += 4) {
             const int mine = r + (lane >> 3);
@@ -230,9 +236,9 @@ struct TaRows {
         for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
         ma = mb = -INFINITY; la = lb = 0.f;
     }
-    // mask_a, mask_b: the rows' words (null: a row that sees nothing), looked at where the block holds nodes or ends behind the last key
-    template <typename KF, typename VF>
-    __device__ __forceinline__ void block(const uint32_t (*qf)[4], int k0, int len, float scale, int words, const uint32_t* mask_a, const uint32_t* mask_b, KF kf, VF vf) {
+    // window_a, window_b(base): what the rows see of 32 keys, asked where the block holds nodes or ends behind the last key
+    template <typename WA, typename WB, typename KF, typename VF>
+    __device__ __forceinline__ void block(const uint32_t (*qf)[4], int k0, int len, float scale, WA window_a, WB window_b, KF kf, VF vf) {
         const int lane = threadIdx.x & 31;
         float sc[NK][4];
 #pragma unroll
@@ -250,7 +256,7 @@ struct TaRows {
 #pragma unroll
             for (int n = 0; n < TA_BLOCK / 32; ++n) {
                 const int base = k0 + n * 32 - len;
-                const uint32_t wa = mask_a ? ta_window(mask_a, words, base) : 0u, wb = mask_b ? ta_window(mask_b, words, base) : 0u;
+                const uint32_t wa = window_a(base), wb = window_b(base);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int bit = i * 8 + (lane & 3) * 2;

@@ -104,9 +104,30 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
                 qf[kk][3] = live_b && hi ? two(qb + kk * 32 + 16) : 0u;
             }
         }
-        ta_load_masks<32 * TM_WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
-        const uint32_t* mask_a = live_a ? mask + (ta - t0) * a.words : nullptr;
-        const uint32_t* mask_b = live_b ? mask + (tb - t0) * a.words : nullptr;
+        // What the rows see, and the nodes that anyone sees.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for
+        // another; more: in shared memory.
+        const bool own = a.words <= 2;
+        uint32_t ma[2] = {0, 0}, mb[2] = {0, 0}, seen[2] = {0, 0};
+        if (own) {
+            const uint32_t* words = a.mask + it.b * a.mask_sb;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int left = s.nodes - w * 32;
+                if (w >= a.words || left <= 0) break;
+                const uint32_t cut = left < 32 ? (1u << left) - 1u : 0xffffffffu;
+                uint32_t all = lane < s.nodes ? words[lane * a.words + w] : 0u;
+                if (lane + 32 < s.nodes) all |= words[(lane + 32) * a.words + w];
+                if (live_a) ma[w] = words[ta * a.words + w] & cut;
+                if (live_b) mb[w] = words[tb * a.words + w] & cut;
+                seen[w] = __reduce_or_sync(0xffffffffu, all) & cut;
+            }
+        } else {
+            ta_load_masks<32 * TM_WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
+        }
+        const uint32_t* mask_a = mask + (live_a ? ta - t0 : 0) * a.words;
+        const uint32_t* mask_b = mask + (live_b ? tb - t0 : 0) * a.words;
+        auto window_a = [&](int base) { return !live_a ? 0u : own ? ta_window2(ma[0], ma[1], base) : ta_window(mask_a, a.words, base); };
+        auto window_b = [&](int base) { return !live_b ? 0u : own ? ta_window2(mb[0], mb[1], base) : ta_window(mask_b, a.words, base); };
         TaRows<T, DP> rows;
         rows.clear();
         for (int j = wk; j < it.blocks; j += WK, ++count) {
@@ -115,11 +136,14 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
             const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
             const bool tail = k0 + KT > s.len;            // nodes, or what is behind the last key
             if (tail) {                                   // values that no query sees: whatever is in them is multiplied by 0
-                ta_zero_unseen<KT / WM, HALVES>(ring + st * STAGE + SIDE, wm * (KT / WM), k0, s, any, a.words);
+                ta_zero_unseen<KT / WM, HALVES>(ring + st * STAGE + SIDE, wm * (KT / WM), [&](int row) {
+                    const int base = k0 + row - s.len;
+                    return own ? ta_window2(seen[0], seen[1], base) : ta_window(any, a.words, base);
+                });
                 if constexpr (WM == 1) __syncwarp();
                 else asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "n"(32 * WM) : "memory");
             }
-            rows.block(qf, k0, s.len, a.scale, a.words, mask_a, mask_b,
+            rows.block(qf, k0, s.len, a.scale, window_a, window_b,
                        [&](int r, int c) { return ks + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); },
                        [&](int r, int c) { return vs + (c >> 3) * KT * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4); });
             if (tail) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the zeros, ahead of the stage's next boxes
@@ -139,7 +163,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
             }
         }
         if (wk == 0) rows.store(a, it, r0, ra, ROWS);
-        consumers();                                      // masks and partial results may be overwritten
+        if (WK > 1 || !own) consumers();                  // masks and partial results may be overwritten
     }
 }
 
