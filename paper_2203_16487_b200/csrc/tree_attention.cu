@@ -17,7 +17,7 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     extern __shared__ __align__(128) char sm[];
     char* ring = sm;                                      // [NS][K, V][KT][PITCH]; at first the queries
     int4* seqs = (int4*)(sm + NS * STAGE);
-    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
+    uint32_t* any = (uint32_t*)(seqs + (a.direct == 1 ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, wm = tid >> 5;
     op_begin();
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
     float* vt = kt + TF_KT * KP;
     float* pt = vt + TF_KT * KP;                          // [16][PP]
     int4* seqs = reinterpret_cast<int4*>(q + Cfg::FLOATS);
-    uint32_t* any = reinterpret_cast<uint32_t*>(seqs + (a.direct ? 0 : a.B));
+    uint32_t* any = reinterpret_cast<uint32_t*>(seqs + (a.direct == 1 ? 0 : a.B));
     uint32_t* mask = any + a.words;
     op_begin();
     TaWork work;
@@ -389,6 +389,7 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge, which costs about as much as eight
     // blocks.
     p.direct = (whole + at_once - 1) / at_once * blocks <= whole * blocks / at_once + 8 || B > TA_MAX_B;
+    if (p.direct && whole > at_once && 2 * columns <= at_once && B <= TA_MAX_B && p.rows >= 64 && blocks >= 4) p.direct = 2;    // (128 x 51 queries over 51 to 307 keys 29.5 -> 27.9 us; few rows or keys lose 2)
     p.ctas = (int)(at_once / columns < 1 ? 1 : at_once / columns);
     const long long most = (B * blocks + p.min_blocks - 1) / p.min_blocks;                // stretches at most
     if (p.ctas > most) p.ctas = (int)most;
@@ -407,14 +408,14 @@ cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_small_pages<T, DP, NS>, dim3(grid), 128, RING + 65 * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, a);
+    return op_launch(k_ta_small_pages<T, DP, NS>, dim3(ta_grid(a, grid, 2 * TA_SMS)), 128, RING + 65 * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
 template <int DP>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int BYTES = TfCfg<DP>::FLOATS * 4;
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_f32<DP>, dim3(!a.direct || grid < TA_SMS ? grid : TA_SMS), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, a);
+    return op_launch(k_ta_f32<DP>, dim3(ta_grid(a, grid, TA_SMS)), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {

@@ -14,7 +14,8 @@ namespace sd {
 // Rows of one K/V head: query row r = t * group + (head within the group), cut into tiles of a kernel's rows; (K/V head, tile) is a column of work.  The keys of a
 // sequence are its length committed tokens and n nodes behind them, in blocks of `unit` keys (64, or 128).
 //
-// direct: sequences are never cut; CTAs that stay take every gridDim.x-th (sequence, column).
+// direct: sequences are never cut; CTAs that stay take every gridDim.x-th (sequence, column).  direct = 2 (more items than CTAs): each column's sequences are dealt out by
+// falling length, to its CTAs there and back, so that long and short ones meet.
 // Otherwise a column's blocks of all sequences form one line, of which each of its `ctas` CTAs takes an equal stretch (TaWork), so that all CTAs run equally long
 // whatever the lengths are.  A stretch begins and ends inside sequences: a part that is a whole sequence writes the output, other parts write partial results
 // into slots that k_ta_merge joins.  The part of sequence b in the column's CTA c has slot (c + b) * columns + column: along the line either c or b grows.
@@ -57,9 +58,24 @@ struct TaWork {
     __device__ __forceinline__ void begin(const TreeAttn& a, int4* seqs) {
         const int columns = a.kv_heads * a.tiles;
         at = blockIdx.x;
-        if (a.direct) return;
+        if (a.direct == 1) return;
         __shared__ int found[4];
         column = blockIdx.x % columns; at = blockIdx.x / columns;
+        if (a.direct == 2) {
+            __shared__ int length_of[TA_MAX_B];
+            SeqKeys s;
+            for (int i = threadIdx.x; i < a.B; i += blockDim.x) { s = ta_keys(a, i); length_of[i] = s.keys; }
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.B; i += blockDim.x) {
+                if (a.B > blockDim.x) s = ta_keys(a, i);
+                int rank = 0;
+                for (int j = 0; j < a.B; ++j) rank += length_of[j] > s.keys || (length_of[j] == s.keys && j < i);
+                seqs[rank] = make_int4(s.seq, s.len, s.nodes, i);
+            }
+            skip = 0;                                     // rounds so far
+            __syncthreads();
+            return;
+        }
         for (int i = threadIdx.x; i < a.B; i += blockDim.x) {
             const SeqKeys s = ta_keys(a, i);
             seqs[i] = make_int4(s.seq, s.len, s.nodes, max(1, (s.keys + a.unit - 1) / a.unit));        // (at least 1: rows that see nothing are written too)
@@ -101,11 +117,20 @@ struct TaWork {
     // The next part.  notes: whether this thread tells the merge where a sequence's parts are.
     __device__ __forceinline__ bool next(const TreeAttn& a, const int4* seqs, Part& p, bool notes = false) {
         const int columns = a.kv_heads * a.tiles;
-        if (a.direct) {
+        if (a.direct == 1) {
             if (at >= a.B * columns) return false;
             p.b = at / columns; column = at - p.b * columns;
             at += gridDim.x;
             p.s = ta_keys(a, p.b);
+            p.k_begin = 0; p.k_end = p.s.keys; p.whole = 1; p.slot = 0;
+            p.blocks = (p.s.keys + a.unit - 1) / a.unit;
+        } else if (a.direct == 2) {
+            const int ctas = gridDim.x / columns, i = skip * ctas + (skip & 1 ? ctas - 1 - at : at);
+            ++skip;
+            if (i >= a.B) return false;                   // (a later round lies behind as well)
+            const int4 q = seqs[i];
+            p.b = q.w;
+            p.s.seq = q.x; p.s.len = q.y; p.s.nodes = q.z; p.s.keys = q.z ? q.y + q.z : 0;
             p.k_begin = 0; p.k_end = p.s.keys; p.whole = 1; p.slot = 0;
             p.blocks = (p.s.keys + a.unit - 1) / a.unit;
         } else {
@@ -374,6 +399,13 @@ struct TaRows {
         }
     }
 };
+
+// CTAs of a launch of `grid` items or stretches, where `most` run at once.
+inline int ta_grid(const TreeAttn& a, int grid, int most) {
+    if (!a.direct || grid <= most) return grid;
+    const int columns = a.kv_heads * a.tiles;
+    return a.direct == 2 ? most / columns * columns : most;
+}
 
 // A tensor map of one layer's keys and values: {head_dim, heads, tokens of a page, pages, 2 sides}; a box is 64 elements (128 bytes, swizzled) of min(page, TA_BLOCK)
 // tokens of one head.  What lies beyond head_dim or the pages arrives as zeros.

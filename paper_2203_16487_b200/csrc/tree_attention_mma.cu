@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
     __shared__ int abort_flag;
     char* ring = ta_smem + (1024 - (smem_u32(ta_smem) & 1023)) % 1024;
     int4* seqs = (int4*)(ring + NS * STAGE);              // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
+    uint32_t* any = (uint32_t*)(seqs + (a.direct == 1 ? 0 : a.B));
     uint32_t* mask = any + (a.words + 1) / 2 * 2;         // (8-byte aligned, as the partial results behind it are)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
@@ -178,8 +178,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_ta_tma<T, DP, WM, WK, NS>, 32 * (WM * WK + 1), MOST);
         return n < 1 ? 1 : n;
     }();
-    const int most = a.direct ? per_sm * TA_SMS : grid;   // whole sequences: as many CTAs as run at once
-    return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(grid < most ? grid : most), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, tm, a);
+    return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(ta_grid(a, grid, per_sm * TA_SMS)), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {

@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     char* kring = qs + TILES * Cfg::Q;
     char* vring = kring + NS * SIDE;
     int4* seqs = (int4*)(vring + NS * SIDE);              // [B] where sequences are cut
-    uint32_t* any = (uint32_t*)(seqs + (a.direct ? 0 : a.B));
+    uint32_t* any = (uint32_t*)(seqs + (a.direct == 1 ? 0 : a.B));
     uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t kfull = smem_u32(bars), kempty = kfull + NS * 8, vfull = kempty + NS * 8, vempty = vfull + NS * 8;
@@ -418,7 +418,7 @@ cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t
     static_assert(MOST <= 232448 - (TILES == 1 ? 2048 : 1024), "shared memory of an SM");
     static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tc<T, DP, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_tc<T, DP, TILES>, dim3(grid < TA_SMS || !a.direct ? grid : TA_SMS), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct ? 0 : a.B) * 16, st, 1, tm, a);
+    return op_launch(k_ta_tc<T, DP, TILES>, dim3(ta_grid(a, grid, TA_SMS)), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>
 cudaError_t pick(const CUtensorMap& tm, const TreeAttn& a, int rows, int grid, cudaStream_t st) {
