@@ -785,17 +785,18 @@ cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
     if (attr != cudaSuccess) return attr;
     return op_launch(k_sample<T, NT, C>, dim3(rows * C), NT, smem, st, C, a);
 }
-// CTAs of a row: as few as hold it, and more while all rows' run at once and have 8192 entries each (26 rows of 32768, top-p: 1, 2, 4, 8 CTAs 20.8, 20.4, 18.2, 22.6 us).  Two CTAs of 512 threads share an SM while two stretches fit its
-// shared memory; beyond, one CTA of 1024 has the SM to itself.
+// CTAs of a row: as few as hold it, and more while every CTA has an SM to itself and 8192 entries (26 rows of 32768, top-p: 1, 2, 4, 8 CTAs 20.8, 20.4, 18.2, 22.6 us; 128
+// rows: 1, 2, 4 CTAs 21.7, 24.9, 36.4).  1024 threads where a whole row has an SM to itself; else 512, two
+// CTAs to an SM (128 rows of 32768 bf16: 23.2 us with 512, 21.4 with 1024; 26 rows on 4 CTAs each 17.0 and 18.0).
 template <typename T>
 cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
     auto bytes = [&](int c) { return ((size_t)a.V * sizeof(T) / 16 + 2 + c) / c * 16 + 16; };
-    auto two = [&](int c) { return 2 * (bytes(c) + SA_STATIC + 1024) <= SA_SMEM; };
     int c = 1;
     while (bytes(c) > SA_SMEM - SA_STATIC) c *= 2;
-    while (c < 8 && (long long)rows * 2 * c <= 148 * (two(2 * c) ? 2 : 1) && a.V >= 2 * c * 8192) c *= 2;
+    while (c < 8 && (long long)rows * 2 * c <= 148 && a.V >= 2 * c * 8192) c *= 2;
     const size_t smem = bytes(c);
-    if (two(c)) return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
+    if ((c > 1 || rows > 148) && 2 * (smem + SA_STATIC + 1024) <= SA_SMEM)
+        return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
     return c == 1 ? run<T, 1024, 1>(a, rows, smem, st) : c == 2 ? run<T, 1024, 2>(a, rows, smem, st) : c == 4 ? run<T, 1024, 4>(a, rows, smem, st) : run<T, 1024, 8>(a, rows, smem, st);
 }
 
