@@ -8,12 +8,16 @@
 //   greedy  the first index of the maximum.
 //   few     top-k of at most SA_FEW.  The k-th largest of a CTA's threads' own maxima is a bound below the k-th largest entry, so only the entries above the best such
 //           bound are looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No exponential of the others is taken.
-//   order   other cuts: a histogram over 1024 equal steps of x gives the step in which the cut falls, and a list of that step's entries, ranked by counting,
-//           the cut itself.  (More entries in a step than the list holds: that step's range of logits, as ordered integers, is split into 1024 again until a bin is
-//           one value; entries equal to it have equal weights, so how many of them stay is arithmetic; which, is by index.)
+//   window  top-p alone: the numbers of entries in 3072 equal steps of x, without an exponential, give a window of a few steps that the cut must lie in; one pass over
+//           all weights then has their sum, what is ahead of the window, and a list of what is in it.
+//   order   larger top-k, and what a window's list does not hold: a histogram over 1024 equal steps of x gives the step in which the cut falls, and a list of that step's
+//           entries, ranked by counting, the cut itself.  (More entries in a step than the list holds: that step's range of logits, as ordered integers, is split into 1024
+//           again until a bin is one value; entries equal to it have equal weights, so how many of them stay is arithmetic; which, is by index.)
 //   then    the kept weights by stretches of the row, one a warp, and the goal's stretch entry by entry.
 //
-// Per entry the exponential and its two whole parts are some 20 instructions; the histogram adds one atomic (shared memory takes about ten lanes a clock).
+// What bounds it is the instruction rate: per entry the exponential and its two whole parts are some 20 instructions, the histogram adds one atomic (shared memory takes
+// about ten lanes a clock).  3328 rows of 32768 bf16 (218 MB, 33 us at the memory's rate), every row: greedy 42 us, top-k 40 95, no cut 130, top-p 254 (by the histogram
+// over 1024 steps, which takes every exponential twice, 287).  64 rows of 131072 with top-p: 37 us, by the histogram 45.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -26,7 +30,7 @@ namespace sd {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int SA_BINS = 1024, SA_FEW = 128, SA_LIST = 512;
+constexpr int SA_BINS = 1024, SA_FINE = 3072, SA_FEW = 128, SA_LIST = 512, SA_WIDE = 1024;
 constexpr float SA_RANGE = 27.75f;                        // e^-27.73 = 2^-40
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -92,7 +96,7 @@ struct Row {
         return ((u64)(hi - MAGIC) << 20) + (lo - MAGIC);
     }
     // step of x, to the nearest: 0 for the largest; SA_BINS and more: weight 0 (NaN, -inf and all that is too small)
-    static constexpr float STEPS = SA_BINS / SA_RANGE;
+    static constexpr float STEPS = SA_BINS / SA_RANGE, FINE_STEPS = SA_FINE / SA_RANGE;
     __device__ __forceinline__ static uint32_t bin_of(float x) { return __float_as_uint(fmaf(x, -STEPS, 8388608.f)) - MAGIC; }
 };
 
@@ -121,18 +125,20 @@ template <int NT> struct Shared {
     union {
         Hist h;
         struct { u64 units[SA_FEW], part[8][SA_FEW]; };   // few, once the histogram of maxima has been searched
+        uint32_t fine[SA_FINE + 32];                      // entries by finer steps (a lane each for what weighs nothing)
+        struct { u64 wide[SA_WIDE]; uint32_t part_lo[64], part_hi[64]; };  // a longer list and the weights of parts of it, once the finer steps have been searched
     };
     u64 any[SA_LIST], sorted[SA_LIST];                    // entries as key << 32 | ~index: the order's composite
     int rank[SA_LIST];
-    u64 w_sum[32];
+    u64 w_sum[32], w_ahead[32];
     int w_cnt[32];
     float w_max[32];
     // what the CTAs of a cluster tell one another (each written once between two barriers)
-    float x_top, x_bound;
-    int x_bin, x_n;
+    float x_top, x_bound, x_weight;
+    int x_bin, x_end, x_window, x_n;
     u64 x_cnt, x_sum, x_cnt_before, x_sum_before, x_total;
     // answers
-    int bin, n_list, index, winner;
+    int bin, bin_end, n_window, n_list, index, winner;
     u64 cnt_before, sum_before, total, cut, cut_sum;
 };
 
@@ -225,6 +231,105 @@ __device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u6
         }
         __syncthreads();
     }
+}
+
+// The finer steps [sh.bin, sh.bin_end) in which the cut by weight must lie, and how many entries they hold (sh.n_window), from the steps' entries (all CTAs').  An entry's weight is within d = 0.6 of a step of its
+// step's middle (0.5, and room for roundings), so of all weight A + B the share of the steps ahead lies between A (1 - d) / (A (1 - d) + B (1 + d)) and the same with d's sign turned: a cut at
+// 0.95 is known to 0.05 % of all weight before one exponential has been taken.
+// Each CTA weighs its share of the steps.  (Floats: an estimate, of which all CTAs see the same numbers; what is made of it is checked with exact sums.)
+template <int NT, int C>
+__device__ void find_window(Shared<NT>& sh, const Group<C>& cta, float top_p) {
+    constexpr int SHARE = SA_FINE / C, PER = (SHARE + NT - 1) / NT;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = cta.rank * SHARE + threadIdx.x * PER;
+    const bool mine = threadIdx.x * PER < SHARE;
+    uint32_t n[PER];
+    float w[PER], s = 0.f;
+    cta.sync();                                           // the counts are complete
+#pragma unroll
+    for (int j = 0; j < PER; ++j) n[j] = 0;
+    if (mine)
+#pragma unroll
+        for (int r = 0; r < C; ++r) {
+            const uint32_t* fine = cta.of(&sh, r)->fine + b0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) n[j] += fine[j];
+        }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) { w[j] = n[j] * __expf((b0 + j) * (-1.f / Row::FINE_STEPS)); s += w[j]; }
+    float is = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const float y = __shfl_up_sync(0xffffffffu, is, o); if (lane >= o) is += y; }
+    if (lane == 31) sh.w_max[warp] = is;
+    if (threadIdx.x == 0) { sh.bin = 0; sh.bin_end = SA_FINE; sh.n_window = 0; }
+    __syncthreads();
+    float all, before = warps_before<NT>(sh.w_max, all) + (is - s);
+    if (C > 1) {
+        if (threadIdx.x == 0) sh.x_weight = all;
+        cta.sync();
+        all = 0.f;
+        for (int r = 0; r < C; ++r) {
+            if (r == cta.rank) before += all;
+            all += cta.of(&sh, r)->x_weight;
+        }
+    }
+    constexpr float d = 0.6f / Row::FINE_STEPS;
+    const float p = fminf(top_p, 1.f), up = p * (1 + d), down = p * (1 - d), q = 1 - p;
+    const float least = down / (down + q * (1 + d)) * all, most = up / (up + q * (1 - d)) * all;
+    unsigned first = 0, end = SA_FINE, in = 0;
+    if (mine)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (before <= least) first = b0 + j;
+            if (before >= most) end = min(end, (unsigned)(b0 + j));
+            else if (before + w[j] > least) in += n[j];
+            before += w[j];
+        }
+    first = __reduce_max_sync(0xffffffffu, first);
+    end = __reduce_min_sync(0xffffffffu, end);
+    in = __reduce_add_sync(0xffffffffu, in);
+    if (lane == 0) {
+        if (in) atomicAdd(&sh.n_window, (int)in);
+        if (first) atomicMax(&sh.bin, (int)first);
+        if (end < SA_FINE) atomicMin(&sh.bin_end, (int)end);
+    }
+    __syncthreads();
+    if (C > 1) {
+        if (threadIdx.x == 0) { sh.x_bin = sh.bin; sh.x_end = sh.bin_end; sh.x_window = sh.n_window; }
+        cta.sync();
+        if (threadIdx.x == 0) {
+            sh.n_window = 0;
+            for (int r = 0; r < C; ++r) {
+                const Shared<NT>* o = cta.of(&sh, r);
+                sh.bin = max(sh.bin, o->x_bin); sh.bin_end = min(sh.bin_end, o->x_end); sh.n_window += o->x_window;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The bin, in ascending order, that holds entry number k (from 1), or -1; every warp looks for itself.
+__device__ int bin_of_kth(const uint32_t* cnt, int k) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int i = 0; i < SA_BINS / 128; ++i) {
+        const int4 c = reinterpret_cast<const int4*>(cnt)[i * 32 + lane];
+        const int s = c.x + c.y + c.z + c.w, all = __reduce_add_sync(0xffffffffu, s);
+        if (before + all >= k) {
+            int upto = s;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += y; }
+            int bin = -1, b = before + upto - s;
+            if (b < k && k <= b + s) {
+                bin = i * 128 + lane * 4;
+                if ((b += c.x) < k) ++bin;
+                if (b < k && (b += c.y) < k) ++bin;
+                if (b < k && (b += c.z) < k) ++bin;
+            }
+            return __reduce_max_sync(0xffffffffu, bin);
+        }
+        before += all;
+    }
+    return -1;
 }
 
 // Keys whose step is b: [lo, hi].  The step falls as the key grows, so both ends are found by a search of 32 probes at a time.
@@ -348,7 +453,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     const int k = k_in <= 0 || k_in > V ? V : k_in;
     const bool greedy = !(temperature > 0.f) || !(top_p > 0.f) || !(min_p <= 1.f) || k == 1;        // the largest entry alone
     const bool few = k <= SA_FEW && k < V, cuts = k < V || top_p < 1.f;
-    if (cuts) sh.h.template clear<NT>();
+    if (few) for (int i = tid; i < SA_BINS; i += NT) sh.h.cnt[i] = 0;
+    else if (k < V) sh.h.template clear<NT>();
+    else if (cuts) for (int i = tid; i < SA_FINE; i += NT) sh.fine[i] = 0;
     if (tid == 0) { sh.index = V; sh.n_list = 0; sh.winner = -1; }
     asm volatile("cp.async.wait_all;" ::: "memory");
 
@@ -409,9 +516,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     if (few) {
         const uint32_t b = Row::bin_of(row.x_of(mine));
         if (b < SA_BINS) atomicAdd(sh.h.cnt + b, 1u);
-        const Group<1> alone;
-        find_bin<NT, 1>(sh, alone, false, k, 0., 0, 0);
-        const int bin = sh.bin;
+        __syncthreads();
+        const int bin = bin_of_kth(sh.h.cnt, k);
         // entries from here on up: all of steps 0 .. bin (a little more does no harm)
         const float depth = (bin + 0.5f) * (SA_RANGE / SA_BINS) / inv_t;
         float bound = bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
@@ -526,8 +632,164 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                 }
             }
         };
-        fill(k < V);
         u64 total = 0;                                    // of the k largest, where k cuts
+        // All CTAs' lists (each CTA's is list(its shared memory)), behind this one's n entries; the length of the whole.
+        auto gather = [&](int n, int most, auto list) {
+            __syncthreads();                              // all have read n
+            if (C > 1) {
+                if (tid == 0) sh.x_n = n;
+                cta.sync();
+                int at = n;
+                for (int q = 0; q < C; ++q) if (q != cta.rank) {
+                    const Shared<NT>* o = cta.of(&sh, q);
+                    const int m = o->x_n;
+                    if (at + m <= most) for (int i = tid; i < m; i += NT) list(&sh)[at + i] = list(o)[i];
+                    at += m;
+                }
+                n = at;
+                __syncthreads();
+            }
+            if (tid == 0) sh.n_list = 0;
+            return n;
+        };
+        // The cut among the list's n entries, with c0 entries of weight s0 ahead of them.  sum: adds to s what stays of them.  Returns the list's weight.
+        auto cut_in_list = [&](int n, u64 c0, u64 s0, bool by_weight, double thr, bool sum) {
+            rank_list<NT>(sh, n);
+            u64 w = 0;
+            if (tid < n) w = Row::units(row.w_of(logit_of(sh.sorted[tid])));
+            const u64 upto = warp_scan(w);
+            if (lane == 31) sh.w_sum[warp] = upto;
+            __syncthreads();
+            u64 all;
+            const u64 before = s0 + warps_before<NT>(sh.w_sum, all) + upto - w;
+            // the last entry that stays: by weight the last whose weight ahead is below thr
+            const bool stays = tid < n && (by_weight ? (double)before < thr : c0 + tid + 1 <= (u64)k);
+            const bool next = tid + 1 < n && (by_weight ? (double)(before + w) < thr : c0 + tid + 2 <= (u64)k);
+            if (stays && !next) { sh.cut = sh.sorted[tid]; sh.cut_sum = before + w; }
+            __syncthreads();
+            if (sum)                                      // those of this warp's stretch
+                for (int e = lane; e < n; e += 32) {
+                    const u64 y = sh.sorted[e];
+                    const int i = (int)~(uint32_t)y;
+                    if (y >= sh.cut && i >= data.first + v0 * N && i < data.first + v1 * N) {
+                        const float w2 = row.w_of(logit_of(y));
+                        if (w2 >= min_p) s += Row::units(w2);
+                    }
+                }
+            return all;
+        };
+        // By weight alone, in two passes: entries by finer steps, without an exponential, give a window that the cut must lie in; then all weights once, with what is ahead of
+        // the window, and a list of what is in it.  Whether the cut was found this way (sh.cut, s): not where the window holds more than the list does.
+        auto by_window = [&]() {
+            const u64 step2 = pair2(-Row::FINE_STEPS * row.inv_t, -Row::FINE_STEPS * row.inv_t), top2 = pair2(-row.top, -row.top);
+            for (int v = v0 + lane; v < v1; v += 32) {
+                u64 l[N / 2];
+                data.pairs(v, l);
+#pragma unroll
+                for (int j = 0; j < N / 2; ++j) {
+                    const u64 b = fma2(add2(l[j], top2), step2, pair2(8388608.f, 8388608.f));
+                    atomicAdd(sh.fine + (min((uint32_t)b, MAGIC + SA_FINE + lane) - MAGIC), 1u);
+                    atomicAdd(sh.fine + (min((uint32_t)(b >> 32), MAGIC + SA_FINE + lane) - MAGIC), 1u);
+                }
+            }
+            find_window<NT, C>(sh, cta, top_p);
+            if (sh.n_window > SA_WIDE) return false;
+            const float unit = SA_RANGE / SA_FINE / row.inv_t;
+            const float high = sh.bin ? row.top - (sh.bin - 0.5f) * unit : INFINITY, low = row.top - (sh.bin_end - 0.5f) * unit;
+            uint32_t all_hi = 0, all_lo = 0, ahead_hi = 0, ahead_lo = 0, n_ahead = 0, drop_hi = 0, drop_lo = 0, n_drop = 0, n = 0;
+            for (int v = v0 + lane; v < v1; v += 32, n += N) {
+                u64 l[N / 2];
+                data.pairs(v, l);
+                bool near = false;
+#pragma unroll
+                for (int j = 0; j < N / 2; ++j) {
+                    const u64 x = row.x_of2(l[j]);
+                    const float w0 = fmaxf(expf(lo2(x)), 0.f), w1 = fmaxf(expf(hi2(x)), 0.f), l0 = lo2(l[j]), l1 = hi2(l[j]);
+                    u64 hi, lo;
+                    split_units2(pair2(w0, w1), hi, lo);
+                    all_hi += (uint32_t)hi + (uint32_t)(hi >> 32); all_lo += (uint32_t)lo + (uint32_t)(lo >> 32);
+                    if (l0 > high) {
+                        ahead_hi += (uint32_t)hi; ahead_lo += (uint32_t)lo; ++n_ahead;
+                        if (!(w0 >= min_p)) { drop_hi += (uint32_t)hi; drop_lo += (uint32_t)lo; ++n_drop; }
+                    }
+                    if (l1 > high) {
+                        ahead_hi += (uint32_t)(hi >> 32); ahead_lo += (uint32_t)(lo >> 32); ++n_ahead;
+                        if (!(w1 >= min_p)) { drop_hi += (uint32_t)(hi >> 32); drop_lo += (uint32_t)(lo >> 32); ++n_drop; }
+                    }
+                    near |= (l0 >= low && !(l0 > high)) || (l1 >= low && !(l1 > high));
+                }
+                if (near)
+                    data.vec(v, [&](float le, int i) {
+                        if (le >= low && !(le > high)) {
+                            const int at = atomicAdd(&sh.n_list, 1);
+                            if (at < SA_WIDE) sh.wide[at] = composite(le, i);
+                        }
+                    });
+            }
+            auto units = [](uint32_t hi, uint32_t lo, uint32_t m) { return ((u64)(hi - m * MAGIC) << 20) + (lo - m * MAGIC); };
+            const u64 mine_ahead = units(ahead_hi, ahead_lo, n_ahead);
+            const u64 wa = warp_sum(units(all_hi, all_lo, n)), wh = warp_sum(mine_ahead);
+            s = mine_ahead - units(drop_hi, drop_lo, n_drop);
+            if (lane == 0) { sh.w_sum[warp] = wa; sh.w_ahead[warp] = wh; }
+            __syncthreads();
+            u64 all, ahead;
+            warps_before<NT>(sh.w_sum, all);
+            warps_before<NT>(sh.w_ahead, ahead);
+            if (C > 1 && tid == 0) { sh.x_sum = all; sh.x_cnt = ahead; }
+            const int m = gather(sh.n_list, SA_WIDE, [](auto* o) { return o->wide; });
+            if (C > 1) {
+                all = ahead = 0;
+                for (int q = 0; q < C; ++q) { all += cta.of(&sh, q)->x_sum; ahead += cta.of(&sh, q)->x_cnt; }
+            }
+            const double thr = (double)top_p * (double)all;
+            if (m > SA_WIDE || !((double)ahead < thr)) return false;
+            if (m <= SA_LIST / 2) {                       // few enough to be ranked as they are
+                for (int e = tid; e < m; e += NT) sh.any[e] = sh.wide[e];
+                __syncthreads();
+                return (double)(ahead + cut_in_list(m, 0, ahead, true, thr, true)) >= thr;
+            }
+            // the part of the window that holds the cut: of 64 equal ones the last of any weight with weight ahead below thr
+            const float from = fminf(high, row.top), scale = 64.f / (from - low);
+            auto part_of = [&](u64 e) { return max(0, min((int)((from - logit_of(e)) * scale), 63)); };
+            if (tid < 64) sh.part_lo[tid] = sh.part_hi[tid] = 0;
+            __syncthreads();
+            for (int e = tid; e < m; e += NT) {
+                const u64 y = sh.wide[e];
+                const u64 w = Row::units(row.w_of(logit_of(y)));
+                const int b = part_of(y);
+                const uint32_t old = atomicAdd(sh.part_lo + b, (uint32_t)w), h = (uint32_t)(w >> 32) + (old + (uint32_t)w < old);
+                if (h) atomicAdd(sh.part_hi + b, h);
+            }
+            __syncthreads();
+            const u64 p0 = (u64)sh.part_hi[2 * lane] << 32 | sh.part_lo[2 * lane], p1 = (u64)sh.part_hi[2 * lane + 1] << 32 | sh.part_lo[2 * lane + 1];
+            const u64 upto = warp_scan(p0 + p1), before = ahead + upto - p0 - p1;
+            if (!((double)(ahead + __shfl_sync(0xffffffffu, upto, 31)) >= thr)) return false;
+            const bool in0 = p0 && (double)before < thr, in1 = p1 && (double)(before + p0) < thr;
+            const int part = __reduce_max_sync(0xffffffffu, in1 ? 2 * lane + 1 : in0 ? 2 * lane : 0);
+            const u64 s0 = __shfl_sync(0xffffffffu, part & 1 ? before + p0 : before, part >> 1);
+            for (int e = tid; e < m; e += NT) {
+                const u64 y = sh.wide[e];
+                if (part_of(y) == part) {
+                    const int at = atomicAdd(&sh.n_list, 1);
+                    if (at < SA_LIST) sh.any[at] = y;
+                }
+            }
+            __syncthreads();
+            const int of_part = sh.n_list;
+            __syncthreads();                              // all have read it
+            if (tid == 0) sh.n_list = 0;
+            if (of_part > SA_LIST) return false;
+            cut_in_list(of_part, 0, s0, true, thr, false);
+            for (int e = lane; e < m; e += 32) {          // what stays of the window, that of this warp's stretch
+                const u64 y = sh.wide[e];
+                const int i = (int)~(uint32_t)y;
+                if (y >= sh.cut && i >= data.first + v0 * N && i < data.first + v1 * N) {
+                    const float w = row.w_of(logit_of(y));
+                    if (w >= min_p) s += Row::units(w);
+                }
+            }
+            return true;
+        };
         // The cut in sh.bin: sh.cut = composite of the last entry that stays, sh.cut_sum = weight of all that stay.  sum: whether to add up the kept weights ahead of the step.
         bool filled = true;                               // whether sh.h is the histogram over steps
         auto locate = [&](bool by_weight, double thr, bool sum) {
@@ -570,45 +832,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                 }
             s = ((u64)(sum_hi - added * MAGIC) << 20) + (sum_lo - added * MAGIC);
             __syncthreads();
-            int n = usable ? sh.n_list : SA_LIST + 1;
-            __syncthreads();                              // all have read it
-            if (C > 1) {                                  // every CTA takes all lists, behind its own
-                if (tid == 0) sh.x_n = n;
-                cta.sync();
-                int at = n;
-                for (int q = 0; q < C; ++q) if (q != cta.rank) {
-                    const Shared<NT>* o = cta.of(&sh, q);
-                    const int m = o->x_n;
-                    if (at + m <= SA_LIST) for (int i = tid; i < m; i += NT) sh.any[at + i] = o->any[i];
-                    at += m;
-                }
-                n = at;
-                __syncthreads();
-            }
-            if (tid == 0) sh.n_list = 0;
+            const int n = gather(usable ? sh.n_list : SA_LIST + 1, SA_LIST, [](auto* o) { return o->any; });
             if (n <= SA_LIST) {
-                rank_list<NT>(sh, n);
-                u64 w = 0;
-                if (tid < n) w = Row::units(row.w_of(logit_of(sh.sorted[tid])));
-                const u64 upto = warp_scan(w);
-                if (lane == 31) sh.w_sum[warp] = upto;
-                __syncthreads();
-                u64 unused;
-                const u64 before = s0 + warps_before<NT>(sh.w_sum, unused) + upto - w;
-                // the last entry that stays: by weight the last whose weight ahead is below thr
-                const bool stays = tid < n && (by_weight ? (double)before < thr : c0 + tid + 1 <= (u64)k);
-                const bool next = tid + 1 < n && (by_weight ? (double)(before + w) < thr : c0 + tid + 2 <= (u64)k);
-                if (stays && !next) { sh.cut = sh.sorted[tid]; sh.cut_sum = before + w; }
-                __syncthreads();
-                if (sum)                                  // the step's own entries, those of this warp's stretch
-                    for (int e = lane; e < n; e += 32) {
-                        const u64 y = sh.sorted[e];
-                        const int i = (int)~(uint32_t)y;
-                        if (y >= sh.cut && i >= data.first + v0 * N && i < data.first + v1 * N) {
-                            const float w2 = row.w_of(logit_of(y));
-                            if (w2 >= min_p) s += Row::units(w2);
-                        }
-                    }
+                cut_in_list(n, c0, s0, by_weight, thr, sum);
                 return sum;
             }
             // more than the list holds
@@ -679,26 +905,36 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             cta.sync();
             return false;
         };
-        bool summed = false;
-        if (k < V) {
-            find_bin<NT, C>(sh, cta, false, k, 0., 0, 0);
-            if (sh.bin >= 0) {
-                summed = locate(false, 0., !(top_p < 1.f));
-                cut = sh.cut; total = sh.cut_sum;
-            }
-        }
-        if (top_p < 1.f) {
-            if (!filled) {                                // the search for the k-th entry took the histogram
+        bool summed = k == V && by_window();
+        if (summed) {
+            cut = sh.cut;
+        } else {
+            if (k == V) {
                 cta.sync();
                 sh.h.template clear<NT>();
                 __syncthreads();
-                fill(false);
             }
-            double thr = (double)top_p * (double)total;
-            find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0, total ? 0.f : top_p);
-            if (!total) thr = (double)top_p * (double)sh.total;
-            summed = locate(true, thr, true);
-            cut = sh.cut;
+            fill(k < V);
+            if (k < V) {
+                find_bin<NT, C>(sh, cta, false, k, 0., 0, 0);
+                if (sh.bin >= 0) {
+                    summed = locate(false, 0., !(top_p < 1.f));
+                    cut = sh.cut; total = sh.cut_sum;
+                }
+            }
+            if (top_p < 1.f) {
+                if (!filled) {                            // the search for the k-th entry took the histogram
+                    cta.sync();
+                    sh.h.template clear<NT>();
+                    __syncthreads();
+                    fill(false);
+                }
+                double thr = (double)top_p * (double)total;
+                find_bin<NT, C>(sh, cta, true, 0, thr, 0, 0, total ? 0.f : top_p);
+                if (!total) thr = (double)top_p * (double)sh.total;
+                summed = locate(true, thr, true);
+                cut = sh.cut;
+            }
         }
         if (!summed) {
             s = 0;
@@ -797,7 +1033,9 @@ cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
     const size_t smem = bytes(c);
     if ((c > 1 || rows > 148) && 2 * (smem + SA_STATIC + 1024) <= SA_SMEM)
         return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
-    return c == 1 ? run<T, 1024, 1>(a, rows, smem, st) : c == 2 ? run<T, 1024, 2>(a, rows, smem, st) : c == 4 ? run<T, 1024, 4>(a, rows, smem, st) : run<T, 1024, 8>(a, rows, smem, st);
+    if constexpr (sizeof(T) == 4)                         // (an eighth of the longest 16-bit row leaves room for two CTAs)
+        if (c == 8) return run<T, 1024, 8>(a, rows, smem, st);
+    return c == 1 ? run<T, 1024, 1>(a, rows, smem, st) : c == 2 ? run<T, 1024, 2>(a, rows, smem, st) : run<T, 1024, 4>(a, rows, smem, st);
 }
 
 }  // namespace
