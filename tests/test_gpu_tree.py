@@ -250,6 +250,13 @@ def test_attention_uneven_long_sequences(dtype, T, H, Hkv, D):
     check_attention(got, want, mag, dtype, 5100)
 
 
+@pytest.mark.parametrize("T,H,Hkv,D,lens", [(1024, 1, 1, 128, [70]), (970, 2, 1, 128, [0]), (1024, 1, 1, 64, [5, 1]), (300, 3, 1, 128, [129, 0]), (40, 12, 12, 64, [(i * 53) % 400 for i in range(41)])])
+def test_attention_wide_trees(T, H, Hkv, D, lens):
+    """The most nodes a tree may have (whose masks are 32 words a row), and whole sequences of 64 rows dealt to CTAs by length."""
+    got, want, mag, _ = attention_case(torch.bfloat16, lens, T, H, Hkv, D, 32, seed=T, one_mask=len(lens) > 5)
+    check_attention(got, want, mag, torch.bfloat16, T + max(lens))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("kw", [dict(nodes=[9, 0, 3]), dict(one_mask=True), dict(strided=True), dict(heads_first=True), dict(layer=2), dict(nodes=[1, 9, 8], strided=True, heads_first=True)])
 def test_attention_ragged_shared_strided(dtype, kw):
@@ -415,6 +422,30 @@ def test_sample_parameters_and_strides():
     d = tree.sample(logits, u, t.repeat_interleave(3))
     assert torch.equal(c[0].view(-1), d[0]) and torch.equal(c[1].view(-1), d[1])
     assert tree.sample(logits[:0], u[:0])[0].shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [900, 32768, 50265, 131072, 262144])
+def test_sample_is_the_same_by_every_route(V, dtype):
+    """Weights are whole numbers, so nothing may depend on how a row is cut: alone (a cluster a row) and among many, and with a top-k that drops one entry of weight 0
+    (which is found by other means than top-p alone).  Flat rows, whose cut lies among thousands of nearly equal entries, and steep ones."""
+    from paper_2203_16487_b200 import tree
+    rows = 160 if V < 100000 else 12
+    g = torch.Generator(device="cuda").manual_seed(V)
+    scale = torch.tensor([0.0, 1e-3, 0.05, 0.5, 2.0, 6.0], device="cuda").repeat(rows)[:rows, None]
+    l = (torch.randn(rows, V, generator=g, device="cuda") * scale).to(dtype)
+    l[:, V - 1] = -math.inf
+    u = torch.rand(rows, generator=g, device="cuda")
+    t = 0.3 + torch.rand(rows, generator=g, device="cuda")
+    p = 0.02 + 0.979 * torch.rand(rows, generator=g, device="cuda")
+    m = torch.where(torch.rand(rows, generator=g, device="cuda") < 0.5, 0, 0.3 * torch.rand(rows, generator=g, device="cuda"))
+    token, logp = tree.sample(l, u, t, None, p, m)
+    k = torch.full((rows,), V - 1, dtype=torch.int32, device="cuda")
+    again = tree.sample(l, u, t, k, p, m)
+    assert torch.equal(token, again[0]) and torch.equal(logp, again[1])
+    for r in range(0, rows, 7):
+        one = tree.sample(l[r:r + 1], u[r:r + 1], t[r:r + 1], None, p[r:r + 1], m[r:r + 1])
+        assert torch.equal(token[r:r + 1], one[0]) and torch.equal(logp[r:r + 1], one[1]), r
 
 
 def test_sample_frequencies():
