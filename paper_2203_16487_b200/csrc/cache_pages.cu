@@ -4,7 +4,9 @@
 // are given out first, so that no call's result depends on the order in which CTAs run: reference counts are sums of integers, and everything
 // else is written by one CTA.  A call that cannot get all its pages changes nothing.
 //
-// The data are moved as 16-byte pieces, every piece read once and written once; what bounds the moves is HBM.
+// The data are moved as 16-byte pieces, every piece read once and written once; what bounds large moves is HBM, a decoding step's the five launches behind one another.
+// 8 prompts forked into 4 branches each, 32 layers of pages of 128 tokens (81 MB read, the other three times from L2, 326 MB written): 74 us, 65 of them the copy.  32 sentences
+// of 26 new tokens, 6 layers of 8 heads of 64 in bf16: fork, reserve, append (20 MB) and compact 26 us together.
 #include <cuda_runtime.h>
 #include <stdint.h>
 

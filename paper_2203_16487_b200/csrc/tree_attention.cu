@@ -105,22 +105,23 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
 // fetched under this block's second product, its values under the next scores.  A call of few rows is bounded by the chain of one warp, one of many
 // by the fused multiply-adds and the shared-memory reads that feed them (6 of 16 bytes for 32).  (8 warps with blocks of 32 keys, two to a scheduler:
 // 20.5 us for 8 x 9 queries over 300 to 512 keys.)
-constexpr int TF_ROWS = 16, TF_KT = 16;
-template <int DP> struct TfCfg {
+constexpr int TF_KT = 16;
+template <int DP, int RI> struct TfCfg {
+    static constexpr int ROWS = 4 * RI;
     static constexpr int WK = DP > 64 ? 8 : 16, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
-    static constexpr int WARP = 2 * TF_KT * KP + TF_ROWS * PP;                         // a warp's keys, values and probabilities
-    static constexpr int FLOATS = TF_ROWS * KP + WK * WARP;
+    static constexpr int WARP = 2 * TF_KT * KP + ROWS * PP;                         // a warp's keys, values and probabilities
+    static constexpr int FLOATS = ROWS * KP + WK * WARP;
 };
-template <int DP>
-__global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
-    using Cfg = TfCfg<DP>;
-    constexpr int WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32, KE = TF_KT / 8;
+template <int DP, int RI>
+__global__ void __launch_bounds__(32 * TfCfg<DP, RI>::WK) k_ta_f32(TreeAttn a) {
+    using Cfg = TfCfg<DP, RI>;
+    constexpr int ROWS = Cfg::ROWS, WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32, KE = TF_KT / 8;
     extern __shared__ __align__(128) char sm[];
-    float* q = reinterpret_cast<float*>(sm);              // [16][KP]
+    float* q = reinterpret_cast<float*>(sm);              // [ROWS][KP]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rg = lane >> 3, x = lane & 7;
-    float* kt = q + TF_ROWS * KP + warp * Cfg::WARP;      // [32][KP]
+    float* kt = q + ROWS * KP + warp * Cfg::WARP;      // [16][KP]
     float* vt = kt + TF_KT * KP;
-    float* pt = vt + TF_KT * KP;                          // [16][PP]
+    float* pt = vt + TF_KT * KP;                          // [ROWS][PP]
     int4* seqs = reinterpret_cast<int4*>(q + Cfg::FLOATS);
     uint32_t* any = reinterpret_cast<uint32_t*>(seqs + (a.direct == 1 ? 0 : a.B));
     uint32_t* mask = any + a.words;
@@ -131,7 +132,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
     Part it;
     while (work.next(a, seqs, it, tid == 0)) {
         __syncthreads();
-        const int r0 = it.tile * TF_ROWS, all_rows = a.T * a.group, t0 = ta_node(a, r0);
+        const int r0 = it.tile * ROWS, all_rows = a.T * a.group, t0 = ta_node(a, r0);
         const SeqKeys& s = it.s;
         const int blocks = (it.k_end - it.k_begin + TF_KT - 1) / TF_KT;
         auto page_of = [&](int j) -> int {                // of this lane's key in block j
@@ -144,7 +145,8 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
         };
         int page = page_of(warp);
 #pragma unroll
-        for (int i0 = 0; i0 < TF_ROWS * (DP / 4); i0 += NT) {
+        for (int i0 = 0; i0 < ROWS * (DP / 4); i0 += NT) {
+            if (ROWS * (DP / 4) % NT && i0 + tid >= ROWS * (DP / 4)) break;
             const int i = i0 + tid, r = i / (DP / 4), d = i % (DP / 4) * 4, gr = r0 + r, node = ta_node(a, gr);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (gr < all_rows && node < s.nodes && d < a.dim) {
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
         }
         if (a.dim < DP)                                   // columns beyond the head
             for (int i = lane; i < 2 * TF_KT * (DP - a.dim); i += 32) kt[i / (DP - a.dim) * KP + a.dim + i % (DP - a.dim)] = 0.f;
-        ta_load_masks<NT, 0>(a, it.b, r0, min(TF_ROWS, all_rows - r0), s.nodes, mask, any);
+        ta_load_masks<NT, 0>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
         auto fetch = [&](float* to, const char* base, long long off) {
 #pragma unroll
             for (int r0 = 0; r0 < TF_KT; r0 += 4) {       // four keys at a time, eight lanes each
@@ -167,13 +169,13 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        bool live[4];
-        const uint32_t* row[4];
-        float m[4], l[4];
-        float4 o[4][DC];
+        bool live[RI];
+        const uint32_t* row[RI];
+        float m[RI], l[RI];
+        float4 o[RI][DC];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int gr = r0 + rg * 4 + i, node = ta_node(a, gr);
+        for (int i = 0; i < RI; ++i) {
+            const int gr = r0 + rg * RI + i, node = ta_node(a, gr);
             live[i] = gr < all_rows && node < s.nodes;
             row[i] = mask + (live[i] ? (node - t0) * a.words : 0);
             m[i] = -INFINITY; l[i] = 0.f;
@@ -187,20 +189,20 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
             page = page_of(j + WK);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
-            float sc[4][KE];                              // [row][key x + 8 e]
+            float sc[RI][KE];                              // [row][key x + 8 e]
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < RI; ++i)
 #pragma unroll
                 for (int e = 0; e < KE; ++e) sc[i][e] = 0.f;
 #pragma unroll 4
             for (int d = 0; d < DP; d += 4) {
-                float4 qv[4], kv[KE];
+                float4 qv[RI], kv[KE];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(q + (rg * 4 + i) * KP + d);
+                for (int i = 0; i < RI; ++i) qv[i] = *reinterpret_cast<const float4*>(q + (rg * RI + i) * KP + d);
 #pragma unroll
                 for (int e = 0; e < KE; ++e) kv[e] = *reinterpret_cast<const float4*>(kt + (x + 8 * e) * KP + d);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RI; ++i)
 #pragma unroll
                     for (int e = 0; e < KE; ++e)
                         sc[i][e] = fmaf(qv[i].x, kv[e].x, fmaf(qv[i].y, kv[e].y, fmaf(qv[i].z, kv[e].z, fmaf(qv[i].w, kv[e].w, sc[i][e]))));
@@ -210,7 +212,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
             fetch(kt, a.k, off);
             const int base = it.k_begin + j * TF_KT - s.len;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < RI; ++i) {
                 const uint32_t w = live[i] ? ta_window(row[i], a.words, base) : 0u;
                 float top = -INFINITY;
 #pragma unroll
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
                 for (int e = 0; e < KE; ++e) {
                     const float p = ta_exp2(sc[i][e] - z);
                     l[i] += p;
-                    pt[(rg * 4 + i) * PP + x + 8 * e] = p;
+                    pt[(rg * RI + i) * PP + x + 8 * e] = p;
                 }
 #pragma unroll
                 for (int c = 0; c < DC; ++c) { o[i][c].x *= f; o[i][c].y *= f; o[i][c].z *= f; o[i][c].w *= f; }
@@ -236,16 +238,16 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
             __syncwarp();
 #pragma unroll 2
             for (int key = 0; key < TF_KT; key += 4) {
-                float4 p[4];
+                float4 p[RI];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = *reinterpret_cast<const float4*>(pt + (rg * 4 + i) * PP + key);
+                for (int i = 0; i < RI; ++i) p[i] = *reinterpret_cast<const float4*>(pt + (rg * RI + i) * PP + key);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int c = 0; c < DC; ++c) {
                         const float4 v = *reinterpret_cast<const float4*>(vt + (key + e) * KP + x * 4 + 32 * c);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < RI; ++i) {
                             const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
                             o[i][c].x = fmaf(w, v.x, o[i][c].x); o[i][c].y = fmaf(w, v.y, o[i][c].y); o[i][c].z = fmaf(w, v.z, o[i][c].z); o[i][c].w = fmaf(w, v.w, o[i][c].w);
                         }
@@ -257,16 +259,16 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
         // the warps' results meet: output in the keys' place, (maximum, sum) in the probabilities'
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < RI; ++i) {
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1); l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2); l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
             const bool none = l[i] == 0.f;                // sees nothing here: values times 0
 #pragma unroll
-            for (int c = 0; c < DC; ++c) *reinterpret_cast<float4*>(kt + (rg * 4 + i) * KP + x * 4 + 32 * c) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : o[i][c];
-            if (x == 0) { pt[rg * 4 + i] = none ? -INFINITY : m[i]; pt[16 + rg * 4 + i] = l[i]; }
+            for (int c = 0; c < DC; ++c) *reinterpret_cast<float4*>(kt + (rg * RI + i) * KP + x * 4 + 32 * c) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : o[i][c];
+            if (x == 0) { pt[rg * RI + i] = none ? -INFINITY : m[i]; pt[ROWS + rg * RI + i] = l[i]; }
         }
         __syncthreads();
-        const float* w0 = q + TF_ROWS * KP;               // warp w's keys: + w * WARP; its probabilities: + 2 * TF_KT * KP
-        for (int i = tid; i < TF_ROWS * (DP / 4); i += NT) {
+        const float* w0 = q + ROWS * KP;               // warp w's keys: + w * WARP; its probabilities: + 2 * TF_KT * KP
+        for (int i = tid; i < ROWS * (DP / 4); i += NT) {
             const int r = i / (DP / 4), c = i % (DP / 4), gr = r0 + r;
             float top = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -278,7 +280,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
                 const float* p = w0 + w * Cfg::WARP;
                 const float f = exp2f(p[2 * TF_KT * KP + r] - z);
                 const float4 v = *reinterpret_cast<const float4*>(p + r * KP + c * 4);
-                sum += p[2 * TF_KT * KP + 16 + r] * f;
+                sum += p[2 * TF_KT * KP + ROWS + r] * f;
                 y.x = fmaf(v.x, f, y.x); y.y = fmaf(v.y, f, y.y); y.z = fmaf(v.z, f, y.z); y.w = fmaf(v.w, f, y.w);
             }
             if (gr >= all_rows || c * 4 >= a.dim) continue;
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(32 * TfCfg<DP>::WK) k_ta_f32(TreeAttn a) {
                 if (a.out_vec) *reinterpret_cast<float4*>(p) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
                 else { p[0] = y.x * inv; p[1] = y.y * inv; p[2] = y.z * inv; p[3] = y.w * inv; }
             } else {
-                const long long slot = it.slot * TF_ROWS + r;
+                const long long slot = it.slot * ROWS + r;
                 *reinterpret_cast<float4*>(a.part + slot * a.dim + c * 4) = y;
                 if (c == 0) a.part_ml[slot] = make_float2(top, sum);
             }
@@ -380,7 +382,7 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
     const int most_mma = head_dim > 64 ? 32 : 64;
-    p.rows = dtype == SPECDEC_DTYPE_F32 ? TF_ROWS : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma ? 64 : all <= 128 || (head_dim > 64 && T > TA_WIDE_T) ? 128 : 256;
+    p.rows = dtype == SPECDEC_DTYPE_F32 ? ((all + (all + 15) / 16 - 1) / ((all + 15) / 16) + 3) / 4 * 4 : page_tokens < TA_MIN_PAGE ? 64 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma ? 64 : all <= 128 || (head_dim > 64 && T > TA_WIDE_T) ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
     p.min_blocks = 4;
@@ -410,12 +412,17 @@ cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     if (attr != cudaSuccess) return attr;
     return op_launch(k_ta_small_pages<T, DP, NS>, dim3(ta_grid(a, grid, 2 * TA_SMS)), 128, RING + 65 * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
-template <int DP>
+template <int DP, int RI>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
-    constexpr int BYTES = TfCfg<DP>::FLOATS * 4;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (TF_ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
+    using Cfg = TfCfg<DP, RI>;
+    constexpr int BYTES = Cfg::FLOATS * 4;
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP, RI>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (Cfg::ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_f32<DP>, dim3(ta_grid(a, grid, TA_SMS)), 32 * TfCfg<DP>::WK, BYTES + (TF_ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
+    return op_launch(k_ta_f32<DP, RI>, dim3(ta_grid(a, grid, TA_SMS)), 32 * Cfg::WK, BYTES + (Cfg::ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
+}
+template <int DP>
+cudaError_t pick_f32(const TreeAttn& a, int rows, int grid, cudaStream_t st) {
+    return rows == 4 ? run_f32<DP, 1>(a, grid, st) : rows == 8 ? run_f32<DP, 2>(a, grid, st) : rows == 12 ? run_f32<DP, 3>(a, grid, st) : run_f32<DP, 4>(a, grid, st);
 }
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
@@ -503,7 +510,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     const bool wide = a.dim > 64, bf = c->dtype == SPECDEC_DTYPE_BF16;
     cudaError_t rc;
     CUtensorMap tm;
-    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? run_f32<128>(a, (int)p.grid, s) : run_f32<64>(a, (int)p.grid, s);
+    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? pick_f32<128>(a, p.rows, (int)p.grid, s) : pick_f32<64>(a, p.rows, (int)p.grid, s);
     else if (c->page_tokens < TA_MIN_PAGE) {
         if (bf) rc = wide ? run_small_pages<__nv_bfloat16, 128>(a, (int)p.grid, s) : run_small_pages<__nv_bfloat16, 64>(a, (int)p.grid, s);
         else rc = wide ? run_small_pages<__half, 128>(a, (int)p.grid, s) : run_small_pages<__half, 64>(a, (int)p.grid, s);

@@ -14,7 +14,7 @@ constexpr int TO_MAX = 1024;
 
 // One CTA a tree.  Rows of bits in shared memory: node i begins with itself and a pointer to its parent; every round takes over the row that the pointer leads to
 // and then that node's pointer, so a chain of d nodes takes log2 d rounds.  (Rows are updated in place: one that is read while it grows holds more ancestors, never
-// anything else.)  128 trees of 256 nodes: 4.6 us; with a warp a node that walks to the root 18.
+// anything else.)  128 trees of 256 nodes: 6.0 us, a launch by itself some 4; with a warp a node that walks to the root 18.
 __global__ void k_tree_ancestors(const int* parents, const int* n_nodes, int T, uint32_t* mask, int* depth) {
     extern __shared__ uint32_t ta_rows[];                 // [T][pitch], then two sets of pointers [T]
     const int b = blockIdx.x, W = (T + 31) / 32, pitch = W | 1;
@@ -55,7 +55,7 @@ __global__ void k_tree_ancestors(const int* parents, const int* n_nodes, int T, 
 }
 
 // Thread i: whether node i is the first child of its parent that carries the parent's sampled token; next[parent] = that child.  The chain from the root is
-// then walked by one thread.
+// then walked by one thread, a read of shared memory a step.  128 trees of 256 nodes: 4.2 us.
 __global__ void k_tree_accept(const int* parents, const int* tokens, const int* sampled,
                               const int* n_nodes, int T, int* path, int* n_path, int* emitted) {
     __shared__ int next[TO_MAX], walk[TO_MAX], smp[TO_MAX];
