@@ -100,21 +100,21 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
 }
 
 // ------------------------------------------------------------------ fp32: FFMA
-// CTA = WK warps over the same 16 rows, each with every WK-th block of 16 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
-// another warp until the results meet).  Lane (rg, x): four rows, for the scores the keys x and x + 8, for the output the columns 4 x + 32 c.  The next block's keys are
+// CTA = WK warps over the same 4 RI rows, each with every WK-th block of 16 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
+// another warp until the results meet).  Lane (rg, x): RI rows, for the scores the keys x and x + 8, for the output the columns 4 x + 32 c.  The next block's keys are
 // fetched under this block's second product, its values under the next scores.  A call of few rows is bounded by the chain of one warp, one of many
 // by the fused multiply-adds and the shared-memory reads that feed them (6 of 16 bytes for 32).  (8 warps with blocks of 32 keys, two to a scheduler:
 // 20.5 us for 8 x 9 queries over 300 to 512 keys.)
 constexpr int TF_KT = 16;
-template <int DP, int RI> struct TfCfg {
+template <int DP, int RI, int PER_SM> struct TfCfg {
     static constexpr int ROWS = 4 * RI;
-    static constexpr int WK = DP > 64 ? 8 : 16, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
+    static constexpr int WK = (DP > 64 ? 8 : 16) / PER_SM, KP = DP + 4, PP = TF_KT + 4;            // pitches in floats
     static constexpr int WARP = 2 * TF_KT * KP + ROWS * PP;                         // a warp's keys, values and probabilities
     static constexpr int FLOATS = ROWS * KP + WK * WARP;
 };
-template <int DP, int RI>
-__global__ void __launch_bounds__(32 * TfCfg<DP, RI>::WK) k_ta_f32(TreeAttn a) {
-    using Cfg = TfCfg<DP, RI>;
+template <int DP, int RI, int PER_SM>
+__global__ void __launch_bounds__(32 * TfCfg<DP, RI, PER_SM>::WK, PER_SM) k_ta_f32(TreeAttn a) {
+    using Cfg = TfCfg<DP, RI, PER_SM>;
     constexpr int ROWS = Cfg::ROWS, WK = Cfg::WK, KP = Cfg::KP, PP = Cfg::PP, NT = 32 * WK, DC = DP / 32, KE = TF_KT / 8;
     extern __shared__ __align__(128) char sm[];
     float* q = reinterpret_cast<float*>(sm);              // [ROWS][KP]
@@ -374,10 +374,13 @@ __global__ void __launch_bounds__(128, 8) k_ta_merge(TreeAttn a, int rows) {
 }
 
 // ------------------------------------------------------------------ host
-struct Plan { int rows, tiles, direct, ctas, unit, min_blocks; long long grid, slots; };       // see TreeAttn; slots of partial results
+struct Plan { int rows, tiles, per_sm, direct, ctas, unit, min_blocks; long long grid, slots; };       // see TreeAttn; slots of partial results
 // Rows of a tile.  16-bit types: 16, 32 or 64 with mma.sync by the rows there are (64 share a block's keys among four warps; fewer rows give the warps keys of their own
 // instead), 128 or 256 with tcgen05 beyond 64 rows, of heads wider than 64 beyond 32.  (64 rows, 2 x 8 heads of 128 over 8000 keys: 31 us with tcgen05, 33 without; over 2000 keys of 64
 // sequences 43 and 48; heads of 64: 24.5 and 23, 32 and 27.  128 rows: 69 and 120, 136 and 243; heads of 64 50 and 67, 93 and 138.)
+// fp32: as few tiles of up to 16 as there must be, of equal size in fours (8 x 1 query over 8000 keys: 57 us with 4 rows, 90 with 16; 8 x 9 over 300 to 512: 15.9 with 12, 18.3).
+// CTAs that an SM holds (at least): of fp32 the more, each of fewer warps, the more work there is that they take in turn: 4 or 2 of 4 rows (64 x 1 over 0 to 512 keys 22 and 25 us, 8 x
+// 1 over 8000 52 and 54, 1 x 1 over 64 5.0 and 4.4), 2 or 1 of 12 and 16 (32 x 17 over 0 to 512 keys 40 and 49; 8 x 9 over 300 to 512 16.8 and 15.9).
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, int page_tokens, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
@@ -386,8 +389,10 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
     p.min_blocks = 4;
-    const int at_once = TA_SMS * (p.rows >= 128 || dtype == SPECDEC_DTYPE_F32 ? 1 : head_dim > 64 ? 2 : 3);     // CTAs that an SM holds at least
     const long long columns = (long long)n_kv_heads * p.tiles, whole = B * columns, blocks = (max_keys + p.unit - 1) / p.unit;
+    p.per_sm = dtype != SPECDEC_DTYPE_F32 ? (p.rows >= 128 ? 1 : head_dim > 64 ? 2 : 3)
+               : p.rows == 4 ? (whole * blocks >= 4 * TA_SMS ? 4 : 2) : p.rows == 8 || whole > TA_SMS ? 2 : 1;
+    const int at_once = TA_SMS * p.per_sm;
     // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge, which costs about as much as eight
     // blocks.
     p.direct = (whole + at_once - 1) / at_once * blocks <= whole * blocks / at_once + 8 || B > TA_MAX_B;
@@ -412,17 +417,21 @@ cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     if (attr != cudaSuccess) return attr;
     return op_launch(k_ta_small_pages<T, DP, NS>, dim3(ta_grid(a, grid, 2 * TA_SMS)), 128, RING + 65 * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
-template <int DP, int RI>
+template <int DP, int RI, int PER_SM>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
-    using Cfg = TfCfg<DP, RI>;
+    using Cfg = TfCfg<DP, RI, PER_SM>;
     constexpr int BYTES = Cfg::FLOATS * 4;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP, RI>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (Cfg::ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
+    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP, RI, PER_SM>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (Cfg::ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
     if (attr != cudaSuccess) return attr;
-    return op_launch(k_ta_f32<DP, RI>, dim3(ta_grid(a, grid, TA_SMS)), 32 * Cfg::WK, BYTES + (Cfg::ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
+    return op_launch(k_ta_f32<DP, RI, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 32 * Cfg::WK, BYTES + (Cfg::ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
 template <int DP>
-cudaError_t pick_f32(const TreeAttn& a, int rows, int grid, cudaStream_t st) {
-    return rows == 4 ? run_f32<DP, 1>(a, grid, st) : rows == 8 ? run_f32<DP, 2>(a, grid, st) : rows == 12 ? run_f32<DP, 3>(a, grid, st) : run_f32<DP, 4>(a, grid, st);
+cudaError_t pick_f32(const TreeAttn& a, const Plan& p, cudaStream_t st) {
+    const int grid = (int)p.grid;
+    if (p.rows == 4) return p.per_sm == 4 ? run_f32<DP, 1, 4>(a, grid, st) : run_f32<DP, 1, 2>(a, grid, st);
+    if (p.rows == 8) return run_f32<DP, 2, 2>(a, grid, st);
+    if (p.rows == 12) return p.per_sm == 2 ? run_f32<DP, 3, 2>(a, grid, st) : run_f32<DP, 3, 1>(a, grid, st);
+    return p.per_sm == 2 ? run_f32<DP, 4, 2>(a, grid, st) : run_f32<DP, 4, 1>(a, grid, st);
 }
 template <typename T>
 cudaError_t run_merge(const TreeAttn& a, int rows, cudaStream_t st) {
@@ -510,7 +519,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     const bool wide = a.dim > 64, bf = c->dtype == SPECDEC_DTYPE_BF16;
     cudaError_t rc;
     CUtensorMap tm;
-    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? pick_f32<128>(a, p.rows, (int)p.grid, s) : pick_f32<64>(a, p.rows, (int)p.grid, s);
+    if (c->dtype == SPECDEC_DTYPE_F32) rc = wide ? pick_f32<128>(a, p, s) : pick_f32<64>(a, p, s);
     else if (c->page_tokens < TA_MIN_PAGE) {
         if (bf) rc = wide ? run_small_pages<__nv_bfloat16, 128>(a, (int)p.grid, s) : run_small_pages<__nv_bfloat16, 64>(a, (int)p.grid, s);
         else rc = wide ? run_small_pages<__half, 128>(a, (int)p.grid, s) : run_small_pages<__half, 64>(a, (int)p.grid, s);
