@@ -102,9 +102,10 @@ __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
 // ------------------------------------------------------------------ fp32: FFMA
 // CTA = WK warps over the same 4 RI rows, each with every WK-th block of 16 keys to itself (rings, scores and running sums are a warp's own, so nothing waits for
 // another warp until the results meet).  Lane (rg, x): RI rows, for the scores the keys x and x + 8, for the output the columns 4 x + 32 c.  The next block's keys are
-// fetched under this block's second product, its values under the next scores.  A call of few rows is bounded by the chain of one warp, one of many
-// by the fused multiply-adds and the shared-memory reads that feed them (6 of 16 bytes for 32).  (8 warps with blocks of 32 keys, two to a scheduler:
-// 20.5 us for 8 x 9 queries over 300 to 512 keys.)
+// fetched under this block's second product, its values under the next scores.  One row is bounded by HBM (2 x 1 query, 32/8 heads of 128, over 30000 keys 5.3 TB/s), a call of
+// few CTAs by the chain of one warp, one of many rows by the shared memory's reads, 24 wavefronts for 32 fused multiply-adds (8 x 26 queries over 2000 keys 49 us, 16.7 TFLOP/s;
+// two columns an instruction, with every probability twice in shared memory, 46.5, but 2 to 5 % slower where there are fewer rows).  (8 warps with blocks of 32 keys, two to a
+// scheduler: no faster for 8 x 9 queries over 300 to 512 keys.)
 constexpr int TF_KT = 16;
 template <int DP, int RI, int PER_SM> struct TfCfg {
     static constexpr int ROWS = 4 * RI;
