@@ -29,11 +29,11 @@ def _fail(rc):
     raise SpecDecError(rc, lib().specdec_last_error(None).decode())
 
 
-def _ints(name, t, shape):
-    """Address of a contiguous int32 device tensor of that shape."""
-    if t.dtype is _I32 and t.shape == shape and t.is_cuda and t.is_contiguous():
+def _ints(name, t, shape, device):
+    """Address of a contiguous int32 tensor of that shape on that device (a number; -1 is none)."""
+    if t.dtype is _I32 and t.shape == shape and t.get_device() == device >= 0 and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: a contiguous int32 device tensor of shape {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    raise ValueError(f"{name}: a contiguous int32 device tensor of shape {tuple(shape)} is wanted, on the device of the others, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class PagedCache:
@@ -59,7 +59,8 @@ class PagedCache:
             raise ValueError("kv: a device tensor [n_layers, 2, n_pages, page_tokens, n_heads, head_dim] with a contiguous last dimension is wanted")
         L, _, P, page, H, D = kv.shape
         n_seqs = length.numel()
-        _ints("table", table, (n_seqs, table.shape[1])), _ints("length", length, (n_seqs,)), _ints("held", held, (n_seqs,)), _ints("refs", refs, (P,))
+        at = kv.get_device()
+        _ints("table", table, (n_seqs, table.shape[1]), at), _ints("length", length, (n_seqs,), at), _ints("held", held, (n_seqs,), at), _ints("refs", refs, (P,), at)
         self.kv, self.table, self.length, self.held, self.refs = kv, table, length, held, refs
         self.status = torch.zeros(1, dtype=torch.int32, device=kv.device)
         n = lib().specdec_cache_scratch(n_seqs, table.shape[1], P)
@@ -77,7 +78,7 @@ class PagedCache:
     def reserve(self, seqs, n_tokens: int):
         """Pages for n_tokens tokens behind the committed ones."""
         n = seqs.numel()
-        rc = self._lib.specdec_cache_reserve(self._ref, _ints("seqs", seqs, (n,)), n, n_tokens, _raw_stream(self._device))
+        rc = self._lib.specdec_cache_reserve(self._ref, _ints("seqs", seqs, (n,), self._device), n, n_tokens, _raw_stream(self._device))
         if rc:
             _fail(rc)
 
@@ -91,18 +92,18 @@ class PagedCache:
         else:
             layers, shape, s = 1, (1,) + tuple(shape), (0,) + tuple(s)
             good = len(shape) == 5
-        if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.is_cuda and v.is_cuda
+        if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
                 and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
             raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")
-        rc = self._lib.specdec_cache_append(self._ref, _ints("seqs", seqs, (n,)), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2], s[0], s[1], s[2], s[3],
-                                            None if count is None else _ints("count", count, (n,)), _raw_stream(self._device))
+        rc = self._lib.specdec_cache_append(self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2], s[0], s[1], s[2], s[3],
+                                            None if count is None else _ints("count", count, (n,), self._device), _raw_stream(self._device))
         if rc:
             _fail(rc)
 
     def compact(self, seqs, path, n_path):
         """Commits the nodes path[i, :n_path[i]] of each sequence's block and gives back the pages behind them."""
         n, T = seqs.numel(), path.shape[-1]
-        rc = self._lib.specdec_cache_compact(self._ref, _ints("seqs", seqs, (n,)), n, _ints("path", path, (n, T)), T, _ints("n_path", n_path, (n,)),
+        rc = self._lib.specdec_cache_compact(self._ref, _ints("seqs", seqs, (n,), self._device), n, _ints("path", path, (n, T), self._device), T, _ints("n_path", n_path, (n,), self._device),
                                              _raw_stream(self._device))
         if rc:
             _fail(rc)
@@ -110,14 +111,14 @@ class PagedCache:
     def release(self, seqs):
         """Gives back all pages of the sequences; their lengths are 0."""
         n = seqs.numel()
-        rc = self._lib.specdec_cache_release(self._ref, _ints("seqs", seqs, (n,)), n, _raw_stream(self._device))
+        rc = self._lib.specdec_cache_release(self._ref, _ints("seqs", seqs, (n,), self._device), n, _raw_stream(self._device))
         if rc:
             _fail(rc)
 
     def fork(self, src, dst):
         """Sequence dst[i] becomes a copy of what src[i] was before the call: full pages shared, the last, partly filled one copied."""
         n = src.numel()
-        rc = self._lib.specdec_cache_fork(self._ref, _ints("src", src, (n,)), _ints("dst", dst, (n,)), n, _raw_stream(self._device))
+        rc = self._lib.specdec_cache_fork(self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n, _raw_stream(self._device))
         if rc:
             _fail(rc)
 
@@ -134,10 +135,11 @@ class PagedCache:
 def ancestors(parents, n_nodes=None):
     """(mask [B, T, ceil(T / 32)] int32 of ancestor bits, depth [B, T] int32) of trees given by their parents [B, T]."""
     B, T = parents.shape
-    p = _ints("parents", parents, (B, T))
+    at = parents.get_device()
+    p = _ints("parents", parents, (B, T), at)
     mask, depth = parents.new_empty((B, T, (T + 31) // 32)), torch.empty_like(parents)
-    rc = lib().specdec_tree_ancestors(p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)), B, T, mask.data_ptr(), depth.data_ptr(),
-                                      _raw_stream(parents.get_device()))
+    rc = lib().specdec_tree_ancestors(p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at), B, T, mask.data_ptr(), depth.data_ptr(),
+                                      _raw_stream(at))
     if rc:
         _fail(rc)
     return mask, depth
@@ -147,10 +149,11 @@ def accept(parents, tokens, sampled, n_nodes=None):
     """(path [B, T], n_path [B], emitted [B, T]): the nodes from the root along the sampled tokens, and the sampled token of each (-1 behind)."""
     shape = parents.shape
     B, T = shape
-    p = _ints("parents", parents, shape)
+    at = parents.get_device()
+    p = _ints("parents", parents, shape, at)
     path, emitted, n_path = torch.empty_like(parents), torch.empty_like(parents), parents.new_empty((B,))
-    rc = lib().specdec_tree_accept(p, _ints("tokens", tokens, shape), _ints("sampled", sampled, shape), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)),
-                                   B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _raw_stream(parents.get_device()))
+    rc = lib().specdec_tree_accept(p, _ints("tokens", tokens, shape, at), _ints("sampled", sampled, shape, at), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at),
+                                   B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _raw_stream(at))
     if rc:
         _fail(rc)
     return path, n_path, emitted
@@ -160,16 +163,16 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     """Attention of tree nodes q [B, T, n_q_heads, head_dim] over the committed tokens of sequences seqs [B] and, by mask [B or 1, T, ceil(T / 32)], over
     the block's nodes (appended before).  max_length: an upper bound of the committed lengths, if known.  scale: 1 / sqrt(head_dim)."""
     B, T, H, D = q.shape
-    sq = q.stride()
-    if q.dtype is not cache.dtype or D != cache.head_dim or sq[3] != 1 or not q.is_cuda:
+    sq, at = q.stride(), cache._device
+    if q.dtype is not cache.dtype or D != cache.head_dim or sq[3] != 1 or q.get_device() != at:
         raise ValueError(f"q: a device tensor [B, T, heads, {cache.head_dim}] of {cache.dtype} with a contiguous last dimension is wanted")
     if out is None:
         out = q.new_empty((B, T, H, D))
-    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(3) != 1 or not out.is_cuda:
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(3) != 1 or out.get_device() != at:
         raise ValueError("out: of q's shape and type, with a contiguous last dimension")
     W, so = (T + 31) // 32, out.stride()
     one = mask.shape[0] == 1
-    m = _ints("mask", mask, (1 if one else B, T, W))
+    m = _ints("mask", mask, (1 if one else B, T, W), at)
     bound = cache.max_length
     if 0 < max_length < bound:
         bound = max_length
@@ -183,10 +186,10 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
             cache._workspaces.clear()
         cache._workspaces[B, T, H, bound] = n
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, (B,)), m,
-                          0 if one else T * W, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,)), bound, D ** -0.5 if scale is None else scale,
+    a = TreeAttentionArgs(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, (B,), at), m,
+                          0 if one else T * W, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at), bound, D ** -0.5 if scale is None else scale,
                           ws.data_ptr() if n else None, n)
-    rc = L.specdec_tree_attention(cache._ref, C.byref(a), _raw_stream(cache._device))
+    rc = L.specdec_tree_attention(cache._ref, C.byref(a), _raw_stream(at))
     if rc:
         _fail(rc)
     return out
@@ -197,10 +200,10 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     probability fp32 [...]).  The parameters (fp32, top_k int32; None: off) are tensors of one entry for each row, or for each equal run of rows ([n] for logits [n, T, V])."""
     shape = logits.shape
     V, lead = shape[-1], shape[:-1]
-    code = DTYPES.get(logits.dtype)
+    code, at = DTYPES.get(logits.dtype), logits.get_device()
     if code is None or not logits.is_cuda or logits.stride(-1) != 1:
         raise ValueError("logits: a device tensor of fp32, bf16 or fp16 with a contiguous last dimension is wanted")
-    if uniform.shape != lead or uniform.dtype is not torch.float32 or not uniform.is_cuda or not uniform.is_contiguous():
+    if uniform.shape != lead or uniform.dtype is not torch.float32 or uniform.get_device() != at or not uniform.is_contiguous():
         raise ValueError("uniform: a contiguous fp32 device tensor, one number a row, is wanted")
     rows, stride = uniform.numel(), V
     if not logits.is_contiguous():
@@ -210,7 +213,7 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     for i, t in enumerate((temperature, top_k, top_p, min_p)):
         if t is not None:
             m = t.numel()
-            if t.dtype is not (_I32 if i == 1 else torch.float32) or not t.is_cuda or not t.is_contiguous() or m < 1 or rows % m or (n and n != m):
+            if t.dtype is not (_I32 if i == 1 else torch.float32) or t.get_device() != at or not t.is_contiguous() or m < 1 or rows % m or (n and n != m):
                 raise ValueError(("temperature", "top_k", "top_p", "min_p")[i] + ": a contiguous fp32 (top_k: int32) device tensor is wanted, one entry for each "
                                  "equal run of rows, as many as the other parameters")
             n = m
@@ -218,7 +221,7 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     logprob = torch.empty_like(uniform)
     token = torch.empty_like(uniform, dtype=_I32)
     rc = lib().specdec_sample(logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(),
-                              _raw_stream(logits.get_device()))
+                              _raw_stream(at))
     if rc:
         _fail(rc)
     return token, logprob
