@@ -137,7 +137,7 @@ def ancestors(parents, n_nodes=None):
     B, T = parents.shape
     at = parents.get_device()
     p = _ints("parents", parents, (B, T), at)
-    mask, depth = parents.new_empty((B, T, (T + 31) // 32)), torch.empty_like(parents)
+    mask, depth = parents.new_empty(B, T, (T + 31) // 32), torch.empty_like(parents)
     rc = lib().specdec_tree_ancestors(p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at), B, T, mask.data_ptr(), depth.data_ptr(),
                                       _raw_stream(at))
     if rc:
@@ -151,7 +151,7 @@ def accept(parents, tokens, sampled, n_nodes=None):
     B, T = shape
     at = parents.get_device()
     p = _ints("parents", parents, shape, at)
-    path, emitted, n_path = torch.empty_like(parents), torch.empty_like(parents), parents.new_empty((B,))
+    path, emitted, n_path = torch.empty_like(parents), torch.empty_like(parents), parents.new_empty(B)
     rc = lib().specdec_tree_accept(p, _ints("tokens", tokens, shape, at), _ints("sampled", sampled, shape, at), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at),
                                    B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _raw_stream(at))
     if rc:
@@ -167,7 +167,7 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     if q.dtype is not cache.dtype or D != cache.head_dim or sq[3] != 1 or q.get_device() != at:
         raise ValueError(f"q: a device tensor [B, T, heads, {cache.head_dim}] of {cache.dtype} with a contiguous last dimension is wanted")
     if out is None:
-        out = q.new_empty((B, T, H, D))
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(B, T, H, D)
     elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(3) != 1 or out.get_device() != at:
         raise ValueError("out: of q's shape and type, with a contiguous last dimension")
     W, so = (T + 31) // 32, out.stride()
