@@ -527,15 +527,33 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             for (int q = 0; q < C; ++q) bound = fmaxf(bound, cta.of(&sh, q)->x_bound);
         }
         Shared<NT>* lead_sh = cta.of(&sh, 0);
-        if (bound > -INFINITY && mine >= bound)
-            for (int v = v0 + lane; v < v1; v += 32)
-                if (data.most(v) >= bound)
-                    data.vec(v, [&](float l, int i) {
-                        if (l >= bound) {
-                            const int at = atomicAdd(&lead_sh->n_list, 1);
-                            if (at < SA_LIST) lead_sh->any[at] = composite(l, i);
-                        }
-                    });
+        // the threads that have seen one, four at a time: eight lanes take a vector each of one thread's
+        const unsigned seen = __ballot_sync(0xffffffffu, bound > -INFINITY && mine >= bound);
+        int nth = 0;                                      // the lane-th of them
+#pragma unroll
+        for (int s = 16; s; s >>= 1) if (__popc(seen & ((1u << (nth + s)) - 1)) <= lane) nth += s;
+        for (int first = 0; first < __popc(seen); first += 4) {
+            const int of = __shfl_sync(0xffffffffu, nth, first + (lane >> 3));
+            const bool some = first + (lane >> 3) < __popc(seen);
+            for (int v = v0 + of + 32 * (lane & 7), more = v1 - v0; more > 0; v += 256, more -= 256) {
+                unsigned in = 0;
+                if (some && v < v1) {
+                    int bit = 0;
+                    data.vec(v, [&](float l, int) { in |= (l >= bound ? 1u : 0u) << bit++; });
+                }
+                const int n = __popc(in);
+                int upto = n;
+#pragma unroll
+                for (int s = 1; s < 32; s <<= 1) { const int y = __shfl_up_sync(0xffffffffu, upto, s); if (lane >= s) upto += y; }
+                int at = 0;
+                if (lane == 31 && upto) at = atomicAdd(&lead_sh->n_list, upto);
+                at = __shfl_sync(0xffffffffu, at, 31) + upto - n;
+                for (; in; in &= in - 1, ++at) {
+                    const int i = data.first + v * N + __ffs(in) - 1;
+                    if (at < SA_LIST) lead_sh->any[at] = composite(data.at(i), i);
+                }
+            }
+        }
         cta.sync();
         const int n = lead_sh->n_list;
         cta.sync();                                       // all have read it
