@@ -718,7 +718,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             for (int v = v0 + lane; v < v1; v += 32, n += N) {
                 u64 l[N / 2];
                 data.pairs(v, l);
-                bool near = false;
+                unsigned in = 0;                          // those of the window
 #pragma unroll
                 for (int j = 0; j < N / 2; ++j) {
                     const u64 x = row.x_of2(l[j]);
@@ -734,15 +734,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
                         ahead_hi += (uint32_t)(hi >> 32); ahead_lo += (uint32_t)(lo >> 32); ++n_ahead;
                         if (!(w1 >= min_p)) { drop_hi += (uint32_t)(hi >> 32); drop_lo += (uint32_t)(lo >> 32); ++n_drop; }
                     }
-                    near |= (l0 >= low && !(l0 > high)) || (l1 >= low && !(l1 > high));
+                    if (l0 >= low && !(l0 > high)) in |= 1u << 2 * j;
+                    if (l1 >= low && !(l1 > high)) in |= 2u << 2 * j;
                 }
-                if (near)
-                    data.vec(v, [&](float le, int i) {
-                        if (le >= low && !(le > high)) {
-                            const int at = atomicAdd(&sh.n_list, 1);
-                            if (at < SA_WIDE) sh.wide[at] = composite(le, i);
-                        }
-                    });
+                for (; in; in &= in - 1) {
+                    const int i = data.first + v * N + __ffs(in) - 1, at = atomicAdd(&sh.n_list, 1);
+                    if (at < SA_WIDE) sh.wide[at] = composite(data.at(i), i);
+                }
             }
             auto units = [](uint32_t hi, uint32_t lo, uint32_t m) { return ((u64)(hi - m * MAGIC) << 20) + (lo - m * MAGIC); };
             const u64 mine_ahead = units(ahead_hi, ahead_lo, n_ahead);
