@@ -23,6 +23,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "barriers.cuh"
 #include "op_error.cuh"
 
@@ -715,33 +717,37 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             const float unit = SA_RANGE / SA_FINE / row.inv_t;
             const float high = sh.bin ? row.top - (sh.bin - 0.5f) * unit : INFINITY, low = row.top - (sh.bin_end - 0.5f) * unit;
             uint32_t all_hi = 0, all_lo = 0, ahead_hi = 0, ahead_lo = 0, n_ahead = 0, drop_hi = 0, drop_lo = 0, n_drop = 0, n = 0;
-            for (int v = v0 + lane; v < v1; v += 32, n += N) {
-                u64 l[N / 2];
-                data.pairs(v, l);
-                unsigned in = 0;                          // those of the window
+            auto weigh = [&](auto drops) {                // drops: whether min_p drops any
+                for (int v = v0 + lane; v < v1; v += 32, n += N) {
+                    u64 l[N / 2];
+                    data.pairs(v, l);
+                    unsigned in = 0;                          // those of the window
 #pragma unroll
-                for (int j = 0; j < N / 2; ++j) {
-                    const u64 x = row.x_of2(l[j]);
-                    const float w0 = fmaxf(expf(lo2(x)), 0.f), w1 = fmaxf(expf(hi2(x)), 0.f), l0 = lo2(l[j]), l1 = hi2(l[j]);
-                    u64 hi, lo;
-                    split_units2(pair2(w0, w1), hi, lo);
-                    all_hi += (uint32_t)hi + (uint32_t)(hi >> 32); all_lo += (uint32_t)lo + (uint32_t)(lo >> 32);
-                    if (l0 > high) {
-                        ahead_hi += (uint32_t)hi; ahead_lo += (uint32_t)lo; ++n_ahead;
-                        if (!(w0 >= min_p)) { drop_hi += (uint32_t)hi; drop_lo += (uint32_t)lo; ++n_drop; }
+                    for (int j = 0; j < N / 2; ++j) {
+                        const u64 x = row.x_of2(l[j]);
+                        const float w0 = fmaxf(expf(lo2(x)), 0.f), w1 = fmaxf(expf(hi2(x)), 0.f), l0 = lo2(l[j]), l1 = hi2(l[j]);
+                        u64 hi, lo;
+                        split_units2(pair2(w0, w1), hi, lo);
+                        all_hi += (uint32_t)hi + (uint32_t)(hi >> 32); all_lo += (uint32_t)lo + (uint32_t)(lo >> 32);
+                        if (l0 > high) {
+                            ahead_hi += (uint32_t)hi; ahead_lo += (uint32_t)lo; ++n_ahead;
+                            if (drops.value && !(w0 >= min_p)) { drop_hi += (uint32_t)hi; drop_lo += (uint32_t)lo; ++n_drop; }
+                        }
+                        if (l1 > high) {
+                            ahead_hi += (uint32_t)(hi >> 32); ahead_lo += (uint32_t)(lo >> 32); ++n_ahead;
+                            if (drops.value && !(w1 >= min_p)) { drop_hi += (uint32_t)(hi >> 32); drop_lo += (uint32_t)(lo >> 32); ++n_drop; }
+                        }
+                        if (l0 >= low && !(l0 > high)) in |= 1u << 2 * j;
+                        if (l1 >= low && !(l1 > high)) in |= 2u << 2 * j;
                     }
-                    if (l1 > high) {
-                        ahead_hi += (uint32_t)(hi >> 32); ahead_lo += (uint32_t)(lo >> 32); ++n_ahead;
-                        if (!(w1 >= min_p)) { drop_hi += (uint32_t)(hi >> 32); drop_lo += (uint32_t)(lo >> 32); ++n_drop; }
+                    for (; in; in &= in - 1) {
+                        const int i = data.first + v * N + __ffs(in) - 1, at = atomicAdd(&sh.n_list, 1);
+                        if (at < SA_WIDE) sh.wide[at] = composite(data.at(i), i);
                     }
-                    if (l0 >= low && !(l0 > high)) in |= 1u << 2 * j;
-                    if (l1 >= low && !(l1 > high)) in |= 2u << 2 * j;
                 }
-                for (; in; in &= in - 1) {
-                    const int i = data.first + v * N + __ffs(in) - 1, at = atomicAdd(&sh.n_list, 1);
-                    if (at < SA_WIDE) sh.wide[at] = composite(data.at(i), i);
-                }
-            }
+            };
+            if (min_p > 0.f) weigh(std::true_type());
+            else weigh(std::false_type());
             auto units = [](uint32_t hi, uint32_t lo, uint32_t m) { return ((u64)(hi - m * MAGIC) << 20) + (lo - m * MAGIC); };
             const u64 mine_ahead = units(ahead_hi, ahead_lo, n_ahead);
             const u64 wa = warp_sum(units(all_hi, all_lo, n)), wh = warp_sum(mine_ahead);
