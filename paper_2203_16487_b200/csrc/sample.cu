@@ -16,8 +16,8 @@
 //   then    the kept weights by stretches of the row, one a warp, and the goal's stretch entry by entry.
 //
 // What bounds it is the instruction rate: per entry the exponential and its two whole parts are some 20 instructions, the histogram adds one atomic (shared memory takes
-// about ten lanes a clock).  3328 rows of 32768 bf16 (218 MB, 33 us at the memory's rate), every row: greedy 42 us, top-k 40 95, no cut 130, top-p 254 (by the histogram
-// over 1024 steps, which takes every exponential twice, 287).  64 rows of 131072 with top-p: 37 us, by the histogram 45.
+// about ten lanes a clock).  3328 rows of 32768 bf16 (218 MB, 33 us at the memory's rate), every row: greedy 42 us, top-k 40 83, no cut 126, top-p 251 (by the histogram
+// over 1024 steps, which takes every exponential twice, 287).  64 rows of 131072 with top-p: 34 us, by the histogram 45.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -394,8 +394,10 @@ template <typename T> struct RowData {
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) l[j] = pair2(to_f(u.x[2 * j]), to_f(u.x[2 * j + 1]));
     }
-    template <typename F> __device__ __forceinline__ void each(int v0, int v1, F f) const {       // vectors [v0, v1), by one warp
-        for (int v = v0 + (threadIdx.x & 31); v < v1; v += 32) vec(v, f);
+    template <typename F> __device__ __forceinline__ void each(int v0, int v1, F f) const {       // vectors [v0, v1), by one warp, in few instructions
+        for (int v = v0 + (threadIdx.x & 31); v < v1; v += 32)
+#pragma unroll 1
+            for (int i = first + v * N; i < first + v * N + N; ++i) f(at(i), i);
     }
 };
 __device__ __forceinline__ u64 composite(float l, int i) { return (u64)key_of(l) << 32 | (uint32_t)~i; }
@@ -1007,8 +1009,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         if (C > 1) cluster_wait();
         return;
     }
-    // its stretch again, consecutive vectors to a thread
-    const int w0 = min(sh.winner * per_warp, mine_vec), w1 = min(w0 + per_warp, mine_vec), each = (w1 - w0 + NT - 1) / NT;
+    // its stretch again, consecutive entries to a thread (loops as they stand: unrolled, the code of a row's rarer parts pushes the rest out of the instruction cache)
+    const int w0 = data.first + min(sh.winner * per_warp, mine_vec) * N, w1 = data.first + min((sh.winner + 1) * per_warp, mine_vec) * N, each = (w1 - w0 + NT - 1) / NT;
     const int t0 = min(w0 + tid * each, w1), t1 = min(t0 + each, w1);
     auto kept = [&](float l, int i) -> u64 {
         if (composite(l, i) < cut) return 0;
@@ -1016,22 +1018,23 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         return w >= min_p ? Row::units(w) : 0;
     };
     u64 t = 0;
-    for (int v = t0; v < t1; ++v) data.vec(v, [&](float l, int i) { t += kept(l, i); });
+#pragma unroll 1
+    for (int i = t0; i < t1; ++i) t += kept(data.at(i), i);
     const u64 start = sh.sum_before, upto = warp_scan(t);
     if (lane == 31) sh.w_sum[warp] = upto;
     __syncthreads();
     u64 unused;
     u64 at = start + warps_before<NT>(sh.w_sum, unused) + upto - t;
     if (at <= goal && goal < at + t)
-        for (int v = t0; v < t1; ++v)
-            data.vec(v, [&](float l, int i) {
-                const u64 w = kept(l, i);
-                if (at <= goal && goal < at + w) {
-                    a.token[r] = i;
-                    if (a.logprob) a.logprob[r] = row.x_of(l) - log_of(total);
-                }
-                at += w;
-            });
+#pragma unroll 1
+        for (int i = t0; i < t1; ++i) {
+            const u64 w = kept(data.at(i), i);
+            if (at <= goal && goal < at + w) {
+                a.token[r] = i;
+                if (a.logprob) a.logprob[r] = row.x_of(data.at(i)) - log_of(total);
+            }
+            at += w;
+        }
     if (C > 1) { __syncwarp(); cluster_wait(); }
 }
 
