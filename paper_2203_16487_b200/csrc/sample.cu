@@ -1046,15 +1046,16 @@ cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
     if (attr != cudaSuccess) return attr;
     return op_launch(k_sample<T, NT, C>, dim3(rows * C), NT, smem, st, C, a);
 }
-// CTAs of a row: as few as hold it, and more while every CTA has an SM to itself and 8192 entries (26 rows of 32768, top-p: 1, 2, 4, 8 CTAs 20.8, 20.4, 18.2, 22.6 us; 128
-// rows: 1, 2, 4 CTAs 21.7, 24.9, 36.4).  1024 threads where a whole row has an SM to itself; else 512, two
-// CTAs to an SM (128 rows of 32768 bf16: 23.2 us with 512, 21.4 with 1024; 26 rows on 4 CTAs each 17.0 and 18.0).
+// CTAs of a row: as few as hold it, and more while every CTA has an SM to itself and 8192 entries (26 rows of 32768 fp32, top-p: 1, 2, 4, 8 CTAs 17.8, 16.3, 15.1, 20.3 us).  An SM to
+// itself have 74 clusters of 2 CTAs, 33 of 4 and 15 of 8 (SMs come in groups of up to 18 that a cluster does not leave): 33 and 34 rows of 32768 on 4 CTAs 15.4 and 17.9 us, on 2 16.2 and
+// 16.3; 15 and 16 rows of 131072 on 8 CTAs 23.0 and 28.6, on 4 25.6 and 25.6; 74 rows of 50265 on 1 and 2 25.6 and 21.8, 96 rows 25.6 and 37.9.  1024 threads where a whole row has an SM to
+// itself (74 rows of 50265 25.6, with 512 26.4); else 512, two CTAs to an SM (160 rows of 32768 bf16: 25.0 us, with 1024 31.1; 26 rows on 4 CTAs each 15.1 and 17.3).
 template <typename T>
 cudaError_t launch(const SampleArgs& a, int rows, cudaStream_t st) {
     auto bytes = [&](int c) { return ((size_t)a.V * sizeof(T) / 16 + 2 + c) / c * 16 + 16; };
     int c = 1;
     while (bytes(c) > SA_SMEM - SA_STATIC) c *= 2;
-    while (c < 8 && (long long)rows * 2 * c <= 148 && a.V >= 2 * c * 8192) c *= 2;
+    while (c < 8 && rows <= (c == 1 ? 74 : c == 2 ? 33 : 15) && a.V >= 2 * c * 8192) c *= 2;
     const size_t smem = bytes(c);
     if ((c > 1 || rows > 148) && 2 * (smem + SA_STATIC + 1024) <= SA_SMEM)
         return c == 1 ? run<T, 512, 1>(a, rows, smem, st) : c == 2 ? run<T, 512, 2>(a, rows, smem, st) : c == 4 ? run<T, 512, 4>(a, rows, smem, st) : run<T, 512, 8>(a, rows, smem, st);
