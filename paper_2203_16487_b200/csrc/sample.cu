@@ -8,7 +8,7 @@
 //   greedy  the first index of the maximum.
 //   few     top-k of at most SA_FEW.  The k-th largest of a CTA's threads' own maxima is a bound below the k-th largest entry, so only the entries above the best such
 //           bound are looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No exponential of the others is taken.
-//   window  top-p alone: the numbers of entries in 3072 equal steps of x, without an exponential, give a window of a few steps that the cut must lie in; one pass over
+//   window  top-p alone: the numbers of entries in 3000 equal steps of x, without an exponential, give a window of a few steps that the cut must lie in; one pass over
 //           all weights then has their sum, what is ahead of the window, and a list of what is in it.
 //   order   larger top-k, and what a window's list does not hold: a histogram over 1024 equal steps of x gives the step in which the cut falls, and a list of that step's
 //           entries, ranked by counting, the cut itself.  (More entries in a step than the list holds: that step's range of logits, as ordered integers, is split into 1024
@@ -32,7 +32,7 @@ namespace sd {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int SA_BINS = 1024, SA_FINE = 3072, SA_FEW = 128, SA_LIST = 512, SA_WIDE = 1024;
+constexpr int SA_BINS = 1024, SA_FINE = 3000, SA_FEW = 128, SA_LIST = 512, SA_WIDE = 1024;
 constexpr float SA_RANGE = 27.75f;                        // e^-27.73 = 2^-40
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -242,6 +242,7 @@ __device__ void find_bin(Shared<NT>& sh, const Group<C>& cta, bool by_weight, u6
 template <int NT, int C>
 __device__ void find_window(Shared<NT>& sh, const Group<C>& cta, float top_p) {
     constexpr int SHARE = SA_FINE / C, PER = (SHARE + NT - 1) / NT;
+    static_assert(SA_FINE % C == 0 && SHARE % PER == 0, "equal shares");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = cta.rank * SHARE + threadIdx.x * PER;
     const bool mine = threadIdx.x * PER < SHARE;
     uint32_t n[PER];
