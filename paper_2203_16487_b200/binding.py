@@ -123,7 +123,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.specdec_tree_ancestors.argtypes = [ip, ip, i, i, vp, ip, vp]
     lib.specdec_tree_accept.argtypes = [ip, ip, ip, ip, i, i, ip, ip, ip, vp]
     lib.specdec_tree_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
-    lib.specdec_tree_attention.argtypes = [cp, C.POINTER(TreeAttentionArgs), vp]
+    lib.specdec_tree_attention.argtypes = [cp, vp, vp]         # (TreeAttentionArgs by reference, or its bytes)
     lib.specdec_sample.argtypes = [vp, i, L, i, i, vp, vp, ip, vp, vp, i, ip, vp, vp]
     for name in EXPORTS:
         if name not in ("specdec_launch_count", "specdec_last_error"):

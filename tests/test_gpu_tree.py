@@ -336,6 +336,13 @@ def test_attention_refusals():
                 lambda: tree.attention(q, cache, 0, ints([0]), m, scale=0.0), lambda: tree.attention(q, cache, 0, ints([0]), m, scale=math.nan)):
         with pytest.raises(binding.SpecDecError):
             bad()
+    with pytest.raises(binding.SpecDecError):
+        tree.attention(q, cache, 0, ints([0]), m, scale=1e300)
+    with pytest.raises(ValueError):
+        tree.attention(q, cache, 1 << 40, ints([0]), m)
+    for bad in (lambda: tree.attention(q, cache, 0, ints([0]).cpu(), m), lambda: tree.attention(q.cpu(), cache, 0, ints([0]), m), lambda: tree.sample(q[0, :, 0], q[0, :, 0, 0].float().cpu())):
+        with pytest.raises(ValueError):
+            bad()
     out = tree.attention(q, cache, 0, ints([7]), m)            # no such sequence: nothing to see
     assert (out == 0).all()
 
