@@ -6,8 +6,9 @@
 // A row is read from memory once, into the shared memory of one CTA or, where rows are few or long, of a cluster of up to 8, each with an equal stretch.  What a row
 // goes through depends on its parameters:
 //   greedy  the first index of the maximum.
-//   few     top-k of at most SA_FEW.  The k-th largest of a CTA's threads' own maxima is a bound below the k-th largest entry, so only the entries above the best such
-//           bound are looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No exponential of the others is taken.
+//   few     top-k of at most SA_FEW.  The k-th largest of a CTA's threads' own maxima is a bound below the k-th largest entry, and so is, in a cluster of C, the least of the
+//           CTAs' (k / C)-th; only the entries above the best bound are looked at again: a list of some k to 3k, ranked by counting, cut, and walked in index order.  No
+//           exponential of the others is taken.  (3328 rows of 32768 bf16: k = 128 127 us, k = 129 by the histogram 299.)
 //   window  top-p alone: the numbers of entries in 3000 equal steps of x, without an exponential, give a window of a few steps that the cut must lie in; one pass over
 //           all weights then has their sum, what is ahead of the window, and a list of what is in it.
 //   order   larger top-k, and what a window's list does not hold: a histogram over 1024 equal steps of x gives the step in which the cut falls, and a list of that step's
@@ -136,7 +137,7 @@ template <int NT> struct Shared {
     int w_cnt[32];
     float w_max[32];
     // what the CTAs of a cluster tell one another (each written once between two barriers)
-    float x_top, x_bound, x_weight;
+    float x_top, x_bound, x_share, x_weight;
     int x_bin, x_end, x_window, x_n;
     u64 x_cnt, x_sum, x_cnt_before, x_sum_before, x_total;
     // answers
@@ -522,14 +523,19 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         const uint32_t b = Row::bin_of(row.x_of(mine));
         if (b < SA_BINS) atomicAdd(sh.h.cnt + b, 1u);
         __syncthreads();
-        const int bin = bin_of_kth(sh.h.cnt, k);
-        // entries from here on up: all of steps 0 .. bin (a little more does no harm)
-        const float depth = (bin + 0.5f) * (SA_RANGE / SA_BINS) / inv_t;
-        float bound = bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
-        if (C > 1) {
-            if (tid == 0) sh.x_bound = bound;
+        // entries from a step on up: all of steps 0 .. bin (a little more does no harm)
+        auto from_step = [&](int bin) {
+            const float depth = (bin + 0.5f) * (SA_RANGE / SA_BINS) / inv_t;
+            return bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
+        };
+        float bound = from_step(bin_of_kth(sh.h.cnt, k));
+        if (C > 1) {                                      // k entries of one CTA, or k / C of each
+            const float share = from_step(bin_of_kth(sh.h.cnt, (k + C - 1) / C));
+            if (tid == 0) { sh.x_bound = bound; sh.x_share = share; }
             cta.sync();
-            for (int q = 0; q < C; ++q) bound = fmaxf(bound, cta.of(&sh, q)->x_bound);
+            float least = INFINITY;
+            for (int q = 0; q < C; ++q) { bound = fmaxf(bound, cta.of(&sh, q)->x_bound); least = fminf(least, cta.of(&sh, q)->x_share); }
+            bound = fmaxf(bound, least);
         }
         Shared<NT>* lead_sh = cta.of(&sh, 0);
         // the threads that have seen one, four at a time: eight lanes take a vector each of one thread's
@@ -768,7 +774,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             }
             const double thr = (double)top_p * (double)all;
             if (m > SA_WIDE || !((double)ahead < thr)) return false;
-            if (m <= SA_LIST / 2) {                       // few enough to be ranked as they are
+            if (m <= SA_LIST / 2) {                       // few enough to be ranked as they are (some 150 entries: 1 us less than in parts; 700: 64 rows of 131072 50 us, in parts 37)
                 for (int e = tid; e < m; e += NT) sh.any[e] = sh.wide[e];
                 __syncthreads();
                 return (double)(ahead + cut_in_list(m, 0, ahead, true, thr, true)) >= thr;
