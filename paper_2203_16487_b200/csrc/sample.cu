@@ -17,7 +17,7 @@
 //   then    the kept weights by stretches of the row, one a warp, and the goal's stretch entry by entry.
 //
 // What bounds it is the instruction rate: per entry the exponential and its two whole parts are some 20 instructions, the histogram adds one atomic (shared memory takes
-// about ten lanes a clock).  3328 rows of 32768 bf16 (218 MB, 33 us at the memory's rate), every row: greedy 42 us, top-k 40 83, no cut 126, top-p 251 (by the histogram
+// about ten lanes a clock).  3328 rows of 32768 bf16 (218 MB, 33 us at the memory's rate), every row: greedy 46 us, top-k 40 83, no cut 128, top-p 249 (by the histogram
 // over 1024 steps, which takes every exponential twice, 287).  64 rows of 131072 with top-p: 34 us, by the histogram 45.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -484,7 +484,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
     if (top == -INFINITY || greedy) {
         if (top > -INFINITY && mine == top) {
             int first = V;
-            data.each(v0, v1, [&](float l, int i) { if (l == top) first = min(first, i); });
+            for (int v = v0 + lane; v < v1; v += 32)
+                if (data.most(v) == top) data.vec(v, [&](float l, int i) { if (l == top) first = min(first, i); });
             atomicMin(&sh.index, first);
         }
         if (C > 1) {                                      // the first CTA that holds the maximum answers
