@@ -191,8 +191,8 @@ int specdec_accept_scan_static(const float* d_logits, const int32_t* d_draft, in
  * instead of taking the top token, and keeps the paged K/V cache in its own memory.  One decoding step is
  *     cache_reserve, (cache_append, tree_attention) in every layer, sample, tree_accept, cache_compact;
  * cache_fork and cache_release begin and end branches.  No handle; nothing is allocated; failures are reported as by
- * every other call (message: specdec_last_error(NULL)).  Operators on one cache are ordered by the caller (one stream,
- * or events).
+ * every other call (message: specdec_last_error(NULL)).  The device that holds a call's memory, and to which its stream
+ * belongs, has to be the current one.  Operators on one cache are ordered by the caller (one stream, or events).
  *
  * A tree is its nodes' parents: node 0 is the root (the last committed token), node i > 0 hangs off parents[i] in
  * [0, i).  Any other value is no parent: the node begins a tree of its own, which a walk from node 0 never reaches.
