@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "../../include/specdec.h"
 
 namespace sd {
@@ -20,6 +22,18 @@ inline cudaError_t op_launch(void (*kernel)(P...), dim3 grid, int threads, size_
     at[1].id = cudaLaunchAttributeClusterDimension; at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+// Lets `Kernel` have up to `bytes` of dynamic shared memory on the current device: set once for each device, as the limit belongs to both (beyond 64 devices: every time).  A
+// refusal is not kept.
+template <auto* Kernel> inline cudaError_t op_allow(int bytes) {
+    static std::atomic<unsigned long long> done{0};
+    int d;
+    if (const cudaError_t e = cudaGetDevice(&d)) return e;
+    const unsigned long long bit = d < 64 ? 1ull << d : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 #ifdef __CUDACC__
 __device__ __forceinline__ void op_begin() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -1050,8 +1050,7 @@ constexpr size_t SA_STATIC = 25 * 1024, SA_SMEM = 232448; // shared memory besid
 template <typename T, int NT, int C>
 cudaError_t run(const SampleArgs& a, int rows, size_t smem, cudaStream_t st) {
     static_assert(sizeof(Shared<NT>) <= SA_STATIC, "what is beside the row");
-    static const cudaError_t attr = cudaFuncSetAttribute(k_sample<T, NT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SA_SMEM - SA_STATIC));
-    if (attr != cudaSuccess) return attr;
+    if (const cudaError_t e = op_allow<k_sample<T, NT, C>>((int)(SA_SMEM - SA_STATIC))) return e;
     return op_launch(k_sample<T, NT, C>, dim3(rows * C), NT, smem, st, C, a);
 }
 // CTAs of a row: as few as hold it, and more while every CTA has an SM to itself and 8192 entries (26 rows of 32768 fp32, top-p: 1, 2, 4, 8 CTAs 17.8, 16.3, 15.1, 20.3 us).  An SM to

@@ -416,16 +416,14 @@ long long workspace(const Plan& p, int B, int n_kv_heads, int head_dim) {
 template <typename T, int DP>
 cudaError_t run_small_pages(const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int NS = 3, RING = NS * 2 * TA_BLOCK * DP * 2;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_small_pages<T, DP, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING + 65 * 32 * 4 + TA_MAX_B * 16);
-    if (attr != cudaSuccess) return attr;
+    if (const cudaError_t e = op_allow<k_ta_small_pages<T, DP, NS>>(RING + 65 * 32 * 4 + TA_MAX_B * 16)) return e;
     return op_launch(k_ta_small_pages<T, DP, NS>, dim3(ta_grid(a, grid, 2 * TA_SMS)), 128, RING + 65 * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
 template <int DP, int RI, int PER_SM>
 cudaError_t run_f32(const TreeAttn& a, int grid, cudaStream_t st) {
     using Cfg = TfCfg<DP, RI, PER_SM>;
     constexpr int BYTES = Cfg::FLOATS * 4;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_f32<DP, RI, PER_SM>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES + (Cfg::ROWS + 1) * 32 * 4 + TA_MAX_B * 16);
-    if (attr != cudaSuccess) return attr;
+    if (const cudaError_t e = op_allow<k_ta_f32<DP, RI, PER_SM>>(BYTES + (Cfg::ROWS + 1) * 32 * 4 + TA_MAX_B * 16)) return e;
     return op_launch(k_ta_f32<DP, RI, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 32 * Cfg::WK, BYTES + (Cfg::ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, a);
 }
 template <int DP>

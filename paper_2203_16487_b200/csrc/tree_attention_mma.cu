@@ -175,13 +175,14 @@ template <typename T, int DP, int WM, int WK, int NS>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int ROWS = 16 * WM, RING = NS * 2 * TA_BLOCK * DP * 2, RED = (WK > 1) * ROWS * ((DP + 8) * 4 + 8);
     constexpr int MOST = RING + RED + 1024 + (ROWS + 2) * 32 * 4 + TA_MAX_B * 16;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tma<T, DP, WM, WK, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
-    if (attr != cudaSuccess) return attr;
-    static const int per_sm = [] {
-        int n = 1;
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_ta_tma<T, DP, WM, WK, NS>, 32 * (WM * WK + 1), MOST);
-        return n < 1 ? 1 : n;
-    }();
+    if (const cudaError_t e = op_allow<k_ta_tma<T, DP, WM, WK, NS>>(MOST)) return e;
+    static std::atomic<int> found{0};                     // (the same on every device this code runs on)
+    int per_sm = found.load(std::memory_order_relaxed);
+    if (!per_sm) {
+        if (const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_ta_tma<T, DP, WM, WK, NS>, 32 * (WM * WK + 1), MOST)) return e;
+        if (per_sm < 1) per_sm = 1;
+        found.store(per_sm, std::memory_order_relaxed);
+    }
     return op_launch(k_ta_tma<T, DP, WM, WK, NS>, dim3(ta_grid(a, grid, per_sm * TA_SMS)), 32 * (WM * WK + 1), RING + RED + 1024 + (ROWS + 2) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>

@@ -419,8 +419,7 @@ template <typename T, int DP, int TILES>
 cudaError_t run(const CUtensorMap& tm, const TreeAttn& a, int grid, cudaStream_t st) {
     constexpr int BYTES = TcAttn<DP, TILES>::BYTES + 1024, MOST = BYTES + (TILES * TC_ROWS + 1) * (TILES == 2 && DP > 64 ? TA_WIDE_T / 32 : 32) * 4 + TA_MAX_B * 16;
     static_assert(MOST <= 232448 - (TILES == 1 ? 2048 : 1024), "shared memory of an SM");
-    static const cudaError_t attr = cudaFuncSetAttribute(k_ta_tc<T, DP, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
-    if (attr != cudaSuccess) return attr;
+    if (const cudaError_t e = op_allow<k_ta_tc<T, DP, TILES>>(MOST)) return e;
     return op_launch(k_ta_tc<T, DP, TILES>, dim3(ta_grid(a, grid, TA_SMS)), 32 * TC_WARPS, BYTES + (TILES * TC_ROWS + 1) * a.words * 4 + (a.direct == 1 ? 0 : a.B) * 16, st, 1, tm, a);
 }
 template <typename T>

@@ -101,8 +101,7 @@ extern "C" {
 int specdec_tree_ancestors(const int32_t* d_parents, const int32_t* d_n_nodes, int B, int T, uint32_t* d_mask, int32_t* d_depth, void* stream) {
     if (int rc = check("tree_ancestors", B, T, d_parents && (d_mask || d_depth))) return rc;
     if (B == 0) return SPECDEC_OK;
-    static const cudaError_t attr = cudaFuncSetAttribute(k_tree_ancestors, cudaFuncAttributeMaxDynamicSharedMemorySize, TO_MAX * (TO_MAX / 32 + 1 + 2) * 4);
-    if (attr != cudaSuccess) return op_done("tree_ancestors", attr);
+    if (const cudaError_t e = op_allow<k_tree_ancestors>(TO_MAX * (TO_MAX / 32 + 1 + 2) * 4)) return op_done("tree_ancestors", e);
     const int threads = T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256;
     return op_done("tree_ancestors", op_launch(k_tree_ancestors, dim3(B), threads, (size_t)T * ((((T + 31) / 32) | 1) + 2) * 4, (cudaStream_t)stream, 1, d_parents, d_n_nodes, T, d_mask, d_depth));
 }

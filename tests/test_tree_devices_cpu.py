@@ -1,8 +1,11 @@
-"""The tree operators in a process of several devices, without any: which device is current when the library is entered."""
+"""The tree operators in a process of several devices, without any: which device is current when the library is entered, what it sets for each."""
+import os
+import subprocess
+
 import pytest
 import torch
 
-from paper_2203_16487_b200 import tree
+from paper_2203_16487_b200 import build, tree
 
 
 class OnDevice1:
@@ -83,3 +86,23 @@ def test_every_operator_runs_on_the_tensors_device(library, current):
     for name, on, stream in library.calls:
         assert on == 1 and stream == 0, name
     assert library.state["current"] == current                # and left as it was
+
+
+@pytest.fixture(scope="module")
+def host_side(tmp_path_factory):
+    """The operators' object files, as they are in the library, on a runtime that is tests/stub_runtime.cpp."""
+    build.build()
+    objs = [os.path.join(build.OBJ, n + ".o") for n in ("sample", "tree_ops", "tree_attention", "tree_attention_mma", "tree_attention_tc")]
+    if not all(os.path.exists(o) for o in objs):
+        build.build(force=True)
+    here, exe = os.path.dirname(os.path.abspath(__file__)), str(tmp_path_factory.mktemp("stub") / "host_side")
+    r = subprocess.run(["g++", "-std=c++17", "-I/usr/local/cuda/include", "-o", exe, os.path.join(here, "stub_runtime.cpp")] + objs, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+    return {name: int(n) for name, n in (line.split() for line in r.stdout.splitlines())}, r.stderr
+
+
+def test_shared_memory_limits_are_set_on_every_device(host_side):
+    """A limit belongs to a kernel and a device: set once on each, and asked for again where it was refused."""
+    assert not any(host_side[0].values()), host_side
