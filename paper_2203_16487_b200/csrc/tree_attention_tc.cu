@@ -336,9 +336,10 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
         float f = l == 0.f ? 0.f : 1.f, f1 = 0.f;         // shares of this group's output and, TILES = 1, of the other's
         const int rr = (warp & 3) * 32 + lane, n1 = steps(it.blocks, 1);
         if constexpr (TILES == 1) {                       // both outputs are in this lane's tensor memory: the first group adds them up
-            if (g == 1) other[rr] = make_float2(m, l);
+            if (g == 1) { other[rr] = make_float2(m, l); tc_fence_before(); }      // (what the second group has waited for, the first reads)
             softmax_warps();
             if (g == 0) {
+                tc_fence_after();
                 const float m1 = other[rr].x, l1 = other[rr].y, mm = fmaxf(m, m1), z = mm == -INFINITY ? 0.f : mm;
                 f = ta_exp2(m - z); f1 = ta_exp2(m1 - z);
                 l = l * f + l1 * f1;

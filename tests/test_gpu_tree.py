@@ -250,6 +250,19 @@ def test_attention_uneven_long_sequences(dtype, T, H, Hkv, D):
     check_attention(got, want, mag, dtype, 5100)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("H,Hkv,D", [(2, 1, 64), (2, 1, 128)])
+def test_attention_two_groups_meet(dtype, H, Hkv, D):
+    """Tiles of 128 rows, whose two groups take every second block of 128 keys and add up their outputs: none, one, two, three and many blocks, parts of a long sequence,
+    the same bits every time."""
+    from paper_2203_16487_b200 import tree
+    T, lens = 50, [0, 70, 128 - 50, 206, 300, 1000, 6000]
+    got, want, mag, (cache, q, seqs, bits, nodes) = attention_case(dtype, lens, T, H, Hkv, D, 16, seed=11, nodes=[T, T, T, T, 7, T, T])
+    check_attention(got, want, mag, dtype, 6100)
+    for _ in range(20):
+        assert torch.equal(got, tree.attention(q, cache, 0, ints(seqs), bits, n_nodes=ints(nodes)))
+
+
 @pytest.mark.parametrize("T,H,Hkv,D,lens", [(1024, 1, 1, 128, [70]), (970, 2, 1, 128, [0]), (1024, 1, 1, 64, [5, 1]), (300, 3, 1, 128, [129, 0]), (40, 12, 12, 64, [(i * 53) % 400 for i in range(41)])])
 def test_attention_wide_trees(T, H, Hkv, D, lens):
     """The most nodes a tree may have (whose masks are 32 words a row), and whole sequences of 64 rows dealt to CTAs by length."""
