@@ -34,13 +34,13 @@ def _fail(rc):
     raise SpecDecError(rc, lib().specdec_last_error(None).decode())
 
 
-def _launch(f, at, *args):
-    """f(*args, stream) with the tensors' device `at` current: the library launches on the current device, and the default streams of all devices are one handle."""
+def _launch(f, at, args):
+    """f(*args) with the tensors' device `at` current: the library launches on the current device, and the default streams of all devices are one handle."""
     if _current_device() == at:
-        rc = f(*args, _raw_stream(at))
+        rc = f(*args)
     else:
         with torch.cuda.device(at):
-            rc = f(*args, _raw_stream(at))
+            rc = f(*args)
     if rc:
         _fail(rc)
 
@@ -94,7 +94,7 @@ class PagedCache:
     def reserve(self, seqs, n_tokens: int):
         """Pages for n_tokens tokens behind the committed ones."""
         n = seqs.numel()
-        _launch(self._lib.specdec_cache_reserve, self._device, self._ref, _ints("seqs", seqs, (n,), self._device), n, n_tokens)
+        _launch(self._lib.specdec_cache_reserve, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, n_tokens, _raw_stream(self._device)))
 
     def append(self, seqs, k, v, layer: Optional[int] = None, count=None):
         """Writes k, v [n, T, n_heads, head_dim] (layer=None: [n_layers, n, T, n_heads, head_dim], every layer) behind the committed tokens; of
@@ -109,24 +109,24 @@ class PagedCache:
         if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
                 and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
             raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")
-        _launch(self._lib.specdec_cache_append, self._device, self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
-                s[0], s[1], s[2], s[3], None if count is None else _ints("count", count, (n,), self._device))
+        _launch(self._lib.specdec_cache_append, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
+                s[0], s[1], s[2], s[3], None if count is None else _ints("count", count, (n,), self._device), _raw_stream(self._device)))
 
     def compact(self, seqs, path, n_path):
         """Commits the nodes path[i, :n_path[i]] of each sequence's block and gives back the pages behind them."""
         n, T = seqs.numel(), path.shape[-1]
-        _launch(self._lib.specdec_cache_compact, self._device, self._ref, _ints("seqs", seqs, (n,), self._device), n, _ints("path", path, (n, T), self._device), T,
-                _ints("n_path", n_path, (n,), self._device))
+        _launch(self._lib.specdec_cache_compact, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _ints("path", path, (n, T), self._device), T,
+                _ints("n_path", n_path, (n,), self._device), _raw_stream(self._device)))
 
     def release(self, seqs):
         """Gives back all pages of the sequences; their lengths are 0."""
         n = seqs.numel()
-        _launch(self._lib.specdec_cache_release, self._device, self._ref, _ints("seqs", seqs, (n,), self._device), n)
+        _launch(self._lib.specdec_cache_release, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _raw_stream(self._device)))
 
     def fork(self, src, dst):
         """Sequence dst[i] becomes a copy of what src[i] was before the call: full pages shared, the last, partly filled one copied."""
         n = src.numel()
-        _launch(self._lib.specdec_cache_fork, self._device, self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n)
+        _launch(self._lib.specdec_cache_fork, self._device, (self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n, _raw_stream(self._device)))
 
     def check(self):
         """Raises if a call found too few pages or bad numbers since the last check (waits for the stream)."""
@@ -144,7 +144,7 @@ def ancestors(parents, n_nodes=None):
     at = parents.get_device()
     p = _ints("parents", parents, (B, T), at)
     mask, depth = parents.new_empty(B, T, (T + 31) // 32), torch.empty_like(parents)
-    _launch(lib().specdec_tree_ancestors, at, p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at), B, T, mask.data_ptr(), depth.data_ptr())
+    _launch(lib().specdec_tree_ancestors, at, (p, None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at), B, T, mask.data_ptr(), depth.data_ptr(), _raw_stream(at)))
     return mask, depth
 
 
@@ -155,8 +155,8 @@ def accept(parents, tokens, sampled, n_nodes=None):
     at = parents.get_device()
     p = _ints("parents", parents, shape, at)
     path, emitted, n_path = torch.empty_like(parents), torch.empty_like(parents), parents.new_empty(B)
-    _launch(lib().specdec_tree_accept, at, p, _ints("tokens", tokens, shape, at), _ints("sampled", sampled, shape, at), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at),
-            B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr())
+    _launch(lib().specdec_tree_accept, at, (p, _ints("tokens", tokens, shape, at), _ints("sampled", sampled, shape, at), None if n_nodes is None else _ints("n_nodes", n_nodes, (B,), at),
+            B, T, path.data_ptr(), n_path.data_ptr(), emitted.data_ptr(), _raw_stream(at)))
     return path, n_path, emitted
 
 
@@ -193,7 +193,7 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
                                  ws.data_ptr() if n else 0, n)
     except struct.error as e:
         raise ValueError(f"layer or scale: {e}") from None
-    _launch(L.specdec_tree_attention, at, cache._ref, a)
+    _launch(L.specdec_tree_attention, at, (cache._ref, a, _raw_stream(at)))
     return out
 
 
@@ -222,5 +222,5 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
             ptrs[i] = t.data_ptr()
     logprob = torch.empty_like(uniform)
     token = torch.empty_like(uniform, dtype=_I32)
-    _launch(lib().specdec_sample, at, logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr())
+    _launch(lib().specdec_sample, at, (logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _raw_stream(at)))
     return token, logprob
