@@ -28,6 +28,8 @@ __device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity)
 // Bounded wait: gives up after ~2e8 clocks, raises the CTA-wide abort flag and the global error word.  The warp that gives up then holds the
 // CTA, and with it the shared memory that its copies in flight and its peers still write to, for about a millisecond longer: many times what
 // a copy that was issued before the flag was up can take.
+// GATHERS: the word is one of bits, to which `code` is added; else it holds the last code.
+template <bool GATHERS = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err_word,
                                           int code) {
     if (mbar_try_wait(bar, parity)) return true;      // fast path: no other shared-memory access
@@ -38,15 +40,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         if (*abort_flag) return false;
         if (clock64() - t0 > 200000000LL) {
             *abort_flag = 1;
-            atomicExch(err_word, code);
+            if (GATHERS) atomicOr(err_word, code);
+            else atomicExch(err_word, code);
             while (clock64() - t0 < 202000000LL) {}
             return false;
         }
     }
 }
 // The same for a converged warp: every lane gets the same answer, as an elected instruction behind it needs all of them there.
+template <bool GATHERS = false>
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* err_word, int code) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, err_word, code));
+    return __all_sync(0xffffffffu, mbar_wait<GATHERS>(bar, parity, abort_flag, err_word, code));
 }
 // 16 consecutive bytes to the shared memory of CTA `rank` of this cluster, counted on its mbarrier.
 __device__ __forceinline__ void st_peer16(uint32_t local_addr, uint32_t local_bar, uint32_t rank, uint4 v) {

@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
             for (int j = 0; j < it.blocks; ++j) {
                 const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), key = it.k_begin + j * KT + lane * box, cur = p;
                 if (j + 1 < it.blocks) p = page_of(j + 1);
-                if (n >= NG && !mbar_wait_warp(empty + st * 8, (n / NG - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
+                if (n >= NG && !mbar_wait_warp<true>(empty + st * 8, (n / NG - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
                 const bool mine = lane < n_pages && key < it.k_end;
                 const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine));
                 if (lane == 0) mbar_expect_tx(full + st * 8, boxes * box * 128 * HALVES * 2);
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         rows.clear();
         for (int j = wk; j < it.blocks; j += WK, ++count) {
             const int st = wk + WK * (count % NG), k0 = it.k_begin + j * KT;
-            if (!mbar_wait_warp(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
+            if (!mbar_wait_warp<true>(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
             const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
             const bool tail = k0 + KT > s.len;            // nodes, or what is behind the last key
             if (tail) {                                   // values that no query sees: whatever is in them is multiplied by 0

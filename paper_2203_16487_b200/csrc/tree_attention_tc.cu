@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
     // steps of group g in a part of `blocks` blocks of 128 keys; its i-th is block_of(g, i)
     auto steps = [](int blocks, int g) { return TILES == 2 ? blocks : (blocks + 1 - g) / 2; };
     auto block_of = [](int g, int i) { return TILES == 2 ? i : 2 * i + g; };
-    auto wait = [&](uint32_t bar, int n) { return mbar_wait_warp(bar, n & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT); };     // for its completion number n
+    auto wait = [&](uint32_t bar, int n) { return mbar_wait_warp<true>(bar, n & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT); };     // for its completion number n
     Part it;
     int done = 0;                                         // blocks of the parts before: block j is in stage (done + j) % NS
     bool ok = true;
