@@ -282,7 +282,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
  * units, so that their sums are exact, and a token is the same however the work is split.
  *   top_k  > 0: the k largest (ties: lower index first) stay;
  *   top_p  < 1: of those, in that order, entry i stays if the weight ahead of it is below top_p times their total;
- *   min_p  > 0: entries with exp((l_i - m) / T) >= min_p stay;     the largest always stays.
+ *   min_p  > 0: entries with exp((l_i - m) / T) >= min_p stay;     the largest always stays (top_p, min_p NaN: off).
  *   token = the first index at which the running sum of the kept weights exceeds floor(uniform * total).
  * temperature <= 0 (or NaN) takes the largest entry (lowest index).  d_logprob (or NULL) = log of the token's share of the kept weights.  A row
  * of only -inf and NaN gives token -1, log probability -inf.

@@ -453,7 +453,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
         }
     }
     const float temperature = a.temperature ? a.temperature[pr] : 1.f;
-    const float top_p = a.top_p ? a.top_p[pr] : 1.f, min_p = a.min_p ? a.min_p[pr] : 0.f;
+    const float p_in = a.top_p ? a.top_p[pr] : 1.f, m_in = a.min_p ? a.min_p[pr] : 0.f;
+    const float top_p = p_in < 1.f ? p_in : 1.f, min_p = m_in > 0.f ? m_in : 0.f;        // (NaN: off)
     const int k_in = a.top_k ? a.top_k[pr] : 0;
     const float u = a.uniform[r];
     const int k = k_in <= 0 || k_in > V ? V : k_in;

@@ -428,6 +428,17 @@ def test_sample_hard_rows(what, V):
                  most_near=rows // 2)                        # (few distinct weights: top_p of them is often a whole number of entries)
 
 
+@pytest.mark.parametrize("V", [700, 50265])
+def test_sample_parameters_that_are_no_numbers(V):
+    """top_p and min_p of NaN cut nothing, as neither top_p < 1 nor min_p > 0 holds; a temperature of NaN is none above 0.  By every route: top-k small, large or off."""
+    rng = np.random.default_rng(V)
+    rows = 36
+    l = (rng.standard_normal((rows, V)) * 2).astype(np.float32)
+    p, m = rng.choice([1, 0.7, math.nan, math.inf], rows), rng.choice([0, 0.05, math.nan, -1], rows)
+    p[:3], m[:3] = (math.nan, math.nan, 0.9), (math.nan, 0.1, math.nan)
+    check_sample(torch.from_numpy(l), rng.random(rows).astype(np.float32), rng.choice([1, 0.7, math.nan], rows, p=[0.5, 0.4, 0.1]), rng.choice([0, 40, V // 2], rows), p, m)
+
+
 def test_sample_parameters_and_strides():
     """No parameters, one for a run of rows, rows inside wider tensors that begin anywhere; the same token however the rows lie."""
     from paper_2203_16487_b200 import tree
