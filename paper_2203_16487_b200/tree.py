@@ -1,6 +1,7 @@
 """Operators of tree speculation on the caller's own tensors: a paged K/V cache, attention of drafted trees over it, sampling,
 and the walk that accepts a branch.  Thin wrappers of the specdec_cache_* / specdec_tree_* / specdec_sample calls (contracts: include/specdec.h);
-every call runs on the tensors' device, on its current stream, and returns without waiting for it.
+every call runs on the tensors' device, on its current stream, and returns without waiting for it.  They serve inference: a result of tensors that require a gradient
+passes on, and raises when the gradient is asked for.
 
     mask, depth = tree.ancestors(parents)                    # once a step
     cache.reserve(seqs, T)
@@ -43,6 +44,19 @@ def _launch(f, at, args):
             rc = f(*args)
     if rc:
         _fail(rc)
+
+
+class _NoGradient(torch.autograd.Function):
+    """Passes a result on as one of `source`, which requires a gradient; there is none to give."""
+
+    @staticmethod
+    def forward(ctx, result, source, name):
+        ctx.name = name
+        return result
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name} has no gradient: call it under torch.no_grad(), or on detached tensors")
 
 
 def _ints(name, t, shape, device):
@@ -89,6 +103,7 @@ class PagedCache:
         self._ref, self._lib, self._device = C.byref(self._c), lib(), kv.get_device()
         self._code, self._page = DTYPES[kv.dtype], page
         self._workspaces = {}                              # bytes by sizes of a call
+        self._source = None                                # requires a gradient, where keys or values did
         self.dtype, self.n_heads, self.head_dim, self.max_length = kv.dtype, H, D, table.shape[1] * page
 
     def reserve(self, seqs, n_tokens: int):
@@ -109,6 +124,8 @@ class PagedCache:
         if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
                 and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
             raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")
+        if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled() and self._source is None:
+            self._source = torch.zeros((), requires_grad=True)
         _launch(self._lib.specdec_cache_append, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
                 s[0], s[1], s[2], s[3], None if count is None else _ints("count", count, (n,), self._device), _raw_stream(self._device)))
 
@@ -194,6 +211,8 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     except struct.error as e:
         raise ValueError(f"layer or scale: {e}") from None
     _launch(L.specdec_tree_attention, at, (cache._ref, a, _raw_stream(at)))
+    if (q.requires_grad or cache._source is not None) and torch.is_grad_enabled():
+        return _NoGradient.apply(out, q if q.requires_grad else cache._source, "tree.attention")
     return out
 
 
@@ -223,4 +242,6 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     logprob = torch.empty_like(uniform)
     token = torch.empty_like(uniform, dtype=_I32)
     _launch(lib().specdec_sample, at, (logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _raw_stream(at)))
+    if (logits.requires_grad or (temperature is not None and temperature.requires_grad)) and torch.is_grad_enabled():
+        logprob = _NoGradient.apply(logprob, logits if logits.requires_grad else temperature, "tree.sample")
     return token, logprob

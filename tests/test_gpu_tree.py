@@ -501,6 +501,41 @@ def test_sample_refusals():
         tree.sample(torch.zeros(1, 262145, device="cuda"), u[:1])
 
 
+def test_there_are_no_gradients_and_that_is_said():
+    """Tensors that require a gradient give the same values, and an error where the gradient is asked for; without autograd nothing is kept of it."""
+    from paper_2203_16487_b200 import tree
+    def cache():
+        return tree.PagedCache(1, 2, 64, n_pages=4, n_seqs=2, max_pages=2)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, q = torch.randn(1, 3, 2, 64, generator=g, device="cuda").bfloat16(), torch.randn(1, 3, 4, 64, generator=g, device="cuda").bfloat16()
+    m, s = ints([[[1], [3], [7]]]), ints([0])
+    def run(k, q, out=None):
+        c = cache()
+        c.reserve(s, 3)
+        c.append(s, k, k, layer=0)
+        return tree.attention(q, c, 0, s, m, out=out)
+    want = run(k, q)
+    assert not want.requires_grad
+    for a, b in ((k, q.clone().requires_grad_()), (k.clone().requires_grad_(), q)):
+        for out in (None, torch.empty_like(q)):
+            got = run(a, b, out)
+            assert torch.equal(got, want) and got.requires_grad
+            with pytest.raises(RuntimeError, match="tree.attention has no gradient"):
+                got.float().sum().backward()
+        with torch.no_grad():
+            got = run(a, b)
+        assert torch.equal(got, want) and not got.requires_grad
+    l, u, t = torch.randn(4, 50, generator=g, device="cuda"), torch.rand(4, generator=g, device="cuda"), torch.ones(4, device="cuda")
+    want = tree.sample(l, u, t)
+    for a, b in ((l.clone().requires_grad_(), t), (l, t.clone().requires_grad_())):
+        token, logp = tree.sample(a, u, b)
+        assert torch.equal(token, want[0]) and torch.equal(logp, want[1]) and logp.requires_grad and not token.requires_grad
+        with pytest.raises(RuntimeError, match="tree.sample has no gradient"):
+            logp.sum().backward()
+        with torch.no_grad():
+            assert not tree.sample(a, u, b)[1].requires_grad
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("batch,prompt,tokens", [(1, 1, 20), (5, 12, 48)])
 def test_tree_decoding_is_sampling_token_by_token(batch, prompt, tokens):
