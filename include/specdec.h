@@ -199,7 +199,8 @@ int specdec_accept_scan_static(const float* d_logits, const int32_t* d_draft, in
  *
  * The cache: page p holds page_tokens token slots of every layer; a slot's row of n_heads x head_dim elements is found
  * by the strides (elements; head_dim is contiguous; stride_side leads from a layer's keys to its values), so pages of
- * [token, head] and of [head, token] order both do.  d_kv and all strides are multiples of 16 bytes.  Slot t of
+ * [token, head] and of [head, token] order both do.  d_kv and all strides are multiples of 16 bytes (the stride of a
+ * dimension of 1, here and of every other tensor, does not matter).  Slot t of
  * sequence s is slot t % page_tokens of page d_table[s * max_pages + t / page_tokens].  d_length[s] tokens are
  * committed, d_held[s] pages are in the sequence's table (entries behind them are -1), d_refs[p] sequences hold page p
  * (0: free).  Pages are given out lowest number first, so what a call does depends on its arguments alone.  A new cache has

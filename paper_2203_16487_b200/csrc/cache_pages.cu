@@ -333,7 +333,8 @@ const char* view(const specdec_cache* c, Cache& v) {
     if (c->n_layers < 1 || c->n_heads < 1 || c->head_dim < 1 || c->n_pages < 1 || c->n_seqs < 1 || c->max_pages < 1) return "a size is below 1";
     if (c->page_tokens < 1 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens is not a power of two";
     if ((long long)c->max_pages * c->page_tokens > 0x7fffffffLL - 65536) return "a sequence could pass 2^31 tokens";
-    const long long st[5] = {c->stride_layer, c->stride_side, c->stride_page, c->stride_token, c->stride_head};
+    const long long st[5] = {op_stride(c->stride_layer, c->n_layers), c->stride_side, op_stride(c->stride_page, c->n_pages), op_stride(c->stride_token, c->page_tokens),
+                             op_stride(c->stride_head, c->n_heads)};
     if (!aligned16(c->d_kv) || (long long)c->head_dim * e % 16) return "d_kv or head_dim is not a multiple of 16 bytes";
     for (long long s : st) if (s < 0 || s * e % 16) return "a stride is negative or not a multiple of 16 bytes";
     v.kv = (char*)c->d_kv;
@@ -382,7 +383,7 @@ int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, i
     const int e = op_elem_bytes(c->dtype);
     if ((n && T && (!d_seqs || !d_k || !d_v)) || n < 0 || n > c->n_seqs || n > 65535 || T < 0 || layer < 0 || n_layers < 1 || n_layers > 65535 || layer > c->n_layers - n_layers)
         return op_bad("cache_append", "a pointer is NULL, or n, T or the layers are out of range");
-    const long long st[4] = {stride_layer, stride_seq, stride_token, stride_head};
+    const long long st[4] = {op_stride(stride_layer, n_layers), op_stride(stride_seq, n), op_stride(stride_token, T), op_stride(stride_head, c->n_heads)};
     for (long long s : st) if (s * e % 16) return op_bad("cache_append", "a stride is not a multiple of 16 bytes");
     if (!aligned16(d_k) || !aligned16(d_v)) return op_bad("cache_append", "d_k or d_v is not 16-byte aligned");
     if (n == 0 || T == 0) return SPECDEC_OK;

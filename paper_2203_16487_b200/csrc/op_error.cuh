@@ -10,6 +10,7 @@ namespace sd {
 int op_fail(int code, const char* who, const char* why) noexcept;      // returns code
 inline int op_bad(const char* who, const char* why) { return op_fail(SPECDEC_ERR_INVALID_ARG, who, why); }
 inline int op_elem_bytes(int dtype) { return dtype == SPECDEC_DTYPE_F32 ? 4 : dtype == SPECDEC_DTYPE_BF16 || dtype == SPECDEC_DTYPE_F16 ? 2 : 0; }
+inline long long op_stride(long long stride, long long extent) { return extent > 1 ? stride : 0; }     // (a dimension of 1 may come with any)
 // Launches behind one another: a kernel that begins with op_begin() is set up while its predecessor in the stream still runs, and waits for it there.  What such a kernel
 // reads comes by pointers without __restrict__: the compiler may fetch what those lead to ahead of the wait.
 // (cluster > 1: CTAs of a cluster.)

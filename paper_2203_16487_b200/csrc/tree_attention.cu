@@ -452,7 +452,8 @@ PFN_encodeTiled encoder() {
 bool tensor_map(CUtensorMap& tm, const specdec_cache* c, const void* keys) {
     const cuuint64_t e = 2;
     cuuint64_t dims[5] = {(cuuint64_t)c->head_dim, (cuuint64_t)c->n_heads, (cuuint64_t)c->page_tokens, (cuuint64_t)c->n_pages, 2};
-    cuuint64_t strides[4] = {c->stride_head * e, c->stride_token * e, c->stride_page * e, c->stride_side * e};
+    auto of = [&](long long stride, int extent) -> cuuint64_t { return (extent > 1 ? stride : c->head_dim) * e; };
+    cuuint64_t strides[4] = {of(c->stride_head, c->n_heads), of(c->stride_token, c->page_tokens), of(c->stride_page, c->n_pages), c->stride_side * e};
     cuuint32_t box[5] = {64, 1, (cuuint32_t)(c->page_tokens < TA_BLOCK ? c->page_tokens : TA_BLOCK), 1, 1}, one[5] = {1, 1, 1, 1, 1};
     return encoder() && encoder()(&tm, c->dtype == SPECDEC_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, const_cast<void*>(keys), dims, strides,
                                   box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -485,17 +486,18 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
     if ((long long)c->max_pages * c->page_tokens > 0x7fffffffLL - 65536) return op_bad(who, "a sequence could pass 2^31 tokens");
     if (g->T > 1024) return op_fail(SPECDEC_ERR_CAPACITY, who, "trees have at most 1024 nodes");
     if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return op_fail(SPECDEC_ERR_UNSUPPORTED, who, "head_dim is no multiple of 8 up to 128");
-    const long long st[5] = {c->stride_layer, c->stride_side, c->stride_page, c->stride_token, c->stride_head};
+    const long long st[5] = {op_stride(c->stride_layer, c->n_layers), c->stride_side, op_stride(c->stride_page, c->n_pages), op_stride(c->stride_token, c->page_tokens),
+                             op_stride(c->stride_head, c->n_heads)};
     for (long long s : st) if (s < 0 || s * e % 16) return op_bad(who, "a stride of the cache is negative or not a multiple of 16 bytes");
     if ((uintptr_t)c->d_kv % 16 || (uintptr_t)g->d_q % e || (uintptr_t)g->d_out % e) return op_bad(who, "d_kv is not 16-byte aligned, or q or out not to its type");
     if (!(g->scale > 0.f) || g->scale > 3e38f) return op_bad(who, "scale is not a positive number");
     if (g->B == 0) return SPECDEC_OK;
     TreeAttn a;
     a.q = (const char*)g->d_q; a.out = (char*)g->d_out;
-    a.k = (const char*)c->d_kv + g->layer * c->stride_layer * e; a.v = a.k + c->stride_side * e;
-    a.q_sb = g->q_stride_b * e; a.q_st = g->q_stride_t * e; a.q_sh = g->q_stride_h * e;
-    a.o_sb = g->out_stride_b * e; a.o_st = g->out_stride_t * e; a.o_sh = g->out_stride_h * e;
-    a.s_page = c->stride_page * e; a.s_token = c->stride_token * e; a.s_head = c->stride_head * e;
+    a.k = (const char*)c->d_kv + g->layer * st[0] * e; a.v = a.k + st[1] * e;
+    a.q_sb = op_stride(g->q_stride_b, g->B) * e; a.q_st = op_stride(g->q_stride_t, g->T) * e; a.q_sh = op_stride(g->q_stride_h, g->n_q_heads) * e;
+    a.o_sb = op_stride(g->out_stride_b, g->B) * e; a.o_st = op_stride(g->out_stride_t, g->T) * e; a.o_sh = op_stride(g->out_stride_h, g->n_q_heads) * e;
+    a.s_page = st[2] * e; a.s_token = st[3] * e; a.s_head = st[4] * e;
     a.table = c->d_table; a.length = c->d_length; a.status = c->d_status; a.seqs = g->d_seqs; a.n_nodes = g->d_n_nodes;
     a.mask = g->d_mask; a.mask_sb = g->mask_stride_b;
     a.n_pages = c->n_pages; a.n_seqs = c->n_seqs; a.max_pages = c->max_pages; a.page_shift = __builtin_ctz(c->page_tokens);

@@ -121,9 +121,9 @@ class PagedCache:
         else:
             layers, shape, s = 1, (1,) + tuple(shape), (0,) + tuple(s)
             good = len(shape) == 5
-        if not (good and v.shape == k.shape and v.stride() == k.stride() and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
+        if not (good and v.shape == k.shape and (v.stride() == k.stride() or all(a == b or m == 1 for a, b, m in zip(v.stride(), k.stride(), k.shape))) and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
                 and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
-            raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")
+            raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")      # (a dimension of 1 has none)
         if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled() and self._source is None:
             self._source = torch.zeros((), requires_grad=True)
         _launch(self._lib.specdec_cache_append, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
@@ -222,7 +222,7 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     shape = logits.shape
     V, lead = shape[-1], shape[:-1]
     code, at = DTYPES.get(logits.dtype), logits.get_device()
-    if code is None or not logits.is_cuda or logits.stride(-1) != 1:
+    if code is None or not logits.is_cuda or (logits.stride(-1) != 1 and V != 1):
         raise ValueError("logits: a device tensor of fp32, bf16 or fp16 with a contiguous last dimension is wanted")
     if uniform.shape != lead or uniform.dtype is not torch.float32 or uniform.get_device() != at or not uniform.is_contiguous():
         raise ValueError("uniform: a contiguous fp32 device tensor, one number a row, is wanted")

@@ -501,6 +501,41 @@ def test_sample_refusals():
         tree.sample(torch.zeros(1, 262145, device="cuda"), u[:1])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page", [1, 4, 16])
+def test_strides_of_dimensions_of_one_do_not_matter(dtype, page):
+    """Layers, pages, tokens, heads, sequences and entries of which there is one may come with any stride; the results are those of plain tensors."""
+    from paper_2203_16487_b200 import tree
+    D, g = 64, torch.Generator(device="cuda").manual_seed(page)
+    n = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    def odd(x):
+        """x again, with strides of 3, 5, 7, ... where its extent is 1."""
+        c = x.clone(memory_format=torch.contiguous_format)
+        y = torch.as_strided(c, c.shape, [s if m > 1 else 3 + 2 * i for i, (s, m) in enumerate(zip(c.stride(), c.shape))])
+        assert torch.equal(x, y)
+        return y
+    for P, H in ((1, 1), (3, 1), (1, 2)):
+        k, v, q, k1 = n(1, 1, page, H, D), n(1, 1, page, H, D), n(1, 1, 2 * H, D), n(1, 1, H, D)
+        outs = []
+        for f in (lambda x: x, odd):
+            kv = f(torch.zeros(1, 2, P, page, H, D, dtype=dtype, device="cuda"))
+            cache = tree.PagedCache.over(kv, ints([[-1]]), ints([0]), ints([0]), ints([0] * P))
+            s = ints([0])
+            cache.reserve(s, page)
+            cache.append(s, f(k), v)                           # (strides of keys and values differ where there is one)
+            cache.append(s, k1, f(k1), layer=0)
+            if page > 1:                                       # (all but the last token committed; with none, its page would be given back)
+                cache.compact(s, torch.arange(page, dtype=torch.int32, device="cuda")[None], ints([page - 1]))
+            out = tree.attention(f(q), cache, 0, s, ints([[[1]]]), out=f(torch.zeros_like(q)))
+            cache.check()
+            outs.append((out, kv))
+        assert torch.equal(*(o[0] for o in outs)) and torch.equal(*(o[1] for o in outs))
+        assert torch.equal(outs[0][1][0, 0, 0, 0], k1[0, 0]) and not (outs[0][0] == 0).all()
+    l, u = n(6, 50), torch.rand(6, generator=g, device="cuda")
+    assert torch.equal(tree.sample(odd(l[:, 7:8]), u)[0], torch.zeros_like(u).int())
+    assert torch.equal(tree.sample(l.T[7:8].T, u)[0], tree.sample(l[:, 7:8].contiguous(), u)[0])
+
+
 def test_there_are_no_gradients_and_that_is_said():
     """Tensors that require a gradient give the same values, and an error where the gradient is asked for; without autograd nothing is kept of it."""
     from paper_2203_16487_b200 import tree
