@@ -182,6 +182,7 @@ __global__ void k_cache_append(Cache c, AppendArgs a) {
 // CTA = (64 columns' worth of pieces of one layer and side, sequence).  A thread moves its piece of every token of the path, in the path's order and
 // up to eight at a time, all eight read before the first is written: path[i] >= i, so a write goes to a slot whose own token was read before or is dropped.
 // The CTA that finishes a sequence last moves its length and gives pages back.
+// The whole path is checked before anything moves; addresses are at hand for CC_PATH of its tokens at a time.
 constexpr int CC_PATH = 1024;
 __global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* seqs, const int* path, int path_stride,
                                                        const int* n_path, int sides) {
@@ -192,27 +193,35 @@ __global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* seqs,
     const int* pa = path + (long long)b * path_stride;
     if (!c.seq_ok(s)) { if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX); return; }
     const int len = c.length[s];
-    int bad = n < 0 || n > path_stride || n > CC_PATH ? SPECDEC_CACHE_BAD_INDEX : 0;
+    int bad = n < 0 || n > path_stride ? SPECDEC_CACHE_BAD_INDEX : 0;
     if (!bad)
         for (int j = threadIdx.x; j < n; j += blockDim.x) {
             const int x = pa[j];
             if (x < j || (j && pa[j - 1] >= x)) { bad = SPECDEC_CACHE_BAD_INDEX; break; }
-            from[j] = own_slot(c, s, len + x);
-            to[j] = own_slot(c, s, len + j);
-            if (from[j] < 0 || to[j] < 0) bad = SPECDEC_CACHE_UNRESERVED;
+            const long long f = own_slot(c, s, len + x), t = own_slot(c, s, len + j);
+            if (f < 0 || t < 0) bad = SPECDEC_CACHE_UNRESERVED;
+            if (j < CC_PATH) { from[j] = f; to[j] = t; }
         }
     const bool index = __syncthreads_or(bad & SPECDEC_CACHE_BAD_INDEX), slot = __syncthreads_or(bad & SPECDEC_CACHE_UNRESERVED);
     if (index || slot) { if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(c.status, index ? SPECDEC_CACHE_BAD_INDEX : SPECDEC_CACHE_UNRESERVED); return; }
     const int per = c.heads * c.chunks;
-    for (long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x; u < (long long)sides * per; u += (long long)gridDim.x * blockDim.x) {
-        const int side = (int)(u / per), r = (int)(u % per), h = c.heads == 1 ? 0 : r / c.chunks;
-        char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + h * c.s_head + (r - h * c.chunks) * 16;
-        for (int j0 = 0; j0 < n; j0 += 8) {
-            int4 x[8];
+    for (int n0 = 0; n0 < n; n0 += CC_PATH) {
+        const int m = min(n - n0, CC_PATH);
+        if (n0) {
+            __syncthreads();                              // the last ones' addresses have been used
+            for (int j = threadIdx.x; j < m; j += blockDim.x) { from[j] = own_slot(c, s, len + pa[n0 + j]); to[j] = own_slot(c, s, len + n0 + j); }
+            __syncthreads();
+        }
+        for (long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x; u < (long long)sides * per; u += (long long)gridDim.x * blockDim.x) {
+            const int side = (int)(u / per), r = (int)(u % per), h = c.heads == 1 ? 0 : r / c.chunks;
+            char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + h * c.s_head + (r - h * c.chunks) * 16;
+            for (int j0 = 0; j0 < m; j0 += 8) {
+                int4 x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) if (j0 + j < n) x[j] = ld16(base + from[j0 + j]);
+                for (int j = 0; j < 8; ++j) if (j0 + j < m) x[j] = ld16(base + from[j0 + j]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) if (j0 + j < n && from[j0 + j] != to[j0 + j]) st16(base + to[j0 + j], x[j]);
+                for (int j = 0; j < 8; ++j) if (j0 + j < m && from[j0 + j] != to[j0 + j]) st16(base + to[j0 + j], x[j]);
+            }
         }
     }
     __syncthreads();

@@ -105,6 +105,39 @@ def test_pages_random_walk(page, H, D, L, dtype, heads_first):
     assert refused, "the walk should meet a full pool"
 
 
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2049, 2600])
+def test_pages_long_paths(n):
+    """A prompt's tokens committed in one go, some left out: more than any tree has.  A path that goes wrong late moves nothing."""
+    from paper_2203_16487_b200 import tree
+    rng, T, page, H, D, L = np.random.default_rng(n), 2600, 16, 3, 24, 2
+    kv = torch.zeros(L, 2, 400, page, H, D, dtype=torch.float16, device="cuda")
+    cache = tree.PagedCache.over(kv, torch.full((2, 200), -1, dtype=torch.int32, device="cuda"), ints([0, 0]), ints([0, 0]), ints([0] * 400))
+    ref, seqs = R.Pages(kv.cpu(), 2, 200), [1, 0]
+    k, v = (torch.randn(L, 2, T + 5, H, D, device="cuda").half() for _ in "kv")
+    for c in (cache, ref):
+        c.reserve(ints(seqs) if c is cache else seqs, T + 5)
+    cache.append(ints(seqs), k[:, :, :5].contiguous(), v[:, :, :5].contiguous())
+    ref.append(seqs, k[:, :, :5].cpu(), v[:, :, :5].cpu(), range(L), [5, 5])
+    cache.compact(ints(seqs), ints([[0, 2]] * 2), ints([2, 2]))                # (blocks that begin inside a page)
+    ref.compact(seqs, [[0, 2]] * 2)
+    cache.reserve(ints(seqs), T)
+    ref.reserve(seqs, T)
+    cache.append(ints(seqs), k[:, :, 5:], v[:, :, 5:])
+    ref.append(seqs, k[:, :, 5:].cpu(), v[:, :, 5:].cpu(), range(L), [T, T])
+    paths = [sorted(rng.permutation(T)[:n].tolist()), list(range(n))]
+    before = kv.clone()
+    for at, to, status in ((n - 1, paths[0][n - 2], 4), (n - 1, T + 100, 8)):
+        bad = list(paths[0])
+        bad[at] = to
+        cache.compact(ints(seqs[:1]), ints([bad]), ints([n]))
+        assert int(cache.status.item()) == status and torch.equal(kv, before) and cache.length.tolist() == ref.length
+        cache.status.zero_()
+    cache.compact(ints(seqs), ints([p + [-1] * (T - n) for p in paths]), ints([n, n]))
+    ref.compact(seqs, paths)
+    cache.check()
+    same(cache, ref)
+
+
 def test_pages_refuse_what_is_wrong():
     from paper_2203_16487_b200 import binding, tree
     cache = tree.PagedCache(1, 2, 8, n_pages=4, n_seqs=3, max_pages=2, page_tokens=4)
