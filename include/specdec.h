@@ -273,7 +273,8 @@ typedef struct {
     float       scale;
     void       *d_workspace; long long workspace_bytes;   /* see below                                                   */
 } specdec_tree_attention_args;
-/* Bytes of workspace (0: none) that spread a call of these sizes over the GPU; 16-byte aligned, no state between calls.  With less, a call
+/* Bytes of workspace (0: none) that spread a call of these sizes over the GPU; 16-byte aligned, no state between calls.  max_length: what the call
+ * takes it to be (its own, or max_pages * page_tokens if that is smaller or its own is 0), or 0 for as much as any length needs.  With less, a call
  * returns SPECDEC_ERR_CAPACITY.  head_dim: multiples of 8 up to 128. */
 long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length);
 int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* a, void* stream);

@@ -471,7 +471,8 @@ long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv
         !op_elem_bytes(dtype) || page_tokens < 1 || max_length < 0)
         return op_bad("tree_attention_workspace", "sizes that tree_attention does not take");
     if (B == 0) return 0;
-    return workspace(plan(B, T, n_q_heads, n_kv_heads, dtype, head_dim, page_tokens, (long long)max_length + T), B, n_kv_heads, head_dim);
+    // Unknown lengths: the longest.  Sequences are cut into the more parts the longer they are, and never where they need not be cut however long they are.
+    return workspace(plan(B, T, n_q_heads, n_kv_heads, dtype, head_dim, page_tokens, (max_length ? max_length : 0x7fffffffLL) + T), B, n_kv_heads, head_dim);
 }
 
 int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* g, void* stream) {

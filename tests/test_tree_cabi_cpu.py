@@ -75,6 +75,26 @@ def test_tree_attention_refuses_caches_and_small_workspaces(lib):
     assert lib.specdec_tree_attention_workspace(0, 8, 4, 4, 64, 1, 16, 100) == 0
 
 
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_the_workspace_for_unknown_lengths_is_enough_for_any(lib, dtype):
+    """max_length = 0 is "unknown" to the size function as it is to the call."""
+    for B in (1, 2, 3, 7, 8, 37, 74, 128, 129):
+        for T in (1, 2, 3, 5, 9, 17, 64, 200, 1024):
+            for hq, hkv in ((8, 8), (32, 4), (4, 4), (37, 37), (296, 296)):
+                for dim, page in ((64, 16), (128, 64), (64, 4)):
+                    most = lib.specdec_tree_attention_workspace(B, T, hq, hkv, dim, dtype, page, 0)
+                    for n in (1, 64, 300, 1000, 3000, 10000, 100000, 2000000, 0x7fff0000 - 1):
+                        assert lib.specdec_tree_attention_workspace(B, T, hq, hkv, dim, dtype, page, n) <= most, (B, T, hq, hkv, dim, page, n)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="with a device the addresses would be used")
+def test_unknown_lengths_pass_both_halves(lib):
+    """A long cache, unknown lengths: what the size function says is what the call wants (it goes on to the launch, which fails without a device)."""
+    need = lib.specdec_tree_attention_workspace(2, 8, 4, 4, 64, 1, 1024, 0)
+    long = cache(page_tokens=1024, max_pages=64)
+    assert need > 0 and lib.specdec_tree_attention(long, attention(workspace_bytes=need, d_workspace=4096), None) == -5, said(lib)
+
+
 def test_trees_and_sample_refuse(lib):
     assert lib.specdec_tree_ancestors(None, None, 1, 8, 64, 64, None) == -1 and lib.specdec_tree_ancestors(64, None, 1, 8, None, None, None) == -1
     assert lib.specdec_tree_ancestors(64, None, 1, 0, 64, 64, None) == -1 and lib.specdec_tree_ancestors(64, None, 1, 1025, 64, 64, None) == -3
