@@ -22,6 +22,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -116,7 +117,7 @@ __device__ __forceinline__ u64 warp_scan(u64 v) {
 }
 
 struct Hist {
-    uint32_t cnt[SA_BINS], lo[SA_BINS + 32], hi[SA_BINS]; // entries; weight as two words (bins beyond the last: a lane each for what weighs nothing)
+    alignas(16) uint32_t cnt[SA_BINS]; uint32_t lo[SA_BINS + 32], hi[SA_BINS]; // entries; weight as two words (bins beyond the last: a lane each for what weighs nothing)
     template <int NT> __device__ __forceinline__ void clear() { for (int i = threadIdx.x; i < SA_BINS; i += NT) { cnt[i] = 0; lo[i] = 0; hi[i] = 0; } }
     __device__ __forceinline__ u64 sum(int b) const { return (u64)hi[b] << 32 | lo[b]; }
     __device__ __forceinline__ void add(int b, u64 u) {
@@ -312,7 +313,9 @@ __device__ void find_window(Shared<NT>& sh, const Group<C>& cta, float top_p) {
 }
 
 // The bin, in ascending order, that holds entry number k (from 1), or -1; every warp looks for itself.
-__device__ int bin_of_kth(const uint32_t* cnt, int k) {
+__device__ int bin_of_kth(const Hist& hist, int k) {
+    static_assert(alignof(Hist) % 16 == 0 && offsetof(Hist, cnt) == 0, "counts are read four at a time");
+    const uint32_t* cnt = hist.cnt;
     const int lane = threadIdx.x & 31;
     int before = 0;
     for (int i = 0; i < SA_BINS / 128; ++i) {
@@ -530,9 +533,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample(SampleArgs a) {
             const float depth = (bin + 0.5f) * (SA_RANGE / SA_BINS) / inv_t;
             return bin < 0 ? -INFINITY : row.top - depth - (fabsf(row.top) + depth) * 1e-6f;
         };
-        float bound = from_step(bin_of_kth(sh.h.cnt, k));
+        float bound = from_step(bin_of_kth(sh.h, k));
         if (C > 1) {                                      // k entries of one CTA, or k / C of each
-            const float share = from_step(bin_of_kth(sh.h.cnt, (k + C - 1) / C));
+            const float share = from_step(bin_of_kth(sh.h, (k + C - 1) / C));
             if (tid == 0) { sh.x_bound = bound; sh.x_share = share; }
             cta.sync();
             float least = INFINITY;
