@@ -237,6 +237,10 @@ template <> struct Half<__nv_bfloat16> {
         const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
+    static __device__ __forceinline__ float add(float s, uint32_t x) {          // s + both of x
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tadd.f32.bf16 %0, l, %0;\n\tadd.f32.bf16 %0, h, %0;\n\t}" : "+f"(s) : "r"(x));
+        return s;
+    }
 };
 template <> struct Half<__half> {
     static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -247,11 +251,16 @@ template <> struct Half<__half> {
         const __half2 h = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
+    static __device__ __forceinline__ float add(float s, uint32_t x) {
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tadd.f32.f16 %0, l, %0;\n\tadd.f32.f16 %0, h, %0;\n\t}" : "+f"(s) : "r"(x));
+        return s;
+    }
 };
 
 
 // Sixteen query rows of a warp over blocks of 64 keys: lane l holds rows l / 4 and l / 4 + 8.  Running maximum m and sum l of 2^(s - m), output o; scores
-// in units of log2.  kf(row, piece) / vf(row, piece): shared-memory address of 16-byte piece `piece` of a key's row.
+// in units of log2.  The second product takes the probabilities as 16-bit numbers, and the sum adds up those: the weights add up to 1, so that their rounding moves
+// the output by its share of the values' spread, not of their size, and a dominating key's cancels (sums of the unrounded ones take as long, within 1 %).  kf(row, piece) / vf(row, piece): shared-memory address of 16-byte piece `piece` of a key's row.
 template <typename T, int DP>
 struct TaRows {
     static constexpr int NK = TA_BLOCK / 8, ND = DP / 8;
@@ -313,9 +322,9 @@ struct TaRows {
                 float* c = sc[2 * n + e];
                 c[0] = ta_exp2(fmaf(c[0], scale, -za)); c[1] = ta_exp2(fmaf(c[1], scale, -za));
                 c[2] = ta_exp2(fmaf(c[2], scale, -zb)); c[3] = ta_exp2(fmaf(c[3], scale, -zb));
-                la += c[0] + c[1]; lb += c[2] + c[3];
                 pf[2 * e] = Half<T>::pack(c[0], c[1]);
                 pf[2 * e + 1] = Half<T>::pack(c[2], c[3]);
+                la = Half<T>::add(la, pf[2 * e]); lb = Half<T>::add(lb, pf[2 * e + 1]);
             }
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {

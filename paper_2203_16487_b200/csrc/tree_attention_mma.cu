@@ -2,7 +2,7 @@
 //
 // CTA = WM x WK consumer warps and one that loads.  A block of 64 keys is a stage of a ring: one TMA box a page, keys and values each in column halves of
 // 128 swizzled bytes a row.  Warp (wm, wk) takes 16 rows and every WK-th block: scores (m16n8k16, fp32), running maximum and sum in registers, probabilities (rounded
-// to the type; the sum keeps the unrounded ones) straight from the score registers into the second product.  The WK groups' partial outputs
+// to the type, as mma.sync takes them; the sum adds up the rounded ones) straight from the score registers into the second product.  The WK groups' partial outputs
 // meet in shared memory at the end.
 //
 // Few rows: HBM bounds it, so what counts is bytes in flight (a ring of NS stages of 16 or 32 KB an SM) and that nothing but the boxes' addresses passes through

@@ -1,8 +1,8 @@
 // Attention of drafted trees over the paged cache for 16-bit types and many query rows: tcgen05 (contract: specdec.h, work: tree_attention.cuh).
 //
 // One CTA an SM.  A block is 128 keys; the scores of 128 rows against it are one accumulator in tensor memory (a row a lane), which the row's thread takes into
-// registers for maximum and exponentials; the probabilities go back into the same columns as 16-bit pairs and are the second product's A operand, the
-// values its B operand as they lie ([key, column], N-major).  Two groups of four softmax warps keep the tensor pipe busy in turn:
+// registers for maximum and exponentials; the probabilities go back into the same columns as 16-bit pairs and are the second product's A operand
+// (of B's type, as tcgen05.mma wants it; the sum adds up the rounded ones), the values its B operand as they lie ([key, column], N-major).  Two groups of four softmax warps keep the tensor pipe busy in turn:
 //   TILES = 2: the groups have 128 rows each and share the blocks of a 256-row tile.
 //   TILES = 1: the groups have the same 128 rows and take every second block; their results meet at the end.
 // Warps: 0 loads (one TMA box a page), 1 issues the products, 4-7 and 8-11 are the groups.
@@ -15,7 +15,7 @@
 // lower clocks.  (A quarter of the exponentials as polynomials on the fused multiply-adds: 130 us; it is the chain, not their rate.)
 //
 // The running maximum is only moved (and the output, in tensor memory, rescaled) when it grows by more than 2^8: until then probabilities up to 2^8 are relative to
-// the old one, which changes neither the quotient nor its relative precision.
+// the old one, which changes neither the quotient nor its relative precision: a dominating one is not exactly 1 any more, but its rounding is in the sum as well.
 #include <type_traits>
 
 #include "tree_attention.cuh"
@@ -57,11 +57,6 @@ __device__ __forceinline__ uint64_t pair2(float lo, float hi) {
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -303,7 +298,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                 }
             }
             const float z = m == -INFINITY ? 0.f : m;
-            uint64_t sum[2] = {0, 0};                     // two pairs of fp32
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};          // of the rounded probabilities
             const uint64_t scale2 = pair2(a.scale, a.scale), z2 = pair2(-z, -z);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
@@ -314,8 +309,8 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                     for (int e = 0; e < 16; ++e) {
                         const uint64_t d = fma2(pair2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale2, z2);
                         const float u = ta_exp2(__uint_as_float((uint32_t)d)), v = ta_exp2(__uint_as_float((uint32_t)(d >> 32)));
-                        sum[e & 1] = add2(sum[e & 1], pair2(u, v));
                         y[e] = Half<T>::pack(u, v);
+                        sum[e & 3] = Half<T>::add(sum[e & 3], y[e]);
                     }
                     tmem_st16(ts + c * 16, y);
                 }
@@ -324,8 +319,7 @@ __global__ void __launch_bounds__(32 * TC_WARPS, 1) k_ta_tc(const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pready + g * 16 + hf * 8);
             }
-            const uint64_t both = add2(sum[0], sum[1]);
-            l += __uint_as_float((uint32_t)both) + __uint_as_float((uint32_t)(both >> 32));
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         if (ok && n) ok = wait(ofin + g * 8, outputs++);
         taken += n;

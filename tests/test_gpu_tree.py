@@ -321,6 +321,44 @@ def test_attention_masks(dtype):
     assert (got[0, ::3] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,H,Hkv,D,page", [(1, 4, 4, 64, 16), (1, 16, 2, 128, 16), (20, 2, 2, 128, 16), (13, 4, 2, 64, 16), (50, 2, 2, 64, 16), (26, 4, 2, 64, 4), (9, 4, 2, 128, 2),
+                                            (50, 4, 2, 128, 16), (100, 2, 2, 64, 32), (200, 4, 2, 128, 64), (70, 8, 2, 64, 16)])
+def test_attention_weights_add_up_to_one(dtype, T, H, Hkv, D, page):
+    """Values that lie around 8, peaked weights.  With weights w_j (1 + e_j) / sum_i w_i (1 + e_i), |e| <= u by the probabilities' rounding, the result is off by at most
+    u / (1 - u) sum_j w_j |v_j - o|: by the spread of the values around the result, not by their size.  Then the output's rounding, u |o|, and fp32's."""
+    from paper_2203_16487_b200 import tree
+    g, lens = torch.Generator().manual_seed(T + D), [0, 40, 200, 1500]
+    B, S = len(lens), max(lens)
+    k, v = torch.randn(1, B, S + T, Hkv, D, generator=g).to(dtype), (8 + torch.randn(1, B, S + T, Hkv, D, generator=g) / 2).to(dtype)
+    q = (torch.randn(B, T, H, D, generator=g) * 3).to(dtype)
+    pages = -(-(S + T) // page)
+    cache = tree.PagedCache(1, Hkv, D, n_pages=B * pages, n_seqs=B, max_pages=pages, page_tokens=page, dtype=dtype)
+    seqs, n = ints(list(range(B))), ints(lens)
+    cache.reserve(seqs, S)
+    cache.append(seqs, k[:, :, :S].cuda(), v[:, :, :S].cuda(), count=n)
+    cache.compact(seqs, torch.arange(S, dtype=torch.int32, device="cuda").expand(B, -1).contiguous(), n)
+    cache.reserve(seqs, T)
+    cache.append(seqs, k[:, :, S:].cuda(), v[:, :, S:].cuda())
+    see, _ = R.ancestors(random_parents(np.random.default_rng(T), 1, T), [T])
+    got = tree.attention(q.cuda(), cache, 0, seqs, R.pack(see, T).cuda()).double().cpu()
+    cache.check()
+    u = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -11
+    for b, m in enumerate(lens):
+        sees = torch.zeros(T, m + T, dtype=torch.bool)
+        sees[:, :m] = True
+        for t in range(T):
+            sees[t, [m + j for j in see[0][t]]] = True
+        kk, vv = (torch.cat([x[0, b, :m], x[0, b, S:]]).double().repeat_interleave(H // Hkv, 1).transpose(0, 1) for x in (k, v))      # [H, S, D]
+        w = torch.softmax((q[b].double().transpose(0, 1) @ kk.transpose(1, 2) * D ** -0.5).masked_fill(~sees, -math.inf), -1)
+        o = w @ vv
+        spread = torch.stack([(w[:, t, :, None] * (vv - o[:, t, None]).abs()).sum(1) for t in range(T)], 1)
+        small = (m + T) * 2.0 ** -25 * 8 if dtype == torch.float16 else 0                                     # (probabilities below fp16's normal numbers)
+        tol = u * o.abs() + u / (1 - u) * spread + 1e-5 * o.abs() + small
+        off = (got[b].transpose(0, 1) - o).abs() - tol
+        assert (off <= 0).all(), (m, float(off.max()), float((off > 0).double().mean()))
+
+
 def test_attention_grows_along_the_keys():
     """Scores that rise block by block, by more than a type's range at once: the running maximum is rescaled every time."""
     from paper_2203_16487_b200 import tree
