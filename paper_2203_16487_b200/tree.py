@@ -11,6 +11,8 @@ passes on, and raises when the gradient is asked for.
     sampled, logprob = tree.sample(logits, uniform, temperature, top_k, top_p, min_p)
     path, n_path, emitted = tree.accept(parents, tokens, sampled)
     cache.compact(seqs, path, n_path)                        # the accepted nodes are committed tokens now
+
+Lengths and pages are read on the device, so a step may be captured in a CUDA graph and replayed as the sequences grow (without max_length, which a graph would keep).
 """
 from __future__ import annotations
 

@@ -651,6 +651,54 @@ def test_tree_decoding_is_sampling_token_by_token(batch, prompt, tokens):
     assert same == 1.0 and steps == tokens and fewer < steps
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_step_in_a_graph(dtype):
+    """One step's calls, captured once and replayed while the sequences grow: bit for bit what calling them gives."""
+    from paper_2203_16487_b200 import tree
+    g = torch.Generator(device="cuda").manual_seed(6)
+    L, B, T, H, Hkv, D, V, steps = 3, 5, 9, 8, 2, 64, 300, 12
+    parents = ints(random_parents(np.random.default_rng(6), B, T))
+    def new(*s):
+        return torch.randn(*s, generator=g, device="cuda")
+    steps = [dict(k=new(L, B, T, Hkv, D).to(dtype), v=new(L, B, T, Hkv, D).to(dtype), q=new(L, B, T, H, D).to(dtype), logits=new(B, T, V) * 3, u=torch.rand(B, T, generator=g, device="cuda"),
+                  tokens=torch.randint(0, V, (B, T), generator=g, device="cuda").int()) for _ in range(steps)]
+    seqs, k = ints([3, 0, 5, 1, 4]), torch.full((B,), 3, dtype=torch.int32, device="cuda")
+    def call(cache, x):
+        mask, depth = tree.ancestors(parents)
+        cache.reserve(seqs, T)
+        outs = [mask, depth]
+        for layer in range(L):
+            cache.append(seqs, x["k"][layer], x["v"][layer], layer=layer)
+            outs.append(tree.attention(x["q"][layer], cache, layer, seqs, mask))
+        outs += tree.sample(x["logits"], x["u"], top_k=k)
+        outs += tree.accept(parents, x["tokens"], outs[-2])
+        cache.compact(seqs, outs[-3], outs[-2])
+        return outs
+    for x in steps:                                            # drafts that the samples often follow
+        sampled, _ = tree.sample(x["logits"], x["u"], top_k=k)
+        x["tokens"][:, 1:] = sampled.gather(1, parents[:, 1:].long())
+    caches = [tree.PagedCache(L, Hkv, D, n_pages=60, n_seqs=6, max_pages=10, page_tokens=16, dtype=dtype) for _ in range(2)]
+    at, warm = {n: t.clone() for n, t in steps[0].items()}, tree.PagedCache(L, Hkv, D, n_pages=60, n_seqs=6, max_pages=10, page_tokens=16, dtype=dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(warm, at)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        replayed = call(caches[0], at)
+    for x in steps:
+        for n, t in x.items():
+            at[n].copy_(t)
+        graph.replay()
+        for a, b in zip(replayed, call(caches[1], x)):
+            assert torch.equal(a, b)
+    for c in caches:
+        c.check()
+    assert torch.equal(caches[0].length, caches[1].length) and torch.equal(caches[0].kv, caches[1].kv) and torch.equal(caches[0].table, caches[1].table)
+    assert int(caches[0].length.max()) > 2 * len(steps)
+
+
 def test_branches_of_a_prompt():
     """Forked sequences continue a shared prompt each its own way, as sequences that hold copies of it would."""
     from paper_2203_16487_b200 import tree
