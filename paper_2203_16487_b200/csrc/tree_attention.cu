@@ -11,7 +11,7 @@ namespace {
 // ------------------------------------------------------------------ 16-bit types, pages of fewer than TA_MIN_PAGE tokens
 // Such pages are no TMA boxes: every thread fetches 16-byte pieces (cp.async).  4 warps of 16 rows, a ring of NS blocks of 64 keys, rows of
 // DP elements whose 16-byte pieces are XORed with the row's low three bits.  Every piece is an instruction, a wait and an address of its own, which is what bounds it:
-// 128 x 51 queries over 51 to 307 keys in pages of 4 tokens 42 us (by boxes, pages of 16: 28), 8 x 1 query over 8000 keys 63 (34).
+// 128 x 51 queries over 51 to 307 keys in pages of 4 tokens 42 us (by boxes, pages of 16: 28), 8 x 1 query over 8000 keys 63 (34; a tile is 64 rows here however few are real).
 template <typename T, int DP, int NS>
 __global__ void __launch_bounds__(128) k_ta_small_pages(TreeAttn a) {
     constexpr int ROWS = 64, KT = TA_BLOCK, PITCH = DP * 2, PIECES = DP / 8, STAGE = 2 * KT * PITCH;
@@ -397,7 +397,8 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
                : p.rows == 4 ? (whole * blocks >= 4 * TA_SMS ? 4 : 2) : p.rows == 8 || whole > TA_SMS ? 2 : 1;
     const int at_once = TA_SMS * p.per_sm;
     // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge, which costs about as much as eight
-    // blocks.
+    // blocks of 64 keys (of 128 with tcgen05 some four: there fewer sequences are cut than might be).  The longest is what max_length says: 128 x 51 queries over 51 to 307
+    // keys take 27 us with it, 41 where it is unknown and the table twice as wide.
     p.direct = (whole + at_once - 1) / at_once * blocks <= whole * blocks / at_once + 8 || B > TA_MAX_B;
     if (p.direct && whole > at_once && 2 * columns <= at_once && B <= TA_MAX_B && p.rows >= 64 && blocks >= 4) p.direct = 2;    // (128 x 51 queries over 51 to 307 keys 29.5 -> 27.9 us; few rows or keys lose 2)
     p.ctas = (int)(at_once / columns < 1 ? 1 : at_once / columns);

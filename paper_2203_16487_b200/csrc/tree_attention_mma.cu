@@ -7,9 +7,9 @@
 //
 // Few rows: HBM bounds it, so what counts is bytes in flight (a ring of NS stages of 16 or 32 KB an SM) and that nothing but the boxes' addresses passes through
 // registers on the way.  A box needs its page number: the loading warp's lanes read a block's numbers together.  2 x 1 query, 32/8 heads of 128, over 65,537 to
-// 131,071 keys: 150 us with the merge, 6.5 TB/s; 8 x 1 query, 8 heads of 64, over 8000 in pages of 16: 34 us, 3.8 TB/s, of which start and merge are some 14.
+// 131,071 keys: 150 us with the merge, 6.5 TB/s; 8 x 1 query, 8 heads of 64, over 8000 in pages of 16: 34 us (both in a graph), 3.8 TB/s, of which start and merge are some 14.
 // 64 rows over short sequences: the chain of a warp bounds it (scores, maximum, exponentials, second product: some 3000 clocks a block, 5500 more a sequence and head),
-// of which 3 CTAs an SM overlap.  128 x 51 queries, 8 heads of 64, over 51 to 307 keys: 28 us, 55 TFLOP/s.  (Four CTAs need 96 registers a thread, which spills
+// of which 3 CTAs an SM overlap.  128 x 51 queries, 8 heads of 64, over 51 to 307 keys: 28 us in a graph, 55 TFLOP/s; 29.4 as a call among others.  (Four CTAs need 96 registers a thread, which spills
 // 700 bytes; two CTAs of eight computing warps the same, 39 us.)
 #include "tree_attention.cuh"
 

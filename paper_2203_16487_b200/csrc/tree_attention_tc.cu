@@ -11,7 +11,7 @@
 // exponentials), and its scores' columns are taken by the probabilities until that is done.  Blocks of 64 keys leave room for both, so that
 // the next scores can be under way meanwhile, but each issue of products costs some 200 clocks beside their own: 256 rows took 5760 clocks for 128 keys instead of 3700.
 //
-// 8 x 64 queries, 32/8 heads of 128, over 8191 to 16,385 keys: 122 us with the merge (8 us) in a burst, 861 TFLOP/s, the tensor pipe 50 % active; 145 us back to back, at
+// 8 x 64 queries, 32/8 heads of 128, over 8191 to 16,385 keys: 121 us with the merge (8 us) in a burst, 866 TFLOP/s, the tensor pipe 50 % active; 145 us as a call among others, at
 // lower clocks.  (A quarter of the exponentials as polynomials on the fused multiply-adds: 130 us; it is the chain, not their rate.)
 //
 // The running maximum is only moved (and the output, in tensor memory, rescaled) when it grows by more than 2^8: until then probabilities up to 2^8 are relative to
