@@ -50,6 +50,7 @@ extern "C" {
 #define SPECDEC_DTYPE_F32   0
 #define SPECDEC_DTYPE_BF16  1
 #define SPECDEC_DTYPE_F16   2      /* operators on the caller's tensors only: handles take the first two */
+#define SPECDEC_DTYPE_FP4   3      /* specdec_packed_cache only */
 
 #define SPECDEC_ACT_RELU    0
 #define SPECDEC_ACT_GELU    1
@@ -235,7 +236,11 @@ long long specdec_cache_scratch(int n_seqs, int max_pages, int n_pages);
  *   whose path does not is skipped (BAD_INDEX).
  * release: gives a sequence's pages back; its length is 0.
  * fork: sequence d_dst[i] becomes a copy of d_src[i] as that was before the call (so a permutation reorders beams), its old pages are
- *   given back.  Full pages are shared, the last, partly filled one is copied.  d_dst all different; a pair of equal numbers does nothing. */
+ *   given back.  Full pages are shared, the last, partly filled one is copied.  d_dst all different; a pair of equal numbers does nothing.
+ * reorder: the n sequences are beams, in groups of `beams` that follow one another.  Sequence i of a group becomes what sequence d_parents[i] (0 .. beams - 1; -1: none, it
+ *   is released) of the group was before the call.  Full pages are shared; the last, partly filled one goes on with one child (the parent itself if it is one, else the first) and is
+ *   copied for the others, so that a permutation moves no data.  Pages that nobody holds any more are free, for the copies of this call too; they are given to the entries
+ *   that copy in their order.  Pages behind the committed tokens are given back.  Any other parent, or one whose sequence number is out of range: the entry is its own (BAD_INDEX). */
 int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream);
 int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int T,
                          long long stride_layer, long long stride_seq, long long stride_token, long long stride_head,
@@ -244,6 +249,7 @@ int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, 
                           const int32_t* d_n_path, void* stream);
 int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, void* stream);
 int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream);
+int specdec_cache_reorder(const specdec_cache* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream);
 
 /* Trees of up to 1024 nodes.  d_n_nodes [B] (or NULL: T each) cuts a tree short.
  * ancestors: bit j of d_mask [B, T, ceil(T / 32)] row i is set iff node j is node i or one of its ancestors; d_depth [B, T] is the
@@ -278,6 +284,36 @@ typedef struct {
  * returns SPECDEC_ERR_CAPACITY.  head_dim: multiples of 8 up to 128. */
 long long specdec_tree_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length);
 int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_args* a, void* stream);
+
+/* A cache in 4 bits.  Sixteen channels of a token and head share a scale s, an 8-bit float (e4m3: 4 bits of exponent, 3 of fraction); a channel is a code of 0, 0.5, 1, 1.5, 2, 3, 4, 6 or
+ * their negatives (e2m1; number 0 .. 7, + 8 for the sign), and stands for unit * s * code.  unit: d_unit [n_layers, 2, n_heads] fp32, positive and finite, or NULL: 1.  What is
+ * written is, with x' = x / unit in fp32, s = the scale nearest to max |x'| / 6 (at most 448), code = the one nearest to x' / s, halfway the even number (beyond 6: 6; s = 0: 0).  A NaN makes its
+ * block NaN.
+ *   codes:    a specdec_cache of dtype SPECDEC_DTYPE_FP4 whose strides count bytes: channel 2 i of a token and head is in the low half of byte i of head_dim / 2; the tokens of a page
+ *             and head follow one another (stride_token does not matter).  head_dim is 64 or 128, page_tokens a power of two from 16 on.
+ *   d_scales: head_dim / 16 bytes a token and head, tokens of a page and head behind one another, with strides of their own (bytes).
+ * Addresses and strides of both are multiples of 16 bytes.  Everything else, and the calls of the same names, are as above; they move codes and scales as they are.
+ * append, read: d_k, d_v [n_layers, n, T, n_heads, head_dim] of `dtype` (fp32, bf16, fp16), strides in elements.  read: the values of tokens d_start[i] + t (NULL: d_length + t, the
+ *   block behind the committed tokens), rounded to dtype once; zeros where the sequence has no page.  It takes sequences more than once. */
+typedef struct {
+    specdec_cache codes;
+    void*         d_scales;
+    long long     scale_stride_layer, scale_stride_side, scale_stride_page, scale_stride_head;
+    const float*  d_unit;
+} specdec_packed_cache;
+int specdec_packed_cache_reserve(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream);
+int specdec_packed_cache_append(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int dtype, int T,
+                             long long stride_layer, long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_count, void* stream);
+int specdec_packed_cache_read(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, void* d_k, void* d_v, int dtype, int T,
+                           long long stride_layer, long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_start, void* stream);
+int specdec_packed_cache_compact(const specdec_packed_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride, const int32_t* d_n_path, void* stream);
+int specdec_packed_cache_release(const specdec_packed_cache* c, const int32_t* d_seqs, int n, void* stream);
+int specdec_packed_cache_fork(const specdec_packed_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream);
+int specdec_packed_cache_reorder(const specdec_packed_cache* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream);
+/* tree_attention over it: q and out are of `dtype` (fp32, bf16, fp16); the rest as there.  Products with the exact values, scores and sums in fp32; bf16 and fp32 queries are taken with a row's
+ * largest number moved below 2^15 by a power of two, as fp16 (fp32: two of them, 22 bits), probabilities as fp16 (fp32: two). */
+long long specdec_packed_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length);
+int specdec_packed_attention(const specdec_packed_cache* c, const specdec_tree_attention_args* a, int dtype, void* stream);
 
 /* One token per row of d_logits [rows, V] (row r at r * stride; V contiguous) from a given uniform random number in [0, 1).
  * With l = fp32 logits (NaN: never taken) and m their maximum, w_i = floor(2^40 exp((l_i - m) / T)) 2^-40: weights are whole numbers of

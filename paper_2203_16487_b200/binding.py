@@ -28,7 +28,9 @@ EXPORTS = [
     "specdec_debug_integrity", "specdec_debug_mma_rate_bg",
     "specdec_cache_scratch", "specdec_cache_reserve", "specdec_cache_append", "specdec_cache_compact", "specdec_cache_release",
     "specdec_cache_fork", "specdec_tree_ancestors", "specdec_tree_accept", "specdec_tree_attention_workspace",
-    "specdec_tree_attention", "specdec_sample",
+    "specdec_tree_attention", "specdec_sample", "specdec_cache_reorder",
+    "specdec_packed_cache_reserve", "specdec_packed_cache_append", "specdec_packed_cache_read", "specdec_packed_cache_compact", "specdec_packed_cache_release",
+    "specdec_packed_cache_fork", "specdec_packed_cache_reorder", "specdec_packed_attention_workspace", "specdec_packed_attention",
 ]
 
 
@@ -58,6 +60,11 @@ class Cache(C.Structure):
         "dtype", "n_layers", "n_heads", "head_dim", "n_pages", "page_tokens", "n_seqs", "max_pages")] + [
         (n, C.c_longlong) for n in ("stride_layer", "stride_side", "stride_page", "stride_token", "stride_head")] + [
         (n, C.c_void_p) for n in ("d_table", "d_length", "d_held", "d_refs", "d_status", "d_scratch")]
+
+
+class Fp4Cache(C.Structure):
+    _fields_ = [("codes", Cache), ("d_scales", C.c_void_p)] + [(n, C.c_longlong) for n in (
+        "scale_stride_layer", "scale_stride_side", "scale_stride_page", "scale_stride_head")] + [("d_unit", C.c_void_p)]
 
 
 class TreeAttentionArgs(C.Structure):
@@ -120,6 +127,13 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.specdec_cache_compact.argtypes = [cp, ip, i, ip, i, ip, vp]
     lib.specdec_cache_release.argtypes = [cp, ip, i, vp]
     lib.specdec_cache_fork.argtypes = [cp, ip, ip, i, vp]
+    lib.specdec_cache_reorder.argtypes = [cp, ip, ip, i, i, vp]
+    fp = C.POINTER(Fp4Cache)
+    for name in ("reserve", "compact", "release", "fork", "reorder"):
+        getattr(lib, "specdec_packed_cache_" + name).argtypes = [fp] + getattr(lib, "specdec_cache_" + name).argtypes[1:]
+    lib.specdec_packed_cache_append.argtypes = lib.specdec_packed_cache_read.argtypes = [fp, ip, i, i, i, vp, vp, i, i, L, L, L, L, ip, vp]
+    lib.specdec_packed_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
+    lib.specdec_packed_attention.argtypes = [fp, vp, i, vp]
     lib.specdec_tree_ancestors.argtypes = [ip, ip, i, i, vp, ip, vp]
     lib.specdec_tree_accept.argtypes = [ip, ip, ip, ip, i, i, ip, ip, ip, vp]
     lib.specdec_tree_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
@@ -128,7 +142,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     for name in EXPORTS:
         if name not in ("specdec_launch_count", "specdec_last_error"):
             getattr(lib, name).restype = i
-    lib.specdec_cache_scratch.restype = lib.specdec_tree_attention_workspace.restype = L
+    lib.specdec_cache_scratch.restype = lib.specdec_tree_attention_workspace.restype = lib.specdec_packed_attention_workspace.restype = L
     return lib
 
 

@@ -1,4 +1,4 @@
-// Pages of a K/V cache in the caller's memory: reserve, append, compact, release, fork (contract: specdec.h).
+// Pages of a K/V cache in the caller's memory, of 16- or 32-bit elements or of 4-bit codes and their scales: reserve, append, compact, release, fork, reorder (contract: specdec.h).
 //
 // Bookkeeping is a table of pages a sequence and a reference count a page; a free page is one whose count is 0, and the lowest free ones
 // are given out first, so that no call's result depends on the order in which CTAs run: reference counts are sums of integers, and everything
@@ -10,6 +10,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "fp4.cuh"
 #include "op_error.cuh"
 
 namespace sd {
@@ -23,17 +24,22 @@ struct Cache {                                            // specdec_cache with 
     long long s_layer, s_side, s_page, s_token, s_head;
     int n_pages, n_seqs, max_pages, page_shift;
     int heads, chunks;                                    // a token's row: heads (1 where they are contiguous) x chunks
+    char* sc;                                             // 4 bits: the scales, strides in bytes, a token and head's in 4-byte pieces
+    long long c_layer, c_side, c_page, c_token, c_head;
+    int c_heads, c_chunks;
     __device__ __forceinline__ bool seq_ok(int s) const { return (unsigned)s < (unsigned)n_seqs; }
     __device__ __forceinline__ bool page_ok(int p) const { return (unsigned)p < (unsigned)n_pages; }
     __device__ __forceinline__ int held_of(int s) const { return min(max(held[s], 0), max_pages); }
     // scratch: [0] whether the call got its pages, then per entry of the call the rank of its first new page, [n_pages] the pages given
-    // out, per sequence the tickets of compact; fork: per pair source page / tokens / length, and the sources' tables
+    // out, per sequence the tickets of compact; fork, reorder: per pair length and whether its last page is copied (or goes on), and the sources' tables; reorder: the entries
+    // that copy
     __device__ __forceinline__ int* sc_ok() const { return scratch; }
     __device__ __forceinline__ int* sc_first() const { return scratch + 16; }
     __device__ __forceinline__ int* sc_pages() const { return scratch + 16 + n_seqs; }
     __device__ __forceinline__ int* sc_ticket() const { return scratch + 16 + n_seqs + n_pages; }
     __device__ __forceinline__ int* sc_pair() const { return scratch + 16 + 2 * n_seqs + n_pages; }
-    __device__ __forceinline__ int* sc_rows() const { return scratch + 16 + 4 * n_seqs + n_pages; }
+    __device__ __forceinline__ int* sc_jobs() const { return scratch + 16 + 4 * n_seqs + n_pages; }
+    __device__ __forceinline__ int* sc_rows() const { return scratch + 16 + 5 * n_seqs + n_pages; }
 };
 
 __device__ __forceinline__ int4 ld16(const char* p) { return *reinterpret_cast<const int4*>(p); }
@@ -144,14 +150,19 @@ __global__ void k_cache_release(Cache c, const int* seqs) {
     if (threadIdx.x == 0) { c.held[s] = 0; c.length[s] = 0; }
 }
 
-// Where slot `pos` of sequence s is (bytes from the side's begin), or -1 where that is no page of the sequence's own.
+// Where slot `pos` of sequence s is, or -1 where that is no page of the sequence's own: bytes from the side's begin, or (FP4) the slot's number among all pages' slots.
+template <bool FP4 = false>
 __device__ __forceinline__ long long own_slot(const Cache& c, int s, int pos) {
     const int i = pos >> c.page_shift;
     if (pos < 0 || i >= c.held_of(s)) return -1;
     const int p = c.table[(long long)s * c.max_pages + i];
     if (!c.page_ok(p) || c.refs[p] != 1) return -1;
-    return p * c.s_page + (pos & ((1 << c.page_shift) - 1)) * c.s_token;
+    const int t = pos & ((1 << c.page_shift) - 1);
+    return FP4 ? ((long long)p << c.page_shift) + t : p * c.s_page + t * c.s_token;
 }
+// Bytes from a side's begin to slot `slot` of the codes, and of the scales.
+__device__ __forceinline__ long long code_at(const Cache& c, long long slot) { return (slot >> c.page_shift) * c.s_page + (slot & ((1 << c.page_shift) - 1)) * c.s_token; }
+__device__ __forceinline__ long long scale_at(const Cache& c, long long slot) { return (slot >> c.page_shift) * c.c_page + (slot & ((1 << c.page_shift) - 1)) * c.c_token; }
 
 struct AppendArgs {
     const char* k; const char* v;
@@ -184,6 +195,7 @@ __global__ void k_cache_append(Cache c, AppendArgs a) {
 // The CTA that finishes a sequence last moves its length and gives pages back.
 // The whole path is checked before anything moves; addresses are at hand for CC_PATH of its tokens at a time.
 constexpr int CC_PATH = 1024;
+template <bool FP4>
 __global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* seqs, const int* path, int path_stride,
                                                        const int* n_path, int sides) {
     __shared__ long long from[CC_PATH], to[CC_PATH];
@@ -198,30 +210,38 @@ __global__ void __launch_bounds__(128) k_cache_compact(Cache c, const int* seqs,
         for (int j = threadIdx.x; j < n; j += blockDim.x) {
             const int x = pa[j];
             if (x < j || (j && pa[j - 1] >= x)) { bad = SPECDEC_CACHE_BAD_INDEX; break; }
-            const long long f = own_slot(c, s, len + x), t = own_slot(c, s, len + j);
+            const long long f = own_slot<FP4>(c, s, len + x), t = own_slot<FP4>(c, s, len + j);
             if (f < 0 || t < 0) bad = SPECDEC_CACHE_UNRESERVED;
             if (j < CC_PATH) { from[j] = f; to[j] = t; }
         }
     const bool index = __syncthreads_or(bad & SPECDEC_CACHE_BAD_INDEX), slot = __syncthreads_or(bad & SPECDEC_CACHE_UNRESERVED);
     if (index || slot) { if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(c.status, index ? SPECDEC_CACHE_BAD_INDEX : SPECDEC_CACHE_UNRESERVED); return; }
-    const int per = c.heads * c.chunks;
+    const int codes = c.heads * c.chunks, per = codes + (FP4 ? c.c_heads * c.c_chunks : 0);
     for (int n0 = 0; n0 < n; n0 += CC_PATH) {
         const int m = min(n - n0, CC_PATH);
         if (n0) {
             __syncthreads();                              // the last ones' addresses have been used
-            for (int j = threadIdx.x; j < m; j += blockDim.x) { from[j] = own_slot(c, s, len + pa[n0 + j]); to[j] = own_slot(c, s, len + n0 + j); }
+            for (int j = threadIdx.x; j < m; j += blockDim.x) { from[j] = own_slot<FP4>(c, s, len + pa[n0 + j]); to[j] = own_slot<FP4>(c, s, len + n0 + j); }
             __syncthreads();
         }
-        for (long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x; u < (long long)sides * per; u += (long long)gridDim.x * blockDim.x) {
-            const int side = (int)(u / per), r = (int)(u % per), h = c.heads == 1 ? 0 : r / c.chunks;
-            char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + h * c.s_head + (r - h * c.chunks) * 16;
+        auto move = [&](auto piece, char* base, auto at) {
             for (int j0 = 0; j0 < m; j0 += 8) {
-                int4 x[8];
+                decltype(piece) x[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) if (j0 + j < m) x[j] = ld16(base + from[j0 + j]);
+                for (int j = 0; j < 8; ++j) if (j0 + j < m) x[j] = *reinterpret_cast<const decltype(piece)*>(base + at(from[j0 + j]));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) if (j0 + j < m && from[j0 + j] != to[j0 + j]) st16(base + to[j0 + j], x[j]);
+                for (int j = 0; j < 8; ++j) if (j0 + j < m && from[j0 + j] != to[j0 + j]) *reinterpret_cast<decltype(piece)*>(base + at(to[j0 + j])) = x[j];
             }
+        };
+        for (long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x; u < (long long)sides * per; u += (long long)gridDim.x * blockDim.x) {
+            const int side = (int)(u / per), r = (int)(u % per);
+            if (FP4 && r >= codes) {                      // a piece of the scales
+                const int x = r - codes, h = x / c.c_chunks;
+                move(0, c.sc + (side >> 1) * c.c_layer + (side & 1) * c.c_side + h * c.c_head + (x - h * c.c_chunks) * 4, [&](long long slot) { return scale_at(c, slot); });
+                continue;
+            }
+            const int h = c.heads == 1 ? 0 : r / c.chunks;
+            move(int4(), c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + h * c.s_head + (r - h * c.chunks) * 16, [&](long long slot) { return FP4 ? code_at(c, slot) : slot; });
         }
     }
     __syncthreads();
@@ -283,9 +303,42 @@ __global__ void __launch_bounds__(CP_ALLOC_THREADS) k_fork_take(Cache c, const i
     if (ok) for (int r = threadIdx.x; r < run; r += CP_ALLOC_THREADS) c.refs[c.sc_pages()[r]] = 1;
     if (threadIdx.x == 0) { *c.sc_ok() = ok; if (!ok) atomicOr(c.status, SPECDEC_CACHE_NO_PAGES); }
 }
+
+// A page's share of a copy, by a CTA of 256: the pieces [lo, hi) of a layer and side, of `per` pieces a token, four of a thread's on their way at a time.
+template <typename P, typename At>
+__device__ __forceinline__ void copy_pieces(const char* a, char* b, int lo, int hi, At at) {
+    for (int u0 = lo + threadIdx.x; u0 < hi; u0 += 4 * 256) {
+        P x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (u0 + j * 256 < hi) x[j] = *reinterpret_cast<const P*>(a + at(u0 + j * 256));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (u0 + j * 256 < hi) *reinterpret_cast<P*>(b + at(u0 + j * 256)) = x[j];
+    }
+}
+// How a page lies: whole (its tokens are one stretch of memory), by token and head, or in 4 bits (a head's tokens are one stretch of codes and one of scales).
+enum { PAGE_WHOLE, PAGE_ROWS, PAGE_FP4 };
+// Part `split` of `splits` of the first `part` tokens of one layer and side, page `from` to page `to`.
+template <int LIES>
+__device__ __forceinline__ void copy_part(const Cache& c, int side, int from, int to, int part, int split, int splits) {
+    auto share = [&](long long all, int i) { return (int)(all * i / splits); };
+    char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side;
+    const int per = c.heads * c.chunks, all = part * per;
+    copy_pieces<int4>(base + from * c.s_page, base + to * c.s_page, share(all, split), share(all, split + 1), [&](int u) -> long long {
+        if (LIES == PAGE_WHOLE) return (long long)u * 16;
+        if (LIES == PAGE_FP4) { const int row = part * c.chunks, h = u / row; return h * c.s_head + (u - h * row) * 16LL; }
+        const int t = u / per, r = u - t * per, h = r / c.chunks;
+        return t * c.s_token + h * c.s_head + (r - h * c.chunks) * 16;
+    });
+    if constexpr (LIES == PAGE_FP4) {
+        char* scales = c.sc + (side >> 1) * c.c_layer + (side & 1) * c.c_side;
+        const int row = part * c.c_chunks, n = c.c_heads * row;
+        copy_pieces<int>(scales + from * c.c_page, scales + to * c.c_page, share(n, split), share(n, split + 1), [&](int u) -> long long { const int h = u / row; return h * c.c_head + (u - h * row) * 4LL; });
+    }
+}
+
 // 2 of 2: CTAs (share of the copy, pair) copy the tokens of the last page; the first of a pair writes its table.  Without pages the first
-// part is undone.  CONTIG: a page's tokens are one stretch of memory.
-template <bool CONTIG>
+// part is undone.
+template <int LIES>
 __global__ void __launch_bounds__(256) k_fork_copy(Cache c, const int* dst, int sides, int splits) {
     op_begin();
     const int i = blockIdx.y, d = dst[i], len = c.sc_pair()[2 * i];
@@ -295,26 +348,7 @@ __global__ void __launch_bounds__(256) k_fork_copy(Cache c, const int* dst, int 
     const int* row = c.sc_rows() + (long long)i * c.max_pages;
     const int page = ok && part ? c.sc_pages()[c.sc_first()[i]] : -1;
     const int from = part ? row[full] : -1;
-    if (ok && part && c.page_ok(from)) {
-        const int side = blockIdx.x / splits, split = blockIdx.x % splits;
-        char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side;
-        const char* a = base + from * c.s_page;
-        char* b = base + page * c.s_page;
-        const int per = c.heads * c.chunks, all = part * per;
-        const int lo = (int)((long long)all * split / splits), hi = (int)((long long)all * (split + 1) / splits);
-        auto at = [&](int u) -> long long {
-            if (CONTIG) return (long long)u * 16;
-            const int t = u / per, r = u - t * per, h = r / c.chunks;
-            return t * c.s_token + h * c.s_head + (r - h * c.chunks) * 16;
-        };
-        for (int u0 = lo + threadIdx.x; u0 < hi; u0 += 4 * 256) {
-            int4 x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) if (u0 + j * 256 < hi) x[j] = ld16(a + at(u0 + j * 256));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) if (u0 + j * 256 < hi) st16(b + at(u0 + j * 256), x[j]);
-        }
-    }
+    if (ok && part && c.page_ok(from)) copy_part<LIES>(c, blockIdx.x / splits, from, page, part, blockIdx.x % splits, splits);
     if (blockIdx.x) return;
     int* table = c.table + (long long)d * c.max_pages;
     const int held = c.held_of(d);
@@ -329,6 +363,108 @@ __global__ void __launch_bounds__(256) k_fork_copy(Cache c, const int* dst, int 
         c.length[d] = len;
         c.held[d] = used;
         if (part && c.page_ok(from)) atomicAdd(c.refs + from, -1);
+    }
+}
+
+// reorder.  Entries are the beams of groups of `beams` sequences; entry i's parent is the entry of its group that parents[i] names, itself where that, or a sequence number, is none
+// (BAD_INDEX), nobody where parents[i] is -1.
+struct Beams { const int* seqs; const int* parents; int n, beams; };
+constexpr int NOBODY = -1, NO_ENTRY = -2;                 // no parent: pages given back; no such sequence: nothing is done
+__device__ __forceinline__ int parent_of(const Cache& c, const Beams& b, int i, bool* bad = nullptr) {
+    if (!c.seq_ok(b.seqs[i])) { if (bad) *bad = true; return NO_ENTRY; }
+    const int p = b.parents[i], g = i - i % b.beams;
+    if (p == -1) return NOBODY;
+    if (p < 0 || p >= b.beams || !c.seq_ok(b.seqs[g + p])) { if (bad) *bad = true; return i; }
+    return g + p;
+}
+__device__ __forceinline__ int committed(const Cache& c, int s) { return min(max(c.length[s], 0), c.held_of(s) << c.page_shift); }
+
+// 1 of 2: one CTA an entry.  References move from the sequence's old pages to its parent's, whose table is noted.  A parent's last, partly filled page goes on with one child (the parent
+// itself if it is one, else the first), the others copy it to pages that the CTA that is through last gives out: those of beams that nobody continues are free by then.
+__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_reorder_take(Cache c, Beams b) {
+    __shared__ int warp_sums[32];
+    __shared__ int s_last;
+    op_begin();
+    const int i = blockIdx.x;
+    bool bad = false;
+    const int p = parent_of(c, b, i, &bad), pt = 1 << c.page_shift;
+    int* pair = c.sc_pair() + 2 * i;                      // tokens (-1: nothing to do), whether the last page is copied
+    if (bad && threadIdx.x == 0) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX);
+    if (p == NO_ENTRY) {
+        if (threadIdx.x == 0) { pair[0] = -1; pair[1] = 0; }
+    } else {
+        const int d = b.seqs[i], len = p == NOBODY ? 0 : committed(c, b.seqs[p]), full = len >> c.page_shift, used = full + ((len & (pt - 1)) != 0);
+        bool first = true;                                // of p's children
+        if (p >= 0 && p != i) {
+            const int g = i - i % b.beams;
+            bool mine = true;
+            for (int j = g + threadIdx.x; j < g + b.beams; j += blockDim.x)
+                if ((j < i || j == p) && parent_of(c, b, j) == p) mine = false;
+            first = __syncthreads_and(mine);
+        }
+        const bool copies = used > full && !first;
+        if (p != i) {
+            const int s = p == NOBODY ? d : b.seqs[p], take = copies ? full : used;
+            for (int j = threadIdx.x; j < used; j += blockDim.x) {
+                const int x = c.table[(long long)s * c.max_pages + j];
+                c.sc_rows()[(long long)i * c.max_pages + j] = x;
+                if (j < take && c.page_ok(x)) atomicAdd(c.refs + x, 1);
+            }
+        }
+        for (int j = (p == i ? used : 0) + threadIdx.x; j < c.held_of(d); j += blockDim.x) {
+            const int x = c.table[(long long)d * c.max_pages + j];
+            if (c.page_ok(x)) atomicAdd(c.refs + x, -1);
+        }
+        if (threadIdx.x == 0) { pair[0] = len; pair[1] = copies; }
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicInc((unsigned*)c.sc_ticket(), b.n - 1) == (unsigned)b.n - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    int run = 0;
+    for (int i0 = 0; i0 < b.n; i0 += CP_ALLOC_THREADS) {
+        const int j = i0 + threadIdx.x;
+        int total;
+        const int need = j < b.n ? __ldcg(c.sc_pair() + 2 * j + 1) : 0;
+        const int upto = cta_scan(need, warp_sums, &total);
+        if (j < b.n) c.sc_first()[j] = run + upto - need;
+        if (need) c.sc_jobs()[run + upto - need] = j;
+        run += total;
+    }
+    const bool ok = find_pages(c, run, warp_sums);
+    if (ok) for (int r = threadIdx.x; r < run; r += CP_ALLOC_THREADS) c.refs[c.sc_pages()[r]] = 1;
+    if (threadIdx.x == 0) { c.sc_ok()[0] = ok; c.sc_ok()[1] = ok ? run : 0; if (!ok) atomicOr(c.status, SPECDEC_CACHE_NO_PAGES); }
+}
+// 2 of 2: CTAs that stay write the entries' tables (without pages: undo the references), then take shares of the copies there are.
+template <int LIES>
+__global__ void __launch_bounds__(256) k_reorder_copy(Cache c, Beams b, int sides, int splits) {
+    op_begin();
+    const bool ok = c.sc_ok()[0];
+    const int jobs = c.sc_ok()[1], pt = 1 << c.page_shift;
+    for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
+        const int len = c.sc_pair()[2 * i];
+        if (len < 0) continue;
+        const int d = b.seqs[i], full = len >> c.page_shift, used = full + ((len & (pt - 1)) != 0), held = c.held_of(d), p = parent_of(c, b, i);
+        const bool copies = c.sc_pair()[2 * i + 1];
+        const int* row = c.sc_rows() + (long long)i * c.max_pages;
+        int* table = c.table + (long long)d * c.max_pages;
+        if (!ok) {
+            if (p != i) for (int j = threadIdx.x; j < (copies ? full : used); j += blockDim.x) if (c.page_ok(row[j])) atomicAdd(c.refs + row[j], -1);
+            for (int j = (p == i ? used : 0) + threadIdx.x; j < held; j += blockDim.x) if (c.page_ok(table[j])) atomicAdd(c.refs + table[j], 1);
+            continue;
+        }
+        const int page = copies ? c.sc_pages()[c.sc_first()[i]] : -1;
+        __syncthreads();                                  // every thread has read held[d]
+        for (int j = (p == i ? used : 0) + threadIdx.x; j < max(used, held); j += blockDim.x) table[j] = j >= used ? -1 : j == full && copies ? page : row[j];
+        if (threadIdx.x == 0) { c.length[d] = len; c.held[d] = used; }
+    }
+    const long long all = (long long)jobs * sides * splits;
+    for (long long w = blockIdx.x; w < all; w += gridDim.x) {
+        const int job = (int)(w / (sides * splits)), r = (int)(w % (sides * splits)), i = c.sc_jobs()[job], len = c.sc_pair()[2 * i];
+        const int from = c.sc_rows()[(long long)i * c.max_pages + (len >> c.page_shift)];
+        if (c.page_ok(from)) copy_part<LIES>(c, r / splits, from, c.sc_pages()[job], len & (pt - 1), r % splits, splits);
     }
 }
 
@@ -355,6 +491,84 @@ const char* view(const specdec_cache* c, Cache& v) {
     if (v.heads == 1 || v.s_head == v.chunks * 16LL) { v.chunks *= v.heads; v.heads = 1; }
     return nullptr;
 }
+// The same of a cache in 4 bits.
+const char* view(const specdec_packed_cache* f, Cache& v) {
+    if (const char* why = fp4_why_not(f)) return why;
+    const specdec_cache* c = &f->codes;
+    if (!c->d_refs || !c->d_held || !c->d_scratch) return "a pointer is NULL";
+    v.kv = (char*)c->d_kv; v.sc = (char*)f->d_scales;
+    v.table = c->d_table; v.length = c->d_length; v.held = c->d_held; v.refs = c->d_refs; v.status = c->d_status; v.scratch = c->d_scratch;
+    v.s_layer = op_stride(c->stride_layer, c->n_layers); v.s_side = c->stride_side; v.s_page = op_stride(c->stride_page, c->n_pages); v.s_token = c->head_dim / 2;
+    v.s_head = op_stride(c->stride_head, c->n_heads);
+    v.c_layer = op_stride(f->scale_stride_layer, c->n_layers); v.c_side = f->scale_stride_side; v.c_page = op_stride(f->scale_stride_page, c->n_pages); v.c_token = c->head_dim / 16;
+    v.c_head = op_stride(f->scale_stride_head, c->n_heads);
+    v.n_pages = c->n_pages; v.n_seqs = c->n_seqs; v.max_pages = c->max_pages;
+    v.page_shift = __builtin_ctz(c->page_tokens);
+    v.heads = v.c_heads = c->n_heads; v.chunks = c->head_dim / 32; v.c_chunks = c->head_dim / 64;
+    return nullptr;
+}
+int lies(const specdec_cache*, const Cache& v) { return v.heads == 1 && v.s_token == v.chunks * 16LL ? PAGE_WHOLE : PAGE_ROWS; }
+int lies(const specdec_packed_cache*, const Cache&) { return PAGE_FP4; }
+const specdec_cache& sizes(const specdec_cache* c) { return *c; }
+const specdec_cache& sizes(const specdec_packed_cache* f) { return f->codes; }
+// CTAs that share a layer and side of a page's copy.
+int copy_splits(const specdec_cache& c, const Cache& v) {
+    const long long most = (long long)c.page_tokens * v.heads * v.chunks;              // pieces of a side's page
+    return most <= 4096 ? 1 : most >= 32768 ? 8 : (int)(most / 4096);
+}
+
+// The calls, of either cache.
+template <typename C> int reserve(const char* who, const C* c, const int32_t* d_seqs, int n, int n_tokens, void* stream) {
+    Cache v;
+    if (const char* why = view(c, v)) return op_bad(who, why);
+    if ((n && !d_seqs) || n < 0 || n > v.n_seqs || n_tokens < 0) return op_bad(who, "d_seqs is NULL, n not in 0..n_seqs or n_tokens negative");
+    if (n == 0) return SPECDEC_OK;
+    return op_done(who, op_launch(k_cache_reserve, dim3(1), CP_ALLOC_THREADS, 0, (cudaStream_t)stream, 1, v, d_seqs, n, n_tokens));
+}
+template <typename C> int release(const char* who, const C* c, const int32_t* d_seqs, int n, void* stream) {
+    Cache v;
+    if (const char* why = view(c, v)) return op_bad(who, why);
+    if ((n && !d_seqs) || n < 0 || n > v.n_seqs) return op_bad(who, "d_seqs is NULL or n not in 0..n_seqs");
+    if (n == 0) return SPECDEC_OK;
+    return op_done(who, op_launch(k_cache_release, dim3(n), 256, 0, (cudaStream_t)stream, 1, v, d_seqs));
+}
+template <bool FP4, typename C>
+int compact(const char* who, const C* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride, const int32_t* d_n_path, void* stream) {
+    Cache v;
+    if (const char* why = view(c, v)) return op_bad(who, why);
+    if ((n && (!d_seqs || !d_path || !d_n_path)) || n < 0 || n > v.n_seqs || n > 65535 || path_stride < 1)
+        return op_bad(who, "a pointer is NULL, n not in 0..n_seqs or path_stride below 1");
+    if (n == 0) return SPECDEC_OK;
+    const int sides = 2 * sizes(c).n_layers;
+    const long long ctas = ((long long)sides * (v.heads * v.chunks + (FP4 ? v.c_heads * v.c_chunks : 0)) + 127) / 128;
+    return op_done(who, op_launch(k_cache_compact<FP4>, dim3((unsigned)(ctas < 1024 ? ctas : 1024), n), 128, 0, (cudaStream_t)stream, 1, v, d_seqs, d_path, path_stride, d_n_path, sides));
+}
+template <typename C> int fork(const char* who, const C* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream) {
+    Cache v;
+    if (const char* why = view(c, v)) return op_bad(who, why);
+    if ((n && (!d_src || !d_dst)) || n < 0 || n > v.n_seqs || n > 65535) return op_bad(who, "a pointer is NULL or n not in 0..n_seqs");
+    if (n == 0) return SPECDEC_OK;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const cudaError_t e = op_launch(k_fork_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, d_src, d_dst);
+    if (e != cudaSuccess) return op_done(who, e);
+    const int sides = 2 * sizes(c).n_layers, splits = copy_splits(sizes(c), v), l = lies(c, v);
+    return op_done(who, op_launch(l == PAGE_WHOLE ? k_fork_copy<PAGE_WHOLE> : l == PAGE_ROWS ? k_fork_copy<PAGE_ROWS> : k_fork_copy<PAGE_FP4>, dim3(sides * splits, n), 256, 0, st, 1, v, d_dst,
+                                  sides, splits));
+}
+template <typename C> int reorder(const char* who, const C* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream) {
+    Cache v;
+    if (const char* why = view(c, v)) return op_bad(who, why);
+    if ((n && (!d_seqs || !d_parents)) || n < 0 || n > v.n_seqs || beams < 1 || n % beams) return op_bad(who, "a pointer is NULL, n not in 0..n_seqs or no multiple of beams, or beams below 1");
+    if (n == 0) return SPECDEC_OK;
+    const cudaStream_t st = (cudaStream_t)stream;
+    const Beams b{d_seqs, d_parents, n, beams};
+    const cudaError_t e = op_launch(k_reorder_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, b);
+    if (e != cudaSuccess) return op_done(who, e);
+    const int sides = 2 * sizes(c).n_layers, splits = copy_splits(sizes(c), v), l = lies(c, v);
+    const long long items = (long long)n * sides * splits, most = 8 * 148;             // (how many copies there are is known on the device)
+    return op_done(who, op_launch(l == PAGE_WHOLE ? k_reorder_copy<PAGE_WHOLE> : l == PAGE_ROWS ? k_reorder_copy<PAGE_ROWS> : k_reorder_copy<PAGE_FP4>,
+                                  dim3((unsigned)(items < most ? items : most)), 256, 0, st, 1, v, b, sides, splits));
+}
 
 }  // namespace
 }  // namespace sd
@@ -365,23 +579,26 @@ extern "C" {
 
 long long specdec_cache_scratch(int n_seqs, int max_pages, int n_pages) {
     if (n_seqs < 1 || max_pages < 1 || n_pages < 1) return op_bad("cache_scratch", "a size is below 1");
-    return 16 + 4LL * n_seqs + n_pages + (long long)n_seqs * max_pages;
+    return 16 + 5LL * n_seqs + n_pages + (long long)n_seqs * max_pages;
 }
 
-int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream) {
-    Cache v;
-    if (const char* why = view(c, v)) return op_bad("cache_reserve", why);
-    if ((n && !d_seqs) || n < 0 || n > c->n_seqs || n_tokens < 0) return op_bad("cache_reserve", "d_seqs is NULL, n not in 0..n_seqs or n_tokens negative");
-    if (n == 0) return SPECDEC_OK;
-    return op_done("cache_reserve", op_launch(k_cache_reserve, dim3(1), CP_ALLOC_THREADS, 0, (cudaStream_t)stream, 1, v, d_seqs, n, n_tokens));
+int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream) { return reserve("cache_reserve", c, d_seqs, n, n_tokens, stream); }
+int specdec_packed_cache_reserve(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream) { return reserve("packed_cache_reserve", c, d_seqs, n, n_tokens, stream); }
+int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, void* stream) { return release("cache_release", c, d_seqs, n, stream); }
+int specdec_packed_cache_release(const specdec_packed_cache* c, const int32_t* d_seqs, int n, void* stream) { return release("packed_cache_release", c, d_seqs, n, stream); }
+int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride, const int32_t* d_n_path, void* stream) {
+    return compact<false>("cache_compact", c, d_seqs, n, d_path, path_stride, d_n_path, stream);
 }
-
-int specdec_cache_release(const specdec_cache* c, const int32_t* d_seqs, int n, void* stream) {
-    Cache v;
-    if (const char* why = view(c, v)) return op_bad("cache_release", why);
-    if ((n && !d_seqs) || n < 0 || n > c->n_seqs) return op_bad("cache_release", "d_seqs is NULL or n not in 0..n_seqs");
-    if (n == 0) return SPECDEC_OK;
-    return op_done("cache_release", op_launch(k_cache_release, dim3(n), 256, 0, (cudaStream_t)stream, 1, v, d_seqs));
+int specdec_packed_cache_compact(const specdec_packed_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride, const int32_t* d_n_path, void* stream) {
+    return compact<true>("packed_cache_compact", c, d_seqs, n, d_path, path_stride, d_n_path, stream);
+}
+int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream) { return sd::fork("cache_fork", c, d_src, d_dst, n, stream); }
+int specdec_packed_cache_fork(const specdec_packed_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream) { return sd::fork("packed_cache_fork", c, d_src, d_dst, n, stream); }
+int specdec_cache_reorder(const specdec_cache* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream) {
+    return reorder("cache_reorder", c, d_seqs, d_parents, n, beams, stream);
+}
+int specdec_packed_cache_reorder(const specdec_packed_cache* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream) {
+    return reorder("packed_cache_reorder", c, d_seqs, d_parents, n, beams, stream);
 }
 
 int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int T,
@@ -400,33 +617,6 @@ int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, i
     if (v.heads == 1 && (c->n_heads == 1 || a.s_head == a.chunks * 16LL)) { a.chunks *= a.heads; a.heads = 1; }
     const int all = a.heads * a.chunks, threads = all <= 32 ? 32 : all <= 64 ? 64 : all <= 128 ? 128 : 256;
     return op_done("cache_append", op_launch(k_cache_append, dim3(T, n, n_layers), threads, 0, (cudaStream_t)stream, 1, v, a));
-}
-
-int specdec_cache_compact(const specdec_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride,
-                          const int32_t* d_n_path, void* stream) {
-    Cache v;
-    if (const char* why = view(c, v)) return op_bad("cache_compact", why);
-    if ((n && (!d_seqs || !d_path || !d_n_path)) || n < 0 || n > c->n_seqs || n > 65535 || path_stride < 1)
-        return op_bad("cache_compact", "a pointer is NULL, n not in 0..n_seqs or path_stride below 1");
-    if (n == 0) return SPECDEC_OK;
-    const int sides = 2 * c->n_layers;
-    const long long ctas = ((long long)sides * v.heads * v.chunks + 127) / 128;
-    return op_done("cache_compact", op_launch(k_cache_compact, dim3((unsigned)(ctas < 1024 ? ctas : 1024), n), 128, 0, (cudaStream_t)stream, 1, v, d_seqs, d_path, path_stride, d_n_path, sides));
-}
-
-int specdec_cache_fork(const specdec_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream) {
-    Cache v;
-    if (const char* why = view(c, v)) return op_bad("cache_fork", why);
-    if ((n && (!d_src || !d_dst)) || n < 0 || n > c->n_seqs || n > 65535) return op_bad("cache_fork", "a pointer is NULL or n not in 0..n_seqs");
-    if (n == 0) return SPECDEC_OK;
-    const cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = op_launch(k_fork_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, d_src, d_dst);
-    if (e != cudaSuccess) return op_done("cache_fork", e);
-    const int sides = 2 * c->n_layers;
-    const long long most = (long long)c->page_tokens * v.heads * v.chunks;             // pieces of a side's page
-    const int splits = most <= 4096 ? 1 : most >= 32768 ? 8 : (int)(most / 4096);
-    const bool contig = v.heads == 1 && v.s_token == v.chunks * 16LL;
-    return op_done("cache_fork", op_launch(contig ? k_fork_copy<true> : k_fork_copy<false>, dim3(sides * splits, n), 256, 0, st, 1, v, d_dst, sides, splits));
 }
 
 }  // extern "C"

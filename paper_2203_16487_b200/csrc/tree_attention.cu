@@ -461,6 +461,10 @@ bool tensor_map(CUtensorMap& tm, const specdec_cache* c, const void* keys) {
 }
 
 }  // namespace
+
+cudaError_t ta_merge(const TreeAttn& a, int dtype, int rows, cudaStream_t st) {
+    return dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, rows, st) : dtype == SPECDEC_DTYPE_BF16 ? run_merge<__nv_bfloat16>(a, rows, st) : run_merge<__half>(a, rows, st);
+}
 }  // namespace sd
 
 using namespace sd;
@@ -532,7 +536,7 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
         if (!tensor_map(tm, c, a.k)) return op_fail(SPECDEC_ERR_CUDA, who, "the driver makes no tensor map of this cache");
         rc = p.rows >= 128 ? ta_tc(tm, a, c->dtype, p.rows, (int)p.grid, s) : ta_tma_mma(tm, a, c->dtype, p.rows, (int)p.grid, s);
     }
-    if (rc == cudaSuccess && need) rc = c->dtype == SPECDEC_DTYPE_F32 ? run_merge<float>(a, p.rows, s) : bf ? run_merge<__nv_bfloat16>(a, p.rows, s) : run_merge<__half>(a, p.rows, s);
+    if (rc == cudaSuccess && need) rc = ta_merge(a, c->dtype, p.rows, s);
     return op_done(who, rc);
 }
 

@@ -425,6 +425,7 @@ __device__ __forceinline__ void ta_box(uint32_t dst, const CUtensorMap* tm, int 
 constexpr int TA_MIN_PAGE = 8;                            // tokens: a box fills whole swizzle groups of 8 rows
 
 cudaError_t ta_tma_mma(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);         // tiles of 16, 32, 64 rows
+cudaError_t ta_merge(const TreeAttn& a, int dtype, int rows, cudaStream_t st);                                            // joins the parts of sequences that were cut
 cudaError_t ta_tc(const CUtensorMap& tm, const TreeAttn& a, int dtype, int rows, int grid, cudaStream_t st);              // of 128, 256
 
 }  // namespace sd

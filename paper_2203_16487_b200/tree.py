@@ -95,57 +95,82 @@ class PagedCache:
         _ints("table", table, (n_seqs, table.shape[1]), at), _ints("length", length, (n_seqs,), at), _ints("held", held, (n_seqs,), at), _ints("refs", refs, (P,), at)
         self.kv, self.table, self.length, self.held, self.refs = kv, table, length, held, refs
         self.status = torch.zeros(1, dtype=torch.int32, device=kv.device)
-        n = lib().specdec_cache_scratch(n_seqs, table.shape[1], P)
-        if n < 0:
-            _fail(n)
-        self._scratch = torch.zeros(n, dtype=torch.int32, device=kv.device)
+        self._scratch = self._new_scratch(n_seqs, table.shape[1], P, kv.device)
         s = kv.stride()
         self._c = Cache(kv.data_ptr(), DTYPES[kv.dtype], L, H, D, P, page, n_seqs, table.shape[1], s[0], s[1], s[2], s[3], s[4],
                         table.data_ptr(), length.data_ptr(), held.data_ptr(), refs.data_ptr(), self.status.data_ptr(), self._scratch.data_ptr())
-        self._ref, self._lib, self._device = C.byref(self._c), lib(), kv.get_device()
-        self._code, self._page = DTYPES[kv.dtype], page
+        self._ref, self._code = C.byref(self._c), DTYPES[kv.dtype]
+        self.dtype = kv.dtype
+        self._finish("specdec_cache_", kv.get_device(), n_layers=L, n_heads=H, head_dim=D, page=page, max_pages=table.shape[1])
+
+    @staticmethod
+    def _new_scratch(n_seqs, max_pages, n_pages, device):
+        n = lib().specdec_cache_scratch(n_seqs, max_pages, n_pages)
+        if n < 0:
+            _fail(n)
+        return torch.zeros(n, dtype=torch.int32, device=device)
+
+    def _finish(self, calls, device, *, n_layers, n_heads, head_dim, page, max_pages):
+        """What every cache has: the library's calls of its kind, sizes, workspaces."""
+        self._lib, self._device, self._page = lib(), device, page
+        self._call = {name: getattr(self._lib, calls + name) for name in ("reserve", "append", "compact", "release", "fork", "reorder")}
         self._workspaces = {}                              # bytes by sizes of a call
         self._source = None                                # requires a gradient, where keys or values did
-        self.dtype, self.n_heads, self.head_dim, self.max_length = kv.dtype, H, D, table.shape[1] * page
+        self.n_layers, self.n_heads, self.head_dim, self.max_length = n_layers, n_heads, head_dim, max_pages * page
 
     def reserve(self, seqs, n_tokens: int):
         """Pages for n_tokens tokens behind the committed ones."""
         n = seqs.numel()
-        _launch(self._lib.specdec_cache_reserve, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, n_tokens, _raw_stream(self._device)))
+        _launch(self._call["reserve"], self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, n_tokens, _raw_stream(self._device)))
 
-    def append(self, seqs, k, v, layer: Optional[int] = None, count=None):
-        """Writes k, v [n, T, n_heads, head_dim] (layer=None: [n_layers, n, T, n_heads, head_dim], every layer) behind the committed tokens; of
-        sequence i the first count[i] of the T.  Lengths stay: compact moves them."""
-        n, shape, s = seqs.numel(), k.shape, k.stride()
+    def _block(self, n, k, v, layer, dtype):
+        """(layer, layers, shape, strides) of tokens k, v [(n_layers,) n, T, n_heads, head_dim]; raises where they are none."""
+        shape, s = k.shape, k.stride()
         if layer is None:
-            layer, layers = 0, self._c.n_layers
+            layer, layers = 0, self.n_layers
             good = len(shape) == 5 and shape[0] == layers
         else:
             layers, shape, s = 1, (1,) + tuple(shape), (0,) + tuple(s)
             good = len(shape) == 5
-        if not (good and v.shape == k.shape and (v.stride() == k.stride() or all(a == b or m == 1 for a, b, m in zip(v.stride(), k.stride(), k.shape))) and k.dtype is self.dtype and v.dtype is self.dtype and k.get_device() == v.get_device() == self._device
+        if not (good and v.shape == k.shape and (v.stride() == k.stride() or all(a == b or m == 1 for a, b, m in zip(v.stride(), k.stride(), k.shape))) and k.dtype is dtype and v.dtype is dtype and k.get_device() == v.get_device() == self._device
                 and s[4] == 1 and shape[1] == n and shape[3] == self.n_heads and shape[4] == self.head_dim):
             raise ValueError("k, v: device tensors [(n_layers,) n, T, n_heads, head_dim] of the cache's type and alike in their strides are wanted")      # (a dimension of 1 has none)
+        return layer, layers, shape, s
+
+    def append(self, seqs, k, v, layer: Optional[int] = None, count=None):
+        """Writes k, v [n, T, n_heads, head_dim] (layer=None: [n_layers, n, T, n_heads, head_dim], every layer) behind the committed tokens; of
+        sequence i the first count[i] of the T.  Lengths stay: compact moves them."""
+        n = seqs.numel()
+        layer, layers, shape, s = self._block(n, k, v, layer, self.dtype)
         if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled() and self._source is None:
             self._source = torch.zeros((), requires_grad=True)
-        _launch(self._lib.specdec_cache_append, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
+        _launch(self._call["append"], self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), shape[2],
                 s[0], s[1], s[2], s[3], None if count is None else _ints("count", count, (n,), self._device), _raw_stream(self._device)))
 
     def compact(self, seqs, path, n_path):
         """Commits the nodes path[i, :n_path[i]] of each sequence's block and gives back the pages behind them."""
         n, T = seqs.numel(), path.shape[-1]
-        _launch(self._lib.specdec_cache_compact, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _ints("path", path, (n, T), self._device), T,
+        _launch(self._call["compact"], self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _ints("path", path, (n, T), self._device), T,
                 _ints("n_path", n_path, (n,), self._device), _raw_stream(self._device)))
 
     def release(self, seqs):
         """Gives back all pages of the sequences; their lengths are 0."""
         n = seqs.numel()
-        _launch(self._lib.specdec_cache_release, self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _raw_stream(self._device)))
+        _launch(self._call["release"], self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, _raw_stream(self._device)))
 
     def fork(self, src, dst):
         """Sequence dst[i] becomes a copy of what src[i] was before the call: full pages shared, the last, partly filled one copied."""
         n = src.numel()
-        _launch(self._lib.specdec_cache_fork, self._device, (self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n, _raw_stream(self._device)))
+        _launch(self._call["fork"], self._device, (self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n, _raw_stream(self._device)))
+
+    def reorder(self, seqs, parents):
+        """Beams: of seqs [..., K], groups of K sequences, each becomes what sequence parents [..., K] (its place in the group, 0 .. K - 1; -1: none) was before the call.  Full pages
+        are shared; the last, partly filled one goes on with one child (the parent itself if it is one, else the first) and is copied for the others."""
+        if seqs.dim() < 1:
+            raise ValueError("seqs: groups of sequences [..., K] are wanted")
+        shape, n = seqs.shape, seqs.numel()
+        _launch(self._call["reorder"], self._device, (self._ref, _ints("seqs", seqs, shape, self._device), _ints("parents", parents, shape, self._device), n, max(shape[-1], 1),
+                                                      _raw_stream(self._device)))
 
     def check(self):
         """Raises if a call found too few pages or bad numbers since the last check (waits for the stream)."""
@@ -181,11 +206,13 @@ def accept(parents, tokens, sampled, n_nodes=None):
 
 def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max_length: int = 0, scale: Optional[float] = None, out=None):
     """Attention of tree nodes q [B, T, n_q_heads, head_dim] over the committed tokens of sequences seqs [B] and, by mask [B or 1, T, ceil(T / 32)], over
-    the block's nodes (appended before).  max_length: an upper bound of the committed lengths, if known.  scale: 1 / sqrt(head_dim)."""
+    the block's nodes (appended before).  max_length: an upper bound of the committed lengths, if known.  scale: 1 / sqrt(head_dim).  q is of the cache's type; over a cache in 4 bits
+    (fp4.Fp4Cache) of any of the three."""
     B, T, H, D = q.shape
-    sq, at = q.stride(), cache._device
-    if q.dtype is not cache.dtype or D != cache.head_dim or sq[3] != 1 or q.get_device() != at:
-        raise ValueError(f"q: a device tensor [B, T, heads, {cache.head_dim}] of {cache.dtype} with a contiguous last dimension is wanted")
+    sq, at, fp4 = q.stride(), cache._device, cache.dtype is None
+    code = DTYPES.get(q.dtype) if fp4 else cache._code
+    if (code is None if fp4 else q.dtype is not cache.dtype) or D != cache.head_dim or sq[3] != 1 or q.get_device() != at:
+        raise ValueError(f"q: a device tensor [B, T, heads, {cache.head_dim}] of {cache.dtype or 'fp32, bf16 or fp16'} with a contiguous last dimension is wanted")
     if out is None:
         out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(B, T, H, D)
     elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(3) != 1 or out.get_device() != at:
@@ -197,14 +224,14 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     if 0 < max_length < bound:
         bound = max_length
     L = cache._lib
-    n = cache._workspaces.get((B, T, H, bound))
+    n = cache._workspaces.get((B, T, H, bound, code))
     if n is None:
-        n = L.specdec_tree_attention_workspace(B, T, H, cache.n_heads, D, cache._code, cache._page, bound)
+        n = (L.specdec_packed_attention_workspace if fp4 else L.specdec_tree_attention_workspace)(B, T, H, cache.n_heads, D, code, cache._page, bound)
         if n < 0:
             _fail(n)
         if len(cache._workspaces) > 4096:
             cache._workspaces.clear()
-        cache._workspaces[B, T, H, bound] = n
+        cache._workspaces[B, T, H, bound, code] = n
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     try:
         a = _attention_args.pack(q.data_ptr(), out.data_ptr(), sq[0], sq[1], sq[2], so[0], so[1], so[2], B, T, H, layer, _ints("seqs", seqs, (B,), at), m,
@@ -212,7 +239,10 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
                                  ws.data_ptr() if n else 0, n)
     except struct.error as e:
         raise ValueError(f"layer or scale: {e}") from None
-    _launch(L.specdec_tree_attention, at, (cache._ref, a, _raw_stream(at)))
+    if fp4:
+        _launch(L.specdec_packed_attention, at, (cache._ref, a, code, _raw_stream(at)))
+    else:
+        _launch(L.specdec_tree_attention, at, (cache._ref, a, _raw_stream(at)))
     if (q.requires_grad or cache._source is not None) and torch.is_grad_enabled():
         return _NoGradient.apply(out, q if q.requires_grad else cache._source, "tree.attention")
     return out
