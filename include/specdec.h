@@ -329,6 +329,17 @@ int specdec_sample(const void* d_logits, int dtype, long long stride, int rows, 
                    const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, int rows_per_param,
                    int32_t* d_token, float* d_logprob, void* stream);
 
+/* Beam search: the n best continuations of each sentence's K beams.  Row (b, k) of d_logits [B, K, V] (row b * K + k at stride times that; V contiguous; fp32, bf16, fp16; NaN: never taken) belongs to a
+ * beam of score d_scores [B, K] (-inf or NaN: none; its row is not read).  With l = a row's logits, log p_v = l_v - ln sum_w exp(l_w) (of infinite logits each has an equal share, the others
+ * none).  Candidates are (k, v) with score s = d_scores[b, k] + log p_v and rank s * d_norm[b, k] (NULL: s), and for a beam with d_finished[b, k] != 0 only (k, end_token) with
+ * s = d_scores[b, k].  The n of largest rank come out, best first: d_out_scores (s), d_out_parent (k), d_out_token (v) [B, n]; where there are fewer with a rank above
+ * -inf, -inf, -1 and -1 follow.  Order: rank; of ranks alike the lower beam; of one beam the larger logit, then the lower token.  What is taken is what exact sums would give: sums are fp32
+ * unless ranks of different beams lie within some 2^-19 of one another, then 64 bits.  d_norm is a length penalty's factor (positive, finite); scores and ranks are 64 bits inside.
+ * K and n: at most 64, V 2^20, B * K 65535.  The workspace (8-byte aligned, no state between calls) has specdec_beam_select_workspace() bytes. */
+long long specdec_beam_select_workspace(int B, int K, int V, int n, int dtype);
+int specdec_beam_select(const void* d_logits, int dtype, long long stride, int B, int K, int V, const float* d_scores, const unsigned char* d_finished, int end_token, const float* d_norm, int n,
+                        float* d_out_scores, int32_t* d_out_parent, int32_t* d_out_token, void* d_workspace, long long workspace_bytes, void* stream);
+
 /* Debug / parity helpers (not on the hot path).
  * specdec_debug_logits: re-runs the vocabulary projection of the last verify
  *   (which = 0, rows [B*(k+1)]) or draft (which = 1, rows [n_active*k]) pass

@@ -31,6 +31,7 @@ EXPORTS = [
     "specdec_tree_attention", "specdec_sample", "specdec_cache_reorder",
     "specdec_packed_cache_reserve", "specdec_packed_cache_append", "specdec_packed_cache_read", "specdec_packed_cache_compact", "specdec_packed_cache_release",
     "specdec_packed_cache_fork", "specdec_packed_cache_reorder", "specdec_packed_attention_workspace", "specdec_packed_attention",
+    "specdec_beam_select_workspace", "specdec_beam_select",
 ]
 
 
@@ -134,6 +135,8 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.specdec_packed_cache_append.argtypes = lib.specdec_packed_cache_read.argtypes = [fp, ip, i, i, i, vp, vp, i, i, L, L, L, L, ip, vp]
     lib.specdec_packed_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
     lib.specdec_packed_attention.argtypes = [fp, vp, i, vp]
+    lib.specdec_beam_select_workspace.argtypes = [i, i, i, i, i]
+    lib.specdec_beam_select.argtypes = [vp, i, L, i, i, i, vp, vp, i, vp, i, vp, ip, ip, vp, L, vp]
     lib.specdec_tree_ancestors.argtypes = [ip, ip, i, i, vp, ip, vp]
     lib.specdec_tree_accept.argtypes = [ip, ip, ip, ip, i, i, ip, ip, ip, vp]
     lib.specdec_tree_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
@@ -142,7 +145,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     for name in EXPORTS:
         if name not in ("specdec_launch_count", "specdec_last_error"):
             getattr(lib, name).restype = i
-    lib.specdec_cache_scratch.restype = lib.specdec_tree_attention_workspace.restype = lib.specdec_packed_attention_workspace.restype = L
+    lib.specdec_cache_scratch.restype = lib.specdec_tree_attention_workspace.restype = lib.specdec_packed_attention_workspace.restype = lib.specdec_beam_select_workspace.restype = L
     return lib
 
 
