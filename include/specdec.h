@@ -337,8 +337,17 @@ int specdec_sample(const void* d_logits, int dtype, long long stride, int rows, 
  * unless ranks of different beams lie within some 2^-19 of one another, then 64 bits.  d_norm is a length penalty's factor (positive, finite); scores and ranks are 64 bits inside.
  * K and n: at most 64, V 2^20, B * K 65535.  The workspace (8-byte aligned, no state between calls) has specdec_beam_select_workspace() bytes. */
 long long specdec_beam_select_workspace(int B, int K, int V, int n, int dtype);
-int specdec_beam_select(const void* d_logits, int dtype, long long stride, int B, int K, int V, const float* d_scores, const unsigned char* d_finished, int end_token, const float* d_norm, int n,
-                        float* d_out_scores, int32_t* d_out_parent, int32_t* d_out_token, void* d_workspace, long long workspace_bytes, void* stream);
+typedef struct {
+    const void          *d_logits;         /* [B, K, V]; `stride` elements between rows                                  */
+    const float         *d_scores;         /* [B, K]                                                                     */
+    const unsigned char *d_finished;       /* [B, K] or NULL: none                                                       */
+    const float         *d_norm;           /* [B, K] or NULL: 1                                                          */
+    float               *d_out_scores;     /* [B, n]                                                                     */
+    int32_t             *d_out_parent, *d_out_token;
+    void                *d_workspace; long long workspace_bytes, stride;
+    int                  dtype, B, K, V, n, end_token;
+} specdec_beam_select_args;
+int specdec_beam_select(const specdec_beam_select_args* a, void* stream);
 
 /* Debug / parity helpers (not on the hot path).
  * specdec_debug_logits: re-runs the vocabulary projection of the last verify

@@ -9,12 +9,18 @@
 Every call runs on the tensors' device, on its current stream, and returns without waiting for it (contracts: include/specdec.h)."""
 from __future__ import annotations
 
+import ctypes as C
+import struct
+
 import torch
 
 from . import tree
+from .binding import BeamSelectArgs
 from .tree import DTYPES, _I32, _NoGradient, _fail, _launch
 
 _workspaces = {}                                             # bytes by sizes of a call
+_args = struct.Struct("@PPPPPPPPqqiiiiii")                   # BeamSelectArgs in one go
+assert _args.size == C.sizeof(BeamSelectArgs)
 
 
 def _rows(name, t, shape, dtype, at):
@@ -45,8 +51,8 @@ def select(logits, scores, n: int, *, finished=None, end_token: int = 0, norm=No
             raise ValueError("logits: evenly spaced rows are wanted")
     pair = shape[:2]
     p_scores = _rows("scores", scores, pair, torch.float32, at)
-    p_finished = None if finished is None else _rows("finished", finished, pair, torch.bool, at)
-    p_norm = None if norm is None else _rows("norm", norm, pair, torch.float32, at)
+    p_finished = 0 if finished is None else _rows("finished", finished, pair, torch.bool, at)
+    p_norm = 0 if norm is None else _rows("norm", norm, pair, torch.float32, at)
     lib = tree.lib()
     size = _workspaces.get((B, K, V, n, code))
     if size is None:
@@ -56,12 +62,15 @@ def select(logits, scores, n: int, *, finished=None, end_token: int = 0, norm=No
         if len(_workspaces) > 4096:
             _workspaces.clear()
         _workspaces[B, K, V, n, code] = size
-    out = scores.new_empty(B, n)
-    both = torch.empty((2, B, n), dtype=_I32, device=logits.device)
-    parent, token = both[0], both[1]
-    ws = torch.empty(size, dtype=torch.uint8, device=logits.device)
-    _launch(lib.specdec_beam_select, at, (logits.data_ptr(), code, stride, B, K, V, p_scores, p_finished, end_token, p_norm, n, out.data_ptr(), parent.data_ptr(), token.data_ptr(),
-                                          ws.data_ptr(), size, tree._raw_stream(at)))
+    out, m = torch.empty((B, n), dtype=torch.float32, device=logits.device), B * n
+    rest = torch.empty(2 * (m + 1) + size // 4, dtype=_I32, device=logits.device)       # parents, tokens, workspace (8-byte aligned)
+    p = rest.data_ptr()
+    parent, token = rest.as_strided((B, n), (n, 1)), rest.as_strided((B, n), (n, 1), m)
+    try:
+        a = _args.pack(logits.data_ptr(), p_scores, p_finished, p_norm, out.data_ptr(), p, p + 4 * m, p + 8 * m, size, stride, code, B, K, V, n, end_token)
+    except struct.error as e:
+        raise ValueError(f"end_token: {e}") from None
+    _launch(lib.specdec_beam_select, at, (a, tree._raw_stream(at)))
     if (logits.requires_grad or scores.requires_grad) and torch.is_grad_enabled():
         out = _NoGradient.apply(out, logits if logits.requires_grad else scores, "beam.select")
     return out, parent, token

@@ -76,6 +76,11 @@ class TreeAttentionArgs(C.Structure):
         ("max_length", C.c_int), ("scale", C.c_float), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_longlong)]
 
 
+class BeamSelectArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_logits", "d_scores", "d_finished", "d_norm", "d_out_scores", "d_out_parent", "d_out_token", "d_workspace")] + [
+        ("workspace_bytes", C.c_longlong), ("stride", C.c_longlong)] + [(n, C.c_int) for n in ("dtype", "B", "K", "V", "n", "end_token")]
+
+
 class Stats(C.Structure):
     _fields_ = [("iterations", C.c_longlong), ("seq_iterations", C.c_longlong), ("drafted", C.c_longlong),
                 ("accepted", C.c_longlong), ("emitted", C.c_longlong),
@@ -136,7 +141,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.specdec_packed_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
     lib.specdec_packed_attention.argtypes = [fp, vp, i, vp]
     lib.specdec_beam_select_workspace.argtypes = [i, i, i, i, i]
-    lib.specdec_beam_select.argtypes = [vp, i, L, i, i, i, vp, vp, i, vp, i, vp, ip, ip, vp, L, vp]
+    lib.specdec_beam_select.argtypes = [vp, vp]                # (BeamSelectArgs by reference, or its bytes)
     lib.specdec_tree_ancestors.argtypes = [ip, ip, i, i, vp, ip, vp]
     lib.specdec_tree_accept.argtypes = [ip, ip, ip, ip, i, i, ip, ip, ip, vp]
     lib.specdec_tree_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]

@@ -22,7 +22,8 @@ namespace sd {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int BM_NT = 256, BM_WARPS = BM_NT / 32, BM_MOST = 64, BM_LIST = 512, BM_JOIN = 512;       // threads; beams and results at most; listed entries of a stretch, of a sentence
+constexpr int BM_NT = 256, BM_WARPS = BM_NT / 32, BM_MOST = 64, BM_LIST = 512;           // threads of a stretch; beams and results at most; listed entries of a stretch
+constexpr int BJ_NT = 512, BJ_WARPS = BJ_NT / 32, BJ_STAGE = 2048, BJ_LIST = 512;        // threads of a sentence; entries that it keeps in shared memory; that it ranks
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double NEAR = 1.0 / (1 << 19);
 
@@ -38,7 +39,7 @@ __device__ __forceinline__ u64 entry(float l, int index) { return (u64)key_of(l)
 struct BeamArgs {
     const void* logits; long long s_row; int V;           // elements between rows
     const float* scores; const unsigned char* finished; const float* norm;
-    int end_token, B, K, n, stretches;
+    int end_token, B, K, n, stretches, span;             // vectors of a stretch
     float* out_scores; int* out_parent; int* out_token;
     float2* sums; u64* lists;                             // [row, stretch]: (maximum, sum); [row, stretch, n], best first, 0 where there are fewer
     __device__ __forceinline__ bool alive(int row) const { return scores[row] > -INFINITY && !(finished && finished[row]); }       // (NaN: dead)
@@ -46,6 +47,19 @@ struct BeamArgs {
 
 template <typename T> struct Vec {
     static constexpr int N = 16 / sizeof(T);
+    // The largest element (NaN: passed over), of 16-bit types two at a time.
+    static __device__ __forceinline__ float max_of(const uint4& v) {
+        if constexpr (sizeof(T) == 4) return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+        else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            auto h = [](const uint32_t& w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+            const float2 f = __bfloat1622float2(__hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w))));
+            return fmaxf(f.x, f.y);
+        } else {
+            auto h = [](const uint32_t& w) { return *reinterpret_cast<const __half2*>(&w); };
+            const float2 f = __half22float2(__hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w))));
+            return fmaxf(f.x, f.y);
+        }
+    }
     static __device__ __forceinline__ float at(const uint4& v, int i) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
@@ -59,6 +73,11 @@ template <typename T> __device__ __forceinline__ float as_float(T x) {
     else return __half2float(x);
 }
 __device__ __forceinline__ float exp2_of(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ u64 pair2(float lo, float hi) { u64 d; asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi)); return d; }
+__device__ __forceinline__ float lo2(u64 d) { return __uint_as_float((uint32_t)d); }
+__device__ __forceinline__ float hi2(u64 d) { return __uint_as_float((uint32_t)(d >> 32)); }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
 __device__ __forceinline__ u64 warp_max(u64 v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) { const u64 u = __shfl_xor_sync(0xffffffffu, v, o); if (u > v) v = u; }
@@ -67,7 +86,7 @@ __device__ __forceinline__ u64 warp_max(u64 v) {
 
 // CTA = (stretch, row) of NV vectors a thread.
 template <typename T, int NV>
-__global__ void __launch_bounds__(BM_NT) k_beam_rows(BeamArgs a) {
+__global__ void __launch_bounds__(BM_NT, NV == 8 ? 4 : 5) k_beam_rows(BeamArgs a) {
     constexpr int VE = Vec<T>::N;
     __shared__ float w_max[BM_WARPS], w_sum[BM_WARPS];
     __shared__ uint32_t w_bound[BM_WARPS];
@@ -79,32 +98,32 @@ __global__ void __launch_bounds__(BM_NT) k_beam_rows(BeamArgs a) {
     if (!a.alive(row)) return;
     const T* p = (const T*)a.logits + row * a.s_row;
     const int lead = (int)(((uintptr_t)p & 15) / sizeof(T));          // elements of the first vector that lie ahead of the row
-    const int first = blockIdx.x * BM_NT * NV;
+    const int first = blockIdx.x * a.span;
     auto place = [&](int j, int i) { return (first + j * BM_NT + tid) * VE - lead + i; };
+    // Vectors of the stretch, by number from the row's first on: whole ones from whole to whole_end, ends of the row beside them.
+    const T* base = p - lead;
+    const int mine0 = first + tid, end = min(first + a.span, (a.V + lead + VE - 1) / VE), whole = lead > 0, whole_end = min(end, (a.V + lead) / VE);
+    auto fetch = [&](int j) {                             // what lies outside: -inf
+        const int g = mine0 + j * BM_NT;
+        uint4 v = sizeof(T) == 4 ? make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u) : std::is_same<T, __half>::value ? make_uint4(0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u)
+                                                                                                                                   : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+        if (g >= whole && g < whole_end) v = *reinterpret_cast<const uint4*>(base + (long long)g * VE);
+        else if (g < end) {
+            T e[VE];
+            *reinterpret_cast<uint4*>(e) = v;
+            for (int i = 0; i < VE; ++i) if (g * VE + i >= lead && g * VE + i < a.V + lead) e[i] = base[g * VE + i];
+            v = *reinterpret_cast<uint4*>(e);
+        }
+        return v;
+    };
     uint4 x[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i0 = place(j, 0);
-        if (i0 >= 0 && i0 + VE <= a.V) x[j] = *reinterpret_cast<const uint4*>(p + i0);
-        else {
-            T e[VE];
-#pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                if (i0 + i >= 0 && i0 + i < a.V) e[i] = p[i0 + i];
-                else if constexpr (sizeof(T) == 4) e[i] = -INFINITY;
-                else if constexpr (std::is_same<T, __nv_bfloat16>::value) e[i] = __float2bfloat16_rn(-INFINITY);
-                else e[i] = __float2half_rn(-INFINITY);
-            }
-            x[j] = *reinterpret_cast<const uint4*>(e);
-        }
-    }
+    for (int j = 0; j < NV; ++j) x[j] = fetch(j);
     if (tid == 0) count = 0;
     float vmax[NV], top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        vmax[j] = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) vmax[j] = fmaxf(vmax[j], Vec<T>::at(x[j], i));      // (NaN: passed over)
+        vmax[j] = fmaxf(Vec<T>::max_of(x[j]), -INFINITY);                                // (all NaN: none)
         top = fmaxf(top, vmax[j]);
     }
     {   // the warp's q largest lanes' maxima, one after another
@@ -138,42 +157,53 @@ __global__ void __launch_bounds__(BM_NT) k_beam_rows(BeamArgs a) {
     float s = 0.f;
     if (m > -INFINITY && m < INFINITY) {
         const float c = m * LOG2E;
-        float part[4] = {0.f, 0.f, 0.f, 0.f};
+        u64 part[2] = {0, 0};                             // two sums each
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j) {
+            // (hidden from the compiler once more: it would keep what it has unpacked from a vector in registers of their own)
+            asm volatile("" : "+r"(x[j].x), "+r"(x[j].y), "+r"(x[j].z), "+r"(x[j].w));
 #pragma unroll
-            for (int i = 0; i < VE; ++i) part[i & 3] += exp2_of(fmaf(Vec<T>::at(x[j], i), LOG2E, -c));
-        s = (part[0] + part[1]) + (part[2] + part[3]);
+            for (int i = 0; i < VE; i += 2) {
+                const u64 y = fma2(pair2(Vec<T>::at(x[j], i), Vec<T>::at(x[j], i + 1)), pair2(LOG2E, LOG2E), pair2(-c, -c));
+                part[i / 2 & 1] = add2(part[i / 2 & 1], pair2(exp2_of(lo2(y)), exp2_of(hi2(y))));
+            }
+        }
+        part[0] = add2(part[0], part[1]);
+        s = lo2(part[0]) + hi2(part[0]);
         if (s != s) {                                     // NaN weigh nothing
             s = 0.f;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < VE; ++i) s += fmaxf(exp2_of(fmaf(Vec<T>::at(x[j], i), LOG2E, -c)), 0.f);
+#pragma unroll 1
+            for (int j = 0; j < NV; ++j) {
+                const uint4 v = fetch(j);
+                for (int i = 0; i < VE; ++i) s += fmaxf(exp2_of(fmaf(Vec<T>::at(v, i), LOG2E, -c)), 0.f);
+            }
         }
     } else if (m == INFINITY) {                           // the infinite ones share the row
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < VE; ++i) s += Vec<T>::at(x[j], i) == INFINITY ? 1.f : 0.f;
+#pragma unroll 1
+        for (int j = 0; j < NV; ++j) {
+            const uint4 v = fetch(j);
+            for (int i = 0; i < VE; ++i) s += Vec<T>::at(v, i) == INFINITY ? 1.f : 0.f;
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == 0) w_sum[warp] = s;
-    // what is above the bound
+    // what is above the bound: few threads have any, and those read the vector once more (unrolled over all vectors the code ran out of the instruction cache)
     const float least = of_key(bound);
+    uint32_t have = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (vmax[j] >= least) {
+    for (int j = 0; j < NV; ++j) have |= vmax[j] >= least ? 1u << j : 0u;
+    for (uint32_t left = have; left; left &= left - 1) {
+        const int j = __ffs(left) - 1;
+        const uint4 v = fetch(j);
+        uint32_t hits = 0;
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                const float l = Vec<T>::at(x[j], i);
-                if (l >= least) {
-                    const int k = atomicAdd(&count, 1);
-                    if (k < BM_LIST) list[k] = entry(l, place(j, i));
-                }
-            }
+        for (int i = 0; i < VE; ++i) hits |= Vec<T>::at(v, i) >= least ? 1u << i : 0u;
+        for (; hits; hits &= hits - 1) {
+            const int i = __ffs(hits) - 1, k = atomicAdd(&count, 1);
+            if (k < BM_LIST) list[k] = entry(as_float(p[place(j, i)]), place(j, i));
         }
+    }
     __syncthreads();
     if (tid == 0) {
         float sum = 0.f;
@@ -197,15 +227,15 @@ __global__ void __launch_bounds__(BM_NT) k_beam_rows(BeamArgs a) {
     u64 last = ~0ull;
     for (int k = 0; k < a.n; ++k) {
         u64 best = 0;
+        for (uint32_t left = have; left; left &= left - 1) {
+            const int j = __ffs(left) - 1;
+            const uint4 v = fetch(j);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (vmax[j] >= least)
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    const float l = Vec<T>::at(x[j], i);
-                    const u64 e = entry(l, place(j, i));
-                    if (l >= least && e < last && e > best) best = e;
-                }
+            for (int i = 0; i < VE; ++i) {
+                const u64 e = entry(Vec<T>::at(v, i), place(j, i));
+                if (Vec<T>::at(v, i) >= least && e < last && e > best) best = e;
+            }
+        }
         best = warp_max(best);
         if (lane == 0) w_best[warp] = best;
         __syncthreads();
@@ -230,36 +260,24 @@ __device__ __forceinline__ double log_probability(const Beam& b, u64 e) {
     const float l = of_key((uint32_t)(e >> 32));
     return (l == b.top ? 0.0 : (double)l - (double)b.top) - b.ln_sum;
 }
-// The i-th candidate of a sentence: beam, stretch, place in its list.
-__device__ __forceinline__ bool candidate(const BeamArgs& a, const Beam* beams, int row0, int i, Candidate& c) {
-    const int per = a.stretches * a.n;
-    c.beam = i / per;
-    const Beam& b = beams[c.beam];
-    if (b.done == 2) return false;
-    if (b.done) {
-        if (i - c.beam * per) return false;
-        c.e = ~(uint32_t)a.end_token;
-        c.rank = b.score * b.norm;
-    } else {
-        c.e = a.lists[(long long)row0 * per + i];
-        if (!c.e) return false;
-        c.rank = (b.score + log_probability(b, c.e)) * b.norm;
-    }
-    return c.rank > -INFINITY;
-}
 
-// CTA = sentence.
+// CTA = sentence.  Its entries (K lists a stretch) are asked for at once, ahead of the sums.
 template <typename T>
-__global__ void __launch_bounds__(BM_NT) k_beam_join(BeamArgs a) {
+__global__ void __launch_bounds__(BJ_NT) k_beam_join(BeamArgs a) {
     __shared__ Beam beams[BM_MOST];
-    __shared__ Candidate list[BM_JOIN], sorted[BM_MOST + 1];
-    __shared__ uint32_t w_bound[BM_WARPS];
-    __shared__ double w_sum[BM_WARPS];
-    __shared__ Candidate w_best[BM_WARPS];
+    __shared__ u64 stage[BJ_STAGE];
+    __shared__ Candidate list[BJ_LIST], sorted[BM_MOST + 1], w_best[BJ_WARPS];
+    __shared__ uint32_t w_bound[BJ_WARPS];
+    __shared__ double w_sum[BJ_WARPS];
     __shared__ int count, again[BM_MOST];
     op_begin();
     const int b = blockIdx.x, row0 = b * a.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int k = warp; k < a.K; k += BM_WARPS) {          // the rows' sums
+    const int per = a.stretches * a.n, all = a.K * per;
+    const u64* lists = a.lists + (long long)row0 * per;
+    u64 mine_e[BJ_STAGE / BJ_NT];
+#pragma unroll
+    for (int j = 0; j < BJ_STAGE / BJ_NT; ++j) mine_e[j] = tid + j * BJ_NT < all ? lists[tid + j * BJ_NT] : 0;      // (rows that were not read leave anything: see candidate)
+    for (int k = warp; k < a.K; k += BJ_WARPS) {          // the rows' sums
         const int row = row0 + k;
         const float score = a.scores[row];
         Beam x{0.0, (double)score, a.norm ? (double)a.norm[row] : 1.0, -INFINITY, 0, a.finished && a.finished[row] ? 1 : 0};
@@ -278,53 +296,70 @@ __global__ void __launch_bounds__(BM_NT) k_beam_join(BeamArgs a) {
         }
         if (lane == 0) { beams[k] = x; again[k] = 0; }
     }
+#pragma unroll
+    for (int j = 0; j < BJ_STAGE / BJ_NT; ++j) stage[tid + j * BJ_NT] = mine_e[j];
     if (tid == 0) count = 0;
     __syncthreads();
+    auto candidate = [&](int i, Candidate& c) {           // the i-th: beam, stretch, place in its list
+        c.beam = i / per;
+        const Beam& x = beams[c.beam];
+        if (x.done) {
+            c.e = ~(uint32_t)a.end_token;
+            c.rank = x.score * x.norm;
+            if (x.done == 2 || i != c.beam * per) return false;
+        } else {
+            c.e = i < BJ_STAGE ? stage[i] : lists[i];
+            if (!c.e) return false;
+            c.rank = (x.score + log_probability(x, c.e)) * x.norm;
+        }
+        return c.rank > -INFINITY;
+    };
     // a bound below the n-th best, as in a row, by the upper halves of the ranks as ordered integers
-    const int all = a.K * a.stretches * a.n;
+    // (a thread takes entries from all over: neighbours are of one sorted list, and a warp of poor ones makes a poor bound)
     uint32_t mine = 0;
     Candidate c;
-    for (int i = tid; i < all; i += BM_NT) if (candidate(a, beams, row0, i, c)) mine = max(mine, (uint32_t)(ordered(c.rank) >> 32));
+    const int mixed = tid * 97 & (BJ_NT - 1);
+    for (int i = mixed; i < all; i += BJ_NT) if (candidate(i, c)) mine = max(mine, (uint32_t)(ordered(c.rank) >> 32));
     uint32_t bound = 0;
-    for (int q = (a.n + 1 + BM_WARPS - 1) / BM_WARPS; q; --q) {       // (the one behind the n-th is looked at too)
+    for (int q = (a.n + 1 + BJ_WARPS - 1) / BJ_WARPS; q; --q) {       // (the one behind the n-th is looked at too)
         bound = __reduce_max_sync(0xffffffffu, mine);
         const unsigned who = __ballot_sync(0xffffffffu, mine == bound);
         if (lane == __ffs(who) - 1) mine = 0;
     }
     double norm = 0.0;
-    for (int k = lane; k < a.K; k += 32) norm = fmax(norm, fabs(beams[k].norm));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) norm = fmax(norm, __shfl_xor_sync(0xffffffffu, norm, o));
+    for (int k = 0; k < a.K; ++k) norm = fmax(norm, fabs(beams[k].norm));
     if (lane == 0) w_bound[warp] = bound;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < BM_WARPS; ++w) bound = min(bound, w_bound[w]);
+    for (int w = 0; w < BJ_WARPS; ++w) bound = min(bound, w_bound[w]);
     double least = -INFINITY;
     if (bound) {
         const u64 u = (u64)bound << 32;
         least = __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) - 4 * NEAR * norm;       // (ranks may still move by as much)
     }
-    for (int i = tid; i < all; i += BM_NT)
-        if (candidate(a, beams, row0, i, c) && (!(c.rank < least))) {
+    for (int i = mixed; i < all; i += BJ_NT)
+        if (candidate(i, c) && !(c.rank < least)) {
             const int k = atomicAdd(&count, 1);
-            if (k < BM_JOIN) list[k] = c;
+            if (k < BJ_LIST) list[k] = c;
         }
     __syncthreads();
     const int found = count;
     int best_n = min(found, a.n + 1);                     // sorted ones
     for (int round = 0; round <= a.K; ++round) {
-        if (found <= BM_JOIN) {
-            for (int i = tid; i < found; i += BM_NT) {
-                const Candidate x = list[i];
+        if (found <= BJ_LIST) {
+            for (int i = tid / 8; i < (found + 3) / 4 * 4; i += BJ_NT / 8) {          // eight lanes an entry, whole warps
+                const Candidate x = list[min(i, found - 1)];
                 int rank = 0;
-                for (int j = 0; j < found; ++j) rank += ahead(list[j], x);
-                if (rank <= a.n) sorted[rank] = x;
+                for (int j = lane & 7; j < found; j += 8) rank += ahead(list[j], x);
+#pragma unroll
+                for (int o = 4; o; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+                if ((lane & 7) == 0 && i < found && rank <= a.n) sorted[rank] = x;
             }
         } else {                                          // (more ties than the list holds)
             for (int k = 0; k <= a.n; ++k) {
                 Candidate top{-INFINITY, 0, a.K};
-                for (int i = tid; i < all; i += BM_NT)
-                    if (candidate(a, beams, row0, i, c) && (k == 0 || ahead(sorted[k - 1], c)) && ahead(c, top)) top = c;
+                for (int i = tid; i < all; i += BJ_NT)
+                    if (candidate(i, c) && (k == 0 || ahead(sorted[k - 1], c)) && ahead(c, top)) top = c;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) {
                     const Candidate u{__shfl_xor_sync(0xffffffffu, top.rank, o), __shfl_xor_sync(0xffffffffu, top.e, o), __shfl_xor_sync(0xffffffffu, top.beam, o)};
@@ -333,7 +368,7 @@ __global__ void __launch_bounds__(BM_NT) k_beam_join(BeamArgs a) {
                 if (lane == 0) w_best[warp] = top;
                 __syncthreads();
                 if (tid == 0) {
-                    for (int w = 1; w < BM_WARPS; ++w) if (ahead(w_best[w], top)) top = w_best[w];
+                    for (int w = 1; w < BJ_WARPS; ++w) if (ahead(w_best[w], top)) top = w_best[w];
                     sorted[k] = top;
                 }
                 __syncthreads();
@@ -354,7 +389,7 @@ __global__ void __launch_bounds__(BM_NT) k_beam_join(BeamArgs a) {
             const T* p = (const T*)a.logits + (long long)(row0 + k) * a.s_row;
             const double top = beams[k].top;
             double s = 0.0;
-            for (int i = tid; i < a.V; i += BM_NT) {
+            for (int i = tid; i < a.V; i += BJ_NT) {
                 const float l = as_float(p[i]);
                 if (l == l) s += exp((double)l - top);
             }
@@ -363,13 +398,13 @@ __global__ void __launch_bounds__(BM_NT) k_beam_join(BeamArgs a) {
             if (lane == 0) w_sum[warp] = s;
             __syncthreads();
             if (tid == 0) {
-                for (int w = 1; w < BM_WARPS; ++w) s += w_sum[w];
+                for (int w = 1; w < BJ_WARPS; ++w) s += w_sum[w];
                 beams[k].ln_sum = log(s); beams[k].exact = 1;
             }
             __syncthreads();
         }
-        if (found <= BM_JOIN)
-            for (int i = tid; i < found; i += BM_NT) {
+        if (found <= BJ_LIST)
+            for (int i = tid; i < found; i += BJ_NT) {
                 const Beam& x = beams[list[i].beam];
                 if (!x.done) list[i].rank = (x.score + log_probability(x, list[i].e)) * x.norm;
             }
@@ -395,7 +430,8 @@ int vectors(long long rows, int V, int e) {
     for (int nv = 8; nv > 1; nv /= 2) if (rows * ((V + BM_NT * nv * (16 / e) - 1) / (BM_NT * nv * (16 / e))) >= 2 * 148) return nv;
     return 1;
 }
-int stretches(int nv, int V, int e) { const int per = BM_NT * nv * (16 / e); return (V + 16 / e - 1 + per - 1) / per; }       // (a row may begin inside a vector)
+// Stretches of a row whose first element is `lead` elements into a vector.
+int stretches(int nv, int V, int e, int lead) { const int per = BM_NT * nv * (16 / e); return (V + lead + per - 1) / per; }
 const char* why_not(int B, int K, int V, int n, int dtype) {
     if (B < 0 || K < 1 || V < 1 || n < 1) return "a size is below 1";
     if (!op_elem_bytes(dtype)) return "unknown dtype";
@@ -409,7 +445,7 @@ cudaError_t run(const BeamArgs& a, int nv, cudaStream_t st) {
     const dim3 grid(a.stretches, a.B * a.K);
     auto k = nv == 8 ? k_beam_rows<T, 8> : nv == 4 ? k_beam_rows<T, 4> : nv == 2 ? k_beam_rows<T, 2> : k_beam_rows<T, 1>;
     if (const cudaError_t e = op_launch(k, grid, BM_NT, 0, st, 1, a)) return e;
-    return op_launch(k_beam_join<T>, dim3(a.B), BM_NT, 0, st, 1, a);
+    return op_launch(k_beam_join<T>, dim3(a.B), BJ_NT, 0, st, 1, a);
 }
 
 }  // namespace
@@ -423,27 +459,32 @@ long long specdec_beam_select_workspace(int B, int K, int V, int n, int dtype) {
     if (const char* why = why_not(B, K, V, n, dtype)) return op_bad("beam_select_workspace", why);
     if (too_large(B, K, V, n)) return op_fail(SPECDEC_ERR_CAPACITY, "beam_select_workspace", LARGE);
     const int e = op_elem_bytes(dtype);
-    return (long long)B * K * stretches(vectors((long long)B * K, V, e), V, e) * (8 + 8LL * n);
+    return (long long)B * K * stretches(vectors((long long)B * K, V, e), V, e, 16 / e - 1) * (8 + 8LL * n);
 }
 
-int specdec_beam_select(const void* d_logits, int dtype, long long stride, int B, int K, int V, const float* d_scores, const unsigned char* d_finished, int end_token, const float* d_norm, int n,
-                        float* d_out_scores, int32_t* d_out_parent, int32_t* d_out_token, void* d_workspace, long long workspace_bytes, void* stream) {
+int specdec_beam_select(const specdec_beam_select_args* g, void* stream) {
     const char* who = "beam_select";
+    if (!g) return op_bad(who, "a pointer is NULL");
+    const int B = g->B, K = g->K, V = g->V, n = g->n, dtype = g->dtype;
     if (const char* why = why_not(B, K, V, n, dtype)) return op_bad(who, why);
     if (too_large(B, K, V, n)) return op_fail(SPECDEC_ERR_CAPACITY, who, LARGE);
     if (B == 0) return SPECDEC_OK;
-    if (!d_logits || !d_scores || !d_out_scores || !d_out_parent || !d_out_token) return op_bad(who, "a pointer is NULL");
+    if (!g->d_logits || !g->d_scores || !g->d_out_scores || !g->d_out_parent || !g->d_out_token) return op_bad(who, "a pointer is NULL");
     const int e = op_elem_bytes(dtype);
-    if ((uintptr_t)d_logits % e || stride < 0) return op_bad(who, "d_logits is not aligned to its type, or the stride is negative");
+    if ((uintptr_t)g->d_logits % e || g->stride < 0) return op_bad(who, "d_logits is not aligned to its type, or the stride is negative");
     const long long need = specdec_beam_select_workspace(B, K, V, n, dtype);
-    if (!d_workspace || (uintptr_t)d_workspace % 8 || workspace_bytes < need) return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_beam_select_workspace says, or not 8-byte aligned");
+    if (!g->d_workspace || (uintptr_t)g->d_workspace % 8 || g->workspace_bytes < need)
+        return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_beam_select_workspace says, or not 8-byte aligned");
     BeamArgs a;
     const int nv = vectors((long long)B * K, V, e);
-    a.logits = d_logits; a.s_row = op_stride(stride, B * K); a.V = V;
-    a.scores = d_scores; a.finished = d_finished; a.norm = d_norm;
-    a.end_token = end_token; a.B = B; a.K = K; a.n = n; a.stretches = stretches(nv, V, e);
-    a.out_scores = d_out_scores; a.out_parent = d_out_parent; a.out_token = d_out_token;
-    a.sums = (float2*)d_workspace; a.lists = (u64*)(a.sums + (long long)B * K * a.stretches);
+    a.logits = g->d_logits; a.s_row = op_stride(g->stride, B * K); a.V = V;
+    a.scores = g->d_scores; a.finished = g->d_finished; a.norm = g->d_norm;
+    a.end_token = g->end_token; a.B = B; a.K = K; a.n = n;
+    const int lead = ((uintptr_t)g->d_logits | (uintptr_t)(a.s_row * e)) % 16 ? 16 / e - 1 : 0, vecs = (V + lead + 16 / e - 1) / (16 / e);
+    a.stretches = stretches(nv, V, e, lead);
+    a.span = (vecs + a.stretches - 1) / a.stretches;      // (equal ones)
+    a.out_scores = g->d_out_scores; a.out_parent = g->d_out_parent; a.out_token = g->d_out_token;
+    a.sums = (float2*)g->d_workspace; a.lists = (u64*)(a.sums + (long long)B * K * a.stretches);
     const cudaStream_t st = (cudaStream_t)stream;
     return op_done(who, dtype == SPECDEC_DTYPE_F32 ? run<float>(a, nv, st) : dtype == SPECDEC_DTYPE_BF16 ? run<__nv_bfloat16>(a, nv, st) : run<__half>(a, nv, st));
 }
