@@ -453,7 +453,8 @@ constexpr int per_sm_of(int dtype, int dim, int rows) { return rows >= 128 ? 1 :
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
-    p.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
+    const int most_mma = head_dim > 64 ? 32 : 64;
+    p.rows = all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma || dtype == SPECDEC_DTYPE_F32 ? 64 : all <= 128 || !fp4_tc_fits(head_dim, 256, T, n_q_heads / n_kv_heads) ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
     p.min_blocks = 4;
@@ -551,7 +552,7 @@ int specdec_packed_attention(const specdec_packed_cache* f, const specdec_tree_a
     a.where = (int2*)(a.part_ml + p.slots * p.rows);
     const cudaStream_t s = (cudaStream_t)stream;
     const int grid = (int)p.grid;
-    cudaError_t rc = dtype == SPECDEC_DTYPE_F32 ? pick<float>(a, p.rows, grid, s) : dtype == SPECDEC_DTYPE_BF16 ? pick<__nv_bfloat16>(a, p.rows, grid, s) : pick<__half>(a, p.rows, grid, s);
+    cudaError_t rc = p.rows >= 128 ? fp4_tc(a, dtype, p.rows, grid, s) : dtype == SPECDEC_DTYPE_F32 ? pick<float>(a, p.rows, grid, s) : dtype == SPECDEC_DTYPE_BF16 ? pick<__nv_bfloat16>(a, p.rows, grid, s) : pick<__half>(a, p.rows, grid, s);
     if (rc == cudaSuccess && need) rc = ta_merge(a, dtype, p.rows, s);
     return op_done(who, rc);
 }

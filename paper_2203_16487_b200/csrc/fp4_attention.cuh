@@ -27,6 +27,7 @@ __device__ __forceinline__ int row_shift(float top) {
 }
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 .. 127
 
+bool fp4_tc_fits(int dim, int rows, int T, int group);                                    // whether the masks of a tile of 128 or 256 rows fit beside the rest (with 128 they always do)
 cudaError_t fp4_tc(const Fp4Attn& a, int dtype, int rows, int grid, cudaStream_t st);                                     // tiles of 128, 256 rows
 
 }  // namespace sd
