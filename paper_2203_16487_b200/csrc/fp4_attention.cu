@@ -1,39 +1,45 @@
 // Attention of drafted trees over a cache in 4 bits, few query rows: entry point, plan, mma.sync (contract: specdec.h, work: tree_attention.cuh).
 //
-// CTA = WM x WK consumer warps and one that loads.  A block of 64 keys is a stage of a ring: a bulk copy each of a page's codes and scales.  Warp (wm, wk) takes 16 rows and every WK-th block.
+// CTA = WM x WK consumer warps and one that loads.  A block of 64 keys is a stage of a ring: a bulk copy each of a page's codes and scales.  Warp (wm, wk) takes 8 NT rows and every WK-th block.
 // Codes become fp16 in the registers of the lane whose fragment they are part of: values are exact, and nothing of 16 bits passes through shared memory, whose bandwidth
 // (128 bytes a clock) is what a tile of fp16 in between would run into first (32 KB written and read for every 9 KB from HBM).
 //
-// Which channel and key stand where in a fragment is free as long as both operands agree:
-//   scores (m16n8k16, B = keys): a lane's channels are D / 4 that follow one another, so that its codes of a key are one load (8 or 16 bytes); the queries are loaded the same way.
-//   output (B = values): a lane's keys are those of its score columns, its columns D / 8 channels that follow one another; two keys' codes are paired by nibbles
-//     (a shift and a select for four pairs), converted, and multiplied by the two keys' scales.
-// Column c of eight keys is key c ^ (c >> 1 & 1) (D = 128) or c ^ (c >> 2 & 1) (D = 64): lanes that load together then hit different banks, or two lanes one.
+// The cache is the A operand of both products (m16n8k16: sixteen keys or channels), queries and probabilities are B, so that rows come in eights: a group of four query heads wastes half of a
+// fragment, not three quarters.  What is unpacked once serves NT products.  Which channel and key stand where in a fragment is free as long as both operands agree:
+//   scores: a lane's channels are D / 4 that follow one another, so that its codes of a key are one load (8 or 16 bytes); the queries are loaded the same way.
+//   output: a lane's keys are those of the probabilities' columns (the scores, transposed in eights by movmatrix), its channels D / 8 that follow one another; two keys' codes are paired by
+//     nibbles (a shift and a select for four pairs), converted, and multiplied by the two keys' scales.
+// Row c of eight keys is key c ^ (c >> 1 & 1) (D = 128) or c ^ (c >> 2 & 1) (D = 64): lanes that load values together then hit different banks, or two lanes one.
 //
-// Probabilities are fp16, 2^15 times their value: a weight 2^-29 of the largest is still a normal number, so that a hundred thousand small ones add up.
+// Probabilities are fp16, 2^15 times their value: a weight 2^-29 of the largest is still a normal number, so that a hundred thousand small ones add up.  Their sum is one more product, with ones:
+// of the rounded ones, so that the weights add up to 1.
 #include "fp4_attention.cuh"
 
 namespace sd {
 namespace {
 
 constexpr float P_SHIFT = 15.f;
-// Two numbers as fp16, and what the rounding left.
 __device__ __forceinline__ uint32_t half_pair(float x, float y) { return Half<__half>::pack(x, y); }
-__device__ __forceinline__ uint32_t rest_pair(float x, float y, uint32_t h) {
+__device__ __forceinline__ uint32_t rest_pair(float x, float y, uint32_t h) {             // what the rounding has left
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
     return Half<__half>::pack(x - f.x, y - f.y);
 }
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {                               // of 8 x 8 numbers, lane (g, t) has [g][2 t], [g][2 t + 1]
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 
-// Sixteen query rows of a warp: lane (g, t) = (lane / 4, lane % 4) holds rows g and g + 8, and of the output the channels D / 4 * t ...
-template <typename T, int D> struct Fp4Rows {
+// 8 NT query rows of a warp, lane (g, t) = (lane / 4, lane % 4).  It loads row g of each eight, and has scores and outputs of rows 2 t and 2 t + 1: of the output the channels D / 8 * g ...
+template <typename T, int D, int NT> struct Fp4Rows {
     static constexpr bool WIDE = sizeof(T) == 4;          // fp32: queries and probabilities in two parts
-    static constexpr int KK = D / 16, ND = D / 8, NK = TA_BLOCK / 8, PARTS = WIDE ? 2 : 1;
-    uint32_t q[PARTS][KK][4];
-    float o[ND][4], ma, mb, la, lb, sa, sb;               // s: scale of the row's scores
-    // Row `e` (0: g, 1: g + 8) from its channels at p; times: what its scores are multiplied by.
-    __device__ __forceinline__ void query(int e, const char* p, bool live, bool vec, float times) {
-        float x[D / 4];
+    static constexpr int KK = D / 16, MD = D / 16, MK = TA_BLOCK / 16, PARTS = WIDE ? 2 : 1;
+    uint32_t q[PARTS][NT][KK][2];
+    float o[NT][MD][4], l[NT][4], m[NT][2], s[NT][2];     // l: sums in [0], [1]; s: scale of the row's scores
+    // Eight rows: row g from this lane's channels at p; times: what scores are multiplied by.
+    __device__ __forceinline__ void query(int n, const char* p, bool live, bool vec, float times) {
         constexpr int N = D / 4;
+        float x[N];
         if (!live) {
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = 0.f;
@@ -74,116 +80,136 @@ template <typename T, int D> struct Fp4Rows {
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] *= f;
         }
-        (e ? sb : sa) = times * power2(-shift);
+        const float mine = times * power2(-shift);
+        s[n][0] = __shfl_sync(0xffffffffu, mine, (threadIdx.x & 3) * 8); s[n][1] = __shfl_sync(0xffffffffu, mine, (threadIdx.x & 3) * 8 + 4);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float u = x[4 * kk + 2 * i], w = x[4 * kk + 2 * i + 1];
-                q[0][kk][e + 2 * i] = half_pair(u, w);
-                if constexpr (WIDE) q[PARTS - 1][kk][e + 2 * i] = rest_pair(u, w, q[0][kk][e + 2 * i]);
+                q[0][n][kk][i] = half_pair(u, w);
+                if constexpr (WIDE) q[PARTS - 1][n][kk][i] = rest_pair(u, w, q[0][n][kk][i]);
             }
     }
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-        ma = mb = -INFINITY; la = lb = 0.f;
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < MD; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+            l[n][0] = l[n][1] = l[n][2] = l[n][3] = 0.f;
+            m[n][0] = m[n][1] = -INFINITY;
+        }
     }
     static __device__ __forceinline__ int key_of(int c) { return D == 128 ? c ^ (c >> 1 & 1) : c ^ (c >> 2 & 1); }
-    // One block at st; window_a, window_b(base): what the rows see of 32 keys, asked where the block holds nodes or ends behind the last key
-    template <typename WA, typename WB>
-    __device__ __forceinline__ void block(const char* st, bool tail, int base0, WA window_a, WB window_b) {
+    // One block at st; window(n, e, base): what row 2 t + e of the n-th eight sees of 32 keys, asked where the block holds nodes or ends behind the last key
+    template <typename W>
+    __device__ __forceinline__ void block(const char* st, bool tail, int base0, W window) {
         using Stage = Fp4Stage<D>;
-        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, x = D == 128 ? t & 1 : t >> 1;      // x: whether this lane's two columns are exchanged
-        float sc[NK][4];
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, x = D == 128 ? t & 1 : t >> 1;      // x: whether keys 2 t and 2 t + 1 are exchanged
+        float sc[NT][MK][4];
         const char* kc = st + key_of(g) * (D / 2) + t * (D / 8);
         const char* kq = st + Stage::KS + key_of(g) * (D / 16) + t * (D / 64);
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-            uint32_t w[D / 32], s2[2];
-            if constexpr (D == 128) {
-                const uint4 v = *reinterpret_cast<const uint4*>(kc + n * 8 * (D / 2));
-                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                const uint32_t s = fp4_scales2(*reinterpret_cast<const unsigned short*>(kq + n * 8 * (D / 16)));
-                s2[0] = __byte_perm(s, s, 0x1010); s2[1] = __byte_perm(s, s, 0x3232);
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2*>(kc + n * 8 * (D / 2));
-                w[0] = v.x; w[1] = v.y;
-                const uint32_t s = *reinterpret_cast<const unsigned char*>(kq + n * 8 * (D / 16));
-                s2[0] = s2[1] = fp4_scales2(s | s << 8);
+        for (int i = 0; i < MK; ++i) {
+            uint32_t w[2][D / 32], s2[2][2];              // [key g, g + 8 of sixteen]
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const char* c = kc + (i * 16 + e * 8) * (D / 2);
+                const char* z = kq + (i * 16 + e * 8) * (D / 16);
+                if constexpr (D == 128) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(c);
+                    w[e][0] = v.x; w[e][1] = v.y; w[e][2] = v.z; w[e][3] = v.w;
+                    const uint32_t f = fp4_scales2(*reinterpret_cast<const unsigned short*>(z));
+                    s2[e][0] = __byte_perm(f, f, 0x1010); s2[e][1] = __byte_perm(f, f, 0x3232);
+                } else {
+                    const uint2 v = *reinterpret_cast<const uint2*>(c);
+                    w[e][0] = v.x; w[e][1] = v.y;
+                    const uint32_t f = *reinterpret_cast<const unsigned char*>(z);
+                    s2[e][0] = s2[e][1] = fp4_scales2(f | f << 8);
+                }
             }
-            sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                uint32_t k[4];
-                fp4_unpack8(w[i], k);
+            for (int n = 0; n < NT; ++n) sc[n][i][0] = sc[n][i][1] = sc[n][i][2] = sc[n][i][3] = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = h2_mul(k[j], s2[D == 128 ? i >> 1 : 0]);
+            for (int j = 0; j < D / 32; ++j) {
+                uint32_t k[2][4];
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    Half<__half>::mma(sc[n], q[p][2 * i], k[0], k[1]);
-                    Half<__half>::mma(sc[n], q[p][2 * i + 1], k[2], k[3]);
+                for (int e = 0; e < 2; ++e) {
+                    fp4_unpack8(w[e][j], k[e]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) k[e][u] = h2_mul(k[e][u], s2[e][D == 128 ? j >> 1 : 0]);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t f[4] = {k[0][2 * h], k[1][2 * h], k[0][2 * h + 1], k[1][2 * h + 1]};
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) Half<__half>::mma(sc[n][i], f, q[p][n][2 * j + h][0], q[p][n][2 * j + h][1]);
                 }
             }
         }
-        if (tail) {
+        uint32_t pf[PARTS][NT][MK][2];
 #pragma unroll
-            for (int n = 0; n < TA_BLOCK / 32; ++n) {
-                const uint32_t wa = window_a(base0 + n * 32), wb = window_b(base0 + n * 32);
+        for (int n = 0; n < NT; ++n) {
+            if (tail) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int b0 = i * 8 + 2 * t + x, b1 = b0 ^ 1;
-                    float* c = sc[n * 4 + i];
-                    if (!(wa >> b0 & 1)) c[0] = -INFINITY;
-                    if (!(wa >> b1 & 1)) c[1] = -INFINITY;
-                    if (!(wb >> b0 & 1)) c[2] = -INFINITY;
-                    if (!(wb >> b1 & 1)) c[3] = -INFINITY;
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t w = window(n, e, base0 + h * 32) >> key_of(g);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            if (!(w >> (i * 16) & 1)) sc[n][2 * h + i][e] = -INFINITY;
+                            if (!(w >> (i * 16 + 8) & 1)) sc[n][2 * h + i][2 + e] = -INFINITY;
+                        }
+                    }
+            }
+            float top[2] = {-INFINITY, -INFINITY}, z[2], f[2] = {s[n][0], s[n][1]};
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                for (int i = 0; i < MK; ++i) top[e] = fmaxf(top[e], fmaxf(sc[n][i][e], sc[n][i][2 + e]));
+                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 4)); top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
+                top[e] = fmaxf(m[n][e], fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16)) * f[e]);
+            }
+            // Fused with the subtraction of their maximum, products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge they are rounded first.
+            if (__any_sync(0xffffffffu, fmaxf(fabsf(top[0]), fabsf(top[1])) > 1048576.f)) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int i = 0; i < MK; ++i) { sc[n][i][e] *= f[e]; sc[n][i][2 + e] *= f[e]; }
+                    f[e] = 1.f;
                 }
             }
-        }
-        // (scaled ahead of the maximum: fused with its subtraction, a product's own rounding would be left where scores are beyond 2^27)
-        float na = -INFINITY, nb = -INFINITY;
+            if (__any_sync(0xffffffffu, top[0] != m[n][0] || top[1] != m[n][1])) {
+                const float fa = ta_exp2(m[n][0] - (top[0] == -INFINITY ? 0.f : top[0])), fb = ta_exp2(m[n][1] - (top[1] == -INFINITY ? 0.f : top[1]));
+                l[n][0] *= fa; l[n][1] *= fb;
 #pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            sc[i][0] *= sa; sc[i][1] *= sa; sc[i][2] *= sb; sc[i][3] *= sb;
-            na = fmaxf(na, fmaxf(sc[i][0], sc[i][1])); nb = fmaxf(nb, fmaxf(sc[i][2], sc[i][3]));
-        }
-        na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 1)); na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 2));
-        nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
-        na = fmaxf(ma, na); nb = fmaxf(mb, nb);
-        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
-        if (__any_sync(0xffffffffu, na != ma || nb != mb)) {
-            const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
-            la *= fa; lb *= fb;
+                for (int i = 0; i < MD; ++i) { o[n][i][0] *= fa; o[n][i][1] *= fb; o[n][i][2] *= fa; o[n][i][3] *= fb; }
+                m[n][0] = top[0]; m[n][1] = top[1];
+            }
 #pragma unroll
-            for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
+            for (int e = 0; e < 2; ++e) z[e] = P_SHIFT - (top[e] == -INFINITY ? 0.f : top[e]);
+#pragma unroll
+            for (int i = 0; i < MK; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float u = ta_exp2(fmaf(sc[n][i][2 * h], f[0], z[0])), v = ta_exp2(fmaf(sc[n][i][2 * h + 1], f[1], z[1]));
+                    const uint32_t y = half_pair(u, v);
+                    pf[0][n][i][h] = transpose8(y);
+                    if constexpr (WIDE) pf[PARTS - 1][n][i][h] = transpose8(rest_pair(u, v, y));
+                }
         }
-        ma = na; mb = nb;
         const char* vc = st + Stage::V + (2 * t) * (D / 2) + g * (D / 16);
         const char* vq = st + Stage::VS + (2 * t) * (D / 16) + g * (D / 16) / 8;
 #pragma unroll
-        for (int n = 0; n < TA_BLOCK / 16; ++n) {
-            uint32_t pf[PARTS][4];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float* c = sc[2 * n + e];
-                c[0] = ta_exp2(c[0] - za + P_SHIFT); c[1] = ta_exp2(c[1] - za + P_SHIFT);
-                c[2] = ta_exp2(c[2] - zb + P_SHIFT); c[3] = ta_exp2(c[3] - zb + P_SHIFT);
-                pf[0][2 * e] = half_pair(c[0], c[1]);
-                pf[0][2 * e + 1] = half_pair(c[2], c[3]);
-                if constexpr (WIDE) {
-                    pf[PARTS - 1][2 * e] = rest_pair(c[0], c[1], pf[0][2 * e]);
-                    pf[PARTS - 1][2 * e + 1] = rest_pair(c[2], c[3], pf[0][2 * e + 1]);
-                    la += c[0] + c[1]; lb += c[2] + c[3];
-                } else {                                  // (the sum adds up the rounded ones: the weights add up to 1)
-                    la = Half<__half>::add(la, pf[0][2 * e]); lb = Half<__half>::add(lb, pf[0][2 * e + 1]);
-                }
-            }
+        for (int i = 0; i < MK; ++i) {
             // keys 2 t + x and 2 t + 1 - x of each eight
             uint32_t w[2][2][D / 64], s2[2];              // [eight][key][word]
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int r0 = n * 16 + e * 8 + x, r1 = n * 16 + e * 8 + 1 - x;
+                const int r0 = i * 16 + e * 8 + x, r1 = i * 16 + e * 8 + 1 - x;
                 if constexpr (D == 128) {
                     const uint2 u = *reinterpret_cast<const uint2*>(vc + r0 * (D / 2)), v = *reinterpret_cast<const uint2*>(vc + r1 * (D / 2));
                     w[e][0][0] = u.x; w[e][0][1] = u.y; w[e][1][0] = v.x; w[e][1][1] = v.y;
@@ -192,122 +218,137 @@ template <typename T, int D> struct Fp4Rows {
                 }
                 s2[e] = fp4_scales2(*reinterpret_cast<const unsigned char*>(vq + r0 * (D / 16)) | (uint32_t)*reinterpret_cast<const unsigned char*>(vq + r1 * (D / 16)) << 8);
             }
+            const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {            // eight channels
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) Half<__half>::mma(l[n], ones, pf[p][n][i][0], pf[p][n][i][1]);
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {            // eight channels
                 uint32_t b[2][2][4];                      // [eight keys][even, odd channels][pair]
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t u = w[e][0][i], v = w[e][1][i];
+                    const uint32_t u = w[e][0][j], v = w[e][1][j];
                     fp4_unpack8((u & 0x0f0f0f0fu) | (v << 4 & 0xf0f0f0f0u), b[e][0]);
                     fp4_unpack8((u >> 4 & 0x0f0f0f0fu) | (v & 0xf0f0f0f0u), b[e][1]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) { b[e][0][j] = h2_mul(b[e][0][j], s2[e]); b[e][1][j] = h2_mul(b[e][1][j], s2[e]); }
+                    for (int h = 0; h < 4; ++h) { b[e][0][h] = h2_mul(b[e][0][h], s2[e]); b[e][1][h] = h2_mul(b[e][1][h], s2[e]); }
                 }
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p)
+                for (int h = 0; h < 4; ++h) {             // channels 2 h and 2 h + 1 of them
+                    const uint32_t f[4] = {b[0][0][h], b[0][1][h], b[1][0][h], b[1][1][h]};
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) Half<__half>::mma(o[8 * i + j], pf[p], b[0][j & 1][j >> 1], b[1][j & 1][j >> 1]);
+                    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) Half<__half>::mma(o[n][4 * j + h], f, pf[p][n][i][0], pf[p][n][i][1]);
+                }
             }
         }
     }
-    // The lanes' sums together.  A query behind the nodes has taken the committed keys of blocks without a mask; one that sees nothing has multiplied values by 0.
-    __device__ __forceinline__ void finish(bool live_a, bool live_b, float unit) {
-        la += __shfl_xor_sync(0xffffffffu, la, 1); la += __shfl_xor_sync(0xffffffffu, la, 2);
-        lb += __shfl_xor_sync(0xffffffffu, lb, 1); lb += __shfl_xor_sync(0xffffffffu, lb, 2);
-        const bool none_a = !live_a || la == 0.f, none_b = !live_b || lb == 0.f;
-        if (none_a) { ma = -INFINITY; la = 0.f; }
-        if (none_b) { mb = -INFINITY; lb = 0.f; }
+    // A query behind the nodes has taken the committed keys of blocks without a mask; one that sees nothing has multiplied values by 0.
+    template <typename L>
+    __device__ __forceinline__ void finish(L live, float unit) {
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            o[i][0] = none_a ? 0.f : o[i][0] * unit; o[i][1] = none_a ? 0.f : o[i][1] * unit;
-            o[i][2] = none_b ? 0.f : o[i][2] * unit; o[i][3] = none_b ? 0.f : o[i][3] * unit;
-        }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const bool none = !live(n, e) || l[n][e] == 0.f;
+                if (none) { m[n][e] = -INFINITY; l[n][e] = 0.f; }
+#pragma unroll
+                for (int i = 0; i < MD; ++i) { o[n][i][e] = none ? 0.f : o[n][i][e] * unit; o[n][i][2 + e] = none ? 0.f : o[n][i][2 + e] * unit; }
+            }
     }
-    // This lane's D / 4 channels of row e, in order.
-    __device__ __forceinline__ float channel(int e, int i) const { return i < ND ? o[i][2 * e] : o[i - ND][2 * e + 1]; }
-    // Partial results in shared memory: rows of RP floats, and (maximum, sum) of each.
+    // This lane's D / 8 channels of a row, in order.
+    __device__ __forceinline__ float channel(int n, int e, int i) const { return o[n][i / 2][(i & 1) * 2 + e]; }
+    // Partial results in shared memory: rows of RP floats from row r0 on, and (maximum, sum) of each.
     static constexpr int RP = D + 4;
-    __device__ __forceinline__ void leave(float* red, float2* red_ml, int ra) const {
-        const int t = threadIdx.x & 3;
+    __device__ __forceinline__ void leave(float* red, float2* red_ml, int r0) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float* p = red + (ra + 8 * e) * RP + t * (D / 4);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < D / 4; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(channel(e, i), channel(e, i + 1), channel(e, i + 2), channel(e, i + 3));
-            if (t == 0) red_ml[ra + 8 * e] = make_float2(e ? mb : ma, e ? lb : la);
-        }
-    }
-    __device__ __forceinline__ void join(const float* red, const float2* red_ml, int ra) {
-        const float2 xa = red_ml[ra], xb = red_ml[ra + 8];
-        const float na = fmaxf(ma, xa.x), nb = fmaxf(mb, xb.x);
-        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
-        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb), ea = ta_exp2(xa.x - za), eb = ta_exp2(xb.x - zb);
-        ma = na; mb = nb;
-        la = la * fa + xa.y * ea; lb = lb * fb + xb.y * eb;
-        const float* pa = red + ra * RP + (threadIdx.x & 3) * (D / 4);
+            for (int e = 0; e < 2; ++e) {
+                const int r = r0 + n * 8 + 2 * t + e;
+                float* p = red + r * RP + g * (D / 8);
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            o[i][0] = o[i][0] * fa + pa[i] * ea; o[i][1] = o[i][1] * fa + pa[ND + i] * ea;
-            o[i][2] = o[i][2] * fb + pa[8 * RP + i] * eb; o[i][3] = o[i][3] * fb + pa[8 * RP + ND + i] * eb;
-        }
-    }
-    // Rows ra and ra + 8 of a tile of `rows` that begins at query row r0: the output, or the part's partial results.
-    __device__ __forceinline__ void store(const TreeAttn& a, const Part& it, int r0, int ra, int rows) const {
-        const int t = threadIdx.x & 3;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = ra + 8 * e, gr = r0 + r;
-            const float l = e ? lb : la;
-            if (gr >= a.T * a.group) continue;
-            if (!it.whole) {
-                const long long slot = it.slot * rows + r;
-                float* p = a.part + slot * D + t * (D / 4);
-#pragma unroll
-                for (int i = 0; i < D / 4; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(channel(e, i), channel(e, i + 1), channel(e, i + 2), channel(e, i + 3));
-                if (t == 0) a.part_ml[slot] = make_float2(e ? mb : ma, l);
-                continue;
+                for (int i = 0; i < D / 8; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(channel(n, e, i), channel(n, e, i + 1), channel(n, e, i + 2), channel(n, e, i + 3));
+                if (g == 0) red_ml[r] = make_float2(m[n][e], l[n][e]);
             }
-            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-            const int node = ta_node(a, gr);
-            char* p = a.out + it.b * a.o_sb + node * a.o_st + (it.h * a.group + gr - node * a.group) * a.o_sh + t * (D / 4) * (int)sizeof(T);
-            if constexpr (WIDE) {
+    }
+    __device__ __forceinline__ void join(const float* red, const float2* red_ml, int r0) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
-                for (int i = 0; i < D / 4; i += 4) {
-                    const float4 v = make_float4(channel(e, i) * inv, channel(e, i + 1) * inv, channel(e, i + 2) * inv, channel(e, i + 3) * inv);
-                    float* f = reinterpret_cast<float*>(p) + i;
-                    if (a.out_vec) *reinterpret_cast<float4*>(f) = v;
-                    else { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = r0 + n * 8 + 2 * t + e;
+                const float2 y = red_ml[r];
+                const float top = fmaxf(m[n][e], y.x), z = top == -INFINITY ? 0.f : top, f = ta_exp2(m[n][e] - z), h = ta_exp2(y.x - z);
+                m[n][e] = top; l[n][e] = l[n][e] * f + y.y * h;
+                const float* p = red + r * RP + g * (D / 8);
+#pragma unroll
+                for (int i = 0; i < MD; ++i) { o[n][i][e] = o[n][i][e] * f + p[2 * i] * h; o[n][i][2 + e] = o[n][i][2 + e] * f + p[2 * i + 1] * h; }
+            }
+    }
+    // Rows w0 ... of a tile of `rows` that begins at query row r0: the output, or the part's partial results.
+    __device__ __forceinline__ void store(const TreeAttn& a, const Part& it, int r0, int w0, int rows) const {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        constexpr int N = D / 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = w0 + n * 8 + 2 * t + e, gr = r0 + r;
+                if (gr >= a.T * a.group) continue;
+                if (!it.whole) {
+                    const long long slot = it.slot * rows + r;
+                    float* p = a.part + slot * D + g * N;
+#pragma unroll
+                    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(channel(n, e, i), channel(n, e, i + 1), channel(n, e, i + 2), channel(n, e, i + 3));
+                    if (g == 0) a.part_ml[slot] = make_float2(m[n][e], l[n][e]);
+                    continue;
                 }
-            } else {
+                const float inv = l[n][e] > 0.f || l[n][e] != l[n][e] ? 1.f / l[n][e] : 0.f;
+                const int node = ta_node(a, gr);
+                char* p = a.out + it.b * a.o_sb + node * a.o_st + (it.h * a.group + gr - node * a.group) * a.o_sh + g * N * (int)sizeof(T);
+                if constexpr (WIDE) {
 #pragma unroll
-                for (int i = 0; i < D / 4; i += 8) {
-                    uint32_t w[4];
+                    for (int i = 0; i < N; i += 4) {
+                        const float4 v = make_float4(channel(n, e, i) * inv, channel(n, e, i + 1) * inv, channel(n, e, i + 2) * inv, channel(n, e, i + 3) * inv);
+                        float* f = reinterpret_cast<float*>(p) + i;
+                        if (a.out_vec) *reinterpret_cast<float4*>(f) = v;
+                        else { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+                    }
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = Half<T>::pack(channel(e, i + 2 * j) * inv, channel(e, i + 2 * j + 1) * inv);
-                    unsigned short* f = reinterpret_cast<unsigned short*>(p) + i;
-                    if (a.out_vec) *reinterpret_cast<uint4*>(f) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else
+                    for (int i = 0; i < N; i += 8) {
+                        uint32_t w[4];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) f[j] = (unsigned short)(w[j / 2] >> (j & 1) * 16);
+                        for (int j = 0; j < 4; ++j) w[j] = Half<T>::pack(channel(n, e, i + 2 * j) * inv, channel(n, e, i + 2 * j + 1) * inv);
+                        unsigned short* f = reinterpret_cast<unsigned short*>(p) + i;
+                        if (a.out_vec) *reinterpret_cast<uint4*>(f) = make_uint4(w[0], w[1], w[2], w[3]);
+                        else
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) f[j] = (unsigned short)(w[j / 2] >> (j & 1) * 16);
+                    }
                 }
             }
-        }
     }
 };
 
 // Group wk has the stages wk, wk + WK, ... to itself and so waits for every phase of their barriers.
-template <typename T, int D, int WM, int WK, int NS, int PER_SM>
+template <typename T, int D, int NT, int WM, int WK, int NS, int PER_SM>
 __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn a) {
     static_assert(NS % WK == 0, "a stage serves one group");
     using Stage = Fp4Stage<D>;
-    constexpr int WARPS = WM * WK, NG = NS / WK, ROWS = 16 * WM, KT = TA_BLOCK, STAGE = Stage::BYTES;
+    constexpr int WARPS = WM * WK, NG = NS / WK, ROWS = 8 * NT * WM, KT = TA_BLOCK, STAGE = Stage::BYTES;
     extern __shared__ __align__(128) char fp4_smem[];
     __shared__ __align__(8) uint64_t bars[2 * NS];
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, left_in[WK];               // stage that holds a group's partial results
     char* ring = fp4_smem;
     int4* seqs = (int4*)(ring + NS * STAGE);              // [B] where sequences are cut
     uint32_t* any = (uint32_t*)(seqs + (a.direct == 1 ? 0 : a.B));
-    uint32_t* mask = any + (a.words + 3) / 4 * 4;         // (16-byte aligned, as the partial results behind it are)
+    uint32_t* mask = any + a.words;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t full = smem_u32(bars), empty = full + NS * 8;
     if (warp == WARPS && lane == 0) {
@@ -322,42 +363,41 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
 
     if (warp == WARPS) {                                  // loads, running ahead into the next parts
         const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
+        // What a lane copies of a block: lane / 4-th page's codes of keys, of values, scales of keys, of values
+        const int page_of = lane >> 2;
+        const bool scales = lane & 2, values = lane & 1;
+        const char* base = scales ? (values ? a.vs : a.ks) : values ? a.v : a.k;
+        const long long s_page = scales ? a.c_page : a.s_page, s_head = scales ? a.c_head : a.s_head;
+        const int size = box * (scales ? D / 16 : D / 2), at = (scales ? Stage::KS : 0) + (values ? (scales ? Stage::SCALES : Stage::V) : 0) + page_of * size;
         int count = 0;                                    // lane g: blocks that group g had in the parts before
         Part it, ahead;
-        for (bool more = work.next(a, seqs, ahead); more;) {
+        // This lane's page of the 32 from the b0-th of a part on; -1 where there is none.  Asked for 32 at a time and well ahead: a lookup a block, waited for, is 0.7 us a block.
+        auto pages_of = [&](const Part& part, int b0) {
+            const int key = part.k_begin + (b0 + lane) * box, i = key >> a.page_shift;
+            int p = -1;
+            if (key < part.k_end && i < a.max_pages) p = a.table[(long long)part.s.seq * a.max_pages + i];
+            return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+        };
+        bool more = work.next(a, seqs, ahead);
+        int first = more ? pages_of(ahead, 0) : 0;
+        while (more) {
             it = ahead;
-            const int* table = a.table + (long long)it.s.seq * a.max_pages;
-            auto page_of = [&](int j) {                   // this lane's page of block j: -1 where there is none
-                const int key = it.k_begin + j * KT + lane * box, i = key >> a.page_shift;
-                int p = -1;
-                if (lane < n_pages && key < it.k_end && i < a.max_pages) p = table[i];
-                return (unsigned)p < (unsigned)a.n_pages ? p : -1;
-            };
-            int p = it.blocks ? page_of(0) : 0;
+            int now = first, then = pages_of(it, 32);
             more = work.next(a, seqs, ahead);
+            if (more) first = pages_of(ahead, 0);
             for (int j = 0; j < it.blocks; ++j) {
-                const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), key = it.k_begin + j * KT + lane * box, cur = p;
-                if (j + 1 < it.blocks) p = page_of(j + 1);
+                const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), b0 = j * n_pages, key = it.k_begin + (b0 + page_of) * box;
+                if (b0 && b0 % 32 == 0) { now = then; then = pages_of(it, b0 + 32); }
+                const int cur = __shfl_sync(0xffffffffu, now, (b0 + page_of) % 32);
                 if (n >= NG && !mbar_wait_warp<true>(empty + st * 8, (n / NG - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
-                char* to = ring + st * STAGE;
-                const bool mine = lane < n_pages && key < it.k_end;
-                if (mine && cur < 0)                      // a page that is none: zeros
-                    for (int i = 0; i < box * D / 16; i += 16) {
-                        *reinterpret_cast<uint4*>(to + Stage::KS + lane * box * (D / 16) + i) = make_uint4(0, 0, 0, 0);
-                        *reinterpret_cast<uint4*>(to + Stage::VS + lane * box * (D / 16) + i) = make_uint4(0, 0, 0, 0);
-                    }
-                const unsigned boxes = __popc(__ballot_sync(0xffffffffu, mine && cur >= 0));
-                if (lane == 0) mbar_expect_tx(full + st * 8, boxes * box * (D + D / 8));
+                char* to = ring + st * STAGE + at;
+                const bool mine = lane < 4 * n_pages && key < it.k_end, real = mine && cur >= 0;
+                if (mine && cur < 0 && scales)            // a page that is none: zeros
+                    for (int i = 0; i < size; i += 16) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
+                const unsigned pieces = __popc(__ballot_sync(0xffffffffu, real));          // four a page
+                if (lane == 0) mbar_expect_tx(full + st * 8, pieces / 4 * box * (D + D / 8));
                 __syncwarp();
-                if (mine && cur >= 0) {
-                    const int first = key & (page - 1);
-                    const long long codes = cur * a.s_page + it.h * a.s_head + first * (D / 2), scales = cur * a.c_page + it.h * a.c_head + first * (D / 16);
-                    const uint32_t d = smem_u32(to) + lane * box * (D / 2), s = smem_u32(to) + Stage::KS + lane * box * (D / 16), bar = full + st * 8;
-                    bulk_copy(d, a.k + codes, box * (D / 2), bar);
-                    bulk_copy(s, a.ks + scales, box * (D / 16), bar);
-                    bulk_copy(d + Stage::V, a.v + codes, box * (D / 2), bar);
-                    bulk_copy(s + Stage::SCALES, a.vs + scales, box * (D / 16), bar);
-                }
+                if (real) bulk_copy(smem_u32(to), base + cur * s_page + it.h * s_head + (key & (page - 1)) * (scales ? D / 16 : D / 2), size, full + st * 8);
             }
             count += (it.blocks - lane + WK - 1) / WK;    // (lanes below WK)
         }
@@ -372,21 +412,24 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
         it = ahead;
         more = work.next(a, seqs, ahead, tid == 0);
         const SeqKeys& s = it.s;
-        const int r0 = it.tile * ROWS, t0 = ta_node(a, r0);
-        const int ra = wm * 16 + (lane >> 2), rb = ra + 8;
-        const int ga = r0 + ra, gb = r0 + rb, ta = ta_node(a, ga), tb = ta_node(a, gb);
-        const bool live_a = ga < all_rows && ta < s.nodes, live_b = gb < all_rows && tb < s.nodes;
-        Fp4Rows<T, D> rows;
-        {
-            const float times = a.unit_k ? a.scale * a.unit_k[it.h] : a.scale;
-            const int c = (lane & 3) * (D / 4) * (int)sizeof(T);
-            rows.query(0, a.q + it.b * a.q_sb + ta * a.q_st + (it.h * a.group + ga - ta * a.group) * a.q_sh + c, live_a, a.q_vec, times);
-            rows.query(1, a.q + it.b * a.q_sb + tb * a.q_st + (it.h * a.group + gb - tb * a.group) * a.q_sh + c, live_b, a.q_vec, times);
+        const int r0 = it.tile * ROWS, t0 = ta_node(a, r0), w0 = wm * 8 * NT;
+        Fp4Rows<T, D, NT> rows;
+        auto live = [&](int n, int e) {                   // this lane's rows
+            const int gr = r0 + w0 + n * 8 + 2 * (lane & 3) + e;
+            return gr < all_rows && ta_node(a, gr) < s.nodes;
+        };
+        const float times = a.unit_k ? a.scale * a.unit_k[it.h] : a.scale;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int gr = r0 + w0 + n * 8 + (lane >> 2), node = ta_node(a, gr);
+            rows.query(n, a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + (lane & 3) * (D / 4) * (int)sizeof(T), gr < all_rows && node < s.nodes, a.q_vec, times);
         }
         // What the rows see, and the nodes that anyone sees.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for
         // another; more: in shared memory.
         const bool own = a.words <= 2;
-        uint32_t ma[2] = {0, 0}, mb[2] = {0, 0}, seen[2] = {0, 0};
+        uint32_t see[NT][2][2], seen[2] = {0, 0};         // [row][word]
+#pragma unroll
+        for (int n = 0; n < NT; ++n) see[n][0][0] = see[n][0][1] = see[n][1][0] = see[n][1][1] = 0;
         if (own) {
             const uint32_t* words = a.mask + it.b * a.mask_sb;
 #pragma unroll
@@ -396,18 +439,21 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
                 const uint32_t cut = left < 32 ? (1u << left) - 1u : 0xffffffffu;
                 uint32_t all = lane < s.nodes ? words[lane * a.words + w] : 0u;
                 if (lane + 32 < s.nodes) all |= words[(lane + 32) * a.words + w];
-                if (live_a) ma[w] = words[ta * a.words + w] & cut;
-                if (live_b) mb[w] = words[tb * a.words + w] & cut;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) if (live(n, e)) see[n][e][w] = words[ta_node(a, r0 + w0 + n * 8 + 2 * (lane & 3) + e) * a.words + w] & cut;
                 seen[w] = __reduce_or_sync(0xffffffffu, all) & cut;
             }
         } else {
             ta_load_masks<32 * WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
         }
-        const uint32_t* mask_a = mask + (live_a ? ta - t0 : 0) * a.words;
-        const uint32_t* mask_b = mask + (live_b ? tb - t0 : 0) * a.words;
-        auto window_a = [&](int base) { return !live_a ? 0u : own ? ta_window2(ma[0], ma[1], base) : ta_window(mask_a, a.words, base); };
-        auto window_b = [&](int base) { return !live_b ? 0u : own ? ta_window2(mb[0], mb[1], base) : ta_window(mask_b, a.words, base); };
+        auto window = [&](int n, int e, int base) {
+            if (!live(n, e)) return 0u;
+            return own ? ta_window2(see[n][e][0], see[n][e][1], base) : ta_window(mask + (ta_node(a, r0 + w0 + n * 8 + 2 * (lane & 3) + e) - t0) * a.words, a.words, base);
+        };
         rows.clear();
+        int left = -1;
         for (int j = wk; j < it.blocks; j += WK, ++count) {
             const int st = wk + WK * (count % NG), k0 = it.k_begin + j * KT;
             if (!mbar_wait_warp<true>(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
@@ -425,36 +471,49 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
                 if constexpr (WM == 1) __syncwarp();
                 else asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "n"(32 * WM) : "memory");
             }
-            rows.block(at, tail, k0 - s.len, window_a, window_b);
+            rows.block(at, tail, k0 - s.len, window);
             if (tail) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the zeros, ahead of the stage's next copies
             __syncwarp();
-            if (lane == 0) mbar_arrive(empty + st * 8);
+            if (WK > 1 && wk > 0 && j + WK >= it.blocks) left = st;                    // (the group's last block here: its place is taken by the partial results)
+            else if (lane == 0) mbar_arrive(empty + st * 8);
         }
-        rows.finish(live_a, live_b, a.unit_v ? a.unit_v[it.h] : 1.f);
-        if constexpr (WK > 1) {                           // the groups' results meet in the first group
-            constexpr int RP = Fp4Rows<T, D>::RP;
-            float* red = reinterpret_cast<float*>(mask + (ROWS * a.words + 3) / 4 * 4);      // [ROWS][RP], then [ROWS] (maximum, sum): one group's at a time, so that more CTAs fit an SM
-            float2* red_ml = reinterpret_cast<float2*>(red + ROWS * RP);
-            for (int g = 1; g < WK; ++g) {
-                if (wk == g) rows.leave(red, red_ml, ra);
-                consumers();
-                if (wk == 0) rows.join(red, red_ml, ra);
-                if (g + 1 < WK) consumers();
+        rows.finish(live, a.unit_v ? a.unit_v[it.h] : 1.f);
+        if constexpr (WK > 1) {                           // the groups' results meet in the first group: [ROWS][RP] floats, then [ROWS] (maximum, sum), in a stage of each group
+            constexpr int RP = Fp4Rows<T, D, NT>::RP;
+            static_assert(ROWS * (RP * 4 + 8) <= STAGE, "a stage holds a group's partial results");
+            if (wk > 0) {
+                if (WM > 1) asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "n"(32 * WM) : "memory");       // (the group's other warps may still read it)
+                if (left >= 0) { float* red = reinterpret_cast<float*>(ring + left * STAGE); rows.leave(red, reinterpret_cast<float2*>(red + ROWS * RP), w0); }
+                if (wm == 0 && lane == 0) left_in[wk] = left;
             }
+            consumers();
+            if (wk == 0)
+                for (int g = 1; g < WK; ++g)
+                    if (left_in[g] >= 0) { const float* red = reinterpret_cast<const float*>(ring + left_in[g] * STAGE); rows.join(red, reinterpret_cast<const float2*>(red + ROWS * RP), w0); }
         }
-        if (wk == 0) rows.store(a, it, r0, ra, ROWS);
+        if (wk == 0) rows.store(a, it, r0, w0, ROWS);
         if (WK > 1 || !own) consumers();                  // masks and partial results may be overwritten
+        if (WK > 1 && left >= 0) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + left * 8);
+        }
     }
 }
 
 // ------------------------------------------------------------------ host
 struct Plan { int rows, tiles, per_sm, direct, ctas, unit, min_blocks; long long grid, slots; };       // see TreeAttn; slots of partial results
-constexpr int per_sm_of(int dtype, int dim, int rows) { return rows >= 128 ? 1 : dim == 128 || dtype == SPECDEC_DTYPE_F32 ? 2 : 3; }
+// CTAs that an SM holds, as pick has them.
+constexpr int per_sm_of(int dtype, int dim, int rows) {
+    if (rows >= 128) return 1;
+    if (dtype == SPECDEC_DTYPE_F32) return dim > 64 ? (rows == 64 ? 1 : 2) : rows == 8 ? 3 : 2;
+    return rows == 8 ? (dim > 64 ? 3 : 4) : dim > 64 ? 2 : 3;
+}
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
     const int most_mma = head_dim > 64 ? 32 : 64;
-    p.rows = all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma || dtype == SPECDEC_DTYPE_F32 ? 64 : all <= 128 || !fp4_tc_fits(head_dim, 256, T, n_q_heads / n_kv_heads) ? 128 : 256;
+    p.rows = all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma || dtype == SPECDEC_DTYPE_F32 ? 64 : all <= 128 || !fp4_tc_fits(head_dim, 256, T, n_q_heads / n_kv_heads) ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
     p.unit = p.rows >= 128 ? 128 : TA_BLOCK;
     p.min_blocks = 4;
@@ -477,19 +536,23 @@ long long workspace(const Plan& p, int B, int n_kv_heads, int head_dim) {
     return p.direct ? 0 : part_floats(p, head_dim) * 4 + p.slots * p.rows * 8 + (long long)B * n_kv_heads * p.tiles * 8;
 }
 
-template <typename T, int D, int WM, int WK, int NS, int PER_SM>
+template <typename T, int D, int NT, int WM, int WK, int NS, int PER_SM>
 cudaError_t run(const Fp4Attn& a, int grid, cudaStream_t st) {
-    constexpr int ROWS = 16 * WM, RED = (WK > 1) * ROWS * (Fp4Rows<T, D>::RP * 4 + 8);
-    auto bytes = [](int words, int B) { return NS * Fp4Stage<D>::BYTES + RED + ((words + 3) / 4 + (ROWS * words + 3) / 4) * 16 + B * 16; };
-    static_assert(NS * Fp4Stage<D>::BYTES + RED + (ROWS + 1) * 128 + TA_MAX_B * 16 + 1024 <= 232448 / PER_SM, "shared memory of an SM");
-    if (const cudaError_t e = op_allow<k_fp4_mma<T, D, WM, WK, NS, PER_SM>>(bytes(32, TA_MAX_B))) return e;
-    return op_launch(k_fp4_mma<T, D, WM, WK, NS, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 32 * (WM * WK + 1), bytes(a.words, a.direct == 1 ? 0 : a.B), st, 1, a);
+    constexpr int ROWS = 8 * NT * WM, WORDS = ROWS < 64 ? 1 : 32;                      // words of a mask at most (smaller tiles are chosen where one holds the tree)
+    auto bytes = [](int words, int B) { return NS * Fp4Stage<D>::BYTES + (ROWS + 1) * words * 4 + B * 16; };
+    static_assert(NS * Fp4Stage<D>::BYTES + (ROWS + 1) * WORDS * 4 + TA_MAX_B * 16 + 1024 + 512 <= 233472 / PER_SM, "shared memory of an SM");
+    if (const cudaError_t e = op_allow<k_fp4_mma<T, D, NT, WM, WK, NS, PER_SM>>(bytes(WORDS, TA_MAX_B))) return e;
+    return op_launch(k_fp4_mma<T, D, NT, WM, WK, NS, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 32 * (WM * WK + 1), bytes(a.words, a.direct == 1 ? 0 : a.B), st, 1, a);
 }
 template <typename T>
 cudaError_t pick(const Fp4Attn& a, int rows, int grid, cudaStream_t st) {
-    constexpr int P = sizeof(T) == 4 ? 2 : 3;
-    if (a.dim > 64) return rows == 16 ? run<T, 128, 1, 3, 9, 2>(a, grid, st) : rows == 32 ? run<T, 128, 2, 2, 8, 2>(a, grid, st) : run<T, 128, 4, 1, 6, 2>(a, grid, st);
-    return rows == 16 ? run<T, 64, 1, 4, 8, P>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 8, P>(a, grid, st) : run<T, 64, 4, 1, 6, P>(a, grid, st);
+    if constexpr (sizeof(T) == 4) {
+        if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 3, 9, 2>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 8, 2>(a, grid, st) : rows == 32 ? run<T, 128, 1, 4, 1, 6, 2>(a, grid, st) : run<T, 128, 1, 8, 1, 8, 1>(a, grid, st);
+        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 3>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 2>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 2>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 2>(a, grid, st);
+    } else {
+        if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 4, 8, 3>(a, grid, st) : rows == 16 ? run<T, 128, 2, 1, 3, 9, 2>(a, grid, st) : run<T, 128, 2, 2, 1, 8, 2>(a, grid, st);
+        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 3>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 3>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 3>(a, grid, st);
+    }
 }
 
 }  // namespace
