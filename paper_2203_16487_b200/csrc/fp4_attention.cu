@@ -424,33 +424,26 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
             const int gr = r0 + w0 + n * 8 + (lane >> 2), node = ta_node(a, gr);
             rows.query(n, a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + (lane & 3) * (D / 4) * (int)sizeof(T), gr < all_rows && node < s.nodes, a.q_vec, times);
         }
-        // What the rows see, and the nodes that anyone sees.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for
-        // another; more: in shared memory.
+        // The nodes that anyone sees.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for another; more: in shared memory.
         const bool own = a.words <= 2;
-        uint32_t see[NT][2][2], seen[2] = {0, 0};         // [row][word]
-#pragma unroll
-        for (int n = 0; n < NT; ++n) see[n][0][0] = see[n][0][1] = see[n][1][0] = see[n][1][1] = 0;
+        uint32_t seen[2] = {0, 0};
+        const uint32_t* words = a.mask + it.b * a.mask_sb;
         if (own) {
-            const uint32_t* words = a.mask + it.b * a.mask_sb;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const int left = s.nodes - w * 32;
                 if (w >= a.words || left <= 0) break;
-                const uint32_t cut = left < 32 ? (1u << left) - 1u : 0xffffffffu;
                 uint32_t all = lane < s.nodes ? words[lane * a.words + w] : 0u;
                 if (lane + 32 < s.nodes) all |= words[(lane + 32) * a.words + w];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) if (live(n, e)) see[n][e][w] = words[ta_node(a, r0 + w0 + n * 8 + 2 * (lane & 3) + e) * a.words + w] & cut;
-                seen[w] = __reduce_or_sync(0xffffffffu, all) & cut;
+                seen[w] = __reduce_or_sync(0xffffffffu, all) & (left < 32 ? (1u << left) - 1u : 0xffffffffu);
             }
         } else {
             ta_load_masks<32 * WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
         }
-        auto window = [&](int n, int e, int base) {
+        auto window = [&](int n, int e, int base) {       // (a row's own words: from the first-level cache, where they are from a moment ago; in registers they cost more)
             if (!live(n, e)) return 0u;
-            return own ? ta_window2(see[n][e][0], see[n][e][1], base) : ta_window(mask + (ta_node(a, r0 + w0 + n * 8 + 2 * (lane & 3) + e) - t0) * a.words, a.words, base);
+            const int node = ta_node(a, r0 + w0 + n * 8 + 2 * (lane & 3) + e);
+            return own ? ta_window2(words[node * a.words] & seen[0], a.words > 1 ? words[node * a.words + 1] & seen[1] : 0u, base) : ta_window(mask + (node - t0) * a.words, a.words, base);
         };
         rows.clear();
         int left = -1;

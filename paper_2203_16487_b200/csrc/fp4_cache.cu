@@ -1,7 +1,7 @@
 // Tokens into and out of a K/V cache in 4 bits (contract: specdec.h, format: fp4.cuh).
 //
-// A thread takes the sixteen channels of a scale: 32 or 64 bytes in, 8 bytes of codes and one of scales out (read: the reverse).  Threads run along a head's tokens, so that a
-// warp's codes and scales are whole stretches of a page.
+// CTA = up to 64 tokens of a sequence, one layer, keys or values: their slots are looked up once, then a thread takes the sixteen channels of a scale at a time, two of them on their way:
+// 32 or 64 bytes in, 8 bytes of codes and one of scales out (read: the reverse).  Threads run along a head's tokens, so that a warp's codes and scales are whole stretches of a page.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -70,98 +70,118 @@ template <typename T> __device__ __forceinline__ void store16(char* p, const flo
     }
 }
 
-// What one thread does: sequence, layer and side of its CTA; head, token, block of its own.
-template <int D> struct Item { int i, s, layer, side, h, t, b; };
-template <int D> __device__ __forceinline__ bool item_of(const Fp4Io& a, Item<D>& m) {
-    constexpr int NB = D / FP4_BLOCK;
-    const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    m.b = (int)(u % NB);
-    const long long v = u / NB;
-    m.t = (int)(v % a.T);
-    m.h = (int)(v / a.T);
-    m.i = blockIdx.y; m.layer = blockIdx.z >> 1; m.side = blockIdx.z & 1;
-    m.s = a.seqs[m.i];
-    return v < (long long)a.heads * a.T;
-}
+constexpr int TOKENS = 64;
 
-// Division by the scale: a 16-bit x has at most 11 significant bits and a halfway point between codes times a scale at most 7, so x / s lies on such a point or at least 2^-13 beside it (points
-// from 0.25 on).  The product with 1 / s is off by less than 2^-20; rounded to a multiple of 2^-15 it lies on the point, or on the same side of it, as the quotient does.  That is a product and
-// two sums in place of a division.  Other x are divided.
-template <typename T, int D, bool UNIT>
-__global__ void __launch_bounds__(256) k_fp4_append(Fp4Io a) {
-    op_begin();
-    Item<D> m;
-    if (!item_of(a, m)) return;
-    const bool known = (unsigned)m.s < (unsigned)a.n_seqs;
-    if (a.some && m.t >= a.some[m.i]) return;
-    const int pos = known ? a.length[m.s] + m.t : 0, p = known ? page_at(a, m.s, pos, true) : -1;
-    if (p < 0) { if (m.b == 0 && m.h == 0) atomicOr(a.status, known ? SPECDEC_CACHE_UNRESERVED : SPECDEC_CACHE_BAD_INDEX); return; }
-    float x[16];
-    load16<T>(a.x[m.side] + m.layer * a.x_layer + m.i * a.x_seq + m.t * a.x_token + m.h * a.x_head + m.b * 16 * (int)sizeof(T), x);
-    if (UNIT) {
-        const float unit = a.unit[(m.layer * 2 + m.side) * a.heads + m.h];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], unit);
-    }
+__device__ __forceinline__ float bits16(float x) { return __uint_as_float((__float_as_uint(x) + 0x80u) & 0xffffff00u); }         // rounded to 16 significant bits
+
+// Sixteen numbers to codes and a scale.
+// EXACT: by division.  Else x has at most 11 significant bits (a 16-bit type), and the two quotients are taken as products, whose errors are rounded away: a point halfway between scales has 5
+// significant bits, and six times it 7; a point halfway between codes (from 0.25 on) times a scale has 7.  So a quotient lies on such a point, or at least 2^-13 of itself beside it.  The products
+// with 1 / 6 and 1 / s are off by less than 2^-21; rounded to 16 bits they lie on the point, or on the same side of it, as the quotient does.
+template <bool EXACT> __device__ __forceinline__ uint2 pack16(float* x, uint32_t& scale) {
     float top = 0.f;
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < 16; ++i) { top = fmaxf(top, fabsf(x[i])); nan |= x[i] != x[i]; }
-    const uint32_t scale = nan ? 0x7fu : fp4_scale_of(__fdiv_rn(top, 6.f));
+    scale = nan ? 0x7fu : fp4_scale_of(EXACT ? __fdiv_rn(top, 6.f) : bits16(top * (1.f / 6.f)));
     const uint32_t s2 = fp4_scales2(scale);
     const float s = __half2float(__low2half(*reinterpret_cast<const __half2*>(&s2)));
-    if (scale == 0) {
+    if (EXACT) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    } else if (UNIT || sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], s);
+        for (int i = 0; i < 16; ++i) x[i] = scale ? __fdiv_rn(x[i], s) : 0.f;
     } else {
-        const float r = __fdiv_rn(1.f, s), grid = 384.f;  // (sums from 256 to 512 are multiples of 2^-15; beyond 6.4, where x is beyond 2688, the code is 6's all the same)
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+        if (!scale) r = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = copysignf(__fsub_rn(__fadd_rn(fabsf(x[i] * r), grid), grid), x[i]);
+        for (int i = 0; i < 16; ++i) x[i] = bits16(x[i] * r);
     }
-    const int t = pos & ((1 << a.page_shift) - 1);
-    const uint2 w = make_uint2(fp4_pack8(x), fp4_pack8(x + 8));
-    *reinterpret_cast<uint2*>(a.codes + m.layer * a.s_layer + m.side * a.s_side + p * a.s_page + m.h * a.s_head + t * (D / 2) + m.b * 8) = w;
-    *reinterpret_cast<unsigned char*>(a.scales + m.layer * a.c_layer + m.side * a.c_side + p * a.c_page + m.h * a.c_head + t * (D / 16) + m.b) = (unsigned char)scale;
+    return make_uint2(fp4_pack8(x), fp4_pack8(x + 8));
 }
 
-template <typename T, int D, bool UNIT>
-__global__ void __launch_bounds__(256) k_fp4_read(Fp4Io a) {
+template <bool READ, typename T, int D, bool UNIT>
+__global__ void __launch_bounds__(256) k_fp4_move(Fp4Io a) {
+    constexpr int NB = D / FP4_BLOCK, U = sizeof(T) == 4 ? 1 : 2;
+    __shared__ int slot_page[TOKENS], slot_at[TOKENS];    // page (-1: none), place in it
     op_begin();
-    Item<D> m;
-    if (!item_of(a, m)) return;
-    const bool known = (unsigned)m.s < (unsigned)a.n_seqs;
-    if (!known && m.b == 0 && m.h == 0) atomicOr(a.status, SPECDEC_CACHE_BAD_INDEX);
-    const long long at = known ? (long long)(a.some ? a.some[m.i] : a.length[m.s]) + m.t : -1;
-    const int pos = at > 0x7fffffff ? -1 : (int)at, p = known ? page_at(a, m.s, pos, false) : -1;
-    float x[16];
+    const int i = blockIdx.y, layer = blockIdx.z >> 1, side = blockIdx.z & 1, t0 = blockIdx.x * TOKENS, s = a.seqs[i];
+    const bool known = (unsigned)s < (unsigned)a.n_seqs;
+    const int n = min(TOKENS, (!READ && a.some ? min(a.some[i], a.T) : a.T) - t0);
+    if (n <= 0) return;
+    int lost = known ? 0 : SPECDEC_CACHE_BAD_INDEX;
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+        const long long at = known ? (long long)(READ && a.some ? a.some[i] : a.length[s]) + t0 + j : -1;
+        const int pos = at > 0x7fffffff ? -1 : (int)at, p = known ? page_at(a, s, pos, !READ) : -1;
+        slot_page[j] = p; slot_at[j] = pos & ((1 << a.page_shift) - 1);
+        if (!READ && known && p < 0) lost = SPECDEC_CACHE_UNRESERVED;
+    }
+    if (lost) atomicOr(a.status, lost);
+    __syncthreads();
+    char* x0 = a.x[side] + layer * a.x_layer + i * a.x_seq + t0 * a.x_token;
+    char* codes = a.codes + layer * a.s_layer + side * a.s_side;
+    char* scales = a.scales + layer * a.c_layer + side * a.c_side;
+    const float* units = UNIT ? a.unit + (layer * 2 + side) * a.heads : nullptr;
+    const int b = threadIdx.x % NB, step = blockDim.x / NB;
+    int t = threadIdx.x / NB, h = 0;
+    auto settle = [&] { while (t >= n && h < a.heads) { t -= n; ++h; } };
+    settle();
+    while (h < a.heads) {
+        int tt[U], hh[U];
+        float x[U][16];
+        uint2 w[U];
+        uint32_t z[U];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (p >= 0) {
-        const int t = pos & ((1 << a.page_shift) - 1);
-        const uint2 w = *reinterpret_cast<const uint2*>(a.codes + m.layer * a.s_layer + m.side * a.s_side + p * a.s_page + m.h * a.s_head + t * (D / 2) + m.b * 8);
-        const uint32_t scale = *reinterpret_cast<const unsigned char*>(a.scales + m.layer * a.c_layer + m.side * a.c_side + p * a.c_page + m.h * a.c_head + t * (D / 16) + m.b);
-        const uint32_t s2 = fp4_scales2(scale | scale << 8);
-        uint32_t o[8];
-        fp4_unpack8(w.x, o); fp4_unpack8(w.y, o + 4);
-        const float unit = UNIT ? a.unit[(m.layer * 2 + m.side) * a.heads + m.h] : 1.f;
+        for (int u = 0; u < U; ++u) {                     // what is read
+            tt[u] = t; hh[u] = h < a.heads ? h : -1;
+            t += step;
+            settle();
+            if (hh[u] < 0) continue;
+            if (READ) {
+                const int p = slot_page[tt[u]], at = slot_at[tt[u]];
+                w[u] = make_uint2(0, 0); z[u] = 0;
+                if (p >= 0) {
+                    w[u] = *reinterpret_cast<const uint2*>(codes + p * a.s_page + hh[u] * a.s_head + at * (D / 2) + b * 8);
+                    z[u] = *reinterpret_cast<const unsigned char*>(scales + p * a.c_page + hh[u] * a.c_head + at * (D / 16) + b);
+                }
+            } else {
+                load16<T>(x0 + tt[u] * a.x_token + hh[u] * a.x_head + b * 16 * (int)sizeof(T), x[u]);
+            }
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t v = h2_mul(o[i], s2);          // exact
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
-            x[2 * i] = UNIT ? f.x * unit : f.x; x[2 * i + 1] = UNIT ? f.y * unit : f.y;
+        for (int u = 0; u < U; ++u) {
+            if (hh[u] < 0) continue;
+            if constexpr (READ) {
+                const uint32_t s2 = fp4_scales2(z[u] | z[u] << 8);
+                const float unit = UNIT ? units[hh[u]] : 1.f;
+                uint32_t o[8];
+                fp4_unpack8(w[u].x, o); fp4_unpack8(w[u].y, o + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t v = h2_mul(o[e], s2);  // exact
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+                    x[u][2 * e] = UNIT ? f.x * unit : f.x; x[u][2 * e + 1] = UNIT ? f.y * unit : f.y;
+                }
+                store16<T>(x0 + tt[u] * a.x_token + hh[u] * a.x_head + b * 16 * (int)sizeof(T), x[u]);
+            } else {
+                const int p = slot_page[tt[u]], at = slot_at[tt[u]];
+                if (UNIT) {
+                    const float unit = units[hh[u]];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[u][e] = __fdiv_rn(x[u][e], unit);
+                }
+                uint32_t scale;
+                const uint2 y = pack16<UNIT || sizeof(T) == 4>(x[u], scale);
+                if (p < 0) continue;
+                *reinterpret_cast<uint2*>(codes + p * a.s_page + hh[u] * a.s_head + at * (D / 2) + b * 8) = y;
+                *reinterpret_cast<unsigned char*>(scales + p * a.c_page + hh[u] * a.c_head + at * (D / 16) + b) = (unsigned char)scale;
+            }
         }
     }
-    store16<T>(a.x[m.side] + m.layer * a.x_layer + m.i * a.x_seq + m.t * a.x_token + m.h * a.x_head + m.b * 16 * (int)sizeof(T), x);
 }
 
-template <bool READ, typename T, int D> auto kernel(bool unit) {
-    if constexpr (READ) return unit ? k_fp4_read<T, D, true> : k_fp4_read<T, D, false>;
-    else return unit ? k_fp4_append<T, D, true> : k_fp4_append<T, D, false>;
+template <bool READ, typename T> auto kernel(int dim, bool unit) {
+    return dim == 64 ? (unit ? k_fp4_move<READ, T, 64, true> : k_fp4_move<READ, T, 64, false>) : unit ? k_fp4_move<READ, T, 128, true> : k_fp4_move<READ, T, 128, false>;
 }
-template <bool READ, typename T> auto kernel(int dim, bool unit) { return dim == 64 ? kernel<READ, T, 64>(unit) : kernel<READ, T, 128>(unit); }
 
 template <bool READ>
 int move(const char* who, const specdec_packed_cache* f, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int dtype, int T, long long stride_layer,
@@ -187,11 +207,12 @@ int move(const char* who, const specdec_packed_cache* f, const int32_t* d_seqs, 
     a.unit = f->d_unit ? f->d_unit + (long long)layer * 2 * c->n_heads : nullptr;
     a.table = c->d_table; a.length = c->d_length; a.held = c->d_held; a.refs = c->d_refs; a.seqs = d_seqs; a.some = d_some; a.status = c->d_status;
     a.n_pages = c->n_pages; a.n_seqs = c->n_seqs; a.max_pages = c->max_pages; a.page_shift = __builtin_ctz(c->page_tokens); a.heads = c->n_heads; a.T = T;
-    const long long ctas = ((long long)c->n_heads * T * (c->head_dim / FP4_BLOCK) + 255) / 256;
-    if (ctas > 0x7fffffff) return op_fail(SPECDEC_ERR_CAPACITY, who, "too many tokens for one launch");
+    const int tokens = T < TOKENS ? T : TOKENS;
+    const long long items = (long long)c->n_heads * tokens * (c->head_dim / FP4_BLOCK);
+    const int threads = items > 128 ? 256 : items > 64 ? 128 : items > 32 ? 64 : 32;
     const bool unit = a.unit != nullptr;
     auto k = dtype == SPECDEC_DTYPE_F32 ? kernel<READ, float>(c->head_dim, unit) : dtype == SPECDEC_DTYPE_BF16 ? kernel<READ, __nv_bfloat16>(c->head_dim, unit) : kernel<READ, __half>(c->head_dim, unit);
-    return op_done(who, op_launch(k, dim3((unsigned)ctas, n, 2 * n_layers), 256, 0, (cudaStream_t)stream, 1, a));
+    return op_done(who, op_launch(k, dim3((T + TOKENS - 1) / TOKENS, n, 2 * n_layers), threads, 0, (cudaStream_t)stream, 1, a));
 }
 
 }  // namespace
