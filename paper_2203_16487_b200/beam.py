@@ -62,12 +62,13 @@ def select(logits, scores, n: int, *, finished=None, end_token: int = 0, norm=No
         if len(_workspaces) > 4096:
             _workspaces.clear()
         _workspaces[B, K, V, n, code] = size
-    out, m = torch.empty((B, n), dtype=torch.float32, device=logits.device), B * n
-    rest = torch.empty(2 * (m + 1) + size // 4, dtype=_I32, device=logits.device)       # parents, tokens, workspace (8-byte aligned)
-    p = rest.data_ptr()
-    parent, token = rest.as_strided((B, n), (n, 1)), rest.as_strided((B, n), (n, 1), m)
+    m = B * n
+    all_ = scores.new_empty(3 * m)                           # scores, parents, tokens
+    p, ints = all_.data_ptr(), all_.view(_I32)
+    out, parent, token = all_.as_strided((B, n), (n, 1)), ints.as_strided((B, n), (n, 1), m), ints.as_strided((B, n), (n, 1), 2 * m)
+    ws = scores.new_empty(size // 4)
     try:
-        a = _args.pack(logits.data_ptr(), p_scores, p_finished, p_norm, out.data_ptr(), p, p + 4 * m, p + 8 * m, size, stride, code, B, K, V, n, end_token)
+        a = _args.pack(logits.data_ptr(), p_scores, p_finished, p_norm, p, p + 4 * m, p + 8 * m, ws.data_ptr(), size, stride, code, B, K, V, n, end_token)
     except struct.error as e:
         raise ValueError(f"end_token: {e}") from None
     _launch(lib.specdec_beam_select, at, (a, tree._raw_stream(at)))

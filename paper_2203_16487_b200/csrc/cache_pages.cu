@@ -437,34 +437,145 @@ __global__ void __launch_bounds__(CP_ALLOC_THREADS) k_reorder_take(Cache c, Beam
     if (ok) for (int r = threadIdx.x; r < run; r += CP_ALLOC_THREADS) c.refs[c.sc_pages()[r]] = 1;
     if (threadIdx.x == 0) { c.sc_ok()[0] = ok; c.sc_ok()[1] = ok ? run : 0; if (!ok) atomicOr(c.status, SPECDEC_CACHE_NO_PAGES); }
 }
-// 2 of 2: CTAs that stay write the entries' tables (without pages: undo the references), then take shares of the copies there are.
-template <int LIES>
-__global__ void __launch_bounds__(256) k_reorder_copy(Cache c, Beams b, int sides, int splits) {
+constexpr int REORDER_ONE = 160 * 1024;
+// ... where counts and tables fit into the shared memory of one CTA: everything but the copies.  Nothing is written until it is known that there are pages enough.
+__global__ void __launch_bounds__(CP_ALLOC_THREADS) k_reorder_one(Cache c, Beams b) {
+    extern __shared__ int one_smem[];
+    __shared__ int warp_sums[32], s_seq[CP_ALLOC_THREADS], s_held[CP_ALLOC_THREADS], s_len[CP_ALLOC_THREADS], s_up[CP_ALLOC_THREADS], s_used[CP_ALLOC_THREADS], s_full[CP_ALLOC_THREADS],
+        s_new[CP_ALLOC_THREADS];                          // (n <= 1024) up: as parent_of has it; full: place of the page that is copied, -1: none; new: the pages given out
+    int* refs = one_smem;
+    int* rows = refs + c.n_pages;                         // [n][max_pages]: the tables as they were
     op_begin();
-    const bool ok = c.sc_ok()[0];
-    const int jobs = c.sc_ok()[1], pt = 1 << c.page_shift;
-    for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
-        const int len = c.sc_pair()[2 * i];
-        if (len < 0) continue;
-        const int d = b.seqs[i], full = len >> c.page_shift, used = full + ((len & (pt - 1)) != 0), held = c.held_of(d), p = parent_of(c, b, i);
-        const bool copies = c.sc_pair()[2 * i + 1];
-        const int* row = c.sc_rows() + (long long)i * c.max_pages;
-        int* table = c.table + (long long)d * c.max_pages;
-        if (!ok) {
-            if (p != i) for (int j = threadIdx.x; j < (copies ? full : used); j += blockDim.x) if (c.page_ok(row[j])) atomicAdd(c.refs + row[j], -1);
-            for (int j = (p == i ? used : 0) + threadIdx.x; j < held; j += blockDim.x) if (c.page_ok(table[j])) atomicAdd(c.refs + table[j], 1);
-            continue;
-        }
-        const int page = copies ? c.sc_pages()[c.sc_first()[i]] : -1;
-        __syncthreads();                                  // every thread has read held[d]
-        for (int j = (p == i ? used : 0) + threadIdx.x; j < max(used, held); j += blockDim.x) table[j] = j >= used ? -1 : j == full && copies ? page : row[j];
-        if (threadIdx.x == 0) { c.length[d] = len; c.held[d] = used; }
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pt = 1 << c.page_shift, cells = b.n * c.max_pages;
+    bool bad = false;
+    if (tid < b.n) {
+        s_up[tid] = parent_of(c, b, tid, &bad);
+        const int s = b.seqs[tid];
+        s_seq[tid] = s;
+        s_held[tid] = 0;
+        if (c.seq_ok(s)) { s_held[tid] = c.held_of(s); s_len[tid] = committed(c, s); }
     }
-    const long long all = (long long)jobs * sides * splits;
-    for (long long w = blockIdx.x; w < all; w += gridDim.x) {
-        const int job = (int)(w / (sides * splits)), r = (int)(w % (sides * splits)), i = c.sc_jobs()[job], len = c.sc_pair()[2 * i];
-        const int from = c.sc_rows()[(long long)i * c.max_pages + (len >> c.page_shift)];
-        if (c.page_ok(from)) copy_part<LIES>(c, r / splits, from, c.sc_pages()[job], len & (pt - 1), r % splits, splits);
+#pragma unroll 4
+    for (int p = tid; p < c.n_pages; p += CP_ALLOC_THREADS) refs[p] = c.refs[p];
+    if (__syncthreads_or(bad) && tid == 0) atomicOr(c.status, SPECDEC_CACHE_BAD_INDEX);
+#pragma unroll 4
+    for (int x = tid; x < cells; x += CP_ALLOC_THREADS) {
+        const int i = x / c.max_pages, j = x - i * c.max_pages;
+        rows[x] = j < s_held[i] ? c.table[(long long)s_seq[i] * c.max_pages + j] : -1;
+    }
+    int copy = 0;                                         // whether entry tid copies its parent's last page
+    if (tid < b.n) {
+        const int p = s_up[tid], len = p >= 0 ? s_len[p] : 0, g = tid - tid % b.beams;
+        bool first = true;
+        if (p >= 0 && p != tid) for (int j = g; j < g + b.beams; ++j) first &= !((j < tid || j == p) && s_up[j] == p);
+        copy = (len & (pt - 1)) && !first;
+        s_used[tid] = (len + pt - 1) >> c.page_shift;
+        s_full[tid] = copy ? len >> c.page_shift : -1;
+    }
+    __syncthreads();
+    for (int x = tid; x < cells; x += CP_ALLOC_THREADS) { // references: from the old pages to the parent's
+        const int i = x / c.max_pages, j = x - i * c.max_pages, p = s_up[i];
+        if (p == NO_ENTRY) continue;
+        if (j < s_held[i] && (p != i || j >= s_used[i]) && c.page_ok(rows[x])) atomicAdd(refs + rows[x], -1);
+        if (p >= 0 && p != i && j < s_used[i] && j != s_full[i]) { const int y = rows[p * c.max_pages + j]; if (c.page_ok(y)) atomicAdd(refs + y, 1); }
+    }
+    __syncthreads();
+    // The lowest free pages: each warp counts, then lists, those of its own stretch.  One scan for both counts: copies, and (lane 0) free pages.
+    const int per = ((c.n_pages + 31) / 32 + 31) / 32 * 32, lo = min(warp * per, c.n_pages), hi = min(lo + per, c.n_pages);
+    int n = 0;
+    for (int p = lo + lane; p < hi; p += 32) n += refs[p] == 0;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+    int all;
+    const int upto = cta_scan(copy << 20 | (lane == 0 ? n : 0), warp_sums, &all);
+    const int total = all >> 20, rank = (upto >> 20) - copy, free_pages = all & 0xfffff;
+    const bool ok = free_pages >= total;
+    if (tid == 0) { c.sc_ok()[1] = ok ? total : 0; if (!ok) atomicOr(c.status, SPECDEC_CACHE_NO_PAGES); }
+    if (!ok) return;
+    int at = (__shfl_sync(0xffffffffu, upto, 0) & 0xfffff) - n;
+    for (int p0 = lo; p0 < hi && at < total; p0 += 32) {
+        const int p = p0 + lane;
+        const bool f = p < hi && refs[p] == 0;
+        const unsigned m = __ballot_sync(0xffffffffu, f);
+        const int r = at + __popc(m & ((1u << lane) - 1));
+        if (f && r < total) { c.sc_pages()[r] = p; s_new[r] = p; refs[p] = 1; }
+        at += __popc(m);
+    }
+    __syncthreads();
+    if (copy) {                                           // entry tid's new page, and what is copied to it
+        const int p = s_up[tid];
+        c.sc_pair()[2 * rank] = rows[p * c.max_pages + s_full[tid]]; c.sc_pair()[2 * rank + 1] = s_len[p] & (pt - 1);
+        c.table[(long long)s_seq[tid] * c.max_pages + s_full[tid]] = s_new[rank];
+    }
+    for (int p = tid; p < c.n_pages; p += CP_ALLOC_THREADS) c.refs[p] = refs[p];
+    if (tid < b.n && s_up[tid] != NO_ENTRY) { c.held[s_seq[tid]] = s_used[tid]; c.length[s_seq[tid]] = s_up[tid] == NOBODY ? 0 : s_len[s_up[tid]]; }
+    for (int x = tid; x < cells; x += CP_ALLOC_THREADS) { // the tables
+        const int i = x / c.max_pages, j = x - i * c.max_pages, p = s_up[i], used = s_used[i];
+        if (p == NO_ENTRY || j == s_full[i] || j >= max(used, s_held[i]) || (p == i && j < used)) continue;
+        c.table[(long long)s_seq[i] * c.max_pages + j] = j < used ? rows[p * c.max_pages + j] : -1;
+    }
+}
+
+// Pieces [lo, hi) by a warp, eight of a lane's on their way at a time.
+template <typename P, typename At>
+__device__ __forceinline__ void copy_pieces_warp(const char* a, char* b, int lo, int hi, At at) {
+    for (int u0 = lo + (threadIdx.x & 31); u0 < hi; u0 += 256) {
+        P x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (u0 + j * 32 < hi) x[j] = *reinterpret_cast<const P*>(a + at(u0 + j * 32));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (u0 + j * 32 < hi) *reinterpret_cast<P*>(b + at(u0 + j * 32)) = x[j];
+    }
+}
+// 2 of 2: CTAs that stay.  The entries' tables (without pages: the references undone), unless k_reorder_one has written them; then copies, 256 pieces (4 KB) of a layer and side, of 4 bits
+// of one head, a warp.
+template <int LIES, bool ONE>
+__global__ void __launch_bounds__(256) k_reorder_copy(Cache c, Beams b, int sides) {
+    op_begin();
+    const int jobs = c.sc_ok()[1], pt = 1 << c.page_shift;
+    if constexpr (!ONE) {
+        const bool ok = c.sc_ok()[0];
+        for (int i = blockIdx.x; i < b.n; i += gridDim.x) {
+            const int len = c.sc_pair()[2 * i];
+            if (len < 0) continue;
+            const int d = b.seqs[i], full = len >> c.page_shift, used = full + ((len & (pt - 1)) != 0), held = c.held_of(d), p = parent_of(c, b, i);
+            const bool copies = c.sc_pair()[2 * i + 1];
+            const int* row = c.sc_rows() + (long long)i * c.max_pages;
+            int* table = c.table + (long long)d * c.max_pages;
+            if (!ok) {
+                if (p != i) for (int j = threadIdx.x; j < (copies ? full : used); j += blockDim.x) if (c.page_ok(row[j])) atomicAdd(c.refs + row[j], -1);
+                for (int j = (p == i ? used : 0) + threadIdx.x; j < held; j += blockDim.x) if (c.page_ok(table[j])) atomicAdd(c.refs + table[j], 1);
+                continue;
+            }
+            const int page = copies ? c.sc_pages()[c.sc_first()[i]] : -1;
+            __syncthreads();                              // every thread has read held[d]
+            for (int j = (p == i ? used : 0) + threadIdx.x; j < max(used, held); j += blockDim.x) table[j] = j >= used ? -1 : j == full && copies ? page : row[j];
+            if (threadIdx.x == 0) { c.length[d] = len; c.held[d] = used; }
+        }
+    }
+    const int segments = LIES == PAGE_FP4 ? c.heads : 1, per = LIES == PAGE_FP4 ? c.chunks : c.heads * c.chunks, shares = (pt * per + 255) / 256, a_job = sides * segments * shares;
+    const long long all = (long long)jobs * a_job;
+    for (long long w = blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += gridDim.x * 8) {
+        const int job = (int)(w / a_job), r = (int)(w - (long long)job * a_job), share = r % shares, q = r / shares, h = q % segments, side = q / segments;
+        int from, part;
+        if (ONE) { from = c.sc_pair()[2 * job]; part = c.sc_pair()[2 * job + 1]; }
+        else {
+            const int i = c.sc_jobs()[job], len = c.sc_pair()[2 * i];
+            from = c.sc_rows()[(long long)i * c.max_pages + (len >> c.page_shift)]; part = len & (pt - 1);
+        }
+        const int to = c.sc_pages()[job];
+        if (!c.page_ok(from) || share * 256 >= part * per) continue;
+        const char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + (LIES == PAGE_FP4 ? h * c.s_head : 0);
+        copy_pieces_warp<int4>(base + from * c.s_page, const_cast<char*>(base) + to * c.s_page, share * 256, min(part * per, share * 256 + 256), [&](int u) -> long long {
+            if (LIES != PAGE_ROWS) return (long long)u * 16;
+            const int t = u / per, x = u - t * per, g = x / c.chunks;
+            return t * c.s_token + g * c.s_head + (x - g * c.chunks) * 16;
+        });
+        if constexpr (LIES == PAGE_FP4) {
+            char* scales = c.sc + (side >> 1) * c.c_layer + (side & 1) * c.c_side + h * c.c_head;
+            const int n = part * c.c_chunks, each = 256 / c.chunks * c.c_chunks;        // (of the tokens whose codes this share has)
+            copy_pieces_warp<int>(scales + from * c.c_page, scales + to * c.c_page, share * each, min(n, share * each + each), [&](int u) -> long long { return u * 4LL; });
+        }
     }
 }
 
@@ -562,12 +673,18 @@ template <typename C> int reorder(const char* who, const C* c, const int32_t* d_
     if (n == 0) return SPECDEC_OK;
     const cudaStream_t st = (cudaStream_t)stream;
     const Beams b{d_seqs, d_parents, n, beams};
-    const cudaError_t e = op_launch(k_reorder_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, b);
+    const int sides = 2 * sizes(c).n_layers, l = lies(c, v);
+    // In one CTA where counts and tables fit its shared memory: with the copies 128 entries of 1400 pages 11.6 us instead of 12.4, 32 entries of 230 16.4 instead of 18.
+    const long long bytes = 4 * ((long long)v.n_pages + (long long)n * v.max_pages);
+    const bool one = n <= CP_ALLOC_THREADS && beams <= 64 && bytes <= REORDER_ONE;      // (at most 40960 pages: counts of 20 bits)
+    if (one) if (const cudaError_t e = op_allow<k_reorder_one>(REORDER_ONE)) return op_done(who, e);
+    const cudaError_t e = one ? op_launch(k_reorder_one, dim3(1), CP_ALLOC_THREADS, (size_t)bytes, st, 1, v, b) : op_launch(k_reorder_take, dim3(n), CP_ALLOC_THREADS, 0, st, 1, v, b);
     if (e != cudaSuccess) return op_done(who, e);
-    const int sides = 2 * sizes(c).n_layers, splits = copy_splits(sizes(c), v), l = lies(c, v);
-    const long long items = (long long)n * sides * splits, most = 8 * 148;             // (how many copies there are is known on the device)
-    return op_done(who, op_launch(l == PAGE_WHOLE ? k_reorder_copy<PAGE_WHOLE> : l == PAGE_ROWS ? k_reorder_copy<PAGE_ROWS> : k_reorder_copy<PAGE_FP4>,
-                                  dim3((unsigned)(items < most ? items : most)), 256, 0, st, 1, v, b, sides, splits));
+    const long long pieces = (long long)sizes(c).page_tokens * (l == PAGE_FP4 ? v.chunks : v.heads * v.chunks), items = (long long)n * sides * (l == PAGE_FP4 ? v.heads : 1) * ((pieces + 255) / 256);
+    const long long ctas = (items + 7) / 8, most = 4 * 148;                            // (how many copies there are is known on the device)
+    auto k = one ? (l == PAGE_WHOLE ? k_reorder_copy<PAGE_WHOLE, true> : l == PAGE_ROWS ? k_reorder_copy<PAGE_ROWS, true> : k_reorder_copy<PAGE_FP4, true>)
+                 : l == PAGE_WHOLE ? k_reorder_copy<PAGE_WHOLE, false> : l == PAGE_ROWS ? k_reorder_copy<PAGE_ROWS, false> : k_reorder_copy<PAGE_FP4, false>;
+    return op_done(who, op_launch(k, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, st, 1, v, b, sides));
 }
 
 }  // namespace

@@ -79,8 +79,7 @@ class Fp4Cache(PagedCache):
         if code is None or n_tokens < 0:
             raise ValueError("dtype: fp32, bf16 or fp16, and a number of tokens, are wanted")
         layers = self.n_layers if layer is None else 1
-        both = torch.empty(2, *((layers,) if layer is None else ()), n, n_tokens, self.n_heads, self.head_dim, dtype=dtype, device=self.codes.device)
-        k, v = both[0], both[1]
+        k, v = torch.empty((2, layers, n, n_tokens, self.n_heads, self.head_dim) if layer is None else (2, n, n_tokens, self.n_heads, self.head_dim), dtype=dtype, device=self.codes.device).unbind(0)
         token = self.n_heads * self.head_dim
         _launch(self._lib.specdec_packed_cache_read, at, (self._ref, _ints("seqs", seqs, (n,), at), n, layer or 0, layers, k.data_ptr(), v.data_ptr(), code, n_tokens,
                                                        n * n_tokens * token, n_tokens * token, token, self.head_dim, None if start is None else _ints("start", start, (n,), at), _raw_stream(at)))
