@@ -1,6 +1,6 @@
 // Beam search's selection: the n best continuations of a sentence's beams over the whole vocabulary (contract: specdec.h).
 //
-// Two launches.  k_beam_rows: a CTA takes a stretch of a row into registers, with every load under way at once, and leaves its maximum m, its sum of e^(l - m) and its n largest entries.
+// k_beam_rows: a CTA takes a stretch of a row into registers, with every load under way at once, and leaves its maximum m, its sum of e^(l - m) and its n largest entries.
 // k_beam_join: a CTA a sentence joins the stretches' sums, ranks the entries that are left (a few hundred) and writes the best n.  The logits are read once; no log-probability but those of the
 // entries that are left is ever taken.
 //
@@ -16,14 +16,16 @@
 
 #include <type_traits>
 
+#include "barriers.cuh"
 #include "op_error.cuh"
 
 namespace sd {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int BM_NT = 256, BM_WARPS = BM_NT / 32, BM_MOST = 64, BM_LIST = 512;           // threads of a stretch; beams and results at most; listed entries of a stretch
-constexpr int BJ_NT = 512, BJ_WARPS = BJ_NT / 32, BJ_STAGE = 2048, BJ_LIST = 512;        // threads of a sentence; entries that it keeps in shared memory; that it ranks
+constexpr int BM_NT = 256, BM_MOST = 64, BM_LIST = 512;   // threads of a stretch; beams and results at most; listed entries of a stretch
+constexpr int BJ_NT = 512, BJ_STAGE = 2048, BJ_LIST = 512;            // threads of a sentence; entries that it keeps in shared memory; that it ranks
+constexpr int BO_CLUSTER = 8, BO_NV = 8, BO_ITEMS = 2;    // sentences in one launch: CTAs of one, vectors of a thread, stretches of a CTA at most
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr double NEAR = 1.0 / (1 << 19);
 
@@ -84,21 +86,20 @@ __device__ __forceinline__ u64 warp_max(u64 v) {
     return v;
 }
 
-// CTA = (stretch, row) of NV vectors a thread.
-template <typename T, int NV>
-__global__ void __launch_bounds__(BM_NT, NV == 8 ? 4 : 5) k_beam_rows(BeamArgs a) {
-    constexpr int VE = Vec<T>::N;
+// A stretch of a row by a CTA of NT threads, NV vectors each.
+template <typename T, int NV, int NT>
+__device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int stretch) {
+    constexpr int VE = Vec<T>::N, BM_NT = NT, BM_WARPS = NT / 32;
     __shared__ float w_max[BM_WARPS], w_sum[BM_WARPS];
     __shared__ uint32_t w_bound[BM_WARPS];
     __shared__ u64 list[BM_LIST], w_best[BM_WARPS];
     __shared__ int count;
-    op_begin();
-    const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const long long at = (long long)row * a.stretches + blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const long long at = (long long)row * a.stretches + stretch;
     if (!a.alive(row)) return;
     const T* p = (const T*)a.logits + row * a.s_row;
     const int lead = (int)(((uintptr_t)p & 15) / sizeof(T));          // elements of the first vector that lie ahead of the row
-    const int first = blockIdx.x * a.span;
+    const int first = stretch * a.span;
     auto place = [&](int j, int i) { return (first + j * BM_NT + tid) * VE - lead + i; };
     // Vectors of the stretch, by number from the row's first on: whole ones from whole to whole_end, ends of the row beside them.
     const T* base = p - lead;
@@ -246,6 +247,13 @@ __global__ void __launch_bounds__(BM_NT, NV == 8 ? 4 : 5) k_beam_rows(BeamArgs a
     }
 }
 
+// CTA = (stretch, row).
+template <typename T, int NV>
+__global__ void __launch_bounds__(BM_NT, NV == 8 ? 4 : 5) k_beam_rows(BeamArgs a) {
+    op_begin();
+    stretch_of_row<T, NV, BM_NT>(a, blockIdx.y, blockIdx.x);
+}
+
 __device__ __forceinline__ u64 ordered(double r) {        // order-preserving; NaN and -inf are not asked for
     const u64 u = (u64)__double_as_longlong(r);
     return u >> 63 ? ~u : u | 1ull << 63;
@@ -261,17 +269,17 @@ __device__ __forceinline__ double log_probability(const Beam& b, u64 e) {
     return (l == b.top ? 0.0 : (double)l - (double)b.top) - b.ln_sum;
 }
 
-// CTA = sentence.  Its entries (K lists a stretch) are asked for at once, ahead of the sums.
+// A sentence, by a CTA.  Its entries (K lists a stretch) are asked for at once, ahead of the sums.
 template <typename T>
-__global__ void __launch_bounds__(BJ_NT) k_beam_join(BeamArgs a) {
+__device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
+    constexpr int BJ_WARPS = BJ_NT / 32;
     __shared__ Beam beams[BM_MOST];
     __shared__ u64 stage[BJ_STAGE];
     __shared__ Candidate list[BJ_LIST], sorted[BM_MOST + 1], w_best[BJ_WARPS];
     __shared__ uint32_t w_bound[BJ_WARPS];
     __shared__ double w_sum[BJ_WARPS];
     __shared__ int count, again[BM_MOST];
-    op_begin();
-    const int b = blockIdx.x, row0 = b * a.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int row0 = b * a.K, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.stretches * a.n, all = a.K * per;
     const u64* lists = a.lists + (long long)row0 * per;
     u64 mine_e[BJ_STAGE / BJ_NT];
@@ -425,13 +433,37 @@ __global__ void __launch_bounds__(BJ_NT) k_beam_join(BeamArgs a) {
     }
 }
 
+template <typename T>
+__global__ void __launch_bounds__(BJ_NT) k_beam_join(BeamArgs a) {
+    op_begin();
+    join_sentence<T>(a, blockIdx.x);
+}
+// Both in one launch, a cluster a sentence: its CTAs take the stretches of all its rows in turn, the first joins them.
+template <typename T>
+__global__ void __launch_bounds__(BJ_NT, 2) k_beam_one(BeamArgs a) {
+    op_begin();
+    const int b = blockIdx.x / BO_CLUSTER, rank = blockIdx.x % BO_CLUSTER;
+    for (int i = rank; i < a.K * a.stretches; i += BO_CLUSTER) {
+        stretch_of_row<T, BO_NV, BJ_NT>(a, b * a.K + i / a.stretches, i % a.stretches);
+        __syncthreads();
+    }
+    tc_cluster_sync();
+    if (rank == 0) join_sentence<T>(a, b);
+}
+
 // Vectors of a thread: as many as leave two CTAs for every SM, so that few rows are spread over the GPU and many are read in few, large stretches.
-int vectors(long long rows, int V, int e) {
+int vectors(long long rows, int V, int e) {               // (two launches)
     for (int nv = 8; nv > 1; nv /= 2) if (rows * ((V + BM_NT * nv * (16 / e) - 1) / (BM_NT * nv * (16 / e))) >= 2 * 148) return nv;
     return 1;
 }
 // Stretches of a row whose first element is `lead` elements into a vector.
-int stretches(int nv, int V, int e, int lead) { const int per = BM_NT * nv * (16 / e); return (V + lead + per - 1) / per; }
+int stretches(int threads, int nv, int V, int e, int lead) { const int per = threads * nv * (16 / e); return (V + lead + per - 1) / per; }
+// Sentences in one launch: where each CTA has an SM, and two stretches at most.  The host is what small calls wait for, and a launch is 2.7 us of it: one sentence of 4 x 32768 16.3 -> 13.7 us, though the
+// GPU alone takes 9.0 instead of 7.8.  (32 of 5 x 50265, three stretches a CTA and two CTAs an SM: 20 us instead of 12.)
+bool in_one(int B, int K, int V, int e) { return (long long)B * BO_CLUSTER <= 148 && K * stretches(BJ_NT, BO_NV, V, e, 16 / e - 1) <= BO_ITEMS * BO_CLUSTER; }
+int most_stretches(int B, int K, int V, int e) {
+    return in_one(B, K, V, e) ? stretches(BJ_NT, BO_NV, V, e, 16 / e - 1) : stretches(BM_NT, vectors((long long)B * K, V, e), V, e, 16 / e - 1);
+}
 const char* why_not(int B, int K, int V, int n, int dtype) {
     if (B < 0 || K < 1 || V < 1 || n < 1) return "a size is below 1";
     if (!op_elem_bytes(dtype)) return "unknown dtype";
@@ -441,7 +473,8 @@ bool too_large(int B, int K, int V, int n) { return K > BM_MOST || n > BM_MOST |
 constexpr const char* LARGE = "more than 64 beams or results, 2^20 tokens or 65535 rows";
 
 template <typename T>
-cudaError_t run(const BeamArgs& a, int nv, cudaStream_t st) {
+cudaError_t run(const BeamArgs& a, int nv, bool one, cudaStream_t st) {
+    if (one) return op_launch(k_beam_one<T>, dim3(a.B * BO_CLUSTER), BJ_NT, 0, st, BO_CLUSTER, a);
     const dim3 grid(a.stretches, a.B * a.K);
     auto k = nv == 8 ? k_beam_rows<T, 8> : nv == 4 ? k_beam_rows<T, 4> : nv == 2 ? k_beam_rows<T, 2> : k_beam_rows<T, 1>;
     if (const cudaError_t e = op_launch(k, grid, BM_NT, 0, st, 1, a)) return e;
@@ -459,7 +492,7 @@ long long specdec_beam_select_workspace(int B, int K, int V, int n, int dtype) {
     if (const char* why = why_not(B, K, V, n, dtype)) return op_bad("beam_select_workspace", why);
     if (too_large(B, K, V, n)) return op_fail(SPECDEC_ERR_CAPACITY, "beam_select_workspace", LARGE);
     const int e = op_elem_bytes(dtype);
-    return (long long)B * K * stretches(vectors((long long)B * K, V, e), V, e, 16 / e - 1) * (8 + 8LL * n);
+    return (long long)B * K * most_stretches(B, K, V, e) * (8 + 8LL * n);
 }
 
 int specdec_beam_select(const specdec_beam_select_args* g, void* stream) {
@@ -476,17 +509,18 @@ int specdec_beam_select(const specdec_beam_select_args* g, void* stream) {
     if (!g->d_workspace || (uintptr_t)g->d_workspace % 8 || g->workspace_bytes < need)
         return op_fail(SPECDEC_ERR_CAPACITY, who, "the workspace is smaller than specdec_beam_select_workspace says, or not 8-byte aligned");
     BeamArgs a;
-    const int nv = vectors((long long)B * K, V, e);
+    const bool one = in_one(B, K, V, e);
+    const int nv = one ? BO_NV : vectors((long long)B * K, V, e);
     a.logits = g->d_logits; a.s_row = op_stride(g->stride, B * K); a.V = V;
     a.scores = g->d_scores; a.finished = g->d_finished; a.norm = g->d_norm;
     a.end_token = g->end_token; a.B = B; a.K = K; a.n = n;
     const int lead = ((uintptr_t)g->d_logits | (uintptr_t)(a.s_row * e)) % 16 ? 16 / e - 1 : 0, vecs = (V + lead + 16 / e - 1) / (16 / e);
-    a.stretches = stretches(nv, V, e, lead);
+    a.stretches = stretches(one ? BJ_NT : BM_NT, nv, V, e, lead);
     a.span = (vecs + a.stretches - 1) / a.stretches;      // (equal ones)
     a.out_scores = g->d_out_scores; a.out_parent = g->d_out_parent; a.out_token = g->d_out_token;
     a.sums = (float2*)g->d_workspace; a.lists = (u64*)(a.sums + (long long)B * K * a.stretches);
     const cudaStream_t st = (cudaStream_t)stream;
-    return op_done(who, dtype == SPECDEC_DTYPE_F32 ? run<float>(a, nv, st) : dtype == SPECDEC_DTYPE_BF16 ? run<__nv_bfloat16>(a, nv, st) : run<__half>(a, nv, st));
+    return op_done(who, dtype == SPECDEC_DTYPE_F32 ? run<float>(a, nv, one, st) : dtype == SPECDEC_DTYPE_BF16 ? run<__nv_bfloat16>(a, nv, one, st) : run<__half>(a, nv, one, st));
 }
 
 }  // extern "C"

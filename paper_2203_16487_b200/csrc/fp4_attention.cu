@@ -149,10 +149,9 @@ template <typename T, int D, int NT> struct Fp4Rows {
                 }
             }
         }
-        uint32_t pf[PARTS][NT][MK][2];
+        if (tail) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (tail) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -164,38 +163,65 @@ template <typename T, int D, int NT> struct Fp4Rows {
                             if (!(w >> (i * 16 + 8) & 1)) sc[n][2 * h + i][2 + e] = -INFINITY;
                         }
                     }
-            }
-            float top[2] = {-INFINITY, -INFINITY}, z[2], f[2] = {s[n][0], s[n][1]};
+        }
+        // (all rows' maxima side by side, and one vote for all: the lanes' exchanges are what a block waits for)
+        float top[NT][2], f[NT][2];
+        bool huge = false, grown = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+                top[n][e] = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < MK; ++i) top[e] = fmaxf(top[e], fmaxf(sc[n][i][e], sc[n][i][2 + e]));
-                top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 4)); top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 8));
-                top[e] = fmaxf(m[n][e], fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 16)) * f[e]);
+                for (int i = 0; i < MK; ++i) top[n][e] = fmaxf(top[n][e], fmaxf(sc[n][i][e], sc[n][i][2 + e]));
             }
-            // Fused with the subtraction of their maximum, products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge they are rounded first.
-            if (__any_sync(0xffffffffu, fmaxf(fabsf(top[0]), fabsf(top[1])) > 1048576.f)) {
+#pragma unroll
+        for (int of = 4; of < 32; of <<= 1)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], of));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                f[n][e] = s[n][e];
+                top[n][e] = fmaxf(m[n][e], top[n][e] * f[n][e]);
+                huge |= fabsf(top[n][e]) > 1048576.f && fabsf(top[n][e]) < INFINITY;
+                grown |= top[n][e] != m[n][e];
+            }
+        // Fused with the subtraction of their maximum, products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge they are rounded first.
+        if (__any_sync(0xffffffffu, huge)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                    for (int i = 0; i < MK; ++i) { sc[n][i][e] *= f[e]; sc[n][i][2 + e] *= f[e]; }
-                    f[e] = 1.f;
+                    for (int i = 0; i < MK; ++i) { sc[n][i][e] *= f[n][e]; sc[n][i][2 + e] *= f[n][e]; }
+                    f[n][e] = 1.f;
                 }
-            }
-            if (__any_sync(0xffffffffu, top[0] != m[n][0] || top[1] != m[n][1])) {
-                const float fa = ta_exp2(m[n][0] - (top[0] == -INFINITY ? 0.f : top[0])), fb = ta_exp2(m[n][1] - (top[1] == -INFINITY ? 0.f : top[1]));
+        }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float fa = ta_exp2(m[n][0] - (top[n][0] == -INFINITY ? 0.f : top[n][0])), fb = ta_exp2(m[n][1] - (top[n][1] == -INFINITY ? 0.f : top[n][1]));
                 l[n][0] *= fa; l[n][1] *= fb;
 #pragma unroll
                 for (int i = 0; i < MD; ++i) { o[n][i][0] *= fa; o[n][i][1] *= fb; o[n][i][2] *= fa; o[n][i][3] *= fb; }
-                m[n][0] = top[0]; m[n][1] = top[1];
+                m[n][0] = top[n][0]; m[n][1] = top[n][1];
             }
+        }
+        uint32_t pf[PARTS][NT][MK][2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) z[e] = P_SHIFT - (top[e] == -INFINITY ? 0.f : top[e]);
+        for (int n = 0; n < NT; ++n) {
+            float z[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) z[e] = P_SHIFT - (top[n][e] == -INFINITY ? 0.f : top[n][e]);
 #pragma unroll
             for (int i = 0; i < MK; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float u = ta_exp2(fmaf(sc[n][i][2 * h], f[0], z[0])), v = ta_exp2(fmaf(sc[n][i][2 * h + 1], f[1], z[1]));
+                    const float u = ta_exp2(fmaf(sc[n][i][2 * h], f[n][0], z[0])), v = ta_exp2(fmaf(sc[n][i][2 * h + 1], f[n][1], z[1]));
                     const uint32_t y = half_pair(u, v);
                     pf[0][n][i][h] = transpose8(y);
                     if constexpr (WIDE) pf[PARTS - 1][n][i][h] = transpose8(rest_pair(u, v, y));
@@ -261,7 +287,7 @@ template <typename T, int D, int NT> struct Fp4Rows {
     // This lane's D / 8 channels of a row, in order.
     __device__ __forceinline__ float channel(int n, int e, int i) const { return o[n][i / 2][(i & 1) * 2 + e]; }
     // Partial results in shared memory: rows of RP floats from row r0 on, and (maximum, sum) of each.
-    static constexpr int RP = D + 4;
+    [[maybe_unused]] static constexpr int RP = D + 4;
     __device__ __forceinline__ void leave(float* red, float2* red_ml, int r0) const {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
@@ -500,7 +526,7 @@ struct Plan { int rows, tiles, per_sm, direct, ctas, unit, min_blocks; long long
 constexpr int per_sm_of(int dtype, int dim, int rows) {
     if (rows >= 128) return 1;
     if (dtype == SPECDEC_DTYPE_F32) return dim > 64 ? (rows == 64 ? 1 : 2) : rows == 8 ? 3 : 2;
-    return rows == 8 ? (dim > 64 ? 3 : 4) : dim > 64 ? 2 : 3;
+    return rows == 8 && dim == 64 ? 4 : 3;
 }
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
@@ -543,8 +569,8 @@ cudaError_t pick(const Fp4Attn& a, int rows, int grid, cudaStream_t st) {
         if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 3, 9, 2>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 8, 2>(a, grid, st) : rows == 32 ? run<T, 128, 1, 4, 1, 6, 2>(a, grid, st) : run<T, 128, 1, 8, 1, 8, 1>(a, grid, st);
         return rows == 8 ? run<T, 64, 1, 1, 3, 9, 3>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 2>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 2>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 2>(a, grid, st);
     } else {
-        if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 4, 8, 3>(a, grid, st) : rows == 16 ? run<T, 128, 2, 1, 3, 9, 2>(a, grid, st) : run<T, 128, 2, 2, 1, 8, 2>(a, grid, st);
-        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 3>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 3>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 3>(a, grid, st);
+        if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 4, 8, 3>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 6, 3>(a, grid, st) : run<T, 128, 1, 4, 1, 6, 3>(a, grid, st);
+        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 1, 2, 2, 8, 3>(a, grid, st) : rows == 32 ? run<T, 64, 1, 4, 1, 8, 3>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 3>(a, grid, st);
     }
 }
 
