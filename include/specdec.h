@@ -293,8 +293,8 @@ int specdec_tree_attention(const specdec_cache* c, const specdec_tree_attention_
  *             and head follow one another (stride_token does not matter).  head_dim is 64 or 128, page_tokens a power of two from 16 on.
  *   d_scales: head_dim / 16 bytes a token and head, tokens of a page and head behind one another, with strides of their own (bytes).
  * Addresses and strides of both are multiples of 16 bytes.  Everything else, and the calls of the same names, are as above; they move codes and scales as they are.
- * append, read: d_k, d_v [n_layers, n, T, n_heads, head_dim] of `dtype` (fp32, bf16, fp16), strides in elements.  read: the values of tokens d_start[i] + t (NULL: d_length + t, the
- *   block behind the committed tokens), rounded to dtype once; zeros where the sequence has no page.  It takes sequences more than once. */
+ * append: the first d_some[i] (NULL: all T) tokens of sequence i, as above, of fp32, bf16 or fp16.  read: the values of tokens d_some[i] + t (NULL: d_length + t, the block behind the
+ *   committed tokens), rounded to dtype once; zeros where the sequence has no page.  It takes sequences more than once. */
 typedef struct {
     specdec_cache codes;
     void*         d_scales;
@@ -302,10 +302,15 @@ typedef struct {
     const float*  d_unit;
 } specdec_packed_cache;
 int specdec_packed_cache_reserve(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream);
-int specdec_packed_cache_append(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int dtype, int T,
-                             long long stride_layer, long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_count, void* stream);
-int specdec_packed_cache_read(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, void* d_k, void* d_v, int dtype, int T,
-                           long long stride_layer, long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_start, void* stream);
+typedef struct {                           /* tokens of n sequences, append's and read's                                 */
+    const int32_t *d_seqs;                 /* [n]                                                                         */
+    void          *d_k, *d_v;              /* [n_layers, n, T, n_heads, head_dim] of dtype; append only reads them        */
+    const int32_t *d_some;                 /* [n] or NULL: append's counts (T), read's first tokens (d_length)            */
+    long long      stride_layer, stride_seq, stride_token, stride_head;                           /* elements            */
+    int            n, layer, n_layers, dtype, T;
+} specdec_packed_tokens;
+int specdec_packed_cache_append(const specdec_packed_cache* c, const specdec_packed_tokens* t, void* stream);
+int specdec_packed_cache_read(const specdec_packed_cache* c, const specdec_packed_tokens* t, void* stream);
 int specdec_packed_cache_compact(const specdec_packed_cache* c, const int32_t* d_seqs, int n, const int32_t* d_path, int path_stride, const int32_t* d_n_path, void* stream);
 int specdec_packed_cache_release(const specdec_packed_cache* c, const int32_t* d_seqs, int n, void* stream);
 int specdec_packed_cache_fork(const specdec_packed_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream);

@@ -76,6 +76,11 @@ class TreeAttentionArgs(C.Structure):
         ("max_length", C.c_int), ("scale", C.c_float), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_longlong)]
 
 
+class PackedTokens(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_seqs", "d_k", "d_v", "d_some")] + [(n, C.c_longlong) for n in ("stride_layer", "stride_seq", "stride_token", "stride_head")] + [
+        (n, C.c_int) for n in ("n", "layer", "n_layers", "dtype", "T")]
+
+
 class BeamSelectArgs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("d_logits", "d_scores", "d_finished", "d_norm", "d_out_scores", "d_out_parent", "d_out_token", "d_workspace")] + [
         ("workspace_bytes", C.c_longlong), ("stride", C.c_longlong)] + [(n, C.c_int) for n in ("dtype", "B", "K", "V", "n", "end_token")]
@@ -137,7 +142,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     fp = C.POINTER(Fp4Cache)
     for name in ("reserve", "compact", "release", "fork", "reorder"):
         getattr(lib, "specdec_packed_cache_" + name).argtypes = [fp] + getattr(lib, "specdec_cache_" + name).argtypes[1:]
-    lib.specdec_packed_cache_append.argtypes = lib.specdec_packed_cache_read.argtypes = [fp, ip, i, i, i, vp, vp, i, i, L, L, L, L, ip, vp]
+    lib.specdec_packed_cache_append.argtypes = lib.specdec_packed_cache_read.argtypes = [fp, vp, vp]      # (PackedTokens by reference, or its bytes)
     lib.specdec_packed_attention_workspace.argtypes = [i, i, i, i, i, i, i, i]
     lib.specdec_packed_attention.argtypes = [fp, vp, i, vp]
     lib.specdec_beam_select_workspace.argtypes = [i, i, i, i, i]

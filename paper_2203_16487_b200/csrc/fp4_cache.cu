@@ -184,28 +184,27 @@ template <bool READ, typename T> auto kernel(int dim, bool unit) {
 }
 
 template <bool READ>
-int move(const char* who, const specdec_packed_cache* f, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int dtype, int T, long long stride_layer,
-         long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_some, void* stream) {
+int move(const char* who, const specdec_packed_cache* f, const specdec_packed_tokens* g, void* stream) {
     if (const char* why = fp4_why_not(f)) return op_bad(who, why);
     const specdec_cache* c = &f->codes;
-    if (!c->d_held || !c->d_refs) return op_bad(who, "a pointer is NULL");
-    const int e = op_elem_bytes(dtype);
+    if (!c->d_held || !c->d_refs || !g) return op_bad(who, "a pointer is NULL");
+    const int n = g->n, T = g->T, layer = g->layer, n_layers = g->n_layers, dtype = g->dtype, e = op_elem_bytes(dtype);
     if (!e) return op_bad(who, "unknown dtype");
-    if ((n && T && (!d_seqs || !d_k || !d_v)) || n < 0 || (!READ && n > c->n_seqs) || n > 65535 || T < 0 || layer < 0 || n_layers < 1 || n_layers > 32767 || layer > c->n_layers - n_layers)
+    if ((n && T && (!g->d_seqs || !g->d_k || !g->d_v)) || n < 0 || (!READ && n > c->n_seqs) || n > 65535 || T < 0 || layer < 0 || n_layers < 1 || n_layers > 32767 || layer > c->n_layers - n_layers)
         return op_bad(who, "a pointer is NULL, or n, T or the layers are out of range");
-    const long long st[4] = {op_stride(stride_layer, n_layers), op_stride(stride_seq, n), op_stride(stride_token, T), op_stride(stride_head, c->n_heads)};
+    const long long st[4] = {op_stride(g->stride_layer, n_layers), op_stride(g->stride_seq, n), op_stride(g->stride_token, T), op_stride(g->stride_head, c->n_heads)};
     for (long long s : st) if (s * e % 16) return op_bad(who, "a stride is not a multiple of 16 bytes");
-    if (((uintptr_t)d_k | (uintptr_t)d_v) & 15) return op_bad(who, "d_k or d_v is not 16-byte aligned");
+    if (((uintptr_t)g->d_k | (uintptr_t)g->d_v) & 15) return op_bad(who, "d_k or d_v is not 16-byte aligned");
     if (n == 0 || T == 0) return SPECDEC_OK;
     Fp4Io a;
     a.s_layer = op_stride(c->stride_layer, c->n_layers); a.s_side = c->stride_side; a.s_page = op_stride(c->stride_page, c->n_pages); a.s_head = op_stride(c->stride_head, c->n_heads);
     a.c_layer = op_stride(f->scale_stride_layer, c->n_layers); a.c_side = f->scale_stride_side; a.c_page = op_stride(f->scale_stride_page, c->n_pages);
     a.c_head = op_stride(f->scale_stride_head, c->n_heads);
     a.codes = (char*)c->d_kv + layer * a.s_layer; a.scales = (char*)f->d_scales + layer * a.c_layer;
-    a.x[0] = (char*)const_cast<void*>(d_k); a.x[1] = (char*)const_cast<void*>(d_v);
+    a.x[0] = (char*)g->d_k; a.x[1] = (char*)g->d_v;
     a.x_layer = st[0] * e; a.x_seq = st[1] * e; a.x_token = st[2] * e; a.x_head = st[3] * e;
     a.unit = f->d_unit ? f->d_unit + (long long)layer * 2 * c->n_heads : nullptr;
-    a.table = c->d_table; a.length = c->d_length; a.held = c->d_held; a.refs = c->d_refs; a.seqs = d_seqs; a.some = d_some; a.status = c->d_status;
+    a.table = c->d_table; a.length = c->d_length; a.held = c->d_held; a.refs = c->d_refs; a.seqs = g->d_seqs; a.some = g->d_some; a.status = c->d_status;
     a.n_pages = c->n_pages; a.n_seqs = c->n_seqs; a.max_pages = c->max_pages; a.page_shift = __builtin_ctz(c->page_tokens); a.heads = c->n_heads; a.T = T;
     const int tokens = T < TOKENS ? T : TOKENS;
     const long long items = (long long)c->n_heads * tokens * (c->head_dim / FP4_BLOCK);
@@ -222,13 +221,7 @@ using namespace sd;
 
 extern "C" {
 
-int specdec_packed_cache_append(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int dtype, int T, long long stride_layer,
-                             long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_count, void* stream) {
-    return move<false>("packed_cache_append", c, d_seqs, n, layer, n_layers, d_k, d_v, dtype, T, stride_layer, stride_seq, stride_token, stride_head, d_count, stream);
-}
-int specdec_packed_cache_read(const specdec_packed_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, void* d_k, void* d_v, int dtype, int T, long long stride_layer,
-                           long long stride_seq, long long stride_token, long long stride_head, const int32_t* d_start, void* stream) {
-    return move<true>("packed_cache_read", c, d_seqs, n, layer, n_layers, d_k, d_v, dtype, T, stride_layer, stride_seq, stride_token, stride_head, d_start, stream);
-}
+int specdec_packed_cache_append(const specdec_packed_cache* c, const specdec_packed_tokens* t, void* stream) { return move<false>("packed_cache_append", c, t, stream); }
+int specdec_packed_cache_read(const specdec_packed_cache* c, const specdec_packed_tokens* t, void* stream) { return move<true>("packed_cache_read", c, t, stream); }
 
 }  // extern "C"

@@ -10,6 +10,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional
 
 import torch
@@ -19,6 +20,8 @@ from .tree import DTYPES, PagedCache, _ints, _launch, _raw_stream
 
 BLOCK = 16                                                   # channels of a scale
 _FP4 = 3                                                     # SPECDEC_DTYPE_FP4
+_tokens_args = struct.Struct("@PPPPqqqqiiiii0q")             # PackedTokens in one go
+assert _tokens_args.size == C.sizeof(binding.PackedTokens)
 
 
 class Fp4Cache(PagedCache):
@@ -58,18 +61,27 @@ class Fp4Cache(PagedCache):
                                    scales.data_ptr(), z[0], z[1], z[2], z[3], None if unit is None else unit.data_ptr())
         self._ref, self.dtype = C.byref(self._c), None         # (of no type of its own)
         self._finish("specdec_packed_cache_", at, n_layers=L, n_heads=H, head_dim=D, page=page, max_pages=table.shape[1])
+        self._call["read"] = self._lib.specdec_packed_cache_read
 
     def append(self, seqs, k, v, layer: Optional[int] = None, count=None):
         """Writes k, v [n, T, n_heads, head_dim] (layer=None: [n_layers, n, T, n_heads, head_dim], every layer), fp32, bf16 or fp16, in 4 bits behind the committed tokens; of
         sequence i the first count[i] of the T.  Lengths stay: compact moves them."""
-        n, code = seqs.numel(), DTYPES.get(k.dtype)
+        n, dtype = seqs.numel(), k.dtype
+        code = DTYPES.get(dtype)
         if code is None:
             raise ValueError("k, v: fp32, bf16 or fp16 is wanted")
-        layer, layers, shape, s = self._block(n, k, v, layer, k.dtype)
+        layer, layers, shape, s = self._block(n, k, v, layer, dtype)
         if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled() and self._source is None:
             self._source = torch.zeros((), requires_grad=True)
-        _launch(self._call["append"], self._device, (self._ref, _ints("seqs", seqs, (n,), self._device), n, layer, layers, k.data_ptr(), v.data_ptr(), code, shape[2],
-                                                     s[0], s[1], s[2], s[3], None if count is None else _ints("count", count, (n,), self._device), _raw_stream(self._device)))
+        at = self._device
+        self._tokens("append", _ints("seqs", seqs, (n,), at), k.data_ptr(), v.data_ptr(), 0 if count is None else _ints("count", count, (n,), at), s[0], s[1], s[2], s[3], n, layer, layers, code, shape[2])
+
+    def _tokens(self, call, *args):
+        try:
+            a = _tokens_args.pack(*args)
+        except struct.error as e:
+            raise ValueError(f"layer or number of tokens: {e}") from None
+        _launch(self._call[call], self._device, (self._ref, a, _raw_stream(self._device)))
 
     def read(self, seqs, n_tokens: int, layer: Optional[int] = None, start=None, dtype=torch.bfloat16):
         """(k, v) [(n_layers,) n, n_tokens, n_heads, head_dim]: the values of tokens start[i], start[i] + 1, ... of each sequence (start=None: those behind the committed ones); zeros where it
@@ -81,6 +93,6 @@ class Fp4Cache(PagedCache):
         layers = self.n_layers if layer is None else 1
         k, v = torch.empty((2, layers, n, n_tokens, self.n_heads, self.head_dim) if layer is None else (2, n, n_tokens, self.n_heads, self.head_dim), dtype=dtype, device=self.codes.device).unbind(0)
         token = self.n_heads * self.head_dim
-        _launch(self._lib.specdec_packed_cache_read, at, (self._ref, _ints("seqs", seqs, (n,), at), n, layer or 0, layers, k.data_ptr(), v.data_ptr(), code, n_tokens,
-                                                       n * n_tokens * token, n_tokens * token, token, self.head_dim, None if start is None else _ints("start", start, (n,), at), _raw_stream(at)))
+        self._tokens("read", _ints("seqs", seqs, (n,), at), k.data_ptr(), v.data_ptr(), 0 if start is None else _ints("start", start, (n,), at), n * n_tokens * token, n_tokens * token, token,
+                     self.head_dim, n, 0 if layer is None else layer, layers, code, n_tokens)
         return k, v
