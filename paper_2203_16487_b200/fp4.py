@@ -15,8 +15,8 @@ from typing import Optional
 
 import torch
 
-from . import binding
-from .tree import DTYPES, PagedCache, _ints, _launch, _raw_stream
+from . import binding, tree
+from .tree import DTYPES, PagedCache, _ints, _launch
 
 BLOCK = 16                                                   # channels of a scale
 _FP4 = 3                                                     # SPECDEC_DTYPE_FP4
@@ -81,7 +81,7 @@ class Fp4Cache(PagedCache):
             a = _tokens_args.pack(*args)
         except struct.error as e:
             raise ValueError(f"layer or number of tokens: {e}") from None
-        _launch(self._call[call], self._device, (self._ref, a, _raw_stream(self._device)))
+        _launch(self._call[call], self._device, (self._ref, a, tree._raw_stream(self._device)))
 
     def read(self, seqs, n_tokens: int, layer: Optional[int] = None, start=None, dtype=torch.bfloat16):
         """(k, v) [(n_layers,) n, n_tokens, n_heads, head_dim]: the values of tokens start[i], start[i] + 1, ... of each sequence (start=None: those behind the committed ones); zeros where it
