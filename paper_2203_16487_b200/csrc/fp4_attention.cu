@@ -444,24 +444,34 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
             const int gr = r0 + w0 + n * 8 + 2 * (lane & 3) + e;
             return gr < all_rows && ta_node(a, gr) < s.nodes;
         };
+        // The nodes that anyone sees, asked for ahead of the queries.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for another; more:
+        // in shared memory.
+        const bool own = a.words <= 2;
+        const uint32_t* words = a.mask + it.b * a.mask_sb;
+        uint32_t seen[2] = {0, 0};
+        if (own) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                if (w < a.words && lane < s.nodes) seen[w] = words[lane * a.words + w];
+                if (w < a.words && lane + 32 < s.nodes) seen[w] |= words[(lane + 32) * a.words + w];
+            }
+        }
+        auto query_at = [&](const Part& part, int n) {
+            const int gr = part.tile * ROWS + w0 + n * 8 + (lane >> 2), node = ta_node(a, gr);
+            return a.q + part.b * a.q_sb + node * a.q_st + (part.h * a.group + gr - node * a.group) * a.q_sh + (lane & 3) * (D / 4) * (int)sizeof(T);
+        };
+        auto query_live = [&](const Part& part, int n) { const int gr = part.tile * ROWS + w0 + n * 8 + (lane >> 2); return gr < all_rows && ta_node(a, gr) < part.s.nodes; };
         const float times = a.unit_k ? a.scale * a.unit_k[it.h] : a.scale;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int gr = r0 + w0 + n * 8 + (lane >> 2), node = ta_node(a, gr);
-            rows.query(n, a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + (lane & 3) * (D / 4) * (int)sizeof(T), gr < all_rows && node < s.nodes, a.q_vec, times);
-        }
-        // The nodes that anyone sees.  Up to 64 nodes: in every warp's own registers (anyone: any query of the tree), so that no warp waits for another; more: in shared memory.
-        const bool own = a.words <= 2;
-        uint32_t seen[2] = {0, 0};
-        const uint32_t* words = a.mask + it.b * a.mask_sb;
+        for (int n = 0; n < NT; ++n) rows.query(n, query_at(it, n), query_live(it, n), a.q_vec, times);
+        if (more)                                         // the next part's queries, on their way to the second-level cache
+#pragma unroll
+            for (int n = 0; n < NT; ++n) if (query_live(ahead, n)) asm volatile("prefetch.global.L2 [%0];" ::"l"(query_at(ahead, n)));
         if (own) {
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const int left = s.nodes - w * 32;
-                if (w >= a.words || left <= 0) break;
-                uint32_t all = lane < s.nodes ? words[lane * a.words + w] : 0u;
-                if (lane + 32 < s.nodes) all |= words[(lane + 32) * a.words + w];
-                seen[w] = __reduce_or_sync(0xffffffffu, all) & (left < 32 ? (1u << left) - 1u : 0xffffffffu);
+                seen[w] = __reduce_or_sync(0xffffffffu, seen[w]) & (left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u);
             }
         } else {
             ta_load_masks<32 * WARPS, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
