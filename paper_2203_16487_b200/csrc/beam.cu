@@ -68,6 +68,14 @@ template <typename T> struct Vec {
         else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
         else { const __half2 h = *reinterpret_cast<const __half2*>(w + i / 2); return i & 1 ? __high2float(h) : __low2float(h); }
     }
+    static __device__ __forceinline__ float pick(const uint4& v, int i) {                // ... of an index that is not known before
+        const int q = sizeof(T) == 4 ? i : i >> 1;
+        const uint32_t w = q & 2 ? (q & 1 ? v.w : v.z) : q & 1 ? v.y : v.x;
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+        const uint32_t h = i & 1 ? w >> 16 : w & 0xffffu;
+        if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(h << 16);
+        else return __half2float(__ushort_as_half((unsigned short)h));
+    }
 };
 template <typename T> __device__ __forceinline__ float as_float(T x) {
     if constexpr (sizeof(T) == 4) return x;
@@ -202,7 +210,7 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
         for (int i = 0; i < VE; ++i) hits |= Vec<T>::at(v, i) >= least ? 1u << i : 0u;
         for (; hits; hits &= hits - 1) {
             const int i = __ffs(hits) - 1, k = atomicAdd(&count, 1);
-            if (k < BM_LIST) list[k] = entry(as_float(p[place(j, i)]), place(j, i));
+            if (k < BM_LIST) list[k] = entry(Vec<T>::pick(v, i), place(j, i));
         }
     }
     __syncthreads();
@@ -217,11 +225,13 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
     const int c = count;
     if (c <= BM_LIST) {
         if (tid < a.n && tid >= c) out[tid] = 0;
-        for (int k = tid; k < c; k += BM_NT) {
-            const u64 mine = list[k];
+        for (int k = tid / 8; k < (c + 3) / 4 * 4; k += BM_NT / 8) {                     // eight lanes an entry, whole warps
+            const u64 mine = list[min(k, c - 1)];
             int rank = 0;
-            for (int i = 0; i < c; ++i) rank += list[i] > mine;
-            if (rank < a.n) out[rank] = mine;
+            for (int i = lane & 7; i < c; i += 8) rank += list[i] > mine;
+#pragma unroll
+            for (int o = 4; o; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+            if ((lane & 7) == 0 && k < c && rank < a.n) out[rank] = mine;
         }
         return;
     }
@@ -308,8 +318,9 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
     for (int j = 0; j < BJ_STAGE / BJ_NT; ++j) stage[tid + j * BJ_NT] = mine_e[j];
     if (tid == 0) count = 0;
     __syncthreads();
+    const float inv_per = 1.f / per;
     auto candidate = [&](int i, Candidate& c) {           // the i-th: beam, stretch, place in its list
-        c.beam = i / per;
+        c.beam = (int)((i + 0.5f) * inv_per);             // i / per: `all` is at most 2^20, so the product is off by less than the half
         const Beam& x = beams[c.beam];
         if (x.done) {
             c.e = ~(uint32_t)a.end_token;
@@ -327,7 +338,10 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
     uint32_t mine = 0;
     Candidate c;
     const int mixed = tid * 97 & (BJ_NT - 1);
-    for (int i = mixed; i < all; i += BJ_NT) if (candidate(i, c)) mine = max(mine, (uint32_t)(ordered(c.rank) >> 32));
+    const bool has = mixed < all && candidate(mixed, c);  // (of most calls a thread's only one)
+    if (has) mine = (uint32_t)(ordered(c.rank) >> 32);
+    Candidate d;
+    for (int i = mixed + BJ_NT; i < all; i += BJ_NT) if (candidate(i, d)) mine = max(mine, (uint32_t)(ordered(d.rank) >> 32));
     uint32_t bound = 0;
     for (int q = (a.n + 1 + BJ_WARPS - 1) / BJ_WARPS; q; --q) {       // (the one behind the n-th is looked at too)
         bound = __reduce_max_sync(0xffffffffu, mine);
@@ -345,10 +359,14 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
         const u64 u = (u64)bound << 32;
         least = __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) - 4 * NEAR * norm;       // (ranks may still move by as much)
     }
-    for (int i = mixed; i < all; i += BJ_NT)
-        if (candidate(i, c) && !(c.rank < least)) {
+    if (has && !(c.rank < least)) {
+        const int k = atomicAdd(&count, 1);
+        if (k < BJ_LIST) list[k] = c;
+    }
+    for (int i = mixed + BJ_NT; i < all; i += BJ_NT)
+        if (candidate(i, d) && !(d.rank < least)) {
             const int k = atomicAdd(&count, 1);
-            if (k < BJ_LIST) list[k] = c;
+            if (k < BJ_LIST) list[k] = d;
         }
     __syncthreads();
     const int found = count;
