@@ -108,7 +108,7 @@ template <typename T, int D, int NT> struct Fp4Rows {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, x = D == 128 ? t & 1 : t >> 1;      // x: whether keys 2 t and 2 t + 1 are exchanged
         float sc[NT][MK][4];
         const char* kc = st + key_of(g) * (D / 2) + t * (D / 8);
-        const char* kq = st + Stage::KS + key_of(g) * (D / 16) + t * (D / 64);
+        const char* kq = st + Stage::CODES + key_of(g) * (D / 16) + t * (D / 64);
 #pragma unroll
         for (int i = 0; i < MK; ++i) {
             uint32_t w[2][D / 32], s2[2][2];              // [key g, g + 8 of sixteen]
@@ -227,8 +227,8 @@ template <typename T, int D, int NT> struct Fp4Rows {
                     if constexpr (WIDE) pf[PARTS - 1][n][i][h] = transpose8(rest_pair(u, v, y));
                 }
         }
-        const char* vc = st + Stage::V + (2 * t) * (D / 2) + g * (D / 16);
-        const char* vq = st + Stage::VS + (2 * t) * (D / 16) + g * (D / 16) / 8;
+        const char* vc = st + Stage::HALF + (2 * t) * (D / 2) + g * (D / 16);
+        const char* vq = st + Stage::HALF + Stage::CODES + (2 * t) * (D / 16) + g * (D / 16) / 8;
 #pragma unroll
         for (int i = 0; i < MK; ++i) {
             // keys 2 t + x and 2 t + 1 - x of each eight
@@ -362,6 +362,53 @@ template <typename T, int D, int NT> struct Fp4Rows {
     }
 };
 
+// The loading warp: blocks of the CTA's parts in order, running ahead into the next parts.  Block j of a part goes to group j % WK, which has the stages j % WK, j % WK + WK, ... to itself.
+template <int D, int WK, int NS>
+__device__ __forceinline__ void fp4_load(const Fp4Attn& a, TaWork work, const int4* seqs, char* ring, uint32_t full, uint32_t empty, int* abort_flag) {
+    using Stage = Fp4Stage<D>;
+    constexpr int KT = TA_BLOCK, NG = NS / WK, STAGE = Stage::BYTES;
+    const int lane = threadIdx.x & 31;
+    const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
+    // What a lane copies of a block: lane / 4-th page's codes of keys, of values, scales of keys, of values
+    const int page_of = lane >> 2;
+    const bool scales = lane & 2, values = lane & 1;
+    const char* base = scales ? (values ? a.vs : a.ks) : values ? a.v : a.k;
+    const long long s_page = scales ? a.c_page : a.s_page, s_head = scales ? a.c_head : a.s_head;
+    const int size = box * (scales ? D / 16 : D / 2), at = (scales ? Stage::CODES : 0) + (values ? Stage::HALF : 0) + page_of * size;
+    int count = 0;                                    // lane g: blocks that group g had in the parts before
+    Part it, ahead;
+    // This lane's page of the 32 from the b0-th of a part on; -1 where there is none.  Asked for 32 at a time and well ahead: a lookup a block, waited for, is 0.7 us a block.
+    auto pages_of = [&](const Part& part, int b0) {
+        const int key = part.k_begin + (b0 + lane) * box, i = key >> a.page_shift;
+        int p = -1;
+        if (key < part.k_end && i < a.max_pages) p = a.table[(long long)part.s.seq * a.max_pages + i];
+        return (unsigned)p < (unsigned)a.n_pages ? p : -1;
+    };
+    bool more = work.next(a, seqs, ahead);
+    int first = more ? pages_of(ahead, 0) : 0;
+    while (more) {
+        it = ahead;
+        int now = first, then = pages_of(it, 32);
+        more = work.next(a, seqs, ahead);
+        if (more) first = pages_of(ahead, 0);
+        for (int j = 0; j < it.blocks; ++j) {
+            const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), b0 = j * n_pages, key = it.k_begin + (b0 + page_of) * box;
+            if (b0 && b0 % 32 == 0) { now = then; then = pages_of(it, b0 + 32); }
+            const int cur = __shfl_sync(0xffffffffu, now, (b0 + page_of) % 32);
+            if (n >= NG && !mbar_wait_warp<true>(empty + st * 8, (n / NG - 1) & 1, abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
+            char* to = ring + st * STAGE + at;
+            const bool mine = lane < 4 * n_pages && key < it.k_end, real = mine && cur >= 0;
+            if (mine && cur < 0 && scales)            // a page that is none: zeros
+                for (int i = 0; i < size; i += 16) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
+            const unsigned pieces = __popc(__ballot_sync(0xffffffffu, real));          // four a page
+            if (lane == 0) mbar_expect_tx(full + st * 8, pieces / 4 * box * (D + D / 8));
+            __syncwarp();
+            if (real) bulk_copy(smem_u32(to), base + cur * s_page + it.h * s_head + (key & (page - 1)) * (scales ? D / 16 : D / 2), size, full + st * 8);
+        }
+        count += (it.blocks - lane + WK - 1) / WK;    // (lanes below WK)
+    }
+}
+
 // Group wk has the stages wk, wk + WK, ... to itself and so waits for every phase of their barriers.
 template <typename T, int D, int NT, int WM, int WK, int NS, int PER_SM>
 __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn a) {
@@ -387,48 +434,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
     work.begin(a, seqs);
     __syncthreads();
 
-    if (warp == WARPS) {                                  // loads, running ahead into the next parts
-        const int page = 1 << a.page_shift, box = min(page, KT), n_pages = KT / box;
-        // What a lane copies of a block: lane / 4-th page's codes of keys, of values, scales of keys, of values
-        const int page_of = lane >> 2;
-        const bool scales = lane & 2, values = lane & 1;
-        const char* base = scales ? (values ? a.vs : a.ks) : values ? a.v : a.k;
-        const long long s_page = scales ? a.c_page : a.s_page, s_head = scales ? a.c_head : a.s_head;
-        const int size = box * (scales ? D / 16 : D / 2), at = (scales ? Stage::KS : 0) + (values ? (scales ? Stage::SCALES : Stage::V) : 0) + page_of * size;
-        int count = 0;                                    // lane g: blocks that group g had in the parts before
-        Part it, ahead;
-        // This lane's page of the 32 from the b0-th of a part on; -1 where there is none.  Asked for 32 at a time and well ahead: a lookup a block, waited for, is 0.7 us a block.
-        auto pages_of = [&](const Part& part, int b0) {
-            const int key = part.k_begin + (b0 + lane) * box, i = key >> a.page_shift;
-            int p = -1;
-            if (key < part.k_end && i < a.max_pages) p = a.table[(long long)part.s.seq * a.max_pages + i];
-            return (unsigned)p < (unsigned)a.n_pages ? p : -1;
-        };
-        bool more = work.next(a, seqs, ahead);
-        int first = more ? pages_of(ahead, 0) : 0;
-        while (more) {
-            it = ahead;
-            int now = first, then = pages_of(it, 32);
-            more = work.next(a, seqs, ahead);
-            if (more) first = pages_of(ahead, 0);
-            for (int j = 0; j < it.blocks; ++j) {
-                const int g = j % WK, n = __shfl_sync(0xffffffffu, count, g) + j / WK, st = g + WK * (n % NG), b0 = j * n_pages, key = it.k_begin + (b0 + page_of) * box;
-                if (b0 && b0 % 32 == 0) { now = then; then = pages_of(it, b0 + 32); }
-                const int cur = __shfl_sync(0xffffffffu, now, (b0 + page_of) % 32);
-                if (n >= NG && !mbar_wait_warp<true>(empty + st * 8, (n / NG - 1) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
-                char* to = ring + st * STAGE + at;
-                const bool mine = lane < 4 * n_pages && key < it.k_end, real = mine && cur >= 0;
-                if (mine && cur < 0 && scales)            // a page that is none: zeros
-                    for (int i = 0; i < size; i += 16) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
-                const unsigned pieces = __popc(__ballot_sync(0xffffffffu, real));          // four a page
-                if (lane == 0) mbar_expect_tx(full + st * 8, pieces / 4 * box * (D + D / 8));
-                __syncwarp();
-                if (real) bulk_copy(smem_u32(to), base + cur * s_page + it.h * s_head + (key & (page - 1)) * (scales ? D / 16 : D / 2), size, full + st * 8);
-            }
-            count += (it.blocks - lane + WK - 1) / WK;    // (lanes below WK)
-        }
-        return;
-    }
+    if (warp == WARPS) { fp4_load<D, WK, NS>(a, work, seqs, ring, full, empty, &abort_flag); return; }
 
     const int wm = warp % WM, wk = warp / WM, all_rows = a.T * a.group;
     auto consumers = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory"); };
@@ -493,8 +499,8 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
                     const int base = k0 + (r & ~31) - s.len;
                     const uint32_t w = own ? ta_window2(seen[0], seen[1], base) : ta_window(any, a.words, base);
                     if (!(w >> (r & 31) & 1)) {
-                        if constexpr (D == 128) *reinterpret_cast<uint2*>(at + Stage::VS + r * 8) = make_uint2(0, 0);
-                        else *reinterpret_cast<uint32_t*>(at + Stage::VS + r * 4) = 0;
+                        if constexpr (D == 128) *reinterpret_cast<uint2*>(at + Stage::HALF + Stage::CODES + r * 8) = make_uint2(0, 0);
+                        else *reinterpret_cast<uint32_t*>(at + Stage::HALF + Stage::CODES + r * 4) = 0;
                     }
                 }
                 if constexpr (WM == 1) __syncwarp();
@@ -527,6 +533,219 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + left * 8);
         }
+    }
+}
+
+// ------------------------------------------------------------------ 33 to 64 rows of 64-wide heads
+// Four warps of sixteen rows over the same blocks would each unpack all of a block (128 x 51 queries over 51 to 307 keys 39 us); here each unpacks a quarter, into a tile of fp16 in shared memory,
+// and the products read that (ldmatrix; rows of 128 bytes, 16-byte pieces XORed with the row's low three bits).  Two tiles: a warp that has met the others at a block's barrier knows that the tile
+// of the block before has been read.
+template <typename T> struct Fp4Tile : TaRows<T, 64> {
+    using Base = TaRows<T, 64>;
+    using Base::o; using Base::ma; using Base::mb; using Base::la; using Base::lb;
+    static constexpr int NK = TA_BLOCK / 8, ND = 8;
+    // As TaRows::block, but operands are fp16, rows have scales of their own, and probabilities are 2^15 times their value.
+    template <typename W>
+    __device__ __forceinline__ void tile(const uint32_t (*qf)[4], uint32_t ks, uint32_t vs, bool tail, int base0, float sa, float sb, W window) {
+        const int lane = threadIdx.x & 31;
+        auto at = [](uint32_t side, int r, int c) { return side + r * 128 + ((c ^ (r & 7)) << 4); };
+        float sc[NK][4];
+#pragma unroll
+        for (int i = 0; i < NK; ++i) sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int n = 0; n < TA_BLOCK / 16; ++n) {
+                uint32_t x[4];
+                ta_ldsm4(at(ks, n * 16 + (lane & 7) + ((lane >> 4) << 3), kk * 2 + ((lane >> 3) & 1)), x);
+                Half<__half>::mma(sc[2 * n], qf[kk], x[0], x[1]);
+                Half<__half>::mma(sc[2 * n + 1], qf[kk], x[2], x[3]);
+            }
+        if (tail) {
+#pragma unroll
+            for (int n = 0; n < TA_BLOCK / 32; ++n) {
+                const uint32_t wa = window(0, base0 + n * 32), wb = window(1, base0 + n * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int bit = i * 8 + (lane & 3) * 2;
+                    float* c = sc[n * 4 + i];
+                    if (!(wa >> bit & 1)) c[0] = -INFINITY;
+                    if (!(wa >> bit & 2)) c[1] = -INFINITY;
+                    if (!(wb >> bit & 1)) c[2] = -INFINITY;
+                    if (!(wb >> bit & 2)) c[3] = -INFINITY;
+                }
+            }
+        }
+        float na = -INFINITY, nb = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) { na = fmaxf(na, fmaxf(sc[i][0], sc[i][1])); nb = fmaxf(nb, fmaxf(sc[i][2], sc[i][3])); }
+        na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1));
+        na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 2)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
+        na = fmaxf(ma, na * sa); nb = fmaxf(mb, nb * sb);
+        auto huge = [](float x) { return fabsf(x) > 1048576.f && fabsf(x) < INFINITY; };
+        if (__any_sync(0xffffffffu, huge(na) || huge(nb))) {            // (as in Fp4Rows)
+#pragma unroll
+            for (int i = 0; i < NK; ++i) { sc[i][0] *= sa; sc[i][1] *= sa; sc[i][2] *= sb; sc[i][3] *= sb; }
+            sa = sb = 1.f;
+        }
+        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
+        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
+        ma = na; mb = nb;
+        la *= fa; lb *= fb;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
+        const float ua = P_SHIFT - za, ub = P_SHIFT - zb;
+#pragma unroll
+        for (int n = 0; n < TA_BLOCK / 16; ++n) {
+            uint32_t pf[4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float* c = sc[2 * n + e];
+                c[0] = ta_exp2(fmaf(c[0], sa, ua)); c[1] = ta_exp2(fmaf(c[1], sa, ua));
+                c[2] = ta_exp2(fmaf(c[2], sb, ub)); c[3] = ta_exp2(fmaf(c[3], sb, ub));
+                pf[2 * e] = half_pair(c[0], c[1]);
+                pf[2 * e + 1] = half_pair(c[2], c[3]);
+                la = Half<__half>::add(la, pf[2 * e]); lb = Half<__half>::add(lb, pf[2 * e + 1]);
+            }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                uint32_t x[4];
+                ta_ldsm4_t(at(vs, n * 16 + (lane & 15), d * 2 + (lane >> 4)), x);
+                Half<__half>::mma(o[2 * d], pf, x[0], x[1]);
+                Half<__half>::mma(o[2 * d + 1], pf, x[2], x[3]);
+            }
+        }
+    }
+};
+
+template <typename T, int NS, int PER_SM>
+__global__ void __launch_bounds__(160, PER_SM) k_fp4_tile(Fp4Attn a) {
+    using Stage = Fp4Stage<64>;
+    constexpr int ROWS = 64, KT = TA_BLOCK, STAGE = Stage::BYTES, SIDE = KT * 128;
+    extern __shared__ __align__(128) char fp4_smem[];
+    __shared__ __align__(8) uint64_t bars[2 * NS];
+    __shared__ int abort_flag;
+    char* tiles = fp4_smem;                               // [2][keys, values][64][128]
+    char* ring = tiles + 4 * SIDE;
+    int4* seqs = (int4*)(ring + NS * STAGE);              // [B] where sequences are cut
+    uint32_t* any = (uint32_t*)(seqs + (a.direct == 1 ? 0 : a.B));
+    uint32_t* mask = any + a.words;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t full = smem_u32(bars), empty = full + NS * 8;
+    if (warp == 4 && lane == 0) {
+        for (int i = 0; i < NS; ++i) { mbar_init(full + i * 8, 1); mbar_init(empty + i * 8, 4); }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    op_begin();
+    TaWork work;
+    work.begin(a, seqs);
+    __syncthreads();
+    if (warp == 4) { fp4_load<64, 1, NS>(a, work, seqs, ring, full, empty, &abort_flag); return; }
+
+    const int all_rows = a.T * a.group;
+    auto together = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+    int count = 0;                                        // blocks so far
+    Part it;
+    while (work.next(a, seqs, it, tid == 0)) {
+        const SeqKeys& s = it.s;
+        const int r0 = it.tile * ROWS, t0 = ta_node(a, r0), ra = warp * 16 + (lane >> 2), ga = r0 + ra, gb = ga + 8, ta = ta_node(a, ga), tb = ta_node(a, gb);
+        const bool live_a = ga < all_rows && ta < s.nodes, live_b = gb < all_rows && tb < s.nodes;
+        const bool own = a.words <= 2;                    // as in k_fp4_mma
+        const uint32_t* words = a.mask + it.b * a.mask_sb;
+        uint32_t seen[2] = {0, 0}, see[2][2] = {{0, 0}, {0, 0}};
+        if (own) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                if (w < a.words && lane < s.nodes) seen[w] = words[lane * a.words + w];
+                if (w < a.words && lane + 32 < s.nodes) seen[w] |= words[(lane + 32) * a.words + w];
+                if (w < a.words && live_a) see[0][w] = words[ta * a.words + w];
+                if (w < a.words && live_b) see[1][w] = words[tb * a.words + w];
+            }
+        }
+        // the queries as fragments: fp16, rows scaled by powers of two
+        uint32_t qf[4][4];
+        float sa = a.unit_k ? a.scale * a.unit_k[it.h] : a.scale, sb = sa;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const bool live = e ? live_b : live_a;
+            const int gr = e ? gb : ga, node = e ? tb : ta;
+            const char* p = a.q + it.b * a.q_sb + node * a.q_st + (it.h * a.group + gr - node * a.group) * a.q_sh + (lane & 3) * 4;
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = 0;
+                if (live) w[i] = a.q_vec ? *reinterpret_cast<const uint32_t*>(p + i * 16) : reinterpret_cast<const unsigned short*>(p + i * 16)[0] | (uint32_t)reinterpret_cast<const unsigned short*>(p + i * 16)[1] << 16;
+            }
+            if constexpr (!std::is_same<T, __half>::value) {
+                float top = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1)); top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int shift = row_shift(top);
+                const float f = power2(shift);
+                (e ? sb : sa) *= power2(-shift);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = half_pair(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qf[i >> 1][e + 2 * (i & 1)] = w[i];
+        }
+        if (own) {
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int left = s.nodes - w * 32;
+                seen[w] = __reduce_or_sync(0xffffffffu, seen[w]) & (left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u);
+            }
+        } else {
+            ta_load_masks<128, 1>(a, it.b, r0, min(ROWS, all_rows - r0), s.nodes, mask, any);
+        }
+        auto window = [&](int e, int base) {
+            if (!(e ? live_b : live_a)) return 0u;
+            return own ? ta_window2(see[e][0] & seen[0], see[e][1] & seen[1], base) : ta_window(mask + ((e ? tb : ta) - t0) * a.words, a.words, base);
+        };
+        Fp4Tile<T> rows;
+        rows.clear();
+        for (int j = 0; j < it.blocks; ++j, ++count) {
+            const int st = count % NS, k0 = it.k_begin + j * KT;
+            const bool tail = k0 + KT > s.len, ok = mbar_wait_warp<true>(full + st * 8, (count / NS) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT);
+            const char* at = ring + st * STAGE;
+            char* to = tiles + (count & 1) * 2 * SIDE;
+            // keys of this warp: sixteen, a lane half a key's codes: four pieces of eight channels.  Values that no query sees: zeros, whatever is there is multiplied by 0
+            const int r = warp * 16 + (lane >> 1), half = lane & 1;
+            bool there = true;
+            if (tail) {
+                const int base = k0 + (r & ~31) - s.len;
+                there = (own ? ta_window2(seen[0], seen[1], base) : ta_window(any, a.words, base)) >> (r & 31) & 1;
+            }
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                const uint4 c = *reinterpret_cast<const uint4*>(at + side * Stage::HALF + r * 32 + half * 16);
+                uint32_t z = fp4_scales2(*reinterpret_cast<const unsigned short*>(at + side * Stage::HALF + Stage::CODES + r * 4 + half * 2));
+                if (side && !there) z = 0;
+                const uint32_t z2[2] = {__byte_perm(z, z, 0x1010), __byte_perm(z, z, 0x3232)}, w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t x[4];
+                    fp4_unpack8(w[q], x);
+                    *reinterpret_cast<uint4*>(to + side * SIDE + r * 128 + (((half * 4 + q) ^ (r & 7)) << 4)) =
+                        make_uint4(h2_mul(x[0], z2[q >> 1]), h2_mul(x[1], z2[q >> 1]), h2_mul(x[2], z2[q >> 1]), h2_mul(x[3], z2[q >> 1]));
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + st * 8);
+            together();
+            if (!ok) continue;                            // (the others wait at the barrier)
+            rows.tile(qf, smem_u32(to), smem_u32(to) + SIDE, tail, k0 - s.len, sa, sb, window);
+        }
+        rows.finish(live_a, live_b);
+        const float unit = a.unit_v ? a.unit_v[it.h] : 1.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rows.o[i][e] *= unit;
+        rows.store(a, it, r0, ra, ROWS);
+        together();                                       // masks, and the tile of the next block but one, may be overwritten
     }
 }
 
@@ -573,6 +792,13 @@ cudaError_t run(const Fp4Attn& a, int grid, cudaStream_t st) {
     if (const cudaError_t e = op_allow<k_fp4_mma<T, D, NT, WM, WK, NS, PER_SM>>(bytes(WORDS, TA_MAX_B))) return e;
     return op_launch(k_fp4_mma<T, D, NT, WM, WK, NS, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 32 * (WM * WK + 1), bytes(a.words, a.direct == 1 ? 0 : a.B), st, 1, a);
 }
+template <typename T, int NS, int PER_SM>
+cudaError_t run_tile(const Fp4Attn& a, int grid, cudaStream_t st) {
+    auto bytes = [](int words, int B) { return 4 * TA_BLOCK * 128 + NS * Fp4Stage<64>::BYTES + 65 * words * 4 + B * 16; };
+    static_assert(4 * TA_BLOCK * 128 + NS * Fp4Stage<64>::BYTES + 65 * 128 + TA_MAX_B * 16 + 1024 + 512 <= 233472 / PER_SM, "shared memory of an SM");
+    if (const cudaError_t e = op_allow<k_fp4_tile<T, NS, PER_SM>>(bytes(32, TA_MAX_B))) return e;
+    return op_launch(k_fp4_tile<T, NS, PER_SM>, dim3(ta_grid(a, grid, PER_SM * TA_SMS)), 160, bytes(a.words, a.direct == 1 ? 0 : a.B), st, 1, a);
+}
 template <typename T>
 cudaError_t pick(const Fp4Attn& a, int rows, int grid, cudaStream_t st) {
     if constexpr (sizeof(T) == 4) {
@@ -580,7 +806,7 @@ cudaError_t pick(const Fp4Attn& a, int rows, int grid, cudaStream_t st) {
         return rows == 8 ? run<T, 64, 1, 1, 3, 9, 3>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 2>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 2>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 2>(a, grid, st);
     } else {
         if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 4, 8, 3>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 6, 3>(a, grid, st) : run<T, 128, 1, 4, 1, 6, 3>(a, grid, st);
-        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 1, 2, 2, 8, 3>(a, grid, st) : rows == 32 ? run<T, 64, 1, 4, 1, 8, 3>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 3>(a, grid, st);
+        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 1, 2, 2, 8, 3>(a, grid, st) : rows == 32 ? run<T, 64, 1, 4, 1, 8, 3>(a, grid, st) : run_tile<T, 5, 3>(a, grid, st);
     }
 }
 

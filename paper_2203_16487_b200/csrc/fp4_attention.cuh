@@ -12,9 +12,9 @@ struct Fp4Attn : TreeAttn {                               // k, v, s_page, s_hea
     const float* unit_k; const float* unit_v;             // [K/V head] or null
 };
 
-// A block of 64 keys of one head as it lies in memory: codes of keys and values, then their scales.
+// A block of 64 keys of one head as it lies in memory: keys, then values, of each the codes and their scales.
 template <int D> struct Fp4Stage {
-    static constexpr int CODES = TA_BLOCK * D / 2, SCALES = TA_BLOCK * D / 16, V = CODES, KS = 2 * CODES, VS = 2 * CODES + SCALES, BYTES = 2 * CODES + 2 * SCALES;
+    static constexpr int CODES = TA_BLOCK * D / 2, HALF = CODES + TA_BLOCK * D / 16, BYTES = 2 * HALF;
 };
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
