@@ -516,21 +516,10 @@ __global__ void __launch_bounds__(CP_ALLOC_THREADS) k_reorder_one(Cache c, Beams
     }
 }
 
-// Pieces [lo, hi) by a warp, eight of a lane's on their way at a time.
-template <typename P, typename At>
-__device__ __forceinline__ void copy_pieces_warp(const char* a, char* b, int lo, int hi, At at) {
-    for (int u0 = lo + (threadIdx.x & 31); u0 < hi; u0 += 256) {
-        P x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) if (u0 + j * 32 < hi) x[j] = *reinterpret_cast<const P*>(a + at(u0 + j * 32));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) if (u0 + j * 32 < hi) *reinterpret_cast<P*>(b + at(u0 + j * 32)) = x[j];
-    }
-}
 // 2 of 2: CTAs that stay.  The entries' tables (without pages: the references undone), unless k_reorder_one has written them; then copies, 256 pieces (4 KB) of a layer and side, of 4 bits
 // of one head, a warp.
 template <int LIES, bool ONE>
-__global__ void __launch_bounds__(256) k_reorder_copy(Cache c, Beams b, int sides) {
+__global__ void __launch_bounds__(256, 4) k_reorder_copy(Cache c, Beams b, int sides) {
     op_begin();
     const int jobs = c.sc_ok()[1], pt = 1 << c.page_shift;
     if constexpr (!ONE) {
@@ -565,17 +554,28 @@ __global__ void __launch_bounds__(256) k_reorder_copy(Cache c, Beams b, int side
         }
         const int to = c.sc_pages()[job];
         if (!c.page_ok(from) || share * 256 >= part * per) continue;
-        const char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + (LIES == PAGE_FP4 ? h * c.s_head : 0);
-        copy_pieces_warp<int4>(base + from * c.s_page, const_cast<char*>(base) + to * c.s_page, share * 256, min(part * per, share * 256 + 256), [&](int u) -> long long {
+        // eight pieces of a lane and (4 bits) four of scales, all read before the first is written
+        char* base = c.kv + (side >> 1) * c.s_layer + (side & 1) * c.s_side + (LIES == PAGE_FP4 ? h * c.s_head : 0);
+        const int lane = threadIdx.x & 31, lo = share * 256 + lane, hi = min(part * per, share * 256 + 256);
+        auto at = [&](int u) -> long long {
             if (LIES != PAGE_ROWS) return (long long)u * 16;
             const int t = u / per, x = u - t * per, g = x / c.chunks;
             return t * c.s_token + g * c.s_head + (x - g * c.chunks) * 16;
-        });
+        };
+        int4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (lo + j * 32 < hi) x[j] = ld16(base + from * c.s_page + at(lo + j * 32));
         if constexpr (LIES == PAGE_FP4) {
             char* scales = c.sc + (side >> 1) * c.c_layer + (side & 1) * c.c_side + h * c.c_head;
-            const int n = part * c.c_chunks, each = 256 / c.chunks * c.c_chunks;        // (of the tokens whose codes this share has)
-            copy_pieces_warp<int>(scales + from * c.c_page, scales + to * c.c_page, share * each, min(n, share * each + each), [&](int u) -> long long { return u * 4LL; });
+            const int s_lo = share * 128 + lane, s_hi = min(part * c.c_chunks, share * 128 + 128);         // (of the tokens whose codes this share has: two scales' pieces for four of codes, or one for two)
+            int y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (s_lo + j * 32 < s_hi) y[j] = *reinterpret_cast<const int*>(scales + from * c.c_page + (s_lo + j * 32) * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (s_lo + j * 32 < s_hi) *reinterpret_cast<int*>(scales + to * c.c_page + (s_lo + j * 32) * 4) = y[j];
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (lo + j * 32 < hi) st16(base + to * c.s_page + at(lo + j * 32), x[j]);
     }
 }
 

@@ -754,7 +754,7 @@ struct Plan { int rows, tiles, per_sm, direct, ctas, unit, min_blocks; long long
 // CTAs that an SM holds, as pick has them.
 constexpr int per_sm_of(int dtype, int dim, int rows) {
     if (rows >= 128) return 1;
-    if (dtype == SPECDEC_DTYPE_F32) return dim > 64 ? (rows == 64 ? 1 : 2) : rows == 8 ? 3 : 2;
+    if (dtype == SPECDEC_DTYPE_F32) return dim > 64 ? (rows == 64 ? 1 : 2) : rows <= 16 ? 3 : 2;
     return rows == 8 && dim == 64 ? 4 : 3;
 }
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, long long max_keys) {
@@ -803,7 +803,7 @@ template <typename T>
 cudaError_t pick(const Fp4Attn& a, int rows, int grid, cudaStream_t st) {
     if constexpr (sizeof(T) == 4) {
         if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 3, 9, 2>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 8, 2>(a, grid, st) : rows == 32 ? run<T, 128, 1, 4, 1, 6, 2>(a, grid, st) : run<T, 128, 1, 8, 1, 8, 1>(a, grid, st);
-        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 3>(a, grid, st) : rows == 16 ? run<T, 64, 2, 1, 3, 9, 2>(a, grid, st) : rows == 32 ? run<T, 64, 2, 2, 1, 8, 2>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 2>(a, grid, st);
+        return rows == 8 ? run<T, 64, 1, 1, 3, 9, 3>(a, grid, st) : rows == 16 ? run<T, 64, 1, 2, 2, 8, 3>(a, grid, st) : rows == 32 ? run<T, 64, 1, 4, 1, 8, 2>(a, grid, st) : run<T, 64, 2, 4, 1, 8, 2>(a, grid, st);
     } else {
         if (a.dim > 64) return rows == 8 ? run<T, 128, 1, 1, 4, 8, 3>(a, grid, st) : rows == 16 ? run<T, 128, 1, 2, 2, 6, 3>(a, grid, st) : run<T, 128, 1, 4, 1, 6, 3>(a, grid, st);
         return rows == 8 ? run<T, 64, 1, 1, 3, 9, 4>(a, grid, st) : rows == 16 ? run<T, 64, 1, 2, 2, 8, 3>(a, grid, st) : rows == 32 ? run<T, 64, 1, 4, 1, 8, 3>(a, grid, st) : run_tile<T, 5, 3>(a, grid, st);
