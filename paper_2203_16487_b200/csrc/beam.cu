@@ -88,6 +88,9 @@ __device__ __forceinline__ float lo2(u64 d) { return __uint_as_float((uint32_t)d
 __device__ __forceinline__ float hi2(u64 d) { return __uint_as_float((uint32_t)(d >> 32)); }
 __device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+// A term of a stretch's sum: e^(l - m) with c = m log2 e rounded, and what that rounding has put into every term.
+__device__ __forceinline__ float term(float l, float c) { return exp2_of(fmaf(l, LOG2E, -c)); }
+__device__ __forceinline__ float remainder_of(float m) { return exp2f(-fmaf(m, LOG2E, -(m * LOG2E))); }
 __device__ __forceinline__ u64 warp_max(u64 v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) { const u64 u = __shfl_xor_sync(0xffffffffu, v, o); if (u > v) v = u; }
@@ -184,7 +187,7 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
 #pragma unroll 1
             for (int j = 0; j < NV; ++j) {
                 const uint4 v = fetch(j);
-                for (int i = 0; i < VE; ++i) s += fmaxf(exp2_of(fmaf(Vec<T>::at(v, i), LOG2E, -c)), 0.f);
+                for (int i = 0; i < VE; ++i) s += fmaxf(term(Vec<T>::at(v, i), c), 0.f);
             }
         }
     } else if (m == INFINITY) {                           // the infinite ones share the row
@@ -218,7 +221,7 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < BM_WARPS; ++w) sum += w_sum[w];
-        if (m > -INFINITY && m < INFINITY) sum *= exp2f(-fmaf(m, LOG2E, -(m * LOG2E)));          // what the rounding of m log2 e has put into every term
+        if (m > -INFINITY && m < INFINITY) sum *= remainder_of(m);
         a.sums[at] = make_float2(m, sum);
     }
     u64* out = a.lists + at * a.n;
@@ -415,9 +418,12 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
             const T* p = (const T*)a.logits + (long long)(row0 + k) * a.s_row;
             const double top = beams[k].top;
             double s = 0.0;
-            for (int i = tid; i < a.V; i += BJ_NT) {
-                const float l = as_float(p[i]);
-                if (l == l) s += exp((double)l - top);
+            for (int i0 = tid; i0 < a.V; i0 += 8 * BJ_NT) {
+                float l[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) l[j] = i0 + j * BJ_NT < a.V ? as_float(p[i0 + j * BJ_NT]) : -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += l[j] > -INFINITY ? exp((double)l[j] - top) : 0.0;     // (NaN weigh nothing; eight in flight)
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);

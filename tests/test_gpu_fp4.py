@@ -204,6 +204,29 @@ def test_reorder_of_many_beams():
             assert torch.equal(cache.kv, before)
 
 
+@pytest.mark.parametrize("n,K,H,D,page,L", [(1100, 550, 1, 64, 16, 2), (1400, 100, 3, 128, 16, 1), (200, 100, 2, 64, 64, 1)])
+def test_reorder_of_many_beams_in_4_bits(n, K, H, D, page, L):
+    """Codes and scales of more entries, or wider groups, than one CTA settles."""
+    rng = np.random.default_rng(n)
+    cache = empty(L, H, D, 2 * n, page, n, 2, fill=n)
+    ref = F.Pages(bytes_of(cache), n, 2)
+    seqs, top = list(range(n)), 2 * page - 1
+    lens = [int(x) for x in rng.integers(0, top + 1, n)]
+    cache.reserve(ints(seqs), top)
+    ref.reserve(seqs, top)
+    path = [list(range(m)) for m in lens]
+    cache.compact(ints(seqs), ints([p + [-1] * (top - len(p)) for p in path]), ints(lens))
+    ref.compact(seqs, path)
+    for _ in range(2):
+        groups = rng.permutation(n).reshape(-1, K).tolist()
+        parents = rng.integers(0, K, (n // K, K))
+        parents[0, ::7] = -1
+        assert ref.reorder(groups, parents.tolist()) == 0
+        cache.reorder(ints(groups), ints(parents.tolist()))
+        cache.check()
+        same(cache, ref)
+
+
 # ------------------------------------------------------------------ attention
 def attention_case(dtype, lens, T, H, Hkv, D, page, *, nodes=None, one_mask=False, seed=0, strided=False, mask=None, layer=0, spare=0, unit=None, q_times=2.0):
     """A cache with those lengths (the scales of slots that nobody sees are NaN), queries, masks, and the answer in 64 bits."""
