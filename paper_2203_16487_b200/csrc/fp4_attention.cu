@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), PER_SM) k_fp4_mma(Fp4Attn 
 }
 
 // ------------------------------------------------------------------ 33 to 64 rows of 64-wide heads
-// Four warps of sixteen rows over the same blocks would each unpack all of a block (128 x 51 queries over 51 to 307 keys 39 us); here each unpacks a quarter, into a tile of fp16 in shared memory,
+// Four warps of sixteen rows over the same blocks would each unpack all of a block (128 x 51 queries over 51 to 307 keys 39 us against 30); here each unpacks a quarter, into a tile of fp16 in shared memory,
 // and the products read that (ldmatrix; rows of 128 bytes, 16-byte pieces XORed with the row's low three bits).  Two tiles: a warp that has met the others at a block's barrier knows that the tile
 // of the block before has been read.
 template <typename T> struct Fp4Tile : TaRows<T, 64> {
@@ -760,6 +760,8 @@ constexpr int per_sm_of(int dtype, int dim, int rows) {
 Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, long long max_keys) {
     const int all = T * (n_q_heads / n_kv_heads);
     Plan p;
+    // 33 to 64 rows of 128-wide heads by eight warps of eight rows, each unpacking all of a block: 16 x 51 queries over 300 to 1000 keys 39 us, by tcgen05 28; of 64-wide heads by tcgen05
+    // 128 x 51 queries 64 us, by k_fp4_tile 30.  256 rows that share what is unpacked against twice 128: 8 x 64 queries, 32/8 heads, 152 and 224 us; 100 x 256 over 10 to 60 keys 117 and 145.
     const int most_mma = head_dim > 64 ? 32 : 64;
     p.rows = all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : all <= most_mma || dtype == SPECDEC_DTYPE_F32 ? 64 : all <= 128 || !fp4_tc_fits(head_dim, 256, T, n_q_heads / n_kv_heads) ? 128 : 256;
     p.tiles = (all + p.rows - 1) / p.rows;
@@ -768,9 +770,10 @@ Plan plan(int B, int T, int n_q_heads, int n_kv_heads, int dtype, int head_dim, 
     const long long columns = (long long)n_kv_heads * p.tiles, whole = B * columns, blocks = (max_keys + p.unit - 1) / p.unit;
     p.per_sm = per_sm_of(dtype, head_dim, p.rows);
     const int at_once = TA_SMS * p.per_sm;
-    // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge.
+    // Whole sequences take their rounds of CTAs times the longest's blocks, stretches an equal share of all blocks and the merge.  (64 x 51 queries over 0 to 256 keys whole 18 us, cut 29;
+    // 16 x 51 over 300 to 1000 28 and 38; 32 x 16 over 1000 to 2000 37 and 30.)  Dealt by length, where they are more than CTAs: 64 x 10 over 0 to 512 keys 20 -> 15, 128 x 26 39 -> 32, 128 x 51 33 -> 30.
     p.direct = (whole + at_once - 1) / at_once * blocks <= whole * blocks / at_once + 8 || B > TA_MAX_B;
-    if (p.direct && whole > at_once && 2 * columns <= at_once && B <= TA_MAX_B && p.rows >= 64 && blocks >= 4) p.direct = 2;
+    if (p.direct && whole > at_once && 2 * columns <= at_once && B <= TA_MAX_B && blocks >= 4) p.direct = 2;
     p.ctas = (int)(at_once / columns < 1 ? 1 : at_once / columns);
     const long long most = (B * blocks + p.min_blocks - 1) / p.min_blocks;                // stretches at most
     if (p.ctas > most) p.ctas = (int)most;

@@ -321,7 +321,7 @@ def test_attention_split_keys(dtype, T, H, Hkv, D, lens):
 
 @pytest.mark.parametrize("dtype", ALL)
 @pytest.mark.parametrize("T,H,Hkv,D,n", [(2, 12, 12, 64, 41), (2, 12, 12, 128, 41), (20, 12, 12, 64, 41), (3, 48, 4, 64, 60), (20, 12, 12, 128, 30), (66, 7, 7, 64, 30), (130, 6, 3, 64, 30),
-                                         (66, 7, 7, 128, 30), (40, 12, 12, 64, 41)])
+                                         (66, 7, 7, 128, 30), (40, 12, 12, 64, 41), (11, 12, 12, 64, 41), (4, 48, 12, 128, 41), (13, 16, 16, 128, 61)])
 def test_attention_many_short_sequences(dtype, T, H, Hkv, D, n):
     """More sequences and heads than CTAs that run at once, of every number of key blocks: CTAs that take several."""
     lens = [(i * 37) % 331 for i in range(n)]
