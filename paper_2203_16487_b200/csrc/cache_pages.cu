@@ -674,7 +674,7 @@ template <typename C> int reorder(const char* who, const C* c, const int32_t* d_
     const cudaStream_t st = (cudaStream_t)stream;
     const Beams b{d_seqs, d_parents, n, beams};
     const int sides = 2 * sizes(c).n_layers, l = lies(c, v);
-    // In one CTA where counts and tables fit its shared memory: with the copies 128 entries of 1400 pages 11.6 us instead of 12.4, 32 entries of 230 16.4 instead of 18.
+    // In one CTA where counts and tables fit its shared memory: with the copies 128 entries of 1400 pages 11.3 us instead of 12.3, 32 entries of 230 15.4 instead of 17.5.
     const long long bytes = 4 * ((long long)v.n_pages + (long long)n * v.max_pages);
     const bool one = n <= CP_ALLOC_THREADS && beams <= 64 && bytes <= REORDER_ONE;      // (at most 40960 pages: counts of 20 bits)
     if (one) if (const cudaError_t e = op_allow<k_reorder_one>(REORDER_ONE)) return op_done(who, e);

@@ -13,6 +13,9 @@
 //
 // Probabilities are fp16, 2^15 times their value: a weight 2^-29 of the largest is still a normal number, so that a hundred thousand small ones add up.  Their sum is one more product, with ones:
 // of the rounded ones, so that the weights add up to 1.
+//
+// What bounds it is instructions: 4 x 1 query, 32/8 heads of 128, over 65,537 to 131,071 keys (544 MB) 124 us with the merge, 4.4 TB/s; its loads alone 100, its products alone 103; issue 55 %.
+// (Over 16 bits two such sequences, 978 MB, take 151.)
 #include "fp4_attention.cuh"
 
 namespace sd {
