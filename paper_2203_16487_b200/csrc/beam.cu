@@ -168,6 +168,7 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
     bound = max(bound, NOTHING + 1);
     // the sum
     float s = 0.f;
+    const bool far = fabsf(m) >= 65536.f;                 // (as where a mask has put its type's lowest value) there m log2 e overflows, or its rounding is larger than the exponents that a float has
     if (m > -INFINITY && m < INFINITY) {
         const float c = m * LOG2E;
         u64 part[2] = {0, 0};                             // two sums each
@@ -183,12 +184,12 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
         }
         part[0] = add2(part[0], part[1]);
         s = lo2(part[0]) + hi2(part[0]);
-        if (s != s) {                                     // NaN weigh nothing
+        if (far || s != s) {                              // NaN weigh nothing
             s = 0.f;
 #pragma unroll 1
             for (int j = 0; j < NV; ++j) {
                 const uint4 v = fetch(j);
-                for (int i = 0; i < VE; ++i) s += fmaxf(term(Vec<T>::at(v, i), c), 0.f);
+                for (int i = 0; i < VE; ++i) s += fmaxf(far ? exp2_of((Vec<T>::at(v, i) - m) * LOG2E) : term(Vec<T>::at(v, i), c), 0.f);
             }
         }
     } else if (m == INFINITY) {                           // the infinite ones share the row
@@ -222,7 +223,7 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < BM_WARPS; ++w) sum += w_sum[w];
-        if (m > -INFINITY && m < INFINITY) sum *= remainder_of(m);
+        if (!far) sum *= remainder_of(m);
         a.sums[at] = make_float2(m, sum);
     }
     u64* out = a.lists + at * a.n;

@@ -28,7 +28,8 @@ def run(logits, scores, n, finished=None, end_token=0, norm=None):
         if near > 1e-12 or near == 0:
             assert parent[b].tolist() == [w[1] for w in want] and token[b].tolist() == [w[2] for w in want], (b, near)
         for x, w in zip(s[b], want):
-            assert x == w[0] or abs(x - w[0]) <= 2.0 ** -20 + 2.0 ** -24 * abs(w[0]), (b, x, w)
+            # (beyond fp32's largest number the nearest one is an infinity)
+            assert x == w[0] or abs(x - w[0]) <= 2.0 ** -20 + 2.0 ** -24 * abs(w[0]) or x == (-math.inf if w[0] < -2.0 ** 128 else w[0]), (b, x, w)
     return got
 
 
@@ -86,6 +87,25 @@ def test_select_ties_infinities_nan(dtype):
     for n in (1, 8, 63, 64):
         run(logits, scores, n)
     run(logits[:, :, :40], scores, 64)                         # rows that begin anywhere, evenly spaced
+
+
+@pytest.mark.parametrize("dtype", ALL)
+@pytest.mark.parametrize("V", [90, 32768, 50265])
+def test_select_masks_of_the_lowest_value_and_logits_of_any_size(dtype, V):
+    """Tokens that a mask has set to the type's lowest value: some, whole stretches, whole rows; logits around numbers of every size, whose sums' shares are whole or gone."""
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    logits, scores = rows(12, 3, V, dtype, V)
+    logits[0, :, ::3] = low
+    logits[1, :, 40:] = low
+    logits[2, :, :-5] = low
+    logits[3] = low
+    logits[4, 0], logits[4, 1, 7:] = low, -math.inf
+    logits[5], logits[5, :, 11], logits[5, 1, 50:] = low, high, math.nan
+    logits[6], logits[6, 1] = high, 0.0
+    for b, size in zip(range(7, 12), (6e4, 65536.0, 1e6, 1e9, 1e30)):
+        logits[b] = (logits[b].float() + (size if b % 2 else -size)).to(dtype).clamp(low, high)
+    for n in (1, 7):
+        run(logits, scores, n)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
