@@ -401,8 +401,11 @@ __device__ __forceinline__ void fp4_load(const Fp4Attn& a, TaWork work, const in
             if (n >= NG && !mbar_wait_warp<true>(empty + st * 8, (n / NG - 1) & 1, abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) return;
             char* to = ring + st * STAGE + at;
             const bool mine = lane < 4 * n_pages && key < it.k_end, real = mine && cur >= 0;
-            if (mine && cur < 0 && scales)            // a page that is none: zeros
+            if (mine && cur < 0 && scales) {          // a page that is none: zeros, ahead of what the stage's next block brings
                 for (int i = 0; i < size; i += 16) *reinterpret_cast<uint4*>(to + i) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            __syncwarp();
             const unsigned pieces = __popc(__ballot_sync(0xffffffffu, real));          // four a page
             if (lane == 0) mbar_expect_tx(full + st * 8, pieces / 4 * box * (D + D / 8));
             __syncwarp();

@@ -192,8 +192,10 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
                     if (h >= NR) ok = ok && wait(rempty + slot * 8, h / NR - 1);
                     if (!ok) break;
                     char* to = raw + slot * RAW;
-                    if (mine && cur < 0)                  // a page that is none: zeros
+                    if (mine && cur < 0) {                // a page that is none: zeros, ahead of what the slot's next block brings
                         for (int i = 0; i < box * DP / 16; i += 16) *reinterpret_cast<uint4*>(to + Cfg::CODES + lane * box * (DP / 16) + i) = make_uint4(0, 0, 0, 0);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
                     __syncwarp();
                     if (lane == 0) mbar_expect_tx(rfull + slot * 8, boxes * box * (DP / 2 + DP / 16));
                     __syncwarp();

@@ -380,6 +380,24 @@ def test_attention_queries_of_any_size(dtype, size):
     assert g1.isfinite().all() and ((g1 - g2).abs()[:, same_rows] <= 40 * 6 * u).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,Hkv,D,page", [(1, 8, 2, 128, 16), (20, 4, 4, 64, 64), (50, 4, 4, 64, 16), (50, 8, 4, 128, 32), (64, 16, 4, 64, 128)])
+def test_attention_pages_that_are_none(dtype, T, H, Hkv, D, page):
+    """Table entries below zero or beyond the pages read as a page of zeros, whatever else is on its way, and later blocks are as they were."""
+    from paper_2203_16487_b200 import tree
+    _, _, _, (cache, q, seqs, bits, nodes) = attention_case(dtype, [700, 0, 331], T, H, Hkv, D, page, seed=4)
+    free = sorted(set(range(cache.refs.numel())) - set(cache.table.flatten().tolist()))[0]
+    cache.codes[:, :, free], cache.scales.view(torch.uint8)[:, :, free] = 0, 0
+    at = [(0, 1), (0, 600 // page), (2, 0)]
+    out = []
+    for fill in (free, -1, cache.refs.numel(), 2 ** 31 - 1, -2 ** 31):
+        for b, i in at:
+            cache.table[int(seqs[b]), i] = fill
+        out.append(tree.attention(q, cache, 0, ints(seqs), bits, n_nodes=ints(nodes)))
+    cache.check()
+    assert all(torch.equal(x, out[0]) for x in out) and out[0].isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", ALL)
 def test_attention_masks(dtype):
     """Queries that see nothing, nodes that nobody sees (their slots hold NaN), nodes that see later ones."""
