@@ -193,15 +193,22 @@ template <typename T, int D, int NT> struct Fp4Rows {
                 huge |= fabsf(top[n][e]) > 1048576.f && fabsf(top[n][e]) < INFINITY;
                 grown |= top[n][e] != m[n][e];
             }
-        // Fused with the subtraction of their maximum, products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge they are rounded first.
+        // 2^(score * f + z) = 2^P_SHIFT * 2^(score - maximum).  Fused, the products leave what the maximum's rounding has cut off, and z is rounded too: nothing to speak of, but where scores are huge either
+        // is more than fp16 has room for above 2^P_SHIFT.  There the products are rounded as the maximum was, which is taken off before the shift is put on.
+        float z[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) z[n][e] = P_SHIFT - (top[n][e] == -INFINITY ? 0.f : top[n][e]);
         if (__any_sync(0xffffffffu, huge)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    const float y = top[n][e] == -INFINITY ? 0.f : top[n][e];
 #pragma unroll
-                    for (int i = 0; i < MK; ++i) { sc[n][i][e] *= f[n][e]; sc[n][i][2 + e] *= f[n][e]; }
-                    f[n][e] = 1.f;
+                    for (int i = 0; i < MK; ++i) { sc[n][i][e] = __fsub_rn(__fmul_rn(sc[n][i][e], f[n][e]), y); sc[n][i][2 + e] = __fsub_rn(__fmul_rn(sc[n][i][2 + e], f[n][e]), y); }
+                    f[n][e] = 1.f; z[n][e] = P_SHIFT;
                 }
         }
         if (__any_sync(0xffffffffu, grown)) {
@@ -217,14 +224,11 @@ template <typename T, int D, int NT> struct Fp4Rows {
         uint32_t pf[PARTS][NT][MK][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float z[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) z[e] = P_SHIFT - (top[n][e] == -INFINITY ? 0.f : top[n][e]);
 #pragma unroll
             for (int i = 0; i < MK; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float u = ta_exp2(fmaf(sc[n][i][2 * h], f[n][0], z[0])), v = ta_exp2(fmaf(sc[n][i][2 * h + 1], f[n][1], z[1]));
+                    const float u = ta_exp2(fmaf(sc[n][i][2 * h], f[n][0], z[n][0])), v = ta_exp2(fmaf(sc[n][i][2 * h + 1], f[n][1], z[n][1]));
                     const uint32_t y = half_pair(u, v);
                     pf[0][n][i][h] = transpose8(y);
                     if constexpr (WIDE) pf[PARTS - 1][n][i][h] = transpose8(rest_pair(u, v, y));
@@ -588,19 +592,23 @@ template <typename T> struct Fp4Tile : TaRows<T, 64> {
         na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1));
         na = fmaxf(na, __shfl_xor_sync(0xffffffffu, na, 2)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
         na = fmaxf(ma, na * sa); nb = fmaxf(mb, nb * sb);
+        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
+        float ua = P_SHIFT - za, ub = P_SHIFT - zb;
         auto huge = [](float x) { return fabsf(x) > 1048576.f && fabsf(x) < INFINITY; };
         if (__any_sync(0xffffffffu, huge(na) || huge(nb))) {            // (as in Fp4Rows)
 #pragma unroll
-            for (int i = 0; i < NK; ++i) { sc[i][0] *= sa; sc[i][1] *= sa; sc[i][2] *= sb; sc[i][3] *= sb; }
+            for (int i = 0; i < NK; ++i) {
+                sc[i][0] = __fsub_rn(__fmul_rn(sc[i][0], sa), za); sc[i][1] = __fsub_rn(__fmul_rn(sc[i][1], sa), za);
+                sc[i][2] = __fsub_rn(__fmul_rn(sc[i][2], sb), zb); sc[i][3] = __fsub_rn(__fmul_rn(sc[i][3], sb), zb);
+            }
             sa = sb = 1.f;
+            ua = ub = P_SHIFT;
         }
-        const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
         const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
         ma = na; mb = nb;
         la *= fa; lb *= fb;
 #pragma unroll
         for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
-        const float ua = P_SHIFT - za, ub = P_SHIFT - zb;
 #pragma unroll
         for (int n = 0; n < TA_BLOCK / 16; ++n) {
             uint32_t pf[4];
