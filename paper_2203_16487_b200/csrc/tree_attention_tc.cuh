@@ -404,7 +404,7 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
             for (int e = 0; e < KT; e += 2)
                 t4[e / 2 % 4] = fmaxf(t4[e / 2 % 4], fmaxf(__uint_as_float(x[e / 32][e % 32]), __uint_as_float(x[e / 32][e % 32 + 1])));
             const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * scale;
-            const bool grow = top > (m == -INFINITY ? m : m + 8.f);
+            const bool grow = top - m > 8.f;              // (not top > m + 8, which may be rounded up to the next number behind m; nothing seen so far: infinite)
             if (__any_sync(0xffffffffu, grow)) {
                 const float f = grow ? ta_exp2(m - top) : 1.f;              // (m = -inf: 0)
                 if (grow) m = top;
@@ -421,9 +421,17 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
                     }
                 }
             }
-            const float z = (m == -INFINITY ? 0.f : m) - P_SHIFT;
+            // Fused, the products leave what the maximum's rounding has cut off, and the difference to the shift is rounded too: nothing to speak of, but where scores are huge either is more than the
+            // probabilities' type has room for.  There the products are rounded as the maximum was, which is taken off before the shift is put on.
+            const float y0 = m == -INFINITY ? 0.f : m;
+            float times = scale, plus = P_SHIFT - y0;
+            if (__any_sync(0xffffffffu, fabsf(y0) > 1048576.f && fabsf(y0) < INFINITY)) {
+#pragma unroll
+                for (int e = 0; e < KT; ++e) x[e / 32][e % 32] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x[e / 32][e % 32]), scale), y0));
+                times = 1.f; plus = P_SHIFT;
+            }
             float sum[4] = {0.f, 0.f, 0.f, 0.f};          // of the rounded probabilities
-            const uint64_t scale2 = pair2(scale, scale), z2 = pair2(-z, -z);
+            const uint64_t scale2 = pair2(times, times), z2 = pair2(plus, plus);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
