@@ -314,14 +314,25 @@ struct TaRows {
         la *= fa; lb *= fb;
 #pragma unroll
         for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
+        // Fused, the products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge it is more than the type has room for, and they are rounded as the maximum was.
+        float times = scale, ua = -za, ub = -zb;
+        auto huge = [](float x) { return fabsf(x) > 1048576.f && fabsf(x) < INFINITY; };
+        if (__any_sync(0xffffffffu, huge(na) || huge(nb))) {
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+                sc[i][0] = __fsub_rn(__fmul_rn(sc[i][0], scale), za); sc[i][1] = __fsub_rn(__fmul_rn(sc[i][1], scale), za);
+                sc[i][2] = __fsub_rn(__fmul_rn(sc[i][2], scale), zb); sc[i][3] = __fsub_rn(__fmul_rn(sc[i][3], scale), zb);
+            }
+            times = 1.f; ua = ub = 0.f;
+        }
 #pragma unroll
         for (int n = 0; n < TA_BLOCK / 16; ++n) {
             uint32_t pf[4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float* c = sc[2 * n + e];
-                c[0] = ta_exp2(fmaf(c[0], scale, -za)); c[1] = ta_exp2(fmaf(c[1], scale, -za));
-                c[2] = ta_exp2(fmaf(c[2], scale, -zb)); c[3] = ta_exp2(fmaf(c[3], scale, -zb));
+                c[0] = ta_exp2(fmaf(c[0], times, ua)); c[1] = ta_exp2(fmaf(c[1], times, ua));
+                c[2] = ta_exp2(fmaf(c[2], times, ub)); c[3] = ta_exp2(fmaf(c[3], times, ub));
                 pf[2 * e] = Half<T>::pack(c[0], c[1]);
                 pf[2 * e + 1] = Half<T>::pack(c[2], c[3]);
                 la = Half<T>::add(la, pf[2 * e]); lb = Half<T>::add(lb, pf[2 * e + 1]);

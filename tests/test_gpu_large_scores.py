@@ -13,7 +13,7 @@ KINDS = [("4", torch.bfloat16), ("4", torch.float16), ("4", torch.float32), ("16
 # nodes, heads, K/V heads, width, page, lengths: tiles of 8, 16, 32, 64, 128 and 256 rows; one block of keys, several, sequences that are cut
 SHAPES = [(1, 8, 8, 64, 16, [0, 9, 63]), (1, 8, 2, 128, 16, [300, 70]), (1, 2, 2, 64, 16, [5000]), (1, 4, 1, 128, 64, [4000, 3]), (12, 2, 2, 64, 16, [20, 300]), (26, 2, 2, 128, 16, [130, 1900]), (51, 2, 2, 64, 16, [10, 300]),
           (51, 2, 2, 64, 32, [3000]), (40, 4, 2, 128, 16, [7, 400]), (60, 4, 2, 64, 16, [20, 500]), (64, 8, 2, 128, 64, [30, 700]), (64, 4, 1, 64, 64, [3000]), (40, 3, 1, 128, 32, [2500])]
-CASES = [(*k, s) for k in KINDS for s in SHAPES[0 if k[0] == "4" or k[1] is torch.float32 else 8:]] + [(*k, (12, 2, 2, 64, 4, [20, 300])) for k in KINDS[5:]]
+CASES = [(*k, s) for k in KINDS for s in SHAPES] + [(*k, (12, 2, 2, 64, 4, [20, 300])) for k in KINDS if k[0] == "16"]
 
 
 def filled(kind, dtype, k, v, count, T, page):
