@@ -368,7 +368,19 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
         }
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;                  // this warp's lanes: 32 (warp % 4) in bits 16..31
         const uint32_t ts = tmem + g * KT + lanes, to = tmem + 256 + g * DP + lanes;
-        float m = -INFINITY, l = 0.f;
+        // Fused with the subtraction of its maximum, a product leaves what the maximum's rounding has cut off, and the difference to the shift is rounded too: nothing to speak of, but from 2^20 on either may be
+        // more than the probabilities' type has room for.
+        //   16 bits: such a maximum becomes 0, by taking the score that it came from off all of the row's scores, this block's and, `moved`, the later ones'.
+        //   4 bits: the products are rounded as the maximum was, which is taken off before the shift is put on.
+        // (8 x 64 queries over 8191 to 16385 keys without either 144.2 and 145.4 us, so 144.2 and 145.9; the first way over 4 bits 153, the second over 16 146.6.)
+        constexpr bool MOVES = !FP4;
+        auto beyond = [](float y) { return fabsf(y) > 1048576.f && fabsf(y) < INFINITY; };
+        float m = -INFINITY, l = 0.f, from = 0.f;
+        bool moved = false;                               // whether a row of the warp has a number taken off its scores
+        auto take_off = [](uint32_t (&x)[KT / 32][32], float y) {
+#pragma unroll
+            for (int e = 0; e < KT; ++e) x[e / 32][e % 32] = __float_as_uint(__fsub_rn(__uint_as_float(x[e / 32][e % 32]), y));
+        };
         for (int i = 0; i < n; ++i) {
             const int j = block_of(g, i), k0 = it.k_begin + j * KT;
             ok = ok && wait(sfull + g * 8, taken + i);    // (and with it the last second product, which was issued before)
@@ -380,7 +392,9 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
 #pragma unroll
             for (int c = 0; c < KT / 32; ++c) tmem_ld_done<32>(x[c]);
             const bool tail = k0 + KT > s.len;
-            if (tail) {
+            if (tail || moved) {                          // (one branch: two take 1 % longer)
+                if (moved) take_off(x, from);
+                if (tail) {
 #pragma unroll
                 for (int c = 0; c < KT / 32; ++c) {
                     const uint32_t w = live ? ta_window(row, a.words, k0 + c * 32 - s.len) : 0u;
@@ -398,17 +412,26 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
+                }
             }
             float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int e = 0; e < KT; e += 2)
                 t4[e / 2 % 4] = fmaxf(t4[e / 2 % 4], fmaxf(__uint_as_float(x[e / 32][e % 32]), __uint_as_float(x[e / 32][e % 32 + 1])));
-            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * scale;
-            const bool grow = top - m > 8.f;              // (not top > m + 8, which may be rounded up to the next number behind m; nothing seen so far: infinite)
+            const float most = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])), top = most * scale;
+            // (4 bits: not top > m + 8, which for a large m is rounded up to the next number behind it; nothing seen so far: infinite)
+            const bool grow = MOVES ? top > (m == -INFINITY ? m : m + 8.f) : top - m > 8.f;
             if (__any_sync(0xffffffffu, grow)) {
                 const float f = grow ? ta_exp2(m - top) : 1.f;              // (m = -inf: 0)
                 if (grow) m = top;
                 l *= f;
+                if (MOVES && __any_sync(0xffffffffu, beyond(m))) {
+                    const float y = beyond(m) ? most : 0.f;             // (a maximum beyond is of this block: older ones are 0 by now)
+                    take_off(x, y);
+                    from += y;
+                    if (beyond(m)) m = 0.f;
+                    moved = true;
+                }
                 if (i > 0) {
 #pragma unroll 1
                     for (int c = 0; c < DP / 16; ++c) {
@@ -421,13 +444,12 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
                     }
                 }
             }
-            // Fused, the products leave what the maximum's rounding has cut off, and the difference to the shift is rounded too: nothing to speak of, but where scores are huge either is more than the
-            // probabilities' type has room for.  There the products are rounded as the maximum was, which is taken off before the shift is put on.
             const float y0 = m == -INFINITY ? 0.f : m;
             float times = scale, plus = P_SHIFT - y0;
-            if (__any_sync(0xffffffffu, fabsf(y0) > 1048576.f && fabsf(y0) < INFINITY)) {
+            if (!MOVES && __any_sync(0xffffffffu, beyond(y0))) {
 #pragma unroll
-                for (int e = 0; e < KT; ++e) x[e / 32][e % 32] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x[e / 32][e % 32]), scale), y0));
+                for (int e = 0; e < KT; ++e) x[e / 32][e % 32] = __float_as_uint(__fmul_rn(__uint_as_float(x[e / 32][e % 32]), scale));
+                take_off(x, y0);
                 times = 1.f; plus = P_SHIFT;
             }
             float sum[4] = {0.f, 0.f, 0.f, 0.f};          // of the rounded probabilities
@@ -457,6 +479,7 @@ __device__ __forceinline__ void ta_tc(const CUtensorMap* tm, const Args& a) {
         taken += n;
         done += it.blocks;
         tc_fence_after();
+        if (moved) m = fmaf(from, scale, m);
         if (!live) { m = -INFINITY; l = 0.f; }
         if (l == 0.f) m = -INFINITY;
         float f = l == 0.f ? 0.f : 1.f, f1 = 0.f;         // shares of this group's output and, TILES = 1, of the other's
