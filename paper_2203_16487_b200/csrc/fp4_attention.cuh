@@ -19,9 +19,9 @@ template <int D> struct Fp4Stage {
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// The power of two that takes a row's largest number into [2^14, 2^15) is 2^(14 - e); 1 where there is none.  Returns 14 - e.
+// The power of two that takes a row's largest number into [2^14, 2^15) is 2^(14 - e); 1 where there is none, or an infinite one.  Returns 14 - e.
 __device__ __forceinline__ int row_shift(float top) {
-    if (!(top > 0.f) || top > 3e38f) return 0;
+    if (!(top > 0.f) || !(top < INFINITY)) return 0;
     const int e = (int)(__float_as_uint(top) >> 23) - 127;
     return 14 - max(e, -100);
 }

@@ -94,6 +94,29 @@ def test_the_winner_of_large_scores(kind, dtype, shape):
     cache.check()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_queries_up_to_the_largest_number(dtype, shape):
+    """Rows whose largest number is the type's, over 4 bits: finite, so they are scaled like any other."""
+    from paper_2203_16487_b200 import tree
+    T, H, Hkv, D, page, lens = shape
+    g = torch.Generator(device="cuda").manual_seed(T + D)
+    B, S, count = len(lens), max(lens) + T, [n + T for n in lens]
+    k, v = (torch.randn(B, S, Hkv, D, generator=g, device="cuda").to(dtype) for _ in "kv")
+    cache, seqs, kk, vv = filled("4", dtype, k, v, count, T, page)
+    words, see = chain(T)
+    q = torch.randn(B, T, H, D, generator=g, device="cuda").double()
+    q = (q / q.abs().amax(-1, keepdim=True) * torch.finfo(dtype).max).to(dtype)
+    assert q.isfinite().all()
+    for scale in (2.0 ** -121, 2.0 ** -100):
+        got = tree.attention(q, cache, 0, seqs, words, scale=scale)
+        want, _, lead, size = exact(q, kk, vv, count, scale, see)
+        if scale == 2.0 ** -121:                               # scores of some 2^9: winners are rarer
+            assert got.isfinite().all()
+        else:
+            check_winners(got, want, lead, size, dtype)
+
+
 @pytest.mark.parametrize("kind,dtype,shape", CASES)
 def test_later_keys_ahead_by_what_rounding_hides(kind, dtype, shape):
     """Scores that are exact in fp32, 1.125 * 2^27 and, of some keys, 16 and of later ones 32 (of log2) more.  One unit in the last place is 16 there: a maximum's next neighbour weighs 2^16 times as much."""
