@@ -309,12 +309,8 @@ struct TaRows {
         nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 1)); nb = fmaxf(nb, __shfl_xor_sync(0xffffffffu, nb, 2));
         na = fmaxf(ma, na * scale); nb = fmaxf(mb, nb * scale);
         const float za = na == -INFINITY ? 0.f : na, zb = nb == -INFINITY ? 0.f : nb;
-        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
-        ma = na; mb = nb;
-        la *= fa; lb *= fb;
-#pragma unroll
-        for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
         // Fused, the products leave what the maximum's rounding has cut off: nothing to speak of, but where scores are huge it is more than the type has room for, and they are rounded as the maximum was.
+        // (Ahead of the rescaling, which runs beside the exponentials.)
         float times = scale, ua = -za, ub = -zb;
         auto huge = [](float x) { return fabsf(x) > 1048576.f && fabsf(x) < INFINITY; };
         if (__any_sync(0xffffffffu, huge(na) || huge(nb))) {
@@ -325,6 +321,11 @@ struct TaRows {
             }
             times = 1.f; ua = ub = 0.f;
         }
+        const float fa = ta_exp2(ma - za), fb = ta_exp2(mb - zb);
+        ma = na; mb = nb;
+        la *= fa; lb *= fb;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) { o[i][0] *= fa; o[i][1] *= fa; o[i][2] *= fb; o[i][3] *= fb; }
 #pragma unroll
         for (int n = 0; n < TA_BLOCK / 16; ++n) {
             uint32_t pf[4];
