@@ -136,7 +136,14 @@ __global__ void __launch_bounds__(32 * (WM * WK + 1), DP > 64 ? 2 : 3) k_ta_tma(
         rows.clear();
         for (int j = wk; j < it.blocks; j += WK, ++count) {
             const int st = wk + WK * (count % NG), k0 = it.k_begin + j * KT;
-            if (!mbar_wait_warp<true>(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) break;
+            if (!mbar_wait_warp<true>(full + st * 8, (count / NG) & 1, &abort_flag, a.status, SPECDEC_CACHE_TIMEOUT)) {
+                // The part is given up; but warps of the group that have not given up wait at the barriers of its blocks for this one.
+                if constexpr (WM > 1)
+#pragma unroll 1
+                    for (; j < it.blocks; j += WK)
+                        if (it.k_begin + j * KT + KT > s.len) asm volatile("bar.sync %0, %1;" ::"r"(2 + wk), "n"(32 * WM) : "memory");
+                break;
+            }
             const uint32_t ks = smem_u32(ring + st * STAGE), vs = ks + SIDE;
             const bool tail = k0 + KT > s.len;            // nodes, or what is behind the last key
             if (tail) {                                   // values that no query sees: whatever is in them is multiplied by 0
