@@ -8,8 +8,8 @@
 // The n largest: the q-th largest of a warp's lanes' maxima, q = n / 8 rounded up, has q entries of the warp at or above it, so the least of the eight warps' is a bound below the n-th largest entry of
 // the stretch.  What lies above it (some 2 n entries) is listed and ranked by counting.  Where ties make more of it than the list holds, the largest entry below the last one is looked for n times.
 //
-// Sums are fp32, off by some 2^-22; scores and ranks are 64 bits from there on.  Where ranks of two beams lie within 2^-19 (times norm) of one another and the order of the best n would turn on it, the
-// sums of those beams are taken again in 64 bits: the choice is that of exact sums.
+// Sums are fp32, off by some 2^-22, by less than 2^-19 in any case; scores and ranks are 64 bits from there on.  Of two entries of different beams, one of which is among the best n, either the order is certain, as
+// their ranks lie more than twice that (times norm) apart, or the sums of both beams are taken again in 64 bits: the choice is that of exact sums.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -290,7 +290,7 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
     constexpr int BJ_WARPS = BJ_NT / 32;
     __shared__ Beam beams[BM_MOST];
     __shared__ u64 stage[BJ_STAGE];
-    __shared__ Candidate list[BJ_LIST], sorted[BM_MOST + 1], w_best[BJ_WARPS];
+    __shared__ Candidate list[BJ_LIST], sorted[BM_MOST], w_best[BJ_WARPS];
     __shared__ uint32_t w_bound[BJ_WARPS];
     __shared__ double w_sum[BJ_WARPS];
     __shared__ int count, again[BM_MOST];
@@ -348,7 +348,7 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
     Candidate d;
     for (int i = mixed + BJ_NT; i < all; i += BJ_NT) if (candidate(i, d)) mine = max(mine, (uint32_t)(ordered(d.rank) >> 32));
     uint32_t bound = 0;
-    for (int q = (a.n + 1 + BJ_WARPS - 1) / BJ_WARPS; q; --q) {       // (the one behind the n-th is looked at too)
+    for (int q = (a.n + BJ_WARPS - 1) / BJ_WARPS; q; --q) {
         bound = __reduce_max_sync(0xffffffffu, mine);
         const unsigned who = __ballot_sync(0xffffffffu, mine == bound);
         if (lane == __ffs(who) - 1) mine = 0;
@@ -362,7 +362,7 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
     double least = -INFINITY;
     if (bound) {
         const u64 u = (u64)bound << 32;
-        least = __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) - 4 * NEAR * norm;       // (ranks may still move by as much)
+        least = __longlong_as_double((long long)(u >> 63 ? u & ~(1ull << 63) : ~u)) - 4 * NEAR * norm;       // (ranks may still move by a quarter of that, the n-th's too, and twice that is near)
     }
     if (has && !(c.rank < least)) {
         const int k = atomicAdd(&count, 1);
@@ -375,7 +375,8 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
         }
     __syncthreads();
     const int found = count;
-    int best_n = min(found, a.n + 1);                     // sorted ones
+    const int best_n = min(found, a.n);                   // sorted ones
+    const double near = 2 * NEAR * norm;
     for (int round = 0; round <= a.K; ++round) {
         if (found <= BJ_LIST) {
             for (int i = tid / 8; i < (found + 3) / 4 * 4; i += BJ_NT / 8) {          // eight lanes an entry, whole warps
@@ -384,10 +385,10 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
                 for (int j = lane & 7; j < found; j += 8) rank += ahead(list[j], x);
 #pragma unroll
                 for (int o = 4; o; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
-                if ((lane & 7) == 0 && i < found && rank <= a.n) sorted[rank] = x;
+                if ((lane & 7) == 0 && i < found && rank < a.n) sorted[rank] = x;
             }
         } else {                                          // (more ties than the list holds)
-            for (int k = 0; k <= a.n; ++k) {
+            for (int k = 0; k < a.n; ++k) {
                 Candidate top{-INFINITY, 0, a.K};
                 for (int i = tid; i < all; i += BJ_NT)
                     if (candidate(i, c) && (k == 0 || ahead(sorted[k - 1], c)) && ahead(c, top)) top = c;
@@ -406,14 +407,20 @@ __device__ __forceinline__ void join_sentence(const BeamArgs& a, int b) {
             }
         }
         __syncthreads();
-        // neighbours of different beams whose order the sums' errors could turn
+        // entries of different beams whose order the sums' errors could turn, one of them at least among the best
         bool open = false;
-        if (tid + 1 < best_n) {
-            const Candidate x = sorted[tid], y = sorted[tid + 1];
-            if (x.beam != y.beam && x.rank - y.rank <= NEAR * (fabs(beams[x.beam].norm) + fabs(beams[y.beam].norm)))
-                for (int k : {x.beam, y.beam})
-                    if (!beams[k].done && !beams[k].exact && beams[k].top < INFINITY) { again[k] = 1; open = true; }
-        }
+        auto settle = [&](const Candidate& one, const Candidate& other) {
+            if (one.beam == other.beam || one.rank - other.rank > NEAR * (fabs(beams[one.beam].norm) + fabs(beams[other.beam].norm))) return;
+            for (int k : {one.beam, other.beam})
+                if (!beams[k].done && !beams[k].exact && beams[k].top < INFINITY) { again[k] = 1; open = true; }
+        };
+        if (tid < best_n)
+            for (int i = tid + 1; i < best_n && sorted[tid].rank - sorted[i].rank <= near; ++i) settle(sorted[tid], sorted[i]);
+        auto behind = [&](const Candidate& x) {
+            for (int i = best_n - 1; i >= 0 && sorted[i].rank - x.rank <= near && ahead(sorted[i], x); --i) settle(sorted[i], x);
+        };
+        if (found <= BJ_LIST) { if (tid < found) behind(list[tid]); }
+        else for (int i = tid; i < all; i += BJ_NT) if (candidate(i, c)) behind(c);
         if (!__syncthreads_or(open)) break;
         for (int k = 0; k < a.K; ++k) {                   // (the same for all threads)
             if (!again[k] || beams[k].exact) continue;
