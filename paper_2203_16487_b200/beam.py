@@ -72,6 +72,6 @@ def select(logits, scores, n: int, *, finished=None, end_token: int = 0, norm=No
     except struct.error as e:
         raise ValueError(f"end_token: {e}") from None
     _launch(lib.specdec_beam_select, at, (a, tree._raw_stream(at)))
-    if (logits.requires_grad or scores.requires_grad) and torch.is_grad_enabled():
-        out = _NoGradient.apply(out, logits if logits.requires_grad else scores, "beam.select")
+    if (logits.requires_grad or scores.requires_grad or (norm is not None and norm.requires_grad)) and torch.is_grad_enabled():
+        out = _NoGradient.apply(out, "beam.select", logits, scores, norm)
     return out, parent, token

@@ -16,7 +16,7 @@ from typing import Optional
 import torch
 
 from . import binding, tree
-from .tree import DTYPES, PagedCache, _ints, _launch
+from .tree import DTYPES, PagedCache, _ints, _launch, _NoGradient
 
 BLOCK = 16                                                   # channels of a scale
 _FP4 = 3                                                     # SPECDEC_DTYPE_FP4
@@ -95,4 +95,6 @@ class Fp4Cache(PagedCache):
         token = self.n_heads * self.head_dim
         self._tokens("read", _ints("seqs", seqs, (n,), at), k.data_ptr(), v.data_ptr(), 0 if start is None else _ints("start", start, (n,), at), n * n_tokens * token, n_tokens * token, token,
                      self.head_dim, n, 0 if layer is None else layer, layers, code, n_tokens)
+        if self._source is not None and torch.is_grad_enabled():
+            return tuple(_NoGradient.apply(x, "Fp4Cache.read", self._source) for x in (k, v))
         return k, v

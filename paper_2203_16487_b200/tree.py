@@ -49,10 +49,10 @@ def _launch(f, at, args):
 
 
 class _NoGradient(torch.autograd.Function):
-    """Passes a result on as one of `source`, which requires a gradient; there is none to give."""
+    """Passes a result on as one of `sources` (None: none), some of which require a gradient; there is none to give."""
 
     @staticmethod
-    def forward(ctx, result, source, name):
+    def forward(ctx, result, name, *sources):
         ctx.name = name
         return result
 
@@ -244,7 +244,7 @@ def attention(q, cache: PagedCache, layer: int, seqs, mask, *, n_nodes=None, max
     else:
         _launch(L.specdec_tree_attention, at, (cache._ref, a, _raw_stream(at)))
     if (q.requires_grad or cache._source is not None) and torch.is_grad_enabled():
-        return _NoGradient.apply(out, q if q.requires_grad else cache._source, "tree.attention")
+        return _NoGradient.apply(out, "tree.attention", q, cache._source)
     return out
 
 
@@ -275,5 +275,5 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     token = torch.empty_like(uniform, dtype=_I32)
     _launch(lib().specdec_sample, at, (logits.data_ptr(), code, stride, rows, V, uniform.data_ptr(), *ptrs, rows // n if n and rows else 1, token.data_ptr(), logprob.data_ptr(), _raw_stream(at)))
     if (logits.requires_grad or (temperature is not None and temperature.requires_grad)) and torch.is_grad_enabled():
-        logprob = _NoGradient.apply(logprob, logits if logits.requires_grad else temperature, "tree.sample")
+        logprob = _NoGradient.apply(logprob, "tree.sample", logits, temperature)
     return token, logprob
