@@ -239,7 +239,7 @@ long long specdec_cache_scratch(int n_seqs, int max_pages, int n_pages);
  *   given back.  Full pages are shared, the last, partly filled one is copied.  d_dst all different; a pair of equal numbers does nothing.
  * reorder: the n sequences are beams, in groups of `beams` that follow one another.  Sequence i of a group becomes what sequence d_parents[i] (0 .. beams - 1; -1: none, it
  *   is released) of the group was before the call.  Full pages are shared; the last, partly filled one goes on with one child (the parent itself if it is one, else the first) and is
- *   copied for the others, so that a permutation moves no data.  Pages that nobody holds any more are free, for the copies of this call too; they are given to the entries
+ *   copied for the others, so that a permutation moves no data.  d_seqs all different, over all groups.  Pages that nobody holds any more are free, for the copies of this call too; they are given to the entries
  *   that copy in their order.  Pages behind the committed tokens are given back.  Any other parent, or one whose sequence number is out of range: the entry is its own (BAD_INDEX). */
 int specdec_cache_reserve(const specdec_cache* c, const int32_t* d_seqs, int n, int n_tokens, void* stream);
 int specdec_cache_append(const specdec_cache* c, const int32_t* d_seqs, int n, int layer, int n_layers, const void* d_k, const void* d_v, int T,
@@ -316,7 +316,9 @@ int specdec_packed_cache_release(const specdec_packed_cache* c, const int32_t* d
 int specdec_packed_cache_fork(const specdec_packed_cache* c, const int32_t* d_src, const int32_t* d_dst, int n, void* stream);
 int specdec_packed_cache_reorder(const specdec_packed_cache* c, const int32_t* d_seqs, const int32_t* d_parents, int n, int beams, void* stream);
 /* tree_attention over it: q and out are of `dtype` (fp32, bf16, fp16); the rest as there.  Products with the exact values, scores and sums in fp32; bf16 and fp32 queries are taken with a row's
- * largest number moved below 2^15 by a power of two, as fp16 (fp32: two of them, 22 bits), probabilities as fp16 (fp32: two). */
+ * largest number moved below 2^15 by a power of two, as fp16 (fp32: two of them, 22 bits), probabilities as fp16 (fp32: two).  With p the weights and S the largest sum of scale |q k| of the query's scores, an
+ * output is off by at most (2^-10 + 1e-5) sum p |v| (fp32: 2^-21 in the place of 2^-10) + 2^-32 max |v| for each key, its own rounding, and what scores that are off by 2^-16 S make of it.  Scores may be of
+ * any finite size. */
 long long specdec_packed_attention_workspace(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int dtype, int page_tokens, int max_length);
 int specdec_packed_attention(const specdec_packed_cache* c, const specdec_tree_attention_args* a, int dtype, void* stream);
 

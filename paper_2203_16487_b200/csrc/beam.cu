@@ -154,7 +154,9 @@ __device__ __forceinline__ void stretch_of_row(const BeamArgs& a, int row, int s
     uint32_t bound = w_bound[0];
 #pragma unroll
     for (int w = 1; w < BM_WARPS; ++w) { m = fmaxf(m, w_max[w]); bound = min(bound, w_bound[w]); }
-    if (bound <= NOTHING) {                               // (the same for all threads) a warp has too few, as at a row's end: the n-th largest of all threads' maxima
+    // (the same for all threads) a warp has too few, as at a row's end: the n-th largest of all threads' maxima, each compared with all.  Rows that fill no stretch all go this way, 4 x 12 of 1000 in fp32 29 us
+    // in a graph (of 32768: 10), 128 x 8 of 1000 in bf16 28 (27).
+    if (bound <= NOTHING) {
         const uint32_t mine = key_of(top);
         uint32_t* maxima = reinterpret_cast<uint32_t*>(list);
         maxima[tid] = mine;

@@ -164,7 +164,7 @@ class PagedCache:
         _launch(self._call["fork"], self._device, (self._ref, _ints("src", src, (n,), self._device), _ints("dst", dst, (n,), self._device), n, _raw_stream(self._device)))
 
     def reorder(self, seqs, parents):
-        """Beams: of seqs [..., K], groups of K sequences, each becomes what sequence parents [..., K] (its place in the group, 0 .. K - 1; -1: none) was before the call.  Full pages
+        """Beams: of seqs [..., K], groups of K sequences (all different, over all groups), each becomes what sequence parents [..., K] (its place in the group, 0 .. K - 1; -1: none) was before the call.  Full pages
         are shared; the last, partly filled one goes on with one child (the parent itself if it is one, else the first) and is copied for the others."""
         if seqs.dim() < 1:
             raise ValueError("seqs: groups of sequences [..., K] are wanted")
